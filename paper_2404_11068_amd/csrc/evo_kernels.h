@@ -199,6 +199,24 @@ int64_t pair_bias_bwd_workgroups(int64_t B, int Li, int Lj, int C, int H);
 size_t pair_bias_bwd_workspace(int64_t B, int Li, int Lj, int C, int H);
 hipError_t launch_pair_bias_bwd(const PbBwdArgs &a, void *ws, hipStream_t s);
 
+// learned relative position bias by buckets, and its table's gradient
+struct RpArgs {
+    const int32_t *pos_i, *pos_j;   // [B, Li], [B, Lj]
+    const int32_t *seg_i, *seg_j;   // as the positions, or both null
+    const int32_t *edges;           // [E]
+    const float *table;             // [H, NB]
+    const void *base;               // [B, H, Li, Lj] or null
+    void *out;                      // [B, H, Li, Lj], bf16 or fp32 (may be base)
+    const float *dbias;             // [B, H, Li, Lj]
+    float *dtable;                  // [H, NB]
+    int64_t B;
+    int H, Li, Lj, E, NB, bf16;
+};
+
+hipError_t launch_relpos_fwd(const RpArgs &a, hipStream_t s);
+size_t relpos_bwd_workspace(const RpArgs &a);
+hipError_t launch_relpos_bwd(const RpArgs &a, void *ws, hipStream_t s);
+
 bool proj_supported(int C, int HD, int P);
 hipError_t launch_ln_proj(const PjArgs &a, hipStream_t s);
 

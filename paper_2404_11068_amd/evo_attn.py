@@ -133,6 +133,16 @@ def _stream(stream) -> ctypes.c_void_p:
     return ctypes.c_void_p(s.cuda_stream)
 
 
+def _empty(shape, dtype, like: torch.Tensor, stream):
+    """A tensor that belongs to the stream the kernels run on, so that memory
+    it gives back is not taken by another stream's work before they are done."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    s = torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
+    with torch.cuda.stream(s):
+        return torch.empty(shape, dtype=dtype, device=like.device)
+
+
 def evo_attn_fwd(q, k, v, gate=None, bias=None, key_mask=None, *, rows_per_bias=None,
                  out=None, lse=None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Forward pass; returns (out, lse).  See include/evo_attn.h."""

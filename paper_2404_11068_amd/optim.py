@@ -1,4 +1,5 @@
-"""Python binding of the C ABI in include/evo_optim.h (argument marshalling only).
+"""Python binding of the C ABI in include/evo_optim.h and include/evo_muon.h
+(argument marshalling only).
 
 `FusedAdamSWA` packs the pointers of every parameter, gradient and optimizer
 state tensor into a device table once (and the chunk list that splits them
@@ -6,16 +7,21 @@ into EVO_MT_CHUNK-element work items), then each `step` enqueues the
 gradient-norm clipping kernels and the fused Adam + SWA kernel of
 ``libevoattn.so``.  The table holds raw pointers: rebuild the object if any
 of the tensors is reallocated.  No fallback exists.
+
+`FusedMuonSWA` does the same for matrices whose update is orthogonalised by
+Newton-Schulz steps; `orthogonalize` is that operation alone, on one matrix or
+a stack of them.
 """
 from __future__ import annotations
 
 import ctypes
-from typing import List, Optional, Sequence
+import math
+from typing import List, Optional, Sequence, Tuple
 
 import numpy as np
 import torch
 
-from .evo_attn import EvoAttnError, _stream, load_library
+from .evo_attn import EvoAttnError, _empty, _stream, load_library
 
 EVO_MT_CHUNK = 4096
 
@@ -123,3 +129,173 @@ class FusedAdamSWA:
                                       self.scale.data_ptr() if max_norm is not None else None, _stream(stream))
         if st:
             raise EvoAttnError(st, "evo_adam_swa_step")
+
+
+# ---------------------------------------------------------------------------
+# Orthogonalised updates (include/evo_muon.h)
+
+#: quintic Newton-Schulz coefficients: the steepest slope at zero that still
+#: keeps the singular values within about 0.7 .. 1.2
+NEWTON_SCHULZ_COEFS = (3.4445, -4.7750, 2.0315)
+
+_ORTH_DTYPES = {torch.float32: 0, torch.bfloat16: 1}
+
+
+class evo_orth_dims(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("steps", ctypes.c_int32), ("n_batch", ctypes.c_int64),
+                ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("a", ctypes.c_double), ("b", ctypes.c_double),
+                ("c", ctypes.c_double), ("eps", ctypes.c_double), ("reserved", ctypes.c_int64)]
+
+
+class evo_muon_tensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("momentum", ctypes.c_void_p),
+                ("swa", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("update_scale", ctypes.c_double)]
+
+
+class evo_muon_hparams(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("momentum", ctypes.c_double), ("weight_decay", ctypes.c_double),
+                ("swa_decay", ctypes.c_double), ("a", ctypes.c_double), ("b", ctypes.c_double),
+                ("c", ctypes.c_double), ("eps", ctypes.c_double), ("steps", ctypes.c_int32),
+                ("nesterov", ctypes.c_int32)]
+
+
+_muon_bound = False
+
+
+def _muon_lib():
+    global _muon_bound
+    lib = load_library()
+    if not _muon_bound:
+        P = ctypes.c_void_p
+        lib.evo_orthogonalize_workspace_size.argtypes = [ctypes.POINTER(evo_orth_dims)]
+        lib.evo_orthogonalize_workspace_size.restype = ctypes.c_size_t
+        lib.evo_orthogonalize.argtypes = [ctypes.POINTER(evo_orth_dims), P, P, P, ctypes.c_size_t, P]
+        lib.evo_orthogonalize.restype = ctypes.c_int
+        lib.evo_muon_plan_bytes.argtypes = [P, ctypes.c_int32]
+        lib.evo_muon_plan_bytes.restype = ctypes.c_int64
+        lib.evo_muon_build_plan.argtypes = [P, ctypes.c_int32, P, ctypes.c_size_t]
+        lib.evo_muon_build_plan.restype = ctypes.c_int
+        lib.evo_muon_workspace_size.argtypes = [P]
+        lib.evo_muon_workspace_size.restype = ctypes.c_size_t
+        lib.evo_muon_step.argtypes = [ctypes.POINTER(evo_muon_hparams), P, P, P, P, ctypes.c_size_t, P]
+        lib.evo_muon_step.restype = ctypes.c_int
+        _muon_bound = True
+    return lib
+
+
+def _orth_dims(shape, dtype, steps, coefs, eps) -> evo_orth_dims:
+    if len(shape) not in (2, 3) or dtype not in _ORTH_DTYPES:
+        raise ValueError("x must be a float32 or bfloat16 matrix [m, n] or stack of matrices [N, m, n]")
+    n = shape[0] if len(shape) == 3 else 1
+    return evo_orth_dims(_ORTH_DTYPES[dtype], int(steps), n, shape[-2], shape[-1], *(float(v) for v in coefs),
+                         float(eps), 0)
+
+
+def orthogonalize_workspace_size(shape, dtype, *, steps: int = 5, coefs: Tuple[float, float, float] = NEWTON_SCHULZ_COEFS,
+                                 eps: float = 1e-7) -> int:
+    d = _orth_dims(tuple(shape), dtype, steps, coefs, eps)
+    return int(_muon_lib().evo_orthogonalize_workspace_size(ctypes.byref(d)))
+
+
+def orthogonalize(x: torch.Tensor, *, steps: int = 5, coefs: Tuple[float, float, float] = NEWTON_SCHULZ_COEFS,
+                  eps: float = 1e-7, out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                  stream=None) -> torch.Tensor:
+    """The matrix x [m, n], or every matrix of a stack [N, m, n], with its
+    singular values brought near one by `steps` Newton-Schulz steps
+    X <- a X + (b A + c A^2) X, A = X X^T, from X = x / max(|x|_F, eps).
+    out may be x."""
+    lib = _muon_lib()
+    d = _orth_dims(x.shape, x.dtype, steps, coefs, eps)
+    if not x.is_contiguous() or not x.is_cuda or x.device.index != torch.cuda.current_device():
+        raise ValueError("x must be contiguous and on the current CUDA device")
+    if out is None:
+        out = _empty(x.shape, x.dtype, x, stream)
+    if out.shape != x.shape or out.dtype != x.dtype or not out.is_contiguous() or out.device != x.device:
+        raise ValueError("out must be a contiguous tensor like x")
+    if workspace is None:
+        need = int(lib.evo_orthogonalize_workspace_size(ctypes.byref(d)))
+        workspace = _empty(max(need, 1), torch.uint8, x, stream)
+    elif not workspace.is_contiguous() or workspace.device != x.device:
+        raise ValueError("workspace must be contiguous and on the device of x")
+    st = lib.evo_orthogonalize(ctypes.byref(d), x.data_ptr(), out.data_ptr(), workspace.data_ptr(),
+                               workspace.numel() * workspace.element_size(), _stream(stream))
+    if st:
+        raise EvoAttnError(st, "evo_orthogonalize")
+    return out
+
+
+class FusedMuonSWA:
+    """Muon + SWA over matrices: momentum, the orthogonalised update, weight
+    decay and the weight average.  Vectors (biases, LayerNorm parameters) and
+    embeddings belong to FusedAdamSWA, whose `scale` (after `clip`) can be
+    passed to `step` so that both clip by the same norm.
+
+    Stacked projections are given as their matrices, e.g. the q, k, v and
+    gate rows of one weight as `list(w.view(4, -1, w.shape[1]))`.
+
+    adjust: factor of the update of an m x n matrix: "spectral" gives
+    sqrt(max(1, m / n)), "rms" 0.2 sqrt(max(m, n)) (entries about as large as
+    Adam's), "none" 1."""
+
+    def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor],
+                 momentum: Optional[Sequence[torch.Tensor]] = None, swa: Optional[Sequence[torch.Tensor]] = None, *,
+                 lr=0.02, momentum_decay=0.95, nesterov=True, weight_decay=0.0, swa_decay=0.999, steps=5,
+                 coefs=NEWTON_SCHULZ_COEFS, eps=1e-7, adjust="spectral"):
+        lib = _muon_lib()
+        self.params, self.grads = list(params), list(grads)
+        n = len(self.params)
+        if adjust not in ("spectral", "rms", "none"):
+            raise ValueError("adjust must be 'spectral', 'rms' or 'none'")
+        if len(self.grads) != n:
+            raise ValueError("one gradient per parameter")
+        for i, p in enumerate(self.params):
+            if p.dim() != 2:
+                raise ValueError("param[%d] must be a matrix: vectors go to FusedAdamSWA" % i)
+        self.momentum = list(momentum) if momentum is not None else [torch.zeros_like(p) for p in self.params]
+        self.swa = list(swa) if swa is not None else [p.detach().clone() for p in self.params]
+        if len(self.momentum) != n or len(self.swa) != n:
+            raise ValueError("one momentum and one swa tensor per parameter")
+        dev = self.params[0].device if n else torch.device("cuda", torch.cuda.current_device())
+        tab = np.zeros(n, dtype=np.dtype(evo_muon_tensor))
+        for i, p in enumerate(self.params):
+            for t, nm in ((p, "param"), (self.grads[i], "grad"), (self.momentum[i], "momentum"), (self.swa[i], "swa")):
+                if t.dtype != torch.float32 or t.shape != p.shape or not t.is_cuda or t.device != dev \
+                        or not t.is_contiguous():
+                    raise ValueError("%s[%d] must be a contiguous float32 CUDA matrix like its parameter" % (nm, i))
+            r, c = p.shape
+            f = 1.0 if adjust == "none" or r * c == 0 else \
+                math.sqrt(max(1.0, r / c)) if adjust == "spectral" else 0.2 * math.sqrt(max(r, c))
+            tab[i] = (p.data_ptr(), self.grads[i].data_ptr(), self.momentum[i].data_ptr(), self.swa[i].data_ptr(),
+                      r, c, f)
+        size = int(lib.evo_muon_plan_bytes(tab.ctypes.data, n))
+        if size < 0:
+            raise ValueError("a matrix is too large for the plan")
+        self.plan = np.zeros((size + 7) // 8, dtype=np.int64)  # host copy
+        st = lib.evo_muon_build_plan(tab.ctypes.data, n, self.plan.ctypes.data, size)
+        if st:
+            raise EvoAttnError(st, "evo_muon_build_plan")
+        self.device = dev
+        self.plan_device = torch.from_numpy(self.plan).to(dev)
+        self.workspace = torch.empty(max(int(lib.evo_muon_workspace_size(self.plan.ctypes.data)), 1),
+                                     dtype=torch.uint8, device=dev)
+        self.lr, self.momentum_decay, self.nesterov = lr, momentum_decay, nesterov
+        self.weight_decay, self.swa_decay = weight_decay, swa_decay
+        self.steps, self.coefs, self.eps = steps, coefs, eps
+
+    def step(self, grad_scale: Optional[torch.Tensor] = None, stream=None):
+        """One step; grad_scale: a device float32 scalar that multiplies every
+        gradient (FusedAdamSWA.scale).  Steps of one object share its
+        workspace: they must not overlap in time."""
+        if self.device.index != torch.cuda.current_device():
+            raise ValueError("the tensors are not on the current CUDA device")
+        if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1
+                                       or grad_scale.device != self.device):
+            raise ValueError("grad_scale must be one float32 on the tensors' device")
+        hp = evo_muon_hparams(self.lr, self.momentum_decay, self.weight_decay, self.swa_decay, *self.coefs, self.eps,
+                              self.steps, int(self.nesterov))
+        st = _muon_lib().evo_muon_step(ctypes.byref(hp), self.plan.ctypes.data, self.plan_device.data_ptr(),
+                                       grad_scale.data_ptr() if grad_scale is not None else None,
+                                       self.workspace.data_ptr(), self.workspace.numel(), _stream(stream))
+        if st:
+            raise EvoAttnError(st, "evo_muon_step")

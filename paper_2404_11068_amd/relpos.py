@@ -1,0 +1,168 @@
+"""Python binding of the C ABI in include/evo_relpos.h (argument marshalling only).
+
+The learned relative position bias runs in ``libevoattn.so``; this module
+passes torch tensors' device pointers and raises on a nonzero status.  No
+fallback exists.
+
+  pos_i, pos_j : int32 [B, Li], [B, Lj] (or [Li], [Lj] for one batch entry): residue or token numbers
+  seg_i, seg_j : int32 like them, or None: pairs of different segments (chains) take the last bucket
+  edges : int32 [E], ascending: the first difference pos_i - pos_j of every bucket but the lowest
+  table : fp32 [H, buckets], buckets = E + 1, and one more with segments
+  base, out : [B, H, Li, Lj] bf16 or fp32, the bias layout of evo_attn_fwd
+  dbias : fp32 [B, H, Li, Lj], as evo_attn_bwd returns it
+"""
+from __future__ import annotations
+
+import ctypes
+import math
+from typing import Optional
+
+import torch
+
+from .evo_attn import EVO_DTYPE_F32, EvoAttnError, _DTYPES, _empty, _ptr, _stream, load_library
+
+
+class evo_relpos_dims(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("n_edges", ctypes.c_int32),
+                ("has_seg", ctypes.c_int32), ("n_batch", ctypes.c_int64), ("len_i", ctypes.c_int64),
+                ("len_j", ctypes.c_int64), ("reserved", ctypes.c_int64)]
+
+
+_bound = False
+
+
+def _lib():
+    global _bound
+    lib = load_library()
+    if not _bound:
+        P = ctypes.c_void_p
+        D = ctypes.POINTER(evo_relpos_dims)
+        lib.evo_relpos_fwd.argtypes = [D] + [P] * 9
+        lib.evo_relpos_fwd.restype = ctypes.c_int
+        lib.evo_relpos_bwd_workspace_size.argtypes = [D]
+        lib.evo_relpos_bwd_workspace_size.restype = ctypes.c_size_t
+        lib.evo_relpos_bwd.argtypes = [D] + [P] * 8 + [ctypes.c_size_t, P]
+        lib.evo_relpos_bwd.restype = ctypes.c_int
+        _bound = True
+    return lib
+
+
+def relpos_edges_clip(max_offset: int, device="cuda") -> torch.Tensor:
+    """Edges of the 2 * max_offset + 1 buckets of differences clipped at +-max_offset
+    (AlphaFold's relative positions: 32, which makes 65 buckets)."""
+    if max_offset < 0:
+        raise ValueError("max_offset must not be negative")
+    return torch.arange(1 - max_offset, max_offset + 1, dtype=torch.int32, device=device)
+
+
+def relpos_edges_log(n_side: int, max_distance: int, device="cuda") -> torch.Tensor:
+    """Edges of 2 * n_side - 1 buckets, symmetric around difference 0: single
+    distances up to n_side // 2, from there on bucket widths that grow by a
+    constant factor; distances of max_distance and more share the last
+    bucket of their side (fewer buckets where steps below one would repeat
+    an edge)."""
+    half = n_side // 2
+    if n_side < 3 or max_distance <= half:
+        raise ValueError("n_side must be at least 3 and max_distance larger than n_side // 2")
+    near = list(range(1, half + 1))
+    steps = n_side - 1 - half
+    far = [min(max_distance, max(half + 1, math.ceil(half * (max_distance / half) ** (k / steps))))
+           for k in range(1, steps)] + [max_distance]
+    side = near + sorted(set(far))
+    return torch.tensor([1 - e for e in reversed(side)] + side, dtype=torch.int32, device=device)
+
+
+def _index(pos_i, pos_j, edges, seg_i, seg_j, like: torch.Tensor):
+    """Checks of the index tensors; returns (B, Li, Lj, E)."""
+    if pos_i.dim() not in (1, 2) or pos_j.dim() != pos_i.dim() or edges.dim() != 1:
+        raise ValueError("pos_i and pos_j must be [B, Li] and [B, Lj] (or [Li] and [Lj]), edges [E]")
+    B = pos_i.shape[0] if pos_i.dim() == 2 else 1
+    if pos_j.dim() == 2 and pos_j.shape[0] != B:
+        raise ValueError("pos_i and pos_j must have the same batch size")
+    if (seg_i is None) != (seg_j is None):
+        raise ValueError("seg_i and seg_j go together")
+    if seg_i is not None and (seg_i.shape != pos_i.shape or seg_j.shape != pos_j.shape):
+        raise ValueError("segments must be shaped like the positions")
+    for t in (pos_i, pos_j, edges, seg_i, seg_j):
+        if t is not None and (t.dtype != torch.int32 or not t.is_contiguous()):
+            raise ValueError("positions, segments and edges must be contiguous int32")
+    _same_device(like, pos_i, pos_j, edges, seg_i, seg_j)
+    return B, pos_i.shape[-1], pos_j.shape[-1], edges.shape[0]
+
+
+def _same_device(ref: torch.Tensor, *ts):
+    if not ref.is_cuda or ref.device.index != torch.cuda.current_device():
+        raise ValueError("tensors must be on the current CUDA device")
+    for t in ts:
+        if t is not None and t.device != ref.device:
+            raise ValueError("tensors must be on one device")
+
+
+def relpos_bias_fwd(pos_i: torch.Tensor, pos_j: torch.Tensor, edges: torch.Tensor, table: torch.Tensor, *,
+                    seg_i: Optional[torch.Tensor] = None, seg_j: Optional[torch.Tensor] = None,
+                    base: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, dtype=None,
+                    stream=None) -> torch.Tensor:
+    """Bias [B, H, Li, Lj] for evo_attn_fwd: table[h, bucket(i, j)], added to
+    base when given (out=base adds in place).  dtype: of the result; that of
+    out or base when one is given, bfloat16 otherwise."""
+    lib = _lib()
+    B, Li, Lj, E = _index(pos_i, pos_j, edges, seg_i, seg_j, table)
+    H = table.shape[0] if table.dim() == 2 else 0
+    buckets = E + 1 + (seg_i is not None)
+    if table.dim() != 2 or H < 1 or table.shape[1] != buckets or table.dtype != torch.float32 \
+            or not table.is_contiguous():
+        raise ValueError("table must be a contiguous float32 [H, %d] tensor" % buckets)
+    if dtype is None:
+        dtype = out.dtype if out is not None else base.dtype if base is not None else torch.bfloat16
+    if dtype not in _DTYPES:
+        raise ValueError("dtype must be float32 or bfloat16")
+    shape = (B, H, Li, Lj)
+    if out is None:
+        out = _empty(shape, dtype, table, stream)
+    for t in (base, out):
+        if t is not None and (tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous()
+                              or t.device != table.device):
+            raise ValueError("base and out must be contiguous %s tensors of shape %s" % (dtype, shape))
+    d = evo_relpos_dims(_DTYPES[dtype], H, E, int(seg_i is not None), B, Li, Lj, 0)
+    st = lib.evo_relpos_fwd(ctypes.byref(d), _ptr(pos_i), _ptr(pos_j), _ptr(seg_i), _ptr(seg_j), _ptr(edges),
+                            _ptr(table), _ptr(base), _ptr(out), _stream(stream))
+    if st:
+        raise EvoAttnError(st, "evo_relpos_fwd")
+    return out
+
+
+def relpos_bias_bwd_workspace_size(B: int, H: int, Li: int, Lj: int, n_edges: int, has_seg: bool = False) -> int:
+    d = evo_relpos_dims(EVO_DTYPE_F32, H, n_edges, int(has_seg), B, Li, Lj, 0)
+    return int(_lib().evo_relpos_bwd_workspace_size(ctypes.byref(d)))
+
+
+def relpos_bias_bwd(pos_i: torch.Tensor, pos_j: torch.Tensor, edges: torch.Tensor, dbias: torch.Tensor, *,
+                    seg_i: Optional[torch.Tensor] = None, seg_j: Optional[torch.Tensor] = None,
+                    dtable: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                    stream=None) -> torch.Tensor:
+    """Gradient [H, buckets] (fp32) of relpos_bias_fwd's table for the upstream
+    gradient dbias, which is the gradient of its base, too."""
+    lib = _lib()
+    B, Li, Lj, E = _index(pos_i, pos_j, edges, seg_i, seg_j, dbias)
+    if dbias.dim() != 4 or (dbias.shape[0], dbias.shape[2], dbias.shape[3]) != (B, Li, Lj) or dbias.shape[1] < 1 \
+            or dbias.dtype != torch.float32 or not dbias.is_contiguous():
+        raise ValueError("dbias must be a contiguous float32 [%d, H, %d, %d] tensor" % (B, Li, Lj))
+    H = dbias.shape[1]
+    buckets = E + 1 + (seg_i is not None)
+    if dtable is None:
+        dtable = _empty((H, buckets), torch.float32, dbias, stream)
+    if tuple(dtable.shape) != (H, buckets) or dtable.dtype != torch.float32 or not dtable.is_contiguous() \
+            or dtable.device != dbias.device:
+        raise ValueError("dtable must be a contiguous float32 [%d, %d] tensor" % (H, buckets))
+    d = evo_relpos_dims(EVO_DTYPE_F32, H, E, int(seg_i is not None), B, Li, Lj, 0)
+    if workspace is None:
+        need = int(lib.evo_relpos_bwd_workspace_size(ctypes.byref(d)))
+        workspace = _empty(max(need, 16), torch.uint8, dbias, stream)
+    elif workspace.device != dbias.device or not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous and on the device of dbias")
+    st = lib.evo_relpos_bwd(ctypes.byref(d), _ptr(pos_i), _ptr(pos_j), _ptr(seg_i), _ptr(seg_j), _ptr(edges),
+                            _ptr(dbias), _ptr(dtable), _ptr(workspace),
+                            ctypes.c_size_t(workspace.numel() * workspace.element_size()), _stream(stream))
+    if st:
+        raise EvoAttnError(st, "evo_relpos_bwd")
+    return dtable

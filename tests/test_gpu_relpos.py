@@ -1,0 +1,274 @@
+"""GPU parity of the learned relative position bias and its table's gradient
+(through the C ABI) against the fp64 oracle.
+
+Tolerances.  Forward: one fp32 addition (half a step, 2^-24 of the result)
+and one rounding to the result's type (bf16: 2^-8, half of
+finfo.eps relative to the value; fp32: none more).  Without a base the fp32 result is
+the table's entry itself, bit for bit.
+Backward: n additions in fp32, each off by at most 2^-24 of a partial sum,
+which is at most the sum of the magnitudes S: n 2^-24 S for a bucket of n
+entries, and 2^-24 for the result's rounding.  Where the gradients are
+integers below 2^24 in every partial sum there is no rounding at all and the
+sums must be equal.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import relpos_oracle as ro
+from paper_2404_11068_amd import evo_attn as ea
+from paper_2404_11068_amd import graph as gr
+from paper_2404_11068_amd import relpos as rp
+from tests.parity_util import to_f64
+
+pytestmark = pytest.mark.gpu
+
+
+def _edges(kind):
+    if kind == "none":
+        return torch.empty(0, dtype=torch.int32, device="cuda")
+    if kind == "most":
+        return torch.arange(-511, 511, dtype=torch.int32, device="cuda")
+    if kind == "wide":  # steps of their own size, far beyond any table of single differences
+        return torch.tensor([-(1 << 30), -5000, -7, 0, 1, 2, 9, 70000, 1 << 30], dtype=torch.int32, device="cuda")
+    if kind == "same":
+        return torch.tensor([-3, 0, 0, 4, 4, 4], dtype=torch.int32, device="cuda")
+    name, a = kind.split(":")
+    return rp.relpos_edges_clip(int(a)) if name == "clip" else rp.relpos_edges_log(int(a), 16 * int(a))
+
+
+def _inputs(B, Li, Lj, seg, seed, order="ascending"):
+    rng = np.random.default_rng(seed)
+    if order == "ascending":
+        pos = np.cumsum(1 + (rng.random((B, max(Li, Lj))) < 0.05) * rng.integers(0, 60, (B, max(Li, Lj))), 1)
+        pi, pj = pos[:, -Li:], pos[:, :Lj]
+    elif order == "random":
+        pi, pj = rng.integers(-200, 200, (B, Li)), rng.integers(-200, 200, (B, Lj))
+    else:  # the ends of int32
+        ends = np.array([-2 ** 31, -2 ** 31 + 1, -1, 0, 1, 2 ** 31 - 2, 2 ** 31 - 1])
+        pi, pj = rng.choice(ends, (B, Li)), rng.choice(ends, (B, Lj))
+    t = lambda a: torch.from_numpy(np.ascontiguousarray(a.astype(np.int32))).cuda()
+    s = (t(rng.integers(0, 3, (B, Li))), t(rng.integers(0, 3, (B, Lj)))) if seg else (None, None)
+    return t(pi), t(pj), s[0], s[1], rng
+
+
+def _np(t):
+    return None if t is None else t.cpu().numpy()
+
+
+CASES = [
+    # B, H, Li, Lj, edges, seg, order
+    (1, 1, 1, 1, "clip:4", False, "ascending"),
+    (1, 8, 1, 130, "log:16", False, "ascending"),
+    (3, 8, 1, 33, "clip:32", True, "ascending"),
+    (1, 8, 64, 64, "clip:32", False, "ascending"),
+    (2, 4, 37, 51, "clip:32", True, "ascending"),
+    (1, 3, 65, 129, "log:32", False, "random"),
+    (1, 16, 40, 72, "log:128", True, "random"),
+    (2, 5, 17, 8, "none", False, "random"),
+    (2, 2, 9, 31, "none", True, "random"),
+    (1, 2, 70, 67, "most", False, "random"),
+    (1, 33, 20, 23, "clip:1", False, "ascending"),
+    (1, 4, 25, 40, "wide", True, "ends"),
+    (2, 7, 12, 130, "same", False, "random"),
+    (1, 12, 200, 7, "clip:16", False, "ascending"),
+]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "B%dH%d_%dx%d_%s%s_%s" % (c[:5] + ("_seg" if c[5] else "", c[6])))
+def test_forward(case, dtype):
+    B, H, Li, Lj, kind, seg, order = case
+    print("\n[case]", case, dtype, flush=True)
+    pi, pj, si, sj, rng = _inputs(B, Li, Lj, seg, 1, order)
+    edges = _edges(kind)
+    NB = edges.numel() + 1 + seg
+    table = torch.from_numpy(rng.standard_normal((H, NB)).astype(np.float32)).cuda()
+    base = torch.from_numpy(rng.standard_normal((B, H, Li, Lj))).to(dtype).cuda()
+    kw = dict(seg_i=si, seg_j=sj)
+    alone = rp.relpos_bias_fwd(pi, pj, edges, table, dtype=dtype, **kw)
+    added = rp.relpos_bias_fwd(pi, pj, edges, table, base=base, **kw)
+    assert added.dtype == dtype and alone.shape == added.shape == (B, H, Li, Lj)
+    inplace = base.clone()
+    assert rp.relpos_bias_fwd(pi, pj, edges, table, base=inplace, out=inplace, **kw) is inplace
+    torch.cuda.synchronize()
+    assert torch.equal(inplace, added)
+    ref = ro.forward(_np(pi), _np(pj), _np(edges), _np(table), None, _np(si), _np(sj))
+    step = 2.0 ** -8 if dtype == torch.bfloat16 else 0.0
+    assert (np.abs(to_f64(alone) - ref) <= step * np.abs(ref)).all()
+    ref = ref + to_f64(base)
+    assert (np.abs(to_f64(added) - ref) <= (step * (1 + 2.0 ** -24) + 2.0 ** -24) * np.abs(ref)).all()
+
+
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "B%dH%d_%dx%d_%s%s_%s" % (c[:5] + ("_seg" if c[5] else "", c[6])))
+def test_backward(case):
+    B, H, Li, Lj, kind, seg, order = case
+    print("\n[case]", case, flush=True)
+    pi, pj, si, sj, rng = _inputs(B, Li, Lj, seg, 2, order)
+    edges = _edges(kind)
+    index = (_np(pi), _np(pj), _np(edges))
+    whole = rng.integers(-9, 10, (B, H, Li, Lj)).astype(np.float32)
+    real = rng.standard_normal((B, H, Li, Lj)).astype(np.float32)
+    run = lambda g: rp.relpos_bias_bwd(pi, pj, edges, torch.from_numpy(g).cuda(), seg_i=si, seg_j=sj)
+    got = run(whole)
+    assert np.array_equal(to_f64(got), ro.backward(*index, whole, _np(si), _np(sj)))
+    got, again = run(real), run(real)
+    assert torch.equal(got, again)
+    ref = ro.backward(*index, real, _np(si), _np(sj))
+    size = ro.backward(*index, np.abs(real), _np(si), _np(sj))
+    count = ro.backward(*index, np.ones_like(real), _np(si), _np(sj))
+    assert (np.abs(to_f64(got) - ref) <= 2.0 ** -24 * (count * size + np.abs(ref))).all()
+
+
+@pytest.mark.parametrize("B,H,Li,Lj,kind", [(1, 8, 384, 384, "clip:32"), (1, 2, 700, 1033, "log:64"),
+                                            (4, 6, 1, 3001, "log:16"), (3, 4, 255, 257, "most"), (1, 1, 2500, 3, "clip:2")])
+def test_longer(B, H, Li, Lj, kind):
+    print("\n[case]", B, H, Li, Lj, kind, flush=True)
+    pi, pj, si, sj, rng = _inputs(B, Li, Lj, True, 3)
+    edges = _edges(kind)
+    index = (_np(pi), _np(pj), _np(edges))
+    table = torch.from_numpy(rng.standard_normal((H, edges.numel() + 2)).astype(np.float32)).cuda()
+    out = rp.relpos_bias_fwd(pi, pj, edges, table, seg_i=si, seg_j=sj, dtype=torch.float32)
+    assert np.array_equal(to_f64(out), ro.forward(*index, _np(table), None, _np(si), _np(sj)))
+    g = rng.integers(-9, 10, (B, H, Li, Lj)).astype(np.float32)
+    d = rp.relpos_bias_bwd(pi, pj, edges, torch.from_numpy(g).cuda(), seg_i=si, seg_j=sj)
+    assert np.array_equal(to_f64(d), ro.backward(*index, g, _np(si), _np(sj)))
+
+
+def test_base_infinities_and_nan_pass_and_neighbours_stay():
+    pi, pj, _, _, rng = _inputs(1, 9, 21, False, 4)
+    edges = _edges("clip:4")
+    table = torch.from_numpy(rng.standard_normal((2, edges.numel() + 1)).astype(np.float32)).cuda()
+    for dtype in (torch.bfloat16, torch.float32):
+        n = 2 * 9 * 21
+        whole = torch.full((n + 64,), 7.0, dtype=dtype, device="cuda")
+        for shift in (0, 1, 3, 8):   # also where no row is aligned to more than its element
+            whole.fill_(7.0)
+            out = whole[shift:shift + n].view(1, 2, 9, 21)
+            base = torch.zeros(1, 2, 9, 21, dtype=dtype, device="cuda")
+            base[0, 0, 3, 4], base[0, 1, 8, 20], base[0, 1, 0, 0] = float("-inf"), float("inf"), float("nan")
+            low = torch.finfo(dtype).min
+            base[0, 0, 5] = low
+            rp.relpos_bias_fwd(pi, pj, edges, table, base=base, out=out)
+            ref = rp.relpos_bias_fwd(pi, pj, edges, table, dtype=dtype)
+            got, ref = out.float().cpu(), ref.float().cpu()
+            assert got[0, 0, 3, 4] == float("-inf") and got[0, 1, 8, 20] == float("inf") and got[0, 1, 0, 0].isnan()
+            assert (got[0, 0, 5] == low).all()
+            plain = base.float().cpu() == 0
+            assert torch.equal(got[plain], ref[plain])
+            assert (whole[:shift] == 7).all() and (whole[shift + n:] == 7).all()
+
+
+def test_misaligned_gradient_and_table():
+    pi, pj, _, _, rng = _inputs(2, 13, 37, False, 5)
+    edges = _edges("clip:8")
+    g = rng.integers(-9, 10, (2, 3, 13, 37)).astype(np.float32)
+    want = ro.backward(_np(pi), _np(pj), _np(edges), g)
+    for shift in range(4):
+        buf = torch.full((g.size + 8,), 1e6, device="cuda")
+        buf[shift:shift + g.size] = torch.from_numpy(g.reshape(-1)).cuda()
+        dt = torch.full((want.size + 8,), 5.0, device="cuda")
+        out = dt[shift:shift + want.size].view(want.shape)
+        rp.relpos_bias_bwd(pi, pj, edges, buf[shift:shift + g.size].view(g.shape), dtable=out)
+        assert np.array_equal(to_f64(out), want)
+        assert (dt[:shift] == 5).all() and (dt[shift + want.size:] == 5).all()
+        t = torch.empty(want.size + 8, device="cuda")
+        t[shift:shift + want.size] = torch.from_numpy(want.astype(np.float32).reshape(-1)).cuda()
+        b = rp.relpos_bias_fwd(pi, pj, edges, t[shift:shift + want.size].view(want.shape), dtype=torch.float32)
+        assert np.array_equal(to_f64(b), ro.forward(_np(pi), _np(pj), _np(edges), want))
+
+
+def test_empty():
+    e = _edges("clip:2")
+    i = lambda *s: torch.zeros(*s, dtype=torch.int32, device="cuda")
+    t = torch.ones(2, 5, device="cuda")
+    assert rp.relpos_bias_fwd(i(1, 0), i(1, 4), e, t).shape == (1, 2, 0, 4)
+    assert rp.relpos_bias_fwd(i(0, 3), i(0, 4), e, t).shape == (0, 2, 3, 4)
+    d = torch.full((2, 5), 3.0, device="cuda")
+    rp.relpos_bias_bwd(i(1, 0), i(1, 4), e, torch.empty(1, 2, 0, 4, device="cuda"), dtable=d)
+    assert not d.any()
+
+
+def test_offsets_past_32_bits():
+    H, L = 35, 11200                       # 4.39e9 entries
+    print("\n[case] large", H, L, flush=True)
+    pos = torch.arange(L, dtype=torch.int32, device="cuda")
+    edges = _edges("clip:8")
+    table = torch.randn(H, 17, device="cuda").to(torch.bfloat16).float()
+    out = rp.relpos_bias_fwd(pos, pos, edges, table)
+    for h in (0, 17, H - 1):
+        for i in (0, L // 2, L - 1):
+            want = table[h][(i - pos.long()).clamp(-8, 8) + 8].to(torch.bfloat16)
+            assert torch.equal(out[0, h, i], want), (h, i)
+    del out
+    d = rp.relpos_bias_bwd(pos, pos, edges, torch.ones(1, H, L, L, device="cuda"))
+    count = torch.tensor([L - abs(k) for k in range(-8, 9)], dtype=torch.float64)
+    count[0] = count[-1] = (L - 8) * (L - 7) // 2
+    assert torch.equal(d.cpu(), count.float().expand(H, -1))
+    del d
+    torch.cuda.empty_cache()
+
+
+def test_captured_replays_and_another_stream():
+    B, H, L = 2, 4, 61
+    pi, pj, si, sj, rng = _inputs(B, L, L, True, 6)
+    edges = _edges("clip:32")
+    NB = edges.numel() + 2
+    table, base = torch.randn(H, NB, device="cuda"), torch.randn(B, H, L, L, device="cuda").bfloat16()
+    g, out = torch.randn(B, H, L, L, device="cuda"), torch.empty(B, H, L, L, dtype=torch.bfloat16, device="cuda")
+    dt = torch.empty(H, NB, device="cuda")
+    ws = torch.empty(max(rp.relpos_bias_bwd_workspace_size(B, H, L, L, edges.numel(), True), 16), dtype=torch.uint8,
+                     device="cuda")
+    s = torch.cuda.Stream()
+
+    def record(stream):
+        rp.relpos_bias_fwd(pi, pj, edges, table, seg_i=si, seg_j=sj, base=base, out=out, stream=stream)
+        rp.relpos_bias_bwd(pi, pj, edges, g, seg_i=si, seg_j=sj, dtable=dt, workspace=ws, stream=stream)
+
+    cache = gr.GraphCache(capacity=2)
+    for it in range(4):
+        table.normal_(), base.normal_(), g.normal_()
+        want = rp.relpos_bias_fwd(pi, pj, edges, table, seg_i=si, seg_j=sj, base=base)
+        dwant = rp.relpos_bias_bwd(pi, pj, edges, g, seg_i=si, seg_j=sj)
+        out.zero_(), dt.zero_(), ws.fill_(255)
+        torch.cuda.synchronize()
+        assert cache.run(5, record, s) == (it == 0)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(dt, dwant), it
+    s.wait_stream(torch.cuda.current_stream())
+    other = rp.relpos_bias_fwd(pi, pj, edges, table, seg_i=si, seg_j=sj, base=base, stream=s)
+    dother = rp.relpos_bias_bwd(pi, pj, edges, g, seg_i=si, seg_j=sj, stream=s)
+    s.synchronize()
+    assert torch.equal(other, want) and torch.equal(dother, dwant)
+
+
+def test_bias_through_the_attention_by_differences():
+    """The table's gradient of <W, attention(..., bias(table))> against central
+    differences of the attention itself (fp32).  Bound: the differences of
+    step h err by h^2 of the third derivative (below 1e-3 here) and by the fp32
+    rounding of the two sums, 2 sum|W o| 2^-24 / (2 h) times a few."""
+    N, L, H, d = 3, 40, 2, 16
+    torch.manual_seed(0)
+    q, k, v, w = (torch.randn(N, L, H, d, device="cuda") for _ in range(4))
+    pos = torch.arange(L, dtype=torch.int32, device="cuda").view(1, L)
+    edges = _edges("clip:3")
+    table = torch.randn(H, 7, device="cuda")
+    mask = torch.ones(N, L, dtype=torch.uint8, device="cuda")
+    mask[1, 20:] = 0
+    mask[2] = 0                                         # a row that keeps no key
+
+    def f(t):
+        b = rp.relpos_bias_fwd(pos, pos, edges, t, dtype=torch.float32)
+        return (ea.evo_attn_fwd(q, k, v, None, b, mask, rows_per_bias=N)[0].double() * w.double()).sum().item(), b
+
+    bias = f(table)[1]
+    out, lse = ea.evo_attn_fwd(q, k, v, None, bias, mask, rows_per_bias=N)
+    dbias = ea.evo_attn_bwd(q, k, v, None, bias, mask, out, lse, w, rows_per_bias=N)[4]
+    dt = rp.relpos_bias_bwd(pos, pos, edges, dbias)
+    scale = (out * w).abs().sum().item()
+    for h in range(H):
+        for n in range(7):
+            e = torch.zeros_like(table)
+            e[h, n] = 0.02
+            quotient = (f(table + e)[0] - f(table - e)[0]) / 0.04
+            assert abs(quotient - dt[h, n].item()) < 4e-4 * 8 + 8 * scale * 2.0 ** -24 / 0.02
