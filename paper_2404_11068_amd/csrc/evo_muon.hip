@@ -1,22 +1,52 @@
 // evo_muon.hip -- Newton-Schulz orthogonalisation and the Muon step, gfx950.
+//
+//   X = x / max(|x|_F, eps);  steps times:  A = X X^T,  P = a I + b A + c A A,  X = P X
+//
+// Precision.  A direction that X hardly has grows by up to a^steps = 485, and so do
+// the roundings of the iterate.  fp32 matrices therefore keep every iterate
+// as a pair of fp16 (value = hi + lo, 22 bits) and form each product as hi hi + hi lo + lo hi
+// on the fp16 matrix instructions with fp32 accumulation: the error of fp32
+// arithmetic (1e-6 .. 1e-5 of the result over five steps, low-rank inputs
+// too) at a third of the fp16 rate, which is five times the fp32 matrix rate.
+// bf16 matrices take one fp16 plane: an iterate rounded to 2^-11 costs 2e-3 of
+// the result, about its own rounding to bf16 (with bf16 iterates it would be
+// 1e-2, and all of it for low-rank inputs).  Iterates are stored times 2^10:
+// their entries stay below 8 (coefficients that could take them further
+// are refused), and those near 1 / sqrt(m n) stay clear of fp16's subnormals.
+//
+// Layout.  Iterates lie in the workspace as units of 32 x 32 entries, 2 KB per
+// plane, zero beyond the matrix.  Inside a unit 16-byte chunks (8 entries of a
+// row) are ordered so that both ways of reading it touch every LDS bank once:
+// an operand fragment by rows (ds_read_b128, lane = row) and one by columns
+// (ds_read_b64_tr_b16, four rows of four chunks at a time).  A unit goes from
+// memory to LDS as it is, so one copy of X serves X X^T (rows) and P X (columns).
 #include "evo_frag.h"
 #include "evo_ns.h"
 
 namespace evo {
 namespace {
 
-constexpr int kT = kNsTile;
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 
-struct View {  // a matrix of this call and its buffers
+constexpr float kScale = 1024.0f;                  // iterates are stored times this
+constexpr float kUnscale = 1.0f / (1024.0f * 1024.0f);  // of a product of two
+constexpr int kPlane = 2048;                       // bytes of a unit's plane
+
+__host__ __device__ inline int units(int n) { return (n + 31) / 32; }
+
+// ---- matrices and their buffers
+
+struct View {
     NsMat m;
-    int r, c;
-    bool tr;            // the iterate is the transposed matrix
-    float *x0, *x1, *A, *P;
+    int r, c;         // the iterate's rows and columns, r <= c
+    int R, C;         // in units
+    bool tr;          // the iterate is the transposed matrix
+    char *x0, *x1, *A, *P;
 };
 
-__host__ __device__ int64_t up(int64_t n) { return (n + 63) & ~int64_t(63); }
-
-__device__ View view_of(const NsWork &w, int k) {
+template <int PL>
+__device__ __forceinline__ View view_of(const NsWork &w, int k) {
     View v;
     if (w.mats) {
         v.m = w.mats[k];
@@ -29,191 +59,503 @@ __device__ View view_of(const NsWork &w, int k) {
     v.tr = v.m.rows > v.m.cols;
     v.r = v.tr ? v.m.cols : v.m.rows;
     v.c = v.tr ? v.m.rows : v.m.cols;
-    v.x0 = (float *)(w.ws + v.m.off);
-    v.x1 = v.x0 + up((int64_t)v.r * v.c);
-    v.A = v.x1 + up((int64_t)v.r * v.c);
-    v.P = v.A + up((int64_t)v.r * v.r);
+    v.R = units(v.r);
+    v.C = units(v.c);
+    const int64_t unit = PL * kPlane, nx = (int64_t)v.R * v.C * unit;
+    v.x0 = w.ws + v.m.off;
+    v.x1 = v.x0 + nx;
+    v.A = v.x1 + nx;
+    v.P = v.A + (int64_t)v.R * v.R * unit;
     return v;
 }
 
-__device__ NsTile tile_of(const NsWork &w, int k) {
+// Workgroups go round the eight XCDs, each with an L2 of its own.  A stack of eight matrices
+// or more puts matrix k on XCD k % 8, so that the tiles of a matrix share an L2;
+// the tables of a plan are ordered likewise on the host.  GRAM: the upper triangle of tiles
+template <bool GRAM>
+__device__ __forceinline__ NsTile tile_of(const NsWork &w, int k) {
     if (w.tiles) return w.tiles[k];
-    const int per = w.nti * w.ntj, e = k % per;
-    return NsTile{k / per, e / w.ntj, e % w.ntj};
-}
-
-__device__ int64_t place(const View &v, int i, int j) {  // of iterate element (i, j) in the matrix
-    return v.tr ? (int64_t)j * v.m.cols + i : (int64_t)i * v.m.cols + j;
-}
-
-template <bool MUON, bool BF16>
-__device__ float value_in(const View &v, const NsParams &p, float gs, int64_t at) {
-    if constexpr (MUON) {
-        const float g = ((const float *)v.m.in)[at] * gs;
-        return fmaf(p.u_m, v.m.mom[at], p.u_g * g);
-    } else if constexpr (BF16) {
-        return bf2f(((const uint16_t *)v.m.in)[at]);
+    const int per = GRAM ? w.nti * (w.nti + 1) / 2 : w.nti * w.ntj;
+    int e, mat;
+    if (w.n_mats >= 8) {
+        const int q = k >> 3;
+        mat = (k & 7) + 8 * (q / per);
+        e = q % per;
+        if (mat >= w.n_mats) mat = -1;
     } else {
-        return ((const float *)v.m.in)[at];
+        mat = k / per;
+        e = k % per;
+    }
+    if (!GRAM) return NsTile{mat, e / w.ntj, e % w.ntj};
+    int ti = 0;  // rows of nti, nti - 1, ... tiles
+    while (e >= w.nti - ti) {
+        e -= w.nti - ti;
+        ++ti;
+    }
+    return NsTile{mat, ti, ti + e};
+}
+
+// ---- units
+
+// byte of chunk `half` (k 8 half .. + 7 of 16-entry block blk) of a row inside a plane
+__device__ __forceinline__ int chunk(int row, int half, int blk) {
+    const int g = row >> 2;
+    return g * 256 + (((row & 3) | ((half ^ (g & 1)) << 2) | ((blk ^ ((g >> 1) & 1)) << 3)) << 4);
+}
+
+// operand fragment of 16 contraction entries from a unit's plane in LDS: lane
+// = row, entries 16 s + 8 (lane / 32) ..
+__device__ __forceinline__ half8 frag_rows(const char *plane, int lane, int s) {
+    return *(const half8 *)(plane + chunk(lane & 31, lane >> 5, s));
+}
+// the same with lane = column of the unit, contraction over its rows
+__device__ __forceinline__ half8 frag_cols(const char *plane, int lane, int s) {
+    const int G = lane >> 4, i = lane & 15;
+    const int row = 16 * s + 8 * (G >> 1) + (i >> 2);
+    const int half = (i >> 1) & 1, blk = G & 1, sub = (i & 1) * 8;
+    typedef __attribute__((address_space(3))) short4tr lds4;
+    const short4tr a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(plane + chunk(row, half, blk) + sub));
+    const short4tr b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(plane + chunk(row + 4, half, blk) + sub));
+    return __builtin_bit_cast(half8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// a value (already scaled) as one fp16, or as two that sum up to it within 22 bits
+template <int PL>
+__device__ __forceinline__ void split4(const float (&v)[4], half4 (&p)[PL]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const _Float16 hi = (_Float16)v[e];
+        p[0][e] = hi;
+        if constexpr (PL == 2) p[1][e] = (_Float16)(v[e] - (float)hi);
     }
 }
 
-// momentum, and the sum of squares of each tile
-template <bool MUON, bool BF16>
+template <int PL> struct Frag { half8 p[PL]; };
+
+template <int PL>
+__device__ __forceinline__ void mma(f32x16 &acc, const Frag<PL> &a, const Frag<PL> &b) {
+    if constexpr (PL == 2) {
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a.p[1], b.p[0], acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a.p[0], b.p[1], acc, 0, 0, 0);
+    }
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a.p[0], b.p[0], acc, 0, 0, 0);
+}
+
+// ---- norm and scaling: a thread owns 4 x 4 entries of a 64 x 64 tile
+
+// four consecutive entries of a memory row, zeros past its end
+__device__ __forceinline__ void load4(float (&v)[4], const float *p, int left) {
+    if (left >= 4) {
+        __builtin_memcpy(v, p, 16);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = e < left ? p[e] : 0.0f;
+    }
+}
+__device__ __forceinline__ void load4(float (&v)[4], const uint16_t *p, int left) {
+    uint16_t u[4] = {0, 0, 0, 0};
+    if (left >= 4) {
+        __builtin_memcpy(u, p, 8);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) u[e] = e < left ? p[e] : 0;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = bf2f(u[e]);
+}
+__device__ __forceinline__ void store4(const float (&v)[4], float *p, int left) {
+    if (left >= 4) {
+        __builtin_memcpy(p, v, 16);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < left) p[e] = v[e];
+    }
+}
+
+// the thread's entries u[4][4] by memory rows; UPDATE: the momentum is formed
+// and written, otherwise it is read as written
+template <bool MUON, bool BF16, bool UPDATE>
+__device__ __forceinline__ void load_block(float (&u)[4][4], const View &v, const NsParams &p, int row0, int col0) {
+    const float gs = MUON && p.grad_scale ? *p.grad_scale : 1.0f;
+    float m[4][4];
+#pragma unroll
+    for (int a = 0; a < 4; ++a) {
+        const int left = row0 + a < v.m.rows ? v.m.cols - col0 : 0;
+        const int64_t at = (int64_t)(row0 + a) * v.m.cols + col0;
+        if constexpr (BF16) load4(u[a], (const uint16_t *)v.m.in + at, left);
+        else load4(u[a], (const float *)v.m.in + at, left);
+        if constexpr (MUON) load4(m[a], v.m.mom + at, left);
+    }
+    if constexpr (MUON) {
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float g = u[a][e] * gs;
+                if constexpr (UPDATE) m[a][e] = fmaf(p.mu, m[a][e], p.om_mu * g);
+                u[a][e] = fmaf(p.u_m, m[a][e], p.u_g * g);
+            }
+            if constexpr (UPDATE)
+                store4(m[a], v.m.mom + (int64_t)(row0 + a) * v.m.cols + col0,
+                       row0 + a < v.m.rows ? v.m.cols - col0 : 0);
+        }
+    }
+}
+
+// momentum, and the sum of squares of each tile (fp64: no overflow or underflow of fp32 squares)
+template <bool MUON, bool BF16, int PL>
 __global__ __launch_bounds__(256) void ns_norm_kernel(NsWork w, NsParams p) {
-    __shared__ double red[256];
-    const NsTile t = tile_of(w, blockIdx.x);
-    const View v = view_of(w, t.mat);
-    const float gs = MUON && p.grad_scale ? *p.grad_scale : 1.0f;
+    __shared__ double red[4];
+    const NsTile t = tile_of<false>(w, blockIdx.x);
+    if (t.mat < 0) return;
+    const View v = view_of<PL>(w, t.mat);
+    const int tid = threadIdx.x;
+    const int mi = v.tr ? t.tj : t.ti, mj = v.tr ? t.ti : t.tj;
+    float u[4][4];
+    load_block<MUON, BF16, true>(u, v, p, mi * kNsBlock + (tid >> 4) * 4, mj * kNsBlock + (tid & 15) * 4);
     double s = 0.0;
-    for (int e = threadIdx.x; e < kT * kT; e += 256) {
-        const int hi = e / kT, lo = e % kT;
-        const int i = t.ti * kT + (v.tr ? lo : hi), j = t.tj * kT + (v.tr ? hi : lo);
-        if (i >= v.r || j >= v.c) continue;
-        const int64_t at = place(v, i, j);
-        if constexpr (MUON) v.m.mom[at] = fmaf(p.mu, v.m.mom[at], p.om_mu * (((const float *)v.m.in)[at] * gs));
-        const double u = value_in<MUON, BF16>(v, p, gs, at);
-        s += u * u;
-    }
-    red[threadIdx.x] = s;
+#pragma unroll
+    for (int a = 0; a < 4; ++a)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s += (double)u[a][e] * u[a][e];
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) s += __shfl_xor(s, m, 64);
+    if ((tid & 63) == 0) red[tid >> 6] = s;
     __syncthreads();
-    for (int m = 128; m >= 1; m >>= 1) {
-        if (threadIdx.x < m) red[threadIdx.x] += red[threadIdx.x + m];
-        __syncthreads();
-    }
-    if (threadIdx.x == 0) w.part[blockIdx.x] = red[0];
+    const int ntj = (v.c + kNsBlock - 1) / kNsBlock, nti = (v.r + kNsBlock - 1) / kNsBlock;
+    const int64_t first = w.mats ? v.m.part0 : (int64_t)t.mat * nti * ntj;
+    if (tid == 0) w.part[first + t.ti * ntj + t.tj] = ((red[0] + red[1]) + red[2]) + red[3];
 }
 
-template <bool MUON, bool BF16>
+// X = u / max(|u|, eps), in units
+template <bool MUON, bool BF16, int PL>
 __global__ __launch_bounds__(256) void ns_scale_kernel(NsWork w, NsParams p) {
-    __shared__ double inv;
-    const NsTile t = tile_of(w, blockIdx.x);
-    const View v = view_of(w, t.mat);
-    const float gs = MUON && p.grad_scale ? *p.grad_scale : 1.0f;
-    const int n = ((v.r + kT - 1) / kT) * ((v.c + kT - 1) / kT);
-    if (threadIdx.x == 0) {
-        const double *part = w.part + (w.mats ? v.m.part0 : t.mat * n);
-        double s = 0.0;
-        for (int k = 0; k < n; ++k) s += part[k];
-        s = sqrt(s);
-        inv = 1.0 / (s < p.eps ? p.eps : s);
-    }
+    __shared__ double red[4];
+    const NsTile t = tile_of<false>(w, blockIdx.x);
+    if (t.mat < 0) return;
+    const View v = view_of<PL>(w, t.mat);
+    const int tid = threadIdx.x;
+    const int mi = v.tr ? t.tj : t.ti, mj = v.tr ? t.ti : t.tj;
+    const int row0 = mi * kNsBlock + (tid >> 4) * 4, col0 = mj * kNsBlock + (tid & 15) * 4;
+    float u[4][4];
+    load_block<MUON, BF16, false>(u, v, p, row0, col0);
+    // every workgroup sums the matrix's partial sums itself, in the same order
+    const int ntj = (v.c + kNsBlock - 1) / kNsBlock, nti = (v.r + kNsBlock - 1) / kNsBlock, n = nti * ntj;
+    const double *part = w.part + (w.mats ? v.m.part0 : (int64_t)t.mat * n);
+    double s = 0.0;
+    for (int k = tid; k < n; k += 256) s += part[k];
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) s += __shfl_xor(s, m, 64);
+    if ((tid & 63) == 0) red[tid >> 6] = s;
     __syncthreads();
-    for (int e = threadIdx.x; e < kT * kT; e += 256) {
-        const int hi = e / kT, lo = e % kT;
-        const int i = t.ti * kT + (v.tr ? lo : hi), j = t.tj * kT + (v.tr ? hi : lo);
-        if (i >= v.r || j >= v.c) continue;
-        v.x0[(int64_t)i * v.c + j] = (float)(value_in<MUON, BF16>(v, p, gs, place(v, i, j)) * inv);
+    const double norm = sqrt(((red[0] + red[1]) + red[2]) + red[3]);
+    const double f = (double)kScale / (norm < p.eps ? p.eps : norm);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+        // row i of the iterate, columns j .. j + 3
+        const int i = v.tr ? col0 + x : row0 + x, j = v.tr ? row0 : col0;
+        if ((i >> 5) >= v.R || (j >> 5) >= v.C) continue;
+        float q[4];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) q[y] = (float)((double)(v.tr ? u[y][x] : u[x][y]) * f);
+        half4 h[PL];
+        split4<PL>(q, h);
+        char *unit = v.x0 + ((int64_t)(i >> 5) * v.C + (j >> 5)) * (PL * kPlane);
+        const int k = j & 31, at = chunk(i & 31, (k >> 3) & 1, k >> 4) + (k & 4) * 2;
+#pragma unroll
+        for (int q2 = 0; q2 < PL; ++q2) *(half4 *)(unit + q2 * kPlane + at) = h[q2];
     }
 }
 
-// acc += the 64 x 64 tile of L R, L[i][k] and R[k][j] by functions; 4 x 4 per thread
-template <class FL, class FR>
-__device__ void tile_product(float (&acc)[4][4], int K, FL L, FR R) {
-    __shared__ float ls[16][kT + 4], rs[16][kT + 4];
-    const int tid = threadIdx.x, ty = tid / 16, tx = tid % 16;
-    for (int k0 = 0; k0 < K; k0 += 16) {
-        for (int e = tid; e < 16 * kT; e += 256) {
-            ls[e % 16][e / 16] = L(e / 16, k0 + e % 16);
-            rs[e / kT][e % kT] = R(k0 + e / kT, e % kT);
+// ---- products
+//
+// A workgroup of 4 waves forms a T x T tile, a wave a quarter of it, from units staged
+// in LDS, one unit column (32 contraction entries) per stage, copied by
+// global_load_lds 16 bytes a lane, S - 1 stages ahead: the copies are counted
+// by hand (vmcnt), one barrier per stage.
+
+enum { kGram, kPoly, kApply, kLast };
+struct Yes { static constexpr bool value = true; };
+struct No { static constexpr bool value = false; };
+
+// 16 bytes per lane from base + off to LDS at lds + 16 lane.  In asm because the compiler would
+// wait for all copies in flight before every LDS read; nothing but the counter below waits for these.
+// (M0 holds the LDS address; nothing else in these kernels uses it)
+__device__ __forceinline__ void copy_to_lds(const char *base, uint32_t off, uint32_t lds) {
+    asm volatile(
+        "s_mov_b32 m0, %0\n\t"
+        "s_nop 0\n\t"
+        "global_load_lds_dwordx4 %1, %2"
+        :
+        : "s"(lds), "v"(off), "s"(base)
+        : "memory");
+}
+template <int N>
+__device__ __forceinline__ void wait_copies_and_barrier() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(N) : "memory");
+}
+
+template <int T, int PL, int S, int KIND, bool MUON, bool BF16>
+__global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, int odd) {
+    constexpr int U = T / 64;             // units of a wave's tile in each direction
+    constexpr int N = T / 32;             // units of the workgroup's
+    constexpr int UNIT = PL * kPlane;
+    constexpr int STAGE = 2 * N * UNIT;
+    constexpr int COPIES = U * UNIT / 1024;  // of a wave and stage
+    constexpr bool SQUARE = KIND == kGram || KIND == kPoly;
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    const NsTile t = tile_of<SQUARE>(w, blockIdx.x);
+    if (t.mat < 0) return;
+    const View v = view_of<PL>(w, t.mat);
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wr = wave >> 1, wc = wave & 1, h = lane >> 5, n = lane & 31;
+    const char *x = KIND == kPoly ? v.A : odd ? v.x1 : v.x0;
+    const int K = KIND == kGram ? v.C : v.R;  // unit columns of the contraction
+
+    // this wave's share of a stage: U units; units past the matrix repeat its
+    // last one, for results that are not stored
+    const char *src[U];
+    int64_t step;
+#pragma unroll
+    for (int q = 0; q < U; ++q) {
+        const int e = wave * U + q, op = e / N, k = e % N;  // operand (wave-uniform: N is a multiple of U)
+        const int first = (op == 0 ? t.ti : t.tj) * N + k;
+        if (SQUARE) {
+            const int row = first < v.R ? first : v.R - 1;
+            src[q] = x + (int64_t)row * K * UNIT;
+            step = UNIT;
+        } else if (op == 0) {
+            const int row = first < v.R ? first : v.R - 1;
+            src[q] = v.P + (int64_t)row * v.R * UNIT;
+            step = UNIT;
+        } else {
+            const int col = first < v.C ? first : v.C - 1;
+            src[q] = x + (int64_t)col * UNIT;
+            step = (int64_t)v.C * UNIT;
         }
-        __syncthreads();
-        for (int k = 0; k < 16; ++k)
-            for (int x = 0; x < 4; ++x)
-                for (int y = 0; y < 4; ++y) acc[x][y] = fmaf(ls[k][ty * 4 + x], rs[k][tx * 4 + y], acc[x][y]);
-        __syncthreads();
     }
-}
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
+    auto copy_stage = [&](int k) {
+        const uint32_t dst = lds0 + (uint32_t)(k % S) * STAGE + (uint32_t)(wave * U) * UNIT;
+#pragma unroll
+        for (int q = 0; q < U; ++q)
+#pragma unroll
+            for (int e = 0; e < UNIT / 1024; ++e)
+                copy_to_lds(src[q] + k * step, (uint32_t)(e * 1024 + lane * 16), dst + q * UNIT + e * 1024);
+    };
 
-// POLY: P = a I + b A + c A A; otherwise A = X X^T
-template <bool POLY>
-__global__ __launch_bounds__(256) void ns_gram_kernel(NsWork w, NsParams p, bool odd) {
-    const NsTile t = tile_of(w, blockIdx.x);
-    const View v = view_of(w, t.mat);
-    const float *x = POLY ? v.A : odd ? v.x1 : v.x0;
-    const int K = POLY ? v.r : v.c, i0 = t.ti * kT, j0 = t.tj * kT;
-    auto at = [&](int row, int k) { return row < v.r && k < K ? x[(int64_t)row * K + k] : 0.0f; };
-    float acc[4][4] = {};
-    tile_product(acc, K, [&](int i, int k) { return at(i0 + i, k); }, [&](int k, int j) { return at(j0 + j, k); });
-    const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
-    for (int a = 0; a < 4; ++a)
-        for (int b = 0; b < 4; ++b) {
-            const int i = i0 + ty * 4 + a, j = j0 + tx * 4 + b;
-            if (i >= v.r || j >= v.r) continue;
-            const int64_t e = (int64_t)i * v.r + j;
-            if constexpr (POLY) v.P[e] = p.b * v.A[e] + p.c * acc[a][b] + (i == j ? p.a : 0.0f);
-            else v.A[e] = acc[a][b];
-        }
-}
+    f32x16 acc[U][U];  // [row unit or, where the operands are swapped, ...]: see below
+#pragma unroll
+    for (int a = 0; a < U; ++a)
+#pragma unroll
+        for (int b = 0; b < U; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[a][b][e] = 0.0f;
 
-// X = P X, or (LAST) the result
-template <bool LAST, bool MUON, bool BF16>
-__global__ __launch_bounds__(256) void ns_apply_kernel(NsWork w, NsParams p, bool odd) {
-    const NsTile t = tile_of(w, blockIdx.x);
-    const View v = view_of(w, t.mat);
-    const float *x = odd ? v.x1 : v.x0;
-    float *y = odd ? v.x0 : v.x1;
-    const int i0 = t.ti * kT, j0 = t.tj * kT;
-    float acc[4][4] = {};
-    tile_product(
-        acc, v.r, [&](int i, int k) { return i0 + i < v.r && k < v.r ? v.P[(int64_t)(i0 + i) * v.r + k] : 0.0f; },
-        [&](int k, int j) { return k < v.r && j0 + j < v.c ? x[(int64_t)k * v.c + j0 + j] : 0.0f; });
-    const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
-    for (int a = 0; a < 4; ++a)
-        for (int b = 0; b < 4; ++b) {
-            const int i = i0 + ty * 4 + a, j = j0 + tx * 4 + b;
-            if (i >= v.r || j >= v.c) continue;
-            if constexpr (!LAST) {
-                y[(int64_t)i * v.c + j] = acc[a][b];
-            } else {
-                const int64_t e = place(v, i, j);
-                if constexpr (MUON) {
-                    float *prm = (float *)v.m.out;
-                    const float q = fmaf(-p.lr * v.m.scale, acc[a][b], p.decay * prm[e]);
-                    prm[e] = q;
-                    if (v.m.swa) v.m.swa[e] = fmaf(p.sd, v.m.swa[e], p.om_sd * q);
-                } else if constexpr (BF16) {
-                    ((uint16_t *)v.m.out)[e] = f2bf(acc[a][b]);
-                } else {
-                    ((float *)v.m.out)[e] = acc[a][b];
-                }
+    // operand 0's fragments f0 (tile rows), operand 1's f1 (tile columns).  D = f0 f1 has lane = column,
+    // registers = rows; D = f1 f0 the other way round, which is what an iterate's units store
+    // (lane = row, four consecutive columns)
+    auto products = [&](auto swapped) {
+#pragma unroll
+        for (int k = 0; k < S - 1; ++k)
+            if (k < K) copy_stage(k);
+        for (int k = 0; k < K; ++k) {
+            // stage k has arrived when at most the later ones' copies are outstanding
+            if (k + S - 2 < K) wait_copies_and_barrier<(S - 2) * COPIES>();
+            else wait_copies_and_barrier<0>();
+            if (k + S - 1 < K) copy_stage(k + S - 1);
+            const char *s0 = lds + (k % S) * STAGE + wr * U * UNIT, *s1 = lds + (k % S) * STAGE + (N + wc * U) * UNIT;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                Frag<PL> f0[U], f1[U];
+#pragma unroll
+                for (int a = 0; a < U; ++a)
+#pragma unroll
+                    for (int q = 0; q < PL; ++q) {
+                        f0[a].p[q] = frag_rows(s0 + a * UNIT + q * kPlane, lane, s);
+                        f1[a].p[q] = SQUARE ? frag_rows(s1 + a * UNIT + q * kPlane, lane, s)
+                                            : frag_cols(s1 + a * UNIT + q * kPlane, lane, s);
+                    }
+#pragma unroll
+                for (int a = 0; a < U; ++a)
+#pragma unroll
+                    for (int b = 0; b < U; ++b) {
+                        if constexpr (decltype(swapped)::value) mma<PL>(acc[a][b], f1[b], f0[a]);
+                        else mma<PL>(acc[a][b], f0[a], f1[b]);
+                    }
             }
         }
+    };
+    const int i0 = t.ti * N + wr * U, j0 = t.tj * N + wc * U;  // this wave's first units
+    if constexpr (SQUARE) {
+        // lane = column: stored as row `column` of the symmetric matrix's unit (j, i)
+        products(No{});
+        __syncthreads();  // the stages become scratch
+        char *const scratch = lds + wave * UNIT;
+        char *const dst = KIND == kPoly ? v.P : v.A;
+#pragma unroll
+        for (int a = 0; a < U; ++a)
+#pragma unroll
+            for (int b = 0; b < U; ++b) {
+                const int i = i0 + a, j = j0 + b;
+                if (i >= v.R || j >= v.R) continue;  // wave-uniform
+                const int64_t at = ((int64_t)j * v.R + i) * UNIT;
+                half4 out[4][PL];
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {  // rows 8 g + 4 h .. + 3 of the tile
+                    const int pos = chunk(n, g & 1, g >> 1) + h * 8;
+                    float q[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) q[e] = acc[a][b][4 * g + e] * (kUnscale * kScale);
+                    if constexpr (KIND == kPoly) {
+                        half4 old[PL];
+#pragma unroll
+                        for (int z = 0; z < PL; ++z) old[z] = *(const half4 *)(v.A + at + z * kPlane + pos);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            float o = (float)old[0][e];
+                            if constexpr (PL == 2) o += (float)old[1][e];
+                            q[e] = fmaf(p.c, q[e], p.b * o);
+                            if (i == j && 8 * g + 4 * h + e == n) q[e] = fmaf(p.a, kScale, q[e]);
+                        }
+                    }
+                    split4<PL>(q, out[g]);
+#pragma unroll
+                    for (int z = 0; z < PL; ++z) *(half4 *)(dst + at + z * kPlane + pos) = out[g][z];
+                }
+                if (t.ti != t.tj) {  // the mirrored unit (i, j), through LDS by columns
+#pragma unroll
+                    for (int g = 0; g < 4; ++g)
+#pragma unroll
+                        for (int z = 0; z < PL; ++z)
+                            *(half4 *)(scratch + z * kPlane + chunk(n, g & 1, g >> 1) + h * 8) = out[g][z];
+                    __builtin_amdgcn_wave_barrier();
+                    const int64_t mirrored = ((int64_t)i * v.R + j) * UNIT;
+#pragma unroll
+                    for (int z = 0; z < PL; ++z)
+#pragma unroll
+                        for (int s = 0; s < 2; ++s)
+                            *(half8 *)(dst + mirrored + z * kPlane + chunk(n, h, s)) = frag_cols(scratch + z * kPlane, lane, s);
+                    __builtin_amdgcn_wave_barrier();
+                }
+            }
+    } else if constexpr (KIND == kApply) {
+        products(Yes{});  // lane = row, registers = columns
+        char *const dst = odd ? v.x0 : v.x1;
+#pragma unroll
+        for (int a = 0; a < U; ++a)
+#pragma unroll
+            for (int b = 0; b < U; ++b) {
+                const int i = i0 + a, j = j0 + b;
+                if (i >= v.R || j >= v.C) continue;
+                char *unit = dst + ((int64_t)i * v.C + j) * UNIT;
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    float q[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) q[e] = acc[a][b][4 * g + e] * (kUnscale * kScale);
+                    half4 out[PL];
+                    split4<PL>(q, out);
+#pragma unroll
+                    for (int z = 0; z < PL; ++z)
+                        *(half4 *)(unit + z * kPlane + chunk(n, g & 1, g >> 1) + h * 8) = out[z];
+                }
+            }
+    } else {
+        // the lanes go along the matrix's memory rows: columns of the iterate, or its rows where it is transposed
+        if (v.tr) products(Yes{});
+        else products(No{});
+#pragma unroll
+        for (int a = 0; a < U; ++a)
+#pragma unroll
+            for (int b = 0; b < U; ++b) {
+                const int iu = i0 + a, ju = j0 + b;
+                // memory row of register 0 and column of the lane
+                const int mr = (v.tr ? ju : iu) * 32 + 4 * h, mc = (v.tr ? iu : ju) * 32 + n;
+                if (mc >= v.m.cols) continue;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int row = mr + 8 * (e >> 2) + (e & 3);
+                    if (row >= v.m.rows) continue;
+                    const int64_t at = (int64_t)row * v.m.cols + mc;
+                    const float o = acc[a][b][e] * kUnscale;
+                    if constexpr (MUON) {
+                        float *prm = (float *)v.m.out;
+                        const float q = fmaf(-p.lr * v.m.scale, o, p.decay * prm[at]);
+                        prm[at] = q;
+                        if (v.m.swa) v.m.swa[at] = fmaf(p.sd, v.m.swa[at], p.om_sd * q);
+                    } else if constexpr (BF16) {
+                        ((uint16_t *)v.m.out)[at] = f2bf(o);
+                    } else {
+                        ((float *)v.m.out)[at] = o;
+                    }
+                }
+            }
+    }
 }
 
-template <bool MUON, bool BF16>
-hipError_t launch_all(NsWork w, const NsParams &p, int64_t n_x, const NsTile *tx, int64_t n_a, const NsTile *ta,
-                      hipStream_t s) {
-    NsWork wx = w, wa = w;
+// S stages: with the large tile two workgroups per CU, with the small one enough copies in
+// flight for a CU that has one
+template <int T, int PL> constexpr int kStages = T == 128 ? (PL == 2 ? 2 : 4) : 4;
+
+template <int T, int PL, int KIND, bool MUON, bool BF16>
+hipError_t launch_product(NsWork w, const NsTile *tiles, int64_t grid, const NsParams &p, int odd, hipStream_t s) {
+    w.tiles = tiles;
     const int r = w.uni.rows < w.uni.cols ? w.uni.rows : w.uni.cols, c = w.uni.rows + w.uni.cols - r;
-    wx.tiles = tx;
-    wx.nti = (r + kT - 1) / kT;
-    wx.ntj = (c + kT - 1) / kT;
-    wa.tiles = ta;
-    wa.nti = wa.ntj = wx.nti;
-    const dim3 gx((unsigned)n_x), ga((unsigned)n_a), b(256);
-    hipLaunchKernelGGL((ns_norm_kernel<MUON, BF16>), gx, b, 0, s, wx, p);
-    hipLaunchKernelGGL((ns_scale_kernel<MUON, BF16>), gx, b, 0, s, wx, p);
-    for (int k = 0; k < p.steps; ++k) {
-        hipLaunchKernelGGL(ns_gram_kernel<false>, ga, b, 0, s, wa, p, (k & 1) != 0);
-        hipLaunchKernelGGL(ns_gram_kernel<true>, ga, b, 0, s, wa, p, (k & 1) != 0);
-        if (k + 1 < p.steps) hipLaunchKernelGGL((ns_apply_kernel<false, MUON, BF16>), gx, b, 0, s, wx, p, (k & 1) != 0);
-        else hipLaunchKernelGGL((ns_apply_kernel<true, MUON, BF16>), gx, b, 0, s, wx, p, (k & 1) != 0);
-    }
+    w.nti = (r + T - 1) / T;
+    w.ntj = (c + T - 1) / T;
+    constexpr int S = kStages<T, PL>;
+    hipLaunchKernelGGL((ns_product_kernel<T, PL, S, KIND, MUON, BF16>), dim3((unsigned)grid), dim3(256),
+                       S * 2 * (T / 32) * PL * kPlane, s, w, p, odd);
     return hipGetLastError();
+}
+
+template <int T, bool MUON, bool BF16>
+hipError_t launch_all(NsWork w, const NsLists &l, const NsParams &p, hipStream_t s) {
+    constexpr int PL = BF16 ? 1 : 2;
+    NsWork wx = w;
+    const int r = w.uni.rows < w.uni.cols ? w.uni.rows : w.uni.cols, c = w.uni.rows + w.uni.cols - r;
+    wx.tiles = l.x;
+    wx.nti = (r + kNsBlock - 1) / kNsBlock;
+    wx.ntj = (c + kNsBlock - 1) / kNsBlock;
+    const dim3 gx((unsigned)l.n_x), b(256);
+    hipLaunchKernelGGL((ns_norm_kernel<MUON, BF16, PL>), gx, b, 0, s, wx, p);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((ns_scale_kernel<MUON, BF16, PL>), gx, b, 0, s, wx, p);
+    e = hipGetLastError();
+    for (int k = 0; k < p.steps && e == hipSuccess; ++k) {
+        const int odd = k & 1;
+        e = launch_product<T, PL, kGram, false, false>(w, l.gram, l.n_gram, p, odd, s);
+        if (e != hipSuccess) return e;
+        e = launch_product<T, PL, kPoly, false, false>(w, l.gram, l.n_gram, p, odd, s);
+        if (e != hipSuccess) return e;
+        e = k + 1 < p.steps ? launch_product<T, PL, kApply, false, false>(w, l.apply, l.n_apply, p, odd, s)
+                            : launch_product<T, PL, kLast, MUON, BF16>(w, l.apply, l.n_apply, p, odd, s);
+    }
+    return e;
 }
 
 }  // namespace
 
-int64_t ns_matrix_bytes(int64_t rows, int64_t cols) {
+int64_t ns_matrix_bytes(int64_t rows, int64_t cols, int planes) {
     const int64_t r = rows < cols ? rows : cols, c = rows + cols - r;
-    return 4 * (2 * up(r * c) + 2 * up(r * r));
+    const int64_t R = (r + 31) / 32, C = (c + 31) / 32;
+    return 2 * (R * C + R * R) * planes * kPlane;
 }
 
-hipError_t launch_ns(NsWork w, const NsParams &p, bool muon, bool bf16, int64_t n_x, const NsTile *tx, int64_t n_a,
-                     const NsTile *ta, hipStream_t s) {
-    if (muon) return launch_all<true, false>(w, p, n_x, tx, n_a, ta, s);
-    return bf16 ? launch_all<false, true>(w, p, n_x, tx, n_a, ta, s) : launch_all<false, false>(w, p, n_x, tx, n_a, ta, s);
+// 128 x 128 tiles read each staged unit twice as often; once they do not fill
+// the CUs, tiles of a quarter the size do the work sooner
+int ns_tile(int64_t tiles128) { return tiles128 >= 256 ? 128 : 64; }
+
+hipError_t launch_ns(const NsWork &w, const NsLists &l, const NsParams &p, bool muon, bool bf16, hipStream_t s) {
+    if (l.tile == 128)
+        return muon ? launch_all<128, true, false>(w, l, p, s)
+                    : bf16 ? launch_all<128, false, true>(w, l, p, s) : launch_all<128, false, false>(w, l, p, s);
+    return muon ? launch_all<64, true, false>(w, l, p, s)
+                : bf16 ? launch_all<64, false, true>(w, l, p, s) : launch_all<64, false, false>(w, l, p, s);
 }
 
 }  // namespace evo

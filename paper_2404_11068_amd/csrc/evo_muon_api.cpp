@@ -6,11 +6,14 @@
 #include <math.h>
 #include <string.h>
 
+#include <algorithm>
+#include <vector>
+
 #include "evo_ns.h"
 
 namespace {
 
-using evo::kNsTile;
+using evo::NsLists;
 using evo::NsMat;
 using evo::NsTile;
 
@@ -18,7 +21,8 @@ constexpr int64_t kMostSide = 32768;
 
 bool aligned(const void *p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
-int64_t tiles_of(int64_t n) { return (n + kNsTile - 1) / kNsTile; }
+int64_t tiles_of(int64_t n, int64_t tile) { return (n + tile - 1) / tile; }
+int64_t blocks_of(int64_t rows, int64_t cols) { return tiles_of(rows, evo::kNsBlock) * tiles_of(cols, evo::kNsBlock); }
 
 // whether the iterate stays in the kernels' range: the largest singular value,
 // followed from 1 (no singular value of X exceeds the Frobenius norm) through
@@ -42,36 +46,134 @@ int check_coefs(double a, double b, double c, double eps, int steps) {
     return top <= 8.0 ? EVO_OK : EVO_ERR_UNSUPPORTED;
 }
 
-// ---- Muon plan: header, matrices, tiles of the iterate, tiles of the Gram matrix
+// ---- Muon plan: header, matrices, tiles of the norm, of the Gram matrix and of the iterate
 struct PlanHeader {
     uint64_t magic;
-    int64_t bytes, n_mats, n_x, n_a, ws_bytes, part_bytes;
-    int64_t off_mats, off_x, off_a;
+    int64_t bytes, n_mats, ws_bytes, part_bytes;
+    int64_t tile, n_x, n_gram, n_apply;  // entries of the lists, padding included
+    int64_t off_mats, off_x, off_gram, off_apply;
 };
-constexpr uint64_t kMagic = 0x45564f4d554f4e31ull;
+constexpr uint64_t kMagic = 0x45564f4d554f4e32ull;
 
 int64_t round256(int64_t n) { return (n + 255) & ~int64_t(255); }
 
-bool measure(const evo_muon_tensor *t, int32_t n, PlanHeader &h) {
+struct Size {
+    int64_t r, c;
+};
+Size size_of(const evo_muon_tensor &t) {
+    return t.rows < t.cols ? Size{t.rows, t.cols} : Size{t.cols, t.rows};
+}
+
+template <class F>
+void each_gram(int64_t r, int64_t tile, F f) {
+    const int64_t n = tiles_of(r, tile);
+    for (int64_t i = 0; i < n; ++i)
+        for (int64_t j = i; j < n; ++j) f((int32_t)i, (int32_t)j);
+}
+template <class F>
+void each_tile(int64_t r, int64_t c, int64_t tile, F f) {
+    for (int64_t i = 0; i < tiles_of(r, tile); ++i)
+        for (int64_t j = 0; j < tiles_of(c, tile); ++j) f((int32_t)i, (int32_t)j);
+}
+
+// lists by XCD -> one list in which entry k belongs to XCD k % 8
+struct Lists {
+    std::vector<NsTile> by[8];
+    int next = 0;
+    void add(int xcd, const NsTile &t) {
+        if (xcd == 8) {
+            xcd = next;
+            next = (next + 1) & 7;
+        }
+        by[xcd].push_back(t);
+    }
+    int64_t total() const {
+        size_t most = 0;
+        for (const auto &v : by) most = v.size() > most ? v.size() : most;
+        return (int64_t)most * 8;
+    }
+    void write(NsTile *out) const {
+        const int64_t n = total();
+        for (int64_t k = 0; k < n; ++k) {
+            const auto &v = by[k & 7];
+            out[k] = (size_t)(k >> 3) < v.size() ? v[k >> 3] : NsTile{-1, 0, 0};
+        }
+    }
+};
+
+struct Plan {
+    PlanHeader h{};
+    std::vector<NsMat> mats;
+    Lists x, gram, apply;
+};
+
+// false: invalid sizes
+bool make_plan(const evo_muon_tensor *t, int32_t n, Plan &p) {
     if (n < 0 || (n > 0 && !t)) return false;
-    h = PlanHeader{};
+    PlanHeader &h = p.h;
+    std::vector<int32_t> order;
+    int64_t tiles128 = 0, blocks = 0;
+    double total = 0.0;
+    auto cost = [&](int32_t i) {
+        const Size z = size_of(t[i]);
+        return (double)z.r * z.r * (3.0 * z.c + z.r) + 1e4 * z.c * z.r;
+    };
     for (int32_t i = 0; i < n; ++i) {
         if (t[i].rows < 0 || t[i].cols < 0 || t[i].rows > kMostSide || t[i].cols > kMostSide) return false;
         if (t[i].rows == 0 || t[i].cols == 0) continue;
-        const int64_t r = t[i].rows < t[i].cols ? t[i].rows : t[i].cols, c = t[i].rows + t[i].cols - r;
-        ++h.n_mats;
-        h.n_x += tiles_of(r) * tiles_of(c);
-        h.n_a += tiles_of(r) * tiles_of(r);
-        h.ws_bytes += evo::ns_matrix_bytes(t[i].rows, t[i].cols);
-        if (h.n_x > 0x7fffffff) return false;
+        const Size z = size_of(t[i]);
+        order.push_back(i);
+        tiles128 += tiles_of(z.r, 128) * tiles_of(z.c, 128);
+        blocks += blocks_of(z.r, z.c);
+        total += cost(i);
+        if (blocks > 0x3fffffff) return false;
     }
+    std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return cost(a) > cost(b); });
     h.magic = kMagic;
-    h.part_bytes = round256(h.n_x * 8);
-    h.ws_bytes += h.part_bytes;
+    h.tile = evo::ns_tile(tiles128);
+    h.n_mats = (int64_t)order.size();
+    h.part_bytes = round256(blocks * 8);
+    h.ws_bytes = h.part_bytes;
+    double load[8] = {};
+    int64_t part = 0, off = 0;
+    for (int32_t m = 0; m < (int32_t)order.size(); ++m) {
+        const evo_muon_tensor &s = t[order[m]];
+        const Size z = size_of(s);
+        NsMat M{};
+        M.in = s.grad;
+        M.out = s.param;
+        M.mom = s.momentum;
+        M.swa = s.swa;
+        M.rows = (int32_t)s.rows;
+        M.cols = (int32_t)s.cols;
+        M.scale = (float)s.update_scale;
+        M.part0 = (int32_t)part;
+        M.off = off;
+        part += blocks_of(z.r, z.c);
+        off += evo::ns_matrix_bytes(s.rows, s.cols, 2);
+        p.mats.push_back(M);
+        const double c = cost(order[m]);
+        int xcd = 8;
+        if (c * 8 <= total) {
+            xcd = 0;
+            for (int k = 1; k < 8; ++k)
+                if (load[k] < load[xcd]) xcd = k;
+            load[xcd] += c;
+        }
+        each_tile(z.r, z.c, evo::kNsBlock, [&](int32_t i, int32_t j) { p.x.add(xcd, NsTile{m, i, j}); });
+        each_gram(z.r, h.tile, [&](int32_t i, int32_t j) { p.gram.add(xcd, NsTile{m, i, j}); });
+        each_tile(z.r, z.c, h.tile, [&](int32_t i, int32_t j) { p.apply.add(xcd, NsTile{m, i, j}); });
+    }
+    h.ws_bytes += off;
+    h.n_x = p.x.total();
+    h.n_gram = p.gram.total();
+    h.n_apply = p.apply.total();
+    if (h.n_x > 0x7fffffff) return false;
     h.off_mats = round256(sizeof(PlanHeader));
     h.off_x = h.off_mats + round256(h.n_mats * (int64_t)sizeof(NsMat));
-    h.off_a = h.off_x + round256(h.n_x * (int64_t)sizeof(NsTile));
-    h.bytes = h.off_a + round256(h.n_a * (int64_t)sizeof(NsTile));
+    h.off_gram = h.off_x + round256(h.n_x * (int64_t)sizeof(NsTile));
+    h.off_apply = h.off_gram + round256(h.n_gram * (int64_t)sizeof(NsTile));
+    h.bytes = h.off_apply + round256(h.n_apply * (int64_t)sizeof(NsTile));
     return true;
 }
 
@@ -80,15 +182,25 @@ int check_orth(const evo_orth_dims *d) {
     if (d->dtype != EVO_DTYPE_F32 && d->dtype != EVO_DTYPE_BF16) return EVO_ERR_UNSUPPORTED;
     if (d->n_batch < 0 || d->rows < 0 || d->cols < 0) return EVO_ERR_INVALID_ARG;
     if (d->n_batch > (1 << 20) || d->rows > kMostSide || d->cols > kMostSide) return EVO_ERR_UNSUPPORTED;
-    if (d->n_batch * tiles_of(d->rows) * tiles_of(d->cols) > 0x7fffffff) return EVO_ERR_UNSUPPORTED;
+    if (d->n_batch * blocks_of(d->rows, d->cols) > 0x3fffffff) return EVO_ERR_UNSUPPORTED;
     return check_coefs(d->a, d->b, d->c, d->eps, d->steps);
 }
 
 bool orth_empty(const evo_orth_dims *d) { return d->n_batch == 0 || d->rows == 0 || d->cols == 0; }
 
 size_t orth_workspace(const evo_orth_dims *d) {
-    return (size_t)(round256(d->n_batch * tiles_of(d->rows) * tiles_of(d->cols) * 8) +
-                    d->n_batch * evo::ns_matrix_bytes(d->rows, d->cols));
+    return (size_t)(round256(d->n_batch * blocks_of(d->rows, d->cols) * 8) +
+                    d->n_batch * evo::ns_matrix_bytes(d->rows, d->cols, d->dtype == EVO_DTYPE_BF16 ? 1 : 2));
+}
+
+// no C++ exception leaves a C entry: `none` where the plan's memory cannot be had
+template <class F>
+int guarded(F f, int none) {
+    try {
+        return f();
+    } catch (...) {
+        return none;
+    }
 }
 
 }  // namespace
@@ -115,74 +227,71 @@ int evo_orthogonalize(const evo_orth_dims *d, const void *x, void *out, void *wo
     const size_t need = orth_workspace(d);
     if (!workspace || workspace_bytes < need) return EVO_ERR_WORKSPACE;
     if (!aligned(workspace, 256)) return EVO_ERR_ALIGNMENT;
-    const int64_t r = d->rows < d->cols ? d->rows : d->cols, c = d->rows + d->cols - r;
-    const int64_t n_x = tiles_of(r) * tiles_of(c), n_a = tiles_of(r) * tiles_of(r);
+    const int64_t r = d->rows < d->cols ? d->rows : d->cols, c = d->rows + d->cols - r, n = d->n_batch;
+    const bool bf16 = d->dtype == EVO_DTYPE_BF16;
     evo::NsWork w{};
     w.uni.in = x;
     w.uni.out = out;
     w.uni.rows = (int32_t)d->rows;
     w.uni.cols = (int32_t)d->cols;
     w.in_stride = each;
-    w.ws_stride = evo::ns_matrix_bytes(d->rows, d->cols);
+    w.ws_stride = evo::ns_matrix_bytes(d->rows, d->cols, bf16 ? 1 : 2);
+    w.n_mats = (int32_t)n;
     w.part = (double *)workspace;
-    w.ws = (char *)workspace + round256(d->n_batch * n_x * 8);
+    w.ws = (char *)workspace + round256(n * blocks_of(r, c) * 8);
+    NsLists l{};
+    l.tile = evo::ns_tile(n * tiles_of(r, 128) * tiles_of(c, 128));
+    // eight matrices or more are dealt to the XCDs, so their number is rounded up
+    const int64_t slots = n >= 8 ? (n + 7) / 8 * 8 : n, g = tiles_of(r, l.tile);
+    l.n_x = slots * blocks_of(r, c);
+    l.n_gram = slots * (g * (g + 1) / 2);
+    l.n_apply = slots * g * tiles_of(c, l.tile);
     evo::NsParams p{};
     p.a = (float)d->a;
     p.b = (float)d->b;
     p.c = (float)d->c;
     p.eps = d->eps;
     p.steps = d->steps;
-    return evo::launch_ns(w, p, false, d->dtype == EVO_DTYPE_BF16, d->n_batch * n_x, nullptr, d->n_batch * n_a, nullptr,
-                          (hipStream_t)stream) == hipSuccess
-               ? EVO_OK
-               : EVO_ERR_HIP;
+    return evo::launch_ns(w, l, p, false, bf16, (hipStream_t)stream) == hipSuccess ? EVO_OK : EVO_ERR_HIP;
 }
 
 int64_t evo_muon_plan_bytes(const evo_muon_tensor *tensors, int32_t n_tensors) {
-    PlanHeader h;
-    return measure(tensors, n_tensors, h) ? h.bytes : -1;
+    int64_t bytes = -1;
+    guarded(
+        [&] {
+            Plan p;
+            if (make_plan(tensors, n_tensors, p)) bytes = p.h.bytes;
+            return 0;
+        },
+        0);
+    return bytes;
 }
 
 int evo_muon_build_plan(const evo_muon_tensor *tensors, int32_t n_tensors, void *plan, size_t plan_bytes) {
-    PlanHeader h;
-    if (!measure(tensors, n_tensors, h) || !plan) return EVO_ERR_INVALID_ARG;
-    if (!aligned(plan, 8)) return EVO_ERR_ALIGNMENT;
-    if (plan_bytes < (size_t)h.bytes) return EVO_ERR_WORKSPACE;
-    for (int32_t i = 0; i < n_tensors; ++i) {
-        const evo_muon_tensor &t = tensors[i];
-        if (t.rows == 0 || t.cols == 0) continue;
-        if (!t.param || !t.grad || !t.momentum || !isfinite(t.update_scale)) return EVO_ERR_INVALID_ARG;
-        if (!aligned(t.param, 4) || !aligned(t.grad, 4) || !aligned(t.momentum, 4) || !aligned(t.swa, 4))
-            return EVO_ERR_ALIGNMENT;
-    }
-    memset(plan, 0, (size_t)h.bytes);
-    memcpy(plan, &h, sizeof h);
-    NsMat *mats = (NsMat *)((char *)plan + h.off_mats);
-    NsTile *tx = (NsTile *)((char *)plan + h.off_x), *ta = (NsTile *)((char *)plan + h.off_a);
-    int32_t m = 0, part = 0;
-    int64_t off = 0;
-    for (int32_t i = 0; i < n_tensors; ++i) {
-        const evo_muon_tensor &t = tensors[i];
-        if (t.rows == 0 || t.cols == 0) continue;
-        const int64_t r = t.rows < t.cols ? t.rows : t.cols, c = t.rows + t.cols - r;
-        NsMat &M = mats[m];
-        M.in = t.grad;
-        M.out = t.param;
-        M.mom = t.momentum;
-        M.swa = t.swa;
-        M.rows = (int32_t)t.rows;
-        M.cols = (int32_t)t.cols;
-        M.scale = (float)t.update_scale;
-        M.part0 = part;
-        M.off = off;
-        off += evo::ns_matrix_bytes(t.rows, t.cols);
-        for (int32_t ti = 0; ti < tiles_of(r); ++ti)
-            for (int32_t tj = 0; tj < tiles_of(c); ++tj, ++part) *tx++ = NsTile{m, ti, tj};
-        for (int32_t ti = 0; ti < tiles_of(r); ++ti)
-            for (int32_t tj = 0; tj < tiles_of(r); ++tj) *ta++ = NsTile{m, ti, tj};
-        ++m;
-    }
-    return EVO_OK;
+    return guarded(
+        [&]() -> int {
+            Plan p;
+            if (!make_plan(tensors, n_tensors, p) || !plan) return EVO_ERR_INVALID_ARG;
+            if (!aligned(plan, 8)) return EVO_ERR_ALIGNMENT;
+            const PlanHeader &h = p.h;
+            if (plan_bytes < (size_t)h.bytes) return EVO_ERR_WORKSPACE;
+            for (int32_t i = 0; i < n_tensors; ++i) {
+                const evo_muon_tensor &t = tensors[i];
+                if (t.rows == 0 || t.cols == 0) continue;
+                if (!t.param || !t.grad || !t.momentum || !isfinite(t.update_scale)) return EVO_ERR_INVALID_ARG;
+                if (!aligned(t.param, 4) || !aligned(t.grad, 4) || !aligned(t.momentum, 4) || !aligned(t.swa, 4))
+                    return EVO_ERR_ALIGNMENT;
+            }
+            char *q = (char *)plan;
+            memset(q, 0, (size_t)h.bytes);
+            memcpy(q, &h, sizeof h);
+            if (!p.mats.empty()) memcpy(q + h.off_mats, p.mats.data(), p.mats.size() * sizeof(NsMat));
+            p.x.write((NsTile *)(q + h.off_x));
+            p.gram.write((NsTile *)(q + h.off_gram));
+            p.apply.write((NsTile *)(q + h.off_apply));
+            return EVO_OK;
+        },
+        EVO_ERR_INVALID_ARG);
 }
 
 size_t evo_muon_workspace_size(const void *plan) {
@@ -228,10 +337,15 @@ int evo_muon_step(const evo_muon_hparams *hp, const void *plan, const void *plan
     p.sd = (float)hp->swa_decay;
     p.om_sd = (float)(1.0 - hp->swa_decay);
     p.grad_scale = grad_scale;
-    return evo::launch_ns(w, p, true, false, h.n_x, (const NsTile *)(dev + h.off_x), h.n_a,
-                          (const NsTile *)(dev + h.off_a), (hipStream_t)stream) == hipSuccess
-               ? EVO_OK
-               : EVO_ERR_HIP;
+    NsLists l{};
+    l.tile = (int)h.tile;
+    l.n_x = h.n_x;
+    l.n_gram = h.n_gram;
+    l.n_apply = h.n_apply;
+    l.x = (const NsTile *)(dev + h.off_x);
+    l.gram = (const NsTile *)(dev + h.off_gram);
+    l.apply = (const NsTile *)(dev + h.off_apply);
+    return evo::launch_ns(w, l, p, true, false, (hipStream_t)stream) == hipSuccess ? EVO_OK : EVO_ERR_HIP;
 }
 
 }  // extern "C"

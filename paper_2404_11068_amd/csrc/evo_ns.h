@@ -19,7 +19,7 @@ struct NsMat {
 };
 
 struct NsTile {
-    int32_t mat, ti, tj;
+    int32_t mat, ti, tj;  // mat < 0: nothing to do
 };
 
 // the matrices of a call and the tiles of a launch: from tables, or (null) of
@@ -29,7 +29,7 @@ struct NsWork {
     const NsTile *tiles;
     NsMat uni;
     int64_t in_stride, ws_stride;  // bytes per matrix of in and out, and of the workspace
-    int32_t nti, ntj;              // tiles per matrix of this launch
+    int32_t n_mats, nti, ntj;      // stack: matrices, and tiles per matrix of this launch
     char *ws;                      // workspace behind the partial sums
     double *part;                  // partial sums of squares
 };
@@ -38,17 +38,26 @@ struct NsParams {
     float a, b, c;
     double eps;
     int steps;
-    // Muon (fp32): u = bm_g g + bm_m m
+    // Muon (fp32): m = mu m + om_mu g, u = u_g g + u_m m, p = decay p - lr scale O, w = sd w + om_sd p
     float mu, om_mu, u_g, u_m, decay, lr, sd, om_sd;
     const float *grad_scale;
 };
 
-// bytes of a matrix's buffers in the workspace
-int64_t ns_matrix_bytes(int64_t rows, int64_t cols);
+// work lists, each a launch's grid: every matrix by tiles of 64 x 64 entries (norm, scaling), and
+// the products' tiles of `tile` x `tile`: the Gram matrix's upper triangle, and the iterate
+struct NsLists {
+    int tile;                         // 64 or 128
+    int64_t n_x, n_gram, n_apply;     // entries, padding included
+    const NsTile *x, *gram, *apply;   // device tables, or null for a stack
+};
 
-constexpr int kNsTile = 64;  // tiles of the lists
+constexpr int kNsBlock = 64;  // tiles of the norm and scaling passes
 
-hipError_t launch_ns(NsWork w, const NsParams &p, bool muon, bool bf16, int64_t n_x, const NsTile *tiles_x, int64_t n_a,
-                     const NsTile *tiles_a, hipStream_t s);
+// bytes of a matrix's buffers in the workspace; planes: 2 for fp32, 1 for bf16
+int64_t ns_matrix_bytes(int64_t rows, int64_t cols, int planes);
+// tiles of the products for a call whose iterates have this many 128 x 128 tiles
+int ns_tile(int64_t tiles128);
+
+hipError_t launch_ns(const NsWork &w, const NsLists &l, const NsParams &p, bool muon, bool bf16, hipStream_t s);
 
 }  // namespace evo

@@ -19,7 +19,7 @@ from typing import Optional
 
 import torch
 
-from .evo_attn import EVO_DTYPE_F32, EvoAttnError, _DTYPES, _empty, _ptr, _stream, load_library
+from .evo_attn import EVO_DTYPE_F32, EvoAttnError, _DTYPES, _empty, _stream, load_library
 
 
 class evo_relpos_dims(ctypes.Structure):
@@ -74,28 +74,31 @@ def relpos_edges_log(n_side: int, max_distance: int, device="cuda") -> torch.Ten
 
 def _index(pos_i, pos_j, edges, seg_i, seg_j, like: torch.Tensor):
     """Checks of the index tensors; returns (B, Li, Lj, E)."""
-    if pos_i.dim() not in (1, 2) or pos_j.dim() != pos_i.dim() or edges.dim() != 1:
+    si, sj, se = pos_i.shape, pos_j.shape, edges.shape
+    if len(si) not in (1, 2) or len(sj) != len(si) or len(se) != 1:
         raise ValueError("pos_i and pos_j must be [B, Li] and [B, Lj] (or [Li] and [Lj]), edges [E]")
-    B = pos_i.shape[0] if pos_i.dim() == 2 else 1
-    if pos_j.dim() == 2 and pos_j.shape[0] != B:
+    if len(si) == 2 and si[0] != sj[0]:
         raise ValueError("pos_i and pos_j must have the same batch size")
-    if (seg_i is None) != (seg_j is None):
-        raise ValueError("seg_i and seg_j go together")
-    if seg_i is not None and (seg_i.shape != pos_i.shape or seg_j.shape != pos_j.shape):
-        raise ValueError("segments must be shaped like the positions")
-    for t in (pos_i, pos_j, edges, seg_i, seg_j):
-        if t is not None and (t.dtype != torch.int32 or not t.is_contiguous()):
-            raise ValueError("positions, segments and edges must be contiguous int32")
-    _same_device(like, pos_i, pos_j, edges, seg_i, seg_j)
-    return B, pos_i.shape[-1], pos_j.shape[-1], edges.shape[0]
-
-
-def _same_device(ref: torch.Tensor, *ts):
-    if not ref.is_cuda or ref.device.index != torch.cuda.current_device():
-        raise ValueError("tensors must be on the current CUDA device")
+    ts = (pos_i, pos_j, edges)
+    if seg_i is not None or seg_j is not None:
+        if seg_i is None or seg_j is None:
+            raise ValueError("seg_i and seg_j go together")
+        if seg_i.shape != si or seg_j.shape != sj:
+            raise ValueError("segments must be shaped like the positions")
+        ts = (pos_i, pos_j, edges, seg_i, seg_j)
+    dev = like.device
     for t in ts:
-        if t is not None and t.device != ref.device:
+        if t.dtype != torch.int32 or not t.is_contiguous():
+            raise ValueError("positions, segments and edges must be contiguous int32")
+        if t.device != dev:
             raise ValueError("tensors must be on one device")
+    if dev.type != "cuda" or dev.index != torch.cuda.current_device():
+        raise ValueError("tensors must be on the current CUDA device")
+    return (si[0] if len(si) == 2 else 1), si[-1], sj[-1], se[0]
+
+
+def _addr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
 
 
 def relpos_bias_fwd(pos_i: torch.Tensor, pos_j: torch.Tensor, edges: torch.Tensor, table: torch.Tensor, *,
@@ -107,25 +110,25 @@ def relpos_bias_fwd(pos_i: torch.Tensor, pos_j: torch.Tensor, edges: torch.Tenso
     out or base when one is given, bfloat16 otherwise."""
     lib = _lib()
     B, Li, Lj, E = _index(pos_i, pos_j, edges, seg_i, seg_j, table)
-    H = table.shape[0] if table.dim() == 2 else 0
-    buckets = E + 1 + (seg_i is not None)
-    if table.dim() != 2 or H < 1 or table.shape[1] != buckets or table.dtype != torch.float32 \
-            or not table.is_contiguous():
-        raise ValueError("table must be a contiguous float32 [H, %d] tensor" % buckets)
+    seg = 0 if seg_i is None else 1
+    H = table.shape[0]
+    if table.shape != (H, E + 1 + seg) or H < 1 or table.dtype != torch.float32 or not table.is_contiguous():
+        raise ValueError("table must be a contiguous float32 [H, %d] tensor" % (E + 1 + seg))
     if dtype is None:
         dtype = out.dtype if out is not None else base.dtype if base is not None else torch.bfloat16
     if dtype not in _DTYPES:
         raise ValueError("dtype must be float32 or bfloat16")
     shape = (B, H, Li, Lj)
+    given = (base, out)
     if out is None:
         out = _empty(shape, dtype, table, stream)
-    for t in (base, out):
-        if t is not None and (tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous()
+    for t in given:
+        if t is not None and (t.shape != shape or t.dtype != dtype or not t.is_contiguous()
                               or t.device != table.device):
             raise ValueError("base and out must be contiguous %s tensors of shape %s" % (dtype, shape))
-    d = evo_relpos_dims(_DTYPES[dtype], H, E, int(seg_i is not None), B, Li, Lj, 0)
-    st = lib.evo_relpos_fwd(ctypes.byref(d), _ptr(pos_i), _ptr(pos_j), _ptr(seg_i), _ptr(seg_j), _ptr(edges),
-                            _ptr(table), _ptr(base), _ptr(out), _stream(stream))
+    d = evo_relpos_dims(_DTYPES[dtype], H, E, seg, B, Li, Lj, 0)
+    st = lib.evo_relpos_fwd(d, pos_i.data_ptr(), pos_j.data_ptr(), _addr(seg_i), _addr(seg_j), edges.data_ptr(),
+                            table.data_ptr(), _addr(base), out.data_ptr(), _stream(stream))
     if st:
         raise EvoAttnError(st, "evo_relpos_fwd")
     return out
@@ -144,25 +147,26 @@ def relpos_bias_bwd(pos_i: torch.Tensor, pos_j: torch.Tensor, edges: torch.Tenso
     gradient dbias, which is the gradient of its base, too."""
     lib = _lib()
     B, Li, Lj, E = _index(pos_i, pos_j, edges, seg_i, seg_j, dbias)
-    if dbias.dim() != 4 or (dbias.shape[0], dbias.shape[2], dbias.shape[3]) != (B, Li, Lj) or dbias.shape[1] < 1 \
-            or dbias.dtype != torch.float32 or not dbias.is_contiguous():
+    H = dbias.shape[1] if dbias.dim() == 4 else 0
+    if dbias.shape != (B, H, Li, Lj) or H < 1 or dbias.dtype != torch.float32 or not dbias.is_contiguous():
         raise ValueError("dbias must be a contiguous float32 [%d, H, %d, %d] tensor" % (B, Li, Lj))
-    H = dbias.shape[1]
-    buckets = E + 1 + (seg_i is not None)
+    seg = 0 if seg_i is None else 1
+    shape = (H, E + 1 + seg)
     if dtable is None:
-        dtable = _empty((H, buckets), torch.float32, dbias, stream)
-    if tuple(dtable.shape) != (H, buckets) or dtable.dtype != torch.float32 or not dtable.is_contiguous() \
+        dtable = _empty(shape, torch.float32, dbias, stream)
+    elif dtable.shape != shape or dtable.dtype != torch.float32 or not dtable.is_contiguous() \
             or dtable.device != dbias.device:
-        raise ValueError("dtable must be a contiguous float32 [%d, %d] tensor" % (H, buckets))
-    d = evo_relpos_dims(EVO_DTYPE_F32, H, E, int(seg_i is not None), B, Li, Lj, 0)
+        raise ValueError("dtable must be a contiguous float32 [%d, %d] tensor" % shape)
+    d = evo_relpos_dims(EVO_DTYPE_F32, H, E, seg, B, Li, Lj, 0)
     if workspace is None:
-        need = int(lib.evo_relpos_bwd_workspace_size(ctypes.byref(d)))
-        workspace = _empty(max(need, 16), torch.uint8, dbias, stream)
+        need = ws_bytes = lib.evo_relpos_bwd_workspace_size(d)
+        workspace = _empty((need,), torch.uint8, dbias, stream)
     elif workspace.device != dbias.device or not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous and on the device of dbias")
-    st = lib.evo_relpos_bwd(ctypes.byref(d), _ptr(pos_i), _ptr(pos_j), _ptr(seg_i), _ptr(seg_j), _ptr(edges),
-                            _ptr(dbias), _ptr(dtable), _ptr(workspace),
-                            ctypes.c_size_t(workspace.numel() * workspace.element_size()), _stream(stream))
+    else:
+        ws_bytes = workspace.numel() * workspace.element_size()
+    st = lib.evo_relpos_bwd(d, pos_i.data_ptr(), pos_j.data_ptr(), _addr(seg_i), _addr(seg_j), edges.data_ptr(),
+                            dbias.data_ptr(), dtable.data_ptr(), workspace.data_ptr(), ws_bytes, _stream(stream))
     if st:
         raise EvoAttnError(st, "evo_relpos_bwd")
     return dtable
