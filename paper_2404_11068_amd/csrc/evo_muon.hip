@@ -268,6 +268,66 @@ __global__ __launch_bounds__(256) void ns_scale_kernel(NsWork w, NsParams p) {
     }
 }
 
+// ---- results
+
+// acc (a unit: lane = row, registers = columns, already the unit's scale) as packed quarters
+template <int PL>
+__device__ __forceinline__ void pack_unit(const f32x16 &acc, float f, half4 (&out)[4][PL]) {
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        float q[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) q[e] = acc[4 * g + e] * f;
+        split4<PL>(q, out[g]);
+    }
+}
+template <int PL>
+__device__ __forceinline__ void store_unit(char *unit, const half4 (&out)[4][PL], int n, int h) {
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int z = 0; z < PL; ++z) *(half4 *)(unit + z * kPlane + chunk(n, g & 1, g >> 1) + h * 8) = out[g][z];
+}
+
+// one unit's entries of the result, the lanes along the memory rows; before(): loads what the update needs
+template <bool MUON, bool BF16>
+struct Result {
+    float p[16], w[16];
+    __device__ __forceinline__ void before(const View &v, int iu, int ju, int h, int n) {
+        if constexpr (MUON) {
+            const int mr = (v.tr ? ju : iu) * 32 + 4 * h, mc = (v.tr ? iu : ju) * 32 + n;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int row = mr + 8 * (e >> 2) + (e & 3);
+                const bool ok = mc < v.m.cols && row < v.m.rows;
+                const int64_t at = ok ? (int64_t)row * v.m.cols + mc : 0;
+                p[e] = ((const float *)v.m.out)[at];
+                if (v.m.swa) w[e] = v.m.swa[at];
+            }
+        }
+    }
+    __device__ __forceinline__ void store(const View &v, const NsParams &P, const f32x16 &acc, int iu, int ju, int h, int n) {
+        const int mr = (v.tr ? ju : iu) * 32 + 4 * h, mc = (v.tr ? iu : ju) * 32 + n;
+        if (mc >= v.m.cols) return;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int row = mr + 8 * (e >> 2) + (e & 3);
+            if (row >= v.m.rows) continue;
+            const int64_t at = (int64_t)row * v.m.cols + mc;
+            const float o = acc[e] * kUnscale;
+            if constexpr (MUON) {
+                const float q = fmaf(-P.lr * v.m.scale, o, P.decay * p[e]);
+                ((float *)v.m.out)[at] = q;
+                if (v.m.swa) v.m.swa[at] = fmaf(P.sd, w[e], P.om_sd * q);
+            } else if constexpr (BF16) {
+                ((uint16_t *)v.m.out)[at] = f2bf(o);
+            } else {
+                ((float *)v.m.out)[at] = o;
+            }
+        }
+    }
+};
+
 // ---- products
 //
 // A workgroup of 4 waves forms a T x T tile, a wave a quarter of it, from units staged
@@ -278,6 +338,13 @@ __global__ __launch_bounds__(256) void ns_scale_kernel(NsWork w, NsParams p) {
 enum { kGram, kPoly, kApply, kLast };
 struct Yes { static constexpr bool value = true; };
 struct No { static constexpr bool value = false; };
+
+// a wave-uniform address, in scalar registers whatever the compiler makes of its terms
+__device__ __forceinline__ const char *scalar(const char *p) {
+    const uint64_t a = (uint64_t)p;
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)a), hi = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32));
+    return (const char *)(((uint64_t)hi << 32) | lo);
+}
 
 // 16 bytes per lane from base + off to LDS at lds + 16 lane.  In asm because the compiler would
 // wait for all copies in flight before every LDS read; nothing but the counter below waits for these.
@@ -343,7 +410,7 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, i
         for (int q = 0; q < U; ++q)
 #pragma unroll
             for (int e = 0; e < UNIT / 1024; ++e)
-                copy_to_lds(src[q] + k * step, (uint32_t)(e * 1024 + lane * 16), dst + q * UNIT + e * 1024);
+                copy_to_lds(scalar(src[q] + k * step), (uint32_t)(e * 1024 + lane * 16), dst + q * UNIT + e * 1024);
     };
 
     f32x16 acc[U][U];  // [row unit or, where the operands are swapped, ...]: see below
@@ -471,28 +538,260 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, i
         for (int a = 0; a < U; ++a)
 #pragma unroll
             for (int b = 0; b < U; ++b) {
-                const int iu = i0 + a, ju = j0 + b;
-                // memory row of register 0 and column of the lane
-                const int mr = (v.tr ? ju : iu) * 32 + 4 * h, mc = (v.tr ? iu : ju) * 32 + n;
-                if (mc >= v.m.cols) continue;
+                Result<MUON, BF16> res;
+                res.before(v, i0 + a, j0 + b, h, n);
+                res.store(v, p, acc[a][b], i0 + a, j0 + b, h, n);
+            }
+    }
+}
+
+// ---- matrices that fit into LDS: everything in one workgroup
+//
+// X and A (later P in its place) lie in LDS as units, R C + R R <= 39 of them
+// in pairs (128 x 160 entries, 64 x 544, 32 x 1184) and at most kSmallUnits of
+// X; a product's results wait in registers until every wave has read its
+// operands.  One launch does the norm, the steps and the update: memory sees
+// each entry once.  A wave takes units of the upper triangle (10 of 16 at 128
+// x 128) or pairs of units of X in turn.
+
+constexpr int kSmallUnits = 40;
+constexpr int kSmallLds = 39 * 2 * kPlane;
+constexpr int kSmallWaves = 8;
+
+template <int PL>
+__host__ __device__ inline bool fits_small(int R, int C) {
+    return R * ((C + 1) / 2) <= 3 * kSmallWaves && R * C <= kSmallUnits && (R * C + R * R) * PL * kPlane <= kSmallLds;
+}
+
+template <bool MUON, bool BF16, int PL>
+__global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, NsParams p, int first) {
+    constexpr int UNIT = PL * kPlane, THREADS = 64 * kSmallWaves;
+    constexpr int BLOCKS = kSmallUnits * 64 / THREADS;  // 4 x 4 blocks of a thread
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    __shared__ double red[kSmallWaves];
+    const View v = view_of<PL>(w, first + blockIdx.x);
+    const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, n = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int R = v.R, C = v.C;
+    char *const X = lds, *const A = lds + R * C * UNIT;
+
+    {  // X = u / max(|u|, eps)
+        const int per_row = 8 * (v.tr ? R : C), blocks = 64 * R * C;
+        float u[BLOCKS][4][4];
+        double s = 0.0;
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int row = mr + 8 * (e >> 2) + (e & 3);
-                    if (row >= v.m.rows) continue;
-                    const int64_t at = (int64_t)row * v.m.cols + mc;
-                    const float o = acc[a][b][e] * kUnscale;
-                    if constexpr (MUON) {
-                        float *prm = (float *)v.m.out;
-                        const float q = fmaf(-p.lr * v.m.scale, o, p.decay * prm[at]);
-                        prm[at] = q;
-                        if (v.m.swa) v.m.swa[at] = fmaf(p.sd, v.m.swa[at], p.om_sd * q);
-                    } else if constexpr (BF16) {
-                        ((uint16_t *)v.m.out)[at] = f2bf(o);
-                    } else {
-                        ((float *)v.m.out)[at] = o;
+        for (int q = 0; q < BLOCKS; ++q) {
+            const int k = q * THREADS + tid;
+            if (q * THREADS < blocks) {
+                const int br = k / per_row, bc = k - br * per_row;
+                load_block<MUON, BF16, true>(u[q], v, p, br * 4, bc * 4);
+#pragma unroll
+                for (int a = 0; a < 4; ++a)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s += (double)u[q][a][e] * u[q][a][e];
+            }
+        }
+#pragma unroll
+        for (int m = 32; m >= 1; m >>= 1) s += __shfl_xor(s, m, 64);
+        if (lane == 0) red[wave] = s;
+        __syncthreads();
+        s = red[0];
+#pragma unroll
+        for (int k = 1; k < kSmallWaves; ++k) s += red[k];
+        const double norm = sqrt(s), f = (double)kScale / (norm < p.eps ? p.eps : norm);
+#pragma unroll
+        for (int q = 0; q < BLOCKS; ++q) {
+            const int k = q * THREADS + tid;
+            if (k < blocks) {
+                const int br = k / per_row, bc = k - br * per_row;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const int i = v.tr ? bc * 4 + x : br * 4 + x, j = v.tr ? br * 4 : bc * 4;
+                    float y4[4];
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) y4[y] = (float)((double)(v.tr ? u[q][y][x] : u[q][x][y]) * f);
+                    half4 hh[PL];
+                    split4<PL>(y4, hh);
+                    const int kk = j & 31, at = chunk(i & 31, (kk >> 3) & 1, kk >> 4) + (kk & 4) * 2;
+                    char *unit = X + ((i >> 5) * C + (j >> 5)) * UNIT;
+#pragma unroll
+                    for (int z = 0; z < PL; ++z) *(half4 *)(unit + z * kPlane + at) = hh[z];
+                }
+            }
+        }
+        __syncthreads();
+    }
+
+    // rows of units `a` times rows `b` of M (K units each), summed into acc by parts
+    auto rows_by_rows = [&](const char *M, int K, int a, int b) {
+        f32x16 acc[PL == 2 ? 3 : 1];
+#pragma unroll
+        for (auto &x : acc)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[e] = 0.0f;
+        for (int k = 0; k < K; ++k) {
+            const char *ua = M + (a * K + k) * UNIT, *ub = M + (b * K + k) * UNIT;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const half8 fa = frag_rows(ua, lane, s), fb = frag_rows(ub, lane, s);
+                acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa, fb, acc[0], 0, 0, 0);
+                if constexpr (PL == 2) {
+                    const half8 la = frag_rows(ua + kPlane, lane, s), lb = frag_rows(ub + kPlane, lane, s);
+                    acc[1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa, lb, acc[1], 0, 0, 0);
+                    acc[2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(la, fb, acc[2], 0, 0, 0);
+                }
+            }
+        }
+        if constexpr (PL == 2) acc[0] += acc[1] + acc[2];
+        return acc[0];
+    };
+    const int tri = R * (R + 1) / 2;
+    auto unit_of = [&](int t, int &a, int &b) {  // t-th unit of the upper triangle
+        a = 0;
+        while (t >= R - a) {
+            t -= R - a;
+            ++a;
+        }
+        b = a + t;
+    };
+    // a unit of a symmetric matrix, lane = row b, registers = columns a, and its mirror
+    auto store_pair = [&](const half4 (&out)[4][PL], int a, int b) {
+        char *const at = A + (b * R + a) * UNIT;
+        store_unit<PL>(at, out, n, h);
+        if (a == b) return;
+        __builtin_amdgcn_wave_barrier();
+        char *const mirror = A + (a * R + b) * UNIT;
+#pragma unroll
+        for (int z = 0; z < PL; ++z)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) *(half8 *)(mirror + z * kPlane + chunk(n, h, s)) = frag_cols(at + z * kPlane, lane, s);
+    };
+
+    constexpr int TRI = PL == 2 ? 2 : 3;  // units of a wave: R <= 4 in pairs of planes, R <= 6 in one
+    constexpr int PAIRS = 3;              // pairs of a wave: R ceil(C / 2) <= 20 for R C <= 40, R <= C (checked below)
+    const int half_c = (C + 1) / 2, pairs = R * half_c;
+    // pair t of units of P X: row a, columns b0 and b1 (b0 again where there is one)
+    auto pair_of = [&](int t, int &a, int &b0, int &b1) {
+        a = t / half_c;
+        b0 = (t - a * half_c) * 2;
+        b1 = b0 + 1 < C ? b0 + 1 : b0;
+    };
+    // along: lane = column of the iterate, otherwise its row
+    auto product = [&](f32x16 (&acc)[2], int a, int b0, int b1, bool along) {
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[y][e] = 0.0f;
+        for (int k = 0; k < R; ++k) {
+            const char *up = A + (a * R + k) * UNIT, *u0 = X + (k * C + b0) * UNIT, *u1 = X + (k * C + b1) * UNIT;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                Frag<PL> fp, f0, f1;
+#pragma unroll
+                for (int z = 0; z < PL; ++z) {
+                    fp.p[z] = frag_rows(up + z * kPlane, lane, s);
+                    f0.p[z] = frag_cols(u0 + z * kPlane, lane, s);
+                    f1.p[z] = frag_cols(u1 + z * kPlane, lane, s);
+                }
+                if (along) {
+                    mma<PL>(acc[0], fp, f0);
+                    mma<PL>(acc[1], fp, f1);
+                } else {
+                    mma<PL>(acc[0], f0, fp);
+                    mma<PL>(acc[1], f1, fp);
+                }
+            }
+        }
+    };
+    for (int step = 0; step < p.steps; ++step) {
+        for (int t = wave; t < tri; t += kSmallWaves) {
+            int a, b;
+            unit_of(t, a, b);
+            half4 out[4][PL];
+            pack_unit<PL>(rows_by_rows(X, C, a, b), kUnscale * kScale, out);
+            store_pair(out, a, b);
+        }
+        __syncthreads();
+        {
+            half4 out[TRI][4][PL];
+#pragma unroll
+            for (int x = 0; x < TRI; ++x) {
+                const int t = wave + x * kSmallWaves;
+                if (t < tri) {
+                    int a, b;
+                    unit_of(t, a, b);
+                    const f32x16 acc = rows_by_rows(A, R, a, b);
+                    const char *at = A + (b * R + a) * UNIT;
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        float q[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) q[e] = 0.0f;
+#pragma unroll
+                        for (int z = PL - 1; z >= 0; --z) {
+                            const half4 o = *(const half4 *)(at + z * kPlane + chunk(n, g & 1, g >> 1) + h * 8);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) q[e] += (float)o[e];
+                        }
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            q[e] = fmaf(p.c, acc[4 * g + e] * (kUnscale * kScale), p.b * q[e]);
+                            if (a == b && 8 * g + 4 * h + e == n) q[e] = fmaf(p.a, kScale, q[e]);
+                        }
+                        split4<PL>(q, out[x][g]);
                     }
                 }
             }
+            __syncthreads();
+#pragma unroll
+            for (int x = 0; x < TRI; ++x) {
+                const int t = wave + x * kSmallWaves;
+                if (t < tri) {
+                    int a, b;
+                    unit_of(t, a, b);
+                    store_pair(out[x], a, b);
+                }
+            }
+            __syncthreads();
+        }
+        if (step + 1 == p.steps) break;
+        half4 out[PAIRS][2][4][PL];
+#pragma unroll
+        for (int x = 0; x < PAIRS; ++x) {
+            const int t = wave + x * kSmallWaves;
+            if (t < pairs) {
+                int a, b0, b1;
+                pair_of(t, a, b0, b1);
+                f32x16 acc[2];
+                product(acc, a, b0, b1, false);
+#pragma unroll
+                for (int y = 0; y < 2; ++y) pack_unit<PL>(acc[y], kUnscale * kScale, out[x][y]);
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int x = 0; x < PAIRS; ++x) {
+            const int t = wave + x * kSmallWaves;
+            if (t < pairs) {
+                int a, b0, b1;
+                pair_of(t, a, b0, b1);
+                store_unit<PL>(X + (a * C + b0) * UNIT, out[x][0], n, h);
+                if (b1 != b0) store_unit<PL>(X + (a * C + b1) * UNIT, out[x][1], n, h);
+            }
+        }
+        __syncthreads();
+    }
+    // the last step: the lanes go along the matrix's memory rows
+    for (int t = wave; t < pairs; t += kSmallWaves) {
+        int a, b0, b1;
+        pair_of(t, a, b0, b1);
+        Result<MUON, BF16> r0, r1;
+        r0.before(v, a, b0, h, n);
+        r1.before(v, a, b1, h, n);
+        f32x16 acc[2];
+        product(acc, a, b0, b1, !v.tr);
+        r0.store(v, p, acc[0], a, b0, h, n);
+        if (b1 != b0) r1.store(v, p, acc[1], a, b1, h, n);
     }
 }
 
@@ -515,6 +814,13 @@ hipError_t launch_product(NsWork w, const NsTile *tiles, int64_t grid, const NsP
 template <int T, bool MUON, bool BF16>
 hipError_t launch_all(NsWork w, const NsLists &l, const NsParams &p, hipStream_t s) {
     constexpr int PL = BF16 ? 1 : 2;
+    if (l.n_small > 0) {
+        hipLaunchKernelGGL((ns_small_kernel<MUON, BF16, PL>), dim3((unsigned)l.n_small), dim3(64 * kSmallWaves), l.small_lds, s, w,
+                           p, (int)l.first_small);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (l.n_x == 0) return hipSuccess;
     NsWork wx = w;
     const int r = w.uni.rows < w.uni.cols ? w.uni.rows : w.uni.cols, c = w.uni.rows + w.uni.cols - r;
     wx.tiles = l.x;
@@ -544,6 +850,13 @@ int64_t ns_matrix_bytes(int64_t rows, int64_t cols, int planes) {
     const int64_t r = rows < cols ? rows : cols, c = rows + cols - r;
     const int64_t R = (r + 31) / 32, C = (c + 31) / 32;
     return 2 * (R * C + R * R) * planes * kPlane;
+}
+
+int64_t ns_small_bytes(int64_t rows, int64_t cols, int planes) {
+    const int r = (int)(rows < cols ? rows : cols), c = (int)(rows + cols - r);
+    const int R = units(r), C = units(c);
+    const bool fits = planes == 2 ? fits_small<2>(R, C) : fits_small<1>(R, C);
+    return fits ? (int64_t)(R * C + R * R) * planes * kPlane : 0;
 }
 
 // 128 x 128 tiles read each staged unit twice as often; once they do not fill

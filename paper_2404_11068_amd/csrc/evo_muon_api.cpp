@@ -50,6 +50,7 @@ int check_coefs(double a, double b, double c, double eps, int steps) {
 struct PlanHeader {
     uint64_t magic;
     int64_t bytes, n_mats, ws_bytes, part_bytes;
+    int64_t n_small, small_lds;          // the last matrices, by themselves in a workgroup each
     int64_t tile, n_x, n_gram, n_apply;  // entries of the lists, padding included
     int64_t off_mats, off_x, off_gram, off_apply;
 };
@@ -123,12 +124,23 @@ bool make_plan(const evo_muon_tensor *t, int32_t n, Plan &p) {
         if (t[i].rows == 0 || t[i].cols == 0) continue;
         const Size z = size_of(t[i]);
         order.push_back(i);
+        const int64_t lds = evo::ns_small_bytes(t[i].rows, t[i].cols, 2);
+        if (lds > 0) {
+            ++h.n_small;
+            h.small_lds = lds > h.small_lds ? lds : h.small_lds;
+            continue;
+        }
         tiles128 += tiles_of(z.r, 128) * tiles_of(z.c, 128);
         blocks += blocks_of(z.r, z.c);
         total += cost(i);
         if (blocks > 0x3fffffff) return false;
     }
-    std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return cost(a) > cost(b); });
+    // those that fit into a workgroup's LDS last; the others and they by falling cost
+    auto small = [&](int32_t i) { return evo::ns_small_bytes(t[i].rows, t[i].cols, 2) > 0; };
+    std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) {
+        const bool sa = small(a), sb = small(b);
+        return sa != sb ? sb : cost(a) > cost(b);
+    });
     h.magic = kMagic;
     h.tile = evo::ns_tile(tiles128);
     h.n_mats = (int64_t)order.size();
@@ -147,6 +159,10 @@ bool make_plan(const evo_muon_tensor *t, int32_t n, Plan &p) {
         M.rows = (int32_t)s.rows;
         M.cols = (int32_t)s.cols;
         M.scale = (float)s.update_scale;
+        if (m >= (int32_t)order.size() - h.n_small) {
+            p.mats.push_back(M);
+            continue;
+        }
         M.part0 = (int32_t)part;
         M.off = off;
         part += blocks_of(z.r, z.c);
@@ -165,6 +181,7 @@ bool make_plan(const evo_muon_tensor *t, int32_t n, Plan &p) {
         each_tile(z.r, z.c, h.tile, [&](int32_t i, int32_t j) { p.apply.add(xcd, NsTile{m, i, j}); });
     }
     h.ws_bytes += off;
+    if (h.n_mats > 0 && h.ws_bytes < 256) h.ws_bytes = 256;  // (a size of 0 means that there is nothing to do)
     h.n_x = p.x.total();
     h.n_gram = p.gram.total();
     h.n_apply = p.apply.total();
@@ -188,7 +205,9 @@ int check_orth(const evo_orth_dims *d) {
 
 bool orth_empty(const evo_orth_dims *d) { return d->n_batch == 0 || d->rows == 0 || d->cols == 0; }
 
+// a stack that fits into the workgroups' LDS still asks for a little, so that a size of 0 means a refusal
 size_t orth_workspace(const evo_orth_dims *d) {
+    if (evo::ns_small_bytes(d->rows, d->cols, d->dtype == EVO_DTYPE_BF16 ? 1 : 2) > 0) return 256;
     return (size_t)(round256(d->n_batch * blocks_of(d->rows, d->cols) * 8) +
                     d->n_batch * evo::ns_matrix_bytes(d->rows, d->cols, d->dtype == EVO_DTYPE_BF16 ? 1 : 2));
 }
@@ -239,19 +258,25 @@ int evo_orthogonalize(const evo_orth_dims *d, const void *x, void *out, void *wo
     w.n_mats = (int32_t)n;
     w.part = (double *)workspace;
     w.ws = (char *)workspace + round256(n * blocks_of(r, c) * 8);
-    NsLists l{};
-    l.tile = evo::ns_tile(n * tiles_of(r, 128) * tiles_of(c, 128));
-    // eight matrices or more are dealt to the XCDs, so their number is rounded up
-    const int64_t slots = n >= 8 ? (n + 7) / 8 * 8 : n, g = tiles_of(r, l.tile);
-    l.n_x = slots * blocks_of(r, c);
-    l.n_gram = slots * (g * (g + 1) / 2);
-    l.n_apply = slots * g * tiles_of(c, l.tile);
     evo::NsParams p{};
     p.a = (float)d->a;
     p.b = (float)d->b;
     p.c = (float)d->c;
     p.eps = d->eps;
     p.steps = d->steps;
+    NsLists l{};
+    l.small_lds = evo::ns_small_bytes(d->rows, d->cols, bf16 ? 1 : 2);
+    if (l.small_lds > 0) {
+        l.n_small = n;
+        l.tile = 64;
+        return evo::launch_ns(w, l, p, false, bf16, (hipStream_t)stream) == hipSuccess ? EVO_OK : EVO_ERR_HIP;
+    }
+    l.tile = evo::ns_tile(n * tiles_of(r, 128) * tiles_of(c, 128));
+    // eight matrices or more are dealt to the XCDs, so their number is rounded up
+    const int64_t slots = n >= 8 ? (n + 7) / 8 * 8 : n, g = tiles_of(r, l.tile);
+    l.n_x = slots * blocks_of(r, c);
+    l.n_gram = slots * (g * (g + 1) / 2);
+    l.n_apply = slots * g * tiles_of(c, l.tile);
     return evo::launch_ns(w, l, p, false, bf16, (hipStream_t)stream) == hipSuccess ? EVO_OK : EVO_ERR_HIP;
 }
 
@@ -338,6 +363,9 @@ int evo_muon_step(const evo_muon_hparams *hp, const void *plan, const void *plan
     p.om_sd = (float)(1.0 - hp->swa_decay);
     p.grad_scale = grad_scale;
     NsLists l{};
+    l.n_small = h.n_small;
+    l.first_small = h.n_mats - h.n_small;
+    l.small_lds = h.small_lds;
     l.tile = (int)h.tile;
     l.n_x = h.n_x;
     l.n_gram = h.n_gram;

@@ -43,9 +43,11 @@ struct NsParams {
     const float *grad_scale;
 };
 
-// work lists, each a launch's grid: every matrix by tiles of 64 x 64 entries (norm, scaling), and
+// Matrices n_small of them from first_small on fit into a workgroup's LDS (small_lds bytes)
+// and take one launch.  Work lists for the others, each a launch's grid: every matrix by tiles of 64 x 64 entries (norm, scaling), and
 // the products' tiles of `tile` x `tile`: the Gram matrix's upper triangle, and the iterate
 struct NsLists {
+    int64_t n_small, first_small, small_lds;
     int tile;                         // 64 or 128
     int64_t n_x, n_gram, n_apply;     // entries, padding included
     const NsTile *x, *gram, *apply;   // device tables, or null for a stack
@@ -53,7 +55,9 @@ struct NsLists {
 
 constexpr int kNsBlock = 64;  // tiles of the norm and scaling passes
 
-// bytes of a matrix's buffers in the workspace; planes: 2 for fp32, 1 for bf16
+// LDS that a matrix takes as a whole, 0 if it does not fit; planes: 2 for fp32, 1 for bf16
+int64_t ns_small_bytes(int64_t rows, int64_t cols, int planes);
+// bytes of a matrix's buffers in the workspace where it does not fit
 int64_t ns_matrix_bytes(int64_t rows, int64_t cols, int planes);
 // tiles of the products for a call whose iterates have this many 128 x 128 tiles
 int ns_tile(int64_t tiles128);
