@@ -10,8 +10,8 @@
 // too) at a third of the fp16 rate, which is five times the fp32 matrix rate.
 // bf16 matrices take one fp16 plane: an iterate rounded to 2^-11 costs 2e-3 of
 // the result, about its own rounding to bf16 (with bf16 iterates it would be
-// 1e-2, and all of it for low-rank inputs).  Iterates are stored times 2^10:
-// their entries stay below 8 (coefficients that could take them further
+// 1e-2, and all of it for low-rank inputs).  X and A are stored times 2^10:
+// their entries stay below 64 (coefficients that could take them further
 // are refused), and those near 1 / sqrt(m n) stay clear of fp16's subnormals.
 //
 // Layout.  Iterates lie in the workspace as units of 32 x 32 entries, 2 KB per
@@ -29,8 +29,8 @@ namespace {
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 
-constexpr float kScale = 1024.0f;                  // iterates are stored times this
-constexpr float kUnscale = 1.0f / (1024.0f * 1024.0f);  // of a product of two
+constexpr float kScale = 1024.0f;        // X and A are stored times this, P as it is: P X needs no scaling
+constexpr float kUnscale = 1.0f / 1024.0f;
 constexpr int kPlane = 2048;                       // bytes of a unit's plane
 
 __host__ __device__ inline int units(int n) { return (n + 31) / 32; }
@@ -119,14 +119,23 @@ __device__ __forceinline__ half8 frag_cols(const char *plane, int lane, int s) {
     return __builtin_bit_cast(half8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// a value (already scaled) as one fp16, or as two that sum up to it within 22 bits
+// Four values f v as fp16, or as two fp16 each that sum up to them within 22 bits.  Conversions
+// two at a time, the remainder in one mixed fused multiply-add: 3 operations per value
+typedef float float2v __attribute__((ext_vector_type(2)));
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 template <int PL>
-__device__ __forceinline__ void split4(const float (&v)[4], half4 (&p)[PL]) {
+__device__ __forceinline__ void split4(const float (&v)[4], float f, half4 (&p)[PL]) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const _Float16 hi = (_Float16)v[e];
-        p[0][e] = hi;
-        if constexpr (PL == 2) p[1][e] = (_Float16)(v[e] - (float)hi);
+    for (int e = 0; e < 4; e += 2) {
+        const half2v hi = __builtin_convertvector((float2v{v[e] * f, v[e + 1] * f}), half2v);
+        p[0][e] = hi.x;
+        p[0][e + 1] = hi.y;
+        if constexpr (PL == 2) {
+            const half2v lo =
+                __builtin_convertvector((float2v{fmaf(v[e], f, -(float)hi.x), fmaf(v[e + 1], f, -(float)hi.y)}), half2v);
+            p[1][e] = lo.x;
+            p[1][e + 1] = lo.y;
+        }
     }
 }
 
@@ -203,6 +212,26 @@ __device__ __forceinline__ void load_block(float (&u)[4][4], const View &v, cons
     }
 }
 
+// the thread's entries times f into the units of X
+template <int PL>
+__device__ __forceinline__ void pack_block(const float (&u)[4][4], const View &v, int row0, int col0, double f) {
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+        // row i of the iterate, columns j .. j + 3
+        const int i = v.tr ? col0 + x : row0 + x, j = v.tr ? row0 : col0;
+        if ((i >> 5) >= v.R || (j >> 5) >= v.C) continue;
+        float q[4];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) q[y] = (float)((double)(v.tr ? u[y][x] : u[x][y]) * f);
+        half4 hh[PL];
+        split4<PL>(q, 1.0f, hh);
+        char *unit = v.x0 + ((int64_t)(i >> 5) * v.C + (j >> 5)) * (PL * kPlane);
+        const int k = j & 31, at = chunk(i & 31, (k >> 3) & 1, k >> 4) + (k & 4) * 2;
+#pragma unroll
+        for (int z = 0; z < PL; ++z) *(half4 *)(unit + z * kPlane + at) = hh[z];
+    }
+}
+
 // momentum, and the sum of squares of each tile (fp64: no overflow or underflow of fp32 squares)
 template <bool MUON, bool BF16, int PL>
 __global__ __launch_bounds__(256) void ns_norm_kernel(NsWork w, NsParams p) {
@@ -251,34 +280,33 @@ __global__ __launch_bounds__(256) void ns_scale_kernel(NsWork w, NsParams p) {
     __syncthreads();
     const double norm = sqrt(((red[0] + red[1]) + red[2]) + red[3]);
     const double f = (double)kScale / (norm < p.eps ? p.eps : norm);
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-        // row i of the iterate, columns j .. j + 3
-        const int i = v.tr ? col0 + x : row0 + x, j = v.tr ? row0 : col0;
-        if ((i >> 5) >= v.R || (j >> 5) >= v.C) continue;
-        float q[4];
-#pragma unroll
-        for (int y = 0; y < 4; ++y) q[y] = (float)((double)(v.tr ? u[y][x] : u[x][y]) * f);
-        half4 h[PL];
-        split4<PL>(q, h);
-        char *unit = v.x0 + ((int64_t)(i >> 5) * v.C + (j >> 5)) * (PL * kPlane);
-        const int k = j & 31, at = chunk(i & 31, (k >> 3) & 1, k >> 4) + (k & 4) * 2;
-#pragma unroll
-        for (int q2 = 0; q2 < PL; ++q2) *(half4 *)(unit + q2 * kPlane + at) = h[q2];
-    }
+    pack_block<PL>(u, v, row0, col0, f);
 }
 
 // ---- results
 
-// acc (a unit: lane = row, registers = columns, already the unit's scale) as packed quarters
+// entries of P = a I + b A + c A A from those of the product (scale 2^20) and of A (2^10);
+// diagonal: which of the four lies on it, if any
+template <int PL>
+__device__ __forceinline__ void poly4(float (&q)[4], const half4 (&old)[PL], const NsParams &p, int diagonal) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        float o = (float)old[0][e];
+        if constexpr (PL == 2) o += (float)old[1][e];
+        q[e] = fmaf(p.c * (kUnscale * kUnscale), q[e], p.b * kUnscale * o);
+        q[e] += e == diagonal ? p.a : 0.0f;
+    }
+}
+
+// acc (a unit: lane = row, registers = columns) times f as packed quarters
 template <int PL>
 __device__ __forceinline__ void pack_unit(const f32x16 &acc, float f, half4 (&out)[4][PL]) {
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
         float q[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) q[e] = acc[4 * g + e] * f;
-        split4<PL>(q, out[g]);
+        for (int e = 0; e < 4; ++e) q[e] = acc[4 * g + e];
+        split4<PL>(q, f, out[g]);
     }
 }
 template <int PL>
@@ -475,20 +503,14 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, i
                     const int pos = chunk(n, g & 1, g >> 1) + h * 8;
                     float q[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) q[e] = acc[a][b][4 * g + e] * (kUnscale * kScale);
+                    for (int e = 0; e < 4; ++e) q[e] = acc[a][b][4 * g + e];
                     if constexpr (KIND == kPoly) {
                         half4 old[PL];
 #pragma unroll
                         for (int z = 0; z < PL; ++z) old[z] = *(const half4 *)(v.A + at + z * kPlane + pos);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            float o = (float)old[0][e];
-                            if constexpr (PL == 2) o += (float)old[1][e];
-                            q[e] = fmaf(p.c, q[e], p.b * o);
-                            if (i == j && 8 * g + 4 * h + e == n) q[e] = fmaf(p.a, kScale, q[e]);
-                        }
+                        poly4<PL>(q, old, p, i == j ? n - 8 * g - 4 * h : -1);
                     }
-                    split4<PL>(q, out[g]);
+                    split4<PL>(q, KIND == kPoly ? 1.0f : kUnscale, out[g]);
 #pragma unroll
                     for (int z = 0; z < PL; ++z) *(half4 *)(dst + at + z * kPlane + pos) = out[g][z];
                 }
@@ -522,9 +544,9 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, i
                 for (int g = 0; g < 4; ++g) {
                     float q[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) q[e] = acc[a][b][4 * g + e] * (kUnscale * kScale);
+                    for (int e = 0; e < 4; ++e) q[e] = acc[a][b][4 * g + e];
                     half4 out[PL];
-                    split4<PL>(q, out);
+                    split4<PL>(q, 1.0f, out);
 #pragma unroll
                     for (int z = 0; z < PL; ++z)
                         *(half4 *)(unit + z * kPlane + chunk(n, g & 1, g >> 1) + h * 8) = out[z];
@@ -611,7 +633,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
 #pragma unroll
                     for (int y = 0; y < 4; ++y) y4[y] = (float)((double)(v.tr ? u[q][y][x] : u[q][x][y]) * f);
                     half4 hh[PL];
-                    split4<PL>(y4, hh);
+                    split4<PL>(y4, 1.0f, hh);
                     const int kk = j & 31, at = chunk(i & 31, (kk >> 3) & 1, kk >> 4) + (kk & 4) * 2;
                     char *unit = X + ((i >> 5) * C + (j >> 5)) * UNIT;
 #pragma unroll
@@ -708,7 +730,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
             int a, b;
             unit_of(t, a, b);
             half4 out[4][PL];
-            pack_unit<PL>(rows_by_rows(X, C, a, b), kUnscale * kScale, out);
+            pack_unit<PL>(rows_by_rows(X, C, a, b), kUnscale, out);
             store_pair(out, a, b);
         }
         __syncthreads();
@@ -726,19 +748,13 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
                     for (int g = 0; g < 4; ++g) {
                         float q[4];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) q[e] = 0.0f;
+                        for (int e = 0; e < 4; ++e) q[e] = acc[4 * g + e];
+                        half4 old[PL];
 #pragma unroll
-                        for (int z = PL - 1; z >= 0; --z) {
-                            const half4 o = *(const half4 *)(at + z * kPlane + chunk(n, g & 1, g >> 1) + h * 8);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) q[e] += (float)o[e];
-                        }
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            q[e] = fmaf(p.c, acc[4 * g + e] * (kUnscale * kScale), p.b * q[e]);
-                            if (a == b && 8 * g + 4 * h + e == n) q[e] = fmaf(p.a, kScale, q[e]);
-                        }
-                        split4<PL>(q, out[x][g]);
+                        for (int z = 0; z < PL; ++z)
+                            old[z] = *(const half4 *)(at + z * kPlane + chunk(n, g & 1, g >> 1) + h * 8);
+                        poly4<PL>(q, old, p, a == b ? n - 8 * g - 4 * h : -1);
+                        split4<PL>(q, 1.0f, out[x][g]);
                     }
                 }
             }
@@ -765,7 +781,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
                 f32x16 acc[2];
                 product(acc, a, b0, b1, false);
 #pragma unroll
-                for (int y = 0; y < 2; ++y) pack_unit<PL>(acc[y], kUnscale * kScale, out[x][y]);
+                for (int y = 0; y < 2; ++y) pack_unit<PL>(acc[y], 1.0f, out[x][y]);
             }
         }
         __syncthreads();
@@ -795,6 +811,279 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
     }
 }
 
+// ---- matrices of up to 256 rows, one workgroup each
+//
+// A workgroup of eight waves takes a matrix through all steps: the Gram
+// matrix and P lie in one buffer of the workspace, X in another and is updated
+// in place, block of 256 columns by block, because P X needs only those columns;
+// what one wave writes the others read after a barrier, all in the CU's own
+// caches.  Against the tiles above it saves 16 launches with their tails and
+// most of the traffic, a stage of the Gram matrix is one operand instead of
+// two, and a wave's 64 x 128 entries (RB = 8: up to 256 rows) take two thirds
+// of the LDS reads.  It takes a call with enough matrices for the CUs: a single
+// one is done sooner by tiles on all of them.
+
+constexpr int kWgWaves = 8;
+
+template <int RB, int PL, bool MUON, bool BF16>
+struct MatrixWg {
+    static constexpr int UNIT = PL * kPlane;
+    static constexpr int WA = RB == 8 ? 2 : 1, WB = RB == 8 ? 4 : 2;  // of the symmetric products
+    static constexpr int BU = RB == 8 ? 4 : 2;                        // of P X: 2 x BU units
+    static constexpr int SQ_STAGE = RB * UNIT, SQ_STAGES = 4;
+    static constexpr int AP_STAGE = (RB + 8) * UNIT;                  // two stages
+    static constexpr int LDS = 2 * AP_STAGE > SQ_STAGES * SQ_STAGE ? 2 * AP_STAGE : SQ_STAGES * SQ_STAGE;
+
+    const NsParams &p;
+    const View &v;
+    char *lds;
+    uint32_t lds0;
+    int lane, wave, h, n;
+
+    __device__ __forceinline__ void copy_unit(const char *src, uint32_t dst) const {
+#pragma unroll
+        for (int e = 0; e < UNIT / 1024; ++e)
+            copy_to_lds(scalar(src), (uint32_t)(e * 1024 + lane * 16), dst + e * 1024);
+    }
+
+    // M M^T for the wave's units (i0 + a, j0 + b), b >= a + D; M: K units per row.  Poly: the matrix is then
+    // P = a I + b M + c M M, in M's place, otherwise it goes to A
+    template <int D, bool POLY>
+    __device__ __forceinline__ void square(const char *M, int K, int i0, int j0) const {
+        f32x16 acc[WA][WB];
+#pragma unroll
+        for (int a = 0; a < WA; ++a)
+#pragma unroll
+            for (int b = 0; b < WB; ++b)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[a][b][e] = 0.0f;
+        const char *src = M + (int64_t)wave * K * UNIT;  // this wave copies unit row `wave`
+        const bool copies = wave < v.R;
+        auto copy = [&](int k) {
+            if (copies) copy_unit(src + (int64_t)k * UNIT, lds0 + (uint32_t)(k % SQ_STAGES) * SQ_STAGE + wave * UNIT);
+        };
+#pragma unroll
+        for (int k = 0; k < SQ_STAGES - 1; ++k)
+            if (k < K) copy(k);
+        for (int k = 0; k < K; ++k) {
+            if (k + SQ_STAGES - 2 < K) wait_copies_and_barrier<(SQ_STAGES - 2) * (UNIT / 1024)>();
+            else wait_copies_and_barrier<0>();
+            if (k + SQ_STAGES - 1 < K) copy(k + SQ_STAGES - 1);
+            const char *stage = lds + (k % SQ_STAGES) * SQ_STAGE;
+            if constexpr (D < WB) {
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    Frag<PL> fa[WA], fb[WB];
+#pragma unroll
+                    for (int a = 0; a < WA; ++a)
+#pragma unroll
+                        for (int z = 0; z < PL; ++z) fa[a].p[z] = frag_rows(stage + (i0 + a) * UNIT + z * kPlane, lane, s);
+#pragma unroll
+                    for (int b = D > 0 ? D : 0; b < WB; ++b)
+#pragma unroll
+                        for (int z = 0; z < PL; ++z) fb[b].p[z] = frag_rows(stage + (j0 + b) * UNIT + z * kPlane, lane, s);
+#pragma unroll
+                    for (int a = 0; a < WA; ++a)
+#pragma unroll
+                        for (int b = 0; b < WB; ++b)
+                            if (b >= a + D) mma<PL>(acc[a][b], fa[a], fb[b]);
+                    __builtin_amdgcn_sched_barrier(0);  // (both halves' operands at once do not fit the registers)
+                }
+            }
+        }
+        wait_copies_and_barrier<0>();  // every wave is past its last stage: LDS is scratch, M may be overwritten
+        if constexpr (D < WB) {
+            char *const scratch = lds + wave * UNIT;
+#pragma unroll
+            for (int a = 0; a < WA; ++a)
+#pragma unroll
+                for (int b = 0; b < WB; ++b) {
+                    const int i = i0 + a, j = j0 + b;
+                    if (b < a + D || i >= v.R || j >= v.R) continue;
+                    char *const at = v.A + ((int64_t)j * v.R + i) * UNIT;
+                    half4 out[4][PL];
+                    if constexpr (POLY) {
+                        half4 old[4][PL];
+#pragma unroll
+                        for (int g = 0; g < 4; ++g)
+#pragma unroll
+                            for (int z = 0; z < PL; ++z)
+                                old[g][z] = *(const half4 *)(at + z * kPlane + chunk(n, g & 1, g >> 1) + h * 8);
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) {
+                            float q[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) q[e] = acc[a][b][4 * g + e];
+                            poly4<PL>(q, old[g], p, i == j ? n - 8 * g - 4 * h : -1);
+                            split4<PL>(q, 1.0f, out[g]);
+                        }
+                    } else {
+                        pack_unit<PL>(acc[a][b], kUnscale, out);
+                    }
+                    store_unit<PL>(at, out, n, h);
+                    if (i != j) {
+                        store_unit<PL>(scratch, out, n, h);
+                        __builtin_amdgcn_wave_barrier();
+                        char *const mirror = v.A + ((int64_t)i * v.R + j) * UNIT;
+#pragma unroll
+                        for (int z = 0; z < PL; ++z)
+#pragma unroll
+                            for (int s = 0; s < 2; ++s)
+                                *(half8 *)(mirror + z * kPlane + chunk(n, h, s)) = frag_cols(scratch + z * kPlane, lane, s);
+                        __builtin_amdgcn_wave_barrier();
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+        }
+        wait_copies_and_barrier<0>();  // the stores are done, too
+    }
+
+    template <bool POLY>
+    __device__ __forceinline__ void squares(const char *M, int K) const {
+        // units (i0, j0) of the waves, those at or above the diagonal shared out so that no SIMD (wave % 4)
+        // has more than 10 of 36, or 3 of 10
+        int i0, j0;
+        if constexpr (RB == 8) {
+            const int ri[8] = {0, 2, 0, 4, 4, 6, 2, 6}, rj[8] = {4, 4, 0, 4, 0, 0, 0, 4};
+            i0 = ri[wave];
+            j0 = rj[wave];
+        } else {
+            const int ri[8] = {0, 0, 1, 2, 1, 3, 2, 3}, rj[8] = {0, 2, 2, 2, 0, 2, 0, 0};
+            i0 = ri[wave];
+            j0 = rj[wave];
+        }
+        const int d = i0 - j0;
+        if (d < 0 || (RB == 4 && d == 0)) square<RB == 8 ? -8 : 0, POLY>(M, K, i0, j0);
+        else if (d == 0) square<0, POLY>(M, K, i0, j0);
+        else if (d < WB) square<RB == 8 ? 2 : 1, POLY>(M, K, i0, j0);
+        else square<8, POLY>(M, K, i0, j0);
+    }
+
+    // X = P X in place, or (LAST) the result; ALONG: lane = column of the iterate, otherwise its row
+    template <bool LAST, bool ALONG>
+    __device__ __forceinline__ void apply() const {
+        const int i0 = RB == 8 ? 2 * (wave >> 1) : 2 * (wave >> 2), j1 = RB == 8 ? 4 * (wave & 1) : 2 * (wave & 3);
+        const int K = v.R;
+        for (int J = 0; J < v.C; J += 8) {
+            const char *up = v.P + (int64_t)wave * v.R * UNIT, *ux = v.x0 + (int64_t)(J + wave) * UNIT;
+            auto copy = [&](int k) {
+                const uint32_t dst = lds0 + (uint32_t)(k & 1) * AP_STAGE;
+                if (wave < v.R) copy_unit(up + (int64_t)k * UNIT, dst + wave * UNIT);
+                if (J + wave < v.C) copy_unit(ux + (int64_t)k * v.C * UNIT, dst + (RB + wave) * UNIT);
+            };
+            f32x16 acc[2][BU];
+#pragma unroll
+            for (int a = 0; a < 2; ++a)
+#pragma unroll
+                for (int b = 0; b < BU; ++b)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) acc[a][b][e] = 0.0f;
+            const int j0 = J + j1;
+            const bool active = i0 < v.R && j0 < v.C;
+            copy(0);
+            for (int k = 0; k < K; ++k) {
+                wait_copies_and_barrier<0>();
+                if (k + 1 < K) copy(k + 1);
+                if (!active) continue;
+                const char *stage = lds + (k & 1) * AP_STAGE;
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    Frag<PL> fa[2], fb[BU];
+#pragma unroll
+                    for (int a = 0; a < 2; ++a)
+#pragma unroll
+                        for (int z = 0; z < PL; ++z) fa[a].p[z] = frag_rows(stage + (i0 + a) * UNIT + z * kPlane, lane, s);
+#pragma unroll
+                    for (int b = 0; b < BU; ++b)
+#pragma unroll
+                        for (int z = 0; z < PL; ++z) fb[b].p[z] = frag_cols(stage + (RB + j1 + b) * UNIT + z * kPlane, lane, s);
+#pragma unroll
+                    for (int a = 0; a < 2; ++a)
+#pragma unroll
+                        for (int b = 0; b < BU; ++b) {
+                            if constexpr (ALONG) mma<PL>(acc[a][b], fa[a], fb[b]);
+                            else mma<PL>(acc[a][b], fb[b], fa[a]);
+                        }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            wait_copies_and_barrier<0>();  // the stages are free again
+            if (active) {
+#pragma unroll
+                for (int a = 0; a < 2; ++a)
+#pragma unroll
+                    for (int b = 0; b < BU; ++b) {
+                        const int i = i0 + a, j = j0 + b;
+                        if (i >= v.R || j >= v.C) continue;
+                        if constexpr (LAST) {
+                            Result<MUON, BF16> res;
+                            res.before(v, i, j, h, n);
+                            res.store(v, p, acc[a][b], i, j, h, n);
+                        } else {
+                            half4 out[4][PL];
+                            pack_unit<PL>(acc[a][b], 1.0f, out);
+                            store_unit<PL>(v.x0 + ((int64_t)i * v.C + j) * UNIT, out, n, h);
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+            }
+        }
+        wait_copies_and_barrier<0>();
+    }
+};
+
+template <int RB, int PL, bool MUON, bool BF16>
+__global__ __launch_bounds__(64 * kWgWaves) void ns_matrix_kernel(NsWork w, NsParams p, int first) {
+    using Wg = MatrixWg<RB, PL, MUON, BF16>;
+    constexpr int THREADS = 64 * kWgWaves;
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    __shared__ double red[kWgWaves];
+    View v = view_of<PL>(w, first + blockIdx.x);
+    v.A = v.P = v.x0 + (int64_t)v.R * v.C * (PL * kPlane);  // one buffer of each
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+    {  // momentum and norm, then X = u / max(|u|, eps)
+        const int per_row = 8 * (v.tr ? v.R : v.C), blocks = 64 * v.R * v.C;
+        double s = 0.0;
+        for (int k = tid; k < blocks; k += THREADS) {
+            const int br = k / per_row, bc = k - br * per_row;
+            float u[4][4];
+            load_block<MUON, BF16, true>(u, v, p, br * 4, bc * 4);
+#pragma unroll
+            for (int a = 0; a < 4; ++a)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s += (double)u[a][e] * u[a][e];
+        }
+#pragma unroll
+        for (int m = 32; m >= 1; m >>= 1) s += __shfl_xor(s, m, 64);
+        if (lane == 0) red[wave] = s;
+        __syncthreads();
+        s = red[0];
+#pragma unroll
+        for (int k = 1; k < kWgWaves; ++k) s += red[k];
+        const double norm = sqrt(s), f = (double)kScale / (norm < p.eps ? p.eps : norm);
+        for (int k = tid; k < blocks; k += THREADS) {
+            const int br = k / per_row, bc = k - br * per_row;
+            float u[4][4];
+            load_block<MUON, BF16, false>(u, v, p, br * 4, bc * 4);
+            pack_block<PL>(u, v, br * 4, bc * 4, f);
+        }
+        wait_copies_and_barrier<0>();
+    }
+
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
+    const Wg g{p, v, lds, lds0, lane, wave, lane >> 5, lane & 31};
+    for (int step = 0;; ++step) {
+        g.template squares<false>(v.x0, v.C);
+        g.template squares<true>(v.A, v.R);
+        if (step + 1 == p.steps) break;
+        g.template apply<false, false>();
+    }
+    if (v.tr) g.template apply<true, false>();
+    else g.template apply<true, true>();
+}
+
 // S stages: with the large tile two workgroups per CU, with the small one enough copies in
 // flight for a CU that has one
 template <int T, int PL> constexpr int kStages = T == 128 ? (PL == 2 ? 2 : 4) : 4;
@@ -817,6 +1106,19 @@ hipError_t launch_all(NsWork w, const NsLists &l, const NsParams &p, hipStream_t
     if (l.n_small > 0) {
         hipLaunchKernelGGL((ns_small_kernel<MUON, BF16, PL>), dim3((unsigned)l.n_small), dim3(64 * kSmallWaves), l.small_lds, s, w,
                            p, (int)l.first_small);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    // both forms: the matrices of more than 128 rows first, then the others
+    if (l.n_wg8 > 0) {
+        hipLaunchKernelGGL((ns_matrix_kernel<8, PL, MUON, BF16>), dim3((unsigned)l.n_wg8), dim3(64 * kWgWaves),
+                           (MatrixWg<8, PL, MUON, BF16>::LDS), s, w, p, (int)l.first_wg8);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (l.n_wg4 > 0) {
+        hipLaunchKernelGGL((ns_matrix_kernel<4, PL, MUON, BF16>), dim3((unsigned)l.n_wg4), dim3(64 * kWgWaves),
+                           (MatrixWg<4, PL, MUON, BF16>::LDS), s, w, p, (int)l.first_wg4);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -858,6 +1160,18 @@ int64_t ns_small_bytes(int64_t rows, int64_t cols, int planes) {
     const bool fits = planes == 2 ? fits_small<2>(R, C) : fits_small<1>(R, C);
     return fits ? (int64_t)(R * C + R * R) * planes * kPlane : 0;
 }
+
+int ns_matrix_rows(int64_t rows, int64_t cols) {
+    const int R = units((int)(rows < cols ? rows : cols));
+    return R <= 4 ? 4 : R <= 8 ? 8 : 0;
+}
+
+int64_t ns_matrix_wg_bytes(int64_t rows, int64_t cols, int planes) {
+    return ns_matrix_bytes(rows, cols, planes) / 2;
+}
+
+// A workgroup takes as long for its matrix as tiles on all CUs for about forty of them
+bool ns_by_matrix(double total, double largest) { return total >= 40.0 * largest; }
 
 // 128 x 128 tiles read each staged unit twice as often; once they do not fill
 // the CUs, tiles of a quarter the size do the work sooner

@@ -50,7 +50,8 @@ int check_coefs(double a, double b, double c, double eps, int steps) {
 struct PlanHeader {
     uint64_t magic;
     int64_t bytes, n_mats, ws_bytes, part_bytes;
-    int64_t n_small, small_lds;          // the last matrices, by themselves in a workgroup each
+    // matrices in this order: by tiles, a workgroup each (8 and 4 units of rows), in LDS
+    int64_t n_wg8, n_wg4, n_small, small_lds;
     int64_t tile, n_x, n_gram, n_apply;  // entries of the lists, padding included
     int64_t off_mats, off_x, off_gram, off_apply;
 };
@@ -102,6 +103,9 @@ struct Lists {
     }
 };
 
+// work of a matrix, about: the products' multiply-adds and the passes over its entries
+double cost(const Size &z) { return (double)z.r * z.r * (3.0 * z.c + z.r) + 1e4 * z.c * z.r; }
+
 struct Plan {
     PlanHeader h{};
     std::vector<NsMat> mats;
@@ -113,33 +117,41 @@ bool make_plan(const evo_muon_tensor *t, int32_t n, Plan &p) {
     if (n < 0 || (n > 0 && !t)) return false;
     PlanHeader &h = p.h;
     std::vector<int32_t> order;
+    std::vector<char> form((size_t)n);  // 0 tiles, 1 and 2 a workgroup with 8 and 4 units of rows, 3 in LDS
     int64_t tiles128 = 0, blocks = 0;
-    double total = 0.0;
-    auto cost = [&](int32_t i) {
-        const Size z = size_of(t[i]);
-        return (double)z.r * z.r * (3.0 * z.c + z.r) + 1e4 * z.c * z.r;
-    };
+    double total = 0.0, alone = 0.0, largest = 0.0;
     for (int32_t i = 0; i < n; ++i) {
         if (t[i].rows < 0 || t[i].cols < 0 || t[i].rows > kMostSide || t[i].cols > kMostSide) return false;
         if (t[i].rows == 0 || t[i].cols == 0) continue;
-        const Size z = size_of(t[i]);
         order.push_back(i);
-        const int64_t lds = evo::ns_small_bytes(t[i].rows, t[i].cols, 2);
-        if (lds > 0) {
-            ++h.n_small;
-            h.small_lds = lds > h.small_lds ? lds : h.small_lds;
-            continue;
+        if (evo::ns_small_bytes(t[i].rows, t[i].cols, 2) > 0) {
+            form[i] = 3;
+        } else if (const int rb = evo::ns_matrix_rows(t[i].rows, t[i].cols)) {
+            form[i] = rb == 8 ? 1 : 2;
+            alone += cost(size_of(t[i]));
+            largest = cost(size_of(t[i])) > largest ? cost(size_of(t[i])) : largest;
         }
+    }
+    const bool by_matrix = evo::ns_by_matrix(alone, largest);
+    for (const int32_t i : order) {
+        if (!by_matrix && form[i] != 3) form[i] = 0;
+        const Size z = size_of(t[i]);
+        if (form[i] == 1) ++h.n_wg8;
+        if (form[i] == 2) ++h.n_wg4;
+        if (form[i] == 3) {
+            ++h.n_small;
+            const int64_t lds = evo::ns_small_bytes(t[i].rows, t[i].cols, 2);
+            h.small_lds = lds > h.small_lds ? lds : h.small_lds;
+        }
+        if (form[i] != 0) continue;
         tiles128 += tiles_of(z.r, 128) * tiles_of(z.c, 128);
         blocks += blocks_of(z.r, z.c);
-        total += cost(i);
+        total += cost(z);
         if (blocks > 0x3fffffff) return false;
     }
-    // those that fit into a workgroup's LDS last; the others and they by falling cost
-    auto small = [&](int32_t i) { return evo::ns_small_bytes(t[i].rows, t[i].cols, 2) > 0; };
+    // each form by falling cost: what takes longest begins first
     std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) {
-        const bool sa = small(a), sb = small(b);
-        return sa != sb ? sb : cost(a) > cost(b);
+        return form[a] != form[b] ? form[a] < form[b] : cost(size_of(t[a])) > cost(size_of(t[b]));
     });
     h.magic = kMagic;
     h.tile = evo::ns_tile(tiles128);
@@ -159,16 +171,17 @@ bool make_plan(const evo_muon_tensor *t, int32_t n, Plan &p) {
         M.rows = (int32_t)s.rows;
         M.cols = (int32_t)s.cols;
         M.scale = (float)s.update_scale;
-        if (m >= (int32_t)order.size() - h.n_small) {
+        const int f = form[order[m]];
+        M.off = off;
+        if (f != 3) off += f == 0 ? evo::ns_matrix_bytes(s.rows, s.cols, 2) : evo::ns_matrix_wg_bytes(s.rows, s.cols, 2);
+        if (f != 0) {
             p.mats.push_back(M);
             continue;
         }
         M.part0 = (int32_t)part;
-        M.off = off;
         part += blocks_of(z.r, z.c);
-        off += evo::ns_matrix_bytes(s.rows, s.cols, 2);
         p.mats.push_back(M);
-        const double c = cost(order[m]);
+        const double c = cost(z);
         int xcd = 8;
         if (c * 8 <= total) {
             xcd = 0;
@@ -205,11 +218,17 @@ int check_orth(const evo_orth_dims *d) {
 
 bool orth_empty(const evo_orth_dims *d) { return d->n_batch == 0 || d->rows == 0 || d->cols == 0; }
 
-// a stack that fits into the workgroups' LDS still asks for a little, so that a size of 0 means a refusal
+bool orth_by_matrix(const evo_orth_dims *d) {
+    return evo::ns_matrix_rows(d->rows, d->cols) > 0 && evo::ns_by_matrix((double)d->n_batch, 1.0);
+}
+
+// (a stack that fits into the workgroups' LDS still asks for a little: a size of 0 means a refusal)
 size_t orth_workspace(const evo_orth_dims *d) {
-    if (evo::ns_small_bytes(d->rows, d->cols, d->dtype == EVO_DTYPE_BF16 ? 1 : 2) > 0) return 256;
+    const int planes = d->dtype == EVO_DTYPE_BF16 ? 1 : 2;
+    if (evo::ns_small_bytes(d->rows, d->cols, planes) > 0) return 256;
+    if (orth_by_matrix(d)) return (size_t)(d->n_batch * evo::ns_matrix_wg_bytes(d->rows, d->cols, planes));
     return (size_t)(round256(d->n_batch * blocks_of(d->rows, d->cols) * 8) +
-                    d->n_batch * evo::ns_matrix_bytes(d->rows, d->cols, d->dtype == EVO_DTYPE_BF16 ? 1 : 2));
+                    d->n_batch * evo::ns_matrix_bytes(d->rows, d->cols, planes));
 }
 
 // no C++ exception leaves a C entry: `none` where the plan's memory cannot be had
@@ -266,8 +285,13 @@ int evo_orthogonalize(const evo_orth_dims *d, const void *x, void *out, void *wo
     p.steps = d->steps;
     NsLists l{};
     l.small_lds = evo::ns_small_bytes(d->rows, d->cols, bf16 ? 1 : 2);
-    if (l.small_lds > 0) {
-        l.n_small = n;
+    if (l.small_lds > 0 || orth_by_matrix(d)) {
+        const int rb = evo::ns_matrix_rows(d->rows, d->cols);
+        if (l.small_lds > 0) l.n_small = n;
+        else if (rb == 8) l.n_wg8 = n;
+        else l.n_wg4 = n;
+        w.ws = (char *)workspace;
+        w.ws_stride = evo::ns_matrix_wg_bytes(d->rows, d->cols, bf16 ? 1 : 2);
         l.tile = 64;
         return evo::launch_ns(w, l, p, false, bf16, (hipStream_t)stream) == hipSuccess ? EVO_OK : EVO_ERR_HIP;
     }
@@ -366,6 +390,10 @@ int evo_muon_step(const evo_muon_hparams *hp, const void *plan, const void *plan
     l.n_small = h.n_small;
     l.first_small = h.n_mats - h.n_small;
     l.small_lds = h.small_lds;
+    l.n_wg4 = h.n_wg4;
+    l.first_wg4 = l.first_small - h.n_wg4;
+    l.n_wg8 = h.n_wg8;
+    l.first_wg8 = l.first_wg4 - h.n_wg8;
     l.tile = (int)h.tile;
     l.n_x = h.n_x;
     l.n_gram = h.n_gram;

@@ -43,11 +43,14 @@ struct NsParams {
     const float *grad_scale;
 };
 
-// Matrices n_small of them from first_small on fit into a workgroup's LDS (small_lds bytes)
-// and take one launch.  Work lists for the others, each a launch's grid: every matrix by tiles of 64 x 64 entries (norm, scaling), and
+// The parts of a call.  n_small matrices from first_small on fit into a
+// workgroup's LDS (small_lds bytes); n_wg8 (up to 8 units of 32 rows) and n_wg4 (up to 4) matrices
+// take a workgroup each with buffers in the workspace; the others work lists,
+// each a launch's grid: every matrix by tiles of 64 x 64 entries (norm, scaling), and
 // the products' tiles of `tile` x `tile`: the Gram matrix's upper triangle, and the iterate
 struct NsLists {
     int64_t n_small, first_small, small_lds;
+    int64_t n_wg8, first_wg8, n_wg4, first_wg4;
     int tile;                         // 64 or 128
     int64_t n_x, n_gram, n_apply;     // entries, padding included
     const NsTile *x, *gram, *apply;   // device tables, or null for a stack
@@ -57,6 +60,11 @@ constexpr int kNsBlock = 64;  // tiles of the norm and scaling passes
 
 // LDS that a matrix takes as a whole, 0 if it does not fit; planes: 2 for fp32, 1 for bf16
 int64_t ns_small_bytes(int64_t rows, int64_t cols, int planes);
+// 8 or 4: the form of workgroup that can take the matrix by itself, 0 if none
+int ns_matrix_rows(int64_t rows, int64_t cols);
+int64_t ns_matrix_wg_bytes(int64_t rows, int64_t cols, int planes);  // its buffers then
+// whether matrices of this much work in all, and the largest alone, are done a workgroup each
+bool ns_by_matrix(double total, double largest);
 // bytes of a matrix's buffers in the workspace where it does not fit
 int64_t ns_matrix_bytes(int64_t rows, int64_t cols, int planes);
 // tiles of the products for a call whose iterates have this many 128 x 128 tiles
