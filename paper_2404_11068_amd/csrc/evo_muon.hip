@@ -212,20 +212,22 @@ __device__ __forceinline__ void load_block(float (&u)[4][4], const View &v, cons
     }
 }
 
-// the thread's entries times f into the units of X
-template <int PL>
+// the thread's entries times f into the units of X, or (TRANSPOSED) of its transpose
+template <int PL, bool TRANSPOSED>
 __device__ __forceinline__ void pack_block(const float (&u)[4][4], const View &v, int row0, int col0, double f) {
+    const bool by_cols = v.tr != TRANSPOSED;  // a unit's rows are the columns in memory
+    const int rows = TRANSPOSED ? v.C : v.R, cols = TRANSPOSED ? v.R : v.C;
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
-        // row i of the iterate, columns j .. j + 3
-        const int i = v.tr ? col0 + x : row0 + x, j = v.tr ? row0 : col0;
-        if ((i >> 5) >= v.R || (j >> 5) >= v.C) continue;
+        // row i, columns j .. j + 3
+        const int i = by_cols ? col0 + x : row0 + x, j = by_cols ? row0 : col0;
+        if ((i >> 5) >= rows || (j >> 5) >= cols) continue;
         float q[4];
 #pragma unroll
-        for (int y = 0; y < 4; ++y) q[y] = (float)((double)(v.tr ? u[y][x] : u[x][y]) * f);
+        for (int y = 0; y < 4; ++y) q[y] = (float)((double)(by_cols ? u[y][x] : u[x][y]) * f);
         half4 hh[PL];
         split4<PL>(q, 1.0f, hh);
-        char *unit = v.x0 + ((int64_t)(i >> 5) * v.C + (j >> 5)) * (PL * kPlane);
+        char *unit = v.x0 + ((int64_t)(i >> 5) * cols + (j >> 5)) * (PL * kPlane);
         const int k = j & 31, at = chunk(i & 31, (k >> 3) & 1, k >> 4) + (k & 4) * 2;
 #pragma unroll
         for (int z = 0; z < PL; ++z) *(half4 *)(unit + z * kPlane + at) = hh[z];
@@ -280,7 +282,7 @@ __global__ __launch_bounds__(256) void ns_scale_kernel(NsWork w, NsParams p) {
     __syncthreads();
     const double norm = sqrt(((red[0] + red[1]) + red[2]) + red[3]);
     const double f = (double)kScale / (norm < p.eps ? p.eps : norm);
-    pack_block<PL>(u, v, row0, col0, f);
+    pack_block<PL, false>(u, v, row0, col0, f);
 }
 
 // ---- results
@@ -317,41 +319,51 @@ __device__ __forceinline__ void store_unit(char *unit, const half4 (&out)[4][PL]
         for (int z = 0; z < PL; ++z) *(half4 *)(unit + z * kPlane + chunk(n, g & 1, g >> 1) + h * 8) = out[g][z];
 }
 
-// one unit's entries of the result, the lanes along the memory rows; before(): loads what the update needs
+// One unit's entries of the result, the lanes along the memory rows; before() loads what the update
+// needs.  An address is a scalar row plus the lane's part, which is the same in every row
 template <bool MUON, bool BF16>
 struct Result {
     float p[16], w[16];
+
+    // f(entry, offset of its row in elements, the lane's) for the entries inside the matrix
+    template <class F>
+    __device__ __forceinline__ static void each(const View &v, int iu, int ju, int h, int n, F f) {
+        int row0 = __builtin_amdgcn_readfirstlane((v.tr ? ju : iu) * 32), col0 = (v.tr ? iu : ju) * 32;
+        asm volatile("" : "+s"(row0));  // (or a loop over units has all of its rows' addresses made before it)
+        asm volatile("" : "+v"(h), "+v"(n));
+        const uint32_t lane = (uint32_t)(4 * h) * (uint32_t)v.m.cols + (uint32_t)n;
+        const bool in = col0 + n < v.m.cols;
+        const int left = v.m.rows - row0 - 4 * h;
+        const int64_t first = (int64_t)row0 * v.m.cols + col0;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int r = 8 * (e >> 2) + (e & 3);
+            if (in && r < left) f(e, first + (int64_t)r * v.m.cols, lane);
+        }
+    }
     __device__ __forceinline__ void before(const View &v, int iu, int ju, int h, int n) {
         if constexpr (MUON) {
-            const int mr = (v.tr ? ju : iu) * 32 + 4 * h, mc = (v.tr ? iu : ju) * 32 + n;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int row = mr + 8 * (e >> 2) + (e & 3);
-                const bool ok = mc < v.m.cols && row < v.m.rows;
-                const int64_t at = ok ? (int64_t)row * v.m.cols + mc : 0;
-                p[e] = ((const float *)v.m.out)[at];
-                if (v.m.swa) w[e] = v.m.swa[at];
-            }
+            const float *const prm = (const float *)v.m.out, *const swa = v.m.swa;
+            each(v, iu, ju, h, n, [&](int e, int64_t row, uint32_t lane) { p[e] = (prm + row)[lane]; });
+            if (swa) each(v, iu, ju, h, n, [&](int e, int64_t row, uint32_t lane) { w[e] = (swa + row)[lane]; });
         }
     }
     __device__ __forceinline__ void store(const View &v, const NsParams &P, const f32x16 &acc, int iu, int ju, int h, int n) {
-        const int mr = (v.tr ? ju : iu) * 32 + 4 * h, mc = (v.tr ? iu : ju) * 32 + n;
-        if (mc >= v.m.cols) return;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int row = mr + 8 * (e >> 2) + (e & 3);
-            if (row >= v.m.rows) continue;
-            const int64_t at = (int64_t)row * v.m.cols + mc;
-            const float o = acc[e] * kUnscale;
-            if constexpr (MUON) {
-                const float q = fmaf(-P.lr * v.m.scale, o, P.decay * p[e]);
-                ((float *)v.m.out)[at] = q;
-                if (v.m.swa) v.m.swa[at] = fmaf(P.sd, w[e], P.om_sd * q);
-            } else if constexpr (BF16) {
-                ((uint16_t *)v.m.out)[at] = f2bf(o);
-            } else {
-                ((float *)v.m.out)[at] = o;
-            }
+        if constexpr (MUON) {
+            float *const prm = (float *)v.m.out, *const swa = v.m.swa;
+            const float f = -P.lr * v.m.scale * kUnscale;
+            each(v, iu, ju, h, n, [&](int e, int64_t row, uint32_t lane) {
+                p[e] = fmaf(f, acc[e], P.decay * p[e]);
+                (prm + row)[lane] = p[e];
+            });
+            if (swa)
+                each(v, iu, ju, h, n,
+                     [&](int e, int64_t row, uint32_t lane) { (swa + row)[lane] = fmaf(P.sd, w[e], P.om_sd * p[e]); });
+        } else {
+            each(v, iu, ju, h, n, [&](int e, int64_t row, uint32_t lane) {
+                if constexpr (BF16) ((uint16_t *)v.m.out + row)[lane] = f2bf(acc[e] * kUnscale);
+                else ((float *)v.m.out + row)[lane] = acc[e] * kUnscale;
+            });
         }
     }
 };
@@ -813,26 +825,25 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
 
 // ---- matrices of up to 256 rows, one workgroup each
 //
-// A workgroup of eight waves takes a matrix through all steps: the Gram
-// matrix and P lie in one buffer of the workspace, X in another and is updated
-// in place, block of 256 columns by block, because P X needs only those columns;
-// what one wave writes the others read after a barrier, all in the CU's own
-// caches.  Against the tiles above it saves 16 launches with their tails and
-// most of the traffic, a stage of the Gram matrix is one operand instead of
-// two, and a wave's 64 x 128 entries (RB = 8: up to 256 rows) take two thirds
-// of the LDS reads.  It takes a call with enough matrices for the CUs: a single
-// one is done sooner by tiles on all of them.
+// A workgroup of eight waves takes a matrix through all steps.  The Gram
+// matrix and then P lie in LDS, as the units of one triangle (36 of them, 144
+// KB, for 256 rows in pairs of planes): an operand of the other triangle is the mirrored
+// unit read by columns.  X lies in the workspace, transposed, so that the
+// fragments of P X come straight from memory, 1 KB a load: each wave takes unit
+// columns of its own and writes the result in their place, without a barrier.  Memory
+// then sees X read twice and written once per step; with A and P in the workspace, too,
+// 240 matrices of 256 x 256 moved 2.7 GB at 6.4 TB/s and took 430 us.
+// A call with too few matrices for the CUs is done sooner by the tiles above.
 
 constexpr int kWgWaves = 8;
 
 template <int RB, int PL, bool MUON, bool BF16>
 struct MatrixWg {
     static constexpr int UNIT = PL * kPlane;
-    static constexpr int WA = RB == 8 ? 2 : 1, WB = RB == 8 ? 4 : 2;  // of the symmetric products
-    static constexpr int BU = RB == 8 ? 4 : 2;                        // of P X: 2 x BU units
-    static constexpr int SQ_STAGE = RB * UNIT, SQ_STAGES = 4;
-    static constexpr int AP_STAGE = (RB + 8) * UNIT;                  // two stages
-    static constexpr int LDS = 2 * AP_STAGE > SQ_STAGES * SQ_STAGE ? 2 * AP_STAGE : SQ_STAGES * SQ_STAGE;
+    static constexpr int WA = RB == 8 ? 2 : 1, WB = RB == 8 ? 4 : 2;  // units of a wave's tile of the symmetric products
+    static constexpr int STAGE = RB * UNIT, STAGES = 4;               // of the Gram matrix: a unit column of X
+    static constexpr int TRI = RB * (RB + 1) / 2;
+    static constexpr int LDS = TRI * UNIT > STAGES * STAGE ? TRI * UNIT : STAGES * STAGE;
 
     const NsParams &p;
     const View &v;
@@ -840,36 +851,69 @@ struct MatrixWg {
     uint32_t lds0;
     int lane, wave, h, n;
 
-    __device__ __forceinline__ void copy_unit(const char *src, uint32_t dst) const {
-#pragma unroll
-        for (int e = 0; e < UNIT / 1024; ++e)
-            copy_to_lds(scalar(src), (uint32_t)(e * 1024 + lane * 16), dst + e * 1024);
+    // Every address below is the lane's part plus the unit's; out of the loop over the steps the
+    // compiler would compute all sums once and spill them, so each phase makes its own lane's part
+    __device__ __forceinline__ MatrixWg fresh() const {
+        MatrixWg g = *this;
+        asm volatile("" : "+v"(g.lane));
+        g.h = g.lane >> 5;
+        g.n = g.lane & 31;
+        return g;
     }
 
-    // M M^T for the wave's units (i0 + a, j0 + b), b >= a + D; M: K units per row.  Poly: the matrix is then
-    // P = a I + b M + c M M, in M's place, otherwise it goes to A
-    template <int D, bool POLY>
-    __device__ __forceinline__ void square(const char *M, int K, int i0, int j0) const {
+    // unit (r, k), r >= k, of the triangle in LDS: row r, contraction k
+    __device__ __forceinline__ char *tri(int r, int k) const { return lds + (r * (r + 1) / 2 + k) * UNIT; }
+    // rows of unit row r, contraction over unit column k, of the symmetric matrix in LDS
+    __device__ __forceinline__ void frag(Frag<PL> &f, int r, int k, int s) const {
+        if (r >= k) {
+            const char *u = tri(r, k);
+#pragma unroll
+            for (int z = 0; z < PL; ++z) f.p[z] = frag_rows(u + z * kPlane, lane, s);
+        } else {
+            const char *u = tri(k, r);
+#pragma unroll
+            for (int z = 0; z < PL; ++z) f.p[z] = frag_cols(u + z * kPlane, lane, s);
+        }
+    }
+
+    // The wave's units (i0 + a, j0 + b), b >= a + D, of A = X X^T, then of P in its place
+    template <int D>
+    __device__ __forceinline__ void gram_and_poly(int i0, int j0) const {
         f32x16 acc[WA][WB];
+        auto zero = [&] {
 #pragma unroll
-        for (int a = 0; a < WA; ++a)
+            for (int a = 0; a < WA; ++a)
 #pragma unroll
-            for (int b = 0; b < WB; ++b)
+                for (int b = 0; b < WB; ++b)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) acc[a][b][e] = 0.0f;
-        const char *src = M + (int64_t)wave * K * UNIT;  // this wave copies unit row `wave`
-        const bool copies = wave < v.R;
-        auto copy = [&](int k) {
-            if (copies) copy_unit(src + (int64_t)k * UNIT, lds0 + (uint32_t)(k % SQ_STAGES) * SQ_STAGE + wave * UNIT);
+                    for (int e = 0; e < 16; ++e) acc[a][b][e] = 0.0f;
         };
+        auto products = [&](const Frag<PL> (&fa)[WA], const Frag<PL> (&fb)[WB]) {
 #pragma unroll
-        for (int k = 0; k < SQ_STAGES - 1; ++k)
+            for (int a = 0; a < WA; ++a)
+#pragma unroll
+                for (int b = 0; b < WB; ++b)
+                    if (b >= a + D) mma<PL>(acc[a][b], fa[a], fb[b]);
+        };
+        constexpr int B0 = D > 0 ? D : 0;
+        const int K = v.C;
+        auto copy = [&](int k) {  // unit column k of X: this wave's unit of it
+            if (wave < v.R) {
+                const char *src = scalar(v.x0 + ((int64_t)k * v.R + wave) * UNIT);
+                const uint32_t dst = lds0 + (uint32_t)(k % STAGES) * STAGE + wave * UNIT;
+#pragma unroll
+                for (int e = 0; e < UNIT / 1024; ++e) copy_to_lds(src, (uint32_t)(e * 1024 + lane * 16), dst + e * 1024);
+            }
+        };
+        zero();
+#pragma unroll
+        for (int k = 0; k < STAGES - 1; ++k)
             if (k < K) copy(k);
         for (int k = 0; k < K; ++k) {
-            if (k + SQ_STAGES - 2 < K) wait_copies_and_barrier<(SQ_STAGES - 2) * (UNIT / 1024)>();
+            if (k + STAGES - 2 < K) wait_copies_and_barrier<(STAGES - 2) * (UNIT / 1024)>();
             else wait_copies_and_barrier<0>();
-            if (k + SQ_STAGES - 1 < K) copy(k + SQ_STAGES - 1);
-            const char *stage = lds + (k % SQ_STAGES) * SQ_STAGE;
+            if (k + STAGES - 1 < K) copy(k + STAGES - 1);
+            const char *stage = lds + (k % STAGES) * STAGE;
             if constexpr (D < WB) {
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
@@ -877,169 +921,161 @@ struct MatrixWg {
 #pragma unroll
                     for (int a = 0; a < WA; ++a)
 #pragma unroll
-                        for (int z = 0; z < PL; ++z) fa[a].p[z] = frag_rows(stage + (i0 + a) * UNIT + z * kPlane, lane, s);
+                        for (int z = 0; z < PL; ++z) fa[a].p[z] = frag_cols(stage + (i0 + a) * UNIT + z * kPlane, lane, s);
 #pragma unroll
-                    for (int b = D > 0 ? D : 0; b < WB; ++b)
+                    for (int b = B0; b < WB; ++b)
 #pragma unroll
-                        for (int z = 0; z < PL; ++z) fb[b].p[z] = frag_rows(stage + (j0 + b) * UNIT + z * kPlane, lane, s);
-#pragma unroll
-                    for (int a = 0; a < WA; ++a)
-#pragma unroll
-                        for (int b = 0; b < WB; ++b)
-                            if (b >= a + D) mma<PL>(acc[a][b], fa[a], fb[b]);
+                        for (int z = 0; z < PL; ++z) fb[b].p[z] = frag_cols(stage + (j0 + b) * UNIT + z * kPlane, lane, s);
+                    products(fa, fb);
                     __builtin_amdgcn_sched_barrier(0);  // (both halves' operands at once do not fit the registers)
                 }
             }
         }
-        wait_copies_and_barrier<0>();  // every wave is past its last stage: LDS is scratch, M may be overwritten
+        wait_copies_and_barrier<0>();  // every wave is past the last stage
         if constexpr (D < WB) {
-            char *const scratch = lds + wave * UNIT;
 #pragma unroll
             for (int a = 0; a < WA; ++a)
 #pragma unroll
-                for (int b = 0; b < WB; ++b) {
-                    const int i = i0 + a, j = j0 + b;
-                    if (b < a + D || i >= v.R || j >= v.R) continue;
-                    char *const at = v.A + ((int64_t)j * v.R + i) * UNIT;
-                    half4 out[4][PL];
-                    if constexpr (POLY) {
-                        half4 old[4][PL];
+                for (int b = 0; b < WB; ++b)
+                    if (b >= a + D && i0 + a < v.R && j0 + b < v.R) {
+                        half4 out[4][PL];
+                        pack_unit<PL>(acc[a][b], kUnscale, out);
+                        store_unit<PL>(tri(j0 + b, i0 + a), out, n, h);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+        }
+        wait_copies_and_barrier<0>();
+        half4 out[WA][WB][4][PL];
+        if constexpr (D < WB) {
+            zero();
+            for (int k = 0; k < v.R; ++k) {
 #pragma unroll
-                        for (int g = 0; g < 4; ++g)
+                for (int s = 0; s < 2; ++s) {
+                    Frag<PL> fa[WA], fb[WB];
 #pragma unroll
-                            for (int z = 0; z < PL; ++z)
-                                old[g][z] = *(const half4 *)(at + z * kPlane + chunk(n, g & 1, g >> 1) + h * 8);
+                    for (int a = 0; a < WA; ++a) frag(fa[a], i0 + a, k, s);
+#pragma unroll
+                    for (int b = B0; b < WB; ++b) frag(fb[b], j0 + b, k, s);
+                    products(fa, fb);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+#pragma unroll
+            for (int a = 0; a < WA; ++a)
+#pragma unroll
+                for (int b = 0; b < WB; ++b)
+                    if (b >= a + D && i0 + a < v.R && j0 + b < v.R) {
+                        const char *at = tri(j0 + b, i0 + a);
 #pragma unroll
                         for (int g = 0; g < 4; ++g) {
+                            half4 old[PL];
+#pragma unroll
+                            for (int z = 0; z < PL; ++z)
+                                old[z] = *(const half4 *)(at + z * kPlane + chunk(n, g & 1, g >> 1) + h * 8);
                             float q[4];
 #pragma unroll
                             for (int e = 0; e < 4; ++e) q[e] = acc[a][b][4 * g + e];
-                            poly4<PL>(q, old[g], p, i == j ? n - 8 * g - 4 * h : -1);
-                            split4<PL>(q, 1.0f, out[g]);
+                            poly4<PL>(q, old, p, i0 + a == j0 + b ? n - 8 * g - 4 * h : -1);
+                            split4<PL>(q, 1.0f, out[a][b][g]);
                         }
-                    } else {
-                        pack_unit<PL>(acc[a][b], kUnscale, out);
+                        __builtin_amdgcn_sched_barrier(0);
                     }
-                    store_unit<PL>(at, out, n, h);
-                    if (i != j) {
-                        store_unit<PL>(scratch, out, n, h);
-                        __builtin_amdgcn_wave_barrier();
-                        char *const mirror = v.A + ((int64_t)i * v.R + j) * UNIT;
-#pragma unroll
-                        for (int z = 0; z < PL; ++z)
-#pragma unroll
-                            for (int s = 0; s < 2; ++s)
-                                *(half8 *)(mirror + z * kPlane + chunk(n, h, s)) = frag_cols(scratch + z * kPlane, lane, s);
-                        __builtin_amdgcn_wave_barrier();
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-                }
         }
-        wait_copies_and_barrier<0>();  // the stores are done, too
+        wait_copies_and_barrier<0>();  // every wave has read A
+        if constexpr (D < WB) {
+#pragma unroll
+            for (int a = 0; a < WA; ++a)
+#pragma unroll
+                for (int b = 0; b < WB; ++b)
+                    if (b >= a + D && i0 + a < v.R && j0 + b < v.R) store_unit<PL>(tri(j0 + b, i0 + a), out[a][b], n, h);
+        }
+        wait_copies_and_barrier<0>();
     }
 
-    template <bool POLY>
-    __device__ __forceinline__ void squares(const char *M, int K) const {
-        // units (i0, j0) of the waves, those at or above the diagonal shared out so that no SIMD (wave % 4)
-        // has more than 10 of 36, or 3 of 10
+    __device__ __forceinline__ void make_p() const {
+        // unit row and column of the waves' tiles, those at or above the diagonal shared out
+        // so that no SIMD (wave % 4) has more than 10 of 36 units, or 3 of 10; d = 8: none
         int i0, j0;
         if constexpr (RB == 8) {
-            const int ri[8] = {0, 2, 0, 4, 4, 6, 2, 6}, rj[8] = {4, 4, 0, 4, 0, 0, 0, 4};
-            i0 = ri[wave];
-            j0 = rj[wave];
+            i0 = wave == 0 ? 0 : wave == 1 ? 2 : wave == 2 ? 0 : wave == 3 ? 4 : wave == 4 ? 4 : wave == 5 ? 6 : wave == 6 ? 2 : 6;
+            j0 = wave == 0 || wave == 1 || wave == 3 || wave == 7 ? 4 : 0;
         } else {
-            const int ri[8] = {0, 0, 1, 2, 1, 3, 2, 3}, rj[8] = {0, 2, 2, 2, 0, 2, 0, 0};
-            i0 = ri[wave];
-            j0 = rj[wave];
+            i0 = wave == 0 || wave == 1 ? 0 : wave == 2 || wave == 4 ? 1 : wave == 3 || wave == 6 ? 2 : 3;
+            j0 = wave == 1 || wave == 2 || wave == 3 || wave == 5 ? 2 : 0;
         }
         const int d = i0 - j0;
-        if (d < 0 || (RB == 4 && d == 0)) square<RB == 8 ? -8 : 0, POLY>(M, K, i0, j0);
-        else if (d == 0) square<0, POLY>(M, K, i0, j0);
-        else if (d < WB) square<RB == 8 ? 2 : 1, POLY>(M, K, i0, j0);
-        else square<8, POLY>(M, K, i0, j0);
+        if (d < 0) gram_and_poly<-8>(i0, j0);
+        else if (d == 0) gram_and_poly<0>(i0, j0);
+        else if (d < WB) gram_and_poly<WB / 2>(i0, j0);
+        else gram_and_poly<8>(i0, j0);
     }
 
     // X = P X in place, or (LAST) the result; ALONG: lane = column of the iterate, otherwise its row
     template <bool LAST, bool ALONG>
     __device__ __forceinline__ void apply() const {
-        const int i0 = RB == 8 ? 2 * (wave >> 1) : 2 * (wave >> 2), j1 = RB == 8 ? 4 * (wave & 1) : 2 * (wave & 3);
-        const int K = v.R;
-        for (int J = 0; J < v.C; J += 8) {
-            const char *up = v.P + (int64_t)wave * v.R * UNIT, *ux = v.x0 + (int64_t)(J + wave) * UNIT;
-            auto copy = [&](int k) {
-                const uint32_t dst = lds0 + (uint32_t)(k & 1) * AP_STAGE;
-                if (wave < v.R) copy_unit(up + (int64_t)k * UNIT, dst + wave * UNIT);
-                if (J + wave < v.C) copy_unit(ux + (int64_t)k * v.C * UNIT, dst + (RB + wave) * UNIT);
+        for (int j = wave; j < v.C; j += kWgWaves) {
+            char *const col = v.x0 + (int64_t)j * v.R * UNIT;
+            Frag<PL> x[RB > 4 ? 3 : 2][2];  // units of the column, loaded ahead
+            constexpr int RING = RB > 4 ? 3 : 2;
+            auto load = [&](int k) {
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int z = 0; z < PL; ++z)
+                        x[k % RING][s].p[z] = *(const half8 *)(col + k * UNIT + z * kPlane + chunk(n, h, s));
             };
-            f32x16 acc[2][BU];
+            f32x16 acc[RB];
 #pragma unroll
-            for (int a = 0; a < 2; ++a)
+            for (int i = 0; i < RB; ++i)
 #pragma unroll
-                for (int b = 0; b < BU; ++b)
+                for (int e = 0; e < 16; ++e) acc[i][e] = 0.0f;
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) acc[a][b][e] = 0.0f;
-            const int j0 = J + j1;
-            const bool active = i0 < v.R && j0 < v.C;
-            copy(0);
-            for (int k = 0; k < K; ++k) {
-                wait_copies_and_barrier<0>();
-                if (k + 1 < K) copy(k + 1);
-                if (!active) continue;
-                const char *stage = lds + (k & 1) * AP_STAGE;
+            for (int k = 0; k < RING - 1; ++k)
+                if (k < v.R) load(k);
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    Frag<PL> fa[2], fb[BU];
+            for (int k = 0; k < RB; ++k) {
+                if (k < v.R) {
+                    if (k + RING - 1 < v.R) load(k + RING - 1);
 #pragma unroll
-                    for (int a = 0; a < 2; ++a)
+                    for (int s = 0; s < 2; ++s) {
 #pragma unroll
-                        for (int z = 0; z < PL; ++z) fa[a].p[z] = frag_rows(stage + (i0 + a) * UNIT + z * kPlane, lane, s);
-#pragma unroll
-                    for (int b = 0; b < BU; ++b)
-#pragma unroll
-                        for (int z = 0; z < PL; ++z) fb[b].p[z] = frag_cols(stage + (RB + j1 + b) * UNIT + z * kPlane, lane, s);
-#pragma unroll
-                    for (int a = 0; a < 2; ++a)
-#pragma unroll
-                        for (int b = 0; b < BU; ++b) {
-                            if constexpr (ALONG) mma<PL>(acc[a][b], fa[a], fb[b]);
-                            else mma<PL>(acc[a][b], fb[b], fa[a]);
+                        for (int i = 0; i < RB; ++i) {
+                            Frag<PL> f;  // (units past the matrix hold anything: those results are not used)
+                            frag(f, i, k, s);
+                            if constexpr (ALONG || !LAST) mma<PL>(acc[i], f, x[k % RING][s]);
+                            else mma<PL>(acc[i], x[k % RING][s], f);
                         }
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < RB; ++i) {
+                if (i < v.R) {
+                    if constexpr (LAST) {
+                        Result<MUON, BF16> res;
+                        res.before(v, i, j, h, n);
+                        res.store(v, p, acc[i], i, j, h, n);
+                    } else {
+                        half4 out[4][PL];
+                        pack_unit<PL>(acc[i], 1.0f, out);
+                        store_unit<PL>(col + i * UNIT, out, n, h);
+                    }
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
-            wait_copies_and_barrier<0>();  // the stages are free again
-            if (active) {
-#pragma unroll
-                for (int a = 0; a < 2; ++a)
-#pragma unroll
-                    for (int b = 0; b < BU; ++b) {
-                        const int i = i0 + a, j = j0 + b;
-                        if (i >= v.R || j >= v.C) continue;
-                        if constexpr (LAST) {
-                            Result<MUON, BF16> res;
-                            res.before(v, i, j, h, n);
-                            res.store(v, p, acc[a][b], i, j, h, n);
-                        } else {
-                            half4 out[4][PL];
-                            pack_unit<PL>(acc[a][b], 1.0f, out);
-                            store_unit<PL>(v.x0 + ((int64_t)i * v.C + j) * UNIT, out, n, h);
-                        }
-                        __builtin_amdgcn_sched_barrier(0);
-                    }
-            }
         }
-        wait_copies_and_barrier<0>();
+        wait_copies_and_barrier<0>();  // (the stores, too)
     }
 };
 
 template <int RB, int PL, bool MUON, bool BF16>
-__global__ __launch_bounds__(64 * kWgWaves) void ns_matrix_kernel(NsWork w, NsParams p, int first) {
+__global__ __launch_bounds__(64 * kWgWaves) __attribute__((amdgpu_waves_per_eu(RB == 8 ? 2 : 4))) void
+ns_matrix_kernel(NsWork w, NsParams p, int first) {
     using Wg = MatrixWg<RB, PL, MUON, BF16>;
     constexpr int THREADS = 64 * kWgWaves;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     __shared__ double red[kWgWaves];
-    View v = view_of<PL>(w, first + blockIdx.x);
-    v.A = v.P = v.x0 + (int64_t)v.R * v.C * (PL * kPlane);  // one buffer of each
+    const View v = view_of<PL>(w, first + blockIdx.x);
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
@@ -1067,7 +1103,7 @@ __global__ __launch_bounds__(64 * kWgWaves) void ns_matrix_kernel(NsWork w, NsPa
             const int br = k / per_row, bc = k - br * per_row;
             float u[4][4];
             load_block<MUON, BF16, false>(u, v, p, br * 4, bc * 4);
-            pack_block<PL>(u, v, br * 4, bc * 4, f);
+            pack_block<PL, true>(u, v, br * 4, bc * 4, f);
         }
         wait_copies_and_barrier<0>();
     }
@@ -1075,13 +1111,12 @@ __global__ __launch_bounds__(64 * kWgWaves) void ns_matrix_kernel(NsWork w, NsPa
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
     const Wg g{p, v, lds, lds0, lane, wave, lane >> 5, lane & 31};
     for (int step = 0;; ++step) {
-        g.template squares<false>(v.x0, v.C);
-        g.template squares<true>(v.A, v.R);
+        g.fresh().make_p();
         if (step + 1 == p.steps) break;
-        g.template apply<false, false>();
+        g.fresh().template apply<false, true>();
     }
-    if (v.tr) g.template apply<true, false>();
-    else g.template apply<true, true>();
+    if (v.tr) g.fresh().template apply<true, false>();
+    else g.fresh().template apply<true, true>();
 }
 
 // S stages: with the large tile two workgroups per CU, with the small one enough copies in
@@ -1167,7 +1202,8 @@ int ns_matrix_rows(int64_t rows, int64_t cols) {
 }
 
 int64_t ns_matrix_wg_bytes(int64_t rows, int64_t cols, int planes) {
-    return ns_matrix_bytes(rows, cols, planes) / 2;
+    const int64_t r = rows < cols ? rows : cols, c = rows + cols - r;
+    return (r + 31) / 32 * ((c + 31) / 32) * planes * kPlane;
 }
 
 // A workgroup takes as long for its matrix as tiles on all CUs for about forty of them
