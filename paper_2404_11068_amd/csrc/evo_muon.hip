@@ -42,6 +42,7 @@ struct View {
     int r, c;         // the iterate's rows and columns, r <= c
     int R, C;         // in units
     bool tr;          // the iterate is the transposed matrix
+    bool xt;          // a workgroup's matrix: X lies transposed, in x0 alone
     char *x0, *x1, *A, *P;
 };
 
@@ -61,6 +62,7 @@ __device__ __forceinline__ View view_of(const NsWork &w, int k) {
     v.c = v.tr ? v.m.rows : v.m.cols;
     v.R = units(v.r);
     v.C = units(v.c);
+    v.xt = v.m.by_matrix != 0;
     const int64_t unit = PL * kPlane, nx = (int64_t)v.R * v.C * unit;
     v.x0 = w.ws + v.m.off;
     v.x1 = v.x0 + nx;
@@ -259,7 +261,7 @@ __global__ __launch_bounds__(256) void ns_norm_kernel(NsWork w, NsParams p) {
     if (tid == 0) w.part[first + t.ti * ntj + t.tj] = ((red[0] + red[1]) + red[2]) + red[3];
 }
 
-// X = u / max(|u|, eps), in units
+// X = u / max(|u|, eps), in units, transposed for a workgroup's matrix
 template <bool MUON, bool BF16, int PL>
 __global__ __launch_bounds__(256) void ns_scale_kernel(NsWork w, NsParams p) {
     __shared__ double red[4];
@@ -282,7 +284,46 @@ __global__ __launch_bounds__(256) void ns_scale_kernel(NsWork w, NsParams p) {
     __syncthreads();
     const double norm = sqrt(((red[0] + red[1]) + red[2]) + red[3]);
     const double f = (double)kScale / (norm < p.eps ? p.eps : norm);
-    pack_block<PL, false>(u, v, row0, col0, f);
+    if (v.xt) pack_block<PL, true>(u, v, row0, col0, f);
+    else pack_block<PL, false>(u, v, row0, col0, f);
+}
+
+// p = decay p - lr scale O, w = sd w + om_sd p, with O as the last product left it in buffer `odd` of X:
+// 32 x 32 floats in the place of each unit, by memory rows
+__global__ __launch_bounds__(256) void ns_update_kernel(NsWork w, NsParams p, int odd) {
+    const NsTile t = tile_of<false>(w, blockIdx.x);
+    if (t.mat < 0) return;
+    const View v = view_of<2>(w, t.mat);
+    const int tid = threadIdx.x;
+    const int mi = v.tr ? t.tj : t.ti, mj = v.tr ? t.ti : t.tj;
+    const int row0 = mi * kNsBlock + (tid >> 4) * 4, col0 = mj * kNsBlock + (tid & 15) * 4;
+    const int i = (v.tr ? col0 : row0) >> 5, j = (v.tr ? row0 : col0) >> 5;  // unit of the iterate
+    if (i >= v.R || j >= v.C) return;
+    const char *x = v.xt || !odd ? v.x0 : v.x1;
+    const float *o = (const float *)(x + (v.xt ? (int64_t)j * v.R + i : (int64_t)i * v.C + j) * (2 * kPlane));
+    float *const prm = (float *)v.m.out, *const swa = v.m.swa;
+    const float f = -p.lr * v.m.scale;
+    float q[4][4], a[4][4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int64_t at = (int64_t)(row0 + r) * v.m.cols + col0;
+        const int left = row0 + r < v.m.rows ? v.m.cols - col0 : 0;
+        load4(q[r], prm + at, left);
+        if (swa) load4(a[r], swa + at, left);
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int64_t at = (int64_t)(row0 + r) * v.m.cols + col0;
+        const int left = row0 + r < v.m.rows ? v.m.cols - col0 : 0;
+        const f32x4 u = *(const f32x4 *)(o + ((row0 + r) & 31) * 32 + (col0 & 31));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            q[r][e] = fmaf(f, u[e], p.decay * q[r][e]);
+            if (swa) a[r][e] = fmaf(p.sd, a[r][e], p.om_sd * q[r][e]);
+        }
+        store4(q[r], prm + at, left);
+        if (swa) store4(a[r], swa + at, left);
+    }
 }
 
 // ---- results
@@ -367,6 +408,21 @@ struct Result {
         }
     }
 };
+
+// the last product's unit: for Muon as floats by memory rows in the unit's place, for ns_update_kernel,
+// otherwise the result itself
+template <bool MUON, bool BF16>
+__device__ __forceinline__ void store_last(const View &v, const NsParams &p, const f32x16 &acc, char *unit, int iu, int ju, int h,
+                                           int n) {
+    if constexpr (MUON) {
+        float *const o = (float *)unit + 128 * h + n;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[(8 * (e >> 2) + (e & 3)) * 32] = acc[e] * kUnscale;
+    } else {
+        Result<MUON, BF16> res;
+        res.store(v, p, acc, iu, ju, h, n);
+    }
+}
 
 // ---- products
 //
@@ -572,9 +628,9 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, i
         for (int a = 0; a < U; ++a)
 #pragma unroll
             for (int b = 0; b < U; ++b) {
-                Result<MUON, BF16> res;
-                res.before(v, i0 + a, j0 + b, h, n);
-                res.store(v, p, acc[a][b], i0 + a, j0 + b, h, n);
+                const int i = i0 + a, j = j0 + b;
+                if (i >= v.R || j >= v.C) continue;
+                store_last<MUON, BF16>(v, p, acc[a][b], (odd ? v.x0 : v.x1) + ((int64_t)i * v.C + j) * UNIT, i, j, h, n);
             }
     }
 }
@@ -825,7 +881,8 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
 
 // ---- matrices of up to 256 rows, one workgroup each
 //
-// A workgroup of eight waves takes a matrix through all steps.  The Gram
+// A workgroup of eight waves takes a matrix through all steps.  (The norm, the
+// scaling and Muon's update are passes of their own: a CU by itself keeps too little in flight for them.)  The Gram
 // matrix and then P lie in LDS, as the units of one triangle (36 of them, 144
 // KB, for 256 rows in pairs of planes): an operand of the other triangle is the mirrored
 // unit read by columns.  X lies in the workspace, transposed, so that the
@@ -1052,9 +1109,7 @@ struct MatrixWg {
             for (int i = 0; i < RB; ++i) {
                 if (i < v.R) {
                     if constexpr (LAST) {
-                        Result<MUON, BF16> res;
-                        res.before(v, i, j, h, n);
-                        res.store(v, p, acc[i], i, j, h, n);
+                        store_last<MUON, BF16>(v, p, acc[i], col + i * UNIT, i, j, h, n);
                     } else {
                         half4 out[4][PL];
                         pack_unit<PL>(acc[i], 1.0f, out);
@@ -1072,41 +1127,10 @@ template <int RB, int PL, bool MUON, bool BF16>
 __global__ __launch_bounds__(64 * kWgWaves) __attribute__((amdgpu_waves_per_eu(RB == 8 ? 2 : 4))) void
 ns_matrix_kernel(NsWork w, NsParams p, int first) {
     using Wg = MatrixWg<RB, PL, MUON, BF16>;
-    constexpr int THREADS = 64 * kWgWaves;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
-    __shared__ double red[kWgWaves];
     const View v = view_of<PL>(w, first + blockIdx.x);
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-
-    {  // momentum and norm, then X = u / max(|u|, eps)
-        const int per_row = 8 * (v.tr ? v.R : v.C), blocks = 64 * v.R * v.C;
-        double s = 0.0;
-        for (int k = tid; k < blocks; k += THREADS) {
-            const int br = k / per_row, bc = k - br * per_row;
-            float u[4][4];
-            load_block<MUON, BF16, true>(u, v, p, br * 4, bc * 4);
-#pragma unroll
-            for (int a = 0; a < 4; ++a)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s += (double)u[a][e] * u[a][e];
-        }
-#pragma unroll
-        for (int m = 32; m >= 1; m >>= 1) s += __shfl_xor(s, m, 64);
-        if (lane == 0) red[wave] = s;
-        __syncthreads();
-        s = red[0];
-#pragma unroll
-        for (int k = 1; k < kWgWaves; ++k) s += red[k];
-        const double norm = sqrt(s), f = (double)kScale / (norm < p.eps ? p.eps : norm);
-        for (int k = tid; k < blocks; k += THREADS) {
-            const int br = k / per_row, bc = k - br * per_row;
-            float u[4][4];
-            load_block<MUON, BF16, false>(u, v, p, br * 4, bc * 4);
-            pack_block<PL, true>(u, v, br * 4, bc * 4, f);
-        }
-        wait_copies_and_barrier<0>();
-    }
 
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
     const Wg g{p, v, lds, lds0, lane, wave, lane >> 5, lane & 31};
@@ -1144,19 +1168,6 @@ hipError_t launch_all(NsWork w, const NsLists &l, const NsParams &p, hipStream_t
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    // both forms: the matrices of more than 128 rows first, then the others
-    if (l.n_wg8 > 0) {
-        hipLaunchKernelGGL((ns_matrix_kernel<8, PL, MUON, BF16>), dim3((unsigned)l.n_wg8), dim3(64 * kWgWaves),
-                           (MatrixWg<8, PL, MUON, BF16>::LDS), s, w, p, (int)l.first_wg8);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    if (l.n_wg4 > 0) {
-        hipLaunchKernelGGL((ns_matrix_kernel<4, PL, MUON, BF16>), dim3((unsigned)l.n_wg4), dim3(64 * kWgWaves),
-                           (MatrixWg<4, PL, MUON, BF16>::LDS), s, w, p, (int)l.first_wg4);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
     if (l.n_x == 0) return hipSuccess;
     NsWork wx = w;
     const int r = w.uni.rows < w.uni.cols ? w.uni.rows : w.uni.cols, c = w.uni.rows + w.uni.cols - r;
@@ -1169,7 +1180,21 @@ hipError_t launch_all(NsWork w, const NsLists &l, const NsParams &p, hipStream_t
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((ns_scale_kernel<MUON, BF16, PL>), gx, b, 0, s, wx, p);
     e = hipGetLastError();
-    for (int k = 0; k < p.steps && e == hipSuccess; ++k) {
+    if (e != hipSuccess) return e;
+    // matrices of more than 128 rows, then of fewer
+    if (l.n_wg8 > 0) {
+        hipLaunchKernelGGL((ns_matrix_kernel<8, PL, MUON, BF16>), dim3((unsigned)l.n_wg8), dim3(64 * kWgWaves),
+                           (MatrixWg<8, PL, MUON, BF16>::LDS), s, w, p, (int)l.first_wg8);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (l.n_wg4 > 0) {
+        hipLaunchKernelGGL((ns_matrix_kernel<4, PL, MUON, BF16>), dim3((unsigned)l.n_wg4), dim3(64 * kWgWaves),
+                           (MatrixWg<4, PL, MUON, BF16>::LDS), s, w, p, (int)l.first_wg4);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    for (int k = 0; k < p.steps && l.n_apply > 0; ++k) {
         const int odd = k & 1;
         e = launch_product<T, PL, kGram, false, false>(w, l.gram, l.n_gram, p, odd, s);
         if (e != hipSuccess) return e;
@@ -1177,6 +1202,11 @@ hipError_t launch_all(NsWork w, const NsLists &l, const NsParams &p, hipStream_t
         if (e != hipSuccess) return e;
         e = k + 1 < p.steps ? launch_product<T, PL, kApply, false, false>(w, l.apply, l.n_apply, p, odd, s)
                             : launch_product<T, PL, kLast, MUON, BF16>(w, l.apply, l.n_apply, p, odd, s);
+        if (e != hipSuccess) return e;
+    }
+    if constexpr (MUON) {
+        hipLaunchKernelGGL(ns_update_kernel, gx, b, 0, s, wx, p, p.steps & 1);
+        e = hipGetLastError();
     }
     return e;
 }

@@ -143,11 +143,12 @@ bool make_plan(const evo_muon_tensor *t, int32_t n, Plan &p) {
             const int64_t lds = evo::ns_small_bytes(t[i].rows, t[i].cols, 2);
             h.small_lds = lds > h.small_lds ? lds : h.small_lds;
         }
+        if (form[i] == 3) continue;
+        blocks += blocks_of(z.r, z.c);
+        if (blocks > 0x3fffffff) return false;
         if (form[i] != 0) continue;
         tiles128 += tiles_of(z.r, 128) * tiles_of(z.c, 128);
-        blocks += blocks_of(z.r, z.c);
         total += cost(z);
-        if (blocks > 0x3fffffff) return false;
     }
     // each form by falling cost: what takes longest begins first
     std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) {
@@ -173,14 +174,19 @@ bool make_plan(const evo_muon_tensor *t, int32_t n, Plan &p) {
         M.scale = (float)s.update_scale;
         const int f = form[order[m]];
         M.off = off;
-        if (f != 3) off += f == 0 ? evo::ns_matrix_bytes(s.rows, s.cols, 2) : evo::ns_matrix_wg_bytes(s.rows, s.cols, 2);
-        if (f != 0) {
+        if (f == 3) {
             p.mats.push_back(M);
             continue;
         }
         M.part0 = (int32_t)part;
+        M.by_matrix = f != 0;
         part += blocks_of(z.r, z.c);
+        off += f == 0 ? evo::ns_matrix_bytes(s.rows, s.cols, 2) : evo::ns_matrix_wg_bytes(s.rows, s.cols, 2);
         p.mats.push_back(M);
+        if (f != 0) {
+            each_tile(z.r, z.c, evo::kNsBlock, [&](int32_t i, int32_t j) { p.x.add(8, NsTile{m, i, j}); });
+            continue;
+        }
         const double c = cost(z);
         int xcd = 8;
         if (c * 8 <= total) {
@@ -226,9 +232,9 @@ bool orth_by_matrix(const evo_orth_dims *d) {
 size_t orth_workspace(const evo_orth_dims *d) {
     const int planes = d->dtype == EVO_DTYPE_BF16 ? 1 : 2;
     if (evo::ns_small_bytes(d->rows, d->cols, planes) > 0) return 256;
-    if (orth_by_matrix(d)) return (size_t)(d->n_batch * evo::ns_matrix_wg_bytes(d->rows, d->cols, planes));
-    return (size_t)(round256(d->n_batch * blocks_of(d->rows, d->cols) * 8) +
-                    d->n_batch * evo::ns_matrix_bytes(d->rows, d->cols, planes));
+    const int64_t each = orth_by_matrix(d) ? evo::ns_matrix_wg_bytes(d->rows, d->cols, planes)
+                                           : evo::ns_matrix_bytes(d->rows, d->cols, planes);
+    return (size_t)(round256(d->n_batch * blocks_of(d->rows, d->cols) * 8) + d->n_batch * each);
 }
 
 // no C++ exception leaves a C entry: `none` where the plan's memory cannot be had
@@ -285,22 +291,22 @@ int evo_orthogonalize(const evo_orth_dims *d, const void *x, void *out, void *wo
     p.steps = d->steps;
     NsLists l{};
     l.small_lds = evo::ns_small_bytes(d->rows, d->cols, bf16 ? 1 : 2);
-    if (l.small_lds > 0 || orth_by_matrix(d)) {
-        const int rb = evo::ns_matrix_rows(d->rows, d->cols);
-        if (l.small_lds > 0) l.n_small = n;
-        else if (rb == 8) l.n_wg8 = n;
-        else l.n_wg4 = n;
-        w.ws = (char *)workspace;
-        w.ws_stride = evo::ns_matrix_wg_bytes(d->rows, d->cols, bf16 ? 1 : 2);
-        l.tile = 64;
-        return evo::launch_ns(w, l, p, false, bf16, (hipStream_t)stream) == hipSuccess ? EVO_OK : EVO_ERR_HIP;
-    }
     l.tile = evo::ns_tile(n * tiles_of(r, 128) * tiles_of(c, 128));
     // eight matrices or more are dealt to the XCDs, so their number is rounded up
     const int64_t slots = n >= 8 ? (n + 7) / 8 * 8 : n, g = tiles_of(r, l.tile);
-    l.n_x = slots * blocks_of(r, c);
-    l.n_gram = slots * (g * (g + 1) / 2);
-    l.n_apply = slots * g * tiles_of(c, l.tile);
+    if (l.small_lds > 0) {
+        l.n_small = n;
+    } else {
+        l.n_x = slots * blocks_of(r, c);
+        if (orth_by_matrix(d)) {
+            w.ws_stride = evo::ns_matrix_wg_bytes(d->rows, d->cols, bf16 ? 1 : 2);
+            w.uni.by_matrix = 1;
+            (evo::ns_matrix_rows(d->rows, d->cols) == 8 ? l.n_wg8 : l.n_wg4) = n;
+        } else {
+            l.n_gram = slots * (g * (g + 1) / 2);
+            l.n_apply = slots * g * tiles_of(c, l.tile);
+        }
+    }
     return evo::launch_ns(w, l, p, false, bf16, (hipStream_t)stream) == hipSuccess ? EVO_OK : EVO_ERR_HIP;
 }
 

@@ -15,6 +15,7 @@ struct NsMat {
     int32_t rows, cols;
     float scale;         // factor of the update
     int32_t part0;       // first partial sum of squares
+    int32_t by_matrix, pad;  // 1: a workgroup takes it by itself (X transposed in the workspace)
     int64_t off;         // byte offset of the matrix's buffers in the workspace
 };
 
@@ -44,10 +45,10 @@ struct NsParams {
 };
 
 // The parts of a call.  n_small matrices from first_small on fit into a
-// workgroup's LDS (small_lds bytes); n_wg8 (up to 8 units of 32 rows) and n_wg4 (up to 4) matrices
-// take a workgroup each with buffers in the workspace; the others work lists,
-// each a launch's grid: every matrix by tiles of 64 x 64 entries (norm, scaling), and
-// the products' tiles of `tile` x `tile`: the Gram matrix's upper triangle, and the iterate
+// workgroup's LDS (small_lds bytes) and take one launch.  The others have work lists, each
+// a launch's grid: x, tiles of 64 x 64 entries, for norm, scaling and update.  Of them n_wg8 (up to 8
+// units of 32 rows) and n_wg4 (up to 4) go through the steps a workgroup each, the rest by the products'
+// tiles of `tile` x `tile`: gram, the Gram matrix's upper triangle, and apply, the iterate
 struct NsLists {
     int64_t n_small, first_small, small_lds;
     int64_t n_wg8, first_wg8, n_wg4, first_wg4;
