@@ -216,7 +216,7 @@ __device__ __forceinline__ void load_block(float (&u)[4][4], const View &v, cons
 
 // the thread's entries times f into the units of X, or (TRANSPOSED) of its transpose
 template <int PL, bool TRANSPOSED>
-__device__ __forceinline__ void pack_block(const float (&u)[4][4], const View &v, int row0, int col0, double f) {
+__device__ __forceinline__ void pack_block(const float (&u)[4][4], const View &v, char *x0, int row0, int col0, double f) {
     const bool by_cols = v.tr != TRANSPOSED;  // a unit's rows are the columns in memory
     const int rows = TRANSPOSED ? v.C : v.R, cols = TRANSPOSED ? v.R : v.C;
 #pragma unroll
@@ -229,7 +229,7 @@ __device__ __forceinline__ void pack_block(const float (&u)[4][4], const View &v
         for (int y = 0; y < 4; ++y) q[y] = (float)((double)(by_cols ? u[y][x] : u[x][y]) * f);
         half4 hh[PL];
         split4<PL>(q, 1.0f, hh);
-        char *unit = v.x0 + ((int64_t)(i >> 5) * cols + (j >> 5)) * (PL * kPlane);
+        char *unit = x0 + ((int64_t)(i >> 5) * cols + (j >> 5)) * (PL * kPlane);
         const int k = j & 31, at = chunk(i & 31, (k >> 3) & 1, k >> 4) + (k & 4) * 2;
 #pragma unroll
         for (int z = 0; z < PL; ++z) *(half4 *)(unit + z * kPlane + at) = hh[z];
@@ -284,8 +284,8 @@ __global__ __launch_bounds__(256) void ns_scale_kernel(NsWork w, NsParams p) {
     __syncthreads();
     const double norm = sqrt(((red[0] + red[1]) + red[2]) + red[3]);
     const double f = (double)kScale / (norm < p.eps ? p.eps : norm);
-    if (v.xt) pack_block<PL, true>(u, v, row0, col0, f);
-    else pack_block<PL, false>(u, v, row0, col0, f);
+    if (v.xt) pack_block<PL, true>(u, v, v.x0, row0, col0, f);
+    else pack_block<PL, false>(u, v, v.x0, row0, col0, f);
 }
 
 // p = decay p - lr scale O, w = sd w + om_sd p, with O as the last product left it in buffer `odd` of X:
@@ -360,51 +360,62 @@ __device__ __forceinline__ void store_unit(char *unit, const half4 (&out)[4][PL]
         for (int z = 0; z < PL; ++z) *(half4 *)(unit + z * kPlane + chunk(n, g & 1, g >> 1) + h * 8) = out[g][z];
 }
 
-// One unit's entries of the result, the lanes along the memory rows; before() loads what the update
-// needs.  An address is a scalar row plus the lane's part, which is the same in every row
+// One unit's entries of the result, the lanes along the memory rows.  A buffer begins at the unit's
+// first row and ends with the matrix (or 2 GB on, past the unit): rows beyond it read
+// nothing and are not written, so no entry takes a branch; columns beyond it are sent there
+template <bool BF16>
+struct UnitOut {
+    rsrc_t r;
+    uint32_t lane, row;  // byte offset of the lane's first entry, bytes of a memory row
+    __device__ __forceinline__ UnitOut(const View &v, const void *base, int iu, int ju, int h, int n) {
+        constexpr uint32_t ES = BF16 ? 2 : 4;
+        asm volatile("" : "+v"(h), "+v"(n));  // (or a loop over units has all of their addresses made before it)
+        const int row0 = __builtin_amdgcn_readfirstlane((v.tr ? ju : iu) * 32), col0 = (v.tr ? iu : ju) * 32;
+        const int64_t first = (int64_t)row0 * v.m.cols;
+        const int64_t left = ((int64_t)v.m.rows * v.m.cols - first) * ES;
+        r = make_buf((const char *)base + first * ES, (uint32_t)(left < 0x7ffffff0 ? left : 0x7ffffff0));
+        row = (uint32_t)v.m.cols * ES;
+        lane = col0 + n < v.m.cols ? (uint32_t)(4 * h) * row + (uint32_t)(col0 + n) * ES : kOOB;
+    }
+    __device__ __forceinline__ uint32_t at(int e) const { return lane + (uint32_t)(8 * (e >> 2) + (e & 3)) * row; }
+};
+
 template <bool MUON, bool BF16>
 struct Result {
     float p[16], w[16];
-
-    // f(entry, offset of its row in elements, the lane's) for the entries inside the matrix
-    template <class F>
-    __device__ __forceinline__ static void each(const View &v, int iu, int ju, int h, int n, F f) {
-        int row0 = __builtin_amdgcn_readfirstlane((v.tr ? ju : iu) * 32), col0 = (v.tr ? iu : ju) * 32;
-        asm volatile("" : "+s"(row0));  // (or a loop over units has all of its rows' addresses made before it)
-        asm volatile("" : "+v"(h), "+v"(n));
-        const uint32_t lane = (uint32_t)(4 * h) * (uint32_t)v.m.cols + (uint32_t)n;
-        const bool in = col0 + n < v.m.cols;
-        const int left = v.m.rows - row0 - 4 * h;
-        const int64_t first = (int64_t)row0 * v.m.cols + col0;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int r = 8 * (e >> 2) + (e & 3);
-            if (in && r < left) f(e, first + (int64_t)r * v.m.cols, lane);
-        }
-    }
     __device__ __forceinline__ void before(const View &v, int iu, int ju, int h, int n) {
         if constexpr (MUON) {
-            const float *const prm = (const float *)v.m.out, *const swa = v.m.swa;
-            each(v, iu, ju, h, n, [&](int e, int64_t row, uint32_t lane) { p[e] = (prm + row)[lane]; });
-            if (swa) each(v, iu, ju, h, n, [&](int e, int64_t row, uint32_t lane) { w[e] = (swa + row)[lane]; });
+            const UnitOut<false> a(v, v.m.out, iu, ju, h, n);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) p[e] = __uint_as_float(bload4(a.r, a.at(e)));
+            if (v.m.swa) {
+                const UnitOut<false> b(v, v.m.swa, iu, ju, h, n);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) w[e] = __uint_as_float(bload4(b.r, b.at(e)));
+            }
         }
     }
     __device__ __forceinline__ void store(const View &v, const NsParams &P, const f32x16 &acc, int iu, int ju, int h, int n) {
+        const UnitOut<BF16> a(v, v.m.out, iu, ju, h, n);
         if constexpr (MUON) {
-            float *const prm = (float *)v.m.out, *const swa = v.m.swa;
             const float f = -P.lr * v.m.scale * kUnscale;
-            each(v, iu, ju, h, n, [&](int e, int64_t row, uint32_t lane) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
                 p[e] = fmaf(f, acc[e], P.decay * p[e]);
-                (prm + row)[lane] = p[e];
-            });
-            if (swa)
-                each(v, iu, ju, h, n,
-                     [&](int e, int64_t row, uint32_t lane) { (swa + row)[lane] = fmaf(P.sd, w[e], P.om_sd * p[e]); });
+                bstore4(__float_as_uint(p[e]), a.r, a.at(e));
+            }
+            if (v.m.swa) {
+                const UnitOut<false> b(v, v.m.swa, iu, ju, h, n);
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    bstore4(__float_as_uint(fmaf(P.sd, w[e], P.om_sd * p[e])), b.r, b.at(e));
+            }
         } else {
-            each(v, iu, ju, h, n, [&](int e, int64_t row, uint32_t lane) {
-                if constexpr (BF16) ((uint16_t *)v.m.out + row)[lane] = f2bf(acc[e] * kUnscale);
-                else ((float *)v.m.out + row)[lane] = acc[e] * kUnscale;
-            });
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                if constexpr (BF16) __builtin_amdgcn_raw_buffer_store_b16(f2bf(acc[e] * kUnscale), a.r, a.at(e), 0, 0);
+                else bstore4(__float_as_uint(acc[e] * kUnscale), a.r, a.at(e));
+            }
         }
     }
 };
@@ -635,32 +646,54 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, i
     }
 }
 
+// A symmetric matrix in LDS as the units of one triangle: unit (r, k), r >= k, holds rows r, contraction
+// k.  An operand of the other triangle is the mirrored unit read by columns
+template <int PL>
+__device__ __forceinline__ char *tri_unit(char *base, int r, int k) {
+    return base + (r * (r + 1) / 2 + k) * (PL * kPlane);
+}
+// rows of unit row r, contraction over unit column k (both wave-uniform)
+template <int PL>
+__device__ __forceinline__ void tri_frag(Frag<PL> &f, char *base, int r, int k, int s, int lane) {
+    if (r >= k) {
+        const char *u = tri_unit<PL>(base, r, k);
+#pragma unroll
+        for (int z = 0; z < PL; ++z) f.p[z] = frag_rows(u + z * kPlane, lane, s);
+    } else {
+        const char *u = tri_unit<PL>(base, k, r);
+#pragma unroll
+        for (int z = 0; z < PL; ++z) f.p[z] = frag_cols(u + z * kPlane, lane, s);
+    }
+}
+
 // ---- matrices that fit into LDS: everything in one workgroup
 //
-// X and A (later P in its place) lie in LDS as units, R C + R R <= 39 of them
-// in pairs (128 x 160 entries, 64 x 544, 32 x 1184) and at most kSmallUnits of
-// X; a product's results wait in registers until every wave has read its
-// operands.  One launch does the norm, the steps and the update: memory sees
-// each entry once.  A wave takes units of the upper triangle (10 of 16 at 128
-// x 128) or pairs of units of X in turn.
+// X and the triangle of A, then of P in its place, lie in LDS: 128 x 224 entries in pairs
+// of planes, 64 x 608, 32 x 1216.  A product's results wait in registers until every
+// wave has read its operands.  One launch does the norm, the steps and the
+// update: memory sees each entry once.  Each of 16 waves takes a unit of the
+// triangle (10 of them at 128 x 128) and one to three of X; what bounds it is
+// the chain of a unit, LDS reads, matrix instructions, splitting and
+// storing, so the next operands are read before the matrix instructions of the last.
 
 constexpr int kSmallUnits = 40;
 constexpr int kSmallLds = 39 * 2 * kPlane;
-constexpr int kSmallWaves = 8;
+constexpr int kSmallWaves = 16;
 
 template <int PL>
 __host__ __device__ inline bool fits_small(int R, int C) {
-    return R * ((C + 1) / 2) <= 3 * kSmallWaves && R * C <= kSmallUnits && (R * C + R * R) * PL * kPlane <= kSmallLds;
+    return R * C <= kSmallUnits && R <= 6 && (R * C + R * (R + 1) / 2) * PL * kPlane <= kSmallLds;
 }
 
 template <bool MUON, bool BF16, int PL>
 __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, NsParams p, int first) {
     constexpr int UNIT = PL * kPlane, THREADS = 64 * kSmallWaves;
-    constexpr int BLOCKS = kSmallUnits * 64 / THREADS;  // 4 x 4 blocks of a thread
+    constexpr int BLOCKS = (kSmallUnits * 64 + THREADS - 1) / THREADS;  // 4 x 4 blocks of a thread
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     __shared__ double red[kSmallWaves];
     const View v = view_of<PL>(w, first + blockIdx.x);
-    const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, n = lane & 31;
+    const int tid = threadIdx.x;
+    int lane = tid & 63, h = lane >> 5, n = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int R = v.R, C = v.C;
     char *const X = lds, *const A = lds + R * C * UNIT;
@@ -694,112 +727,77 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
             const int k = q * THREADS + tid;
             if (k < blocks) {
                 const int br = k / per_row, bc = k - br * per_row;
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    const int i = v.tr ? bc * 4 + x : br * 4 + x, j = v.tr ? br * 4 : bc * 4;
-                    float y4[4];
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) y4[y] = (float)((double)(v.tr ? u[q][y][x] : u[q][x][y]) * f);
-                    half4 hh[PL];
-                    split4<PL>(y4, 1.0f, hh);
-                    const int kk = j & 31, at = chunk(i & 31, (kk >> 3) & 1, kk >> 4) + (kk & 4) * 2;
-                    char *unit = X + ((i >> 5) * C + (j >> 5)) * UNIT;
-#pragma unroll
-                    for (int z = 0; z < PL; ++z) *(half4 *)(unit + z * kPlane + at) = hh[z];
-                }
+                pack_block<PL, false>(u[q], v, X, br * 4, bc * 4, f);
             }
         }
         __syncthreads();
     }
 
-    // rows of units `a` times rows `b` of M (K units each), summed into acc by parts
-    auto rows_by_rows = [&](const char *M, int K, int a, int b) {
-        f32x16 acc[PL == 2 ? 3 : 1];
-#pragma unroll
-        for (auto &x : acc)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) x[e] = 0.0f;
-        for (int k = 0; k < K; ++k) {
-            const char *ua = M + (a * K + k) * UNIT, *ub = M + (b * K + k) * UNIT;
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                const half8 fa = frag_rows(ua, lane, s), fb = frag_rows(ub, lane, s);
-                acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa, fb, acc[0], 0, 0, 0);
-                if constexpr (PL == 2) {
-                    const half8 la = frag_rows(ua + kPlane, lane, s), lb = frag_rows(ub + kPlane, lane, s);
-                    acc[1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa, lb, acc[1], 0, 0, 0);
-                    acc[2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(la, fb, acc[2], 0, 0, 0);
-                }
-            }
-        }
-        if constexpr (PL == 2) acc[0] += acc[1] + acc[2];
-        return acc[0];
-    };
     const int tri = R * (R + 1) / 2;
-    auto unit_of = [&](int t, int &a, int &b) {  // t-th unit of the upper triangle
-        a = 0;
-        while (t >= R - a) {
-            t -= R - a;
-            ++a;
+    // t-th unit (b, a), b >= a, of the triangle; past its end the last one, not stored
+    auto unit_of = [&](int t, int &a, int &b) {
+        b = 0;
+        while (t > b) {
+            ++b;
+            t -= b;
         }
-        b = a + t;
+        a = t;
     };
-    // a unit of a symmetric matrix, lane = row b, registers = columns a, and its mirror
-    auto store_pair = [&](const half4 (&out)[4][PL], int a, int b) {
-        char *const at = A + (b * R + a) * UNIT;
-        store_unit<PL>(at, out, n, h);
-        if (a == b) return;
-        __builtin_amdgcn_wave_barrier();
-        char *const mirror = A + (a * R + b) * UNIT;
+    auto zero = [](f32x16 &x) {
 #pragma unroll
-        for (int z = 0; z < PL; ++z)
-#pragma unroll
-            for (int s = 0; s < 2; ++s) *(half8 *)(mirror + z * kPlane + chunk(n, h, s)) = frag_cols(at + z * kPlane, lane, s);
+        for (int e = 0; e < 16; ++e) x[e] = 0.0f;
     };
-
-    constexpr int TRI = PL == 2 ? 2 : 3;  // units of a wave: R <= 4 in pairs of planes, R <= 6 in one
-    constexpr int PAIRS = 3;              // pairs of a wave: R ceil(C / 2) <= 20 for R C <= 40, R <= C (checked below)
-    const int half_c = (C + 1) / 2, pairs = R * half_c;
-    // pair t of units of P X: row a, columns b0 and b1 (b0 again where there is one)
-    auto pair_of = [&](int t, int &a, int &b0, int &b1) {
-        a = t / half_c;
-        b0 = (t - a * half_c) * 2;
-        b1 = b0 + 1 < C ? b0 + 1 : b0;
-    };
-    // along: lane = column of the iterate, otherwise its row
-    auto product = [&](f32x16 (&acc)[2], int a, int b0, int b1, bool along) {
-#pragma unroll
-        for (int y = 0; y < 2; ++y)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[y][e] = 0.0f;
-        for (int k = 0; k < R; ++k) {
-            const char *up = A + (a * R + k) * UNIT, *u0 = X + (k * C + b0) * UNIT, *u1 = X + (k * C + b1) * UNIT;
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                Frag<PL> fp, f0, f1;
-#pragma unroll
-                for (int z = 0; z < PL; ++z) {
-                    fp.p[z] = frag_rows(up + z * kPlane, lane, s);
-                    f0.p[z] = frag_cols(u0 + z * kPlane, lane, s);
-                    f1.p[z] = frag_cols(u1 + z * kPlane, lane, s);
-                }
-                if (along) {
-                    mma<PL>(acc[0], fp, f0);
-                    mma<PL>(acc[1], fp, f1);
-                } else {
-                    mma<PL>(acc[0], f0, fp);
-                    mma<PL>(acc[1], f1, fp);
-                }
+    // sum over k of left(k) right(k), each a loader of the operands of unit column k
+    auto contract = [&](f32x16 &acc, int K, auto left, auto right) {
+        zero(acc);
+        Frag<PL> l[2], r[2];  // one half (16 entries) ahead
+        left(l[0], 0, 0);
+        right(r[0], 0, 0);
+        for (int k = 0; k < K; ++k) {
+            left(l[1], k, 1);
+            right(r[1], k, 1);
+            mma<PL>(acc, l[0], r[0]);
+            if (k + 1 < K) {
+                left(l[0], k + 1, 0);
+                right(r[0], k + 1, 0);
             }
+            mma<PL>(acc, l[1], r[1]);
         }
     };
+    auto x_rows = [&](int a) {
+        return [&, a](Frag<PL> &f, int k, int s) {
+#pragma unroll
+            for (int z = 0; z < PL; ++z) f.p[z] = frag_rows(X + (a * C + k) * UNIT + z * kPlane, lane, s);
+        };
+    };
+    auto x_cols = [&](int b) {
+        return [&, b](Frag<PL> &f, int k, int s) {
+#pragma unroll
+            for (int z = 0; z < PL; ++z) f.p[z] = frag_cols(X + (k * C + b) * UNIT + z * kPlane, lane, s);
+        };
+    };
+    auto a_rows = [&](int a) { return [&, a](Frag<PL> &f, int k, int s) { tri_frag<PL>(f, A, a, k, s, lane); }; };
+
+    constexpr int TRI = PL == 2 ? 1 : 2;  // units of a wave: R <= 4 in pairs of planes, R <= 6 in one
+    constexpr int UNITS = (kSmallUnits + kSmallWaves - 1) / kSmallWaves;
     for (int step = 0; step < p.steps; ++step) {
-        for (int t = wave; t < tri; t += kSmallWaves) {
-            int a, b;
-            unit_of(t, a, b);
-            half4 out[4][PL];
-            pack_unit<PL>(rows_by_rows(X, C, a, b), kUnscale, out);
-            store_pair(out, a, b);
+        // (every address is the lane's part plus the unit's: made anew, or the compiler makes all of them
+        // before the loop and spills them)
+        asm volatile("" : "+v"(lane));
+        h = lane >> 5;
+        n = lane & 31;
+#pragma unroll
+        for (int x = 0; x < TRI; ++x) {
+            const int t = wave + x * kSmallWaves;
+            if (t < tri) {
+                int a, b;
+                unit_of(t, a, b);
+                f32x16 acc;  // lane = row of b, registers = rows of a
+                contract(acc, C, x_rows(a), x_rows(b));
+                half4 out[4][PL];
+                pack_unit<PL>(acc, kUnscale, out);
+                store_unit<PL>(tri_unit<PL>(A, b, a), out, n, h);
+            }
         }
         __syncthreads();
         {
@@ -810,8 +808,9 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
                 if (t < tri) {
                     int a, b;
                     unit_of(t, a, b);
-                    const f32x16 acc = rows_by_rows(A, R, a, b);
-                    const char *at = A + (b * R + a) * UNIT;
+                    f32x16 acc;
+                    contract(acc, R, a_rows(a), a_rows(b));
+                    const char *at = tri_unit<PL>(A, b, a);
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
                         float q[4];
@@ -833,49 +832,40 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
                 if (t < tri) {
                     int a, b;
                     unit_of(t, a, b);
-                    store_pair(out[x], a, b);
+                    store_unit<PL>(tri_unit<PL>(A, b, a), out[x], n, h);
                 }
             }
             __syncthreads();
         }
         if (step + 1 == p.steps) break;
-        half4 out[PAIRS][2][4][PL];
+        half4 out[UNITS][4][PL];
 #pragma unroll
-        for (int x = 0; x < PAIRS; ++x) {
+        for (int x = 0; x < UNITS; ++x) {
             const int t = wave + x * kSmallWaves;
-            if (t < pairs) {
-                int a, b0, b1;
-                pair_of(t, a, b0, b1);
-                f32x16 acc[2];
-                product(acc, a, b0, b1, false);
-#pragma unroll
-                for (int y = 0; y < 2; ++y) pack_unit<PL>(acc[y], 1.0f, out[x][y]);
+            if (t < R * C) {
+                const int a = t / C, b = t - a * C;
+                f32x16 acc;  // lane = row, registers = columns
+                contract(acc, R, x_cols(b), a_rows(a));
+                pack_unit<PL>(acc, 1.0f, out[x]);
             }
         }
         __syncthreads();
 #pragma unroll
-        for (int x = 0; x < PAIRS; ++x) {
+        for (int x = 0; x < UNITS; ++x) {
             const int t = wave + x * kSmallWaves;
-            if (t < pairs) {
-                int a, b0, b1;
-                pair_of(t, a, b0, b1);
-                store_unit<PL>(X + (a * C + b0) * UNIT, out[x][0], n, h);
-                if (b1 != b0) store_unit<PL>(X + (a * C + b1) * UNIT, out[x][1], n, h);
-            }
+            if (t < R * C) store_unit<PL>(X + t * UNIT, out[x], n, h);
         }
         __syncthreads();
     }
     // the last step: the lanes go along the matrix's memory rows
-    for (int t = wave; t < pairs; t += kSmallWaves) {
-        int a, b0, b1;
-        pair_of(t, a, b0, b1);
-        Result<MUON, BF16> r0, r1;
-        r0.before(v, a, b0, h, n);
-        r1.before(v, a, b1, h, n);
-        f32x16 acc[2];
-        product(acc, a, b0, b1, !v.tr);
-        r0.store(v, p, acc[0], a, b0, h, n);
-        if (b1 != b0) r1.store(v, p, acc[1], a, b1, h, n);
+    for (int t = wave; t < R * C; t += kSmallWaves) {
+        const int a = t / C, b = t - a * C;
+        Result<MUON, BF16> res;
+        res.before(v, a, b, h, n);
+        f32x16 acc;
+        if (v.tr) contract(acc, R, x_cols(b), a_rows(a));
+        else contract(acc, R, a_rows(a), x_cols(b));
+        res.store(v, p, acc, a, b, h, n);
     }
 }
 
@@ -897,7 +887,6 @@ constexpr int kWgWaves = 8;
 template <int RB, int PL, bool MUON, bool BF16>
 struct MatrixWg {
     static constexpr int UNIT = PL * kPlane;
-    static constexpr int WA = RB == 8 ? 2 : 1, WB = RB == 8 ? 4 : 2;  // units of a wave's tile of the symmetric products
     static constexpr int STAGE = RB * UNIT, STAGES = 4;               // of the Gram matrix: a unit column of X
     static constexpr int TRI = RB * (RB + 1) / 2;
     static constexpr int LDS = TRI * UNIT > STAGES * STAGE ? TRI * UNIT : STAGES * STAGE;
@@ -918,41 +907,26 @@ struct MatrixWg {
         return g;
     }
 
-    // unit (r, k), r >= k, of the triangle in LDS: row r, contraction k
-    __device__ __forceinline__ char *tri(int r, int k) const { return lds + (r * (r + 1) / 2 + k) * UNIT; }
-    // rows of unit row r, contraction over unit column k, of the symmetric matrix in LDS
-    __device__ __forceinline__ void frag(Frag<PL> &f, int r, int k, int s) const {
-        if (r >= k) {
-            const char *u = tri(r, k);
-#pragma unroll
-            for (int z = 0; z < PL; ++z) f.p[z] = frag_rows(u + z * kPlane, lane, s);
-        } else {
-            const char *u = tri(k, r);
-#pragma unroll
-            for (int z = 0; z < PL; ++z) f.p[z] = frag_cols(u + z * kPlane, lane, s);
-        }
-    }
+    __device__ __forceinline__ char *tri(int r, int k) const { return tri_unit<PL>(lds, r, k); }
+    __device__ __forceinline__ void frag(Frag<PL> &f, int r, int k, int s) const { tri_frag<PL>(f, lds, r, k, s, lane); }
 
-    // The wave's units (i0 + a, j0 + b), b >= a + D, of A = X X^T, then of P in its place
-    template <int D>
-    __device__ __forceinline__ void gram_and_poly(int i0, int j0) const {
-        f32x16 acc[WA][WB];
+    // A = X X^T, then P in its place.  A wave has NU units (ui[u], uj[u]), uj >= ui, of the
+    // triangle, products of the unit rows r[0 .. NR) as which[u] says
+    template <class W>
+    __device__ __forceinline__ void gram_and_poly() const {
+        const W t(wave);
+        f32x16 acc[W::NU];
+        Frag<PL> f[2][W::NR];
         auto zero = [&] {
 #pragma unroll
-            for (int a = 0; a < WA; ++a)
+            for (int u = 0; u < W::NU; ++u)
 #pragma unroll
-                for (int b = 0; b < WB; ++b)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) acc[a][b][e] = 0.0f;
+                for (int e = 0; e < 16; ++e) acc[u][e] = 0.0f;
         };
-        auto products = [&](const Frag<PL> (&fa)[WA], const Frag<PL> (&fb)[WB]) {
+        auto products = [&](const Frag<PL> (&x)[W::NR]) {
 #pragma unroll
-            for (int a = 0; a < WA; ++a)
-#pragma unroll
-                for (int b = 0; b < WB; ++b)
-                    if (b >= a + D) mma<PL>(acc[a][b], fa[a], fb[b]);
+            for (int u = 0; u < W::NU; ++u) mma<PL>(acc[u], x[W::left(u)], x[W::right(u)]);
         };
-        constexpr int B0 = D > 0 ? D : 0;
         const int K = v.C;
         auto copy = [&](int k) {  // unit column k of X: this wave's unit of it
             if (wave < v.R) {
@@ -971,100 +945,114 @@ struct MatrixWg {
             else wait_copies_and_barrier<0>();
             if (k + STAGES - 1 < K) copy(k + STAGES - 1);
             const char *stage = lds + (k % STAGES) * STAGE;
-            if constexpr (D < WB) {
+            if (t.any) {
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    Frag<PL> fa[WA], fb[WB];
+                for (int s = 0; s < 2; ++s)
 #pragma unroll
-                    for (int a = 0; a < WA; ++a)
+                    for (int q = 0; q < W::NR; ++q)
 #pragma unroll
-                        for (int z = 0; z < PL; ++z) fa[a].p[z] = frag_cols(stage + (i0 + a) * UNIT + z * kPlane, lane, s);
-#pragma unroll
-                    for (int b = B0; b < WB; ++b)
-#pragma unroll
-                        for (int z = 0; z < PL; ++z) fb[b].p[z] = frag_cols(stage + (j0 + b) * UNIT + z * kPlane, lane, s);
-                    products(fa, fb);
-                    __builtin_amdgcn_sched_barrier(0);  // (both halves' operands at once do not fit the registers)
-                }
+                        for (int z = 0; z < PL; ++z) f[s][q].p[z] = frag_cols(stage + t.row(q) * UNIT + z * kPlane, lane, s);
+                products(f[0]);
+                products(f[1]);
             }
         }
         wait_copies_and_barrier<0>();  // every wave is past the last stage
-        if constexpr (D < WB) {
+        auto mine = [&](int u) { return t.any && t.row(W::right(u)) < v.R; };
 #pragma unroll
-            for (int a = 0; a < WA; ++a)
-#pragma unroll
-                for (int b = 0; b < WB; ++b)
-                    if (b >= a + D && i0 + a < v.R && j0 + b < v.R) {
-                        half4 out[4][PL];
-                        pack_unit<PL>(acc[a][b], kUnscale, out);
-                        store_unit<PL>(tri(j0 + b, i0 + a), out, n, h);
-                        __builtin_amdgcn_sched_barrier(0);
-                    }
-        }
+        for (int u = 0; u < W::NU; ++u)
+            if (mine(u)) {
+                half4 out[4][PL];
+                pack_unit<PL>(acc[u], kUnscale, out);
+                store_unit<PL>(tri(t.row(W::right(u)), t.row(W::left(u))), out, n, h);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         wait_copies_and_barrier<0>();
-        half4 out[WA][WB][4][PL];
-        if constexpr (D < WB) {
+        half4 out[W::NU][4][PL];
+        if (t.any) {
             zero();
             for (int k = 0; k < v.R; ++k) {
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    Frag<PL> fa[WA], fb[WB];
+                for (int s = 0; s < 2; ++s)
 #pragma unroll
-                    for (int a = 0; a < WA; ++a) frag(fa[a], i0 + a, k, s);
-#pragma unroll
-                    for (int b = B0; b < WB; ++b) frag(fb[b], j0 + b, k, s);
-                    products(fa, fb);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
+                    for (int q = 0; q < W::NR; ++q) frag(f[s][q], t.row(q), k, s);
+                products(f[0]);
+                products(f[1]);
             }
 #pragma unroll
-            for (int a = 0; a < WA; ++a)
+            for (int u = 0; u < W::NU; ++u)
+                if (mine(u)) {
+                    const int i = t.row(W::left(u)), j = t.row(W::right(u));
+                    const char *at = tri(j, i);
 #pragma unroll
-                for (int b = 0; b < WB; ++b)
-                    if (b >= a + D && i0 + a < v.R && j0 + b < v.R) {
-                        const char *at = tri(j0 + b, i0 + a);
+                    for (int g = 0; g < 4; ++g) {
+                        half4 old[PL];
 #pragma unroll
-                        for (int g = 0; g < 4; ++g) {
-                            half4 old[PL];
+                        for (int z = 0; z < PL; ++z)
+                            old[z] = *(const half4 *)(at + z * kPlane + chunk(n, g & 1, g >> 1) + h * 8);
+                        float q[4];
 #pragma unroll
-                            for (int z = 0; z < PL; ++z)
-                                old[z] = *(const half4 *)(at + z * kPlane + chunk(n, g & 1, g >> 1) + h * 8);
-                            float q[4];
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) q[e] = acc[a][b][4 * g + e];
-                            poly4<PL>(q, old, p, i0 + a == j0 + b ? n - 8 * g - 4 * h : -1);
-                            split4<PL>(q, 1.0f, out[a][b][g]);
-                        }
-                        __builtin_amdgcn_sched_barrier(0);
+                        for (int e = 0; e < 4; ++e) q[e] = acc[u][4 * g + e];
+                        poly4<PL>(q, old, p, i == j ? n - 8 * g - 4 * h : -1);
+                        split4<PL>(q, 1.0f, out[u][g]);
                     }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
         }
         wait_copies_and_barrier<0>();  // every wave has read A
-        if constexpr (D < WB) {
 #pragma unroll
-            for (int a = 0; a < WA; ++a)
-#pragma unroll
-                for (int b = 0; b < WB; ++b)
-                    if (b >= a + D && i0 + a < v.R && j0 + b < v.R) store_unit<PL>(tri(j0 + b, i0 + a), out[a][b], n, h);
-        }
+        for (int u = 0; u < W::NU; ++u)
+            if (mine(u)) store_unit<PL>(tri(t.row(W::right(u)), t.row(W::left(u))), out[u], n, h);
         wait_copies_and_barrier<0>();
     }
 
+    // Shares of the triangle.  Eight unit rows: blocks of two of them, waves 0 to 5 the six blocks above the
+    // diagonal (four units of two and two rows), 6 and 7 two of the four on it (three units of two rows each): 8 or 10
+    // units per SIMD (wave % 4).  Four unit rows: one or two units of a row a wave, 2 or 3 per SIMD
+    struct Off {
+        static constexpr int NU = 4, NR = 4;
+        int i, j;
+        static constexpr bool any = true;
+        __device__ __forceinline__ Off(int w) : i(w < 3 ? 0 : w < 5 ? 2 : 4), j(w < 3 ? 2 * w + 2 : w < 5 ? 2 * w - 2 : 6) {}
+        __device__ __forceinline__ int row(int q) const { return q < 2 ? i + q : j + q - 2; }
+        static constexpr int left(int u) { return u >> 1; }
+        static constexpr int right(int u) { return 2 + (u & 1); }
+    };
+    struct Diagonal {
+        static constexpr int NU = 6, NR = 4;
+        int i, j;
+        static constexpr bool any = true;
+        __device__ __forceinline__ Diagonal(int w) : i(w == 6 ? 2 : 0), j(w == 6 ? 6 : 4) {}
+        __device__ __forceinline__ int row(int q) const { return q < 2 ? i + q : j + q - 2; }
+        static constexpr int left(int u) { return 2 * (u / 3) + (u % 3 == 2); }
+        static constexpr int right(int u) { return 2 * (u / 3) + (u % 3 > 0); }
+    };
+    struct Pair {  // units (i, j), (i, j + 1)
+        static constexpr int NU = 2, NR = 3;
+        int i, j;
+        static constexpr bool any = true;
+        __device__ __forceinline__ Pair(int w) : i(w < 2 ? 0 : w - 1), j(w == 0 ? 0 : 2) {}
+        __device__ __forceinline__ int row(int q) const { return q == 0 ? i : j + q - 1; }
+        static constexpr int left(int) { return 0; }
+        static constexpr int right(int u) { return 1 + u; }
+    };
+    struct Single {  // unit (i, i), i = 1, 3; waves 6 and 7 none
+        static constexpr int NU = 1, NR = 1;
+        int i;
+        bool any;
+        __device__ __forceinline__ Single(int w) : i(w == 4 ? 1 : 3), any(w < 6) {}
+        __device__ __forceinline__ int row(int) const { return i; }
+        static constexpr int left(int) { return 0; }
+        static constexpr int right(int) { return 0; }
+    };
+
     __device__ __forceinline__ void make_p() const {
-        // unit row and column of the waves' tiles, those at or above the diagonal shared out
-        // so that no SIMD (wave % 4) has more than 10 of 36 units, or 3 of 10; d = 8: none
-        int i0, j0;
         if constexpr (RB == 8) {
-            i0 = wave == 0 ? 0 : wave == 1 ? 2 : wave == 2 ? 0 : wave == 3 ? 4 : wave == 4 ? 4 : wave == 5 ? 6 : wave == 6 ? 2 : 6;
-            j0 = wave == 0 || wave == 1 || wave == 3 || wave == 7 ? 4 : 0;
+            if (wave < 6) gram_and_poly<Off>();
+            else gram_and_poly<Diagonal>();
         } else {
-            i0 = wave == 0 || wave == 1 ? 0 : wave == 2 || wave == 4 ? 1 : wave == 3 || wave == 6 ? 2 : 3;
-            j0 = wave == 1 || wave == 2 || wave == 3 || wave == 5 ? 2 : 0;
+            if (wave < 4) gram_and_poly<Pair>();  // (0, 0..1), (0, 2..3), (1, 2..3), (2, 2..3)
+            else gram_and_poly<Single>();
         }
-        const int d = i0 - j0;
-        if (d < 0) gram_and_poly<-8>(i0, j0);
-        else if (d == 0) gram_and_poly<0>(i0, j0);
-        else if (d < WB) gram_and_poly<WB / 2>(i0, j0);
-        else gram_and_poly<8>(i0, j0);
     }
 
     // X = P X in place, or (LAST) the result; ALONG: lane = column of the iterate, otherwise its row
