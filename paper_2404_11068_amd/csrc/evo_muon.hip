@@ -470,6 +470,9 @@ __device__ __forceinline__ void wait_copies_and_barrier() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(N) : "memory");
 }
 
+// a barrier for what lies in LDS alone
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
+
 template <int T, int PL, int S, int KIND, bool MUON, bool BF16>
 __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, int odd) {
     constexpr int U = T / 64;             // units of a wave's tile in each direction
@@ -910,6 +913,27 @@ struct MatrixWg {
     __device__ __forceinline__ char *tri(int r, int k) const { return tri_unit<PL>(lds, r, k); }
     __device__ __forceinline__ void frag(Frag<PL> &f, int r, int k, int s) const { tri_frag<PL>(f, lds, r, k, s, lane); }
 
+    // operands of unit rows r and r + 1 for unit column k, one branch for both
+    __device__ __forceinline__ void block_frag(Frag<PL> *f, int r, int k, int s) const {
+        if (k <= r) {
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+#pragma unroll
+                for (int z = 0; z < PL; ++z) f[q].p[z] = frag_rows(tri(r + q, k) + z * kPlane, lane, s);
+        } else if (k > r + 1) {
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+#pragma unroll
+                for (int z = 0; z < PL; ++z) f[q].p[z] = frag_cols(tri(k, r + q) + z * kPlane, lane, s);
+        } else {
+#pragma unroll
+            for (int z = 0; z < PL; ++z) {
+                f[0].p[z] = frag_cols(tri(k, r) + z * kPlane, lane, s);
+                f[1].p[z] = frag_rows(tri(k, k) + z * kPlane, lane, s);
+            }
+        }
+    }
+
     // A = X X^T, then P in its place.  A wave has NU units (ui[u], uj[u]), uj >= ui, of the
     // triangle, products of the unit rows r[0 .. NR) as which[u] says
     template <class W>
@@ -940,19 +964,24 @@ struct MatrixWg {
 #pragma unroll
         for (int k = 0; k < STAGES - 1; ++k)
             if (k < K) copy(k);
+        // f[0] holds the first half of a unit column's operands, f[1] the second, each read while the
+        // other's products run: at stage k the copies of stage k + 1 must have arrived, too
+        auto staged = [&](Frag<PL> (&x)[W::NR], int k, int s) {
+            const char *stage = lds + (k % STAGES) * STAGE;
+#pragma unroll
+            for (int q = 0; q < W::NR; ++q)
+#pragma unroll
+                for (int z = 0; z < PL; ++z) x[q].p[z] = frag_cols(stage + t.row(q) * UNIT + z * kPlane, lane, s);
+        };
         for (int k = 0; k < K; ++k) {
-            if (k + STAGES - 2 < K) wait_copies_and_barrier<(STAGES - 2) * (UNIT / 1024)>();
+            if (k + 2 < K) wait_copies_and_barrier<UNIT / 1024>();
             else wait_copies_and_barrier<0>();
             if (k + STAGES - 1 < K) copy(k + STAGES - 1);
-            const char *stage = lds + (k % STAGES) * STAGE;
             if (t.any) {
-#pragma unroll
-                for (int s = 0; s < 2; ++s)
-#pragma unroll
-                    for (int q = 0; q < W::NR; ++q)
-#pragma unroll
-                        for (int z = 0; z < PL; ++z) f[s][q].p[z] = frag_cols(stage + t.row(q) * UNIT + z * kPlane, lane, s);
+                if (k == 0) staged(f[0], 0, 0);
+                staged(f[1], k, 1);
                 products(f[0]);
+                if (k + 1 < K) staged(f[0], k + 1, 0);
                 products(f[1]);
             }
         }
@@ -966,16 +995,24 @@ struct MatrixWg {
                 store_unit<PL>(tri(t.row(W::right(u)), t.row(W::left(u))), out, n, h);
                 __builtin_amdgcn_sched_barrier(0);
             }
-        wait_copies_and_barrier<0>();
+        lds_barrier();
         half4 out[W::NU][4][PL];
         if (t.any) {
             zero();
+            auto operands = [&](Frag<PL> (&x)[W::NR], int k, int s) {
+                if constexpr (W::BLOCKS) {
+                    block_frag(&x[0], t.row(0), k, s);
+                    block_frag(&x[2], t.row(2), k, s);
+                } else {
+#pragma unroll
+                    for (int q = 0; q < W::NR; ++q) frag(x[q], t.row(q), k, s);
+                }
+            };
+            operands(f[0], 0, 0);
             for (int k = 0; k < v.R; ++k) {
-#pragma unroll
-                for (int s = 0; s < 2; ++s)
-#pragma unroll
-                    for (int q = 0; q < W::NR; ++q) frag(f[s][q], t.row(q), k, s);
+                operands(f[1], k, 1);
                 products(f[0]);
+                if (k + 1 < v.R) operands(f[0], k + 1, 0);
                 products(f[1]);
             }
 #pragma unroll
@@ -998,36 +1035,39 @@ struct MatrixWg {
                     __builtin_amdgcn_sched_barrier(0);
                 }
         }
-        wait_copies_and_barrier<0>();  // every wave has read A
+        lds_barrier();  // every wave has read A
 #pragma unroll
         for (int u = 0; u < W::NU; ++u)
             if (mine(u)) store_unit<PL>(tri(t.row(W::right(u)), t.row(W::left(u))), out[u], n, h);
-        wait_copies_and_barrier<0>();
+        lds_barrier();
     }
 
-    // Shares of the triangle.  Eight unit rows: blocks of two of them, waves 0 to 5 the six blocks above the
-    // diagonal (four units of two and two rows), 6 and 7 two of the four on it (three units of two rows each): 8 or 10
-    // units per SIMD (wave % 4).  Four unit rows: one or two units of a row a wave, 2 or 3 per SIMD
+    // Shares of the triangle.  Eight unit rows: blocks of two of them, waves 2 to 7 the six blocks above the
+    // diagonal (four units of two and two rows), 0 and 1 two of the four on it (three units of two rows each): 8 or 10
+    // units per SIMD (wave % 4), the longer waves the older ones, which the SIMD prefers.  Four unit rows: one or two units of a row a wave, 2 or 3 per SIMD
     struct Off {
         static constexpr int NU = 4, NR = 4;
+        static constexpr bool BLOCKS = true;
         int i, j;
         static constexpr bool any = true;
-        __device__ __forceinline__ Off(int w) : i(w < 3 ? 0 : w < 5 ? 2 : 4), j(w < 3 ? 2 * w + 2 : w < 5 ? 2 * w - 2 : 6) {}
+        __device__ __forceinline__ Off(int w) : i(w < 5 ? 0 : w < 7 ? 2 : 4), j(w < 5 ? 2 * w - 2 : w < 7 ? 2 * w - 6 : 6) {}
         __device__ __forceinline__ int row(int q) const { return q < 2 ? i + q : j + q - 2; }
         static constexpr int left(int u) { return u >> 1; }
         static constexpr int right(int u) { return 2 + (u & 1); }
     };
     struct Diagonal {
         static constexpr int NU = 6, NR = 4;
+        static constexpr bool BLOCKS = true;
         int i, j;
         static constexpr bool any = true;
-        __device__ __forceinline__ Diagonal(int w) : i(w == 6 ? 2 : 0), j(w == 6 ? 6 : 4) {}
+        __device__ __forceinline__ Diagonal(int w) : i(2 * w), j(2 * w + 4) {}
         __device__ __forceinline__ int row(int q) const { return q < 2 ? i + q : j + q - 2; }
         static constexpr int left(int u) { return 2 * (u / 3) + (u % 3 == 2); }
         static constexpr int right(int u) { return 2 * (u / 3) + (u % 3 > 0); }
     };
     struct Pair {  // units (i, j), (i, j + 1)
         static constexpr int NU = 2, NR = 3;
+        static constexpr bool BLOCKS = false;
         int i, j;
         static constexpr bool any = true;
         __device__ __forceinline__ Pair(int w) : i(w < 2 ? 0 : w - 1), j(w == 0 ? 0 : 2) {}
@@ -1037,6 +1077,7 @@ struct MatrixWg {
     };
     struct Single {  // unit (i, i), i = 1, 3; waves 6 and 7 none
         static constexpr int NU = 1, NR = 1;
+        static constexpr bool BLOCKS = false;
         int i;
         bool any;
         __device__ __forceinline__ Single(int w) : i(w == 4 ? 1 : 3), any(w < 6) {}
@@ -1047,21 +1088,22 @@ struct MatrixWg {
 
     __device__ __forceinline__ void make_p() const {
         if constexpr (RB == 8) {
-            if (wave < 6) gram_and_poly<Off>();
-            else gram_and_poly<Diagonal>();
+            if (wave < 2) gram_and_poly<Diagonal>();
+            else gram_and_poly<Off>();
         } else {
             if (wave < 4) gram_and_poly<Pair>();  // (0, 0..1), (0, 2..3), (1, 2..3), (2, 2..3)
             else gram_and_poly<Single>();
         }
     }
 
-    // X = P X in place, or (LAST) the result; ALONG: lane = column of the iterate, otherwise its row
+    // X = P X in place, or (LAST) the result; ALONG: lane = column of the iterate, otherwise its row.
+    // (Two waves with four rows of two columns each read P half as often but X twice, and took a fifth longer.)
     template <bool LAST, bool ALONG>
     __device__ __forceinline__ void apply() const {
+        constexpr int RING = RB > 4 ? 3 : 2;  // units of the column, loaded ahead
         for (int j = wave; j < v.C; j += kWgWaves) {
             char *const col = v.x0 + (int64_t)j * v.R * UNIT;
-            Frag<PL> x[RB > 4 ? 3 : 2][2];  // units of the column, loaded ahead
-            constexpr int RING = RB > 4 ? 3 : 2;
+            Frag<PL> x[RING][2];
             auto load = [&](int k) {
 #pragma unroll
                 for (int s = 0; s < 2; ++s)
@@ -1122,13 +1164,16 @@ ns_matrix_kernel(NsWork w, NsParams p, int first) {
 
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
     const Wg g{p, v, lds, lds0, lane, wave, lane >> 5, lane & 31};
-    for (int step = 0;; ++step) {
+    for (int step = 1;; ++step) {
         g.fresh().make_p();
-        if (step + 1 == p.steps) break;
-        g.fresh().template apply<false, true>();
+        if (step < p.steps) {
+            g.fresh().template apply<false, true>();
+        } else {
+            if (v.tr) g.fresh().template apply<true, false>();
+            else g.fresh().template apply<true, true>();
+            return;
+        }
     }
-    if (v.tr) g.fresh().template apply<true, false>();
-    else g.fresh().template apply<true, true>();
 }
 
 // S stages: with the large tile two workgroups per CU, with the small one enough copies in
