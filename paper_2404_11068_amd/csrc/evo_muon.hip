@@ -1269,8 +1269,10 @@ int64_t ns_matrix_wg_bytes(int64_t rows, int64_t cols, int planes) {
     return (r + 31) / 32 * ((c + 31) / 32) * planes * kPlane;
 }
 
-// A workgroup takes as long for its matrix as tiles on all CUs for about forty of them
-bool ns_by_matrix(double total, double largest) { return total >= 40.0 * largest; }
+// A workgroup takes as long for its matrix as tiles on all CUs for about 70 of them (fp32, by tiles and by
+// workgroups: 64 of 256 x 256 211 and 216 us, 96 272 and 240; 96 of 256 x 1024 590 and 640, 128 778 and 690;
+// 52 of 128 x 512 114 and 124)
+bool ns_by_matrix(double total, double largest) { return total >= 72.0 * largest; }
 
 // 128 x 128 tiles read each staged unit twice as often; once they do not fill
 // the CUs, tiles of a quarter the size do the work sooner

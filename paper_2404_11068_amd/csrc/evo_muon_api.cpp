@@ -104,7 +104,7 @@ struct Lists {
 };
 
 // work of a matrix, about: the products' multiply-adds and the passes over its entries
-double cost(const Size &z) { return (double)z.r * z.r * (3.0 * z.c + z.r) + 1e4 * z.c * z.r; }
+double cost(const Size &z) { return (double)z.r * z.r * (3.0 * z.c + z.r) + 100.0 * z.c * z.r; }
 
 struct Plan {
     PlanHeader h{};

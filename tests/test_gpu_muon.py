@@ -68,8 +68,8 @@ def test_flat_spectrum(m, n, dtype):
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("N,m,n", [(1, 40, 40), (5, 128, 128), (3, 200, 70), (2, 33, 500), (4, 256, 257), (40, 9, 12),
                                    # many enough to be taken a workgroup each, wide and tall, odd, up to 256 rows
-                                   (48, 130, 200), (41, 256, 256), (45, 256, 290), (40, 250, 161), (64, 100, 700), (50, 520, 120),
-                                   (40, 33, 1300), (44, 225, 65 * 9)])
+                                   (78, 130, 200), (73, 256, 256), (72, 256, 290), (75, 250, 161), (74, 100, 700), (80, 520, 120),
+                                   (72, 33, 1300), (72, 225, 585)])
 def test_stacks(N, m, n, dtype):
     print("\n[case] stack", N, m, n, dtype, flush=True)
     rng = np.random.default_rng(N)
@@ -174,7 +174,7 @@ def _flat(lists, shift=0):
     (LIST[:1], True, 0.0, "none", None, 2),
     ([(64, 64)] * 70, True, 0.01, "spectral", 2.0, 0),
     ([(200, 220)] * 3, False, 0.01, "spectral", None, 3),
-    ([(200, 130)] * 45 + [(70, 520)] * 30 + [(600, 90)] * 9 + LIST, True, 0.01, "rms", 0.5, 1),
+    ([(200, 130)] * 190 + [(70, 520)] * 30 + [(600, 90)] * 9 + [(256, 200)] * 20, True, 0.01, "rms", 0.5, 1),
 ])
 def test_muon_step(shapes, nesterov, wd, adjust, gscale, shift):
     """Three steps.  Bounds per element: fp32 roundings of the parameter (a few
