@@ -681,6 +681,7 @@ __device__ __forceinline__ void tri_frag(Frag<PL> &f, char *base, int r, int k, 
 
 constexpr int kSmallUnits = 40;
 constexpr int kSmallLds = 39 * 2 * kPlane;
+static_assert(kSmallLds + 1024 <= 160 * 1024, "X, the triangle and the partial sums fill a workgroup's LDS at most");
 constexpr int kSmallWaves = 16;
 
 template <int PL>
@@ -1256,7 +1257,7 @@ int64_t ns_small_bytes(int64_t rows, int64_t cols, int planes) {
     const int r = (int)(rows < cols ? rows : cols), c = (int)(rows + cols - r);
     const int R = units(r), C = units(c);
     const bool fits = planes == 2 ? fits_small<2>(R, C) : fits_small<1>(R, C);
-    return fits ? (int64_t)(R * C + R * R) * planes * kPlane : 0;
+    return fits ? (int64_t)(R * C + R * (R + 1) / 2) * planes * kPlane : 0;
 }
 
 int ns_matrix_rows(int64_t rows, int64_t cols) {

@@ -84,6 +84,16 @@ def test_stacks(N, m, n, dtype):
     assert op.orthogonalize(y, out=y) is y and torch.equal(y, got)
 
 
+@pytest.mark.parametrize("r,c", [(32, 1216), (64, 576), (96, 352), (128, 224), (160, 170), (192, 192)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_the_most_that_a_workgroup_holds(r, c, dtype):
+    """Sizes at which X and a triangle fill the LDS, one row less, and a unit more, wide and tall."""
+    for m, n in ((r, c), (c, r - 1), (r, c + 1), (c, r + 1)):
+        print("\n[case] orthogonalize", m, n, dtype, flush=True)
+        x = torch.from_numpy(np.random.default_rng(m + n).standard_normal((2, m, n))).to(dtype).cuda()
+        _check(op.orthogonalize(x), mo.orthogonalize(to_f64(x)), dtype, flat=False)
+
+
 @pytest.mark.parametrize("kind", ["rank1", "decay", "zero", "tiny", "huge", "one_entry"])
 @pytest.mark.parametrize("m,n", [(96, 96), (150, 280)])
 def test_hard_spectra(kind, m, n):
