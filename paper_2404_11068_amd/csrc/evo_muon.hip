@@ -3,14 +3,15 @@
 //   X = x / max(|x|_F, eps);  steps times:  A = X X^T,  P = a I + b A + c A A,  X = P X
 //
 // Precision.  A direction that X hardly has grows by up to a^steps = 485, and so do
-// the roundings of the iterate.  fp32 matrices therefore keep every iterate
-// as a pair of fp16 (value = hi + lo, 22 bits) and form each product as hi hi + hi lo + lo hi
+// the roundings of the iterate.  Every iterate is therefore a pair of fp16
+// (value = hi + lo, 22 bits), and each product is hi hi + hi lo + lo hi
 // on the fp16 matrix instructions with fp32 accumulation: the error of fp32
 // arithmetic (1e-6 .. 1e-5 of the result over five steps, low-rank inputs
 // too) at a third of the fp16 rate, which is five times the fp32 matrix rate.
-// bf16 matrices take one fp16 plane: an iterate rounded to 2^-11 costs 2e-3 of
-// the result, about its own rounding to bf16 (with bf16 iterates it would be
-// 1e-2, and all of it for low-rank inputs).  X and A are stored times 2^10:
+// The last two steps of a bf16 matrix use hi alone: what
+// they round is amplified by little, and the result is off by at most 1.2 times
+// its own rounding to bf16.  With hi alone in all steps it would be 2.4 times that for
+// low-rank inputs, with bf16 iterates 1e-2 and more.  X and A are stored times 2^10:
 // their entries stay below 64 (coefficients that could take them further
 // are refused), and those near 1 / sqrt(m n) stay clear of fp16's subnormals.
 //
@@ -31,7 +32,7 @@ typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 
 constexpr float kScale = 1024.0f;        // X and A are stored times this, P as it is: P X needs no scaling
 constexpr float kUnscale = 1.0f / 1024.0f;
-constexpr int kPlane = 2048;                       // bytes of a unit's plane
+constexpr int kPlane = 2048, kPlanes = 2, kUnit = kPlanes * kPlane;  // bytes of a unit's plane, planes, bytes of a unit
 
 __host__ __device__ inline int units(int n) { return (n + 31) / 32; }
 
@@ -46,7 +47,6 @@ struct View {
     char *x0, *x1, *A, *P;
 };
 
-template <int PL>
 __device__ __forceinline__ View view_of(const NsWork &w, int k) {
     View v;
     if (w.mats) {
@@ -63,11 +63,11 @@ __device__ __forceinline__ View view_of(const NsWork &w, int k) {
     v.R = units(v.r);
     v.C = units(v.c);
     v.xt = v.m.by_matrix != 0;
-    const int64_t unit = PL * kPlane, nx = (int64_t)v.R * v.C * unit;
+    const int64_t nx = (int64_t)v.R * v.C * kUnit;
     v.x0 = w.ws + v.m.off;
     v.x1 = v.x0 + nx;
     v.A = v.x1 + nx;
-    v.P = v.A + (int64_t)v.R * v.R * unit;
+    v.P = v.A + (int64_t)v.R * v.R * kUnit;
     return v;
 }
 
@@ -125,14 +125,14 @@ __device__ __forceinline__ half8 frag_cols(const char *plane, int lane, int s) {
 // two at a time, the remainder in one mixed fused multiply-add: 3 operations per value
 typedef float float2v __attribute__((ext_vector_type(2)));
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
-template <int PL>
-__device__ __forceinline__ void split4(const float (&v)[4], float f, half4 (&p)[PL]) {
+template <int NP>
+__device__ __forceinline__ void split4(const float (&v)[4], float f, half4 (&p)[NP]) {
 #pragma unroll
     for (int e = 0; e < 4; e += 2) {
         const half2v hi = __builtin_convertvector((float2v{v[e] * f, v[e + 1] * f}), half2v);
         p[0][e] = hi.x;
         p[0][e + 1] = hi.y;
-        if constexpr (PL == 2) {
+        if constexpr (NP == 2) {
             const half2v lo =
                 __builtin_convertvector((float2v{fmaf(v[e], f, -(float)hi.x), fmaf(v[e + 1], f, -(float)hi.y)}), half2v);
             p[1][e] = lo.x;
@@ -141,11 +141,14 @@ __device__ __forceinline__ void split4(const float (&v)[4], float f, half4 (&p)[
     }
 }
 
-template <int PL> struct Frag { half8 p[PL]; };
+constexpr int kSingleSteps = 2;  // last steps of a bf16 matrix that use one plane
+template <int N> struct Int { static constexpr int value = N; };
 
-template <int PL>
-__device__ __forceinline__ void mma(f32x16 &acc, const Frag<PL> &a, const Frag<PL> &b) {
-    if constexpr (PL == 2) {
+template <int NP> struct Frag { half8 p[NP]; };
+
+template <int NP>
+__device__ __forceinline__ void mma(f32x16 &acc, const Frag<NP> &a, const Frag<NP> &b) {
+    if constexpr (NP == 2) {
         acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a.p[1], b.p[0], acc, 0, 0, 0);
         acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a.p[0], b.p[1], acc, 0, 0, 0);
     }
@@ -215,7 +218,7 @@ __device__ __forceinline__ void load_block(float (&u)[4][4], const View &v, cons
 }
 
 // the thread's entries times f into the units of X, or (TRANSPOSED) of its transpose
-template <int PL, bool TRANSPOSED>
+template <bool TRANSPOSED>
 __device__ __forceinline__ void pack_block(const float (&u)[4][4], const View &v, char *x0, int row0, int col0, double f) {
     const bool by_cols = v.tr != TRANSPOSED;  // a unit's rows are the columns in memory
     const int rows = TRANSPOSED ? v.C : v.R, cols = TRANSPOSED ? v.R : v.C;
@@ -227,22 +230,22 @@ __device__ __forceinline__ void pack_block(const float (&u)[4][4], const View &v
         float q[4];
 #pragma unroll
         for (int y = 0; y < 4; ++y) q[y] = (float)((double)(by_cols ? u[y][x] : u[x][y]) * f);
-        half4 hh[PL];
-        split4<PL>(q, 1.0f, hh);
-        char *unit = x0 + ((int64_t)(i >> 5) * cols + (j >> 5)) * (PL * kPlane);
+        half4 hh[kPlanes];
+        split4(q, 1.0f, hh);
+        char *unit = x0 + ((int64_t)(i >> 5) * cols + (j >> 5)) * kUnit;
         const int k = j & 31, at = chunk(i & 31, (k >> 3) & 1, k >> 4) + (k & 4) * 2;
 #pragma unroll
-        for (int z = 0; z < PL; ++z) *(half4 *)(unit + z * kPlane + at) = hh[z];
+        for (int z = 0; z < kPlanes; ++z) *(half4 *)(unit + z * kPlane + at) = hh[z];
     }
 }
 
 // momentum, and the sum of squares of each tile (fp64: no overflow or underflow of fp32 squares)
-template <bool MUON, bool BF16, int PL>
+template <bool MUON, bool BF16>
 __global__ __launch_bounds__(256) void ns_norm_kernel(NsWork w, NsParams p) {
     __shared__ double red[4];
     const NsTile t = tile_of<false>(w, blockIdx.x);
     if (t.mat < 0) return;
-    const View v = view_of<PL>(w, t.mat);
+    const View v = view_of(w, t.mat);
     const int tid = threadIdx.x;
     const int mi = v.tr ? t.tj : t.ti, mj = v.tr ? t.ti : t.tj;
     float u[4][4];
@@ -262,12 +265,12 @@ __global__ __launch_bounds__(256) void ns_norm_kernel(NsWork w, NsParams p) {
 }
 
 // X = u / max(|u|, eps), in units, transposed for a workgroup's matrix
-template <bool MUON, bool BF16, int PL>
+template <bool MUON, bool BF16>
 __global__ __launch_bounds__(256) void ns_scale_kernel(NsWork w, NsParams p) {
     __shared__ double red[4];
     const NsTile t = tile_of<false>(w, blockIdx.x);
     if (t.mat < 0) return;
-    const View v = view_of<PL>(w, t.mat);
+    const View v = view_of(w, t.mat);
     const int tid = threadIdx.x;
     const int mi = v.tr ? t.tj : t.ti, mj = v.tr ? t.ti : t.tj;
     const int row0 = mi * kNsBlock + (tid >> 4) * 4, col0 = mj * kNsBlock + (tid & 15) * 4;
@@ -284,8 +287,8 @@ __global__ __launch_bounds__(256) void ns_scale_kernel(NsWork w, NsParams p) {
     __syncthreads();
     const double norm = sqrt(((red[0] + red[1]) + red[2]) + red[3]);
     const double f = (double)kScale / (norm < p.eps ? p.eps : norm);
-    if (v.xt) pack_block<PL, true>(u, v, v.x0, row0, col0, f);
-    else pack_block<PL, false>(u, v, v.x0, row0, col0, f);
+    if (v.xt) pack_block<true>(u, v, v.x0, row0, col0, f);
+    else pack_block<false>(u, v, v.x0, row0, col0, f);
 }
 
 // p = decay p - lr scale O, w = sd w + om_sd p, with O as the last product left it in buffer `odd` of X:
@@ -293,7 +296,7 @@ __global__ __launch_bounds__(256) void ns_scale_kernel(NsWork w, NsParams p) {
 __global__ __launch_bounds__(256) void ns_update_kernel(NsWork w, NsParams p, int odd) {
     const NsTile t = tile_of<false>(w, blockIdx.x);
     if (t.mat < 0) return;
-    const View v = view_of<2>(w, t.mat);
+    const View v = view_of(w, t.mat);
     const int tid = threadIdx.x;
     const int mi = v.tr ? t.tj : t.ti, mj = v.tr ? t.ti : t.tj;
     const int row0 = mi * kNsBlock + (tid >> 4) * 4, col0 = mj * kNsBlock + (tid & 15) * 4;
@@ -330,34 +333,34 @@ __global__ __launch_bounds__(256) void ns_update_kernel(NsWork w, NsParams p, in
 
 // entries of P = a I + b A + c A A from those of the product (scale 2^20) and of A (2^10);
 // diagonal: which of the four lies on it, if any
-template <int PL>
-__device__ __forceinline__ void poly4(float (&q)[4], const half4 (&old)[PL], const NsParams &p, int diagonal) {
+template <int NP>
+__device__ __forceinline__ void poly4(float (&q)[4], const half4 (&old)[NP], const NsParams &p, int diagonal) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         float o = (float)old[0][e];
-        if constexpr (PL == 2) o += (float)old[1][e];
+        if constexpr (NP == 2) o += (float)old[1][e];
         q[e] = fmaf(p.c * (kUnscale * kUnscale), q[e], p.b * kUnscale * o);
         q[e] += e == diagonal ? p.a : 0.0f;
     }
 }
 
 // acc (a unit: lane = row, registers = columns) times f as packed quarters
-template <int PL>
-__device__ __forceinline__ void pack_unit(const f32x16 &acc, float f, half4 (&out)[4][PL]) {
+template <int NP>
+__device__ __forceinline__ void pack_unit(const f32x16 &acc, float f, half4 (&out)[4][NP]) {
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
         float q[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) q[e] = acc[4 * g + e];
-        split4<PL>(q, f, out[g]);
+        split4(q, f, out[g]);
     }
 }
-template <int PL>
-__device__ __forceinline__ void store_unit(char *unit, const half4 (&out)[4][PL], int n, int h) {
+template <int NP>
+__device__ __forceinline__ void store_unit(char *unit, const half4 (&out)[4][NP], int n, int h) {
 #pragma unroll
     for (int g = 0; g < 4; ++g)
 #pragma unroll
-        for (int z = 0; z < PL; ++z) *(half4 *)(unit + z * kPlane + chunk(n, g & 1, g >> 1) + h * 8) = out[g][z];
+        for (int z = 0; z < NP; ++z) *(half4 *)(unit + z * kPlane + chunk(n, g & 1, g >> 1) + h * 8) = out[g][z];
 }
 
 // One unit's entries of the result, the lanes along the memory rows.  A buffer begins at the unit's
@@ -473,18 +476,18 @@ __device__ __forceinline__ void wait_copies_and_barrier() {
 // a barrier for what lies in LDS alone
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
 
-template <int T, int PL, int S, int KIND, bool MUON, bool BF16>
+template <int T, int NP, int S, int KIND, bool MUON, bool BF16>
 __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, int odd) {
     constexpr int U = T / 64;             // units of a wave's tile in each direction
     constexpr int N = T / 32;             // units of the workgroup's
-    constexpr int UNIT = PL * kPlane;
-    constexpr int STAGE = 2 * N * UNIT;
-    constexpr int COPIES = U * UNIT / 1024;  // of a wave and stage
+    constexpr int HELD = NP * kPlane;     // bytes of a unit in LDS
+    constexpr int STAGE = 2 * N * HELD;
+    constexpr int COPIES = U * HELD / 1024;  // of a wave and stage
     constexpr bool SQUARE = KIND == kGram || KIND == kPoly;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const NsTile t = tile_of<SQUARE>(w, blockIdx.x);
     if (t.mat < 0) return;
-    const View v = view_of<PL>(w, t.mat);
+    const View v = view_of(w, t.mat);
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wr = wave >> 1, wc = wave & 1, h = lane >> 5, n = lane & 31;
@@ -501,26 +504,26 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, i
         const int first = (op == 0 ? t.ti : t.tj) * N + k;
         if (SQUARE) {
             const int row = first < v.R ? first : v.R - 1;
-            src[q] = x + (int64_t)row * K * UNIT;
-            step = UNIT;
+            src[q] = x + (int64_t)row * K * kUnit;
+            step = kUnit;
         } else if (op == 0) {
             const int row = first < v.R ? first : v.R - 1;
-            src[q] = v.P + (int64_t)row * v.R * UNIT;
-            step = UNIT;
+            src[q] = v.P + (int64_t)row * v.R * kUnit;
+            step = kUnit;
         } else {
             const int col = first < v.C ? first : v.C - 1;
-            src[q] = x + (int64_t)col * UNIT;
-            step = (int64_t)v.C * UNIT;
+            src[q] = x + (int64_t)col * kUnit;
+            step = (int64_t)v.C * kUnit;
         }
     }
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
     auto copy_stage = [&](int k) {
-        const uint32_t dst = lds0 + (uint32_t)(k % S) * STAGE + (uint32_t)(wave * U) * UNIT;
+        const uint32_t dst = lds0 + (uint32_t)(k % S) * STAGE + (uint32_t)(wave * U) * HELD;
 #pragma unroll
         for (int q = 0; q < U; ++q)
 #pragma unroll
-            for (int e = 0; e < UNIT / 1024; ++e)
-                copy_to_lds(scalar(src[q] + k * step), (uint32_t)(e * 1024 + lane * 16), dst + q * UNIT + e * 1024);
+            for (int e = 0; e < HELD / 1024; ++e)
+                copy_to_lds(scalar(src[q] + k * step), (uint32_t)(e * 1024 + lane * 16), dst + q * HELD + e * 1024);
     };
 
     f32x16 acc[U][U];  // [row unit or, where the operands are swapped, ...]: see below
@@ -543,24 +546,24 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, i
             if (k + S - 2 < K) wait_copies_and_barrier<(S - 2) * COPIES>();
             else wait_copies_and_barrier<0>();
             if (k + S - 1 < K) copy_stage(k + S - 1);
-            const char *s0 = lds + (k % S) * STAGE + wr * U * UNIT, *s1 = lds + (k % S) * STAGE + (N + wc * U) * UNIT;
+            const char *s0 = lds + (k % S) * STAGE + wr * U * HELD, *s1 = lds + (k % S) * STAGE + (N + wc * U) * HELD;
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
-                Frag<PL> f0[U], f1[U];
+                Frag<NP> f0[U], f1[U];
 #pragma unroll
                 for (int a = 0; a < U; ++a)
 #pragma unroll
-                    for (int q = 0; q < PL; ++q) {
-                        f0[a].p[q] = frag_rows(s0 + a * UNIT + q * kPlane, lane, s);
-                        f1[a].p[q] = SQUARE ? frag_rows(s1 + a * UNIT + q * kPlane, lane, s)
-                                            : frag_cols(s1 + a * UNIT + q * kPlane, lane, s);
+                    for (int q = 0; q < NP; ++q) {
+                        f0[a].p[q] = frag_rows(s0 + a * HELD + q * kPlane, lane, s);
+                        f1[a].p[q] = SQUARE ? frag_rows(s1 + a * HELD + q * kPlane, lane, s)
+                                            : frag_cols(s1 + a * HELD + q * kPlane, lane, s);
                     }
 #pragma unroll
                 for (int a = 0; a < U; ++a)
 #pragma unroll
                     for (int b = 0; b < U; ++b) {
-                        if constexpr (decltype(swapped)::value) mma<PL>(acc[a][b], f1[b], f0[a]);
-                        else mma<PL>(acc[a][b], f0[a], f1[b]);
+                        if constexpr (decltype(swapped)::value) mma(acc[a][b], f1[b], f0[a]);
+                        else mma(acc[a][b], f0[a], f1[b]);
                     }
             }
         }
@@ -570,7 +573,7 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, i
         // lane = column: stored as row `column` of the symmetric matrix's unit (j, i)
         products(No{});
         __syncthreads();  // the stages become scratch
-        char *const scratch = lds + wave * UNIT;
+        char *const scratch = lds + wave * HELD;
         char *const dst = KIND == kPoly ? v.P : v.A;
 #pragma unroll
         for (int a = 0; a < U; ++a)
@@ -578,8 +581,8 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, i
             for (int b = 0; b < U; ++b) {
                 const int i = i0 + a, j = j0 + b;
                 if (i >= v.R || j >= v.R) continue;  // wave-uniform
-                const int64_t at = ((int64_t)j * v.R + i) * UNIT;
-                half4 out[4][PL];
+                const int64_t at = ((int64_t)j * v.R + i) * kUnit;
+                half4 out[4][NP];
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {  // rows 8 g + 4 h .. + 3 of the tile
                     const int pos = chunk(n, g & 1, g >> 1) + h * 8;
@@ -587,25 +590,25 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, i
 #pragma unroll
                     for (int e = 0; e < 4; ++e) q[e] = acc[a][b][4 * g + e];
                     if constexpr (KIND == kPoly) {
-                        half4 old[PL];
+                        half4 old[NP];
 #pragma unroll
-                        for (int z = 0; z < PL; ++z) old[z] = *(const half4 *)(v.A + at + z * kPlane + pos);
-                        poly4<PL>(q, old, p, i == j ? n - 8 * g - 4 * h : -1);
+                        for (int z = 0; z < NP; ++z) old[z] = *(const half4 *)(v.A + at + z * kPlane + pos);
+                        poly4(q, old, p, i == j ? n - 8 * g - 4 * h : -1);
                     }
-                    split4<PL>(q, KIND == kPoly ? 1.0f : kUnscale, out[g]);
+                    split4(q, KIND == kPoly ? 1.0f : kUnscale, out[g]);
 #pragma unroll
-                    for (int z = 0; z < PL; ++z) *(half4 *)(dst + at + z * kPlane + pos) = out[g][z];
+                    for (int z = 0; z < NP; ++z) *(half4 *)(dst + at + z * kPlane + pos) = out[g][z];
                 }
                 if (t.ti != t.tj) {  // the mirrored unit (i, j), through LDS by columns
 #pragma unroll
                     for (int g = 0; g < 4; ++g)
 #pragma unroll
-                        for (int z = 0; z < PL; ++z)
+                        for (int z = 0; z < NP; ++z)
                             *(half4 *)(scratch + z * kPlane + chunk(n, g & 1, g >> 1) + h * 8) = out[g][z];
                     __builtin_amdgcn_wave_barrier();
-                    const int64_t mirrored = ((int64_t)i * v.R + j) * UNIT;
+                    const int64_t mirrored = ((int64_t)i * v.R + j) * kUnit;
 #pragma unroll
-                    for (int z = 0; z < PL; ++z)
+                    for (int z = 0; z < NP; ++z)
 #pragma unroll
                         for (int s = 0; s < 2; ++s)
                             *(half8 *)(dst + mirrored + z * kPlane + chunk(n, h, s)) = frag_cols(scratch + z * kPlane, lane, s);
@@ -621,16 +624,16 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, i
             for (int b = 0; b < U; ++b) {
                 const int i = i0 + a, j = j0 + b;
                 if (i >= v.R || j >= v.C) continue;
-                char *unit = dst + ((int64_t)i * v.C + j) * UNIT;
+                char *unit = dst + ((int64_t)i * v.C + j) * kUnit;
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
                     float q[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) q[e] = acc[a][b][4 * g + e];
-                    half4 out[PL];
-                    split4<PL>(q, 1.0f, out);
+                    half4 out[NP];
+                    split4(q, 1.0f, out);
 #pragma unroll
-                    for (int z = 0; z < PL; ++z)
+                    for (int z = 0; z < NP; ++z)
                         *(half4 *)(unit + z * kPlane + chunk(n, g & 1, g >> 1) + h * 8) = out[z];
                 }
             }
@@ -644,35 +647,34 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, i
             for (int b = 0; b < U; ++b) {
                 const int i = i0 + a, j = j0 + b;
                 if (i >= v.R || j >= v.C) continue;
-                store_last<MUON, BF16>(v, p, acc[a][b], (odd ? v.x0 : v.x1) + ((int64_t)i * v.C + j) * UNIT, i, j, h, n);
+                store_last<MUON, BF16>(v, p, acc[a][b], (odd ? v.x0 : v.x1) + ((int64_t)i * v.C + j) * kUnit, i, j, h, n);
             }
     }
 }
 
 // A symmetric matrix in LDS as the units of one triangle: unit (r, k), r >= k, holds rows r, contraction
 // k.  An operand of the other triangle is the mirrored unit read by columns
-template <int PL>
 __device__ __forceinline__ char *tri_unit(char *base, int r, int k) {
-    return base + (r * (r + 1) / 2 + k) * (PL * kPlane);
+    return base + (r * (r + 1) / 2 + k) * kUnit;
 }
 // rows of unit row r, contraction over unit column k (both wave-uniform)
-template <int PL>
-__device__ __forceinline__ void tri_frag(Frag<PL> &f, char *base, int r, int k, int s, int lane) {
+template <int NP>
+__device__ __forceinline__ void tri_frag(Frag<NP> &f, char *base, int r, int k, int s, int lane) {
     if (r >= k) {
-        const char *u = tri_unit<PL>(base, r, k);
+        const char *u = tri_unit(base, r, k);
 #pragma unroll
-        for (int z = 0; z < PL; ++z) f.p[z] = frag_rows(u + z * kPlane, lane, s);
+        for (int z = 0; z < NP; ++z) f.p[z] = frag_rows(u + z * kPlane, lane, s);
     } else {
-        const char *u = tri_unit<PL>(base, k, r);
+        const char *u = tri_unit(base, k, r);
 #pragma unroll
-        for (int z = 0; z < PL; ++z) f.p[z] = frag_cols(u + z * kPlane, lane, s);
+        for (int z = 0; z < NP; ++z) f.p[z] = frag_cols(u + z * kPlane, lane, s);
     }
 }
 
 // ---- matrices that fit into LDS: everything in one workgroup
 //
-// X and the triangle of A, then of P in its place, lie in LDS: 128 x 224 entries in pairs
-// of planes, 64 x 608, 32 x 1216.  A product's results wait in registers until every
+// X and the triangle of A, then of P in its place, lie in LDS: 128 x 224 entries, 64 x 576,
+// 32 x 1216.  A product's results wait in registers until every
 // wave has read its operands.  One launch does the norm, the steps and the
 // update: memory sees each entry once.  Each of 16 waves takes a unit of the
 // triangle (10 of them at 128 x 128) and one to three of X; what bounds it is
@@ -680,27 +682,26 @@ __device__ __forceinline__ void tri_frag(Frag<PL> &f, char *base, int r, int k, 
 // storing, so the next operands are read before the matrix instructions of the last.
 
 constexpr int kSmallUnits = 40;
-constexpr int kSmallLds = 39 * 2 * kPlane;
+constexpr int kSmallLds = 39 * kUnit;
 static_assert(kSmallLds + 1024 <= 160 * 1024, "X, the triangle and the partial sums fill a workgroup's LDS at most");
 constexpr int kSmallWaves = 16;
 
-template <int PL>
 __host__ __device__ inline bool fits_small(int R, int C) {
-    return R * C <= kSmallUnits && R <= 6 && (R * C + R * (R + 1) / 2) * PL * kPlane <= kSmallLds;
+    return R * C <= kSmallUnits && (R * C + R * (R + 1) / 2) * kUnit <= kSmallLds;
 }
 
-template <bool MUON, bool BF16, int PL>
+template <bool MUON, bool BF16>
 __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, NsParams p, int first) {
-    constexpr int UNIT = PL * kPlane, THREADS = 64 * kSmallWaves;
+    constexpr int THREADS = 64 * kSmallWaves;
     constexpr int BLOCKS = (kSmallUnits * 64 + THREADS - 1) / THREADS;  // 4 x 4 blocks of a thread
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     __shared__ double red[kSmallWaves];
-    const View v = view_of<PL>(w, first + blockIdx.x);
+    const View v = view_of(w, first + blockIdx.x);
     const int tid = threadIdx.x;
     int lane = tid & 63, h = lane >> 5, n = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int R = v.R, C = v.C;
-    char *const X = lds, *const A = lds + R * C * UNIT;
+    char *const X = lds, *const A = lds + R * C * kUnit;
 
     {  // X = u / max(|u|, eps)
         const int per_row = 8 * (v.tr ? R : C), blocks = 64 * R * C;
@@ -731,7 +732,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
             const int k = q * THREADS + tid;
             if (k < blocks) {
                 const int br = k / per_row, bc = k - br * per_row;
-                pack_block<PL, false>(u[q], v, X, br * 4, bc * 4, f);
+                pack_block<false>(u[q], v, X, br * 4, bc * 4, f);
             }
         }
         __syncthreads();
@@ -752,124 +753,118 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
         for (int e = 0; e < 16; ++e) x[e] = 0.0f;
     };
     // sum over k of left(k) right(k), each a loader of the operands of unit column k
-    auto contract = [&](f32x16 &acc, int K, auto left, auto right) {
+    auto contract = [&](auto np, f32x16 &acc, int K, auto left, auto right) {
         zero(acc);
-        Frag<PL> l[2], r[2];  // one half (16 entries) ahead
+        Frag<decltype(np)::value> l[2], r[2];  // one half (16 entries) ahead
         left(l[0], 0, 0);
         right(r[0], 0, 0);
         for (int k = 0; k < K; ++k) {
             left(l[1], k, 1);
             right(r[1], k, 1);
-            mma<PL>(acc, l[0], r[0]);
+            mma(acc, l[0], r[0]);
             if (k + 1 < K) {
                 left(l[0], k + 1, 0);
                 right(r[0], k + 1, 0);
             }
-            mma<PL>(acc, l[1], r[1]);
+            mma(acc, l[1], r[1]);
         }
     };
     auto x_rows = [&](int a) {
-        return [&, a](Frag<PL> &f, int k, int s) {
+        return [&, a](auto &f, int k, int s) {
 #pragma unroll
-            for (int z = 0; z < PL; ++z) f.p[z] = frag_rows(X + (a * C + k) * UNIT + z * kPlane, lane, s);
+            for (int z = 0; z < (int)(sizeof(f.p) / sizeof(f.p[0])); ++z) f.p[z] = frag_rows(X + (a * C + k) * kUnit + z * kPlane, lane, s);
         };
     };
     auto x_cols = [&](int b) {
-        return [&, b](Frag<PL> &f, int k, int s) {
+        return [&, b](auto &f, int k, int s) {
 #pragma unroll
-            for (int z = 0; z < PL; ++z) f.p[z] = frag_cols(X + (k * C + b) * UNIT + z * kPlane, lane, s);
+            for (int z = 0; z < (int)(sizeof(f.p) / sizeof(f.p[0])); ++z) f.p[z] = frag_cols(X + (k * C + b) * kUnit + z * kPlane, lane, s);
         };
     };
-    auto a_rows = [&](int a) { return [&, a](Frag<PL> &f, int k, int s) { tri_frag<PL>(f, A, a, k, s, lane); }; };
+    auto a_rows = [&](int a) { return [&, a](auto &f, int k, int s) { tri_frag(f, A, a, k, s, lane); }; };
 
-    constexpr int TRI = PL == 2 ? 1 : 2;  // units of a wave: R <= 4 in pairs of planes, R <= 6 in one
+    const bool mine = wave < tri;  // (R <= 4: ten units at most)
+    int ta, tb;
+    unit_of(mine ? wave : 0, ta, tb);
     constexpr int UNITS = (kSmallUnits + kSmallWaves - 1) / kSmallWaves;
-    for (int step = 0; step < p.steps; ++step) {
+    // a step on NP planes; the last leaves P
+    auto one_step = [&](auto np, bool last) {
+        constexpr int NP = decltype(np)::value;
         // (every address is the lane's part plus the unit's: made anew, or the compiler makes all of them
         // before the loop and spills them)
         asm volatile("" : "+v"(lane));
         h = lane >> 5;
         n = lane & 31;
-#pragma unroll
-        for (int x = 0; x < TRI; ++x) {
-            const int t = wave + x * kSmallWaves;
-            if (t < tri) {
-                int a, b;
-                unit_of(t, a, b);
-                f32x16 acc;  // lane = row of b, registers = rows of a
-                contract(acc, C, x_rows(a), x_rows(b));
-                half4 out[4][PL];
-                pack_unit<PL>(acc, kUnscale, out);
-                store_unit<PL>(tri_unit<PL>(A, b, a), out, n, h);
-            }
+        char *const at = tri_unit(A, tb, ta);
+        if (mine) {
+            f32x16 acc;  // lane = row of tb, registers = rows of ta
+            contract(np, acc, C, x_rows(ta), x_rows(tb));
+            half4 out[4][NP];
+            pack_unit(acc, kUnscale, out);
+            store_unit(at, out, n, h);
         }
         __syncthreads();
         {
-            half4 out[TRI][4][PL];
+            half4 out[4][NP];
+            if (mine) {
+                f32x16 acc;
+                contract(np, acc, R, a_rows(ta), a_rows(tb));
 #pragma unroll
-            for (int x = 0; x < TRI; ++x) {
-                const int t = wave + x * kSmallWaves;
-                if (t < tri) {
-                    int a, b;
-                    unit_of(t, a, b);
-                    f32x16 acc;
-                    contract(acc, R, a_rows(a), a_rows(b));
-                    const char *at = tri_unit<PL>(A, b, a);
+                for (int g = 0; g < 4; ++g) {
+                    float q[4];
 #pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        float q[4];
+                    for (int e = 0; e < 4; ++e) q[e] = acc[4 * g + e];
+                    half4 old[NP];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) q[e] = acc[4 * g + e];
-                        half4 old[PL];
-#pragma unroll
-                        for (int z = 0; z < PL; ++z)
-                            old[z] = *(const half4 *)(at + z * kPlane + chunk(n, g & 1, g >> 1) + h * 8);
-                        poly4<PL>(q, old, p, a == b ? n - 8 * g - 4 * h : -1);
-                        split4<PL>(q, 1.0f, out[x][g]);
-                    }
+                    for (int z = 0; z < NP; ++z)
+                        old[z] = *(const half4 *)(at + z * kPlane + chunk(n, g & 1, g >> 1) + h * 8);
+                    poly4(q, old, p, ta == tb ? n - 8 * g - 4 * h : -1);
+                    split4(q, 1.0f, out[g]);
                 }
             }
             __syncthreads();
-#pragma unroll
-            for (int x = 0; x < TRI; ++x) {
-                const int t = wave + x * kSmallWaves;
-                if (t < tri) {
-                    int a, b;
-                    unit_of(t, a, b);
-                    store_unit<PL>(tri_unit<PL>(A, b, a), out[x], n, h);
-                }
-            }
+            if (mine) store_unit(at, out, n, h);
             __syncthreads();
         }
-        if (step + 1 == p.steps) break;
-        half4 out[UNITS][4][PL];
+        if (last) return;
+        half4 out[UNITS][4][NP];
 #pragma unroll
         for (int x = 0; x < UNITS; ++x) {
             const int t = wave + x * kSmallWaves;
             if (t < R * C) {
                 const int a = t / C, b = t - a * C;
                 f32x16 acc;  // lane = row, registers = columns
-                contract(acc, R, x_cols(b), a_rows(a));
-                pack_unit<PL>(acc, 1.0f, out[x]);
+                contract(np, acc, R, x_cols(b), a_rows(a));
+                pack_unit(acc, 1.0f, out[x]);
             }
         }
         __syncthreads();
 #pragma unroll
         for (int x = 0; x < UNITS; ++x) {
             const int t = wave + x * kSmallWaves;
-            if (t < R * C) store_unit<PL>(X + t * UNIT, out[x], n, h);
+            if (t < R * C) store_unit(X + t * kUnit, out[x], n, h);
         }
         __syncthreads();
-    }
-    // the last step: the lanes go along the matrix's memory rows
-    for (int t = wave; t < R * C; t += kSmallWaves) {
-        const int a = t / C, b = t - a * C;
-        Result<MUON, BF16> res;
-        res.before(v, a, b, h, n);
-        f32x16 acc;
-        if (v.tr) contract(acc, R, x_cols(b), a_rows(a));
-        else contract(acc, R, a_rows(a), x_cols(b));
-        res.store(v, p, acc, a, b, h, n);
+    };
+    // the last step's P X: the lanes go along the matrix's memory rows
+    auto result = [&](auto np) {
+        for (int t = wave; t < R * C; t += kSmallWaves) {
+            const int a = t / C, b = t - a * C;
+            Result<MUON, BF16> res;
+            res.before(v, a, b, h, n);
+            f32x16 acc;
+            if (v.tr) contract(np, acc, R, x_cols(b), a_rows(a));
+            else contract(np, acc, R, a_rows(a), x_cols(b));
+            res.store(v, p, acc, a, b, h, n);
+        }
+    };
+    const int in_pairs = BF16 ? p.steps - kSingleSteps : p.steps;  // see the top
+    for (int step = 0; step < in_pairs; ++step) one_step(Int<2>{}, step + 1 == p.steps);
+    if constexpr (BF16) {
+        for (int step = in_pairs > 0 ? in_pairs : 0; step < p.steps; ++step) one_step(Int<1>{}, step + 1 == p.steps);
+        result(Int<1>{});
+    } else {
+        result(Int<2>{});
     }
 }
 
@@ -878,7 +873,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
 // A workgroup of eight waves takes a matrix through all steps.  (The norm, the
 // scaling and Muon's update are passes of their own: a CU by itself keeps too little in flight for them.)  The Gram
 // matrix and then P lie in LDS, as the units of one triangle (36 of them, 144
-// KB, for 256 rows in pairs of planes): an operand of the other triangle is the mirrored
+// KB, for 256 rows): an operand of the other triangle is the mirrored
 // unit read by columns.  X lies in the workspace, transposed, so that the
 // fragments of P X come straight from memory, 1 KB a load: each wave takes unit
 // columns of its own and writes the result in their place, without a barrier.  Memory
@@ -888,12 +883,11 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
 
 constexpr int kWgWaves = 8;
 
-template <int RB, int PL, bool MUON, bool BF16>
+template <int RB, bool MUON, bool BF16>
 struct MatrixWg {
-    static constexpr int UNIT = PL * kPlane;
-    static constexpr int STAGE = RB * UNIT, STAGES = 4;               // of the Gram matrix: a unit column of X
+    static constexpr int STAGE = RB * kUnit, STAGES = 4;               // of the Gram matrix: a unit column of X
     static constexpr int TRI = RB * (RB + 1) / 2;
-    static constexpr int LDS = TRI * UNIT > STAGES * STAGE ? TRI * UNIT : STAGES * STAGE;
+    static constexpr int LDS = TRI * kUnit > STAGES * STAGE ? TRI * kUnit : STAGES * STAGE;
 
     const NsParams &p;
     const View &v;
@@ -911,24 +905,26 @@ struct MatrixWg {
         return g;
     }
 
-    __device__ __forceinline__ char *tri(int r, int k) const { return tri_unit<PL>(lds, r, k); }
-    __device__ __forceinline__ void frag(Frag<PL> &f, int r, int k, int s) const { tri_frag<PL>(f, lds, r, k, s, lane); }
+    __device__ __forceinline__ char *tri(int r, int k) const { return tri_unit(lds, r, k); }
+    template <int NP>
+    __device__ __forceinline__ void frag(Frag<NP> &f, int r, int k, int s) const { tri_frag(f, lds, r, k, s, lane); }
 
     // operands of unit rows r and r + 1 for unit column k, one branch for both
-    __device__ __forceinline__ void block_frag(Frag<PL> *f, int r, int k, int s) const {
+    template <int NP>
+    __device__ __forceinline__ void block_frag(Frag<NP> *f, int r, int k, int s) const {
         if (k <= r) {
 #pragma unroll
             for (int q = 0; q < 2; ++q)
 #pragma unroll
-                for (int z = 0; z < PL; ++z) f[q].p[z] = frag_rows(tri(r + q, k) + z * kPlane, lane, s);
+                for (int z = 0; z < NP; ++z) f[q].p[z] = frag_rows(tri(r + q, k) + z * kPlane, lane, s);
         } else if (k > r + 1) {
 #pragma unroll
             for (int q = 0; q < 2; ++q)
 #pragma unroll
-                for (int z = 0; z < PL; ++z) f[q].p[z] = frag_cols(tri(k, r + q) + z * kPlane, lane, s);
+                for (int z = 0; z < NP; ++z) f[q].p[z] = frag_cols(tri(k, r + q) + z * kPlane, lane, s);
         } else {
 #pragma unroll
-            for (int z = 0; z < PL; ++z) {
+            for (int z = 0; z < NP; ++z) {
                 f[0].p[z] = frag_cols(tri(k, r) + z * kPlane, lane, s);
                 f[1].p[z] = frag_rows(tri(k, k) + z * kPlane, lane, s);
             }
@@ -937,28 +933,28 @@ struct MatrixWg {
 
     // A = X X^T, then P in its place.  A wave has NU units (ui[u], uj[u]), uj >= ui, of the
     // triangle, products of the unit rows r[0 .. NR) as which[u] says
-    template <class W>
+    template <class W, int NP>
     __device__ __forceinline__ void gram_and_poly() const {
         const W t(wave);
         f32x16 acc[W::NU];
-        Frag<PL> f[2][W::NR];
+        Frag<NP> f[2][W::NR];
         auto zero = [&] {
 #pragma unroll
             for (int u = 0; u < W::NU; ++u)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) acc[u][e] = 0.0f;
         };
-        auto products = [&](const Frag<PL> (&x)[W::NR]) {
+        auto products = [&](const Frag<NP> (&x)[W::NR]) {
 #pragma unroll
-            for (int u = 0; u < W::NU; ++u) mma<PL>(acc[u], x[W::left(u)], x[W::right(u)]);
+            for (int u = 0; u < W::NU; ++u) mma(acc[u], x[W::left(u)], x[W::right(u)]);
         };
         const int K = v.C;
         auto copy = [&](int k) {  // unit column k of X: this wave's unit of it
             if (wave < v.R) {
-                const char *src = scalar(v.x0 + ((int64_t)k * v.R + wave) * UNIT);
-                const uint32_t dst = lds0 + (uint32_t)(k % STAGES) * STAGE + wave * UNIT;
+                const char *src = scalar(v.x0 + ((int64_t)k * v.R + wave) * kUnit);
+                const uint32_t dst = lds0 + (uint32_t)(k % STAGES) * STAGE + wave * kUnit;
 #pragma unroll
-                for (int e = 0; e < UNIT / 1024; ++e) copy_to_lds(src, (uint32_t)(e * 1024 + lane * 16), dst + e * 1024);
+                for (int e = 0; e < NP * kPlane / 1024; ++e) copy_to_lds(src, (uint32_t)(e * 1024 + lane * 16), dst + e * 1024);
             }
         };
         zero();
@@ -967,15 +963,15 @@ struct MatrixWg {
             if (k < K) copy(k);
         // f[0] holds the first half of a unit column's operands, f[1] the second, each read while the
         // other's products run: at stage k the copies of stage k + 1 must have arrived, too
-        auto staged = [&](Frag<PL> (&x)[W::NR], int k, int s) {
+        auto staged = [&](Frag<NP> (&x)[W::NR], int k, int s) {
             const char *stage = lds + (k % STAGES) * STAGE;
 #pragma unroll
             for (int q = 0; q < W::NR; ++q)
 #pragma unroll
-                for (int z = 0; z < PL; ++z) x[q].p[z] = frag_cols(stage + t.row(q) * UNIT + z * kPlane, lane, s);
+                for (int z = 0; z < NP; ++z) x[q].p[z] = frag_cols(stage + t.row(q) * kUnit + z * kPlane, lane, s);
         };
         for (int k = 0; k < K; ++k) {
-            if (k + 2 < K) wait_copies_and_barrier<UNIT / 1024>();
+            if (k + 2 < K) wait_copies_and_barrier<NP * kPlane / 1024>();
             else wait_copies_and_barrier<0>();
             if (k + STAGES - 1 < K) copy(k + STAGES - 1);
             if (t.any) {
@@ -991,16 +987,16 @@ struct MatrixWg {
 #pragma unroll
         for (int u = 0; u < W::NU; ++u)
             if (mine(u)) {
-                half4 out[4][PL];
-                pack_unit<PL>(acc[u], kUnscale, out);
-                store_unit<PL>(tri(t.row(W::right(u)), t.row(W::left(u))), out, n, h);
+                half4 out[4][NP];
+                pack_unit(acc[u], kUnscale, out);
+                store_unit(tri(t.row(W::right(u)), t.row(W::left(u))), out, n, h);
                 __builtin_amdgcn_sched_barrier(0);
             }
         lds_barrier();
-        half4 out[W::NU][4][PL];
+        half4 out[W::NU][4][NP];
         if (t.any) {
             zero();
-            auto operands = [&](Frag<PL> (&x)[W::NR], int k, int s) {
+            auto operands = [&](Frag<NP> (&x)[W::NR], int k, int s) {
                 if constexpr (W::BLOCKS) {
                     block_frag(&x[0], t.row(0), k, s);
                     block_frag(&x[2], t.row(2), k, s);
@@ -1023,15 +1019,15 @@ struct MatrixWg {
                     const char *at = tri(j, i);
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
-                        half4 old[PL];
+                        half4 old[NP];
 #pragma unroll
-                        for (int z = 0; z < PL; ++z)
+                        for (int z = 0; z < NP; ++z)
                             old[z] = *(const half4 *)(at + z * kPlane + chunk(n, g & 1, g >> 1) + h * 8);
                         float q[4];
 #pragma unroll
                         for (int e = 0; e < 4; ++e) q[e] = acc[u][4 * g + e];
-                        poly4<PL>(q, old, p, i == j ? n - 8 * g - 4 * h : -1);
-                        split4<PL>(q, 1.0f, out[u][g]);
+                        poly4(q, old, p, i == j ? n - 8 * g - 4 * h : -1);
+                        split4(q, 1.0f, out[u][g]);
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
@@ -1039,7 +1035,7 @@ struct MatrixWg {
         lds_barrier();  // every wave has read A
 #pragma unroll
         for (int u = 0; u < W::NU; ++u)
-            if (mine(u)) store_unit<PL>(tri(t.row(W::right(u)), t.row(W::left(u))), out[u], n, h);
+            if (mine(u)) store_unit(tri(t.row(W::right(u)), t.row(W::left(u))), out[u], n, h);
         lds_barrier();
     }
 
@@ -1087,30 +1083,31 @@ struct MatrixWg {
         static constexpr int right(int) { return 0; }
     };
 
+    template <int NP>
     __device__ __forceinline__ void make_p() const {
         if constexpr (RB == 8) {
-            if (wave < 2) gram_and_poly<Diagonal>();
-            else gram_and_poly<Off>();
+            if (wave < 2) gram_and_poly<Diagonal, NP>();
+            else gram_and_poly<Off, NP>();
         } else {
-            if (wave < 4) gram_and_poly<Pair>();  // (0, 0..1), (0, 2..3), (1, 2..3), (2, 2..3)
-            else gram_and_poly<Single>();
+            if (wave < 4) gram_and_poly<Pair, NP>();  // (0, 0..1), (0, 2..3), (1, 2..3), (2, 2..3)
+            else gram_and_poly<Single, NP>();
         }
     }
 
     // X = P X in place, or (LAST) the result; ALONG: lane = column of the iterate, otherwise its row.
     // (Two waves with four rows of two columns each read P half as often but X twice, and took a fifth longer.)
-    template <bool LAST, bool ALONG>
+    template <bool LAST, bool ALONG, int NP>
     __device__ __forceinline__ void apply() const {
         constexpr int RING = RB > 4 ? 3 : 2;  // units of the column, loaded ahead
         for (int j = wave; j < v.C; j += kWgWaves) {
-            char *const col = v.x0 + (int64_t)j * v.R * UNIT;
-            Frag<PL> x[RING][2];
+            char *const col = v.x0 + (int64_t)j * v.R * kUnit;
+            Frag<NP> x[RING][2];
             auto load = [&](int k) {
 #pragma unroll
                 for (int s = 0; s < 2; ++s)
 #pragma unroll
-                    for (int z = 0; z < PL; ++z)
-                        x[k % RING][s].p[z] = *(const half8 *)(col + k * UNIT + z * kPlane + chunk(n, h, s));
+                    for (int z = 0; z < NP; ++z)
+                        x[k % RING][s].p[z] = *(const half8 *)(col + k * kUnit + z * kPlane + chunk(n, h, s));
             };
             f32x16 acc[RB];
 #pragma unroll
@@ -1128,10 +1125,10 @@ struct MatrixWg {
                     for (int s = 0; s < 2; ++s) {
 #pragma unroll
                         for (int i = 0; i < RB; ++i) {
-                            Frag<PL> f;  // (units past the matrix hold anything: those results are not used)
+                            Frag<NP> f;  // (units past the matrix hold anything: those results are not used)
                             frag(f, i, k, s);
-                            if constexpr (ALONG || !LAST) mma<PL>(acc[i], f, x[k % RING][s]);
-                            else mma<PL>(acc[i], x[k % RING][s], f);
+                            if constexpr (ALONG || !LAST) mma(acc[i], f, x[k % RING][s]);
+                            else mma(acc[i], x[k % RING][s], f);
                         }
                     }
                 }
@@ -1140,11 +1137,11 @@ struct MatrixWg {
             for (int i = 0; i < RB; ++i) {
                 if (i < v.R) {
                     if constexpr (LAST) {
-                        store_last<MUON, BF16>(v, p, acc[i], col + i * UNIT, i, j, h, n);
+                        store_last<MUON, BF16>(v, p, acc[i], col + i * kUnit, i, j, h, n);
                     } else {
-                        half4 out[4][PL];
-                        pack_unit<PL>(acc[i], 1.0f, out);
-                        store_unit<PL>(col + i * UNIT, out, n, h);
+                        half4 out[4][NP];
+                        pack_unit(acc[i], 1.0f, out);
+                        store_unit(col + i * kUnit, out, n, h);
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
@@ -1154,24 +1151,28 @@ struct MatrixWg {
     }
 };
 
-template <int RB, int PL, bool MUON, bool BF16>
+template <int RB, bool MUON, bool BF16>
 __global__ __launch_bounds__(64 * kWgWaves) __attribute__((amdgpu_waves_per_eu(RB == 8 ? 2 : 4))) void
 ns_matrix_kernel(NsWork w, NsParams p, int first) {
-    using Wg = MatrixWg<RB, PL, MUON, BF16>;
+    using Wg = MatrixWg<RB, MUON, BF16>;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
-    const View v = view_of<PL>(w, first + blockIdx.x);
+    const View v = view_of(w, first + blockIdx.x);
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
     const Wg g{p, v, lds, lds0, lane, wave, lane >> 5, lane & 31};
+    constexpr int END = BF16 ? 1 : 2;  // planes of the last steps: see the top
     for (int step = 1;; ++step) {
-        g.fresh().make_p();
+        const bool pairs = !BF16 || step + kSingleSteps <= p.steps;
+        if (pairs) g.fresh().template make_p<2>();
+        else g.fresh().template make_p<END>();
         if (step < p.steps) {
-            g.fresh().template apply<false, true>();
+            if (pairs) g.fresh().template apply<false, true, 2>();
+            else g.fresh().template apply<false, true, END>();
         } else {
-            if (v.tr) g.fresh().template apply<true, false>();
-            else g.fresh().template apply<true, true>();
+            if (v.tr) g.fresh().template apply<true, false, END>();
+            else g.fresh().template apply<true, true, END>();
             return;
         }
     }
@@ -1179,25 +1180,34 @@ ns_matrix_kernel(NsWork w, NsParams p, int first) {
 
 // S stages: with the large tile two workgroups per CU, with the small one enough copies in
 // flight for a CU that has one
-template <int T, int PL> constexpr int kStages = T == 128 ? (PL == 2 ? 2 : 4) : 4;
+template <int T, int NP> constexpr int kStages = T == 128 ? (NP == 2 ? 2 : 4) : 4;
 
-template <int T, int PL, int KIND, bool MUON, bool BF16>
+template <int T, int NP, int KIND, bool MUON, bool BF16>
 hipError_t launch_product(NsWork w, const NsTile *tiles, int64_t grid, const NsParams &p, int odd, hipStream_t s) {
     w.tiles = tiles;
     const int r = w.uni.rows < w.uni.cols ? w.uni.rows : w.uni.cols, c = w.uni.rows + w.uni.cols - r;
     w.nti = (r + T - 1) / T;
     w.ntj = (c + T - 1) / T;
-    constexpr int S = kStages<T, PL>;
-    hipLaunchKernelGGL((ns_product_kernel<T, PL, S, KIND, MUON, BF16>), dim3((unsigned)grid), dim3(256),
-                       S * 2 * (T / 32) * PL * kPlane, s, w, p, odd);
+    constexpr int S = kStages<T, NP>;
+    hipLaunchKernelGGL((ns_product_kernel<T, NP, S, KIND, MUON, BF16>), dim3((unsigned)grid), dim3(256),
+                       S * 2 * (T / 32) * NP * kPlane, s, w, p, odd);
     return hipGetLastError();
+}
+
+template <int T, int NP, bool MUON, bool BF16>
+hipError_t launch_step(const NsWork &w, const NsLists &l, const NsParams &p, int odd, bool last, hipStream_t s) {
+    hipError_t e = launch_product<T, NP, kGram, false, false>(w, l.gram, l.n_gram, p, odd, s);
+    if (e != hipSuccess) return e;
+    e = launch_product<T, NP, kPoly, false, false>(w, l.gram, l.n_gram, p, odd, s);
+    if (e != hipSuccess) return e;
+    if (last) return launch_product<T, NP, kLast, MUON, BF16>(w, l.apply, l.n_apply, p, odd, s);
+    return launch_product<T, NP, kApply, false, false>(w, l.apply, l.n_apply, p, odd, s);
 }
 
 template <int T, bool MUON, bool BF16>
 hipError_t launch_all(NsWork w, const NsLists &l, const NsParams &p, hipStream_t s) {
-    constexpr int PL = BF16 ? 1 : 2;
     if (l.n_small > 0) {
-        hipLaunchKernelGGL((ns_small_kernel<MUON, BF16, PL>), dim3((unsigned)l.n_small), dim3(64 * kSmallWaves), l.small_lds, s, w,
+        hipLaunchKernelGGL((ns_small_kernel<MUON, BF16>), dim3((unsigned)l.n_small), dim3(64 * kSmallWaves), l.small_lds, s, w,
                            p, (int)l.first_small);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
@@ -1209,33 +1219,33 @@ hipError_t launch_all(NsWork w, const NsLists &l, const NsParams &p, hipStream_t
     wx.nti = (r + kNsBlock - 1) / kNsBlock;
     wx.ntj = (c + kNsBlock - 1) / kNsBlock;
     const dim3 gx((unsigned)l.n_x), b(256);
-    hipLaunchKernelGGL((ns_norm_kernel<MUON, BF16, PL>), gx, b, 0, s, wx, p);
+    hipLaunchKernelGGL((ns_norm_kernel<MUON, BF16>), gx, b, 0, s, wx, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((ns_scale_kernel<MUON, BF16, PL>), gx, b, 0, s, wx, p);
+    hipLaunchKernelGGL((ns_scale_kernel<MUON, BF16>), gx, b, 0, s, wx, p);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
     // matrices of more than 128 rows, then of fewer
     if (l.n_wg8 > 0) {
-        hipLaunchKernelGGL((ns_matrix_kernel<8, PL, MUON, BF16>), dim3((unsigned)l.n_wg8), dim3(64 * kWgWaves),
-                           (MatrixWg<8, PL, MUON, BF16>::LDS), s, w, p, (int)l.first_wg8);
+        hipLaunchKernelGGL((ns_matrix_kernel<8, MUON, BF16>), dim3((unsigned)l.n_wg8), dim3(64 * kWgWaves),
+                           (MatrixWg<8, MUON, BF16>::LDS), s, w, p, (int)l.first_wg8);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     if (l.n_wg4 > 0) {
-        hipLaunchKernelGGL((ns_matrix_kernel<4, PL, MUON, BF16>), dim3((unsigned)l.n_wg4), dim3(64 * kWgWaves),
-                           (MatrixWg<4, PL, MUON, BF16>::LDS), s, w, p, (int)l.first_wg4);
+        hipLaunchKernelGGL((ns_matrix_kernel<4, MUON, BF16>), dim3((unsigned)l.n_wg4), dim3(64 * kWgWaves),
+                           (MatrixWg<4, MUON, BF16>::LDS), s, w, p, (int)l.first_wg4);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     for (int k = 0; k < p.steps && l.n_apply > 0; ++k) {
-        const int odd = k & 1;
-        e = launch_product<T, PL, kGram, false, false>(w, l.gram, l.n_gram, p, odd, s);
-        if (e != hipSuccess) return e;
-        e = launch_product<T, PL, kPoly, false, false>(w, l.gram, l.n_gram, p, odd, s);
-        if (e != hipSuccess) return e;
-        e = k + 1 < p.steps ? launch_product<T, PL, kApply, false, false>(w, l.apply, l.n_apply, p, odd, s)
-                            : launch_product<T, PL, kLast, MUON, BF16>(w, l.apply, l.n_apply, p, odd, s);
+        const bool last = k + 1 == p.steps;
+        bool single = false;
+        if constexpr (BF16) {
+            single = k + kSingleSteps >= p.steps;  // see the top
+            if (single) e = launch_step<T, 1, MUON, BF16>(w, l, p, k & 1, last, s);
+        }
+        if (!single) e = launch_step<T, 2, MUON, BF16>(w, l, p, k & 1, last, s);
         if (e != hipSuccess) return e;
     }
     if constexpr (MUON) {
@@ -1247,17 +1257,17 @@ hipError_t launch_all(NsWork w, const NsLists &l, const NsParams &p, hipStream_t
 
 }  // namespace
 
-int64_t ns_matrix_bytes(int64_t rows, int64_t cols, int planes) {
+int64_t ns_matrix_bytes(int64_t rows, int64_t cols) {
     const int64_t r = rows < cols ? rows : cols, c = rows + cols - r;
     const int64_t R = (r + 31) / 32, C = (c + 31) / 32;
-    return 2 * (R * C + R * R) * planes * kPlane;
+    return 2 * (R * C + R * R) * kUnit;
 }
 
-int64_t ns_small_bytes(int64_t rows, int64_t cols, int planes) {
+int64_t ns_small_bytes(int64_t rows, int64_t cols) {
     const int r = (int)(rows < cols ? rows : cols), c = (int)(rows + cols - r);
     const int R = units(r), C = units(c);
-    const bool fits = planes == 2 ? fits_small<2>(R, C) : fits_small<1>(R, C);
-    return fits ? (int64_t)(R * C + R * (R + 1) / 2) * planes * kPlane : 0;
+    const bool fits = fits_small(R, C);
+    return fits ? (int64_t)(R * C + R * (R + 1) / 2) * kUnit : 0;
 }
 
 int ns_matrix_rows(int64_t rows, int64_t cols) {
@@ -1265,9 +1275,9 @@ int ns_matrix_rows(int64_t rows, int64_t cols) {
     return R <= 4 ? 4 : R <= 8 ? 8 : 0;
 }
 
-int64_t ns_matrix_wg_bytes(int64_t rows, int64_t cols, int planes) {
+int64_t ns_matrix_wg_bytes(int64_t rows, int64_t cols) {
     const int64_t r = rows < cols ? rows : cols, c = rows + cols - r;
-    return (r + 31) / 32 * ((c + 31) / 32) * planes * kPlane;
+    return (r + 31) / 32 * ((c + 31) / 32) * kUnit;
 }
 
 // A workgroup takes as long for its matrix as tiles on all CUs for about 70 of them (fp32, by tiles and by

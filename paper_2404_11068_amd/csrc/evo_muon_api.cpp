@@ -124,7 +124,7 @@ bool make_plan(const evo_muon_tensor *t, int32_t n, Plan &p) {
         if (t[i].rows < 0 || t[i].cols < 0 || t[i].rows > kMostSide || t[i].cols > kMostSide) return false;
         if (t[i].rows == 0 || t[i].cols == 0) continue;
         order.push_back(i);
-        if (evo::ns_small_bytes(t[i].rows, t[i].cols, 2) > 0) {
+        if (evo::ns_small_bytes(t[i].rows, t[i].cols) > 0) {
             form[i] = 3;
         } else if (const int rb = evo::ns_matrix_rows(t[i].rows, t[i].cols)) {
             form[i] = rb == 8 ? 1 : 2;
@@ -140,7 +140,7 @@ bool make_plan(const evo_muon_tensor *t, int32_t n, Plan &p) {
         if (form[i] == 2) ++h.n_wg4;
         if (form[i] == 3) {
             ++h.n_small;
-            const int64_t lds = evo::ns_small_bytes(t[i].rows, t[i].cols, 2);
+            const int64_t lds = evo::ns_small_bytes(t[i].rows, t[i].cols);
             h.small_lds = lds > h.small_lds ? lds : h.small_lds;
         }
         if (form[i] == 3) continue;
@@ -181,7 +181,7 @@ bool make_plan(const evo_muon_tensor *t, int32_t n, Plan &p) {
         M.part0 = (int32_t)part;
         M.by_matrix = f != 0;
         part += blocks_of(z.r, z.c);
-        off += f == 0 ? evo::ns_matrix_bytes(s.rows, s.cols, 2) : evo::ns_matrix_wg_bytes(s.rows, s.cols, 2);
+        off += f == 0 ? evo::ns_matrix_bytes(s.rows, s.cols) : evo::ns_matrix_wg_bytes(s.rows, s.cols);
         p.mats.push_back(M);
         if (f != 0) {
             each_tile(z.r, z.c, evo::kNsBlock, [&](int32_t i, int32_t j) { p.x.add(8, NsTile{m, i, j}); });
@@ -230,10 +230,9 @@ bool orth_by_matrix(const evo_orth_dims *d) {
 
 // (a stack that fits into the workgroups' LDS still asks for a little: a size of 0 means a refusal)
 size_t orth_workspace(const evo_orth_dims *d) {
-    const int planes = d->dtype == EVO_DTYPE_BF16 ? 1 : 2;
-    if (evo::ns_small_bytes(d->rows, d->cols, planes) > 0) return 256;
-    const int64_t each = orth_by_matrix(d) ? evo::ns_matrix_wg_bytes(d->rows, d->cols, planes)
-                                           : evo::ns_matrix_bytes(d->rows, d->cols, planes);
+    if (evo::ns_small_bytes(d->rows, d->cols) > 0) return 256;
+    const int64_t each = orth_by_matrix(d) ? evo::ns_matrix_wg_bytes(d->rows, d->cols)
+                                           : evo::ns_matrix_bytes(d->rows, d->cols);
     return (size_t)(round256(d->n_batch * blocks_of(d->rows, d->cols) * 8) + d->n_batch * each);
 }
 
@@ -279,7 +278,7 @@ int evo_orthogonalize(const evo_orth_dims *d, const void *x, void *out, void *wo
     w.uni.rows = (int32_t)d->rows;
     w.uni.cols = (int32_t)d->cols;
     w.in_stride = each;
-    w.ws_stride = evo::ns_matrix_bytes(d->rows, d->cols, bf16 ? 1 : 2);
+    w.ws_stride = evo::ns_matrix_bytes(d->rows, d->cols);
     w.n_mats = (int32_t)n;
     w.part = (double *)workspace;
     w.ws = (char *)workspace + round256(n * blocks_of(r, c) * 8);
@@ -290,7 +289,7 @@ int evo_orthogonalize(const evo_orth_dims *d, const void *x, void *out, void *wo
     p.eps = d->eps;
     p.steps = d->steps;
     NsLists l{};
-    l.small_lds = evo::ns_small_bytes(d->rows, d->cols, bf16 ? 1 : 2);
+    l.small_lds = evo::ns_small_bytes(d->rows, d->cols);
     l.tile = evo::ns_tile(n * tiles_of(r, 128) * tiles_of(c, 128));
     // eight matrices or more are dealt to the XCDs, so their number is rounded up
     const int64_t slots = n >= 8 ? (n + 7) / 8 * 8 : n, g = tiles_of(r, l.tile);
@@ -299,7 +298,7 @@ int evo_orthogonalize(const evo_orth_dims *d, const void *x, void *out, void *wo
     } else {
         l.n_x = slots * blocks_of(r, c);
         if (orth_by_matrix(d)) {
-            w.ws_stride = evo::ns_matrix_wg_bytes(d->rows, d->cols, bf16 ? 1 : 2);
+            w.ws_stride = evo::ns_matrix_wg_bytes(d->rows, d->cols);
             w.uni.by_matrix = 1;
             (evo::ns_matrix_rows(d->rows, d->cols) == 8 ? l.n_wg8 : l.n_wg4) = n;
         } else {

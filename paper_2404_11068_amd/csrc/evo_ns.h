@@ -59,15 +59,15 @@ struct NsLists {
 
 constexpr int kNsBlock = 64;  // tiles of the norm and scaling passes
 
-// LDS that a matrix takes as a whole, 0 if it does not fit; planes: 2 for fp32, 1 for bf16
-int64_t ns_small_bytes(int64_t rows, int64_t cols, int planes);
+// LDS that a matrix takes as a whole, 0 if it does not fit
+int64_t ns_small_bytes(int64_t rows, int64_t cols);
 // 8 or 4: the form of workgroup that can take the matrix by itself, 0 if none
 int ns_matrix_rows(int64_t rows, int64_t cols);
-int64_t ns_matrix_wg_bytes(int64_t rows, int64_t cols, int planes);  // its buffers then
+int64_t ns_matrix_wg_bytes(int64_t rows, int64_t cols);  // its buffers then
 // whether matrices of this much work in all, and the largest alone, are done a workgroup each
 bool ns_by_matrix(double total, double largest);
 // bytes of a matrix's buffers in the workspace where it does not fit
-int64_t ns_matrix_bytes(int64_t rows, int64_t cols, int planes);
+int64_t ns_matrix_bytes(int64_t rows, int64_t cols);
 // tiles of the products for a call whose iterates have this many 128 x 128 tiles
 int ns_tile(int64_t tiles128);
 
