@@ -10,7 +10,8 @@ library's kernels on it (no allocation, no synchronisation).
 (LayerNorm + q/k/v/gate projections, LayerNorm(z) + pair-bias projection,
 attention forward, attention backward, backward of the projections and their
 LayerNorm) on static buffers, runnable eagerly (one C-ABI call per stage) or
-through the cache (one graph launch).
+through the cache (one graph launch), with or without a learned relative
+position bias on top of the pair bias.
 """
 from __future__ import annotations
 
@@ -22,6 +23,7 @@ import torch
 
 from . import evo_attn as ea
 from . import proj as pj
+from . import relpos as rp
 from .evo_attn import EvoAttnError, _stream, load_library
 
 RECORD_FN = ctypes.CFUNCTYPE(None, ctypes.c_void_p, ctypes.c_void_p)
@@ -102,10 +104,15 @@ class MSARowAttentionStep:
     """Static buffers and weights of one MSA row attention with pair bias:
     m [N, L, c_m], z [L, L, c_z] -> q, k, v, g, bias -> o, lse -> m_out = o W_out^T + b_out; backward
     from d_m_out: dout (at o), dW_out, db_out -> dq, dk, dv, dg, dbias -> dm and the projection weight
-    gradients, dz and the pair-bias weight gradients."""
+    gradients, dz and the pair-bias weight gradients.
+
+    With relpos_edges (relpos.relpos_edges_clip or relpos_edges_log) a learned relative position
+    bias, relpos_table [H, buckets], is added to the pair bias in place, for the residue numbers
+    relpos_pos [1, L] (0 .. L - 1 to begin with), and the backward gives its gradient, d_relpos;
+    the sum is rounded to bf16 once more than the pair bias alone."""
 
     def __init__(self, N: int, L: int, c_m: int = 256, c_z: int = 128, H: int = 8, d: int = 32, seed: int = 0,
-                 device="cuda"):
+                 device="cuda", relpos_edges: Optional[torch.Tensor] = None):
         g = torch.Generator(device="cpu").manual_seed(seed)
         bf = dict(dtype=torch.bfloat16, device=device)
         f32 = dict(dtype=torch.float32, device=device)
@@ -156,8 +163,19 @@ class MSARowAttentionStep:
         self.dln_z_b = torch.empty(c_z, **f32)
         self.ws_pb = torch.empty(max(pj.pair_bias_bwd_workspace_size(1, L, L, c_z, H), 16), dtype=torch.uint8,
                                  device=device)
+        self.relpos_edges = relpos_edges
+        if relpos_edges is not None:
+            if relpos_edges.dtype != torch.int32 or relpos_edges.dim() != 1 or not relpos_edges.is_contiguous():
+                raise ValueError("relpos_edges must be a contiguous int32 [E] tensor")
+            E = relpos_edges.numel()
+            self.relpos_pos = torch.arange(L, dtype=torch.int32, device=device).view(1, L)
+            self.relpos_table = (0.1 * r(H, E + 1)).to(**f32)
+            self.d_relpos = torch.empty(H, E + 1, **f32)
+            self.ws_rp = torch.empty(max(rp.relpos_bias_bwd_workspace_size(1, H, L, L, E), 16), dtype=torch.uint8,
+                                     device=device)
 
-        self._key = hash((N, L, H, d, self.m.data_ptr(), self.z.data_ptr(), self.dq.data_ptr())) & \
+        more = () if relpos_edges is None else (relpos_edges.data_ptr(), self.d_relpos.data_ptr())
+        self._key = hash((N, L, H, d, self.m.data_ptr(), self.z.data_ptr(), self.dq.data_ptr()) + more) & \
             0xFFFFFFFFFFFFFFFF
 
     def key(self) -> int:
@@ -165,12 +183,16 @@ class MSARowAttentionStep:
         return self._key
 
     def record(self, stream):
-        """Enqueue the step (8 C-ABI calls, 15 kernels) on `stream` (torch stream or raw handle):
-        projections, pair bias, attention, output projection; then the backward in reverse."""
+        """Enqueue the step (8 C-ABI calls, 15 kernels; 10 and 18 with the relative position bias)
+        on `stream` (torch stream or raw handle): projections, pair bias, attention, output
+        projection; then the backward in reverse."""
         pj.ln_proj_fwd(self.m, self.ln_m_w, self.ln_m_b, self.w_qkvg, self.b_qkvg, n_proj=4,
                        outs=[t.view(self.N, self.L, -1) for t in (self.q, self.k, self.v, self.gate)],
                        mean=self.mean, rstd=self.rstd, y_norm=self.y_norm, stream=stream)
         pj.ln_pair_bias_fwd(self.z, self.ln_z_w, self.ln_z_b, self.w_bias, out=self.bias, stream=stream)
+        if self.relpos_edges is not None:
+            rp.relpos_bias_fwd(self.relpos_pos, self.relpos_pos, self.relpos_edges, self.relpos_table,
+                               base=self.bias, out=self.bias, stream=stream)
         ea.evo_attn_fwd(self.q, self.k, self.v, self.gate, self.bias, self.mask, rows_per_bias=self.N,
                         out=self.out, lse=self.lse, stream=stream)
         HDm = self.H * self.d
@@ -182,6 +204,9 @@ class MSARowAttentionStep:
         ea.evo_attn_bwd(self.q, self.k, self.v, self.gate, self.bias, self.mask, self.out, self.lse, self.dout,
                         rows_per_bias=self.N, dq=self.dq, dk=self.dk, dv=self.dv, dgate=self.dg, dbias=self.dbias,
                         workspace=self.ws, stream=stream)
+        if self.relpos_edges is not None:
+            rp.relpos_bias_bwd(self.relpos_pos, self.relpos_pos, self.relpos_edges, self.dbias,
+                               dtable=self.d_relpos, workspace=self.ws_rp, stream=stream)
         pj.ln_proj_bwd(self.m, self.ln_m_w, self.mean, self.rstd, self.y_norm, self.w_qkvg,
                        [t.view(self.N, self.L, -1) for t in (self.dq, self.dk, self.dv, self.dg)],
                        dx=self.dm, dweight=self.dw_qkvg, dbias=self.db_qkvg, dln_weight=self.dln_m_w,
@@ -191,7 +216,8 @@ class MSARowAttentionStep:
                             stream=stream)
 
     def outputs(self):
-        return {k: getattr(self, k) for k in ("q", "k", "v", "gate", "bias", "out", "lse", "dq", "dk", "dv", "dg",
+        more = () if self.relpos_edges is None else ("d_relpos",)
+        return {k: getattr(self, k) for k in more + ("q", "k", "v", "gate", "bias", "out", "lse", "dq", "dk", "dv", "dg",
                                                "dbias", "y_norm", "dm", "dw_qkvg", "db_qkvg", "dln_m_w", "dln_m_b",
                                                "dz", "dw_bias", "dln_z_w", "dln_z_b", "m_out", "dout", "dw_out",
                                                "db_out")}
