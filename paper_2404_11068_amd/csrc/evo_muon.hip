@@ -146,13 +146,16 @@ template <int N> struct Int { static constexpr int value = N; };
 
 template <int NP> struct Frag { half8 p[NP]; };
 
+// the product's t-th term, the small ones first: lo hi, hi lo, hi hi (one plane: hi hi alone)
+template <int NP>
+__device__ __forceinline__ void mma_term(f32x16 &acc, const Frag<NP> &a, const Frag<NP> &b, int t) {
+    const int ia = NP == 2 && t == 0, ib = NP == 2 && t == 1;
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a.p[ia], b.p[ib], acc, 0, 0, 0);
+}
 template <int NP>
 __device__ __forceinline__ void mma(f32x16 &acc, const Frag<NP> &a, const Frag<NP> &b) {
-    if constexpr (NP == 2) {
-        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a.p[1], b.p[0], acc, 0, 0, 0);
-        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a.p[0], b.p[1], acc, 0, 0, 0);
-    }
-    acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a.p[0], b.p[0], acc, 0, 0, 0);
+#pragma unroll
+    for (int t = 0; t < (NP == 2 ? 3 : 1); ++t) mma_term(acc, a, b, t);
 }
 
 // ---- norm and scaling: a thread owns 4 x 4 entries of a 64 x 64 tile
@@ -517,13 +520,10 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, i
         }
     }
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
-    auto copy_stage = [&](int k) {
-        const uint32_t dst = lds0 + (uint32_t)(k % S) * STAGE + (uint32_t)(wave * U) * HELD;
-#pragma unroll
-        for (int q = 0; q < U; ++q)
-#pragma unroll
-            for (int e = 0; e < HELD / 1024; ++e)
-                copy_to_lds(scalar(src[q] + k * step), (uint32_t)(e * 1024 + lane * 16), dst + q * HELD + e * 1024);
+    auto copy = [&](int k, int c) {  // the wave's c-th KB of stage k
+        const int q = c / (HELD / 1024), e = c % (HELD / 1024);
+        copy_to_lds(scalar(src[q] + k * step), (uint32_t)(e * 1024 + lane * 16),
+                    lds0 + (uint32_t)(k % S) * STAGE + (uint32_t)(wave * U + q) * HELD + e * 1024);
     };
 
     f32x16 acc[U][U];  // [row unit or, where the operands are swapped, ...]: see below
@@ -537,35 +537,64 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, i
     // operand 0's fragments f0 (tile rows), operand 1's f1 (tile columns).  D = f0 f1 has lane = column,
     // registers = rows; D = f1 f0 the other way round, which is what an iterate's units store
     // (lane = row, four consecutive columns)
+    // Four waves, one per SIMD: whatever holds up a wave's issue leaves its matrix core idle.  The operands of
+    // a half stage are read while the other half's products run, one at a time between them, and so are the
+    // copies issued (in a row each costs a fifth of the time)
     auto products = [&](auto swapped) {
+        constexpr int TERMS = NP == 2 ? 3 : 1, MMAS = TERMS * U * U, READS = 2 * U * NP;  // of a half
 #pragma unroll
         for (int k = 0; k < S - 1; ++k)
-            if (k < K) copy_stage(k);
-        for (int k = 0; k < K; ++k) {
-            // stage k has arrived when at most the later ones' copies are outstanding
-            if (k + S - 2 < K) wait_copies_and_barrier<(S - 2) * COPIES>();
-            else wait_copies_and_barrier<0>();
-            if (k + S - 1 < K) copy_stage(k + S - 1);
-            const char *s0 = lds + (k % S) * STAGE + wr * U * HELD, *s1 = lds + (k % S) * STAGE + (N + wc * U) * HELD;
+            if (k < K) {
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                Frag<NP> f0[U], f1[U];
+                for (int c = 0; c < COPIES; ++c) copy(k, c);
+            }
+        Frag<NP> f0[2][U], f1[2][U];  // of the two halves of a stage
+        // r-th operand of half s, in the order of their use: the left ones' lo, the right ones' hi, ...
+        auto read = [&](int k, int s, int r) {
+            const int a = r % U, z = r / U, left = z == 0 || z == 3, q = NP == 2 && (z == 0 || z == 2);
+            const char *at = lds + (k % S) * STAGE + q * kPlane + ((left ? wr * U : N + wc * U) + a) * HELD;
+            if (left) f0[s][a].p[q] = frag_rows(at, lane, s);
+            else f1[s][a].p[q] = SQUARE ? frag_rows(at, lane, s) : frag_cols(at, lane, s);
+        };
+        // the products of half s, and between them the reads of the next half (one past the end is read, but
+        // not used: a branch around the read would turn the next wait into one for all reads)
+        auto half = [&](int k, int s, auto copying) {
 #pragma unroll
-                for (int a = 0; a < U; ++a)
-#pragma unroll
-                    for (int q = 0; q < NP; ++q) {
-                        f0[a].p[q] = frag_rows(s0 + a * HELD + q * kPlane, lane, s);
-                        f1[a].p[q] = SQUARE ? frag_rows(s1 + a * HELD + q * kPlane, lane, s)
-                                            : frag_cols(s1 + a * HELD + q * kPlane, lane, s);
-                    }
+            for (int t = 0; t < TERMS; ++t)
 #pragma unroll
                 for (int a = 0; a < U; ++a)
 #pragma unroll
                     for (int b = 0; b < U; ++b) {
-                        if constexpr (decltype(swapped)::value) mma(acc[a][b], f1[b], f0[a]);
-                        else mma(acc[a][b], f0[a], f1[b]);
+                        if constexpr (decltype(swapped)::value) mma_term(acc[a][b], f1[s][b], f0[s][a], t);
+                        else mma_term(acc[a][b], f0[s][a], f1[s][b], t);
+                        const int m = (t * U + a) * U + b, n = s * MMAS + m;
+                        __builtin_amdgcn_sched_barrier(0);
+                        constexpr int EACH = (READS + MMAS - 1) / MMAS;
+#pragma unroll
+                        for (int r = m * EACH; r < (m + 1) * EACH && r < READS; ++r) read(k + s, 1 - s, r);
+                        if constexpr (decltype(copying)::value) {
+#pragma unroll
+                            for (int c = n * COPIES / (2 * MMAS); c < (n + 1) * COPIES / (2 * MMAS); ++c) copy(k + S - 1, c);
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
                     }
+        };
+        int k = 0;
+        auto stage = [&](auto copying) {  // stage k + 1 has arrived, too
+            if (k == 0) {
+#pragma unroll
+                for (int r = 0; r < READS; ++r) read(0, 0, r);
             }
+            half(k, 0, copying);
+            half(k, 1, copying);
+        };
+        for (; k + S - 1 < K; ++k) {
+            wait_copies_and_barrier<(S - 3) * COPIES>();
+            stage(Yes{});
+        }
+        for (; k < K; ++k) {
+            wait_copies_and_barrier<0>();
+            stage(No{});
         }
     };
     const int i0 = t.ti * N + wr * U, j0 = t.tj * N + wc * U;  // this wave's first units
@@ -762,10 +791,9 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
             left(l[1], k, 1);
             right(r[1], k, 1);
             mma(acc, l[0], r[0]);
-            if (k + 1 < K) {
-                left(l[0], k + 1, 0);
-                right(r[0], k + 1, 0);
-            }
+            // (past the end the last ones again, not used: a branch here would make the next wait one for all reads)
+            left(l[0], k + 1 < K ? k + 1 : k, 0);
+            right(r[0], k + 1 < K ? k + 1 : k, 0);
             mma(acc, l[1], r[1]);
         }
     };
@@ -978,7 +1006,7 @@ struct MatrixWg {
                 if (k == 0) staged(f[0], 0, 0);
                 staged(f[1], k, 1);
                 products(f[0]);
-                if (k + 1 < K) staged(f[0], k + 1, 0);
+                staged(f[0], k + 1, 0);  // (past the end: not used)
                 products(f[1]);
             }
         }
@@ -1009,7 +1037,7 @@ struct MatrixWg {
             for (int k = 0; k < v.R; ++k) {
                 operands(f[1], k, 1);
                 products(f[0]);
-                if (k + 1 < v.R) operands(f[0], k + 1, 0);
+                operands(f[0], k + 1 < v.R ? k + 1 : k, 0);
                 products(f[1]);
             }
 #pragma unroll
@@ -1180,7 +1208,7 @@ ns_matrix_kernel(NsWork w, NsParams p, int first) {
 
 // S stages: with the large tile two workgroups per CU, with the small one enough copies in
 // flight for a CU that has one
-template <int T, int NP> constexpr int kStages = T == 128 ? (NP == 2 ? 2 : 4) : 4;
+template <int T, int NP> constexpr int kStages = 4;
 
 template <int T, int NP, int KIND, bool MUON, bool BF16>
 hipError_t launch_product(NsWork w, const NsTile *tiles, int64_t grid, const NsParams &p, int odd, hipStream_t s) {
