@@ -79,22 +79,37 @@ __device__ __forceinline__ NsTile tile_of(const NsWork &w, int k) {
     if (w.tiles) return w.tiles[k];
     const int per = GRAM ? w.nti * (w.nti + 1) / 2 : w.nti * w.ntj;
     int e, mat;
+    // workgroup k runs on XCD k % 8: it has every eighth matrix, or an eighth of a few large ones' tiles
     if (w.n_mats >= 8) {
         const int q = k >> 3;
         mat = (k & 7) + 8 * (q / per);
         e = q % per;
         if (mat >= w.n_mats) mat = -1;
     } else {
-        mat = k / per;
-        e = k % per;
+        const int all = w.n_mats * per, q = (k & 7) * ((all + 7) / 8) + (k >> 3);
+        mat = q < all ? q / per : -1;
+        e = q % per;
     }
-    if (!GRAM) return NsTile{mat, e / w.ntj, e % w.ntj};
-    int ti = 0;  // rows of nti, nti - 1, ... tiles
-    while (e >= w.nti - ti) {
-        e -= w.nti - ti;
-        ++ti;
+    // Bands of four tile rows, column by column: 32 tiles in a row need 12 panels of the operands (row by
+    // row 18 of 16 columns).  A triangle's band begins with the one on its diagonal
+    for (int ti = 0;; ti += 4) {
+        const int nb = w.nti - ti < 4 ? w.nti - ti : 4, diag = GRAM ? nb * (nb + 1) / 2 : 0;
+        const int band = diag + nb * (GRAM ? w.nti - ti - nb : w.ntj);
+        if (e >= band && ti + 4 < w.nti) {
+            e -= band;
+            continue;
+        }
+        if (e >= diag) {
+            e -= diag;
+            return NsTile{mat, ti + e % nb, (GRAM ? ti + nb : 0) + e / nb};
+        }
+        int col = 0;
+        while (e > col) {
+            ++col;
+            e -= col;
+        }
+        return NsTile{mat, ti + e, ti + col};
     }
-    return NsTile{mat, ti, ti + e};
 }
 
 // ---- units
@@ -542,6 +557,7 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, i
     // copies issued (in a row each costs a fifth of the time)
     auto products = [&](auto swapped) {
         constexpr int TERMS = NP == 2 ? 3 : 1, MMAS = TERMS * U * U, READS = 2 * U * NP;  // of a half
+        constexpr bool AHEAD = S > 2;  // the next stage's first half is read, too, while this one's products run
 #pragma unroll
         for (int k = 0; k < S - 1; ++k)
             if (k < K) {
@@ -571,7 +587,8 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, i
                         __builtin_amdgcn_sched_barrier(0);
                         constexpr int EACH = (READS + MMAS - 1) / MMAS;
 #pragma unroll
-                        for (int r = m * EACH; r < (m + 1) * EACH && r < READS; ++r) read(k + s, 1 - s, r);
+                        for (int r = m * EACH; r < (m + 1) * EACH && r < READS; ++r)
+                            if (AHEAD || s == 0) read(k + s, 1 - s, r);
                         if constexpr (decltype(copying)::value) {
 #pragma unroll
                             for (int c = n * COPIES / (2 * MMAS); c < (n + 1) * COPIES / (2 * MMAS); ++c) copy(k + S - 1, c);
@@ -581,15 +598,15 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, i
         };
         int k = 0;
         auto stage = [&](auto copying) {  // stage k + 1 has arrived, too
-            if (k == 0) {
+            if (!AHEAD || k == 0) {
 #pragma unroll
-                for (int r = 0; r < READS; ++r) read(0, 0, r);
+                for (int r = 0; r < READS; ++r) read(k, 0, r);
             }
             half(k, 0, copying);
             half(k, 1, copying);
         };
         for (; k + S - 1 < K; ++k) {
-            wait_copies_and_barrier<(S - 3) * COPIES>();
+            wait_copies_and_barrier<AHEAD ? (S - 3) * COPIES : 0>();
             stage(Yes{});
         }
         for (; k < K; ++k) {
@@ -1206,19 +1223,22 @@ ns_matrix_kernel(NsWork w, NsParams p, int first) {
     }
 }
 
-// S stages: with the large tile two workgroups per CU, with the small one enough copies in
-// flight for a CU that has one
-template <int T, int NP> constexpr int kStages = 4;
-
 template <int T, int NP, int KIND, bool MUON, bool BF16>
 hipError_t launch_product(NsWork w, const NsTile *tiles, int64_t grid, const NsParams &p, int odd, hipStream_t s) {
     w.tiles = tiles;
     const int r = w.uni.rows < w.uni.cols ? w.uni.rows : w.uni.cols, c = w.uni.rows + w.uni.cols - r;
     w.nti = (r + T - 1) / T;
     w.ntj = (c + T - 1) / T;
-    constexpr int S = kStages<T, NP>;
-    hipLaunchKernelGGL((ns_product_kernel<T, NP, S, KIND, MUON, BF16>), dim3((unsigned)grid), dim3(256),
-                       S * 2 * (T / 32) * NP * kPlane, s, w, p, odd);
+    auto launch = [&](auto stages) {
+        constexpr int S = decltype(stages)::value;
+        hipLaunchKernelGGL((ns_product_kernel<T, NP, S, KIND, MUON, BF16>), dim3((unsigned)grid), dim3(256),
+                           S * 2 * (T / 32) * NP * kPlane, s, w, p, odd);
+    };
+    // S stages of copies.  Pairs of 128 x 128 take 32 KB a stage: with four of them a CU has one workgroup, with
+    // two stages it has two, which is better once there are enough (96 matrices of 256 x 256 in 269 us
+    // instead of 318, P X of 8 of 2048 x 2048 in 352 instead of 366) and worse before (one: 57 instead of 44)
+    if (T == 128 && NP == 2 && grid > 256) launch(Int<T == 128 && NP == 2 ? 2 : 4>{});
+    else launch(Int<4>{});
     return hipGetLastError();
 }
 
@@ -1309,8 +1329,7 @@ int64_t ns_matrix_wg_bytes(int64_t rows, int64_t cols) {
 }
 
 // A workgroup takes as long for its matrix as tiles on all CUs for about 70 of them (fp32, by tiles and by
-// workgroups: 64 of 256 x 256 211 and 216 us, 96 272 and 240; 96 of 256 x 1024 590 and 640, 128 778 and 690;
-// 52 of 128 x 512 114 and 124)
+// workgroups: 64 of 256 x 256 210 and 219 us, 96 269 and 221; 64 of 256 x 1024 412 and 586, 128 795 and 666)
 bool ns_by_matrix(double total, double largest) { return total >= 72.0 * largest; }
 
 // 128 x 128 tiles read each staged unit twice as often; once they do not fill

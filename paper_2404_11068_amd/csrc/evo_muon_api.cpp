@@ -291,19 +291,20 @@ int evo_orthogonalize(const evo_orth_dims *d, const void *x, void *out, void *wo
     NsLists l{};
     l.small_lds = evo::ns_small_bytes(d->rows, d->cols);
     l.tile = evo::ns_tile(n * tiles_of(r, 128) * tiles_of(c, 128));
-    // eight matrices or more are dealt to the XCDs, so their number is rounded up
-    const int64_t slots = n >= 8 ? (n + 7) / 8 * 8 : n, g = tiles_of(r, l.tile);
+    // work is dealt to the XCDs: whole matrices, or tiles where there are fewer than eight
+    const int64_t slots = (n + 7) / 8 * 8, g = tiles_of(r, l.tile);
+    auto grid = [&](int64_t per) { return n >= 8 ? slots * per : (n * per + 7) / 8 * 8; };
     if (l.small_lds > 0) {
         l.n_small = n;
     } else {
-        l.n_x = slots * blocks_of(r, c);
+        l.n_x = grid(blocks_of(r, c));
         if (orth_by_matrix(d)) {
             w.ws_stride = evo::ns_matrix_wg_bytes(d->rows, d->cols);
             w.uni.by_matrix = 1;
             (evo::ns_matrix_rows(d->rows, d->cols) == 8 ? l.n_wg8 : l.n_wg4) = n;
         } else {
-            l.n_gram = slots * (g * (g + 1) / 2);
-            l.n_apply = slots * g * tiles_of(c, l.tile);
+            l.n_gram = grid(g * (g + 1) / 2);
+            l.n_apply = grid(g * tiles_of(c, l.tile));
         }
     }
     return evo::launch_ns(w, l, p, false, bf16, (hipStream_t)stream) == hipSuccess ? EVO_OK : EVO_ERR_HIP;
