@@ -1197,16 +1197,13 @@ struct MatrixWg {
 };
 
 template <int RB, bool MUON, bool BF16>
-__global__ __launch_bounds__(64 * kWgWaves) __attribute__((amdgpu_waves_per_eu(RB == 8 ? 2 : 4))) void
-ns_matrix_kernel(NsWork w, NsParams p, int first) {
-    using Wg = MatrixWg<RB, MUON, BF16>;
-    extern __shared__ __attribute__((aligned(1024))) char lds[];
-    const View v = view_of(w, first + blockIdx.x);
+__device__ __forceinline__ void matrix_steps(const NsWork &w, const NsParams &p, int k, char *lds) {
+    const View v = view_of(w, k);
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
-    const Wg g{p, v, lds, lds0, lane, wave, lane >> 5, lane & 31};
+    const MatrixWg<RB, MUON, BF16> g{p, v, lds, lds0, lane, wave, lane >> 5, lane & 31};
     constexpr int END = BF16 ? 1 : 2;  // planes of the last steps: see the top
     for (int step = 1;; ++step) {
         const bool pairs = !BF16 || step + kSingleSteps <= p.steps;
@@ -1221,6 +1218,21 @@ ns_matrix_kernel(NsWork w, NsParams p, int first) {
             return;
         }
     }
+}
+
+// n matrices from `first` on of up to RB unit rows; where RB is 8, those from n8 on have up to 4
+template <int RB, bool MUON, bool BF16>
+__global__ __launch_bounds__(64 * kWgWaves) __attribute__((amdgpu_waves_per_eu(RB == 8 ? 2 : 4))) void
+ns_matrix_kernel(NsWork w, NsParams p, int first, int n8) {
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    const int k = blockIdx.x;
+    if constexpr (RB == 8 && MUON) {
+        if (k >= n8) {
+            matrix_steps<4, MUON, BF16>(w, p, first + k, lds);
+            return;
+        }
+    }
+    matrix_steps<RB, MUON, BF16>(w, p, first + k, lds);
 }
 
 template <int T, int NP, int KIND, bool MUON, bool BF16>
@@ -1273,16 +1285,17 @@ hipError_t launch_all(NsWork w, const NsLists &l, const NsParams &p, hipStream_t
     hipLaunchKernelGGL((ns_scale_kernel<MUON, BF16>), gx, b, 0, s, wx, p);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    // matrices of more than 128 rows, then of fewer
+    // Matrices of more than 128 rows, and in the same launch those of fewer: these fill the CUs that the last of the
+    // longer ones leave idle (578 and 157 matrices: 1088 us instead of 909 + 241).  By themselves they take half
+    // the LDS and registers, and a CU has two
     if (l.n_wg8 > 0) {
-        hipLaunchKernelGGL((ns_matrix_kernel<8, MUON, BF16>), dim3((unsigned)l.n_wg8), dim3(64 * kWgWaves),
-                           (MatrixWg<8, MUON, BF16>::LDS), s, w, p, (int)l.first_wg8);
+        hipLaunchKernelGGL((ns_matrix_kernel<8, MUON, BF16>), dim3((unsigned)(l.n_wg8 + l.n_wg4)), dim3(64 * kWgWaves),
+                           (MatrixWg<8, MUON, BF16>::LDS), s, w, p, (int)l.first_wg8, (int)l.n_wg8);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
-    }
-    if (l.n_wg4 > 0) {
+    } else if (l.n_wg4 > 0) {
         hipLaunchKernelGGL((ns_matrix_kernel<4, MUON, BF16>), dim3((unsigned)l.n_wg4), dim3(64 * kWgWaves),
-                           (MatrixWg<4, MUON, BF16>::LDS), s, w, p, (int)l.first_wg4);
+                           (MatrixWg<4, MUON, BF16>::LDS), s, w, p, (int)l.first_wg4, 0);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
