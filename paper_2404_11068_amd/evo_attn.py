@@ -128,7 +128,7 @@ def _mask_u8(m: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
 def _stream(stream) -> ctypes.c_void_p:
     """hipStream_t of a torch stream (None: the current one) or a raw handle (int)."""
     if stream is None:  # (the handle alone: building the torch stream around it takes 3 us)
-        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
+        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
     return ctypes.c_void_p(stream if isinstance(stream, int) else stream.cuda_stream)
 
 
@@ -136,7 +136,7 @@ def _empty(shape, dtype, like: torch.Tensor, stream):
     """A tensor that belongs to the stream the kernels run on, so that memory
     it gives back is not taken by another stream's work before they are done."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=like.device)
+        return like.new_empty(shape, dtype=dtype)
     s = torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
     with torch.cuda.stream(s):
         return torch.empty(shape, dtype=dtype, device=like.device)

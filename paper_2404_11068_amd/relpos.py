@@ -92,7 +92,7 @@ def _index(pos_i, pos_j, edges, seg_i, seg_j, like: torch.Tensor):
             raise ValueError("positions, segments and edges must be contiguous int32")
         if t.device != dev:
             raise ValueError("tensors must be on one device")
-    if dev.type != "cuda" or dev.index != torch.cuda.current_device():
+    if dev.type != "cuda" or dev.index != torch._C._cuda_getDevice():
         raise ValueError("tensors must be on the current CUDA device")
     return (si[0] if len(si) == 2 else 1), si[-1], sj[-1], se[0]
 
