@@ -36,6 +36,11 @@
  * coefficients that could take it out of it (singular values above 8, or
  * |b| s^2 + |c| s^4 above 60, followed from 1 over the steps) are refused
  * with EVO_ERR_UNSUPPORTED.  A matrix with an infinity or a NaN gives NaN.
+ *
+ * Precision: iterates are pairs of fp16 (22 bits) with fp32 accumulation: fp32 results as
+ * fp32 arithmetic would give them, low-rank matrices included.  The last two steps of bf16
+ * matrices use 11 bits: their results are off by at most about 1.2 times their own
+ * rounding to bf16.
  */
 #ifndef EVO_MUON_H
 #define EVO_MUON_H

@@ -173,7 +173,8 @@ __device__ __forceinline__ void mma(f32x16 &acc, const Frag<NP> &a, const Frag<N
     for (int t = 0; t < (NP == 2 ? 3 : 1); ++t) mma_term(acc, a, b, t);
 }
 
-// ---- norm and scaling: a thread owns 4 x 4 entries of a 64 x 64 tile
+// ---- norm, scaling and update: a thread owns 4 x 4 entries of a 64 x 64 tile.  Streams, bound by HBM:
+// 73 M entries of a model in 182, 196 and 298 us, 12, 12 and 20 bytes each (4.5 to 4.9 TB/s)
 
 // four consecutive entries of a memory row, zeros past its end
 __device__ __forceinline__ void load4(float (&v)[4], const float *p, int left) {
@@ -461,7 +462,10 @@ __device__ __forceinline__ void store_last(const View &v, const NsParams &p, con
 // A workgroup of 4 waves forms a T x T tile, a wave a quarter of it, from units staged
 // in LDS, one unit column (32 contraction entries) per stage, copied by
 // global_load_lds 16 bytes a lane, S - 1 stages ahead: the copies are counted
-// by hand (vmcnt), one barrier per stage.
+// by hand (vmcnt), one barrier per stage.  The matrix instructions bound large
+// products, the copies from L2 those of one plane, the chain of stages and the launch
+// small ones: 8 matrices of 2048 x 2048 in pairs, Gram 217 us (1.0 PFLOP/s of fp16 products), polynomial 224,
+// P X 352 (1.2); one such matrix 37, 40 and 46 us, in one plane 19, 23 and 22; 52 of 128 x 512 6.8, 5.0 and 9.4.
 
 enum { kGram, kPoly, kApply, kLast };
 struct Yes { static constexpr bool value = true; };
@@ -725,7 +729,10 @@ __device__ __forceinline__ void tri_frag(Frag<NP> &f, char *base, int r, int k, 
 // update: memory sees each entry once.  Each of 16 waves takes a unit of the
 // triangle (10 of them at 128 x 128) and one to three of X; what bounds it is
 // the chain of a unit, LDS reads, matrix instructions, splitting and
-// storing, so the next operands are read before the matrix instructions of the last.
+// storing, so the next operands are read before the matrix instructions of the last, and
+// for the whole of it the LDS reads (12000 cycles a step at 128 x 128; the matrix
+// instructions take 7700).  128 x 128: 39 us, bf16 35; one matrix per CU at a time, 1515
+// matrices of a model in 350 us.
 
 constexpr int kSmallUnits = 40;
 constexpr int kSmallLds = 39 * kUnit;
@@ -922,8 +929,10 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
 // unit read by columns.  X lies in the workspace, transposed, so that the
 // fragments of P X come straight from memory, 1 KB a load: each wave takes unit
 // columns of its own and writes the result in their place, without a barrier.  Memory
-// then sees X read twice and written once per step; with A and P in the workspace, too,
-// 240 matrices of 256 x 256 moved 2.7 GB at 6.4 TB/s and took 430 us.
+// then sees X read twice and written once per step: 240 matrices of 256 x 256 take 244 us, of
+// 256 x 1024 793 (with A and P in the workspace, too, the former moved 2.7 GB at 6.4 TB/s and took 430).
+// The matrix instructions would take 45% of that; P X, half the time, reads as much from LDS as it
+// multiplies, with two waves per SIMD to cover each other's reads.
 // A call with too few matrices for the CUs is done sooner by the tiles above.
 
 constexpr int kWgWaves = 8;
@@ -1345,9 +1354,11 @@ int64_t ns_matrix_wg_bytes(int64_t rows, int64_t cols) {
 // workgroups: 64 of 256 x 256 210 and 219 us, 96 269 and 221; 64 of 256 x 1024 412 and 586, 128 795 and 666)
 bool ns_by_matrix(double total, double largest) { return total >= 72.0 * largest; }
 
-// 128 x 128 tiles read each staged unit twice as often; once they do not fill
-// the CUs, tiles of a quarter the size do the work sooner
-int ns_tile(int64_t tiles128) { return tiles128 >= 256 ? 128 : 64; }
+// 128 x 128 tiles read each staged unit twice as often, but the Gram matrix's triangle has few of
+// them: below about 120, tiles of a quarter the size do the work sooner (fp32, small and large tiles: 1 matrix
+// of 1024 x 4096, 36 large ones, 405 and 527 us; 1 of 1792 x 1792, 105, 529 and 517; 12 of 512 x 512, 120, 276
+// and 250; 1 of 2048 x 2048, 136, 778 and 648; 16 of 512 x 2048, 160, 688 and 574)
+int ns_tile(int64_t gram128) { return gram128 >= 120 ? 128 : 64; }
 
 hipError_t launch_ns(const NsWork &w, const NsLists &l, const NsParams &p, bool muon, bool bf16, hipStream_t s) {
     if (l.tile == 128)

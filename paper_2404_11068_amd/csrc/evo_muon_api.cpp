@@ -22,6 +22,7 @@ constexpr int64_t kMostSide = 32768;
 bool aligned(const void *p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
 int64_t tiles_of(int64_t n, int64_t tile) { return (n + tile - 1) / tile; }
+int64_t triangle(int64_t n) { return n * (n + 1) / 2; }
 int64_t blocks_of(int64_t rows, int64_t cols) { return tiles_of(rows, evo::kNsBlock) * tiles_of(cols, evo::kNsBlock); }
 
 // whether the iterate stays in the kernels' range: the largest singular value,
@@ -118,7 +119,7 @@ bool make_plan(const evo_muon_tensor *t, int32_t n, Plan &p) {
     PlanHeader &h = p.h;
     std::vector<int32_t> order;
     std::vector<char> form((size_t)n);  // 0 tiles, 1 and 2 a workgroup with 8 and 4 units of rows, 3 in LDS
-    int64_t tiles128 = 0, blocks = 0;
+    int64_t gram128 = 0, blocks = 0;
     double total = 0.0, alone = 0.0, largest = 0.0;
     for (int32_t i = 0; i < n; ++i) {
         if (t[i].rows < 0 || t[i].cols < 0 || t[i].rows > kMostSide || t[i].cols > kMostSide) return false;
@@ -147,7 +148,7 @@ bool make_plan(const evo_muon_tensor *t, int32_t n, Plan &p) {
         blocks += blocks_of(z.r, z.c);
         if (blocks > 0x3fffffff) return false;
         if (form[i] != 0) continue;
-        tiles128 += tiles_of(z.r, 128) * tiles_of(z.c, 128);
+        gram128 += triangle(tiles_of(z.r, 128));
         total += cost(z);
     }
     // each form by falling cost: what takes longest begins first
@@ -155,7 +156,7 @@ bool make_plan(const evo_muon_tensor *t, int32_t n, Plan &p) {
         return form[a] != form[b] ? form[a] < form[b] : cost(size_of(t[a])) > cost(size_of(t[b]));
     });
     h.magic = kMagic;
-    h.tile = evo::ns_tile(tiles128);
+    h.tile = evo::ns_tile(gram128);
     h.n_mats = (int64_t)order.size();
     h.part_bytes = round256(blocks * 8);
     h.ws_bytes = h.part_bytes;
@@ -290,7 +291,7 @@ int evo_orthogonalize(const evo_orth_dims *d, const void *x, void *out, void *wo
     p.steps = d->steps;
     NsLists l{};
     l.small_lds = evo::ns_small_bytes(d->rows, d->cols);
-    l.tile = evo::ns_tile(n * tiles_of(r, 128) * tiles_of(c, 128));
+    l.tile = evo::ns_tile(n * triangle(tiles_of(r, 128)));
     // work is dealt to the XCDs: whole matrices, or tiles where there are fewer than eight
     const int64_t slots = (n + 7) / 8 * 8, g = tiles_of(r, l.tile);
     auto grid = [&](int64_t per) { return n >= 8 ? slots * per : (n * per + 7) / 8 * 8; };
@@ -303,7 +304,7 @@ int evo_orthogonalize(const evo_orth_dims *d, const void *x, void *out, void *wo
             w.uni.by_matrix = 1;
             (evo::ns_matrix_rows(d->rows, d->cols) == 8 ? l.n_wg8 : l.n_wg4) = n;
         } else {
-            l.n_gram = grid(g * (g + 1) / 2);
+            l.n_gram = grid(triangle(g));
             l.n_apply = grid(g * tiles_of(c, l.tile));
         }
     }

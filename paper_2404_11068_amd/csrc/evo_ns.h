@@ -68,8 +68,8 @@ int64_t ns_matrix_wg_bytes(int64_t rows, int64_t cols);  // its buffers then
 bool ns_by_matrix(double total, double largest);
 // bytes of a matrix's buffers in the workspace where it does not fit
 int64_t ns_matrix_bytes(int64_t rows, int64_t cols);
-// tiles of the products for a call whose iterates have this many 128 x 128 tiles
-int ns_tile(int64_t tiles128);
+// tiles of the products for a call whose Gram matrices' triangles have this many 128 x 128 tiles
+int ns_tile(int64_t gram128);
 
 hipError_t launch_ns(const NsWork &w, const NsLists &l, const NsParams &p, bool muon, bool bf16, hipStream_t s);
 

@@ -173,7 +173,8 @@ __device__ __forceinline__ void rp_store(const T (&v)[N], T *p) {
 // table lies in LDS with a bucket's heads side by side, so one or two 16-byte
 // reads bring an entry's values for the whole group; every eighth bucket adds
 // 16 bytes of padding, because neighbouring lanes are 8 buckets apart and
-// would otherwise all meet in one bank.
+// would otherwise all meet in one bank.  16 planes of 2049 x 2049 in bf16: 34 us,
+// 4.0 TB/s of writes; 8 of 256 x 256 onto a base: 4.0 us, a launch.
 
 constexpr int kRpCols = 8;  // consecutive entries of a lane
 
@@ -341,6 +342,9 @@ hipError_t launch_fwd_t(const RpArgs &a, hipStream_t s) {
 // order: one LDS round trip per piece instead of four.  At the end the columns
 // of every row are summed in a fixed order, and a second kernel adds the
 // waves' sums in order, in fp64.
+//
+// 16 planes of 2048 x 2048: 65 buckets 56 us (4.8 TB/s), 129 79 us, 257 115 us, 513 in two passes 302 us:
+// with more than 66 buckets the turns' chains of LDS reads, additions and writes bound it, not HBM.
 //
 // C is 64, one column per lane, for up to 66 buckets.  With more of them that
 // would leave a SIMD fewer than two waves, so 32 or 16 columns serve the
