@@ -51,7 +51,8 @@
 extern "C" {
 #endif
 
-/* Compiled limits: rows and cols up to 32768, n_batch up to 2^20, steps 1 .. 64. */
+/* Compiled limits: rows and cols up to 32768, n_batch up to 2^20, steps 1 .. 64, and
+ * fewer than 2^24 tiles of 64 x 64 entries in a call (a plan: by XCD, padding included). */
 typedef struct evo_orth_dims {
     int32_t dtype;    /* of x and out: EVO_DTYPE_F32 or EVO_DTYPE_BF16 */
     int32_t steps;    /* >= 1 */
@@ -90,7 +91,10 @@ typedef struct evo_muon_hparams {
     int32_t nesterov;    /* 0 or 1 */
 } evo_muon_hparams;
 
-/* The plan holds the pointers and the work lists of every matrix.  It is
+/* The tensors that a step writes (param, momentum, swa) must not overlap each other
+ * or a gradient: matrices are worked on at the same time.
+ *
+ * The plan holds the pointers and the work lists of every matrix.  It is
  * built once on the host (evo_muon_plan_bytes bytes, 8-byte aligned; the size
  * is -1 for invalid sizes) and copied to the device by the caller, who passes
  * both copies to every step; rebuild it if a tensor is reallocated. */

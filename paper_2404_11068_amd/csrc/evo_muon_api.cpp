@@ -18,6 +18,8 @@ using evo::NsMat;
 using evo::NsTile;
 
 constexpr int64_t kMostSide = 32768;
+// workgroups of a launch: HIP takes fewer than 2^32 threads, and up to 256 are in one here
+constexpr int64_t kMostBlocks = (int64_t(1) << 24) - 1;
 
 bool aligned(const void *p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
@@ -146,7 +148,7 @@ bool make_plan(const evo_muon_tensor *t, int32_t n, Plan &p) {
         }
         if (form[i] == 3) continue;
         blocks += blocks_of(z.r, z.c);
-        if (blocks > 0x3fffffff) return false;
+        if (blocks > kMostBlocks) return false;
         if (form[i] != 0) continue;
         gram128 += triangle(tiles_of(z.r, 128));
         total += cost(z);
@@ -205,7 +207,7 @@ bool make_plan(const evo_muon_tensor *t, int32_t n, Plan &p) {
     h.n_x = p.x.total();
     h.n_gram = p.gram.total();
     h.n_apply = p.apply.total();
-    if (h.n_x > 0x7fffffff) return false;
+    if (h.n_x > kMostBlocks || h.n_gram > kMostBlocks || h.n_apply > kMostBlocks) return false;
     h.off_mats = round256(sizeof(PlanHeader));
     h.off_x = h.off_mats + round256(h.n_mats * (int64_t)sizeof(NsMat));
     h.off_gram = h.off_x + round256(h.n_x * (int64_t)sizeof(NsTile));
@@ -219,7 +221,7 @@ int check_orth(const evo_orth_dims *d) {
     if (d->dtype != EVO_DTYPE_F32 && d->dtype != EVO_DTYPE_BF16) return EVO_ERR_UNSUPPORTED;
     if (d->n_batch < 0 || d->rows < 0 || d->cols < 0) return EVO_ERR_INVALID_ARG;
     if (d->n_batch > (1 << 20) || d->rows > kMostSide || d->cols > kMostSide) return EVO_ERR_UNSUPPORTED;
-    if (d->n_batch * blocks_of(d->rows, d->cols) > 0x3fffffff) return EVO_ERR_UNSUPPORTED;
+    if ((d->n_batch + 7) * blocks_of(d->rows, d->cols) > kMostBlocks) return EVO_ERR_UNSUPPORTED;  // (see `grid`)
     return check_coefs(d->a, d->b, d->c, d->eps, d->steps);
 }
 

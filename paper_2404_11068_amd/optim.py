@@ -268,6 +268,16 @@ class FusedMuonSWA:
                 math.sqrt(max(1.0, r / c)) if adjust == "spectral" else 0.2 * math.sqrt(max(r, c))
             tab[i] = (p.data_ptr(), self.grads[i].data_ptr(), self.momentum[i].data_ptr(), self.swa[i].data_ptr(),
                       r, c, f)
+        # all matrices are worked on at the same time: what one writes, no other may read or write
+        ends = []
+        for kind, ts in ((1, self.params), (1, self.momentum), (1, self.swa), (0, self.grads)):
+            ends += [(t.data_ptr(), t.data_ptr() + 4 * t.numel(), kind) for t in ts if t.numel()]
+        ends.sort()
+        written = read = 0
+        for begin, end, kind in ends:
+            if begin < written or (kind and begin < read):
+                raise ValueError("parameters, momenta and averages must not overlap each other or a gradient")
+            written, read = (max(written, end), read) if kind else (written, max(read, end))
         size = int(lib.evo_muon_plan_bytes(tab.ctypes.data, n))
         if size < 0:
             raise ValueError("a matrix is too large for the plan")

@@ -94,6 +94,71 @@ def test_the_most_that_a_workgroup_holds(r, c, dtype):
         _check(op.orthogonalize(x), mo.orthogonalize(to_f64(x)), dtype, flat=False)
 
 
+def _close(got, ref, dtype):
+    """For any spectrum.  fp32: as _check.  bf16: all steps but the last two as fp32; a rounding of size 2^-11 in
+    the last but one changes the iterate by C 2^-11 of its norm, which the last step's slope takes to 3.4445 times
+    that and adds as much again: 10 (1 + 3.4445) 2^-11, and 2^-8 for the result's rounding."""
+    got = to_f64(got)
+    assert np.isfinite(got).all()
+    for g, r in zip(got.reshape((-1,) + got.shape[-2:]), ref.reshape((-1,) + ref.shape[-2:])):
+        size = np.linalg.norm(r)
+        bound = 24000 * _eps(torch.float32, *r.shape)
+        bound += (44.445 * 2.0 ** -11 + 2.0 ** -8) * size if dtype == torch.bfloat16 else 0.0
+        assert np.linalg.norm(g - r) <= bound, (np.linalg.norm(g - r), bound)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("N,m,n", [
+    # large tiles: up to 256 of them in a launch and more, fewer than eight matrices and more, wide and tall, odd
+    (1, 1930, 2010), (1, 2100, 1990), (2, 1337, 1400), (13, 500, 530), (45, 300, 260), (24, 700, 390)])
+def test_large_tiles(N, m, n, dtype):
+    print("\n[case] large tiles", N, m, n, dtype, flush=True)
+    x = torch.from_numpy(np.random.default_rng(N + m).standard_normal((N, m, n)).astype(np.float32)).to(dtype).cuda()
+    got = op.orthogonalize(x)
+    assert torch.equal(got, op.orthogonalize(x))
+    k = N - 1
+    _close(got[:1], mo.orthogonalize(to_f64(x[:1])), dtype)
+    _close(got[k:], mo.orthogonalize(to_f64(x[k:])), dtype)
+    other = torch.randn_like(x)
+    other[k] = x[k]
+    assert torch.equal(got[k], op.orthogonalize(other)[k])
+
+
+@pytest.mark.parametrize("kind", ["gauss", "rank3", "decay"])
+@pytest.mark.parametrize("N,m,n", [(1, 128, 128), (2, 60, 300), (1, 700, 300), (73, 200, 140), (75, 100, 700)])
+def test_bf16_of_any_spectrum(kind, N, m, n):
+    print("\n[case] bf16", kind, N, m, n, flush=True)
+    rng = np.random.default_rng(17)
+    x = rng.standard_normal((N, m, n))
+    if kind == "rank3":
+        x = rng.standard_normal((N, m, 3)) @ rng.standard_normal((N, 3, n))
+    elif kind == "decay":
+        u, s, v = np.linalg.svd(x, full_matrices=False)
+        x = (u * np.exp(-np.arange(s.shape[1]) / s.shape[1] * 9)) @ v
+    t = torch.from_numpy(x).to(torch.bfloat16).cuda()
+    for steps in (1, 2, 3, 5, 7):
+        _close(op.orthogonalize(t, steps=steps)[:2], mo.orthogonalize(to_f64(t[:2]), steps=steps), torch.bfloat16)
+
+
+def test_muon_with_large_tiles():
+    print("\n[case] muon, large tiles", flush=True)
+    shapes = [(500, 530)] * 7 + [(530, 500)] * 6 + [(1, 1300), (300, 2), (777, 300)]
+    rng = np.random.default_rng(4)
+    P, G, M = ([rng.standard_normal(s).astype(np.float32) for s in shapes] for _ in range(3))
+    gpu = lambda ts: [torch.from_numpy(t).cuda() for t in ts]
+    p, g, m = gpu(P), gpu(G), gpu(M)
+    opt = op.FusedMuonSWA(p, g, m, lr=0.1, adjust="none")
+    opt.step()
+    torch.cuda.synchronize()
+    for k, s in enumerate(shapes):
+        rp_, rm, rw = mo.muon_step(P[k], G[k], M[k], P[k], lr=0.1, momentum_decay=0.95, nesterov=True, weight_decay=0.0,
+                                   swa_decay=0.999)
+        e = 24000 * _eps(torch.float32, *s)
+        assert np.linalg.norm(to_f64(m[k]) - rm) <= 2.0 ** -21 * (np.linalg.norm(M[k]) + np.linalg.norm(G[k])), s
+        assert np.linalg.norm(to_f64(p[k]) - rp_) <= 0.1 * e + 2.0 ** -22 * np.linalg.norm(rp_), s
+        assert np.linalg.norm(to_f64(opt.swa[k]) - rw) <= 0.1 * e + 2.0 ** -22 * np.linalg.norm(rw), s
+
+
 @pytest.mark.parametrize("kind", ["rank1", "decay", "zero", "tiny", "huge", "one_entry"])
 @pytest.mark.parametrize("m,n", [(96, 96), (150, 280)])
 def test_hard_spectra(kind, m, n):
@@ -298,3 +363,17 @@ def test_orthogonalize_on_another_stream_and_in_a_graph():
         cache.run(1, lambda st: op.orthogonalize(x, out=out, workspace=ws, stream=st), s)
         torch.cuda.synchronize()
         assert torch.equal(out, want), it
+
+
+def test_muon_refuses_tensors_that_overlap():
+    """What a step writes may not be another matrix's (or its own) operand; gradients may be shared."""
+    flat = torch.zeros(64 * 64, device="cuda")
+    p, q, g = flat[:1024].view(32, 32), flat[1024:2048].view(32, 32), torch.randn(32, 32, device="cuda")
+    op.FusedMuonSWA([p, q], [g, g]).step()                                       # neighbours, one gradient
+    torch.cuda.synchronize()
+    for params, grads, kw in (([p, p], [g, g], {}), ([p, flat[512:1536].view(32, 32)], [g, g], {}), ([p], [p], {}),
+                              ([p], [flat[992:2016].view(32, 32)], {}), ([p], [g], dict(momentum=[p])),
+                              ([p, q], [g, g], dict(swa=[q, p])), ([p], [g], dict(momentum=[q], swa=[q])),
+                              ([p], [q], dict(momentum=[q]))):
+        with pytest.raises(ValueError, match="overlap"):
+            op.FusedMuonSWA(params, grads, **kw)

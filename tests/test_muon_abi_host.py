@@ -145,3 +145,13 @@ def test_binding_refuses_before_any_launch():
         op.FusedMuonSWA([m], [m], adjust="other")
     with pytest.raises(ValueError, match="float32 CUDA"):
         op.FusedMuonSWA([m], [m])
+
+
+def test_rejects_more_tiles_than_a_launch_takes():
+    # 1 x 1300 is 21 tiles of 64 x 64: 2^20 of them are more than 2^24, and 2^19 are not
+    assert _orth(_dims(n_batch=1 << 20, rows=1, cols=1300)) == 2
+    assert _lib().evo_orthogonalize_workspace_size(ctypes.byref(_dims(n_batch=1 << 20, rows=1, cols=1300))) == 0
+    assert _lib().evo_orthogonalize_workspace_size(ctypes.byref(_dims(n_batch=1 << 19, rows=1, cols=1300))) > 0
+    # 64 of 32768 x 32768 are exactly 2^24
+    assert _orth(_dims(n_batch=64, rows=32768, cols=32768)) == 2
+    assert _plan([(32768, 32768)] * 64)[1] == -1
