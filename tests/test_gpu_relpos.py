@@ -135,6 +135,40 @@ def test_longer(B, H, Li, Lj, kind):
     assert np.array_equal(to_f64(d), ro.backward(*index, g, _np(si), _np(sj)))
 
 
+def _spread(kind, rng):
+    """Edges that a table of single differences cannot hold, or only in steps."""
+    if kind == "log":                 # widths that grow: several differences a step, a few edges in the first ones
+        return rp.relpos_edges_log(64, 20000, device="cpu").numpy().astype(np.int64)
+    if kind == "random":              # one edge or two in a step
+        return np.sort(rng.choice(np.arange(-40000, 40000), 300, replace=False))
+    if kind == "cluster":             # fifty in one step, the others far
+        return np.sort(np.concatenate([np.arange(100, 150), [-10 ** 6, -70000, 10 ** 6]]))
+    return np.array([-2 ** 31, -2 ** 31 + 1, -5, 0, 3, 2 ** 31 - 2, 2 ** 31 - 1])  # the ends
+
+
+@pytest.mark.parametrize("Li,Lj", [(70, 129), (2600, 2503)])   # short ones search; long ones build the table
+@pytest.mark.parametrize("kind", ["log", "random", "cluster", "ends"])
+def test_spread_edges(kind, Li, Lj):
+    print("\n[case] spread edges", kind, Li, Lj, flush=True)
+    rng = np.random.default_rng(12)
+    edges, H = _spread(kind, rng), 2
+    pi, pj = rng.integers(-30000, 30000, Li), rng.integers(-30000, 30000, Lj)
+    pi[:20], pj[:20] = rng.integers(90, 160, 20), rng.integers(-4, 4, 20)
+    if kind == "ends":
+        pi[20:40], pj[20:40] = -2 ** 31, rng.choice([2 ** 31 - 1, 0, -2 ** 31, 1], 20)
+    t = lambda a: torch.from_numpy(a.astype(np.int32)).cuda().view(1, -1)
+    diff = np.clip(pi[:, None].astype(np.int64) - pj[None, :], -2 ** 31, 2 ** 31 - 1)
+    n = np.searchsorted(edges, diff, side="right")
+    e = t(edges).view(-1)
+    table = torch.from_numpy(rng.standard_normal((H, len(edges) + 1)).astype(np.float32)).cuda()
+    out = rp.relpos_bias_fwd(t(pi), t(pj), e, table, dtype=torch.float32)
+    assert np.array_equal(out[0].cpu().numpy(), table.cpu().numpy()[:, n])
+    g = rng.integers(-9, 10, (1, H, Li, Lj)).astype(np.float32)
+    d = rp.relpos_bias_bwd(t(pi), t(pj), e, torch.from_numpy(g).cuda())
+    want = np.stack([np.bincount(n.reshape(-1), g[0, h].reshape(-1), len(edges) + 1) for h in range(H)])
+    assert np.array_equal(to_f64(d), want)
+
+
 def test_base_infinities_and_nan_pass_and_neighbours_stay():
     pi, pj, _, _, rng = _inputs(1, 9, 21, False, 4)
     edges = _edges("clip:4")
