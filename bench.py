@@ -1024,7 +1024,9 @@ KERNEL_SOURCES = {"attn": ("evo_frag.h", "evo_fwd.hip", "evo_bwd.hip", "evo_bwd_
                   "proj_bwd": ("evo_frag.h", "evo_proj_bwd.hip"),
                   "pb": ("evo_frag.h", "evo_pair_bias.hip"),
                   "pb_bwd": ("evo_frag.h", "evo_pair_bias_bwd.hip"),
-                  "optim": ("evo_frag.h", "evo_optim.hip")}
+                  "optim": ("evo_frag.h", "evo_optim.hip"),
+                  "relpos": ("evo_frag.h", "evo_relpos.hip"),
+                  "muon": ("evo_frag.h", "evo_ns.h", "evo_muon.hip")}
 
 
 def kernel_family(kernel: str) -> str:
@@ -1038,6 +1040,10 @@ def kernel_family(kernel: str) -> str:
         return "pb"
     if kernel in ("adam_swa_kernel", "sumsq_kernel", "clip_scale_kernel"):
         return "optim"
+    if kernel.startswith("relpos_"):
+        return "relpos"
+    if kernel.startswith("ns_"):
+        return "muon"
     return "ln" if kernel.startswith("ln_") else "attn"
 
 
