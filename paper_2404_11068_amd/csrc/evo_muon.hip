@@ -724,15 +724,14 @@ __device__ __forceinline__ void tri_frag(Frag<NP> &f, char *base, int r, int k, 
 // ---- matrices that fit into LDS: everything in one workgroup
 //
 // X and the triangle of A, then of P in its place, lie in LDS: 128 x 224 entries, 64 x 576,
-// 32 x 1216.  A product's results wait in registers until every
-// wave has read its operands.  One launch does the norm, the steps and the
+// 32 x 1216.  P's entries wait in registers until every wave has read A.  One launch does the norm, the steps and the
 // update: memory sees each entry once.  Each of 16 waves takes a unit of the
-// triangle (10 of them at 128 x 128) and one to three of X; what bounds it is
-// the chain of a unit, LDS reads, matrix instructions, splitting and
-// storing, so the next operands are read before the matrix instructions of the last, and
-// for the whole of it the LDS reads (12000 cycles a step at 128 x 128; the matrix
-// instructions take 7700).  128 x 128: 39 us, bf16 35; one matrix per CU at a time, 1515
-// matrices of a model in 350 us.
+// triangle (10 of them at 128 x 128), then unit columns of X.  What bounds it are the
+// chains of a unit, LDS reads, matrix instructions, splitting and storing: at 128 x 128
+// 4000 cycles a step for the Gram matrix, 6800 for the polynomial and 6200 for P X,
+// against 1900, 1900 and 3100 of matrix instructions on the busiest SIMD; so the next operands
+// are read before the matrix instructions of the last.  128 x 128: 39 us, bf16 34; 256
+// matrices of 128 x 224 71 us (with a unit of X a wave instead of columns 74; 96 x 352: 66 and 71).
 
 constexpr int kSmallUnits = 40;
 constexpr int kSmallLds = 39 * kUnit;
@@ -838,7 +837,32 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
     const bool mine = wave < tri;  // (R <= 4: ten units at most)
     int ta, tb;
     unit_of(mine ? wave : 0, ta, tb);
-    constexpr int UNITS = (kSmallUnits + kSmallWaves - 1) / kSmallWaves;
+    auto columns = [&](auto np, auto rows) {
+        constexpr int NP = decltype(np)::value, RR = decltype(rows)::value;
+        for (int b = wave; b < C; b += kSmallWaves) {
+            f32x16 acc[RR];  // lane = row, registers = columns
+#pragma unroll
+            for (int a = 0; a < RR; ++a) zero(acc[a]);
+            Frag<NP> x[2], f[2];  // operands one ahead: P's of the next row, X's of the next half unit
+            x_cols(b)(x[0], 0, 0);
+            tri_frag(f[0], A, 0, 0, 0, lane);
+#pragma unroll
+            for (int at = 0; at < 2 * RR * RR; ++at) {
+                const int a = at % RR, half = at / RR, next = at + 1;
+                if (a == 0 && half + 1 < 2 * RR) x_cols(b)(x[(half + 1) & 1], (half + 1) >> 1, (half + 1) & 1);
+                if (next < 2 * RR * RR) tri_frag(f[next & 1], A, next % RR, next / RR >> 1, next / RR & 1, lane);
+                __builtin_amdgcn_sched_barrier(0);
+                mma(acc[a], x[half & 1], f[at & 1]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int a = 0; a < RR; ++a) {
+                half4 out[4][NP];
+                pack_unit(acc[a], 1.0f, out);
+                store_unit(X + (a * C + b) * kUnit, out, n, h);
+            }
+        }
+    };
     // a step on NP planes; the last leaves P
     auto one_step = [&](auto np, bool last) {
         constexpr int NP = decltype(np)::value;
@@ -879,23 +903,12 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
             __syncthreads();
         }
         if (last) return;
-        half4 out[UNITS][4][NP];
-#pragma unroll
-        for (int x = 0; x < UNITS; ++x) {
-            const int t = wave + x * kSmallWaves;
-            if (t < R * C) {
-                const int a = t / C, b = t - a * C;
-                f32x16 acc;  // lane = row, registers = columns
-                contract(np, acc, R, x_cols(b), a_rows(a));
-                pack_unit(acc, 1.0f, out[x]);
-            }
-        }
-        __syncthreads();
-#pragma unroll
-        for (int x = 0; x < UNITS; ++x) {
-            const int t = wave + x * kSmallWaves;
-            if (t < R * C) store_unit(X + t * kUnit, out[x], n, h);
-        }
+        // X = P X: a wave takes whole unit columns, reads each X operand once for all its rows and stores
+        // them in their place, which no other wave reads
+        if (R == 1) columns(np, Int<1>{});
+        else if (R == 2) columns(np, Int<2>{});
+        else if (R == 3) columns(np, Int<3>{});
+        else columns(np, Int<4>{});
         __syncthreads();
     };
     // the last step's P X: the lanes go along the matrix's memory rows
