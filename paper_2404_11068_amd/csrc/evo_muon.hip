@@ -350,16 +350,20 @@ __global__ __launch_bounds__(256) void ns_update_kernel(NsWork w, NsParams p, in
 
 // ---- results
 
-// entries of P = a I + b A + c A A from those of the product (scale 2^20) and of A (2^10);
-// diagonal: which of the four lies on it, if any
+// entries of P = a I + b A + c A A from those of the product (scale 2^20) and of A (2^10), three operations
+// each (mixed fused multiply-adds take the halves as they are); diagonal: whether the unit lies on it
+// (wave-uniform), and then which of the four does, if any
 template <int NP>
-__device__ __forceinline__ void poly4(float (&q)[4], const half4 (&old)[NP], const NsParams &p, int diagonal) {
+__device__ __forceinline__ void poly4(float (&q)[4], const half4 (&old)[NP], const NsParams &p, bool diagonal, int which) {
+    const float b = p.b * kUnscale, c = p.c * (kUnscale * kUnscale);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        float o = (float)old[0][e];
-        if constexpr (NP == 2) o += (float)old[1][e];
-        q[e] = fmaf(p.c * (kUnscale * kUnscale), q[e], p.b * kUnscale * o);
-        q[e] += e == diagonal ? p.a : 0.0f;
+        q[e] = fmaf((float)old[0][e], b, c * q[e]);
+        if constexpr (NP == 2) q[e] = fmaf((float)old[1][e], b, q[e]);
+    }
+    if (diagonal) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) q[e] += e == which ? p.a : 0.0f;
     }
 }
 
@@ -643,7 +647,7 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, i
                         half4 old[NP];
 #pragma unroll
                         for (int z = 0; z < NP; ++z) old[z] = *(const half4 *)(v.A + at + z * kPlane + pos);
-                        poly4(q, old, p, i == j ? n - 8 * g - 4 * h : -1);
+                        poly4(q, old, p, i == j, n - 8 * g - 4 * h);
                     }
                     split4(q, KIND == kPoly ? 1.0f : kUnscale, out[g]);
 #pragma unroll
@@ -728,10 +732,10 @@ __device__ __forceinline__ void tri_frag(Frag<NP> &f, char *base, int r, int k, 
 // update: memory sees each entry once.  Each of 16 waves takes a unit of the
 // triangle (10 of them at 128 x 128), then unit columns of X.  What bounds it are the
 // chains of a unit, LDS reads, matrix instructions, splitting and storing: at 128 x 128
-// 4000 cycles a step for the Gram matrix, 6800 for the polynomial and 6200 for P X,
+// 4000 cycles a step for the Gram matrix, 6200 for the polynomial and 6200 for P X,
 // against 1900, 1900 and 3100 of matrix instructions on the busiest SIMD; so the next operands
-// are read before the matrix instructions of the last.  128 x 128: 39 us, bf16 34; 256
-// matrices of 128 x 224 71 us (with a unit of X a wave instead of columns 74; 96 x 352: 66 and 71).
+// are read before the matrix instructions of the last.  128 x 128: 37 us, bf16 32; 256
+// matrices of 128 x 224 68 us, of 96 x 352 64.
 
 constexpr int kSmallUnits = 40;
 constexpr int kSmallLds = 39 * kUnit;
@@ -894,7 +898,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
 #pragma unroll
                     for (int z = 0; z < NP; ++z)
                         old[z] = *(const half4 *)(at + z * kPlane + chunk(n, g & 1, g >> 1) + h * 8);
-                    poly4(q, old, p, ta == tb ? n - 8 * g - 4 * h : -1);
+                    poly4(q, old, p, ta == tb, n - 8 * g - 4 * h);
                     split4(q, 1.0f, out[g]);
                 }
             }
@@ -1093,7 +1097,7 @@ struct MatrixWg {
                         float q[4];
 #pragma unroll
                         for (int e = 0; e < 4; ++e) q[e] = acc[u][4 * g + e];
-                        poly4(q, old, p, i == j ? n - 8 * g - 4 * h : -1);
+                        poly4(q, old, p, i == j, n - 8 * g - 4 * h);
                         split4(q, 1.0f, out[u][g]);
                     }
                     __builtin_amdgcn_sched_barrier(0);
