@@ -337,18 +337,20 @@ hipError_t launch_fwd_t(const RpArgs &a, hipStream_t s) {
 // in a histogram in LDS, [bucket][C columns], so the wave's accesses touch
 // different banks whatever the buckets are, and nothing depends on timing.
 // (LDS float atomics to the same places took 200 cycles an instruction.)
-// A lane's piece of four entries reads its four sums at once, adds with
-// duplicates among the four resolved in registers, and writes them back in
-// order: one LDS round trip per piece instead of four.  At the end the columns
+// A lane's piece of four entries is first summed within its buckets, each entry with
+// those before it; then it reads its four sums at once, adds, and writes them back
+// in order: one LDS round trip per piece instead of four.  At the end the columns
 // of every row are summed in a fixed order, and a second kernel adds the
 // waves' sums in order, in fp64.
 //
-// 16 planes of 2048 x 2048: 65 buckets 56 us (4.8 TB/s), 129 79 us, 257 115 us, 513 in two passes 302 us:
+// 16 planes of 2048 x 2048: 65 buckets 56 us (4.8 TB/s), 129 72 us, 257 96 us, 513 in two passes 259 us:
 // with more than 66 buckets the turns' chains of LDS reads, additions and writes bound it, not HBM.
+// (The sums within the piece, taken in each turn, were 79, 115 and 302 us; two pieces a round trip 76, 97, 264.)
 //
 // C is 64, one column per lane, for up to 66 buckets.  With more of them that
 // would leave a SIMD fewer than two waves, so 32 or 16 columns serve the
-// wave's halves or quarters in turn.
+// wave's halves or quarters in turn (257 buckets: 16 columns and two workgroups per CU 114 us, 32 and one
+// 124; 127 buckets: 32 and two 79, 64 and one 86, all with the sums in the turns).
 //
 // A wave takes one head and a run of 4-entry pieces of its rows, 64 at a time.
 // The last piece of a row whose length is no multiple of four starts earlier,
@@ -509,6 +511,14 @@ __device__ __forceinline__ void rp_accumulate(const RpArgs &a, const RpFind &f, 
                     n[u][x] = (int)(k < (unsigned)span ? k : (unsigned)span - 1);
                 }
             }
+            // an entry brings along those before it in its bucket: the last one's write holds them all
+#pragma unroll
+            for (int x = 1; x < P; ++x) {
+                float s = 0.0f;
+#pragma unroll
+                for (int y = 0; y < x; ++y) s = n[u][y] == n[u][x] ? g[y] : s;
+                g[x] += s;
+            }
 #pragma unroll
             for (int turn = 0; turn < 64 / C; ++turn) {
                 if (C == 64 || lane / C == turn) {
@@ -516,13 +526,7 @@ __device__ __forceinline__ void rp_accumulate(const RpArgs &a, const RpFind &f, 
 #pragma unroll
                     for (int x = 0; x < P; ++x) v[x] = hist[n[u][x] * C];
 #pragma unroll
-                    for (int x = 0; x < P; ++x) {
-#pragma unroll
-                        for (int y = 0; y < x; ++y) v[x] = n[u][y] == n[u][x] ? v[y] : v[x];
-                        v[x] += g[x];
-                    }
-#pragma unroll
-                    for (int x = 0; x < P; ++x) hist[n[u][x] * C] = v[x];
+                    for (int x = 0; x < P; ++x) hist[n[u][x] * C] = v[x] + g[x];
                 }
                 // the turns' accesses to a column stay in order
                 if (C < 64) __builtin_amdgcn_wave_barrier();
