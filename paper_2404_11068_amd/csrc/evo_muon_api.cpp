@@ -27,23 +27,23 @@ int64_t tiles_of(int64_t n, int64_t tile) { return (n + tile - 1) / tile; }
 int64_t triangle(int64_t n) { return n * (n + 1) / 2; }
 int64_t blocks_of(int64_t rows, int64_t cols) { return tiles_of(rows, evo::kNsBlock) * tiles_of(cols, evo::kNsBlock); }
 
-// whether the iterate stays in the kernels' range: the largest singular value,
-// followed from 1 (no singular value of X exceeds the Frobenius norm) through
-// the steps' polynomial, sampled finely enough that a step between two samples
-// adds less than the margin left below the range's end
+// whether the iterate stays in the kernels' range: the largest singular value, followed from 1 (no
+// singular value of X exceeds the Frobenius norm) through the steps.  Each takes s of [0, top] to
+// |a s + b s^3 + c s^5|, whose largest value lies at the end or where a + 3 b t + 5 c t^2 = 0, t = s^2
 int check_coefs(double a, double b, double c, double eps, int steps) {
     if (!isfinite(a) || !isfinite(b) || !isfinite(c) || !(eps > 0.0) || !isfinite(eps) || steps < 1)
         return EVO_ERR_INVALID_ARG;
     if (steps > 64) return EVO_ERR_UNSUPPORTED;
+    auto value = [&](double t) { return fabs(sqrt(t) * (a + t * (b + t * c))); };
+    const double disc = 9.0 * b * b - 20.0 * a * c, q = -0.5 * (3.0 * b + copysign(sqrt(disc), b));
+    const double turns[] = {q / (5.0 * c), a / q};  // (not a number, or no place in the range, where there is none)
     double top = 1.0;
     for (int k = 0; k < steps; ++k) {
         const double t2 = top * top;
         if (!(top <= 8.0) || !(fabs(a) + fabs(b) * t2 + fabs(c) * t2 * t2 <= 60.0)) return EVO_ERR_UNSUPPORTED;
-        double next = 0.0;
-        for (int i = 0; i <= 1024; ++i) {
-            const double s = top * i / 1024.0, s2 = s * s;
-            next = fmax(next, fabs(s * (a + s2 * (b + s2 * c))));
-        }
+        double next = value(t2);
+        for (const double t : turns)
+            if (t > 0.0 && t < t2) next = fmax(next, value(t));
         top = next;
     }
     return top <= 8.0 ? EVO_OK : EVO_ERR_UNSUPPORTED;

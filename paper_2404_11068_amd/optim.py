@@ -188,8 +188,8 @@ def _orth_dims(shape, dtype, steps, coefs, eps) -> evo_orth_dims:
     if len(shape) not in (2, 3) or dtype not in _ORTH_DTYPES:
         raise ValueError("x must be a float32 or bfloat16 matrix [m, n] or stack of matrices [N, m, n]")
     n = shape[0] if len(shape) == 3 else 1
-    return evo_orth_dims(_ORTH_DTYPES[dtype], int(steps), n, shape[-2], shape[-1], *(float(v) for v in coefs),
-                         float(eps), 0)
+    a, b, c = coefs
+    return evo_orth_dims(_ORTH_DTYPES[dtype], steps, n, shape[-2], shape[-1], a, b, c, eps, 0)
 
 
 def orthogonalize_workspace_size(shape, dtype, *, steps: int = 5, coefs: Tuple[float, float, float] = NEWTON_SCHULZ_COEFS,
@@ -207,19 +207,20 @@ def orthogonalize(x: torch.Tensor, *, steps: int = 5, coefs: Tuple[float, float,
     fp32 to fp32's precision, bf16 to about its rounding.  out may be x."""
     lib = _muon_lib()
     d = _orth_dims(x.shape, x.dtype, steps, coefs, eps)
-    if not x.is_contiguous() or not x.is_cuda or x.device.index != torch.cuda.current_device():
+    if not x.is_contiguous() or not x.is_cuda or x.get_device() != torch._C._cuda_getDevice():
         raise ValueError("x must be contiguous and on the current CUDA device")
     if out is None:
         out = _empty(x.shape, x.dtype, x, stream)
-    if out.shape != x.shape or out.dtype != x.dtype or not out.is_contiguous() or out.device != x.device:
+    elif out.shape != x.shape or out.dtype != x.dtype or not out.is_contiguous() or out.device != x.device:
         raise ValueError("out must be a contiguous tensor like x")
     if workspace is None:
-        need = int(lib.evo_orthogonalize_workspace_size(ctypes.byref(d)))
-        workspace = _empty(max(need, 1), torch.uint8, x, stream)
+        ws_bytes = lib.evo_orthogonalize_workspace_size(d)
+        workspace = _empty((max(ws_bytes, 1),), torch.uint8, x, stream)
     elif not workspace.is_contiguous() or workspace.device != x.device:
         raise ValueError("workspace must be contiguous and on the device of x")
-    st = lib.evo_orthogonalize(ctypes.byref(d), x.data_ptr(), out.data_ptr(), workspace.data_ptr(),
-                               workspace.numel() * workspace.element_size(), _stream(stream))
+    else:
+        ws_bytes = workspace.numel() * workspace.element_size()
+    st = lib.evo_orthogonalize(d, x.data_ptr(), out.data_ptr(), workspace.data_ptr(), ws_bytes, _stream(stream))
     if st:
         raise EvoAttnError(st, "evo_orthogonalize")
     return out

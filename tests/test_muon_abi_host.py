@@ -155,3 +155,26 @@ def test_rejects_more_tiles_than_a_launch_takes():
     # 64 of 32768 x 32768 are exactly 2^24
     assert _orth(_dims(n_batch=64, rows=32768, cols=32768)) == 2
     assert _plan([(32768, 32768)] * 64)[1] == -1
+
+
+def test_coefficients_are_followed_through_the_steps():
+    """The refusal against the largest singular value found on a fine grid, over coefficients of every kind."""
+    rng = np.random.default_rng(0)
+    kinds = {0: 0, 2: 0}
+    for _ in range(400):
+        a, b, c = rng.uniform(-4, 5), rng.choice([0.0, rng.uniform(-8, 8)]), rng.choice([0.0, rng.uniform(-4, 4)])
+        steps, top, ok, near = int(rng.integers(1, 9)), 1.0, True, False
+        for _ in range(steps):
+            size = abs(a) + abs(b) * top ** 2 + abs(c) * top ** 4
+            near |= abs(size - 60) < 1e-3 or abs(top - 8) < 1e-3
+            ok &= top <= 8 and size <= 60
+            if not ok:
+                break
+            s = np.linspace(0, top, 20001)
+            top = np.abs(s * (a + s * s * (b + s * s * c))).max()
+        near |= abs(top - 8) < 1e-3
+        ok &= top <= 8
+        if not near:
+            kinds[0 if ok else 2] += 1
+            assert _orth(_dims(a=a, b=b, c=c, steps=steps, n_batch=0)) == (0 if ok else 2), (a, b, c, steps, top)
+    assert min(kinds.values()) > 50
