@@ -38,9 +38,8 @@
  * with EVO_ERR_UNSUPPORTED.  A matrix with an infinity or a NaN gives NaN.
  *
  * Precision: iterates are pairs of fp16 (22 bits) with fp32 accumulation: fp32 results as
- * fp32 arithmetic would give them, low-rank matrices included.  The last two steps of bf16
- * matrices use 11 bits: their results are off by at most about 1.2 times their own
- * rounding to bf16.
+ * fp32 arithmetic would give them, low-rank matrices included.  bf16 matrices take the
+ * same steps: their results are those of the same values in fp32, rounded once.
  */
 #ifndef EVO_MUON_H
 #define EVO_MUON_H

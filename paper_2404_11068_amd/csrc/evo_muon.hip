@@ -8,10 +8,10 @@
 // on the fp16 matrix instructions with fp32 accumulation: the error of fp32
 // arithmetic (1e-6 .. 1e-5 of the result over five steps, low-rank inputs
 // too) at a third of the fp16 rate, which is five times the fp32 matrix rate.
-// The last two steps of a bf16 matrix use hi alone: what
-// they round is amplified by little, and the result is off by at most 1.2 times
-// its own rounding to bf16.  With hi alone in all steps it would be 2.4 times that for
-// low-rank inputs, with bf16 iterates 1e-2 and more.  X and A are stored times 2^10:
+// bf16 matrices go through the same steps and are rounded once, at the end: with hi
+// alone in the last two steps their error would grow by a tenth (1.84e-3 instead of
+// 1.66e-3 of a result), in all steps to 2.4 times their rounding for low-rank inputs.
+// X and A are stored times 2^10:
 // their entries stay below 64 (coefficients that could take them further
 // are refused), and those near 1 / sqrt(m n) stay clear of fp16's subnormals.
 //
@@ -136,41 +136,35 @@ __device__ __forceinline__ half8 frag_cols(const char *plane, int lane, int s) {
     return __builtin_bit_cast(half8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// Four values f v as fp16, or as two fp16 each that sum up to them within 22 bits.  Conversions
+// Four values f v as two fp16 each that sum up to them within 22 bits.  Conversions
 // two at a time, the remainder in one mixed fused multiply-add: 3 operations per value
 typedef float float2v __attribute__((ext_vector_type(2)));
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
-template <int NP>
-__device__ __forceinline__ void split4(const float (&v)[4], float f, half4 (&p)[NP]) {
+__device__ __forceinline__ void split4(const float (&v)[4], float f, half4 (&p)[kPlanes]) {
 #pragma unroll
     for (int e = 0; e < 4; e += 2) {
         const half2v hi = __builtin_convertvector((float2v{v[e] * f, v[e + 1] * f}), half2v);
         p[0][e] = hi.x;
         p[0][e + 1] = hi.y;
-        if constexpr (NP == 2) {
-            const half2v lo =
-                __builtin_convertvector((float2v{fmaf(v[e], f, -(float)hi.x), fmaf(v[e + 1], f, -(float)hi.y)}), half2v);
-            p[1][e] = lo.x;
-            p[1][e + 1] = lo.y;
-        }
+        const half2v lo =
+            __builtin_convertvector((float2v{fmaf(v[e], f, -(float)hi.x), fmaf(v[e + 1], f, -(float)hi.y)}), half2v);
+        p[1][e] = lo.x;
+        p[1][e + 1] = lo.y;
     }
 }
 
-constexpr int kSingleSteps = 2;  // last steps of a bf16 matrix that use one plane
 template <int N> struct Int { static constexpr int value = N; };
 
-template <int NP> struct Frag { half8 p[NP]; };
+struct Frag { half8 p[kPlanes]; };
 
-// the product's t-th term, the small ones first: lo hi, hi lo, hi hi (one plane: hi hi alone)
-template <int NP>
-__device__ __forceinline__ void mma_term(f32x16 &acc, const Frag<NP> &a, const Frag<NP> &b, int t) {
-    const int ia = NP == 2 && t == 0, ib = NP == 2 && t == 1;
-    acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a.p[ia], b.p[ib], acc, 0, 0, 0);
+// the product's t-th term, the small ones first: lo hi, hi lo, hi hi
+constexpr int kTerms = 3;
+__device__ __forceinline__ void mma_term(f32x16 &acc, const Frag &a, const Frag &b, int t) {
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a.p[t == 0], b.p[t == 1], acc, 0, 0, 0);
 }
-template <int NP>
-__device__ __forceinline__ void mma(f32x16 &acc, const Frag<NP> &a, const Frag<NP> &b) {
+__device__ __forceinline__ void mma(f32x16 &acc, const Frag &a, const Frag &b) {
 #pragma unroll
-    for (int t = 0; t < (NP == 2 ? 3 : 1); ++t) mma_term(acc, a, b, t);
+    for (int t = 0; t < kTerms; ++t) mma_term(acc, a, b, t);
 }
 
 // ---- norm, scaling and update: a thread owns 4 x 4 entries of a 64 x 64 tile.  Streams, bound by HBM:
@@ -353,13 +347,12 @@ __global__ __launch_bounds__(256) void ns_update_kernel(NsWork w, NsParams p, in
 // entries of P = a I + b A + c A A from those of the product (scale 2^20) and of A (2^10), three operations
 // each (mixed fused multiply-adds take the halves as they are); diagonal: whether the unit lies on it
 // (wave-uniform), and then which of the four does, if any
-template <int NP>
-__device__ __forceinline__ void poly4(float (&q)[4], const half4 (&old)[NP], const NsParams &p, bool diagonal, int which) {
+__device__ __forceinline__ void poly4(float (&q)[4], const half4 (&old)[kPlanes], const NsParams &p, bool diagonal, int which) {
     const float b = p.b * kUnscale, c = p.c * (kUnscale * kUnscale);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         q[e] = fmaf((float)old[0][e], b, c * q[e]);
-        if constexpr (NP == 2) q[e] = fmaf((float)old[1][e], b, q[e]);
+        q[e] = fmaf((float)old[1][e], b, q[e]);
     }
     if (diagonal) {
 #pragma unroll
@@ -368,8 +361,7 @@ __device__ __forceinline__ void poly4(float (&q)[4], const half4 (&old)[NP], con
 }
 
 // acc (a unit: lane = row, registers = columns) times f as packed quarters
-template <int NP>
-__device__ __forceinline__ void pack_unit(const f32x16 &acc, float f, half4 (&out)[4][NP]) {
+__device__ __forceinline__ void pack_unit(const f32x16 &acc, float f, half4 (&out)[4][kPlanes]) {
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
         float q[4];
@@ -378,12 +370,11 @@ __device__ __forceinline__ void pack_unit(const f32x16 &acc, float f, half4 (&ou
         split4(q, f, out[g]);
     }
 }
-template <int NP>
-__device__ __forceinline__ void store_unit(char *unit, const half4 (&out)[4][NP], int n, int h) {
+__device__ __forceinline__ void store_unit(char *unit, const half4 (&out)[4][kPlanes], int n, int h) {
 #pragma unroll
     for (int g = 0; g < 4; ++g)
 #pragma unroll
-        for (int z = 0; z < NP; ++z) *(half4 *)(unit + z * kPlane + chunk(n, g & 1, g >> 1) + h * 8) = out[g][z];
+        for (int z = 0; z < kPlanes; ++z) *(half4 *)(unit + z * kPlane + chunk(n, g & 1, g >> 1) + h * 8) = out[g][z];
 }
 
 // One unit's entries of the result, the lanes along the memory rows.  A buffer begins at the unit's
@@ -467,9 +458,9 @@ __device__ __forceinline__ void store_last(const View &v, const NsParams &p, con
 // in LDS, one unit column (32 contraction entries) per stage, copied by
 // global_load_lds 16 bytes a lane, S - 1 stages ahead: the copies are counted
 // by hand (vmcnt), one barrier per stage.  The matrix instructions bound large
-// products, the copies from L2 those of one plane, the chain of stages and the launch
-// small ones: 8 matrices of 2048 x 2048 in pairs, Gram 217 us (1.0 PFLOP/s of fp16 products), polynomial 224,
-// P X 352 (1.2); one such matrix 37, 40 and 46 us, in one plane 19, 23 and 22; 52 of 128 x 512 6.8, 5.0 and 9.4.
+// products, the chain of stages and the launch small
+// ones: 8 matrices of 2048 x 2048 in pairs, Gram 217 us (1.0 PFLOP/s of fp16 products), polynomial 224,
+// P X 352 (1.2); one such matrix 37, 40 and 46 us; 52 of 128 x 512 6.8, 5.0 and 9.4.
 
 enum { kGram, kPoly, kApply, kLast };
 struct Yes { static constexpr bool value = true; };
@@ -502,13 +493,12 @@ __device__ __forceinline__ void wait_copies_and_barrier() {
 // a barrier for what lies in LDS alone
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
 
-template <int T, int NP, int S, int KIND, bool MUON, bool BF16>
+template <int T, int S, int KIND, bool MUON, bool BF16>
 __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, int odd) {
     constexpr int U = T / 64;             // units of a wave's tile in each direction
     constexpr int N = T / 32;             // units of the workgroup's
-    constexpr int HELD = NP * kPlane;     // bytes of a unit in LDS
-    constexpr int STAGE = 2 * N * HELD;
-    constexpr int COPIES = U * HELD / 1024;  // of a wave and stage
+    constexpr int STAGE = 2 * N * kUnit;
+    constexpr int COPIES = U * kUnit / 1024;  // of a wave and stage
     constexpr bool SQUARE = KIND == kGram || KIND == kPoly;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const NsTile t = tile_of<SQUARE>(w, blockIdx.x);
@@ -544,9 +534,9 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, i
     }
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
     auto copy = [&](int k, int c) {  // the wave's c-th KB of stage k
-        const int q = c / (HELD / 1024), e = c % (HELD / 1024);
+        const int q = c / (kUnit / 1024), e = c % (kUnit / 1024);
         copy_to_lds(scalar(src[q] + k * step), (uint32_t)(e * 1024 + lane * 16),
-                    lds0 + (uint32_t)(k % S) * STAGE + (uint32_t)(wave * U + q) * HELD + e * 1024);
+                    lds0 + (uint32_t)(k % S) * STAGE + (uint32_t)(wave * U + q) * kUnit + e * 1024);
     };
 
     f32x16 acc[U][U];  // [row unit or, where the operands are swapped, ...]: see below
@@ -564,7 +554,7 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, i
     // a half stage are read while the other half's products run, one at a time between them, and so are the
     // copies issued (in a row each costs a fifth of the time)
     auto products = [&](auto swapped) {
-        constexpr int TERMS = NP == 2 ? 3 : 1, MMAS = TERMS * U * U, READS = 2 * U * NP;  // of a half
+        constexpr int MMAS = kTerms * U * U, READS = 2 * U * kPlanes;  // of a half
         constexpr bool AHEAD = S > 2;  // the next stage's first half is read, too, while this one's products run
 #pragma unroll
         for (int k = 0; k < S - 1; ++k)
@@ -572,11 +562,11 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, i
 #pragma unroll
                 for (int c = 0; c < COPIES; ++c) copy(k, c);
             }
-        Frag<NP> f0[2][U], f1[2][U];  // of the two halves of a stage
+        Frag f0[2][U], f1[2][U];  // of the two halves of a stage
         // r-th operand of half s, in the order of their use: the left ones' lo, the right ones' hi, ...
         auto read = [&](int k, int s, int r) {
-            const int a = r % U, z = r / U, left = z == 0 || z == 3, q = NP == 2 && (z == 0 || z == 2);
-            const char *at = lds + (k % S) * STAGE + q * kPlane + ((left ? wr * U : N + wc * U) + a) * HELD;
+            const int a = r % U, z = r / U, left = z == 0 || z == 3, q = z == 0 || z == 2;
+            const char *at = lds + (k % S) * STAGE + q * kPlane + ((left ? wr * U : N + wc * U) + a) * kUnit;
             if (left) f0[s][a].p[q] = frag_rows(at, lane, s);
             else f1[s][a].p[q] = SQUARE ? frag_rows(at, lane, s) : frag_cols(at, lane, s);
         };
@@ -584,7 +574,7 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, i
         // not used: a branch around the read would turn the next wait into one for all reads)
         auto half = [&](int k, int s, auto copying) {
 #pragma unroll
-            for (int t = 0; t < TERMS; ++t)
+            for (int t = 0; t < kTerms; ++t)
 #pragma unroll
                 for (int a = 0; a < U; ++a)
 #pragma unroll
@@ -627,7 +617,7 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, i
         // lane = column: stored as row `column` of the symmetric matrix's unit (j, i)
         products(No{});
         __syncthreads();  // the stages become scratch
-        char *const scratch = lds + wave * HELD;
+        char *const scratch = lds + wave * kUnit;
         char *const dst = KIND == kPoly ? v.P : v.A;
 #pragma unroll
         for (int a = 0; a < U; ++a)
@@ -636,7 +626,7 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, i
                 const int i = i0 + a, j = j0 + b;
                 if (i >= v.R || j >= v.R) continue;  // wave-uniform
                 const int64_t at = ((int64_t)j * v.R + i) * kUnit;
-                half4 out[4][NP];
+                half4 out[4][kPlanes];
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {  // rows 8 g + 4 h .. + 3 of the tile
                     const int pos = chunk(n, g & 1, g >> 1) + h * 8;
@@ -644,25 +634,25 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, i
 #pragma unroll
                     for (int e = 0; e < 4; ++e) q[e] = acc[a][b][4 * g + e];
                     if constexpr (KIND == kPoly) {
-                        half4 old[NP];
+                        half4 old[kPlanes];
 #pragma unroll
-                        for (int z = 0; z < NP; ++z) old[z] = *(const half4 *)(v.A + at + z * kPlane + pos);
+                        for (int z = 0; z < kPlanes; ++z) old[z] = *(const half4 *)(v.A + at + z * kPlane + pos);
                         poly4(q, old, p, i == j, n - 8 * g - 4 * h);
                     }
                     split4(q, KIND == kPoly ? 1.0f : kUnscale, out[g]);
 #pragma unroll
-                    for (int z = 0; z < NP; ++z) *(half4 *)(dst + at + z * kPlane + pos) = out[g][z];
+                    for (int z = 0; z < kPlanes; ++z) *(half4 *)(dst + at + z * kPlane + pos) = out[g][z];
                 }
                 if (t.ti != t.tj) {  // the mirrored unit (i, j), through LDS by columns
 #pragma unroll
                     for (int g = 0; g < 4; ++g)
 #pragma unroll
-                        for (int z = 0; z < NP; ++z)
+                        for (int z = 0; z < kPlanes; ++z)
                             *(half4 *)(scratch + z * kPlane + chunk(n, g & 1, g >> 1) + h * 8) = out[g][z];
                     __builtin_amdgcn_wave_barrier();
                     const int64_t mirrored = ((int64_t)i * v.R + j) * kUnit;
 #pragma unroll
-                    for (int z = 0; z < NP; ++z)
+                    for (int z = 0; z < kPlanes; ++z)
 #pragma unroll
                         for (int s = 0; s < 2; ++s)
                             *(half8 *)(dst + mirrored + z * kPlane + chunk(n, h, s)) = frag_cols(scratch + z * kPlane, lane, s);
@@ -684,10 +674,10 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, i
                     float q[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) q[e] = acc[a][b][4 * g + e];
-                    half4 out[NP];
+                    half4 out[kPlanes];
                     split4(q, 1.0f, out);
 #pragma unroll
-                    for (int z = 0; z < NP; ++z)
+                    for (int z = 0; z < kPlanes; ++z)
                         *(half4 *)(unit + z * kPlane + chunk(n, g & 1, g >> 1) + h * 8) = out[z];
                 }
             }
@@ -712,16 +702,15 @@ __device__ __forceinline__ char *tri_unit(char *base, int r, int k) {
     return base + (r * (r + 1) / 2 + k) * kUnit;
 }
 // rows of unit row r, contraction over unit column k (both wave-uniform)
-template <int NP>
-__device__ __forceinline__ void tri_frag(Frag<NP> &f, char *base, int r, int k, int s, int lane) {
+__device__ __forceinline__ void tri_frag(Frag &f, char *base, int r, int k, int s, int lane) {
     if (r >= k) {
         const char *u = tri_unit(base, r, k);
 #pragma unroll
-        for (int z = 0; z < NP; ++z) f.p[z] = frag_rows(u + z * kPlane, lane, s);
+        for (int z = 0; z < kPlanes; ++z) f.p[z] = frag_rows(u + z * kPlane, lane, s);
     } else {
         const char *u = tri_unit(base, k, r);
 #pragma unroll
-        for (int z = 0; z < NP; ++z) f.p[z] = frag_cols(u + z * kPlane, lane, s);
+        for (int z = 0; z < kPlanes; ++z) f.p[z] = frag_cols(u + z * kPlane, lane, s);
     }
 }
 
@@ -734,7 +723,7 @@ __device__ __forceinline__ void tri_frag(Frag<NP> &f, char *base, int r, int k, 
 // chains of a unit, LDS reads, matrix instructions, splitting and storing: at 128 x 128
 // 4000 cycles a step for the Gram matrix, 6200 for the polynomial and 6200 for P X,
 // against 1900, 1900 and 3100 of matrix instructions on the busiest SIMD; so the next operands
-// are read before the matrix instructions of the last.  128 x 128: 37 us, bf16 32; 256
+// are read before the matrix instructions of the last.  128 x 128: 37 us; 256
 // matrices of 128 x 224 68 us, of 96 x 352 64.
 
 constexpr int kSmallUnits = 40;
@@ -809,9 +798,9 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
         for (int e = 0; e < 16; ++e) x[e] = 0.0f;
     };
     // sum over k of left(k) right(k), each a loader of the operands of unit column k
-    auto contract = [&](auto np, f32x16 &acc, int K, auto left, auto right) {
+    auto contract = [&](f32x16 &acc, int K, auto left, auto right) {
         zero(acc);
-        Frag<decltype(np)::value> l[2], r[2];  // one half (16 entries) ahead
+        Frag l[2], r[2];  // one half (16 entries) ahead
         left(l[0], 0, 0);
         right(r[0], 0, 0);
         for (int k = 0; k < K; ++k) {
@@ -825,29 +814,29 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
         }
     };
     auto x_rows = [&](int a) {
-        return [&, a](auto &f, int k, int s) {
+        return [&, a](Frag &f, int k, int s) {
 #pragma unroll
-            for (int z = 0; z < (int)(sizeof(f.p) / sizeof(f.p[0])); ++z) f.p[z] = frag_rows(X + (a * C + k) * kUnit + z * kPlane, lane, s);
+            for (int z = 0; z < kPlanes; ++z) f.p[z] = frag_rows(X + (a * C + k) * kUnit + z * kPlane, lane, s);
         };
     };
     auto x_cols = [&](int b) {
-        return [&, b](auto &f, int k, int s) {
+        return [&, b](Frag &f, int k, int s) {
 #pragma unroll
-            for (int z = 0; z < (int)(sizeof(f.p) / sizeof(f.p[0])); ++z) f.p[z] = frag_cols(X + (k * C + b) * kUnit + z * kPlane, lane, s);
+            for (int z = 0; z < kPlanes; ++z) f.p[z] = frag_cols(X + (k * C + b) * kUnit + z * kPlane, lane, s);
         };
     };
-    auto a_rows = [&](int a) { return [&, a](auto &f, int k, int s) { tri_frag(f, A, a, k, s, lane); }; };
+    auto a_rows = [&](int a) { return [&, a](Frag &f, int k, int s) { tri_frag(f, A, a, k, s, lane); }; };
 
     const bool mine = wave < tri;  // (R <= 4: ten units at most)
     int ta, tb;
     unit_of(mine ? wave : 0, ta, tb);
-    auto columns = [&](auto np, auto rows) {
-        constexpr int NP = decltype(np)::value, RR = decltype(rows)::value;
+    auto columns = [&](auto rows) {
+        constexpr int RR = decltype(rows)::value;
         for (int b = wave; b < C; b += kSmallWaves) {
             f32x16 acc[RR];  // lane = row, registers = columns
 #pragma unroll
             for (int a = 0; a < RR; ++a) zero(acc[a]);
-            Frag<NP> x[2], f[2];  // operands one ahead: P's of the next row, X's of the next half unit
+            Frag x[2], f[2];  // operands one ahead: P's of the next row, X's of the next half unit
             x_cols(b)(x[0], 0, 0);
             tri_frag(f[0], A, 0, 0, 0, lane);
 #pragma unroll
@@ -861,15 +850,13 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
             }
 #pragma unroll
             for (int a = 0; a < RR; ++a) {
-                half4 out[4][NP];
+                half4 out[4][kPlanes];
                 pack_unit(acc[a], 1.0f, out);
                 store_unit(X + (a * C + b) * kUnit, out, n, h);
             }
         }
     };
-    // a step on NP planes; the last leaves P
-    auto one_step = [&](auto np, bool last) {
-        constexpr int NP = decltype(np)::value;
+    auto one_step = [&](bool last) {  // the last leaves P
         // (every address is the lane's part plus the unit's: made anew, or the compiler makes all of them
         // before the loop and spills them)
         asm volatile("" : "+v"(lane));
@@ -878,25 +865,25 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
         char *const at = tri_unit(A, tb, ta);
         if (mine) {
             f32x16 acc;  // lane = row of tb, registers = rows of ta
-            contract(np, acc, C, x_rows(ta), x_rows(tb));
-            half4 out[4][NP];
+            contract(acc, C, x_rows(ta), x_rows(tb));
+            half4 out[4][kPlanes];
             pack_unit(acc, kUnscale, out);
             store_unit(at, out, n, h);
         }
         __syncthreads();
         {
-            half4 out[4][NP];
+            half4 out[4][kPlanes];
             if (mine) {
                 f32x16 acc;
-                contract(np, acc, R, a_rows(ta), a_rows(tb));
+                contract(acc, R, a_rows(ta), a_rows(tb));
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
                     float q[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) q[e] = acc[4 * g + e];
-                    half4 old[NP];
+                    half4 old[kPlanes];
 #pragma unroll
-                    for (int z = 0; z < NP; ++z)
+                    for (int z = 0; z < kPlanes; ++z)
                         old[z] = *(const half4 *)(at + z * kPlane + chunk(n, g & 1, g >> 1) + h * 8);
                     poly4(q, old, p, ta == tb, n - 8 * g - 4 * h);
                     split4(q, 1.0f, out[g]);
@@ -909,31 +896,22 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
         if (last) return;
         // X = P X: a wave takes whole unit columns, reads each X operand once for all its rows and stores
         // them in their place, which no other wave reads
-        if (R == 1) columns(np, Int<1>{});
-        else if (R == 2) columns(np, Int<2>{});
-        else if (R == 3) columns(np, Int<3>{});
-        else columns(np, Int<4>{});
+        if (R == 1) columns(Int<1>{});
+        else if (R == 2) columns(Int<2>{});
+        else if (R == 3) columns(Int<3>{});
+        else columns(Int<4>{});
         __syncthreads();
     };
+    for (int step = 0; step < p.steps; ++step) one_step(step + 1 == p.steps);
     // the last step's P X: the lanes go along the matrix's memory rows
-    auto result = [&](auto np) {
-        for (int t = wave; t < R * C; t += kSmallWaves) {
-            const int a = t / C, b = t - a * C;
-            Result<MUON, BF16> res;
-            res.before(v, a, b, h, n);
-            f32x16 acc;
-            if (v.tr) contract(np, acc, R, x_cols(b), a_rows(a));
-            else contract(np, acc, R, a_rows(a), x_cols(b));
-            res.store(v, p, acc, a, b, h, n);
-        }
-    };
-    const int in_pairs = BF16 ? p.steps - kSingleSteps : p.steps;  // see the top
-    for (int step = 0; step < in_pairs; ++step) one_step(Int<2>{}, step + 1 == p.steps);
-    if constexpr (BF16) {
-        for (int step = in_pairs > 0 ? in_pairs : 0; step < p.steps; ++step) one_step(Int<1>{}, step + 1 == p.steps);
-        result(Int<1>{});
-    } else {
-        result(Int<2>{});
+    for (int t = wave; t < R * C; t += kSmallWaves) {
+        const int a = t / C, b = t - a * C;
+        Result<MUON, BF16> res;
+        res.before(v, a, b, h, n);
+        f32x16 acc;
+        if (v.tr) contract(acc, R, x_cols(b), a_rows(a));
+        else contract(acc, R, a_rows(a), x_cols(b));
+        res.store(v, p, acc, a, b, h, n);
     }
 }
 
@@ -977,25 +955,23 @@ struct MatrixWg {
     }
 
     __device__ __forceinline__ char *tri(int r, int k) const { return tri_unit(lds, r, k); }
-    template <int NP>
-    __device__ __forceinline__ void frag(Frag<NP> &f, int r, int k, int s) const { tri_frag(f, lds, r, k, s, lane); }
+    __device__ __forceinline__ void frag(Frag &f, int r, int k, int s) const { tri_frag(f, lds, r, k, s, lane); }
 
     // operands of unit rows r and r + 1 for unit column k, one branch for both
-    template <int NP>
-    __device__ __forceinline__ void block_frag(Frag<NP> *f, int r, int k, int s) const {
+    __device__ __forceinline__ void block_frag(Frag *f, int r, int k, int s) const {
         if (k <= r) {
 #pragma unroll
             for (int q = 0; q < 2; ++q)
 #pragma unroll
-                for (int z = 0; z < NP; ++z) f[q].p[z] = frag_rows(tri(r + q, k) + z * kPlane, lane, s);
+                for (int z = 0; z < kPlanes; ++z) f[q].p[z] = frag_rows(tri(r + q, k) + z * kPlane, lane, s);
         } else if (k > r + 1) {
 #pragma unroll
             for (int q = 0; q < 2; ++q)
 #pragma unroll
-                for (int z = 0; z < NP; ++z) f[q].p[z] = frag_cols(tri(k, r + q) + z * kPlane, lane, s);
+                for (int z = 0; z < kPlanes; ++z) f[q].p[z] = frag_cols(tri(k, r + q) + z * kPlane, lane, s);
         } else {
 #pragma unroll
-            for (int z = 0; z < NP; ++z) {
+            for (int z = 0; z < kPlanes; ++z) {
                 f[0].p[z] = frag_cols(tri(k, r) + z * kPlane, lane, s);
                 f[1].p[z] = frag_rows(tri(k, k) + z * kPlane, lane, s);
             }
@@ -1004,18 +980,18 @@ struct MatrixWg {
 
     // A = X X^T, then P in its place.  A wave has NU units (ui[u], uj[u]), uj >= ui, of the
     // triangle, products of the unit rows r[0 .. NR) as which[u] says
-    template <class W, int NP>
+    template <class W>
     __device__ __forceinline__ void gram_and_poly() const {
         const W t(wave);
         f32x16 acc[W::NU];
-        Frag<NP> f[2][W::NR];
+        Frag f[2][W::NR];
         auto zero = [&] {
 #pragma unroll
             for (int u = 0; u < W::NU; ++u)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) acc[u][e] = 0.0f;
         };
-        auto products = [&](const Frag<NP> (&x)[W::NR]) {
+        auto products = [&](const Frag (&x)[W::NR]) {
 #pragma unroll
             for (int u = 0; u < W::NU; ++u) mma(acc[u], x[W::left(u)], x[W::right(u)]);
         };
@@ -1025,7 +1001,7 @@ struct MatrixWg {
                 const char *src = scalar(v.x0 + ((int64_t)k * v.R + wave) * kUnit);
                 const uint32_t dst = lds0 + (uint32_t)(k % STAGES) * STAGE + wave * kUnit;
 #pragma unroll
-                for (int e = 0; e < NP * kPlane / 1024; ++e) copy_to_lds(src, (uint32_t)(e * 1024 + lane * 16), dst + e * 1024);
+                for (int e = 0; e < kUnit / 1024; ++e) copy_to_lds(src, (uint32_t)(e * 1024 + lane * 16), dst + e * 1024);
             }
         };
         zero();
@@ -1034,15 +1010,15 @@ struct MatrixWg {
             if (k < K) copy(k);
         // f[0] holds the first half of a unit column's operands, f[1] the second, each read while the
         // other's products run: at stage k the copies of stage k + 1 must have arrived, too
-        auto staged = [&](Frag<NP> (&x)[W::NR], int k, int s) {
+        auto staged = [&](Frag (&x)[W::NR], int k, int s) {
             const char *stage = lds + (k % STAGES) * STAGE;
 #pragma unroll
             for (int q = 0; q < W::NR; ++q)
 #pragma unroll
-                for (int z = 0; z < NP; ++z) x[q].p[z] = frag_cols(stage + t.row(q) * kUnit + z * kPlane, lane, s);
+                for (int z = 0; z < kPlanes; ++z) x[q].p[z] = frag_cols(stage + t.row(q) * kUnit + z * kPlane, lane, s);
         };
         for (int k = 0; k < K; ++k) {
-            if (k + 2 < K) wait_copies_and_barrier<NP * kPlane / 1024>();
+            if (k + 2 < K) wait_copies_and_barrier<kUnit / 1024>();
             else wait_copies_and_barrier<0>();
             if (k + STAGES - 1 < K) copy(k + STAGES - 1);
             if (t.any) {
@@ -1058,16 +1034,16 @@ struct MatrixWg {
 #pragma unroll
         for (int u = 0; u < W::NU; ++u)
             if (mine(u)) {
-                half4 out[4][NP];
+                half4 out[4][kPlanes];
                 pack_unit(acc[u], kUnscale, out);
                 store_unit(tri(t.row(W::right(u)), t.row(W::left(u))), out, n, h);
                 __builtin_amdgcn_sched_barrier(0);
             }
         lds_barrier();
-        half4 out[W::NU][4][NP];
+        half4 out[W::NU][4][kPlanes];
         if (t.any) {
             zero();
-            auto operands = [&](Frag<NP> (&x)[W::NR], int k, int s) {
+            auto operands = [&](Frag (&x)[W::NR], int k, int s) {
                 if constexpr (W::BLOCKS) {
                     block_frag(&x[0], t.row(0), k, s);
                     block_frag(&x[2], t.row(2), k, s);
@@ -1090,9 +1066,9 @@ struct MatrixWg {
                     const char *at = tri(j, i);
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
-                        half4 old[NP];
+                        half4 old[kPlanes];
 #pragma unroll
-                        for (int z = 0; z < NP; ++z)
+                        for (int z = 0; z < kPlanes; ++z)
                             old[z] = *(const half4 *)(at + z * kPlane + chunk(n, g & 1, g >> 1) + h * 8);
                         float q[4];
 #pragma unroll
@@ -1154,30 +1130,29 @@ struct MatrixWg {
         static constexpr int right(int) { return 0; }
     };
 
-    template <int NP>
     __device__ __forceinline__ void make_p() const {
         if constexpr (RB == 8) {
-            if (wave < 2) gram_and_poly<Diagonal, NP>();
-            else gram_and_poly<Off, NP>();
+            if (wave < 2) gram_and_poly<Diagonal>();
+            else gram_and_poly<Off>();
         } else {
-            if (wave < 4) gram_and_poly<Pair, NP>();  // (0, 0..1), (0, 2..3), (1, 2..3), (2, 2..3)
-            else gram_and_poly<Single, NP>();
+            if (wave < 4) gram_and_poly<Pair>();  // (0, 0..1), (0, 2..3), (1, 2..3), (2, 2..3)
+            else gram_and_poly<Single>();
         }
     }
 
     // X = P X in place, or (LAST) the result; ALONG: lane = column of the iterate, otherwise its row.
     // (Two waves with four rows of two columns each read P half as often but X twice, and took a fifth longer.)
-    template <bool LAST, bool ALONG, int NP>
+    template <bool LAST, bool ALONG>
     __device__ __forceinline__ void apply() const {
         constexpr int RING = RB > 4 ? 3 : 2;  // units of the column, loaded ahead
         for (int j = wave; j < v.C; j += kWgWaves) {
             char *const col = v.x0 + (int64_t)j * v.R * kUnit;
-            Frag<NP> x[RING][2];
+            Frag x[RING][2];
             auto load = [&](int k) {
 #pragma unroll
                 for (int s = 0; s < 2; ++s)
 #pragma unroll
-                    for (int z = 0; z < NP; ++z)
+                    for (int z = 0; z < kPlanes; ++z)
                         x[k % RING][s].p[z] = *(const half8 *)(col + k * kUnit + z * kPlane + chunk(n, h, s));
             };
             f32x16 acc[RB];
@@ -1196,7 +1171,7 @@ struct MatrixWg {
                     for (int s = 0; s < 2; ++s) {
 #pragma unroll
                         for (int i = 0; i < RB; ++i) {
-                            Frag<NP> f;  // (units past the matrix hold anything: those results are not used)
+                            Frag f;  // (units past the matrix hold anything: those results are not used)
                             frag(f, i, k, s);
                             if constexpr (ALONG || !LAST) mma(acc[i], f, x[k % RING][s]);
                             else mma(acc[i], x[k % RING][s], f);
@@ -1210,7 +1185,7 @@ struct MatrixWg {
                     if constexpr (LAST) {
                         store_last<MUON, BF16>(v, p, acc[i], col + i * kUnit, i, j, h, n);
                     } else {
-                        half4 out[4][NP];
+                        half4 out[4][kPlanes];
                         pack_unit(acc[i], 1.0f, out);
                         store_unit(col + i * kUnit, out, n, h);
                     }
@@ -1230,17 +1205,13 @@ __device__ __forceinline__ void matrix_steps(const NsWork &w, const NsParams &p,
 
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
     const MatrixWg<RB, MUON, BF16> g{p, v, lds, lds0, lane, wave, lane >> 5, lane & 31};
-    constexpr int END = BF16 ? 1 : 2;  // planes of the last steps: see the top
     for (int step = 1;; ++step) {
-        const bool pairs = !BF16 || step + kSingleSteps <= p.steps;
-        if (pairs) g.fresh().template make_p<2>();
-        else g.fresh().template make_p<END>();
+        g.fresh().make_p();
         if (step < p.steps) {
-            if (pairs) g.fresh().template apply<false, true, 2>();
-            else g.fresh().template apply<false, true, END>();
+            g.fresh().template apply<false, true>();
         } else {
-            if (v.tr) g.fresh().template apply<true, false, END>();
-            else g.fresh().template apply<true, true, END>();
+            if (v.tr) g.fresh().template apply<true, false>();
+            else g.fresh().template apply<true, true>();
             return;
         }
     }
@@ -1261,7 +1232,7 @@ ns_matrix_kernel(NsWork w, NsParams p, int first, int n8) {
     matrix_steps<RB, MUON, BF16>(w, p, first + k, lds);
 }
 
-template <int T, int NP, int KIND, bool MUON, bool BF16>
+template <int T, int KIND, bool MUON, bool BF16>
 hipError_t launch_product(NsWork w, const NsTile *tiles, int64_t grid, const NsParams &p, int odd, hipStream_t s) {
     w.tiles = tiles;
     const int r = w.uni.rows < w.uni.cols ? w.uni.rows : w.uni.cols, c = w.uni.rows + w.uni.cols - r;
@@ -1269,25 +1240,25 @@ hipError_t launch_product(NsWork w, const NsTile *tiles, int64_t grid, const NsP
     w.ntj = (c + T - 1) / T;
     auto launch = [&](auto stages) {
         constexpr int S = decltype(stages)::value;
-        hipLaunchKernelGGL((ns_product_kernel<T, NP, S, KIND, MUON, BF16>), dim3((unsigned)grid), dim3(256),
-                           S * 2 * (T / 32) * NP * kPlane, s, w, p, odd);
+        hipLaunchKernelGGL((ns_product_kernel<T, S, KIND, MUON, BF16>), dim3((unsigned)grid), dim3(256),
+                           S * 2 * (T / 32) * kUnit, s, w, p, odd);
     };
-    // S stages of copies.  Pairs of 128 x 128 take 32 KB a stage: with four of them a CU has one workgroup, with
+    // S stages of copies.  Tiles of 128 x 128 take 32 KB a stage: with four of them a CU has one workgroup, with
     // two stages it has two, which is better once there are enough (96 matrices of 256 x 256 in 269 us
     // instead of 318, P X of 8 of 2048 x 2048 in 352 instead of 366) and worse before (one: 57 instead of 44)
-    if (T == 128 && NP == 2 && grid > 256) launch(Int<T == 128 && NP == 2 ? 2 : 4>{});
+    if (T == 128 && grid > 256) launch(Int<T == 128 ? 2 : 4>{});
     else launch(Int<4>{});
     return hipGetLastError();
 }
 
-template <int T, int NP, bool MUON, bool BF16>
+template <int T, bool MUON, bool BF16>
 hipError_t launch_step(const NsWork &w, const NsLists &l, const NsParams &p, int odd, bool last, hipStream_t s) {
-    hipError_t e = launch_product<T, NP, kGram, false, false>(w, l.gram, l.n_gram, p, odd, s);
+    hipError_t e = launch_product<T, kGram, false, false>(w, l.gram, l.n_gram, p, odd, s);
     if (e != hipSuccess) return e;
-    e = launch_product<T, NP, kPoly, false, false>(w, l.gram, l.n_gram, p, odd, s);
+    e = launch_product<T, kPoly, false, false>(w, l.gram, l.n_gram, p, odd, s);
     if (e != hipSuccess) return e;
-    if (last) return launch_product<T, NP, kLast, MUON, BF16>(w, l.apply, l.n_apply, p, odd, s);
-    return launch_product<T, NP, kApply, false, false>(w, l.apply, l.n_apply, p, odd, s);
+    if (last) return launch_product<T, kLast, MUON, BF16>(w, l.apply, l.n_apply, p, odd, s);
+    return launch_product<T, kApply, false, false>(w, l.apply, l.n_apply, p, odd, s);
 }
 
 template <int T, bool MUON, bool BF16>
@@ -1327,12 +1298,7 @@ hipError_t launch_all(NsWork w, const NsLists &l, const NsParams &p, hipStream_t
     }
     for (int k = 0; k < p.steps && l.n_apply > 0; ++k) {
         const bool last = k + 1 == p.steps;
-        bool single = false;
-        if constexpr (BF16) {
-            single = k + kSingleSteps >= p.steps;  // see the top
-            if (single) e = launch_step<T, 1, MUON, BF16>(w, l, p, k & 1, last, s);
-        }
-        if (!single) e = launch_step<T, 2, MUON, BF16>(w, l, p, k & 1, last, s);
+        e = launch_step<T, MUON, BF16>(w, l, p, k & 1, last, s);
         if (e != hipSuccess) return e;
     }
     if constexpr (MUON) {

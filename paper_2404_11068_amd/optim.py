@@ -204,7 +204,7 @@ def orthogonalize(x: torch.Tensor, *, steps: int = 5, coefs: Tuple[float, float,
     """The matrix x [m, n], or every matrix of a stack [N, m, n], with its
     singular values brought near one by `steps` Newton-Schulz steps
     X <- a X + (b A + c A^2) X, A = X X^T, from X = x / max(|x|_F, eps).
-    fp32 to fp32's precision, bf16 to about its rounding.  out may be x."""
+    fp32 to fp32's precision; bf16 as the fp32 result rounded once.  out may be x."""
     lib = _muon_lib()
     d = _orth_dims(x.shape, x.dtype, steps, coefs, eps)
     if not x.is_contiguous() or not x.is_cuda or x.get_device() != torch._C._cuda_getDevice():
