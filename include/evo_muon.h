@@ -34,7 +34,7 @@
  *
  * Coefficients: the iterate is held in a limited range, so
  * coefficients that could take it out of it (singular values above 8, or
- * |b| s^2 + |c| s^4 above 60, followed from 1 over the steps) are refused
+ * |a| + |b| s^2 + |c| s^4 above 60, followed from 1 over the steps) are refused
  * with EVO_ERR_UNSUPPORTED.  A matrix with an infinity or a NaN gives NaN.
  *
  * Precision: iterates are pairs of fp16 (22 bits) with fp32 accumulation: fp32 results as

@@ -11,9 +11,9 @@
 // bf16 matrices go through the same steps and are rounded once, at the end: with hi
 // alone in the last two steps their error would grow by a tenth (1.84e-3 instead of
 // 1.66e-3 of a result), in all steps to 2.4 times their rounding for low-rank inputs.
-// X and A are stored times 2^10:
-// their entries stay below 64 (coefficients that could take them further
-// are refused), and those near 1 / sqrt(m n) stay clear of fp16's subnormals.
+// fp16's range: X and A are stored times one power of two and P times another, the largest at which no
+// entry passes 65504 for the coefficients' singular values (2^15 and 2^14 for the usual ones), so that
+// a pair holds 22 bits of what is not below 2^-14 of that, and less ends at 2^-25: 2^-40 of X and A, 2^-39 of P.
 //
 // Layout.  Iterates lie in the workspace as units of 32 x 32 entries, 2 KB per
 // plane, zero beyond the matrix.  Inside a unit 16-byte chunks (8 entries of a
@@ -30,8 +30,6 @@ namespace {
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 
-constexpr float kScale = 1024.0f;        // X and A are stored times this, P as it is: P X needs no scaling
-constexpr float kUnscale = 1.0f / 1024.0f;
 constexpr int kPlane = 2048, kPlanes = 2, kUnit = kPlanes * kPlane;  // bytes of a unit's plane, planes, bytes of a unit
 
 __host__ __device__ inline int units(int n) { return (n + 31) / 32; }
@@ -299,7 +297,7 @@ __global__ __launch_bounds__(256) void ns_scale_kernel(NsWork w, NsParams p) {
     if ((tid & 63) == 0) red[tid >> 6] = s;
     __syncthreads();
     const double norm = sqrt(((red[0] + red[1]) + red[2]) + red[3]);
-    const double f = (double)kScale / (norm < p.eps ? p.eps : norm);
+    const double f = p.scale / (norm < p.eps ? p.eps : norm);
     if (v.xt) pack_block<true>(u, v, v.x0, row0, col0, f);
     else pack_block<false>(u, v, v.x0, row0, col0, f);
 }
@@ -344,19 +342,18 @@ __global__ __launch_bounds__(256) void ns_update_kernel(NsWork w, NsParams p, in
 
 // ---- results
 
-// entries of P = a I + b A + c A A from those of the product (scale 2^20) and of A (2^10), three operations
+// entries of P = a I + b A + c A A from those of the product A A and of A, all with their scales, three operations
 // each (mixed fused multiply-adds take the halves as they are); diagonal: whether the unit lies on it
 // (wave-uniform), and then which of the four does, if any
 __device__ __forceinline__ void poly4(float (&q)[4], const half4 (&old)[kPlanes], const NsParams &p, bool diagonal, int which) {
-    const float b = p.b * kUnscale, c = p.c * (kUnscale * kUnscale);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        q[e] = fmaf((float)old[0][e], b, c * q[e]);
-        q[e] = fmaf((float)old[1][e], b, q[e]);
+        q[e] = fmaf((float)old[0][e], p.poly_b, p.poly_c * q[e]);
+        q[e] = fmaf((float)old[1][e], p.poly_b, q[e]);
     }
     if (diagonal) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) q[e] += e == which ? p.a : 0.0f;
+        for (int e = 0; e < 4; ++e) q[e] += e == which ? p.poly_a : 0.0f;
     }
 }
 
@@ -415,7 +412,7 @@ struct Result {
     __device__ __forceinline__ void store(const View &v, const NsParams &P, const f32x16 &acc, int iu, int ju, int h, int n) {
         const UnitOut<BF16> a(v, v.m.out, iu, ju, h, n);
         if constexpr (MUON) {
-            const float f = -P.lr * v.m.scale * kUnscale;
+            const float f = -P.lr * v.m.scale * P.from_last;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 p[e] = fmaf(f, acc[e], P.decay * p[e]);
@@ -430,8 +427,8 @@ struct Result {
         } else {
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                if constexpr (BF16) __builtin_amdgcn_raw_buffer_store_b16(f2bf(acc[e] * kUnscale), a.r, a.at(e), 0, 0);
-                else bstore4(__float_as_uint(acc[e] * kUnscale), a.r, a.at(e));
+                if constexpr (BF16) __builtin_amdgcn_raw_buffer_store_b16(f2bf(acc[e] * P.from_last), a.r, a.at(e), 0, 0);
+                else bstore4(__float_as_uint(acc[e] * P.from_last), a.r, a.at(e));
             }
         }
     }
@@ -445,7 +442,7 @@ __device__ __forceinline__ void store_last(const View &v, const NsParams &p, con
     if constexpr (MUON) {
         float *const o = (float *)unit + 128 * h + n;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) o[(8 * (e >> 2) + (e & 3)) * 32] = acc[e] * kUnscale;
+        for (int e = 0; e < 16; ++e) o[(8 * (e >> 2) + (e & 3)) * 32] = acc[e] * p.from_last;
     } else {
         Result<MUON, BF16> res;
         res.store(v, p, acc, iu, ju, h, n);
@@ -639,7 +636,7 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, i
                         for (int z = 0; z < kPlanes; ++z) old[z] = *(const half4 *)(v.A + at + z * kPlane + pos);
                         poly4(q, old, p, i == j, n - 8 * g - 4 * h);
                     }
-                    split4(q, KIND == kPoly ? 1.0f : kUnscale, out[g]);
+                    split4(q, KIND == kPoly ? 1.0f : p.from_gram, out[g]);
 #pragma unroll
                     for (int z = 0; z < kPlanes; ++z) *(half4 *)(dst + at + z * kPlane + pos) = out[g][z];
                 }
@@ -675,7 +672,7 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, i
 #pragma unroll
                     for (int e = 0; e < 4; ++e) q[e] = acc[a][b][4 * g + e];
                     half4 out[kPlanes];
-                    split4(q, 1.0f, out);
+                    split4(q, p.from_apply, out);
 #pragma unroll
                     for (int z = 0; z < kPlanes; ++z)
                         *(half4 *)(unit + z * kPlane + chunk(n, g & 1, g >> 1) + h * 8) = out[z];
@@ -771,7 +768,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
         s = red[0];
 #pragma unroll
         for (int k = 1; k < kSmallWaves; ++k) s += red[k];
-        const double norm = sqrt(s), f = (double)kScale / (norm < p.eps ? p.eps : norm);
+        const double norm = sqrt(s), f = p.scale / (norm < p.eps ? p.eps : norm);
 #pragma unroll
         for (int q = 0; q < BLOCKS; ++q) {
             const int k = q * THREADS + tid;
@@ -851,7 +848,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
 #pragma unroll
             for (int a = 0; a < RR; ++a) {
                 half4 out[4][kPlanes];
-                pack_unit(acc[a], 1.0f, out);
+                pack_unit(acc[a], p.from_apply, out);
                 store_unit(X + (a * C + b) * kUnit, out, n, h);
             }
         }
@@ -867,7 +864,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
             f32x16 acc;  // lane = row of tb, registers = rows of ta
             contract(acc, C, x_rows(ta), x_rows(tb));
             half4 out[4][kPlanes];
-            pack_unit(acc, kUnscale, out);
+            pack_unit(acc, p.from_gram, out);
             store_unit(at, out, n, h);
         }
         __syncthreads();
@@ -1035,7 +1032,7 @@ struct MatrixWg {
         for (int u = 0; u < W::NU; ++u)
             if (mine(u)) {
                 half4 out[4][kPlanes];
-                pack_unit(acc[u], kUnscale, out);
+                pack_unit(acc[u], p.from_gram, out);
                 store_unit(tri(t.row(W::right(u)), t.row(W::left(u))), out, n, h);
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -1186,7 +1183,7 @@ struct MatrixWg {
                         store_last<MUON, BF16>(v, p, acc[i], col + i * kUnit, i, j, h, n);
                     } else {
                         half4 out[4][kPlanes];
-                        pack_unit(acc[i], 1.0f, out);
+                        pack_unit(acc[i], p.from_apply, out);
                         store_unit(col + i * kUnit, out, n, h);
                     }
                     __builtin_amdgcn_sched_barrier(0);

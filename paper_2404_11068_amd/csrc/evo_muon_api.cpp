@@ -27,26 +27,50 @@ int64_t tiles_of(int64_t n, int64_t tile) { return (n + tile - 1) / tile; }
 int64_t triangle(int64_t n) { return n * (n + 1) / 2; }
 int64_t blocks_of(int64_t rows, int64_t cols) { return tiles_of(rows, evo::kNsBlock) * tiles_of(cols, evo::kNsBlock); }
 
-// whether the iterate stays in the kernels' range: the largest singular value, followed from 1 (no
+// Whether the iterate stays in range: the largest singular value, followed from 1 (no
 // singular value of X exceeds the Frobenius norm) through the steps.  Each takes s of [0, top] to
-// |a s + b s^3 + c s^5|, whose largest value lies at the end or where a + 3 b t + 5 c t^2 = 0, t = s^2
-int check_coefs(double a, double b, double c, double eps, int steps) {
+// |a s + b s^3 + c s^5|, whose largest value lies at the end or where a + 3 b t + 5 c t^2 = 0, t = s^2.
+// p: the coefficients and scales as the kernels take them
+int check_coefs(double a, double b, double c, double eps, int steps, evo::NsParams *p = nullptr) {
     if (!isfinite(a) || !isfinite(b) || !isfinite(c) || !(eps > 0.0) || !isfinite(eps) || steps < 1)
         return EVO_ERR_INVALID_ARG;
-    if (steps > 64) return EVO_ERR_UNSUPPORTED;
+    if (steps > 64 || fabs(a) + fabs(b) + fabs(c) > 60.0) return EVO_ERR_UNSUPPORTED;
     auto value = [&](double t) { return fabs(sqrt(t) * (a + t * (b + t * c))); };
-    const double disc = 9.0 * b * b - 20.0 * a * c, q = -0.5 * (3.0 * b + copysign(sqrt(disc), b));
-    const double turns[] = {q / (5.0 * c), a / q};  // (not a number, or no place in the range, where there is none)
-    double top = 1.0;
+    const double disc = 9.0 * b * b - 20.0 * a * c, q = -0.5 * (3.0 * b + copysign(sqrt(fmax(disc, 0.0)), b));
+    const double turns[] = {disc >= 0.0 && c != 0.0 ? q / (5.0 * c) : 0.0, disc >= 0.0 && q != 0.0 ? a / q : 0.0};  // (0: none)
+    auto largest = [&](double t2) {
+        double v = value(t2);
+        for (const double t : turns)
+            if (t > 0.0 && t < t2) v = fmax(v, value(t));
+        return v;
+    };
+    // `wide` is followed with room for the steps' roundings, far below 2^-12 each, and is what the scales go by
+    double top = 1.0, wide = 1.0, most = 1.0;
     for (int k = 0; k < steps; ++k) {
         const double t2 = top * top;
-        if (!(top <= 8.0) || !(fabs(a) + fabs(b) * t2 + fabs(c) * t2 * t2 <= 60.0)) return EVO_ERR_UNSUPPORTED;
-        double next = value(t2);
-        for (const double t : turns)
-            if (t > 0.0 && t < t2) next = fmax(next, value(t));
-        top = next;
+        if (top > 8.0 || fabs(a) + fabs(b) * t2 + fabs(c) * t2 * t2 > 60.0) return EVO_ERR_UNSUPPORTED;
+        most = fmax(most, wide);
+        top = largest(t2);
+        wide = fmin(largest(wide * wide) * (1.0 + 0x1p-12), 16.0);
     }
-    return top <= 8.0 ? EVO_OK : EVO_ERR_UNSUPPORTED;
+    if (top > 8.0) return EVO_ERR_UNSUPPORTED;
+    if (!p) return EVO_OK;
+    // Entries are at most the matrices' largest singular values: `most` for X, its square for A, and for P
+    // the largest |a + b t + c t^2| up to there, at an end or where b + 2 c t = 0
+    const double t2 = most * most, turn = c != 0.0 ? -b / (2.0 * c) : 0.0;
+    double gain = fmax(1.0, fmax(fabs(a), fabs(a + t2 * (b + t2 * c))));
+    if (turn > 0.0 && turn < t2) gain = fmax(gain, fabs(a + turn * (b + turn * c)));
+    const double xs = exp2(floor(log2(65000.0 / t2))), ps = exp2(floor(log2(65000.0 / gain)));
+    p->scale = xs;
+    p->poly_a = (float)(a * ps);
+    p->poly_b = (float)(b * ps / xs);
+    p->poly_c = (float)(c * ps / (xs * xs));
+    p->from_gram = (float)(1.0 / xs);
+    p->from_apply = (float)(1.0 / ps);
+    p->from_last = (float)(1.0 / (xs * ps));
+    p->eps = eps;
+    p->steps = steps;
+    return EVO_OK;
 }
 
 // ---- Muon plan: header, matrices, tiles of the norm, of the Gram matrix and of the iterate
@@ -216,13 +240,13 @@ bool make_plan(const evo_muon_tensor *t, int32_t n, Plan &p) {
     return true;
 }
 
-int check_orth(const evo_orth_dims *d) {
+int check_orth(const evo_orth_dims *d, evo::NsParams *p = nullptr) {
     if (!d || d->reserved != 0) return EVO_ERR_INVALID_ARG;
     if (d->dtype != EVO_DTYPE_F32 && d->dtype != EVO_DTYPE_BF16) return EVO_ERR_UNSUPPORTED;
     if (d->n_batch < 0 || d->rows < 0 || d->cols < 0) return EVO_ERR_INVALID_ARG;
     if (d->n_batch > (1 << 20) || d->rows > kMostSide || d->cols > kMostSide) return EVO_ERR_UNSUPPORTED;
     if ((d->n_batch + 7) * blocks_of(d->rows, d->cols) > kMostBlocks) return EVO_ERR_UNSUPPORTED;  // (see `grid`)
-    return check_coefs(d->a, d->b, d->c, d->eps, d->steps);
+    return check_coefs(d->a, d->b, d->c, d->eps, d->steps, p);
 }
 
 bool orth_empty(const evo_orth_dims *d) { return d->n_batch == 0 || d->rows == 0 || d->cols == 0; }
@@ -260,7 +284,8 @@ size_t evo_orthogonalize_workspace_size(const evo_orth_dims *d) {
 
 int evo_orthogonalize(const evo_orth_dims *d, const void *x, void *out, void *workspace, size_t workspace_bytes,
                       void *stream) {
-    const int st = check_orth(d);
+    evo::NsParams p{};
+    const int st = check_orth(d, &p);
     if (st) return st;
     if (orth_empty(d)) return EVO_OK;
     if (!x || !out) return EVO_ERR_INVALID_ARG;
@@ -285,12 +310,6 @@ int evo_orthogonalize(const evo_orth_dims *d, const void *x, void *out, void *wo
     w.n_mats = (int32_t)n;
     w.part = (double *)workspace;
     w.ws = (char *)workspace + round256(n * blocks_of(r, c) * 8);
-    evo::NsParams p{};
-    p.a = (float)d->a;
-    p.b = (float)d->b;
-    p.c = (float)d->c;
-    p.eps = d->eps;
-    p.steps = d->steps;
     NsLists l{};
     l.small_lds = evo::ns_small_bytes(d->rows, d->cols);
     l.tile = evo::ns_tile(n * triangle(tiles_of(r, 128)));
@@ -368,7 +387,8 @@ int evo_muon_step(const evo_muon_hparams *hp, const void *plan, const void *plan
     if (hp->momentum < 0.0 || hp->momentum >= 1.0 || hp->swa_decay < 0.0 || hp->swa_decay > 1.0 ||
         (hp->nesterov != 0 && hp->nesterov != 1))
         return EVO_ERR_INVALID_ARG;
-    const int st = check_coefs(hp->a, hp->b, hp->c, hp->eps, hp->steps);
+    evo::NsParams p{};
+    const int st = check_coefs(hp->a, hp->b, hp->c, hp->eps, hp->steps, &p);
     if (st) return st;
     if (h.n_mats == 0) return EVO_OK;
     if (!plan_device) return EVO_ERR_INVALID_ARG;
@@ -380,12 +400,6 @@ int evo_muon_step(const evo_muon_hparams *hp, const void *plan, const void *plan
     w.mats = (const NsMat *)(dev + h.off_mats);
     w.part = (double *)workspace;
     w.ws = (char *)workspace + h.part_bytes;
-    evo::NsParams p{};
-    p.a = (float)hp->a;
-    p.b = (float)hp->b;
-    p.c = (float)hp->c;
-    p.eps = hp->eps;
-    p.steps = hp->steps;
     p.mu = (float)hp->momentum;
     p.om_mu = (float)(1.0 - hp->momentum);
     p.u_g = hp->nesterov ? p.om_mu : 0.0f;

@@ -36,8 +36,10 @@ struct NsWork {
 };
 
 struct NsParams {
-    float a, b, c;
-    double eps;
+    // X and A are held times `scale`, P times a scale of its own, all powers of two.  P's coefficients with what
+    // brings A A and A to P's scale, and the factors of the products X X^T, P X and the last P X
+    float poly_a, poly_b, poly_c, from_gram, from_apply, from_last;
+    double scale, eps;
     int steps;
     // Muon (fp32): m = mu m + om_mu g, u = u_g g + u_m m, p = decay p - lr scale O, w = sd w + om_sd p
     float mu, om_mu, u_g, u_m, decay, lr, sd, om_sd;

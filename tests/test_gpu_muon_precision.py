@@ -1,13 +1,25 @@
-"""How near the Newton-Schulz results are to the fp32 and fp64 ones where the
-other tests' bounds are wide, in every form that a call can take.  bf16
-matrices go through the steps of fp32 ones: their results are the fp32 results
-of the same values, rounded once, bit for bit.
+"""How near the Newton-Schulz results are to the fp64 oracle where the other
+tests' bounds are wide: every form that a call can take (`FORMS`), both types,
+ends of the coefficients' range, norms far below eps, rows far smaller than
+others.
+
+Tolerances, with e = 2^-21 + sqrt(K) 2^-24 (operands of 22 bits, half a step 2^-22 each,
+fp32 accumulation over K <= max(m, n) terms).  A step's roundings change the
+iterate by at most C e of itself, C = 10 (|a| + 2 |b| |A| + 4 |c| |A|^2) / gain, and where the
+spectrum is flat the iterate grows along with the change: the changes of the steps add up,
+and twice that for the spread of the gains, see `_flat`.  bf16 matrices go
+through the same steps: their results are the fp32 ones of the same
+values, rounded once, bit for bit.
 """
+import math
+
 import numpy as np
 import pytest
 import torch
 
+from oracle import muon_oracle as mo
 from paper_2404_11068_amd import optim as op
+from tests.parity_util import to_f64
 
 pytestmark = pytest.mark.gpu
 
@@ -15,6 +27,30 @@ pytestmark = pytest.mark.gpu
 FORMS = [(1, 64, 64), (2, 352, 96), (3, 33, 7), (75, 100, 700), (73, 250, 161), (72, 256, 256), (1, 300, 260), (5, 200, 640),
          (1, 1930, 2010), (45, 300, 260)]
 IDS = lambda f: "%dx%dx%d" % f
+
+
+def _e(m, n):
+    return 2.0 ** -21 + math.sqrt(max(m, n)) * 2.0 ** -24
+
+
+def _frames(rng, N, m, n):
+    """Matrices of singular values 0.5 .. 1, the first and the last of them different from the rest."""
+    r = min(m, n)
+    x = np.empty((N, m, n))
+    some = [(np.linalg.qr(rng.standard_normal((m, r)))[0], np.linalg.qr(rng.standard_normal((n, r)))[0]) for _ in range(min(N, 3))]
+    for k in range(N):
+        u, v = some[0 if k == 0 else 2 if k == N - 1 and N > 2 else min(1, len(some) - 1)]
+        x[k] = (u * rng.uniform(0.5, 1.0, r)) @ v.T
+    return x
+
+
+def _norms(x):
+    return np.linalg.norm(x.reshape(x.shape[0], -1), axis=1)
+
+
+def _ends(x):
+    """First and last matrix: what a stack's others hold is covered by the tests of stacks."""
+    return x if x.shape[0] < 3 else x[[0, -1]]
 
 
 BF16 = FORMS + [(2, 128, 224), (2, 576, 64), (2, 1216, 32), (78, 130, 200), (80, 520, 120), (1, 150, 280), (24, 700, 390), (1, 1, 7)]
@@ -32,3 +68,44 @@ def test_bf16_is_the_fp32_result_rounded(form):
         for steps in (1, 2, 3, 5, 8):
             got, full = (op.orthogonalize(v, steps=steps, eps=1e-30) for v in (t, t.float()))
             assert full.any() and torch.equal(got, full.to(torch.bfloat16)), steps
+
+
+# coefficients that take singular values to 8 and hold them there (and a set that comes within 3e-4 of it once):
+# entries of A = X X^T reach 64
+AT_THE_END = [((1.5, -1 / 128, 0.0), 20), ((1.875, -1.25 / 64, 0.375 / 4096), 16)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("form", FORMS, ids=IDS)
+def test_coefficients_at_the_end_of_their_range(form, dtype):
+    """Slopes are at most the gains here, so changes add up: 2 steps C e of the result, C <= 10 (1.875 + 2.5 + 1.5)
+    with |A| = 64 and gains of one and more."""
+    print("\n[case] range", form, dtype, flush=True)
+    N, m, n = form
+    x = torch.from_numpy(_frames(np.random.default_rng(2), N, m, n)).to(dtype).cuda()
+    for coefs, steps in AT_THE_END:
+        got, ref = _ends(op.orthogonalize(x, steps=steps, coefs=coefs)), mo.orthogonalize(to_f64(_ends(x)), steps, coefs)
+        assert np.abs(np.linalg.norm(ref, 2, (1, 2)) - 8).max() < 0.1
+        bound = (2 * steps * 59 * _e(m, n) + (2.0 ** -8 if dtype == torch.bfloat16 else 0.0)) * _norms(ref)
+        assert (_norms(to_f64(got) - ref) <= bound).all(), (_norms(to_f64(got) - ref), bound)
+
+
+def test_one_singular_value_next_to_the_end():
+    """2 s + b s^3 has its largest value, 7.99973, at s = 5.9998: a matrix of one entry that gets there in its fourth step.
+    Each step's roundings, C = 10 (2 + 2 |b| 64) = 44 at most, are passed on by slopes of 2 at most: 2^8 44 e of 8."""
+    top, steps = 5.9998, 8
+    coefs = (2.0, -2 / (3 * top * top), 0.0)
+    for m, n in ((5, 9), (40, 300), (200, 300)):
+        lo, hi = 0.0, 1.0
+        for _ in range(200):   # the start from which three steps lead to `top`
+            mid = (lo + hi) / 2
+            lo, hi = (mid, hi) if mo.singular_map(mid, 3, coefs) < top else (lo, mid)
+        assert abs(mo.singular_map(hi, 4, coefs) - 2 * top / 1.5) < 1e-6 and hi < 1
+        for dtype in (torch.float32, torch.bfloat16):
+            x = torch.zeros(m, n, device="cuda")
+            x[m // 2, n // 3] = hi
+            x = x.to(dtype)
+            for k in range(1, steps + 1):
+                got, ref = to_f64(op.orthogonalize(x, steps=k, coefs=coefs, eps=1.0)), mo.orthogonalize(to_f64(x), k, coefs, 1.0)
+                tol = 2 ** k * 44 * _e(m, n) * 8 + (2.0 ** -8 * np.abs(ref).max() if dtype == torch.bfloat16 else 0.0)
+                assert np.abs(got - ref).max() <= tol, (m, n, dtype, k)
