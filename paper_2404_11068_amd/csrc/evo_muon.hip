@@ -14,6 +14,8 @@
 // fp16's range: X and A are stored times one power of two and P times another, the largest at which no
 // entry passes 65504 for the coefficients' singular values (2^15 and 2^14 for the usual ones), so that
 // a pair holds 22 bits of what is not below 2^-14 of that, and less ends at 2^-25: 2^-40 of X and A, 2^-39 of P.
+// A matrix whose norm is below eps, so that X is small as a whole, has another power of two on top, less of it
+// each step as X grows (Scales).
 //
 // Layout.  Iterates lie in the workspace as units of 32 x 32 entries, 2 KB per
 // plane, zero beyond the matrix.  Inside a unit 16-byte chunks (8 entries of a
@@ -29,6 +31,36 @@ namespace {
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+
+
+// The scales of X and A before step k, and what a step's products bring to the next ones.  A matrix of norm below
+// eps has a level, log2(eps / norm) rounded down: no singular value of its X is above 2^-level before the first step,
+// nor above 2^(growth k - level) before step k, so X has room for that much more
+constexpr int kMostLevel = 96;  // (what is smaller by more than that keeps fewer bits)
+__device__ __forceinline__ int more_at(const NsParams &p, int level, int k) {
+    const int e = (int)floorf((float)level - (float)k * p.growth);
+    return e > 0 ? e : 0;
+}
+__device__ __forceinline__ int level_of(const NsParams &p, double norm) {
+    if (!(norm < p.eps) || norm == 0.0) return 0;
+    const double q = p.eps / norm;
+    return q < 0x1p96 ? ilogb(q) : kMostLevel;
+}
+// what the entries of a matrix are multiplied with to be those of X before the first step
+__device__ __forceinline__ double first_scale(const NsParams &p, double norm, int level) {
+    return ldexp(p.scale, more_at(p, level, 0)) / (norm < p.eps ? p.eps : norm);
+}
+struct Scales {
+    float poly_a, poly_b, poly_c, from_gram, from_last;
+    __device__ __forceinline__ Scales(const NsParams &p, int level, int k) {
+        const int e = more_at(p, level, k), next = more_at(p, level, k + 1);
+        poly_a = ldexpf(p.poly_a, next - e);
+        poly_b = ldexpf(p.poly_b, next - 2 * e);
+        poly_c = ldexpf(p.poly_c, next - 3 * e);
+        from_gram = ldexpf(p.from_gram, -e);
+        from_last = ldexpf(p.from_last, -next);
+    }
+};
 
 constexpr int kPlane = 2048, kPlanes = 2, kUnit = kPlanes * kPlane;  // bytes of a unit's plane, planes, bytes of a unit
 
@@ -297,7 +329,9 @@ __global__ __launch_bounds__(256) void ns_scale_kernel(NsWork w, NsParams p) {
     if ((tid & 63) == 0) red[tid >> 6] = s;
     __syncthreads();
     const double norm = sqrt(((red[0] + red[1]) + red[2]) + red[3]);
-    const double f = p.scale / (norm < p.eps ? p.eps : norm);
+    const int level = level_of(p, norm);
+    if (tid == 0 && t.ti == 0 && t.tj == 0) w.levels[t.mat] = level;
+    const double f = first_scale(p, norm, level);
     if (v.xt) pack_block<true>(u, v, v.x0, row0, col0, f);
     else pack_block<false>(u, v, v.x0, row0, col0, f);
 }
@@ -345,7 +379,7 @@ __global__ __launch_bounds__(256) void ns_update_kernel(NsWork w, NsParams p, in
 // entries of P = a I + b A + c A A from those of the product A A and of A, all with their scales, three operations
 // each (mixed fused multiply-adds take the halves as they are); diagonal: whether the unit lies on it
 // (wave-uniform), and then which of the four does, if any
-__device__ __forceinline__ void poly4(float (&q)[4], const half4 (&old)[kPlanes], const NsParams &p, bool diagonal, int which) {
+__device__ __forceinline__ void poly4(float (&q)[4], const half4 (&old)[kPlanes], const Scales &p, bool diagonal, int which) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         q[e] = fmaf((float)old[0][e], p.poly_b, p.poly_c * q[e]);
@@ -409,10 +443,10 @@ struct Result {
             }
         }
     }
-    __device__ __forceinline__ void store(const View &v, const NsParams &P, const f32x16 &acc, int iu, int ju, int h, int n) {
+    __device__ __forceinline__ void store(const View &v, const NsParams &P, float from_last, const f32x16 &acc, int iu, int ju, int h, int n) {
         const UnitOut<BF16> a(v, v.m.out, iu, ju, h, n);
         if constexpr (MUON) {
-            const float f = -P.lr * v.m.scale * P.from_last;
+            const float f = -P.lr * v.m.scale * from_last;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 p[e] = fmaf(f, acc[e], P.decay * p[e]);
@@ -427,8 +461,8 @@ struct Result {
         } else {
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                if constexpr (BF16) __builtin_amdgcn_raw_buffer_store_b16(f2bf(acc[e] * P.from_last), a.r, a.at(e), 0, 0);
-                else bstore4(__float_as_uint(acc[e] * P.from_last), a.r, a.at(e));
+                if constexpr (BF16) __builtin_amdgcn_raw_buffer_store_b16(f2bf(acc[e] * from_last), a.r, a.at(e), 0, 0);
+                else bstore4(__float_as_uint(acc[e] * from_last), a.r, a.at(e));
             }
         }
     }
@@ -437,15 +471,15 @@ struct Result {
 // the last product's unit: for Muon as floats by memory rows in the unit's place, for ns_update_kernel,
 // otherwise the result itself
 template <bool MUON, bool BF16>
-__device__ __forceinline__ void store_last(const View &v, const NsParams &p, const f32x16 &acc, char *unit, int iu, int ju, int h,
-                                           int n) {
+__device__ __forceinline__ void store_last(const View &v, const NsParams &p, float from_last, const f32x16 &acc, char *unit, int iu,
+                                           int ju, int h, int n) {
     if constexpr (MUON) {
         float *const o = (float *)unit + 128 * h + n;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) o[(8 * (e >> 2) + (e & 3)) * 32] = acc[e] * p.from_last;
+        for (int e = 0; e < 16; ++e) o[(8 * (e >> 2) + (e & 3)) * 32] = acc[e] * from_last;
     } else {
         Result<MUON, BF16> res;
-        res.store(v, p, acc, iu, ju, h, n);
+        res.store(v, p, from_last, acc, iu, ju, h, n);
     }
 }
 
@@ -491,7 +525,7 @@ __device__ __forceinline__ void wait_copies_and_barrier() {
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
 
 template <int T, int S, int KIND, bool MUON, bool BF16>
-__global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, int odd) {
+__global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, int k0) {
     constexpr int U = T / 64;             // units of a wave's tile in each direction
     constexpr int N = T / 32;             // units of the workgroup's
     constexpr int STAGE = 2 * N * kUnit;
@@ -504,7 +538,9 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, i
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wr = wave >> 1, wc = wave & 1, h = lane >> 5, n = lane & 31;
+    const bool odd = k0 & 1;
     const char *x = KIND == kPoly ? v.A : odd ? v.x1 : v.x0;
+    const Scales sc(p, KIND == kApply ? 0 : w.levels[t.mat], k0);
     const int K = KIND == kGram ? v.C : v.R;  // unit columns of the contraction
 
     // this wave's share of a stage: U units; units past the matrix repeat its
@@ -634,9 +670,9 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, i
                         half4 old[kPlanes];
 #pragma unroll
                         for (int z = 0; z < kPlanes; ++z) old[z] = *(const half4 *)(v.A + at + z * kPlane + pos);
-                        poly4(q, old, p, i == j, n - 8 * g - 4 * h);
+                        poly4(q, old, sc, i == j, n - 8 * g - 4 * h);
                     }
-                    split4(q, KIND == kPoly ? 1.0f : p.from_gram, out[g]);
+                    split4(q, KIND == kPoly ? 1.0f : sc.from_gram, out[g]);
 #pragma unroll
                     for (int z = 0; z < kPlanes; ++z) *(half4 *)(dst + at + z * kPlane + pos) = out[g][z];
                 }
@@ -688,7 +724,7 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsWork w, NsParams p, i
             for (int b = 0; b < U; ++b) {
                 const int i = i0 + a, j = j0 + b;
                 if (i >= v.R || j >= v.C) continue;
-                store_last<MUON, BF16>(v, p, acc[a][b], (odd ? v.x0 : v.x1) + ((int64_t)i * v.C + j) * kUnit, i, j, h, n);
+                store_last<MUON, BF16>(v, p, sc.from_last, acc[a][b], (odd ? v.x0 : v.x1) + ((int64_t)i * v.C + j) * kUnit, i, j, h, n);
             }
     }
 }
@@ -745,6 +781,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
     const int R = v.R, C = v.C;
     char *const X = lds, *const A = lds + R * C * kUnit;
 
+    int level;
     {  // X = u / max(|u|, eps)
         const int per_row = 8 * (v.tr ? R : C), blocks = 64 * R * C;
         float u[BLOCKS][4][4];
@@ -768,7 +805,9 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
         s = red[0];
 #pragma unroll
         for (int k = 1; k < kSmallWaves; ++k) s += red[k];
-        const double norm = sqrt(s), f = p.scale / (norm < p.eps ? p.eps : norm);
+        const double norm = sqrt(s);
+        level = level_of(p, norm);
+        const double f = first_scale(p, norm, level);
 #pragma unroll
         for (int q = 0; q < BLOCKS; ++q) {
             const int k = q * THREADS + tid;
@@ -853,7 +892,8 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
             }
         }
     };
-    auto one_step = [&](bool last) {  // the last leaves P
+    auto one_step = [&](int step, bool last) {  // the last leaves P
+        const Scales sc(p, level, step);
         // (every address is the lane's part plus the unit's: made anew, or the compiler makes all of them
         // before the loop and spills them)
         asm volatile("" : "+v"(lane));
@@ -864,7 +904,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
             f32x16 acc;  // lane = row of tb, registers = rows of ta
             contract(acc, C, x_rows(ta), x_rows(tb));
             half4 out[4][kPlanes];
-            pack_unit(acc, p.from_gram, out);
+            pack_unit(acc, sc.from_gram, out);
             store_unit(at, out, n, h);
         }
         __syncthreads();
@@ -882,7 +922,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
 #pragma unroll
                     for (int z = 0; z < kPlanes; ++z)
                         old[z] = *(const half4 *)(at + z * kPlane + chunk(n, g & 1, g >> 1) + h * 8);
-                    poly4(q, old, p, ta == tb, n - 8 * g - 4 * h);
+                    poly4(q, old, sc, ta == tb, n - 8 * g - 4 * h);
                     split4(q, 1.0f, out[g]);
                 }
             }
@@ -899,8 +939,9 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
         else columns(Int<4>{});
         __syncthreads();
     };
-    for (int step = 0; step < p.steps; ++step) one_step(step + 1 == p.steps);
+    for (int step = 0; step < p.steps; ++step) one_step(step, step + 1 == p.steps);
     // the last step's P X: the lanes go along the matrix's memory rows
+    const float from_last = Scales(p, level, p.steps - 1).from_last;
     for (int t = wave; t < R * C; t += kSmallWaves) {
         const int a = t / C, b = t - a * C;
         Result<MUON, BF16> res;
@@ -908,7 +949,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
         f32x16 acc;
         if (v.tr) contract(acc, R, x_cols(b), a_rows(a));
         else contract(acc, R, a_rows(a), x_cols(b));
-        res.store(v, p, acc, a, b, h, n);
+        res.store(v, p, from_last, acc, a, b, h, n);
     }
 }
 
@@ -978,7 +1019,7 @@ struct MatrixWg {
     // A = X X^T, then P in its place.  A wave has NU units (ui[u], uj[u]), uj >= ui, of the
     // triangle, products of the unit rows r[0 .. NR) as which[u] says
     template <class W>
-    __device__ __forceinline__ void gram_and_poly() const {
+    __device__ __forceinline__ void gram_and_poly(const Scales &sc) const {
         const W t(wave);
         f32x16 acc[W::NU];
         Frag f[2][W::NR];
@@ -1032,7 +1073,7 @@ struct MatrixWg {
         for (int u = 0; u < W::NU; ++u)
             if (mine(u)) {
                 half4 out[4][kPlanes];
-                pack_unit(acc[u], p.from_gram, out);
+                pack_unit(acc[u], sc.from_gram, out);
                 store_unit(tri(t.row(W::right(u)), t.row(W::left(u))), out, n, h);
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -1070,7 +1111,7 @@ struct MatrixWg {
                         float q[4];
 #pragma unroll
                         for (int e = 0; e < 4; ++e) q[e] = acc[u][4 * g + e];
-                        poly4(q, old, p, i == j, n - 8 * g - 4 * h);
+                        poly4(q, old, sc, i == j, n - 8 * g - 4 * h);
                         split4(q, 1.0f, out[u][g]);
                     }
                     __builtin_amdgcn_sched_barrier(0);
@@ -1127,20 +1168,20 @@ struct MatrixWg {
         static constexpr int right(int) { return 0; }
     };
 
-    __device__ __forceinline__ void make_p() const {
+    __device__ __forceinline__ void make_p(const Scales &sc) const {
         if constexpr (RB == 8) {
-            if (wave < 2) gram_and_poly<Diagonal>();
-            else gram_and_poly<Off>();
+            if (wave < 2) gram_and_poly<Diagonal>(sc);
+            else gram_and_poly<Off>(sc);
         } else {
-            if (wave < 4) gram_and_poly<Pair>();  // (0, 0..1), (0, 2..3), (1, 2..3), (2, 2..3)
-            else gram_and_poly<Single>();
+            if (wave < 4) gram_and_poly<Pair>(sc);  // (0, 0..1), (0, 2..3), (1, 2..3), (2, 2..3)
+            else gram_and_poly<Single>(sc);
         }
     }
 
     // X = P X in place, or (LAST) the result; ALONG: lane = column of the iterate, otherwise its row.
     // (Two waves with four rows of two columns each read P half as often but X twice, and took a fifth longer.)
     template <bool LAST, bool ALONG>
-    __device__ __forceinline__ void apply() const {
+    __device__ __forceinline__ void apply(float from_last) const {
         constexpr int RING = RB > 4 ? 3 : 2;  // units of the column, loaded ahead
         for (int j = wave; j < v.C; j += kWgWaves) {
             char *const col = v.x0 + (int64_t)j * v.R * kUnit;
@@ -1180,7 +1221,7 @@ struct MatrixWg {
             for (int i = 0; i < RB; ++i) {
                 if (i < v.R) {
                     if constexpr (LAST) {
-                        store_last<MUON, BF16>(v, p, acc[i], col + i * kUnit, i, j, h, n);
+                        store_last<MUON, BF16>(v, p, from_last, acc[i], col + i * kUnit, i, j, h, n);
                     } else {
                         half4 out[4][kPlanes];
                         pack_unit(acc[i], p.from_apply, out);
@@ -1202,13 +1243,15 @@ __device__ __forceinline__ void matrix_steps(const NsWork &w, const NsParams &p,
 
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
     const MatrixWg<RB, MUON, BF16> g{p, v, lds, lds0, lane, wave, lane >> 5, lane & 31};
-    for (int step = 1;; ++step) {
-        g.fresh().make_p();
-        if (step < p.steps) {
-            g.fresh().template apply<false, true>();
+    const int level = w.levels[k];
+    for (int step = 0;; ++step) {
+        const Scales sc(p, level, step);
+        g.fresh().make_p(sc);
+        if (step + 1 < p.steps) {
+            g.fresh().template apply<false, true>(sc.from_last);
         } else {
-            if (v.tr) g.fresh().template apply<true, false>();
-            else g.fresh().template apply<true, true>();
+            if (v.tr) g.fresh().template apply<true, false>(sc.from_last);
+            else g.fresh().template apply<true, true>(sc.from_last);
             return;
         }
     }
@@ -1230,7 +1273,7 @@ ns_matrix_kernel(NsWork w, NsParams p, int first, int n8) {
 }
 
 template <int T, int KIND, bool MUON, bool BF16>
-hipError_t launch_product(NsWork w, const NsTile *tiles, int64_t grid, const NsParams &p, int odd, hipStream_t s) {
+hipError_t launch_product(NsWork w, const NsTile *tiles, int64_t grid, const NsParams &p, int k0, hipStream_t s) {
     w.tiles = tiles;
     const int r = w.uni.rows < w.uni.cols ? w.uni.rows : w.uni.cols, c = w.uni.rows + w.uni.cols - r;
     w.nti = (r + T - 1) / T;
@@ -1238,7 +1281,7 @@ hipError_t launch_product(NsWork w, const NsTile *tiles, int64_t grid, const NsP
     auto launch = [&](auto stages) {
         constexpr int S = decltype(stages)::value;
         hipLaunchKernelGGL((ns_product_kernel<T, S, KIND, MUON, BF16>), dim3((unsigned)grid), dim3(256),
-                           S * 2 * (T / 32) * kUnit, s, w, p, odd);
+                           S * 2 * (T / 32) * kUnit, s, w, p, k0);
     };
     // S stages of copies.  Tiles of 128 x 128 take 32 KB a stage: with four of them a CU has one workgroup, with
     // two stages it has two, which is better once there are enough (96 matrices of 256 x 256 in 269 us
@@ -1249,13 +1292,13 @@ hipError_t launch_product(NsWork w, const NsTile *tiles, int64_t grid, const NsP
 }
 
 template <int T, bool MUON, bool BF16>
-hipError_t launch_step(const NsWork &w, const NsLists &l, const NsParams &p, int odd, bool last, hipStream_t s) {
-    hipError_t e = launch_product<T, kGram, false, false>(w, l.gram, l.n_gram, p, odd, s);
+hipError_t launch_step(const NsWork &w, const NsLists &l, const NsParams &p, int k0, hipStream_t s) {
+    hipError_t e = launch_product<T, kGram, false, false>(w, l.gram, l.n_gram, p, k0, s);
     if (e != hipSuccess) return e;
-    e = launch_product<T, kPoly, false, false>(w, l.gram, l.n_gram, p, odd, s);
+    e = launch_product<T, kPoly, false, false>(w, l.gram, l.n_gram, p, k0, s);
     if (e != hipSuccess) return e;
-    if (last) return launch_product<T, kLast, MUON, BF16>(w, l.apply, l.n_apply, p, odd, s);
-    return launch_product<T, kApply, false, false>(w, l.apply, l.n_apply, p, odd, s);
+    if (k0 + 1 == p.steps) return launch_product<T, kLast, MUON, BF16>(w, l.apply, l.n_apply, p, k0, s);
+    return launch_product<T, kApply, false, false>(w, l.apply, l.n_apply, p, k0, s);
 }
 
 template <int T, bool MUON, bool BF16>
@@ -1294,8 +1337,7 @@ hipError_t launch_all(NsWork w, const NsLists &l, const NsParams &p, hipStream_t
         if (e != hipSuccess) return e;
     }
     for (int k = 0; k < p.steps && l.n_apply > 0; ++k) {
-        const bool last = k + 1 == p.steps;
-        e = launch_step<T, MUON, BF16>(w, l, p, k & 1, last, s);
+        e = launch_step<T, MUON, BF16>(w, l, p, k, s);
         if (e != hipSuccess) return e;
     }
     if constexpr (MUON) {

@@ -68,6 +68,7 @@ int check_coefs(double a, double b, double c, double eps, int steps, evo::NsPara
     p->from_gram = (float)(1.0 / xs);
     p->from_apply = (float)(1.0 / ps);
     p->from_last = (float)(1.0 / (xs * ps));
+    p->growth = (float)(log2(gain) * (1.0 + 0x1p-12));
     p->eps = eps;
     p->steps = steps;
     return EVO_OK;
@@ -76,13 +77,14 @@ int check_coefs(double a, double b, double c, double eps, int steps, evo::NsPara
 // ---- Muon plan: header, matrices, tiles of the norm, of the Gram matrix and of the iterate
 struct PlanHeader {
     uint64_t magic;
-    int64_t bytes, n_mats, ws_bytes, part_bytes;
+    int64_t bytes, n_mats, ws_bytes, part_bytes;  // part: partial sums of `blocks` tiles, and levels
+    int64_t blocks;
     // matrices in this order: by tiles, a workgroup each (8 and 4 units of rows), in LDS
     int64_t n_wg8, n_wg4, n_small, small_lds;
     int64_t tile, n_x, n_gram, n_apply;  // entries of the lists, padding included
     int64_t off_mats, off_x, off_gram, off_apply;
 };
-constexpr uint64_t kMagic = 0x45564f4d554f4e32ull;
+constexpr uint64_t kMagic = 0x45564f4d554f4e33ull;
 
 int64_t round256(int64_t n) { return (n + 255) & ~int64_t(255); }
 
@@ -182,9 +184,10 @@ bool make_plan(const evo_muon_tensor *t, int32_t n, Plan &p) {
         return form[a] != form[b] ? form[a] < form[b] : cost(size_of(t[a])) > cost(size_of(t[b]));
     });
     h.magic = kMagic;
+    h.blocks = blocks;
     h.tile = evo::ns_tile(gram128);
     h.n_mats = (int64_t)order.size();
-    h.part_bytes = round256(blocks * 8);
+    h.part_bytes = round256(blocks * 8 + h.n_mats * (int64_t)sizeof(int));
     h.ws_bytes = h.part_bytes;
     double load[8] = {};
     int64_t part = 0, off = 0;
@@ -255,12 +258,17 @@ bool orth_by_matrix(const evo_orth_dims *d) {
     return evo::ns_matrix_rows(d->rows, d->cols) > 0 && evo::ns_by_matrix((double)d->n_batch, 1.0);
 }
 
+// partial sums and levels
+int64_t orth_part(const evo_orth_dims *d) {
+    return round256(d->n_batch * (blocks_of(d->rows, d->cols) * 8 + (int64_t)sizeof(int)));
+}
+
 // (a stack that fits into the workgroups' LDS still asks for a little: a size of 0 means a refusal)
 size_t orth_workspace(const evo_orth_dims *d) {
     if (evo::ns_small_bytes(d->rows, d->cols) > 0) return 256;
     const int64_t each = orth_by_matrix(d) ? evo::ns_matrix_wg_bytes(d->rows, d->cols)
                                            : evo::ns_matrix_bytes(d->rows, d->cols);
-    return (size_t)(round256(d->n_batch * blocks_of(d->rows, d->cols) * 8) + d->n_batch * each);
+    return (size_t)(orth_part(d) + d->n_batch * each);
 }
 
 // no C++ exception leaves a C entry: `none` where the plan's memory cannot be had
@@ -309,7 +317,8 @@ int evo_orthogonalize(const evo_orth_dims *d, const void *x, void *out, void *wo
     w.ws_stride = evo::ns_matrix_bytes(d->rows, d->cols);
     w.n_mats = (int32_t)n;
     w.part = (double *)workspace;
-    w.ws = (char *)workspace + round256(n * blocks_of(r, c) * 8);
+    w.levels = (int *)(w.part + n * blocks_of(r, c));
+    w.ws = (char *)workspace + orth_part(d);
     NsLists l{};
     l.small_lds = evo::ns_small_bytes(d->rows, d->cols);
     l.tile = evo::ns_tile(n * triangle(tiles_of(r, 128)));
@@ -399,6 +408,7 @@ int evo_muon_step(const evo_muon_hparams *hp, const void *plan, const void *plan
     evo::NsWork w{};
     w.mats = (const NsMat *)(dev + h.off_mats);
     w.part = (double *)workspace;
+    w.levels = (int *)(w.part + h.blocks);
     w.ws = (char *)workspace + h.part_bytes;
     p.mu = (float)hp->momentum;
     p.om_mu = (float)(1.0 - hp->momentum);

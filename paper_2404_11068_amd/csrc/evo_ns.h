@@ -33,12 +33,14 @@ struct NsWork {
     int32_t n_mats, nti, ntj;      // stack: matrices, and tiles per matrix of this launch
     char *ws;                      // workspace behind the partial sums
     double *part;                  // partial sums of squares
+    int *levels;                   // per matrix: how far its norm lies below eps, see Scales
 };
 
 struct NsParams {
     // X and A are held times `scale`, P times a scale of its own, all powers of two.  P's coefficients with what
-    // brings A A and A to P's scale, and the factors of the products X X^T, P X and the last P X
-    float poly_a, poly_b, poly_c, from_gram, from_apply, from_last;
+    // brings A A and A to P's scale, and the factors of the products X X^T, P X and the last P X; growth: log2 of
+    // what a step multiplies a singular value with at most, 0 where it shrinks
+    float poly_a, poly_b, poly_c, from_gram, from_apply, from_last, growth;
     double scale, eps;
     int steps;
     // Muon (fp32): m = mu m + om_mu g, u = u_g g + u_m m, p = decay p - lr scale O, w = sd w + om_sd p

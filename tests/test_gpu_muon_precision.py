@@ -109,3 +109,32 @@ def test_one_singular_value_next_to_the_end():
                 got, ref = to_f64(op.orthogonalize(x, steps=k, coefs=coefs, eps=1.0)), mo.orthogonalize(to_f64(x), k, coefs, 1.0)
                 tol = 2 ** k * 44 * _e(m, n) * 8 + (2.0 ** -8 * np.abs(ref).max() if dtype == torch.bfloat16 else 0.0)
                 assert np.abs(got - ref).max() <= tol, (m, n, dtype, k)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("form", FORMS, ids=IDS)
+def test_norms_far_below_eps(form, dtype):
+    """Divided by eps instead of the norm: singular values of norm / eps and less, flat: 2 steps C e of the result."""
+    print("\n[case] below eps", form, dtype, flush=True)
+    N, m, n = form
+    x = _frames(np.random.default_rng(3), N, m, n)
+    x = torch.from_numpy(x / _norms(x)[:, None, None] * 1e-9).to(dtype).cuda()
+    for eps, steps in ((3e-9, 5), (1e-7, 5), (1e-4, 5), (1e-4, 8), (1e-1, 5), (1e1, 12), (1e16, 3)):
+        got, ref = _ends(op.orthogonalize(x, eps=eps, steps=steps)), mo.orthogonalize(to_f64(_ends(x)), steps, eps=eps)
+        bound = (2 * steps * 10 * _e(m, n) + (2.0 ** -8 if dtype == torch.bfloat16 else 0.0)) * _norms(ref)
+        assert (_norms(to_f64(got) - ref) <= bound).all(), (eps, steps, _norms(to_f64(got) - ref), bound)
+
+
+def test_muon_of_vanishing_gradients():
+    """Momenta of norm 1e-13 at an eps of 1e-7, and zeros among them; the parameters are the update alone."""
+    shapes = [(64, 64), (7, 33), (300, 260), (700, 90)] + [(200, 130)] * 80
+    rng = np.random.default_rng(4)
+    G = [_frames(rng, 1, *s)[0] * (0.0 if k % 9 == 5 else 20 * 1e-13 / math.sqrt(min(s))) for k, s in enumerate(shapes)]
+    g = [torch.from_numpy(v.astype(np.float32)).cuda() for v in G]
+    p = [torch.zeros_like(v) for v in g]
+    op.FusedMuonSWA(p, g, lr=1.0, momentum_decay=0.95, nesterov=False, adjust="none").step()
+    torch.cuda.synchronize()
+    for k, s in enumerate(shapes):
+        ref = -mo.orthogonalize(to_f64(g[k]) * 0.05)
+        bound = (10 * 10 + 4) * _e(*s) * np.linalg.norm(ref)
+        assert np.linalg.norm(to_f64(p[k]) - ref) <= bound, (k, s)
