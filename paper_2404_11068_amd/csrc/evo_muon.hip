@@ -6,8 +6,9 @@
 // the roundings of the iterate.  Every iterate is therefore a pair of fp16
 // (value = hi + lo, 22 bits), and each product is hi hi + hi lo + lo hi
 // on the fp16 matrix instructions with fp32 accumulation: the error of fp32
-// arithmetic (1e-6 .. 1e-5 of the result over five steps, low-rank inputs
-// too) at a third of the fp16 rate, which is five times the fp32 matrix rate.
+// arithmetic (1e-6 .. 1e-5 of the result over five steps, low-rank inputs too; rows far
+// below the others have an absolute error, see the range below) at a third of the fp16 rate, which
+// is five times the fp32 matrix rate.
 // bf16 matrices go through the same steps and are rounded once, at the end: with hi
 // alone in the last two steps their error would grow by a tenth (1.84e-3 instead of
 // 1.66e-3 of a result), in all steps to 2.4 times their rounding for low-rank inputs.
@@ -31,7 +32,6 @@ namespace {
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef _Float16 half4 __attribute__((ext_vector_type(4)));
-
 
 // The scales of X and A before step k, and what a step's products bring to the next ones.  A matrix of norm below
 // eps has a level, log2(eps / norm) rounded down: no singular value of its X is above 2^-level before the first step,

@@ -138,3 +138,32 @@ def test_muon_of_vanishing_gradients():
         ref = -mo.orthogonalize(to_f64(g[k]) * 0.05)
         bound = (10 * 10 + 4) * _e(*s) * np.linalg.norm(ref)
         assert np.linalg.norm(to_f64(p[k]) - ref) <= bound, (k, s)
+
+
+def _floor(X, steps):
+    """What is added to a row of the iterate by the ends of fp16's range: X and A are held to 2^-40 per entry at the
+    usual coefficients, P = a I + b A + c A A to 2^-39.  X's own error takes its entries' number in a row; P's and A's,
+    which comes into P times |b| + 2 |c| |A|, 11 at most, are independent from entry to entry and go through P X, |X|_F.
+    Each is passed on by slopes of 3.4445 at most.  X: the iterates."""
+    own, made = math.sqrt(X[0].shape[1]) * 2.0 ** -40, 2.0 ** -39 + 11 * 2.0 ** -40
+    return sum(3.4445 ** (steps - k) * own + 3.4445 ** (steps - k - 1) * made * np.linalg.norm(X[k]) for k in range(steps))
+
+
+@pytest.mark.parametrize("ratio", [1e4, 1e6, 1e8])
+@pytest.mark.parametrize("m,n", [(128, 224), (100, 700), (250, 300), (300, 250), (600, 800)])
+def test_rows_far_larger_than_the_others(m, n, ratio):
+    """Two rows of the short side are `ratio` times the others: the error of each row, and of the whole."""
+    print("\n[case] rows", m, n, ratio, flush=True)
+    rng = np.random.default_rng(5)
+    for N in (1, 76) if max(m, n) < 800 and min(m, n) <= 256 else (1,):
+        x = rng.standard_normal((N, min(m, n), max(m, n)))
+        x[:, rng.choice(min(m, n), 2, replace=False)] *= ratio
+        t = torch.from_numpy(x if m <= n else np.ascontiguousarray(x.swapaxes(1, 2))).float().cuda()
+        one = to_f64(t[-1]) if m <= n else to_f64(t[-1]).T
+        X = [one / np.linalg.norm(one)] + [mo.orthogonalize(one, k) for k in range(1, 13)]
+        for steps in (5, 8, 12):
+            got = to_f64(op.orthogonalize(t, steps=steps)[-1])
+            off, rows = (np.linalg.norm(v, axis=1) for v in ((got if m <= n else got.T) - X[steps], X[steps]))
+            e, floor = 20 * steps * _e(m, n), _floor(X, steps)
+            assert (off <= e * rows + floor).all(), (N, steps, (off / (e * rows + floor)).max())
+            assert np.linalg.norm(off) <= e * np.linalg.norm(rows) + floor * math.sqrt(min(m, n)), (N, steps)
