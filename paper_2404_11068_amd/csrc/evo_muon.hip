@@ -48,6 +48,7 @@ __device__ __forceinline__ int level_of(const NsParams &p, double norm) {
 }
 // what the entries of a matrix are multiplied with to be those of X before the first step
 __device__ __forceinline__ double first_scale(const NsParams &p, double norm, int level) {
+    if (norm == 0.0) return 0.0;  // (the smallest eps would make it infinite)
     return ldexp(p.scale, more_at(p, level, 0)) / (norm < p.eps ? p.eps : norm);
 }
 struct Scales {

@@ -167,3 +167,14 @@ def test_rows_far_larger_than_the_others(m, n, ratio):
             e, floor = 20 * steps * _e(m, n), _floor(X, steps)
             assert (off <= e * rows + floor).all(), (N, steps, (off / (e * rows + floor)).max())
             assert np.linalg.norm(off) <= e * np.linalg.norm(rows) + floor * math.sqrt(min(m, n)), (N, steps)
+
+
+def test_zeros_with_the_smallest_eps():
+    for m, n in ((16, 24), (200, 300)):
+        x = torch.zeros(2, m, n, device="cuda")
+        x[1, 3, 4] = 1e-44
+        for eps in (1e-300, 1e-306, 5e-324):
+            got = op.orthogonalize(x, eps=eps)
+            assert not got[0].any() and got[1].isfinite().all(), eps
+            want = mo.singular_map(1.0)
+            assert abs(float(got[1, 3, 4]) - want) <= 24000 * _e(m, n), eps
