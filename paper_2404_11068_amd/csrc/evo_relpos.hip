@@ -132,7 +132,8 @@ struct RpFind {
 #pragma unroll
             for (int x = 0; x < N; ++x) {
                 const int t = d[x] < lo ? lo : d[x] > hi ? hi : d[x];
-                n[x] = MODE == kRpUnit ? t - lo : MODE == kRpTable ? lut[t - lo] : lut[(unsigned)(t - lo) >> shift];
+                const unsigned at = (unsigned)t - (unsigned)lo;  // (the edges of kRpSteps may span more than an int)
+                n[x] = MODE == kRpUnit ? (int)at : MODE == kRpTable ? lut[at] : lut[at >> shift];
             }
             if constexpr (MODE == kRpSteps)
                 for (int k = 0; k < more; ++k) {
