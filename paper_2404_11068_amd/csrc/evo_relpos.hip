@@ -627,10 +627,9 @@ hipError_t launch_bwd_as(const RpArgs &a, const RpBwdPlan &p, float *part, hipSt
 
 template <bool SEG, bool MANY>
 hipError_t launch_bwd(const RpArgs &a, const RpBwdPlan &p, float *part, hipStream_t s) {
-    // rows of one to three entries, and several passes: rare, in one form each
+    // rows of one to three entries, and several passes (of 257 buckets and more: 16 columns): rare, in one form each
     if (p.piece == 1) return launch_bwd_as<1, 16, SEG, MANY, true, 4>(a, p, part, s);
-    if (p.passes > 1) return p.columns == 32 ? launch_bwd_as<4, 32, SEG, MANY, true, 8>(a, p, part, s)
-                                             : launch_bwd_as<4, 16, SEG, MANY, true, 8>(a, p, part, s);
+    if (p.passes > 1) return launch_bwd_as<4, 16, SEG, MANY, true, 8>(a, p, part, s);
     if (p.columns == 16) return launch_bwd_as<4, 16, SEG, MANY, false, 8>(a, p, part, s);
     if (p.columns == 32) return launch_bwd_as<4, 32, SEG, MANY, false, 8>(a, p, part, s);
     // four pieces ahead in short runs, so that few of a round are empty, and with
