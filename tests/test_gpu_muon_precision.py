@@ -178,3 +178,51 @@ def test_zeros_with_the_smallest_eps():
             assert not got[0].any() and got[1].isfinite().all(), eps
             want = mo.singular_map(1.0)
             assert abs(float(got[1, 3, 4]) - want) <= 24000 * _e(m, n), eps
+
+
+def _flat_tolerance(m, n, steps=5):
+    return 20 * steps * _e(m, n)
+
+
+@pytest.mark.parametrize("form", FORMS + [(76, 40, 600), (72, 256, 700), (1, 2100, 1990), (13, 500, 530)], ids=IDS)
+def test_flat_spectra_in_every_form(form):
+    """fp32's precision, not only that of any spectrum: changes add up over the steps."""
+    print("\n[case] flat", form, flush=True)
+    N, m, n = form
+    x = torch.from_numpy(_frames(np.random.default_rng(6), N, m, n) * 1e-3).float().cuda()
+    got, ref = _ends(op.orthogonalize(x)), mo.orthogonalize(to_f64(_ends(x)))
+    off = _norms(to_f64(got) - ref)
+    assert (off <= _flat_tolerance(m, n) * _norms(ref)).all(), off / _norms(ref)
+
+
+@pytest.mark.parametrize("shapes", [
+    [(64, 64), (90, 300), (7, 33), (1, 300), (300, 260), (650, 200)],                       # LDS and tiles of 64 x 64
+    [(200, 130)] * 60 + [(70, 520)] * 30 + [(600, 90)] * 9 + [(256, 200)] * 20,             # a workgroup each
+    [(500, 530)] * 7 + [(530, 500)] * 6 + [(777, 300)]], ids=["lds", "workgroups", "tiles128"])
+def test_muon_of_flat_momenta(shapes):
+    """The parameters' bound: the update's, the fp32 rounding of momentum and update (2^-22 of it), and two of the
+    parameter, 2^-24 each.  The gradients are as they were afterwards."""
+    print("\n[case] muon, flat", len(shapes), flush=True)
+    rng = np.random.default_rng(7)
+    G = [_frames(rng, 1, *s)[0].astype(np.float32) * 1e-2 for s in shapes]
+    P = [(rng.standard_normal(s) * 0.02).astype(np.float32) for s in shapes]
+    p, g = ([torch.from_numpy(v).cuda() for v in L] for L in (P, G))
+    opt = op.FusedMuonSWA(p, g, lr=0.3, momentum_decay=0.9, weight_decay=0.1, swa_decay=0.75, adjust="rms")
+    m, w = ([np.zeros(s) for s in shapes], P)
+    w = [v.astype(np.float64) for v in P]
+    q = [v.astype(np.float64) for v in P]
+    for it in range(2):
+        opt.step()
+        torch.cuda.synchronize()
+        for k, (r, c) in enumerate(shapes):
+            f = 0.2 * math.sqrt(max(r, c))
+            before = q[k]
+            q[k], m[k], w[k] = mo.muon_step(before, G[k], m[k], w[k], lr=0.3, momentum_decay=0.9, nesterov=True,
+                                            weight_decay=0.1, swa_decay=0.75, update_scale=f)
+            update = np.linalg.norm(q[k] - 0.97 * before)
+            bound = (it + 1) * (update * (_flat_tolerance(r, c) + 2.0 ** -21) + 2.0 ** -22 * np.linalg.norm(before))
+            assert np.linalg.norm(to_f64(opt.momentum[k]) - m[k]) <= 2.0 ** -22 * (it + 1) * np.linalg.norm(m[k]), (it, k)
+            assert np.linalg.norm(to_f64(p[k]) - q[k]) <= bound, (it, k, r, c)
+            assert np.linalg.norm(to_f64(opt.swa[k]) - w[k]) <= bound + 2.0 ** -22 * np.linalg.norm(w[k]), (it, k, r, c)
+    for a, b in zip(g, G):
+        assert torch.equal(a.cpu(), torch.from_numpy(b))
