@@ -42,9 +42,9 @@ __device__ __forceinline__ int more_at(const NsParams &p, int level, int k) {
     return e > 0 ? e : 0;
 }
 __device__ __forceinline__ int level_of(const NsParams &p, double norm) {
-    if (!(norm < p.eps) || norm == 0.0) return 0;
-    const double q = p.eps / norm;
-    return q < 0x1p96 ? ilogb(q) : kMostLevel;
+    // (a norm of infinity or NaN gets an end of int from ilogb, and then one of the range's ends)
+    const int l = ilogb(p.eps / norm);
+    return l < 0 ? 0 : l < kMostLevel ? l : kMostLevel;
 }
 // what the entries of a matrix are multiplied with to be those of X before the first step
 __device__ __forceinline__ double first_scale(const NsParams &p, double norm, int level) {

@@ -226,3 +226,19 @@ def test_muon_of_flat_momenta(shapes):
             assert np.linalg.norm(to_f64(opt.swa[k]) - w[k]) <= bound + 2.0 ** -22 * np.linalg.norm(w[k]), (it, k, r, c)
     for a, b in zip(g, G):
         assert torch.equal(a.cpu(), torch.from_numpy(b))
+
+
+@pytest.mark.parametrize("form", [f for f in FORMS if f[0] > 1] + [(3, 64, 64), (9, 500, 530)], ids=IDS)
+def test_nan_and_infinity_in_every_form(form):
+    """A NaN takes the whole of its matrix, and neither takes another one."""
+    print("\n[case] nan", form, flush=True)
+    N, m, n = form
+    x = torch.randn(N, m, n, device="cuda")
+    for eps in (1e-7, 1e9):
+        want, y = op.orthogonalize(x, eps=eps), x.clone()
+        y[0, m // 2, n - 1] = float("nan")
+        y[N - 1, m - 1, 0] = float("-inf")
+        got = op.orthogonalize(y, eps=eps)
+        assert got[0].isnan().all() and got[N - 1].isnan().any(), eps
+        assert torch.equal(got[1:N - 1], want[1:N - 1]), eps
+        assert N < 3 or got[1:N - 1].isfinite().all()
