@@ -199,7 +199,7 @@ __device__ __forceinline__ void mma(f32x16 &acc, const Frag &a, const Frag &b) {
 }
 
 // ---- norm, scaling and update: a thread owns 4 x 4 entries of a 64 x 64 tile.  Streams, bound by HBM:
-// 73 M entries of a model in 182, 196 and 298 us, 12, 12 and 20 bytes each (4.5 to 4.9 TB/s)
+// 73 M entries of a model in 185, 198 and 299 us, 12, 12 and 20 bytes each (4.5 to 4.9 TB/s)
 
 // four consecutive entries of a memory row, zeros past its end
 __device__ __forceinline__ void load4(float (&v)[4], const float *p, int left) {
@@ -491,8 +491,8 @@ __device__ __forceinline__ void store_last(const View &v, const NsParams &p, flo
 // global_load_lds 16 bytes a lane, S - 1 stages ahead: the copies are counted
 // by hand (vmcnt), one barrier per stage.  The matrix instructions bound large
 // products, the chain of stages and the launch small
-// ones: 8 matrices of 2048 x 2048 in pairs, Gram 217 us (1.0 PFLOP/s of fp16 products), polynomial 224,
-// P X 352 (1.2); one such matrix 37, 40 and 46 us; 52 of 128 x 512 6.8, 5.0 and 9.4.
+// ones: 8 matrices of 2048 x 2048 in pairs, Gram 216 us (1.0 PFLOP/s of fp16 products), polynomial 222,
+// P X 355 (1.2); one such matrix 37, 40 and 47 us; 52 of 128 x 512 6.9, 5.1 and 9.7.
 
 enum { kGram, kPoly, kApply, kLast };
 struct Yes { static constexpr bool value = true; };
@@ -758,7 +758,7 @@ __device__ __forceinline__ void tri_frag(Frag &f, char *base, int r, int k, int 
 // 4000 cycles a step for the Gram matrix, 6200 for the polynomial and 6200 for P X,
 // against 1900, 1900 and 3100 of matrix instructions on the busiest SIMD; so the next operands
 // are read before the matrix instructions of the last.  128 x 128: 37 us; 256
-// matrices of 128 x 224 68 us, of 96 x 352 64.
+// matrices of 128 x 224 70 us, of 96 x 352 65.
 
 constexpr int kSmallUnits = 40;
 constexpr int kSmallLds = 39 * kUnit;
@@ -963,10 +963,10 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsWork w, Ns
 // unit read by columns.  X lies in the workspace, transposed, so that the
 // fragments of P X come straight from memory, 1 KB a load: each wave takes unit
 // columns of its own and writes the result in their place, without a barrier.  Memory
-// then sees X read twice and written once per step: 240 matrices of 256 x 256 take 244 us, of
-// 256 x 1024 793 (with A and P in the workspace, too, the former moved 2.7 GB at 6.4 TB/s and took 430).
-// The matrix instructions would take 45% of that; P X, half the time, reads as much from LDS as it
-// multiplies, with two waves per SIMD to cover each other's reads.
+// then sees X read twice and written once per step: 240 matrices of 256 x 256 take 268 us, of
+// 256 x 1024 800 (with A and P in the workspace, too, the former moved 2.7 GB at 6.4 TB/s and took 430).
+// Over a model's matrices the matrix instructions take 41% of the time and the LDS 18%: two waves per SIMD, which
+// wait for memory, LDS and barriers 46% of theirs, cover no more of each other's chains.
 // A call with too few matrices for the CUs is done sooner by the tiles above.
 
 constexpr int kWgWaves = 8;
@@ -1285,8 +1285,8 @@ hipError_t launch_product(NsWork w, const NsTile *tiles, int64_t grid, const NsP
                            S * 2 * (T / 32) * kUnit, s, w, p, k0);
     };
     // S stages of copies.  Tiles of 128 x 128 take 32 KB a stage: with four of them a CU has one workgroup, with
-    // two stages it has two, which is better once there are enough (96 matrices of 256 x 256 in 269 us
-    // instead of 318, P X of 8 of 2048 x 2048 in 352 instead of 366) and worse before (one: 57 instead of 44)
+    // two stages it has two, which is better once there are enough (96 matrices of 256 x 256 in 287 us
+    // instead of 366; 8 of 2048 x 2048 as fast either way) and worse before (one of 2048 x 2048: 798 instead of 630)
     if (T == 128 && grid > 256) launch(Int<T == 128 ? 2 : 4>{});
     else launch(Int<4>{});
     return hipGetLastError();
@@ -1373,14 +1373,16 @@ int64_t ns_matrix_wg_bytes(int64_t rows, int64_t cols) {
     return (r + 31) / 32 * ((c + 31) / 32) * kUnit;
 }
 
-// A workgroup takes as long for its matrix as tiles on all CUs for about 70 of them (fp32, by tiles and by
-// workgroups: 64 of 256 x 256 210 and 219 us, 96 269 and 221; 64 of 256 x 1024 412 and 586, 128 795 and 666)
+// A workgroup takes as long for its matrix as tiles on all CUs for 55 (256 x 256) to 92 (256 x 1024) of them.  The
+// rule has one number between: wide matrices in calls of 72 to 90 would be up to a quarter sooner by tiles.  (fp32, by tiles and by workgroups: 48 of 256 x 256 176 and 200 us, 64 238 and 204, 96 287 and 214; 72 of
+// 256 x 512 312 and 336, 96 404 and 347; 72 of 256 x 1024 481 and 593, 96 645 and 612, 128 847 and 651; 72 of
+// 128 x 512 143 and 123, of 128 x 1024 211 and 218)
 bool ns_by_matrix(double total, double largest) { return total >= 72.0 * largest; }
 
 // 128 x 128 tiles read each staged unit twice as often, but the Gram matrix's triangle has few of
 // them: below about 120, tiles of a quarter the size do the work sooner (fp32, small and large tiles: 1 matrix
-// of 1024 x 4096, 36 large ones, 405 and 527 us; 1 of 1792 x 1792, 105, 529 and 517; 12 of 512 x 512, 120, 276
-// and 250; 1 of 2048 x 2048, 136, 778 and 648; 16 of 512 x 2048, 160, 688 and 574)
+// of 1024 x 4096, 36 large ones, 404 and 527 us; 1 of 1792 x 1792, 105, 504 and 505; 12 of 512 x 512, 120, 262
+// and 237; 1 of 2048 x 2048, 136, 765 and 631; 16 of 512 x 2048, 160, 682 and 576)
 int ns_tile(int64_t gram128) { return gram128 >= 120 ? 128 : 64; }
 
 hipError_t launch_ns(const NsWork &w, const NsLists &l, const NsParams &p, bool muon, bool bf16, hipStream_t s) {

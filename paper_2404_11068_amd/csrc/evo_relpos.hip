@@ -344,14 +344,14 @@ hipError_t launch_fwd_t(const RpArgs &a, hipStream_t s) {
 // of every row are summed in a fixed order, and a second kernel adds the
 // waves' sums in order, in fp64.
 //
-// 16 planes of 2048 x 2048: 65 buckets 56 us (4.8 TB/s), 129 72 us, 257 96 us, 513 in two passes 259 us:
-// with more than 66 buckets the turns' chains of LDS reads, additions and writes bound it, not HBM.
-// (The sums within the piece, taken in each turn, were 79, 115 and 302 us; two pieces a round trip 76, 97, 264.)
+// 16 planes of 2048 x 2048, differences clipped: 65 buckets 57 us (4.7 TB/s), 129 65 us, 257 88 us (by a table
+// 96), 513 in two passes 162 us.  With more than 67 buckets the turns' chains of LDS reads, additions and writes bound
+// it, not HBM: at 257 the LDS is busy 38% and the vector units 43% of the time, and waves wait 36% of theirs.
 //
-// C is 64, one column per lane, for up to 66 buckets.  With more of them that
-// would leave a SIMD fewer than two waves, so 32 or 16 columns serve the
-// wave's halves or quarters in turn (257 buckets: 16 columns and two workgroups per CU 114 us, 32 and one
-// 124; 127 buckets: 32 and two 79, 64 and one 86, all with the sums in the turns).
+// C is 64, one column per lane, for up to 67 buckets.  With more of them that
+// would leave a SIMD fewer than two waves, so 32 (up to 133) or 16 columns serve the
+// wave's halves or quarters in turn (257 buckets: 16 columns and two workgroups per CU 88 us a call, 32 and one
+// 109; 127 buckets: 32 and two 67, 64 and one 80).
 //
 // A wave takes one head and a run of 4-entry pieces of its rows, 64 at a time.
 // The last piece of a row whose length is no multiple of four starts earlier,

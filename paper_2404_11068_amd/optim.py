@@ -235,6 +235,9 @@ class FusedMuonSWA:
     Stacked projections are given as their matrices, e.g. the q, k, v and
     gate rows of one weight as `list(w.view(4, -1, w.shape[1]))`.
 
+    Construction checks every tensor and builds the plan on the host, once: 9 ms
+    for the 2263 matrices of an AlphaFold-sized model, four of its steps.
+
     adjust: factor of the update of an m x n matrix: "spectral" gives
     sqrt(max(1, m / n)), "rms" 0.2 sqrt(max(m, n)) (entries about as large as
     Adam's), "none" 1."""
