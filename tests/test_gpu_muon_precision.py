@@ -242,3 +242,23 @@ def test_nan_and_infinity_in_every_form(form):
         assert got[0].isnan().all() and got[N - 1].isnan().any(), eps
         assert torch.equal(got[1:N - 1], want[1:N - 1]), eps
         assert N < 3 or got[1:N - 1].isfinite().all()
+
+
+def test_no_accepted_coefficients_leave_the_range():
+    """Random coefficients and steps, refused or finite; inputs whose first singular values are one, and flat ones."""
+    rng = np.random.default_rng(8)
+    shapes = [(1, 40, 60), (73, 130, 150), (1, 150, 330)]
+    inputs = []
+    for N, m, n in shapes:
+        one = np.zeros((N, m, n))
+        one[:, m // 3, n // 2] = 1.0
+        inputs += [torch.from_numpy(v).float().cuda() for v in (one, _frames(rng, N, m, n), rng.standard_normal((N, m, n)))]
+    done = 0
+    for _ in range(300):
+        steps, coefs = int(rng.integers(1, 13)), (rng.uniform(-4, 5), rng.choice([0.0, rng.uniform(-8, 8)]), rng.choice([0.0, rng.uniform(-4, 4)]))
+        if not op.orthogonalize_workspace_size((1, 40, 60), torch.float32, steps=steps, coefs=coefs):
+            continue
+        done += 1
+        for eps in (1e-7, 1e3):
+            assert all(op.orthogonalize(x, steps=steps, coefs=coefs, eps=eps).isfinite().all() for x in inputs), (steps, coefs, eps)
+    assert done > 40
