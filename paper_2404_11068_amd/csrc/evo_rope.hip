@@ -1,0 +1,351 @@
+// evo_rope.hip -- rotary positions, and the norm of every head with the
+// rotation in the same pass: forward and backward (include/evo_rope.h).
+//
+// Both directions read each element once and write it once, with a handful of
+// operations between: HBM bandwidth bounds them, and for few tokens the launch.
+// The angles are the expensive part per value (a 64-bit product, a polynomial
+// for the sine and one for the cosine), so a workgroup forms those of its
+// tokens once, in LDS, for all heads: one pair in 2 d / rot * heads elements.
+//
+// A head is a group of GS lanes (the power of two that holds d / VEC chunks of
+// 16 bytes); groups walk over the (token, head) units of a workgroup's tokens.
+// Sums over a head are butterflies inside the group.
+#include "evo_rope_kernels.h"
+
+#include "evo_frag.h"
+
+namespace evo {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMaxTok = 16;  // tokens whose angles a workgroup holds
+
+// How the partner of a channel is found: its own lane (interleaved pairs), the
+// lane rot / 2 / VEC chunks away (half layout with whole chunks), or through
+// LDS element by element (half layout, rot / 2 not a multiple of VEC).
+enum Pairing { kInter, kHalf, kSplit };
+
+struct KArgs {
+    RopeArgs a;
+    uint32_t blocks[2];  // workgroups of each set
+    float *part;         // backward: partial sums of dw, [blocks of set 0 + 1][d]
+    int tb, gs_log;
+};
+
+template <typename E> struct Chunk;  // 16 bytes of a head
+template <> struct Chunk<float> {
+    static constexpr int VEC = 4;
+    __device__ __forceinline__ static void get(u32x4 w, float *v) {
+        const f32x4 x = __builtin_bit_cast(f32x4, w);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = x[e];
+    }
+    __device__ __forceinline__ static u32x4 put(const float *v) {
+        return __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]});
+    }
+};
+template <> struct Chunk<uint16_t> {
+    static constexpr int VEC = 8;
+    __device__ __forceinline__ static void get(u32x4 w, float *v) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[2 * e] = __builtin_bit_cast(f32x4, w << 16)[e];
+            v[2 * e + 1] = __builtin_bit_cast(f32x4, w & 0xffff0000u)[e];
+        }
+    }
+    __device__ __forceinline__ static u32x4 put(const float *v) {
+        u32x4 w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = (uint32_t)f2bf(v[2 * e]) | ((uint32_t)f2bf(v[2 * e + 1]) << 16);
+        return w;
+    }
+};
+
+// (cos, sin) of phase / 2^64 turns.  The upper 32 bits leave 2^-32 turns, far
+// below an fp32 step of the result; the nearest quarter turn is taken off
+// exactly, and the rest, at most pi / 4, goes into the Taylor series, whose
+// first terms left out are below 3e-9.
+__device__ __forceinline__ float2 turn(uint64_t phase) {
+    const uint32_t p = (uint32_t)(phase >> 32);
+    const uint32_t quarter = (p + 0x20000000u) >> 30;
+    const float x = (float)(int32_t)(p - (quarter << 30)) * 1.4629180792671596e-9f;  // 2 pi / 2^32
+    const float z = x * x;
+    float s = fmaf(z, 2.7557319e-6f, -1.9841270e-4f);
+    s = fmaf(z, s, 8.3333333e-3f);
+    s = fmaf(z, s, -1.6666667e-1f);
+    s = fmaf(x * z, s, x);
+    float c = fmaf(z, -2.7557319e-7f, 2.4801587e-5f);
+    c = fmaf(z, c, -1.3888889e-3f);
+    c = fmaf(z, c, 4.1666667e-2f);
+    c = fmaf(z, c, -0.5f);
+    c = fmaf(z, c, 1.0f);
+    const bool odd = quarter & 1;
+    const float cc = odd ? s : c, ss = odd ? c : s;
+    return float2{quarter == 1 || quarter == 2 ? -cc : cc, quarter >= 2 ? -ss : ss};
+}
+
+// Workgroup b of the set takes token blocks b, b + blocks, ...
+template <typename E, Pairing P, bool NORM, bool BWD>
+__device__ __forceinline__ void rope_body(const KArgs &k, float2 *angles, float *line) {
+    constexpr int VEC = Chunk<E>::VEC;
+    const RopeArgs &a = k.a;
+    const int which = blockIdx.x >= k.blocks[0];
+    const RopeSet &s = a.set[which];
+    const uint32_t b0 = blockIdx.x - (which ? k.blocks[0] : 0), nb = k.blocks[which];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int gs = 1 << k.gs_log, c = lane & (gs - 1), nc = a.d / VEC;
+    const int per_wave = 64 >> k.gs_log;
+    const int half = a.rot >> 1, H = s.heads;
+    const bool live = c < nc;
+    const int base = c * VEC;  // the lane's first channel
+    const float inv_d = 1.0f / (float)a.d;
+
+    // what stays with the lane: weights, the partner's chunk
+    float w[VEC], wp[VEC], acc[VEC];
+    int partner = 0;
+    bool low = true;  // the lane holds first channels of its pairs
+    if (P == kHalf) {
+        const int hc = half / VEC;
+        low = c < hc;
+        partner = low ? lane + hc : lane - hc;
+        if (c >= 2 * hc) partner = lane;
+    }
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+        acc[e] = 0.0f;
+        w[e] = NORM && s.w && live ? s.w[base + e] : 1.0f;
+        wp[e] = 1.0f;
+        if (NORM && !BWD && P == kHalf && s.w && live && base < 2 * half) wp[e] = s.w[low ? base + half + e : base - half + e];
+    }
+
+    const int64_t nblocks = (s.tokens + k.tb - 1) / k.tb;
+    for (int64_t blk = b0; blk < nblocks; blk += nb) {
+        const int64_t t0 = blk * k.tb;
+        const int nt = (int)min((int64_t)k.tb, s.tokens - t0);
+        // one 64-bit division a block; within it rows and columns are 32 bits (len <= 2^30)
+        const int64_t row0 = t0 / s.len;
+        const uint32_t col0 = (uint32_t)(t0 - row0 * s.len), len = (uint32_t)s.len;
+        for (int i = tid; i < nt * half; i += kThreads) {
+            const int t = i / half, j = i - t * half;
+            const uint32_t over = (col0 + t) / len;
+            const int64_t pos = s.pos[(row0 + over) * s.pos_stride + (col0 + t - over * len)];
+            const float2 cs = turn((uint64_t)pos * a.steps[j]);
+            angles[i] = float2{cs.x * a.amplitude, (BWD ? -cs.y : cs.y) * a.amplitude};
+        }
+        __syncthreads();
+        const int units = nt * H;
+        // every lane of a wave makes the same number of turns: the shuffles need them all
+        for (int u0 = wave * per_wave; u0 < units; u0 += 4 * per_wave) {
+            const int u = u0 + (lane >> k.gs_log);
+            const bool on = live && u < units;
+            const int t = on ? u / H : 0, h = on ? u - t * H : 0;
+            const uint32_t over = (col0 + t) / len;
+            const int64_t row = row0 + over, col = col0 + t - over * len;
+            const int64_t at = (int64_t)h * a.d + base;
+            u32x4 raw = {0, 0, 0, 0}, xraw = {0, 0, 0, 0};
+            if (on) {
+                raw = *reinterpret_cast<const u32x4 *>((const E *)s.in + row * s.in_row + col * s.in_tok + at);
+                if (NORM && BWD) xraw = *reinterpret_cast<const u32x4 *>((const E *)s.x + row * s.x_row + col * s.x_tok + at);
+            }
+            float v[VEC], o[VEC];
+            Chunk<E>::get(raw, v);
+            float rstd = 1.0f;
+            if (NORM) {
+                float xv[VEC], sum = 0.0f;
+                Chunk<E>::get(BWD ? xraw : raw, xv);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) sum = fmaf(xv[e], xv[e], sum);
+                for (int m = 1; m < gs; m <<= 1) sum += __shfl_xor(sum, m, 64);
+                rstd = 1.0f / sqrtf(fmaf(sum, inv_d, a.eps));
+            }
+            if (NORM && !BWD) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) v[e] *= rstd;
+            }
+            const float2 *row_angles = angles + t * half;
+            if (P == kInter) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e)
+                    if (NORM && !BWD) v[e] *= w[e];
+#pragma unroll
+                for (int e = 0; e < VEC; e += 2) {
+                    const int j = (base + e) >> 1;
+                    o[e] = v[e];
+                    o[e + 1] = v[e + 1];
+                    if (j < half) {
+                        const float2 cs = row_angles[j];
+                        o[e] = v[e] * cs.x - v[e + 1] * cs.y;
+                        o[e + 1] = v[e] * cs.y + v[e + 1] * cs.x;
+                    }
+                }
+            } else if (P == kHalf) {
+                u32x4 praw;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) praw[i] = __shfl(raw[i], partner, 64);
+                float pv[VEC];
+                Chunk<E>::get(praw, pv);
+                const int j0 = low ? base : base - half;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    if (NORM && !BWD) v[e] *= w[e];
+                    o[e] = v[e];
+                    if (j0 < half) {
+                        const float2 cs = row_angles[j0 + e];
+                        const float q = NORM && !BWD ? pv[e] * rstd * wp[e] : pv[e];
+                        o[e] = low ? v[e] * cs.x - q * cs.y : v[e] * cs.x + q * cs.y;
+                    }
+                }
+            } else {
+                float *mine = line + wave * (64 * VEC) + (lane >> k.gs_log << k.gs_log) * VEC;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    if (NORM && !BWD) v[e] *= w[e];
+                    mine[base + e] = v[e];
+                }
+                __builtin_amdgcn_wave_barrier();
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const int i = base + e;
+                    o[e] = v[e];
+                    if (i < 2 * half) {
+                        const bool lo = i < half;
+                        const float2 cs = row_angles[lo ? i : i - half];
+                        const float q = mine[lo ? i + half : i - half];
+                        o[e] = lo ? v[e] * cs.x - q * cs.y : v[e] * cs.x + q * cs.y;
+                    }
+                }
+                __builtin_amdgcn_wave_barrier();
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            }
+            if (NORM && BWD) {
+                float xv[VEC], dot = 0.0f;
+                Chunk<E>::get(xraw, xv);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    xv[e] *= rstd;
+                    acc[e] = fmaf(o[e], xv[e], acc[e]);  // lanes that are off hold zeros
+                    o[e] *= w[e];
+                    dot = fmaf(o[e], xv[e], dot);
+                }
+                for (int m = 1; m < gs; m <<= 1) dot += __shfl_xor(dot, m, 64);
+                dot *= inv_d;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) o[e] = rstd * fmaf(-xv[e], dot, o[e]);
+            }
+            if (on)
+                *reinterpret_cast<u32x4 *>((E *)s.out + row * s.out_row + col * s.out_tok + at) = Chunk<E>::put(o);
+        }
+        __syncthreads();
+    }
+    if (NORM && BWD) {
+        if (!s.dw) return;
+        // groups of a wave, then waves, in a fixed order
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            for (int m = gs; m < 64; m <<= 1) acc[e] += __shfl_xor(acc[e], m, 64);
+        if (lane < nc) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) line[wave * 256 + base + e] = acc[e];
+        }
+        __syncthreads();
+        if (tid < a.d)
+            k.part[(int64_t)blockIdx.x * a.d + tid] = (line[tid] + line[256 + tid]) + (line[512 + tid] + line[768 + tid]);
+    }
+}
+
+template <typename E, Pairing P, bool NORM, bool BWD>
+__global__ __launch_bounds__(kThreads) void rope_kernel(KArgs k) {
+    __shared__ float2 angles[kMaxTok * 128];
+    __shared__ float line[4 * 64 * Chunk<E>::VEC > 1024 ? 4 * 64 * Chunk<E>::VEC : 1024];
+    rope_body<E, P, NORM, BWD>(k, angles, line);
+}
+
+// dw = sum of the workgroups' parts in fp64: 16 columns a workgroup, 16 threads each
+__global__ __launch_bounds__(256) void rope_dw_kernel(const float *part0, int n0, float *dw0, const float *part1, int n1,
+                                                      float *dw1, int d) {
+    __shared__ double sums[256];
+    const float *part = blockIdx.y ? part1 : part0;
+    float *dw = blockIdx.y ? dw1 : dw0;
+    const int n = blockIdx.y ? n1 : n0;
+    if (!dw) return;
+    const int col = blockIdx.x * 16 + (threadIdx.x & 15), r0 = threadIdx.x >> 4;
+    double sum = 0.0;
+    if (col < d)
+        for (int r = r0; r < n; r += 16) sum += (double)part[(int64_t)r * d + col];
+    sums[threadIdx.x] = sum;
+    __syncthreads();
+    if (threadIdx.x < 16 && col < d) {
+        for (int i = 1; i < 16; ++i) sum += sums[threadIdx.x + 16 * i];
+        dw[col] = (float)sum;
+    }
+}
+
+// Tokens per workgroup and workgroups per set
+void plan(const RopeArgs &a, bool bwd, KArgs *k) {
+    const int64_t all = a.set[0].tokens + a.set[1].tokens;
+    int tb = 1;
+    while (tb < kMaxTok && all / (2 * tb) >= 1024) tb *= 2;
+    k->tb = tb;
+    const int chunks = a.d / (a.bf16 ? 8 : 4);
+    k->gs_log = 0;
+    while ((1 << k->gs_log) < chunks) ++k->gs_log;
+    for (int i = 0; i < 2; ++i) {
+        const int64_t blocks = a.set[i].heads > 0 ? (a.set[i].tokens + tb - 1) / tb : 0;
+        const int64_t most = bwd && a.norm ? 1024 : (int64_t)1 << 20;
+        k->blocks[i] = (uint32_t)(blocks < most ? blocks : most);
+    }
+}
+
+template <typename E, bool NORM, bool BWD>
+void launch(const KArgs &k, hipStream_t s) {
+    const dim3 grid(k.blocks[0] + k.blocks[1]);
+    const int half = k.a.rot / 2;
+    if (k.a.interleaved)
+        rope_kernel<E, kInter, NORM, BWD><<<grid, kThreads, 0, s>>>(k);
+    else if (half % Chunk<E>::VEC == 0)
+        rope_kernel<E, kHalf, NORM, BWD><<<grid, kThreads, 0, s>>>(k);
+    else
+        rope_kernel<E, kSplit, NORM, BWD><<<grid, kThreads, 0, s>>>(k);
+}
+
+template <bool BWD>
+hipError_t launch_all(const KArgs &k, hipStream_t s) {
+    if (k.blocks[0] + k.blocks[1] == 0) return hipSuccess;
+    if (k.a.bf16)
+        k.a.norm ? launch<uint16_t, true, BWD>(k, s) : launch<uint16_t, false, BWD>(k, s);
+    else
+        k.a.norm ? launch<float, true, BWD>(k, s) : launch<float, false, BWD>(k, s);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t rope_bwd_workspace(const RopeArgs &a) {
+    if (!a.norm) return 0;
+    KArgs k{};
+    plan(a, true, &k);
+    return (size_t)(k.blocks[0] + k.blocks[1]) * a.d * sizeof(float);
+}
+
+hipError_t launch_rope_fwd(const RopeArgs &a, hipStream_t s) {
+    KArgs k{};
+    k.a = a;
+    plan(a, false, &k);
+    return launch_all<false>(k, s);
+}
+
+hipError_t launch_rope_bwd(const RopeArgs &a, void *ws, hipStream_t s) {
+    KArgs k{};
+    k.a = a;
+    plan(a, true, &k);
+    k.part = (float *)ws;
+    hipError_t e = launch_all<true>(k, s);
+    if (e != hipSuccess || !(a.set[0].dw || a.set[1].dw)) return e;
+    rope_dw_kernel<<<dim3((a.d + 15) / 16, 2), 256, 0, s>>>(k.part, (int)k.blocks[0], a.set[0].dw,
+                                                         k.part + (int64_t)k.blocks[0] * a.d, (int)k.blocks[1],
+                                                         a.set[1].dw, a.d);
+    return hipGetLastError();
+}
+
+}  // namespace evo
