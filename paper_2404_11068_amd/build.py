@@ -19,9 +19,8 @@ OBJDIR = os.path.join(PKG, "_build")
 SOURCES = ["evo_fwd.hip", "evo_bwd.hip", "evo_bwd_qbias.hip", "evo_bwd_fused.hip", "evo_ln.hip", "evo_proj.hip", "evo_pair_bias.hip", "evo_optim.hip",
            "evo_proj_bwd.hip", "evo_pair_bias_bwd.hip", "evo_relpos.hip", "evo_muon.hip",
            "evo_probe.hip", "evo_api.cpp", "evo_ln_api.cpp", "evo_proj_api.cpp", "evo_optim_api.cpp",
-           "evo_relpos_api.cpp", "evo_muon_api.cpp", "evo_rope.hip", "evo_rope_api.cpp", "evo_graph.cpp"]
-# sources whose inputs may hold NaN where a mask covers it
-NAN_SOURCES = {"evo_rope.hip"}
+           "evo_relpos_api.cpp", "evo_muon_api.cpp", "evo_rope.hip", "evo_rope_api.cpp",
+           "evo_cross_fwd.hip", "evo_cross_bwd.hip", "evo_cross_api.cpp", "evo_graph.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
@@ -40,8 +39,7 @@ FLAGS = [
 
 def _compile(src: str) -> str:
     obj = os.path.join(OBJDIR, os.path.splitext(src)[0] + ".o")
-    flags = [f for f in FLAGS if f != "-fno-honor-nans"] if src in NAN_SOURCES else FLAGS
-    cmd = [HIPCC] + flags + ["-c", os.path.join(CSRC, src), "-o", obj]
+    cmd = [HIPCC] + FLAGS + ["-c", os.path.join(CSRC, src), "-o", obj]
     res = subprocess.run(cmd, capture_output=True, text=True)
     # the host pass does not know the device-only feature flag; that warning is noise
     err = "\n".join(l for l in res.stderr.splitlines() if "packed-fp32-ops" not in l)

@@ -1,0 +1,223 @@
+// evo_cross_api.cpp -- the C ABI declared in include/evo_cross_attn.h:
+// validation (before any HIP call), plan and dispatch.
+#include "evo_cross_attn.h"
+
+#include <hip/hip_runtime.h>
+#include <math.h>
+
+#include "evo_cross.h"
+
+namespace {
+
+constexpr int64_t kMost = int64_t(1) << 40, kMostLen = 0x7fffffff - 128, kGrid = 0x7fffffff;
+
+bool aligned(const void *p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// a (row, token) grid of blocks that does not overlap itself
+bool apart(int64_t n, int64_t len, int64_t block, int64_t row, int64_t tok) {
+    if (n == 0 || len == 0) return true;
+    if ((len > 1 && tok < block) || (n > 1 && row < block)) return false;
+    if (n == 1 || len == 1) return true;
+    return row >= (len - 1) * tok + block || tok >= (n - 1) * row + block;
+}
+
+int check_stride(int64_t v, int64_t count, int64_t es) {
+    if (v < 0) return EVO_ERR_INVALID_ARG;
+    if (v > kMost || (v > 0 && count > (kMost << 10) / v)) return EVO_ERR_UNSUPPORTED;
+    return v * es % 16 != 0 ? EVO_ERR_ALIGNMENT : EVO_OK;
+}
+
+int check(const evo_cross_dims *d, bool has_bias, evo::CrArgs *a) {
+    if (!d) return EVO_ERR_INVALID_ARG;
+    if (d->dtype != EVO_DTYPE_F32 && d->dtype != EVO_DTYPE_BF16) return EVO_ERR_UNSUPPORTED;
+    if (d->n_heads < 1 || d->n_kv_heads < 1 || d->n_heads % d->n_kv_heads != 0 || d->head_dim < 1 || d->n_rows < 0 ||
+        d->len_q < 0 || d->len_k < 0)
+        return EVO_ERR_INVALID_ARG;
+    if (d->head_dim % 8 != 0 || d->head_dim > 128 || d->n_heads > 65535) return EVO_ERR_UNSUPPORTED;
+    const int64_t N = d->n_rows, G = d->n_heads / d->n_kv_heads, es = d->dtype == EVO_DTYPE_BF16 ? 2 : 4;
+    if (d->len_q > kMostLen / G || d->len_k > kMostLen || N > kMost) return EVO_ERR_UNSUPPORTED;
+    const int64_t M = d->len_q * G, qe = d->len_q * d->n_heads * d->head_dim, ke = d->len_k * d->n_kv_heads * d->head_dim;
+    if (qe > kMost || ke > kMost || (qe > 0 && N > kMost / qe) || (ke > 0 && N > kMost / ke)) return EVO_ERR_UNSUPPORTED;
+    if (has_bias) {
+        if (d->rows_per_bias < 1 || N % d->rows_per_bias != 0) return EVO_ERR_INVALID_ARG;
+        const int64_t plane = d->n_heads * d->len_q;  // < 2^47
+        const int64_t B = N / d->rows_per_bias;
+        if (d->rows_per_bias > 0x7fffffff) return EVO_ERR_UNSUPPORTED;
+        if (plane > kMost || (plane > 0 && d->len_k > kMost / plane) ||
+            (plane > 0 && d->len_k > 0 && B > kMost / (plane * d->len_k)))
+            return EVO_ERR_UNSUPPORTED;
+        const int64_t wgs = up(d->len_q, 64) * up(d->len_k, 64);  // <= 2^50
+        if (wgs > 0 && B * d->n_heads > kGrid / wgs) return EVO_ERR_UNSUPPORTED;
+    }
+    const int64_t st[6] = {d->q_stride_row, d->q_stride_tok, d->k_stride_row, d->k_stride_tok, d->o_stride_row, d->o_stride_tok};
+    for (int i = 0; i < 6; ++i) {
+        const int e = check_stride(st[i], i % 2 == 0 ? N : (i == 3 ? d->len_k : d->len_q), es);
+        if (e) return e;
+    }
+    // tiles of one unit in any kernel, before splits (which only ever fill up to 512 workgroups)
+    int64_t tiles = up(M, 32) > up(d->len_k, 128) ? up(M, 32) : up(d->len_k, 128);
+    if (tiles < 1) tiles = 1;
+    if (N > kGrid / tiles / d->n_kv_heads) return EVO_ERR_UNSUPPORTED;
+    if (N * d->len_q > (kGrid * 8) / d->n_heads) return EVO_ERR_UNSUPPORTED;
+    *a = evo::CrArgs{};
+    a->N = N;
+    a->rpb = has_bias ? d->rows_per_bias : (N > 0 ? N : 1);
+    a->Lq = (int)d->len_q;
+    a->Lk = (int)d->len_k;
+    a->M = (int)M;
+    a->H = d->n_heads;
+    a->Hk = d->n_kv_heads;
+    a->G = (int)G;
+    a->D = d->head_dim;
+    a->q_row = st[0], a->q_tok = st[1], a->k_row = st[2], a->k_tok = st[3], a->o_row = st[4], a->o_tok = st[5];
+    a->bf16 = d->dtype == EVO_DTYPE_BF16;
+    // x / G = x * ceil(2^(31 + s) / G) >> (31 + s), 2^s >= G, exact for x < 2^31 (the excess over x / G stays below 1 / G)
+    int s = 0;
+    while ((int64_t(1) << s) < G) ++s;
+    a->g_mul = (uint32_t)(((uint64_t(1) << (31 + s)) + G - 1) / G);
+    a->g_shift = 31 + s;
+    a->scale = 1.0f / sqrtf((float)d->head_dim);
+    return EVO_OK;
+}
+
+bool apart_o(const evo::CrArgs &a) { return apart(a.N, a.Lq, (int64_t)a.H * a.D, a.o_row, a.o_tok); }
+
+// the address range of a token tensor
+struct Range {
+    uintptr_t lo, hi;
+};
+Range range(const evo::CrArgs &a, const void *p, int len, int heads, int64_t row, int64_t tok) {
+    const int64_t n = ((a.N - 1) * row + (int64_t)(len - 1) * tok + (int64_t)heads * a.D) * (a.bf16 ? 2 : 4);
+    return Range{(uintptr_t)p, (uintptr_t)p + (p && len > 0 ? (uintptr_t)n : 0)};
+}
+Range flat(const void *p, int64_t bytes) { return Range{(uintptr_t)p, (uintptr_t)p + (p ? (uintptr_t)bytes : 0)}; }
+
+}  // namespace
+
+namespace evo {
+
+// How many workgroups walk one axis together: as many as fill `slots` places,
+// and at least two steps each
+static int split(int64_t wgs, int64_t steps, int64_t slots) {
+    if (wgs <= 0 || steps <= 1 || wgs * 2 > slots) return 1;
+    int64_t n = slots / wgs;
+    if (n > steps / 2) n = steps / 2;
+    if (n < 2) return 1;
+    const int64_t per = up(steps, n);
+    return (int)up(steps, per);
+}
+
+CrPlan cross_plan(const CrArgs &a, bool has_gate, bool has_bias) {
+    CrPlan p{};
+    const int64_t units = a.N * a.Hk;
+    const int few_rows = a.bf16 ? 32 : 64;
+    p.few = a.M <= few_rows;
+    const int64_t tiles = up(a.M, p.few ? few_rows : 128), steps = up(a.Lk, p.few ? (a.bf16 ? 128 : 64) : (a.bf16 ? 64 : 32));
+    p.fwd_splits = split(units * tiles, steps, 512);
+    const auto pad = [](size_t x) { return (x + 255) / 256 * 256; };
+    if (p.fwd_splits > 1) {
+        p.fwd_part = 0;
+        p.fwd_ml = pad((size_t)p.fwd_splits * units * a.M * a.D * 4);
+        p.fwd_total = p.fwd_ml + pad((size_t)p.fwd_splits * units * a.M * 8);
+    }
+    p.kv_splits = split(units * up(a.Lk, 128), up(a.M, a.bf16 && a.D <= 64 ? 64 : 32), 512);
+    p.q_splits = split(units * up(a.M, 128), up(a.Lk, a.bf16 ? 64 : 32), 512);
+    p.bias_chunks = has_bias ? split(a.N / a.rpb * a.H * up(a.Lq, 64) * up(a.Lk, 64), a.rpb, 512) : 1;
+    p.bwd_da = pad((size_t)units * a.M * 4);
+    p.bwd_part = p.bwd_da + (has_gate ? pad((size_t)units * a.M * a.D * (a.bf16 ? 2 : 4)) : 0);
+    size_t part = 0;
+    const auto more = [&](int splits, size_t one) {
+        if (splits > 1 && part < splits * one) part = splits * one;
+    };
+    more(p.kv_splits, (size_t)units * a.Lk * a.D * 8);
+    more(p.q_splits, (size_t)units * a.M * a.D * 4);
+    if (has_bias) more(p.bias_chunks, (size_t)(a.N / a.rpb) * a.H * a.Lq * (size_t)a.Lk * 4);
+    p.bwd_total = p.bwd_part + pad(part);
+    return p;
+}
+
+}  // namespace evo
+
+extern "C" {
+
+size_t evo_cross_fwd_workspace_size(const evo_cross_dims *d) {
+    evo::CrArgs a;
+    if (check(d, false, &a) || a.N == 0 || a.Lq == 0) return 0;
+    return evo::cross_plan(a, false, false).fwd_total;
+}
+
+int evo_cross_fwd(const evo_cross_dims *d, const void *q, const void *k, const void *v, const void *gate, const void *bias,
+                  const uint8_t *mask, void *out, float *lse, void *ws, size_t ws_bytes, void *stream) {
+    evo::CrArgs a;
+    const int st = check(d, bias != nullptr, &a);
+    if (st) return st;
+    if (!apart_o(a)) return EVO_ERR_INVALID_ARG;
+    if (a.N == 0 || a.Lq == 0) return EVO_OK;
+    if (!q || !out || !lse || (a.Lk > 0 && (!k || !v))) return EVO_ERR_INVALID_ARG;
+    const size_t es = a.bf16 ? 2 : 4;
+    if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(gate, 16) || !aligned(out, 16) ||
+        !aligned(bias, es) || !aligned(lse, 4))
+        return EVO_ERR_ALIGNMENT;
+    const Range o = range(a, out, a.Lq, a.H, a.o_row, a.o_tok);
+    const Range in[4] = {range(a, q, a.Lq, a.H, a.q_row, a.q_tok), range(a, gate, a.Lq, a.H, a.q_row, a.q_tok),
+                         range(a, k, a.Lk, a.Hk, a.k_row, a.k_tok), range(a, v, a.Lk, a.Hk, a.k_row, a.k_tok)};
+    for (const Range &r : in)
+        if (r.lo < o.hi && o.lo < r.hi && r.lo != r.hi) return EVO_ERR_INVALID_ARG;
+    const evo::CrPlan p = evo::cross_plan(a, gate != nullptr, bias != nullptr);
+    if (p.fwd_total > 0 && (!ws || ws_bytes < p.fwd_total)) return EVO_ERR_WORKSPACE;
+    if (p.fwd_total > 0 && !aligned(ws, 256)) return EVO_ERR_ALIGNMENT;
+    a.q = q, a.k = k, a.v = v, a.gate = gate, a.bias = bias, a.mask = mask, a.out = out, a.lse = lse;
+    return evo::launch_cross_fwd(a, p, ws, (hipStream_t)stream) == hipSuccess ? EVO_OK : EVO_ERR_HIP;
+}
+
+size_t evo_cross_bwd_workspace_size(const evo_cross_dims *d, int has_gate, int has_bias) {
+    evo::CrArgs a;
+    if (check(d, has_bias != 0, &a) || a.N == 0) return 0;
+    return evo::cross_plan(a, has_gate != 0, has_bias != 0).bwd_total;
+}
+
+int evo_cross_bwd(const evo_cross_dims *d, const void *q, const void *k, const void *v, const void *gate, const void *bias,
+                  const uint8_t *mask, const void *out, const float *lse, const void *dout, void *dq, void *dk, void *dv,
+                  void *dgate, void *dbias, void *ws, size_t ws_bytes, void *stream) {
+    evo::CrArgs a;
+    const int st = check(d, bias != nullptr, &a);
+    if (st) return st;
+    if (!apart(a.N, a.Lq, (int64_t)a.H * a.D, a.q_row, a.q_tok) || !apart(a.N, a.Lk, (int64_t)a.Hk * a.D, a.k_row, a.k_tok))
+        return EVO_ERR_INVALID_ARG;
+    if (a.N == 0 || (a.Lq == 0 && a.Lk == 0)) return EVO_OK;
+    if ((gate != nullptr) != (dgate != nullptr) || (bias != nullptr) != (dbias != nullptr)) return EVO_ERR_INVALID_ARG;
+    if (a.Lq > 0 && (!q || !out || !lse || !dout || !dq)) return EVO_ERR_INVALID_ARG;
+    if (a.Lk > 0 && (!k || !v || !dk || !dv)) return EVO_ERR_INVALID_ARG;
+    const size_t es = a.bf16 ? 2 : 4;
+    const void *wide[] = {q, k, v, gate, out, dout, dq, dk, dv, dgate};
+    for (const void *x : wide)
+        if (!aligned(x, 16)) return EVO_ERR_ALIGNMENT;
+    if (!aligned(bias, es) || !aligned(dbias, es) || !aligned(lse, 4)) return EVO_ERR_ALIGNMENT;
+    // outputs apart from every input and from each other; views of one packed buffer may interleave
+    const bool packed_q = a.q_tok > (int64_t)a.H * a.D, packed_k = a.k_tok > (int64_t)a.Hk * a.D;
+    const auto qr = [&](const void *x) { return range(a, x, a.Lq, a.H, a.q_row, a.q_tok); };
+    const auto kr = [&](const void *x) { return range(a, x, a.Lk, a.Hk, a.k_row, a.k_tok); };
+    const auto orr = [&](const void *x) { return range(a, x, a.Lq, a.H, a.o_row, a.o_tok); };
+    const int64_t nb = a.N / a.rpb * a.H * a.Lq * (int64_t)a.Lk * (int64_t)es;
+    const Range outs[5] = {qr(dq), qr(dgate), kr(dk), kr(dv), flat(dbias, nb)};
+    const Range ins[7] = {qr(q), qr(gate), kr(k), kr(v), orr(out), orr(dout), flat(bias, nb)};
+    const bool packed[5] = {packed_q, packed_q, packed_k, packed_k, false};
+    for (int i = 0; i < 5; ++i) {
+        if (outs[i].lo == outs[i].hi) continue;
+        for (const Range &r : ins)
+            if (r.lo != r.hi && r.lo < outs[i].hi && outs[i].lo < r.hi) return EVO_ERR_INVALID_ARG;
+        for (int j = 0; j < i; ++j)
+            if (outs[j].lo != outs[j].hi && outs[j].lo < outs[i].hi && outs[i].lo < outs[j].hi &&
+                (outs[i].lo == outs[j].lo || !(packed[i] && packed[j])))
+                return EVO_ERR_INVALID_ARG;
+    }
+    const evo::CrPlan p = evo::cross_plan(a, gate != nullptr, bias != nullptr);
+    if (p.bwd_total > 0 && (!ws || ws_bytes < p.bwd_total)) return EVO_ERR_WORKSPACE;
+    if (p.bwd_total > 0 && !aligned(ws, 256)) return EVO_ERR_ALIGNMENT;
+    a.q = q, a.k = k, a.v = v, a.gate = gate, a.bias = bias, a.mask = mask, a.out = (void *)out, a.lse = (float *)lse;
+    a.dout = dout, a.dq = dq, a.dk = dk, a.dv = dv, a.dgate = dgate, a.dbias = dbias;
+    return evo::launch_cross_bwd(a, p, ws, (hipStream_t)stream) == hipSuccess ? EVO_OK : EVO_ERR_HIP;
+}
+
+}  // extern "C"

@@ -1,0 +1,579 @@
+// evo_cross_bwd.hip -- attention to states of another length, backward
+// (include/evo_cross_attn.h).  With P the probabilities, dA = sigmoid(g) dO:
+//   D = sum over channels of dO O,   dP = dA V',   dS = P (dP - D)
+//   dV = P' dA,  dK = dS' Q / sqrt d,  dQ = dS K / sqrt d,  dBias = sum over rows of dS
+//
+// P is formed again from the saved log-sum-exp, in each of three passes:
+//   keys:  a wave owns 32 keys (lane = key) and walks the queries: dK, dV
+//   rows:  a wave owns 32 queries (lane = query) and walks the keys: dQ
+//   bias:  a workgroup owns 64 x 64 entries of one bias plane and walks the
+//          rows that share it
+// Every sum runs in a fixed order; where the tiles do not fill the GPU, the
+// walked axis is split over workgroups, whose fp32 parts a last kernel sums.
+#include "evo_cross.h"
+
+namespace evo {
+namespace {
+
+constexpr int kThreads = 256;
+
+// D, dgate and dA: a group of gs lanes per (row, token, head), 16 bytes a lane
+template <typename T>
+__global__ __launch_bounds__(kThreads) void cross_prep_kernel(CrArgs a, int gs_log) {
+    using Y = Ty<T>;
+    using E = typename Y::E;
+    const int lane = threadIdx.x & 63, c = (lane & ((1 << gs_log) - 1)) * Y::VEC;
+    const int64_t rows = a.N * a.Lq * a.H, per = kThreads >> gs_log;
+    const int64_t row = (int64_t)blockIdx.x * per + (threadIdx.x >> gs_log);
+    const bool on = row < rows && c < a.D;
+    const int64_t tok = row / a.H, n = tok / a.Lq;
+    const int head = (int)(row - tok * a.H), t = (int)(tok - n * a.Lq);
+    const int64_t at = (int64_t)head * a.D + c;
+    float sum = 0.0f;
+    if (on) {
+        E o[Y::VEC], d[Y::VEC];
+        *reinterpret_cast<u32x4 *>(o) = *reinterpret_cast<const u32x4 *>((const E *)a.out + n * a.o_row + t * a.o_tok + at);
+        *reinterpret_cast<u32x4 *>(d) = *reinterpret_cast<const u32x4 *>((const E *)a.dout + n * a.o_row + t * a.o_tok + at);
+#pragma unroll
+        for (int e = 0; e < Y::VEC; ++e) sum = fmaf(Y::f(o[e]), Y::f(d[e]), sum);
+        if (a.gate) {
+            const int64_t q = n * a.q_row + t * a.q_tok + at;
+            E g[Y::VEC], dg[Y::VEC], da[Y::VEC];
+            *reinterpret_cast<u32x4 *>(g) = *reinterpret_cast<const u32x4 *>((const E *)a.gate + q);
+#pragma unroll
+            for (int e = 0; e < Y::VEC; ++e) {
+                // sigmoid and one minus it, each without cancellation
+                const float x = Y::f(g[e]), z = __builtin_amdgcn_exp2f(-fabsf(x) * kLog2e), r = 1.0f / (1.0f + z);
+                const float sig = x >= 0.0f ? r : z * r, rest = x >= 0.0f ? z * r : r;
+                da[e] = Y::e(Y::f(d[e]) * sig);  // rounded to the type: the operand of two matrix products
+                dg[e] = Y::e(Y::f(d[e]) * Y::f(o[e]) * rest);
+            }
+            *reinterpret_cast<u32x4 *>((E *)a.dgate + q) = *reinterpret_cast<u32x4 *>(dg);
+            *reinterpret_cast<u32x4 *>((E *)a.da + row * a.D + c) = *reinterpret_cast<u32x4 *>(da);
+        }
+    }
+    for (int k = 1; k < 1 << gs_log; k <<= 1) sum += __shfl_xor(sum, k, 64);
+    if (on && c == 0) a.dsum[((n * a.Hk + head / a.G) * a.Lq + t) * a.G + head % a.G] = sum;
+}
+
+// dA as the kernels read it: the prepared one, or dO itself without a gate
+struct DaView {
+    int64_t row, tok;
+};
+__device__ __forceinline__ DaView da_view(const CrArgs &a) {
+    return a.gate ? DaView{(int64_t)a.Lq * a.H * a.D, (int64_t)a.H * a.D} : DaView{a.o_row, a.o_tok};
+}
+
+// ---------------------------------------------------------------------------
+// keys: dK, dV
+template <typename T, int DP> struct KeysShape {
+    static constexpr bool WIDE = sizeof(typename Ty<T>::E) == 4;
+    static constexpr int KEYS = 128, XT = WIDE || DP == 128 ? 32 : 64;
+    static constexpr int STR = DP + Ty<T>::PAD, TILE = XT * STR;
+    static constexpr int WAVES = DP == 128 ? 1 : 2;  // per SIMD: the accumulators of 128 channels take half of its registers
+};
+
+template <typename T, int DP, bool BIAS>
+__global__ __launch_bounds__(kThreads, (KeysShape<T, DP>::WAVES)) void cross_keys_kernel(CrArgs a) {
+    using Y = Ty<T>;
+    using E = typename Y::E;
+    using Frag = typename Y::Frag;
+    using S = KeysShape<T, DP>;
+    constexpr int NK = DP / Y::KS, DT = DP / 32;
+    __shared__ __attribute__((aligned(16))) E tiles[2][2][S::TILE];
+    __shared__ __attribute__((aligned(16))) float stats[2][2][S::XT];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5;
+    uint32_t u = xcd_unit32(blockIdx.x, gridDim.x);
+    const int split = u % a.splits;
+    u /= a.splits;
+    const int tile = u % a.tiles;
+    const uint32_t unit = u / a.tiles;
+    const int64_t n = unit / a.Hk;
+    const int hk = unit % a.Hk;
+    const DaView dv = da_view(a);
+    const E *qbase = (const E *)a.q + n * a.q_row + (int64_t)hk * a.G * a.D;
+    const E *abase = (const E *)(a.gate ? a.da : a.dout) + n * dv.row + (int64_t)hk * a.G * a.D;
+
+    const int key = tile * S::KEYS + wave * 32 + (lane & 31), keyc = min(key, a.Lk - 1);
+    const bool keep = key < a.Lk && (!a.mask || a.mask[n * a.Lk + key]);
+    Frag kf[NK], vf[NK];
+    const int64_t koff = n * a.k_row + (int64_t)keyc * a.k_tok + (int64_t)hk * a.D;
+    load_rows<T, DP>(kf, (const E *)a.k + koff, a.D, keep, h);
+    load_rows<T, DP>(vf, (const E *)a.v + koff, a.D, keep, h);
+    const E *bias = BIAS ? (const E *)a.bias + (n / a.rpb * a.H + hk * a.G) * (int64_t)a.Lq * a.Lk + keyc : nullptr;
+
+    f32x16 dk[DT], dvv[DT];
+#pragma unroll
+    for (int i = 0; i < DT; ++i) dk[i] = dvv[i] = zero16();
+    const float to2 = a.scale * kLog2e;
+
+    Stage<T, DP, S::XT, kThreads> qs, as;
+    float lse_in = 0.0f, dsum_in = 0.0f;
+    auto request = [&](int step) {
+        const int x0 = step * S::XT;
+        auto in = [&](int r) { return x0 + r < a.M; };
+        auto at = [&](int r, int64_t tok) {
+            const int x = x0 + r, t = token_of(a, x);
+            return (int64_t)t * tok + (int64_t)(x - t * a.G) * a.D;
+        };
+        qs.load(qbase, a.D, tid, [&](int r) { return qbase + at(r, a.q_tok); }, in);
+        as.load(abase, a.D, tid, [&](int r) { return abase + at(r, dv.tok); }, in);
+        if (tid < S::XT) {
+            // a query without keys, and what lies behind the last: probability exp(-inf)
+            const int x = x0 + tid, xc = min(x, a.M - 1), t = token_of(a, xc), g = xc - t * a.G;
+            lse_in = a.lse[(n * a.H + hk * a.G + g) * a.Lq + t];
+            if (x >= a.M || lse_in == -__builtin_inff()) lse_in = __builtin_inff();
+            dsum_in = x < a.M ? a.dsum[(int64_t)unit * a.M + x] : 0.0f;
+        }
+    };
+    const int s0 = split * a.per_split, s1 = min(s0 + a.per_split, a.ntiles);
+    // a workgroup whose keys are all masked has zeros to write and nothing to read
+    const bool work = __syncthreads_or(keep);
+    if (work && s0 < s1) request(s0);
+    for (int step = s0; work && step < s1; ++step) {
+        const int buf = step & 1, x0 = step * S::XT;
+        E *qt = tiles[buf][0], *at = tiles[buf][1];
+        auto in = [&](int r) { return x0 + r < a.M; };
+        qs.store(qt, a.D, tid, in);
+        as.store(at, a.D, tid, in);
+        if (tid < S::XT) {
+            stats[buf][0][tid] = BIAS ? lse_in : lse_in * kLog2e;
+            stats[buf][1][tid] = dsum_in;
+        }
+        __syncthreads();
+        if (step + 1 < s1) request(step + 1);
+#pragma unroll
+        for (int b = 0; b < S::XT / 32; ++b) {
+            f32x16 s = zero16(), dp = zero16();
+            const int off = (32 * b + (lane & 31)) * S::STR + Y::KS / 2 * h;
+#pragma unroll
+            for (int kk = 0; kk < NK; ++kk) Y::mma(s, Y::row(qt + off + Y::KS * kk), kf[kk]);
+#pragma unroll
+            for (int kk = 0; kk < NK; ++kk) Y::mma(dp, Y::row(at + off + Y::KS * kk), vf[kk]);
+            if (BIAS) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int x = min(x0 + 32 * b + 8 * (i / 4) + 4 * h + i % 4, a.M - 1), t = token_of(a, x);
+                    s[i] = fmaf(s[i], a.scale, Y::f(bias[((int64_t)(x - t * a.G) * a.Lq + t) * a.Lk], keep));
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const f32x4 l = *reinterpret_cast<const f32x4 *>(&stats[buf][0][32 * b + 2 * i + 4 * h]);
+                const f32x4 d = *reinterpret_cast<const f32x4 *>(&stats[buf][1][32 * b + 2 * i + 4 * h]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[i + e] = __builtin_amdgcn_exp2f(BIAS ? (s[i + e] - l[e]) * kLog2e : fmaf(s[i + e], to2, -l[e]));
+                    dp[i + e] = s[i + e] * (dp[i + e] - d[e]);
+                }
+            }
+#pragma unroll
+            for (int g = 0; g < 32 / Y::KS; ++g) {
+                const Frag p = Y::pack(s, g), ds = Y::pack(dp, g);
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    Y::mma(dvv[d], Y::col(at, S::STR, 32 * b + Y::KS * g, 32 * d, lane), p);
+                    Y::mma(dk[d], Y::col(qt, S::STR, 32 * b + Y::KS * g, 32 * d, lane), ds);
+                }
+            }
+        }
+    }
+    if (key >= a.Lk) return;
+    const int64_t rows = a.N * a.Hk * (int64_t)a.Lk;
+    float *pk = a.part + (((int64_t)split * 2) * rows + (int64_t)unit * a.Lk + key) * a.D, *pv = pk + rows * a.D;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const int c = 32 * d + 2 * i + 4 * h;
+            if (c >= a.D) continue;
+            f32x4 x = {0, 0, 0, 0}, y = {0, 0, 0, 0};
+            if (keep) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = dk[d][i + e] * a.scale, y[e] = dvv[d][i + e];
+            }
+            if (a.splits > 1) {
+                *reinterpret_cast<f32x4 *>(pk + c) = x;
+                *reinterpret_cast<f32x4 *>(pv + c) = y;
+            } else {
+                E ex[4], ey[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) ex[e] = Y::e(x[e]), ey[e] = Y::e(y[e]);
+                E *ok = (E *)a.dk + koff + c, *ov = (E *)a.dv + koff + c;
+                __builtin_memcpy(__builtin_assume_aligned(ok, sizeof(ex)), ex, sizeof(ex));
+                __builtin_memcpy(__builtin_assume_aligned(ov, sizeof(ey)), ey, sizeof(ey));
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// rows: dQ
+template <typename T, int DP> struct RowsShape {
+    static constexpr bool WIDE = sizeof(typename Ty<T>::E) == 4;
+    static constexpr int KT = WIDE ? 32 : 64, ROWS = 128;
+    static constexpr int STR = DP + Ty<T>::PAD, TILE = KT * STR;
+    static constexpr int WAVES = WIDE && DP == 128 ? 1 : 2;
+};
+
+template <typename T, int DP, bool BIAS>
+__global__ __launch_bounds__(kThreads, (RowsShape<T, DP>::WAVES)) void cross_rows_kernel(CrArgs a) {
+    using Y = Ty<T>;
+    using E = typename Y::E;
+    using Frag = typename Y::Frag;
+    using S = RowsShape<T, DP>;
+    constexpr int NK = DP / Y::KS, DT = DP / 32;
+    __shared__ __attribute__((aligned(16))) E tiles[2][2][S::TILE];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5;
+    uint32_t u = xcd_unit32(blockIdx.x, gridDim.x);
+    const int split = u % a.splits;
+    u /= a.splits;
+    const int tile = u % a.tiles;
+    const uint32_t unit = u / a.tiles;
+    const int64_t n = unit / a.Hk;
+    const int hk = unit % a.Hk;
+    const DaView dv = da_view(a);
+
+    const int x = tile * S::ROWS + wave * 32 + (lane & 31);
+    const bool on = x < a.M;
+    const int xc = on ? x : a.M - 1, t = token_of(a, xc), head = hk * a.G + (xc - t * a.G);
+    Frag qf[NK], af[NK];
+    const int64_t qoff = n * a.q_row + (int64_t)t * a.q_tok + (int64_t)head * a.D;
+    load_rows<T, DP>(qf, (const E *)a.q + qoff, a.D, on, h);
+    load_rows<T, DP>(af, (const E *)(a.gate ? a.da : a.dout) + n * dv.row + (int64_t)t * dv.tok + (int64_t)head * a.D, a.D, on, h);
+    float lse = a.lse[(n * a.H + head) * a.Lq + t];
+    if (!on || lse == -__builtin_inff()) lse = __builtin_inff();
+    const float dsum = a.dsum[(int64_t)unit * a.M + xc];
+    const float to2 = a.scale * kLog2e, shift = -lse * kLog2e;
+    const E *brow = BIAS ? (const E *)a.bias + ((n / a.rpb * a.H + head) * a.Lq + t) * (int64_t)a.Lk : nullptr;
+
+    const E *kbase = (const E *)a.k + n * a.k_row + (int64_t)hk * a.D;
+    const E *vbase = (const E *)a.v + n * a.k_row + (int64_t)hk * a.D;
+    const uint8_t *mrow = a.mask ? a.mask + n * a.Lk : nullptr;
+    f32x16 dq[DT];
+#pragma unroll
+    for (int i = 0; i < DT; ++i) dq[i] = zero16();
+
+    using Bits = KeyBits<S::KT>;
+    Bits now, next;
+    Stage<T, DP, S::KT, kThreads> ks, vs;
+    auto request = [&](int step, const Bits &bits) {
+        const int64_t off = (int64_t)step * S::KT * a.k_tok;
+        auto keep = [&](int r) { return bits.get(r); };
+        ks.load(kbase, a.D, tid, [&](int r) { return kbase + off + (int64_t)r * a.k_tok; }, keep);
+        vs.load(vbase, a.D, tid, [&](int r) { return vbase + off + (int64_t)r * a.k_tok; }, keep);
+    };
+    typename Bits::Bytes bytes;
+    const int t0 = split * a.per_split, t1 = min(t0 + a.per_split, a.ntiles);
+    if (t0 < t1) {
+        next.set(Bits::request(mrow, t0 * S::KT, a.Lk, lane));
+        request(t0, next);
+        bytes = Bits::request(mrow, (t0 + 1) * S::KT, a.Lk, lane);
+    }
+    for (int step = t0; step < t1; ++step) {
+        E *kt = tiles[step & 1][0], *vt = tiles[step & 1][1];
+        now = next;
+        ks.store(kt, a.D, tid, [&](int r) { return now.get(r); });
+        vs.store(vt, a.D, tid, [&](int r) { return now.get(r); });
+        __syncthreads();
+        if (step + 1 < t1) {
+            next.set(bytes);
+            request(step + 1, next);
+            bytes = Bits::request(mrow, (step + 2) * S::KT, a.Lk, lane);
+        }
+        if (!now.any()) continue;
+#pragma unroll
+        for (int b = 0; b < S::KT / 32; ++b) {
+            f32x16 s = zero16(), dp = zero16();
+            const int off = (32 * b + (lane & 31)) * S::STR + Y::KS / 2 * h;
+#pragma unroll
+            for (int kk = 0; kk < NK; ++kk) Y::mma(s, Y::row(kt + off + Y::KS * kk), qf[kk]);
+#pragma unroll
+            for (int kk = 0; kk < NK; ++kk) Y::mma(dp, Y::row(vt + off + Y::KS * kk), af[kk]);
+            const uint32_t bits = now.sub(b);
+            const int k0 = step * S::KT + 32 * b + 4 * h;
+            if (bits == 0xffffffffu) {
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    f32x4 add = {0, 0, 0, 0};
+                    if (BIAS) add = load4(brow + k0 + 2 * i);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        s[i + e] = __builtin_amdgcn_exp2f(BIAS ? (fmaf(s[i + e], a.scale, add[e]) - lse) * kLog2e
+                                                               : fmaf(s[i + e], to2, shift));
+                }
+            } else {
+                const uint32_t mine = bits >> (4 * h);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const bool keep = (mine >> (8 * (i / 4) + i % 4)) & 1;
+                    float y;
+                    if (BIAS)
+                        y = (fmaf(s[i], a.scale, Y::f(brow[keep ? k0 + 8 * (i / 4) + i % 4 : 0], keep)) - lse) * kLog2e;
+                    else
+                        y = fmaf(s[i], to2, shift);
+                    s[i] = keep ? __builtin_amdgcn_exp2f(y) : 0.0f;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) dp[i] = s[i] * (dp[i] - dsum);
+#pragma unroll
+            for (int g = 0; g < 32 / Y::KS; ++g) {
+                const Frag ds = Y::pack(dp, g);
+#pragma unroll
+                for (int d = 0; d < DT; ++d) Y::mma(dq[d], Y::col(kt, S::STR, 32 * b + Y::KS * g, 32 * d, lane), ds);
+            }
+        }
+    }
+    if (!on) return;
+    float *part = a.part + ((int64_t)split * a.N * a.Hk * a.M + (int64_t)unit * a.M + x) * a.D;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const int c = 32 * d + 2 * i + 4 * h;
+            if (c >= a.D) continue;
+            f32x4 y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = dq[d][i + e] * a.scale;
+            if (a.splits > 1) {
+                *reinterpret_cast<f32x4 *>(part + c) = y;
+            } else {
+                E ey[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) ey[e] = Y::e(y[e]);
+                E *to = (E *)a.dq + qoff + c;
+                __builtin_memcpy(__builtin_assume_aligned(to, sizeof(ey)), ey, sizeof(ey));
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// bias: dBias.  tiles = 64-query tiles, ntiles = 64-key tiles, splits = chunks of
+// per_split rows of a plane
+template <typename T, int DP> struct BiasShape {
+    static constexpr int STR = DP + Ty<T>::PAD, TILE = 64 * STR;
+    static constexpr int WAVES = 4 * TILE * (int)sizeof(typename Ty<T>::E) <= 78 * 1024 ? 2 : 1;
+};
+
+template <typename T, int DP>
+__global__ __launch_bounds__(kThreads, (BiasShape<T, DP>::WAVES)) void cross_bias_kernel(CrArgs a) {
+    using Y = Ty<T>;
+    using E = typename Y::E;
+    using S = BiasShape<T, DP>;
+    constexpr int NK = DP / Y::KS;
+    __shared__ __attribute__((aligned(16))) E tiles[4][S::TILE];  // Q, dA, K, V
+    __shared__ __attribute__((aligned(16))) float stats[2][64];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5;
+    const int qb = wave & 1, kb = wave >> 1;
+    uint32_t u = blockIdx.x;
+    const int chunk = u % a.splits;
+    u /= a.splits;
+    const int kt = u % a.ntiles;
+    u /= a.ntiles;
+    const int qt = u % a.tiles;
+    u /= a.tiles;
+    const int head = u % a.H;
+    const int64_t plane = u / a.H;
+    const int hk = head / a.G, g = head % a.G;
+    const int t0 = qt * 64, k0 = kt * 64;
+    const DaView dv = da_view(a);
+    const int64_t n0 = plane * a.rpb + (int64_t)chunk * a.per_split, n1 = min(n0 + a.per_split, (plane + 1) * a.rpb);
+
+    const int key = k0 + kb * 32 + (lane & 31);
+    const int64_t brow = (plane * a.H + head) * a.Lq;
+    float bias[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const int t = min(t0 + qb * 32 + 8 * (i / 4) + 4 * h + i % 4, a.Lq - 1);
+        bias[i] = Y::f(((const E *)a.bias)[(brow + t) * a.Lk + min(key, a.Lk - 1)]);
+    }
+    f32x16 acc = zero16();
+    using Bits = KeyBits<64>;
+    Bits now, next;
+    Stage<T, DP, 64, kThreads> qs, as, ks, vs;
+    float lse_in = 0.0f, dsum_in = 0.0f;
+    auto in_q = [&](int r) { return t0 + r < a.Lq; };
+    auto request = [&](int64_t n) {
+        next.set(Bits::request(a.mask ? a.mask + n * a.Lk : nullptr, k0, a.Lk, lane));
+        const E *q = (const E *)a.q + n * a.q_row + (int64_t)head * a.D;
+        const E *da = (const E *)(a.gate ? a.da : a.dout) + n * dv.row + (int64_t)head * a.D;
+        const E *k = (const E *)a.k + n * a.k_row + (int64_t)hk * a.D, *v = (const E *)a.v + n * a.k_row + (int64_t)hk * a.D;
+        auto keep = [&](int r) { return next.get(r); };
+        qs.load(q, a.D, tid, [&](int r) { return q + (int64_t)(t0 + r) * a.q_tok; }, in_q);
+        as.load(da, a.D, tid, [&](int r) { return da + (int64_t)(t0 + r) * dv.tok; }, in_q);
+        ks.load(k, a.D, tid, [&](int r) { return k + (int64_t)(k0 + r) * a.k_tok; }, keep);
+        vs.load(v, a.D, tid, [&](int r) { return v + (int64_t)(k0 + r) * a.k_tok; }, keep);
+        if (tid < 64) {
+            const int t = min(t0 + tid, a.Lq - 1);
+            lse_in = a.lse[(n * a.H + head) * a.Lq + t];
+            if (t0 + tid >= a.Lq || lse_in == -__builtin_inff()) lse_in = __builtin_inff();
+            dsum_in = a.dsum[((n * a.Hk + hk) * a.Lq + t) * a.G + g];
+        }
+    };
+    if (n0 < n1) request(n0);
+    for (int64_t n = n0; n < n1; ++n) {
+        now = next;
+        auto keep = [&](int r) { return now.get(r); };
+        qs.store(tiles[0], a.D, tid, in_q);
+        as.store(tiles[1], a.D, tid, in_q);
+        ks.store(tiles[2], a.D, tid, keep);
+        vs.store(tiles[3], a.D, tid, keep);
+        if (tid < 64) stats[0][tid] = lse_in, stats[1][tid] = dsum_in;
+        __syncthreads();
+        if (n + 1 < n1) request(n + 1);
+        if (now.any()) {
+            f32x16 s = zero16(), dp = zero16();
+            const int qo = (32 * qb + (lane & 31)) * S::STR + Y::KS / 2 * h, ko = (32 * kb + (lane & 31)) * S::STR + Y::KS / 2 * h;
+#pragma unroll
+            for (int kk = 0; kk < NK; ++kk) {
+                Y::mma(s, Y::row(tiles[0] + qo + Y::KS * kk), Y::row(tiles[2] + ko + Y::KS * kk));
+                Y::mma(dp, Y::row(tiles[1] + qo + Y::KS * kk), Y::row(tiles[3] + ko + Y::KS * kk));
+            }
+            const bool mine = now.get(32 * kb + (lane & 31));
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const f32x4 l = *reinterpret_cast<const f32x4 *>(&stats[0][32 * qb + 2 * i + 4 * h]);
+                const f32x4 d = *reinterpret_cast<const f32x4 *>(&stats[1][32 * qb + 2 * i + 4 * h]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float b = __uint_as_float(mine ? __float_as_uint(bias[i + e]) : 0xff800000u);
+                    const float p = __builtin_amdgcn_exp2f((fmaf(s[i + e], a.scale, b) - l[e]) * kLog2e);
+                    acc[i + e] = fmaf(p, dp[i + e] - d[e], acc[i + e]);
+                }
+            }
+        }
+        __syncthreads();
+    }
+    if (key >= a.Lk) return;
+    const int64_t all = a.N / a.rpb * a.H * a.Lq * (int64_t)a.Lk;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const int t = t0 + qb * 32 + 8 * (i / 4) + 4 * h + i % 4;
+        if (t >= a.Lq) continue;
+        const int64_t at = (brow + t) * a.Lk + key;
+        if (a.splits > 1)
+            a.part[(int64_t)chunk * all + at] = acc[i];
+        else
+            ((E *)a.dbias)[at] = Y::e(acc[i]);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Sums of parts: rows of D channels written at (unit, i) -> token and head, or a flat array (D == 0)
+template <typename T>
+__global__ __launch_bounds__(kThreads) void cross_sum_kernel(CrArgs a, const float *part, int splits, int64_t stride, int64_t count,
+                                                             int len, int group, void *out, int64_t row_stride, int64_t tok_stride) {
+    using Y = Ty<T>;
+    using E = typename Y::E;
+    const int64_t at = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 4;
+    if (at >= count) return;
+    f32x4 sum = {0, 0, 0, 0};
+    const bool whole = at + 4 <= count;
+    for (int j = 0; j < splits; ++j) {
+        const float *p = part + j * stride + at;
+        if (whole) {
+            f32x4 x;
+            __builtin_memcpy(&x, p, 16);
+            sum += x;
+        } else {
+            for (int e = 0; e < count - at; ++e) sum[e] += p[e];
+        }
+    }
+    if (!row_stride) {
+        for (int e = 0; e < 4 && at + e < count; ++e) ((E *)out)[at + e] = Y::e(sum[e]);
+        return;
+    }
+    const int64_t row = at / a.D, unit = row / len, n = unit / a.Hk;
+    const int c = (int)(at - row * a.D), x = (int)(row - unit * len), t = group ? token_of(a, x) : x;
+    const int head = (int)(unit - n * a.Hk) * (group ? a.G : 1) + (group ? x - t * a.G : 0);
+    E e[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) e[i] = Y::e(sum[i]);
+    E *to = (E *)out + n * row_stride + (int64_t)t * tok_stride + (int64_t)head * a.D + c;
+    __builtin_memcpy(__builtin_assume_aligned(to, sizeof(e)), e, sizeof(e));
+}
+
+template <typename T>
+void sum_parts(const CrArgs &a, const float *part, int splits, int64_t stride, int64_t count, int len, int group, void *out,
+               int64_t row, int64_t tok, hipStream_t s) {
+    const uint32_t grid = (uint32_t)((count + 4 * kThreads - 1) / (4 * kThreads));
+    cross_sum_kernel<T><<<grid, kThreads, 0, s>>>(a, part, splits, stride, count, len, group, out, row, tok);
+}
+
+template <typename T, int DP> void run(CrArgs a, const CrPlan &p, hipStream_t s) {
+    const int64_t units = a.N * a.Hk;
+    const bool bias = a.bias != nullptr;
+    if (a.Lk > 0) {
+        CrArgs k = a;
+        using S = KeysShape<T, DP>;
+        k.tiles = (a.Lk + S::KEYS - 1) / S::KEYS;
+        k.ntiles = (a.M + S::XT - 1) / S::XT;
+        k.splits = p.kv_splits;
+        k.per_split = (k.ntiles + k.splits - 1) / k.splits;
+        const uint32_t grid = (uint32_t)(units * k.tiles * k.splits);
+        if (bias)
+            cross_keys_kernel<T, DP, true><<<grid, kThreads, 0, s>>>(k);
+        else
+            cross_keys_kernel<T, DP, false><<<grid, kThreads, 0, s>>>(k);
+        if (k.splits > 1) {
+            const int64_t count = units * a.Lk * a.D;
+            sum_parts<T>(a, a.part, k.splits, 2 * count, count, a.Lk, 0, a.dk, a.k_row, a.k_tok, s);
+            sum_parts<T>(a, a.part + count, k.splits, 2 * count, count, a.Lk, 0, a.dv, a.k_row, a.k_tok, s);
+        }
+    }
+    if (a.M > 0) {
+        CrArgs k = a;
+        using S = RowsShape<T, DP>;
+        k.tiles = (a.M + S::ROWS - 1) / S::ROWS;
+        k.ntiles = (a.Lk + S::KT - 1) / S::KT;
+        k.splits = p.q_splits;
+        k.per_split = (k.ntiles + k.splits - 1) / k.splits;
+        const uint32_t grid = (uint32_t)(units * k.tiles * k.splits);
+        if (bias)
+            cross_rows_kernel<T, DP, true><<<grid, kThreads, 0, s>>>(k);
+        else
+            cross_rows_kernel<T, DP, false><<<grid, kThreads, 0, s>>>(k);
+        if (k.splits > 1) {
+            const int64_t count = units * a.M * a.D;
+            sum_parts<T>(a, a.part, k.splits, count, count, a.M, 1, a.dq, a.q_row, a.q_tok, s);
+        }
+    }
+    if (bias && a.M > 0 && a.Lk > 0) {
+        CrArgs k = a;
+        k.tiles = (a.Lq + 63) / 64;
+        k.ntiles = (a.Lk + 63) / 64;
+        k.splits = p.bias_chunks;
+        k.per_split = (int)((a.rpb + k.splits - 1) / k.splits);
+        const int64_t planes = a.N / a.rpb * a.H;
+        cross_bias_kernel<T, DP><<<(uint32_t)(planes * k.tiles * k.ntiles * k.splits), kThreads, 0, s>>>(k);
+        if (k.splits > 1) {
+            const int64_t count = planes * a.Lq * a.Lk;
+            sum_parts<T>(a, a.part, k.splits, count, count, 1, 0, a.dbias, 0, 0, s);
+        }
+    }
+}
+
+template <typename T> void run_dim(const CrArgs &a, const CrPlan &p, hipStream_t s) {
+    int gs_log = 0;
+    while ((Ty<T>::VEC << gs_log) < a.D) ++gs_log;
+    const int64_t rows = a.N * a.Lq * a.H, per = kThreads >> gs_log;
+    if (rows > 0) cross_prep_kernel<T><<<(uint32_t)((rows + per - 1) / per), kThreads, 0, s>>>(a, gs_log);
+    a.D <= 32 ? run<T, 32>(a, p, s) : a.D <= 64 ? run<T, 64>(a, p, s) : run<T, 128>(a, p, s);
+}
+
+}  // namespace
+
+hipError_t launch_cross_bwd(CrArgs a, const CrPlan &p, void *ws, hipStream_t s) {
+    a.dsum = (float *)ws;
+    a.da = (char *)ws + p.bwd_da;
+    a.part = (float *)((char *)ws + p.bwd_part);
+    a.bf16 ? run_dim<bf16_t>(a, p, s) : run_dim<float>(a, p, s);
+    return hipGetLastError();
+}
+
+}  // namespace evo

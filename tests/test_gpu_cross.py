@@ -1,0 +1,354 @@
+"""GPU parity of the attention to states of another length (through the C ABI)
+against the fp64 oracle.
+
+Tolerances, element by element, from the oracle's own values.  u is half a step
+of the type (bf16 2^-8, fp32 2^-24), f = 2^-24.  A logit is a sum of d
+products in fp32, scaled: off by f ((d + 4) |q||k| / sqrt d + 4 |x|), and the
+exponent takes in 4 f |lse| more; the largest such sum D of a row makes its
+probabilities off by 1.5 D relative, sums over the keys by (Lk + 64) f: that
+is r.  In bf16 the probabilities are rounded once on their way into a product
+(u).  So
+  out:   (r + u) sig sum p |v| + 4 f |out|, and u |out| for the rounding
+  dv:    (r + 2 u) sum p |da|     (da = sig dout is rounded, too, with a gate)
+  ds:    p (u + f d) (|da||v|)  for da's rounding, p |dout| err(out) for D, which
+         is formed from the rounded output, and (2 r + 4 f) p (|dp| + |D|)
+  dq, dk: sums of (err(ds) + u |ds|) |k|, |q|; dbias: sum of err(ds)
+each and the result's rounding, u of it.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import cross_oracle as co
+from paper_2404_11068_amd import cross
+from paper_2404_11068_amd import evo_attn as ea
+from paper_2404_11068_amd import graph as gr
+from tests.parity_util import to_f64
+
+pytestmark = pytest.mark.gpu
+F = 2.0 ** -24
+
+
+def _bounds(q, k, v, gate, bias, mask, dout, rpb, u):
+    """Bounds on the errors of (out, lse, dq, dk, dv, dgate, dbias)."""
+    N, Lq, H, d = q.shape
+    Lk, Hk = k.shape[1:3]
+    G = H // Hk
+    keep = np.ones((N, Lk), bool) if mask is None else mask != 0
+    k, v = (np.where(keep[:, :, None, None], t, 0.0) for t in (k, v))
+    out, lse, prob = co.forward(q, k, v, gate, bias, mask, rpb)
+    _, _, _, _, _ = co.backward(q, k, v, gate, bias, mask, dout, rpb)
+    sig = 1 / (1 + np.exp(-gate)) if gate is not None else np.ones_like(q)
+    da = dout * sig
+    b = [np.zeros_like(out), np.zeros_like(lse), np.zeros_like(q), np.zeros_like(k), np.zeros_like(v), np.zeros_like(q),
+         None if bias is None else np.zeros_like(bias)]
+    for n in range(N):
+        for h in range(H):
+            j, p = h // G, prob[n, h]
+            on = p > 0
+            qk = np.abs(q[n, :, h]) @ np.abs(k[n, :, j]).T / np.sqrt(d)
+            x = q[n, :, h] @ k[n, :, j].T / np.sqrt(d) + (0 if bias is None else np.where(on, bias[n // rpb, h], 0.0))
+            l = np.where(np.isfinite(lse[n, h]), np.abs(lse[n, h]), 0.0)
+            dl = F * ((d + 4) * qk + 4 * np.abs(x)) * on
+            top = dl.max(1, initial=0.0) + 4 * F * l
+            r = (1.5 * top + (Lk + 64) * F)[:, None]
+            b[1][n, h] = r[:, 0] + 4 * F * l
+            eo = sig[n, :, h] * ((r + u) * (p @ np.abs(v[n, :, j]))) + 4 * F * np.abs(out[n, :, h])
+            eo += u * (np.abs(out[n, :, h]) + eo)
+            b[0][n, :, h] = eo
+            ab = np.abs(da[n, :, h]) @ np.abs(v[n, :, j]).T
+            dd = np.sum(np.abs(dout[n, :, h]) * eo, 1, keepdims=True) + d * F * np.sum(np.abs(dout[n, :, h] * out[n, :, h]), 1, keepdims=True)
+            eds = p * ((u + d * F) * ab + dd + (2 * r + 4 * F) * (ab + np.sum(np.abs(dout[n, :, h] * out[n, :, h]), 1, keepdims=True)))
+            ds = p * (ab + np.sum(np.abs(dout[n, :, h] * out[n, :, h]), 1, keepdims=True))
+            full = eds + (u + (Lk + Lq * G) * F) * ds
+            b[2][n, :, h] += full @ np.abs(k[n, :, j]) / np.sqrt(d)
+            b[3][n, :, j] += full.T @ np.abs(q[n, :, h]) / np.sqrt(d)
+            b[4][n, :, j] += ((r + 2 * u + Lq * G * F) * p).T @ np.abs(da[n, :, h])
+            b[5][n, :, h] = np.abs(dout[n, :, h]) * (eo + 8 * F * np.abs(out[n, :, h])) * (1 - sig[n, :, h])
+            if bias is not None:
+                b[6][n // rpb, h] += eds + N * F * ds
+    return b
+
+
+def _close(got, ref, bound, u, what):
+    got, ref = to_f64(got), np.asarray(ref)
+    assert got.shape == ref.shape, what
+    inf = ~np.isfinite(ref)
+    assert np.array_equal(got[inf], ref[inf]), what
+    off = np.where(inf, 0.0, np.abs(np.where(inf, 0.0, got) - np.where(inf, 0.0, ref)))
+    assert np.isfinite(off).all(), what
+    limit = np.where(inf, 1.0, bound + u * (np.abs(np.where(inf, 0.0, ref)) + bound) + 1e-37)
+    worst = np.unravel_index((off / limit).argmax(), off.shape) if off.size else None
+    assert (off <= limit).all(), (what, worst, float(off[worst]), float(limit[worst]), float(ref[worst]))
+
+
+def _draw(case, dtype, seed=1):
+    N, Lq, Lk, H, Hk, d, gate, planes, mask = case
+    rng = np.random.default_rng(seed)
+    t = lambda *s: torch.from_numpy(rng.standard_normal(s)).to(dtype).cuda()
+    q, k, v, dout = t(N, Lq, H, d), t(N, Lk, Hk, d), t(N, Lk, Hk, d), t(N, Lq, H, d)
+    g = t(N, Lq, H, d) if gate else None
+    bias = t(planes, H, Lq, Lk) if planes else None
+    m = None
+    if mask == "random":
+        m = torch.from_numpy((rng.random((N, Lk)) < 0.6).astype(np.uint8)).cuda()
+    elif mask == "length":
+        m = torch.from_numpy((np.arange(Lk) < rng.integers(0, Lk + 1, (N, 1))).astype(np.uint8)).cuda()
+        m[0] = 0
+    elif mask == "last":
+        m = torch.zeros(N, Lk, dtype=torch.bool, device="cuda")
+        m[:, -1:] = True
+    return q, k, v, g, bias, m, dout
+
+
+def _check(case, dtype, args, rpb, run=None):
+    q, k, v, g, bias, m, dout = args
+    u = 2.0 ** -8 if dtype == torch.bfloat16 else F
+    f = [None if t is None else to_f64(t) for t in (q, k, v, g, bias)]
+    mm = None if m is None else m.cpu().numpy().astype(np.uint8)
+    do = to_f64(dout)
+    out, lse = cross.cross_attn_fwd(q, k, v, g, bias, m, rows_per_bias=rpb)
+    grads = cross.cross_attn_bwd(q, k, v, g, bias, m, out, lse, dout, rows_per_bias=rpb)
+    torch.cuda.synchronize()
+    with np.errstate(invalid="ignore"):
+        ref = co.forward(*f, mm, rpb)[:2] + tuple(co.backward(*f, mm, do, rpb))
+        bounds = _bounds(*f, mm, do, rpb or max(q.shape[0], 1), u)
+    for name, got, r, b in zip(("out", "lse", "dq", "dk", "dv", "dgate", "dbias"), (out, lse) + grads, ref, bounds):
+        assert (got is None) == (r is None), name
+        if got is not None:
+            _close(got, r, b, 0.0 if name == "lse" else u, name)
+    return out, lse, grads
+
+
+CASES = [
+    # N, Lq, Lk, H, Hk, d, gate, bias planes, mask
+    (1, 1, 1, 1, 1, 8, False, 0, None),
+    (2, 1, 5, 4, 4, 16, True, 1, "random"),
+    (3, 1, 300, 8, 2, 64, False, 0, "length"),
+    (1, 1, 2500, 4, 1, 128, False, 1, None),
+    (2, 3, 129, 6, 2, 32, True, 2, "random"),
+    (2, 40, 1, 4, 4, 32, True, 1, None),
+    (2, 33, 31, 2, 2, 24, False, 0, None),
+    (1, 128, 64, 2, 1, 64, True, 0, None),
+    (2, 65, 127, 4, 2, 64, False, 1, "random"),
+    (4, 30, 77, 8, 8, 32, True, 2, "length"),
+    (2, 129, 130, 2, 2, 128, True, 1, "length"),
+    (1, 257, 200, 4, 1, 128, False, 0, "random"),
+    (3, 9, 70, 5, 1, 40, True, 3, "last"),
+    (2, 50, 600, 2, 2, 8, True, 1, "random"),
+    (1, 700, 33, 2, 1, 80, True, 0, None),
+    (2, 17, 64, 12, 4, 104, False, 1, None),
+    (64, 5, 7, 2, 2, 16, True, 1, "random"),
+]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "N%d_%dx%d_H%d_%d_d%d_g%d_b%d_%s" % c)
+def test_forward_and_backward(case, dtype):
+    print("\n[case]", case, dtype, flush=True)
+    args = _draw(case, dtype)
+    rpb = case[0] // case[7] if case[7] else None
+    out, lse, grads = _check(case, dtype, args, rpb)
+    q, k, v, g, bias, m, dout = args
+    out2, lse2 = cross.cross_attn_fwd(q, k, v, g, bias, m, rows_per_bias=rpb)
+    again = cross.cross_attn_bwd(q, k, v, g, bias, m, out, lse, dout, rows_per_bias=rpb)
+    assert torch.equal(out, out2) and torch.equal(lse, lse2)
+    for a, b in zip(grads, again):
+        assert a is None or torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("Lq", [1, 100])
+def test_what_masked_places_hold_does_not_matter(dtype, Lq):
+    case = (2, Lq, 150, 4, 2, 64, True, 1, "random")
+    q, k, v, g, bias, m, dout = _draw(case, dtype, 2)
+    ref = _check(case, dtype, (q, k, v, g, bias, m, dout), None)
+    off = m == 0
+    m2 = m.clone()
+    both = off.all(0)                                                  # bias columns that every row masks
+    for fill in (float("nan"), float("inf"), -float("inf"), torch.finfo(dtype).max):
+        k2, v2, b2 = k.clone(), v.clone(), bias.clone()
+        k2[off], v2[off] = fill, fill
+        b2[..., both] = fill
+        out, lse = cross.cross_attn_fwd(q, k2, v2, g, b2, m2)
+        grads = cross.cross_attn_bwd(q, k2, v2, g, b2, m2, out, lse, dout)
+        torch.cuda.synchronize()
+        assert torch.equal(out, ref[0]) and torch.equal(lse, ref[1])
+        for a, b in zip(grads, ref[2]):
+            assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("Lq", [1, 70])
+def test_bias_as_mask(dtype, Lq):
+    """-inf and the type's lowest value in the bias: of some keys, of a whole tile, of all keys of a query."""
+    case = (2, Lq, 200, 4, 4, 32, True, 1, None)
+    q, k, v, g, bias, m, dout = _draw(case, dtype, 3)
+    low = torch.finfo(dtype).min
+    bias[:, 0, :, ::3] = -float("inf")
+    bias[:, 1, :, 1::2] = low
+    bias[:, 1, :, :128] = low
+    bias[:, 2, 0] = -float("inf")
+    bias[:, 3, Lq - 1] = low
+    out, lse, grads = _check(case, dtype, (q, k, v, g, bias, m, dout), None)
+    assert not out[:, 0, 2].any() and not out[:, Lq - 1, 3].any()
+    assert (lse[:, 2, 0] == -float("inf")).all() and (lse[:, 3, Lq - 1] == -float("inf")).all()
+    assert not grads[0][:, 0, 2].any() and not grads[4][:, 3, Lq - 1].any()
+
+
+def test_large_logits_and_peaked_rows():
+    """Logits of hundreds, the largest anywhere along the keys: the running maximum rises more than once."""
+    for dtype in (torch.bfloat16, torch.float32):
+        case = (1, 40, 500, 2, 1, 64, False, 0, None)
+        q, k, v, g, bias, m, dout = _draw(case, dtype, 4)
+        k *= torch.linspace(0.1, 12.0, 500, device="cuda").view(1, -1, 1, 1).to(dtype)
+        out, lse = cross.cross_attn_fwd(q, k, v)
+        f = [to_f64(t) for t in (q, k, v)]
+        ref = co.forward(*f)
+        b = _bounds(*f, None, None, None, to_f64(dout), 1, 2.0 ** -8 if dtype == torch.bfloat16 else F)
+        _close(out, ref[0], b[0], 0.0, "out")
+        _close(lse, ref[1], b[1], 0.0, "lse")
+
+
+def test_strided_views_and_repeated_states():
+    dtype = torch.bfloat16
+    N, Lq, Lk, H, d = 2, 37, 90, 4, 32
+    torch.manual_seed(0)
+    x = torch.randn(N, Lq, 2 * H, d, device="cuda").to(dtype)          # queries and gate, packed
+    kv = torch.randn(Lk, N, 2, H, d, device="cuda").to(dtype)          # tokens outermost, keys and values packed
+    q, g = x[:, :, :H], x[:, :, H:]
+    k, v = kv[:, :, 0].transpose(0, 1), kv[:, :, 1].transpose(0, 1)
+    c = [t.contiguous() for t in (q, k, v, g)]
+    ref = cross.cross_attn_fwd(*c)
+    back = torch.empty(Lq, N, H, d, device="cuda", dtype=dtype).transpose(0, 1)
+    got = cross.cross_attn_fwd(q, k, v, g, out=back)
+    assert got[0] is back and torch.equal(back, ref[0]) and torch.equal(got[1], ref[1])
+    dout = torch.randn(N, Lq, H, d, device="cuda").to(dtype)
+    dback = torch.empty_like(back)
+    dback.copy_(dout)
+    assert dback.stride() == back.stride()
+    rg = cross.cross_attn_bwd(*c, None, None, *ref, dout)
+    gg = cross.cross_attn_bwd(q, k, v, g, None, None, back, got[1], dback)
+    # gradients into packed buffers
+    dx, dkv = torch.zeros_like(x), torch.zeros_like(kv)
+    pg = cross.cross_attn_bwd(q, k, v, g, None, None, back, got[1], dback, dq=dx[:, :, :H], dgate=dx[:, :, H:],
+                              dk=dkv[:, :, 0].transpose(0, 1), dv=dkv[:, :, 1].transpose(0, 1))
+    torch.cuda.synchronize()
+    for a, b, p in zip(rg, gg, pg):
+        assert a is None or (torch.equal(a, b) and torch.equal(a, p))
+    assert gg[1].stride() == k.stride()
+    # one set of states for all rows
+    one_k, one_v = c[1][:1].expand(N, Lk, H, d), c[2][:1].expand(N, Lk, H, d)
+    a = cross.cross_attn_fwd(c[0], one_k, one_v)
+    b = cross.cross_attn_fwd(c[0], one_k.contiguous(), one_v.contiguous())
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    with pytest.raises(ValueError):
+        cross.cross_attn_bwd(c[0], one_k, one_v, None, None, None, *a, dout)
+    # rows behind the last token of a larger buffer stay as they were
+    big = torch.full((N, Lq + 5, H, d), 7.0, device="cuda", dtype=dtype)
+    cross.cross_attn_fwd(*c, out=big[:, :Lq])
+    torch.cuda.synchronize()
+    assert torch.equal(big[:, :Lq], ref[0]) and (big[:, Lq:] == 7.0).all()
+
+
+@pytest.mark.parametrize("Lq", [1, 48])
+def test_offsets_beyond_32_bits(Lq):
+    """States of more than 2^32 bytes, all but a few keys masked (and never initialised)."""
+    N, Lk, H, d = 1, (1 << 21) + 77, 16, 128
+    k = torch.empty(N, Lk, H, d, device="cuda", dtype=torch.bfloat16)
+    v = torch.empty_like(k)
+    assert k.numel() * 2 > 1 << 33
+    where = torch.tensor([3, (1 << 20) + 5, (1 << 21) - 1, Lk - 2], device="cuda")
+    mask = torch.zeros(N, Lk, dtype=torch.uint8, device="cuda")
+    mask[:, where] = 1
+    g = torch.Generator(device="cuda").manual_seed(1)
+    few_k, few_v = (torch.randn(N, 4, H, d, device="cuda", generator=g).bfloat16() for _ in range(2))
+    k[:, where], v[:, where] = few_k, few_v
+    q, dout = (torch.randn(N, Lq, H, d, device="cuda", generator=g).bfloat16() for _ in range(2))
+    out, lse = cross.cross_attn_fwd(q, k, v, None, None, mask)
+    grads = cross.cross_attn_bwd(q, k, v, None, None, mask, out, lse, dout)
+    torch.cuda.synchronize()
+    f = [to_f64(t) for t in (q, few_k, few_v)]
+    b = _bounds(*f, None, None, None, to_f64(dout), 1, 2.0 ** -8)
+    ref = co.forward(*f)[:2] + tuple(co.backward(*f, None, None, None, to_f64(dout)))
+    u = 2.0 ** -8
+    _close(out, ref[0], b[0], u, "out")
+    _close(lse, ref[1], b[1] + 1e-6, 0.0, "lse")
+    _close(grads[0], ref[2], b[2], u, "dq")
+    _close(grads[1][:, where], ref[3], b[3], u, "dk")
+    _close(grads[2][:, where], ref[4], b[4], u, "dv")
+    assert int((grads[1].view(torch.int16) != 0).any(-1).any(-1).sum()) <= 4
+
+
+def test_empty_axes():
+    q, k = torch.randn(2, 3, 4, 16, device="cuda"), torch.randn(2, 5, 2, 16, device="cuda")
+    out, lse = cross.cross_attn_fwd(q, k[:, :0], k[:, :0], q + 0)
+    g = cross.cross_attn_bwd(q, k[:, :0], k[:, :0], q + 0, None, None, out, lse, q + 0)
+    torch.cuda.synchronize()
+    assert not out.any() and (lse == -float("inf")).all() and not g[0].any() and not g[3].any() and g[1].numel() == 0
+    e = q[:, :0]
+    out, lse = cross.cross_attn_fwd(e, k, k)
+    g = cross.cross_attn_bwd(e, k, k, None, None, None, out, lse, e)
+    torch.cuda.synchronize()
+    assert out.shape == e.shape and not g[1].any() and not g[2].any()
+    out, lse = cross.cross_attn_fwd(q[:0], k[:0], k[:0])
+    assert out.shape == (0, 3, 4, 16) and lse.shape == (0, 4, 3)
+
+
+def test_two_graphs_share_a_workspace():
+    case = (2, 20, 700, 4, 2, 64, True, 1, "random")
+    q, k, v, g, bias, m, dout = _draw(case, torch.bfloat16, 6)
+    need = max(cross.cross_attn_fwd_workspace_size(q, k), cross.cross_attn_bwd_workspace_size(q, k, True, True))
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    out, lse = torch.empty_like(q), torch.empty(2, 4, 20, device="cuda")
+    grads = [torch.empty_like(t) for t in (q, k, v, g, bias)]
+
+    def fwd(s):
+        cross.cross_attn_fwd(q, k, v, g, bias, m, out=out, lse=lse, workspace=ws, stream=s)
+
+    def bwd(s):
+        cross.cross_attn_bwd(q, k, v, g, bias, m, out, lse, dout, dq=grads[0], dk=grads[1], dv=grads[2], dgate=grads[3],
+                             dbias=grads[4], workspace=ws, stream=s)
+
+    s, cache = torch.cuda.Stream(), gr.GraphCache(capacity=4)
+    for replay in range(4):
+        for t in (q, k, v, g, bias, dout):
+            t.normal_()
+        m.random_(0, 2)
+        ws.random_(0, 255)
+        torch.cuda.synchronize()
+        cache.run(1, fwd, s)
+        cache.run(2, bwd, s)
+        torch.cuda.synchronize()
+        o2, l2 = cross.cross_attn_fwd(q, k, v, g, bias, m)
+        ref = cross.cross_attn_bwd(q, k, v, g, bias, m, o2, l2, dout)
+        torch.cuda.synchronize()
+        assert torch.equal(out, o2) and torch.equal(lse, l2)
+        for a, b in zip(grads, ref):
+            assert torch.equal(a, b)
+
+
+def test_refuses():
+    q, k = torch.zeros(2, 3, 4, 16, device="cuda"), torch.zeros(2, 5, 2, 16, device="cuda")
+    bias, mask = torch.zeros(1, 4, 3, 5, device="cuda"), torch.ones(2, 5, dtype=torch.uint8, device="cuda")
+    bad = [dict(v=k[:, :4]), dict(gate=q[:, :2]), dict(gate=q.bfloat16()), dict(bias=bias[..., :4]), dict(bias=bias.bfloat16()),
+           dict(bias=bias, rows_per_bias=1), dict(rows_per_bias=3), dict(key_mask=mask[:1]), dict(key_mask=mask.float()),
+           dict(key_mask=mask.cpu()), dict(out=q[:, :2]), dict(out=q.bfloat16()), dict(lse=torch.zeros(2, 3, 4, device="cuda")),
+           dict(k=k.cpu(), v=k.cpu())]
+    for kw in bad:
+        a = dict(q=q, k=k, v=k)
+        a.update(kw)
+        with pytest.raises(ValueError):
+            cross.cross_attn_fwd(**a)
+    for kw in (dict(out=q), dict(out=torch.zeros(1, 3, 4, 16, device="cuda").expand(2, 3, 4, 16))):
+        with pytest.raises(ea.EvoAttnError):
+            cross.cross_attn_fwd(q, k, k, **kw)
+    out, lse = cross.cross_attn_fwd(q, k, k)
+    with pytest.raises(ValueError):
+        cross.cross_attn_bwd(q, k, k, None, None, None, out, lse, q, dgate=q)
+    with pytest.raises(ValueError):
+        cross.cross_attn_bwd(q, k, k, None, None, None, out, lse, q, dk=k[:1])
+    with pytest.raises(ea.EvoAttnError):
+        cross.cross_attn_bwd(q, k, k, None, None, None, out, lse, q, dq=q)
+    with pytest.raises(ea.EvoAttnError):
+        cross.cross_attn_bwd(q, k, k, None, None, None, out, lse, q, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
