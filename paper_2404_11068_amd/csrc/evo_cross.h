@@ -202,18 +202,51 @@ __device__ __forceinline__ void load_rows(typename Ty<T>::Frag (&f)[DP / Ty<T>::
     }
 }
 
-// Four consecutive values of a bias row that may start at any element
-__device__ __forceinline__ f32x4 load4(const uint16_t *p) {
+// Four consecutive values of a row that may start at any element, as bits of floats
+__device__ __forceinline__ u32x4 load4(const uint16_t *p) {
     uint32_t w[2];
     __builtin_memcpy(w, p, 8);
-    return f32x4{__uint_as_float(w[0] << 16), __uint_as_float(w[0] & 0xffff0000u), __uint_as_float(w[1] << 16),
-                 __uint_as_float(w[1] & 0xffff0000u)};
+    return u32x4{w[0] << 16, w[0] & 0xffff0000u, w[1] << 16, w[1] & 0xffff0000u};
 }
-__device__ __forceinline__ f32x4 load4(const float *p) {
-    f32x4 x;
+__device__ __forceinline__ u32x4 load4(const float *p) {
+    u32x4 x;
     __builtin_memcpy(&x, p, 16);
     return x;
 }
+
+// The lane's bias row: its values for the 16 keys of a block that its registers
+// hold.  A block is read in fours of keys; where it ends behind the row, that is
+// the next row's beginning, which does not count, and only where it ends behind
+// the tensor single values are read.
+template <typename T> struct BiasRow {
+    using E = typename Ty<T>::E;
+    const E *row;
+    int room;  // values from the row's start to the tensor's end
+    __device__ __forceinline__ BiasRow(const CrArgs &a, int64_t r) {
+        const int64_t left = (a.N / a.rpb * a.H * a.Lq - r) * a.Lk;
+        row = (const E *)a.bias + r * a.Lk;
+        room = left < 0x7fffffff ? (int)left : 0x7fffffff;
+    }
+    // k0: the block's first key; bits: its kept keys from 4 h on.  What is not kept is 0.
+    __device__ __forceinline__ void get(float (&out)[16], int k0, int h, uint32_t bits, bool whole) const {
+        u32x4 w[4];
+        if (__all(k0 + 32 <= room)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = load4(row + k0 + 8 * i + 4 * h);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const bool keep = (bits >> (8 * (i / 4) + i % 4)) & 1;
+                w[i / 4][i % 4] = __float_as_uint(Ty<T>::f(row[keep ? k0 + 8 * (i / 4) + 4 * h + i % 4 : 0]));
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const bool keep = whole || ((bits >> (8 * (i / 4) + i % 4)) & 1);
+            out[i] = __uint_as_float(keep ? w[i / 4][i % 4] : 0u);
+        }
+    }
+};
 #endif
 
 }  // namespace evo

@@ -147,16 +147,29 @@ __global__ __launch_bounds__(kThreads, (KeysShape<T, DP>::WAVES)) void cross_key
         for (int b = 0; b < S::XT / 32; ++b) {
             f32x16 s = zero16(), dp = zero16();
             const int off = (32 * b + (lane & 31)) * S::STR + Y::KS / 2 * h;
+            float add[16];
+            if (BIAS) {
+                // the 32 keys of a query's row are neighbours
+                const int xb = x0 + 32 * b;
+                if (a.G == 1 && xb + 32 <= a.M) {
+                    const E *p = bias + (int64_t)(xb + 4 * h) * a.Lk;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) add[i] = Y::f(p[(int64_t)(8 * (i / 4) + i % 4) * a.Lk], keep);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int x = min(xb + 8 * (i / 4) + 4 * h + i % 4, a.M - 1), t = token_of(a, x);
+                        add[i] = Y::f(bias[((int64_t)(x - t * a.G) * a.Lq + t) * a.Lk], keep);
+                    }
+                }
+            }
 #pragma unroll
             for (int kk = 0; kk < NK; ++kk) Y::mma(s, Y::row(qt + off + Y::KS * kk), kf[kk]);
 #pragma unroll
             for (int kk = 0; kk < NK; ++kk) Y::mma(dp, Y::row(at + off + Y::KS * kk), vf[kk]);
             if (BIAS) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int x = min(x0 + 32 * b + 8 * (i / 4) + 4 * h + i % 4, a.M - 1), t = token_of(a, x);
-                    s[i] = fmaf(s[i], a.scale, Y::f(bias[((int64_t)(x - t * a.G) * a.Lq + t) * a.Lk], keep));
-                }
+                for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], a.scale, add[i]);
             }
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
@@ -247,7 +260,7 @@ __global__ __launch_bounds__(kThreads, (RowsShape<T, DP>::WAVES)) void cross_row
     if (!on || lse == -__builtin_inff()) lse = __builtin_inff();
     const float dsum = a.dsum[(int64_t)unit * a.M + xc];
     const float to2 = a.scale * kLog2e, shift = -lse * kLog2e;
-    const E *brow = BIAS ? (const E *)a.bias + ((n / a.rpb * a.H + head) * a.Lq + t) * (int64_t)a.Lk : nullptr;
+    const BiasRow<T> brow(a, BIAS ? (n / a.rpb * a.H + head) * a.Lq + t : 0);
 
     const E *kbase = (const E *)a.k + n * a.k_row + (int64_t)hk * a.D;
     const E *vbase = (const E *)a.v + n * a.k_row + (int64_t)hk * a.D;
@@ -259,18 +272,18 @@ __global__ __launch_bounds__(kThreads, (RowsShape<T, DP>::WAVES)) void cross_row
     using Bits = KeyBits<S::KT>;
     Bits now, next;
     Stage<T, DP, S::KT, kThreads> ks, vs;
-    auto request = [&](int step, const Bits &bits) {
+    auto request = [&](int step, auto keep) {
         const int64_t off = (int64_t)step * S::KT * a.k_tok;
-        auto keep = [&](int r) { return bits.get(r); };
         ks.load(kbase, a.D, tid, [&](int r) { return kbase + off + (int64_t)r * a.k_tok; }, keep);
         vs.load(vbase, a.D, tid, [&](int r) { return vbase + off + (int64_t)r * a.k_tok; }, keep);
     };
     typename Bits::Bytes bytes;
     const int t0 = split * a.per_split, t1 = min(t0 + a.per_split, a.ntiles);
     if (t0 < t1) {
-        next.set(Bits::request(mrow, t0 * S::KT, a.Lk, lane));
-        request(t0, next);
+        const auto first = Bits::request(mrow, t0 * S::KT, a.Lk, lane);
+        request(t0, [&](int r) { return t0 * S::KT + r < a.Lk; });
         bytes = Bits::request(mrow, (t0 + 1) * S::KT, a.Lk, lane);
+        next.set(first);
     }
     for (int step = t0; step < t1; ++step) {
         E *kt = tiles[step & 1][0], *vt = tiles[step & 1][1];
@@ -280,42 +293,29 @@ __global__ __launch_bounds__(kThreads, (RowsShape<T, DP>::WAVES)) void cross_row
         __syncthreads();
         if (step + 1 < t1) {
             next.set(bytes);
-            request(step + 1, next);
+            request(step + 1, [&](int r) { return next.get(r); });
             bytes = Bits::request(mrow, (step + 2) * S::KT, a.Lk, lane);
         }
         if (!now.any()) continue;
 #pragma unroll
         for (int b = 0; b < S::KT / 32; ++b) {
+            const uint32_t bits = now.sub(b), mine = bits >> (4 * h);
+            if (bits == 0) continue;
+            const bool whole = bits == 0xffffffffu;
             f32x16 s = zero16(), dp = zero16();
             const int off = (32 * b + (lane & 31)) * S::STR + Y::KS / 2 * h;
+            float add[16];
+            if (BIAS) brow.get(add, step * S::KT + 32 * b, h, mine, whole);
 #pragma unroll
             for (int kk = 0; kk < NK; ++kk) Y::mma(s, Y::row(kt + off + Y::KS * kk), qf[kk]);
 #pragma unroll
             for (int kk = 0; kk < NK; ++kk) Y::mma(dp, Y::row(vt + off + Y::KS * kk), af[kk]);
-            const uint32_t bits = now.sub(b);
-            const int k0 = step * S::KT + 32 * b + 4 * h;
-            if (bits == 0xffffffffu) {
 #pragma unroll
-                for (int i = 0; i < 16; i += 4) {
-                    f32x4 add = {0, 0, 0, 0};
-                    if (BIAS) add = load4(brow + k0 + 2 * i);
+            for (int i = 0; i < 16; ++i)
+                s[i] = __builtin_amdgcn_exp2f(BIAS ? (fmaf(s[i], a.scale, add[i]) - lse) * kLog2e : fmaf(s[i], to2, shift));
+            if (!whole) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        s[i + e] = __builtin_amdgcn_exp2f(BIAS ? (fmaf(s[i + e], a.scale, add[e]) - lse) * kLog2e
-                                                               : fmaf(s[i + e], to2, shift));
-                }
-            } else {
-                const uint32_t mine = bits >> (4 * h);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const bool keep = (mine >> (8 * (i / 4) + i % 4)) & 1;
-                    float y;
-                    if (BIAS)
-                        y = (fmaf(s[i], a.scale, Y::f(brow[keep ? k0 + 8 * (i / 4) + i % 4 : 0], keep)) - lse) * kLog2e;
-                    else
-                        y = fmaf(s[i], to2, shift);
-                    s[i] = keep ? __builtin_amdgcn_exp2f(y) : 0.0f;
-                }
+                for (int i = 0; i < 16; ++i) s[i] = (mine >> (8 * (i / 4) + i % 4)) & 1 ? s[i] : 0.0f;
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i) dp[i] = s[i] * (dp[i] - dsum);

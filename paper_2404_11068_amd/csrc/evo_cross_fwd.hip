@@ -62,7 +62,20 @@ __global__ __launch_bounds__(kThreads, (Lds<T, DP, FEW>::SIZE <= 80 * 1024 ? 2 :
     const int xc = on ? x : a.M - 1, t = token_of(a, xc), head = hk * a.G + (xc - t * a.G);
     Frag qf[NK];
     load_rows<T, DP>(qf, (const E *)a.q + n * a.q_row + (int64_t)t * a.q_tok + (int64_t)head * a.D, a.D, on, h);
-    const E *brow = BIAS ? (const E *)a.bias + ((n / a.rpb * a.H + head) * a.Lq + t) * (int64_t)a.Lk : nullptr;
+    const BiasRow<T> brow(a, BIAS ? (n / a.rpb * a.H + head) * a.Lq + t : 0);
+    constexpr bool EARLY = DP <= 64;  // the gate's values wait in registers where there is room
+    const E *grow = a.gate ? (const E *)a.gate + n * a.q_row + (int64_t)t * a.q_tok + (int64_t)head * a.D : nullptr;
+    u32x4 gv[EARLY ? DT * 4 : 1];
+    auto gate_at = [&](int d, int i) {
+        const int c = 32 * d + 8 * i + 4 * h;
+        return load4(grow + (c < a.D ? c : 0));
+    };
+    if (EARLY && grow) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) gv[EARLY ? d * 4 + i : 0] = gate_at(d, i);
+    }
 
     const E *kbase = (const E *)a.k + n * a.k_row + (int64_t)hk * a.D;
     const E *vbase = (const E *)a.v + n * a.k_row + (int64_t)hk * a.D;
@@ -79,17 +92,18 @@ __global__ __launch_bounds__(kThreads, (Lds<T, DP, FEW>::SIZE <= 80 * 1024 ? 2 :
     using Bits = KeyBits<S::KT>;
     Bits now, next;
     Stage<T, DP, S::KT, kThreads> ks, vs;
-    auto request = [&](int step, const Bits &bits) {
+    auto request = [&](int step, auto keep) {
         const int64_t off = (int64_t)step * S::KT * a.k_tok;
-        auto keep = [&](int r) { return bits.get(r); };
         ks.load(kbase, a.D, tid, [&](int r) { return kbase + off + (int64_t)r * a.k_tok; }, keep);
         vs.load(vbase, a.D, tid, [&](int r) { return vbase + off + (int64_t)r * a.k_tok; }, keep);
     };
     typename Bits::Bytes bytes;
     if (t0 < t1) {
-        next.set(Bits::request(mrow, t0 * S::KT, a.Lk, lane));
-        request(t0, next);
+        // the first tile does not wait for its mask; of later ones masked keys are not read
+        const auto first = Bits::request(mrow, t0 * S::KT, a.Lk, lane);
+        request(t0, [&](int r) { return t0 * S::KT + r < a.Lk; });
         bytes = Bits::request(mrow, (t0 + 1) * S::KT, a.Lk, lane);
+        next.set(first);
     }
     for (int step = t0; step < t1; ++step) {
         E *kt = (E *)lds + (L::BUFS == 2 ? (step & 1) * 2 * L::TILE : 0), *vt = kt + L::TILE;
@@ -99,7 +113,7 @@ __global__ __launch_bounds__(kThreads, (Lds<T, DP, FEW>::SIZE <= 80 * 1024 ? 2 :
         __syncthreads();
         if (step + 1 < t1) {
             next.set(bytes);
-            request(step + 1, next);
+            request(step + 1, [&](int r) { return next.get(r); });
             bytes = Bits::request(mrow, (step + 2) * S::KT, a.Lk, lane);
         }
         if (now.any()) {
@@ -108,30 +122,22 @@ __global__ __launch_bounds__(kThreads, (Lds<T, DP, FEW>::SIZE <= 80 * 1024 ? 2 :
             float top = -__builtin_inff();
 #pragma unroll
             for (int b = 0; b < S::NS; ++b) {
+                const uint32_t bits = now.sub(sub0 + b), mine = bits >> (4 * h);
+                if (bits == 0) continue;
                 s[b] = zero16();
                 const E *row = kt + ((sub0 + b) * 32 + (lane & 31)) * L::STR + Y::KS / 2 * h;
+                const bool whole = bits == 0xffffffffu;
+                float add[16];
+                if (BIAS) brow.get(add, step * S::KT + (sub0 + b) * 32, h, mine, whole);
 #pragma unroll
                 for (int kk = 0; kk < NK; ++kk) Y::mma(s[b], Y::row(row + Y::KS * kk), qf[kk]);
-                const uint32_t bits = now.sub(sub0 + b);
-                const int k0 = step * S::KT + (sub0 + b) * 32 + 4 * h;
-                if (bits == 0xffffffffu) {
-                    if (BIAS) {
+                if (BIAS) {
 #pragma unroll
-                        for (int i = 0; i < 16; i += 4) {
-                            const f32x4 add = load4(brow + k0 + 2 * i);
+                    for (int i = 0; i < 16; ++i) s[b][i] = fmaf(s[b][i], a.scale, add[i]);
+                }
+                if (!whole) {
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) s[b][i + e] = fmaf(s[b][i + e], a.scale, add[e]);
-                        }
-                    }
-                } else {
-                    const uint32_t mine = bits >> (4 * h);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const bool keep = (mine >> (8 * (i / 4) + i % 4)) & 1;
-                        float y = s[b][i];
-                        if (BIAS) y = fmaf(y, a.scale, Y::f(brow[keep ? k0 + 8 * (i / 4) + i % 4 : 0], keep));
-                        s[b][i] = keep ? y : -__builtin_inff();
-                    }
+                    for (int i = 0; i < 16; ++i) s[b][i] = (mine >> (8 * (i / 4) + i % 4)) & 1 ? s[b][i] : -__builtin_inff();
                 }
 #pragma unroll
                 for (int i = 0; i < 16; i += 2) top = fmaxf(fmaxf(top, s[b][i]), s[b][i + 1]);
@@ -152,6 +158,7 @@ __global__ __launch_bounds__(kThreads, (Lds<T, DP, FEW>::SIZE <= 80 * 1024 ? 2 :
             const float base = m > -__builtin_inff() ? m : 0.0f, shift = -base * to2;
 #pragma unroll
             for (int b = 0; b < S::NS; ++b) {
+                if (now.sub(sub0 + b) == 0) continue;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     // with a bias the difference comes first: a bias of the type's lowest value times log2 e would be infinite
@@ -229,7 +236,6 @@ __global__ __launch_bounds__(kThreads, (Lds<T, DP, FEW>::SIZE <= 80 * 1024 ? 2 :
     if (kw == 0 && h == 0)
         a.lse[(n * a.H + head) * a.Lq + t] = sum == 0.0f ? -__builtin_inff() : fmaf(__builtin_amdgcn_logf(sum), kLn2, BIAS ? m : m * a.scale);
     E *orow = (E *)a.out + n * a.o_row + (int64_t)t * a.o_tok + (int64_t)head * a.D;
-    const E *grow = a.gate ? (const E *)a.gate + n * a.q_row + (int64_t)t * a.q_tok + (int64_t)head * a.D : nullptr;
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
         if (S::KW > 1 && d % S::KW != kw) continue;
@@ -240,7 +246,7 @@ __global__ __launch_bounds__(kThreads, (Lds<T, DP, FEW>::SIZE <= 80 * 1024 ? 2 :
             E e[4];
             f32x4 g = {1.0f, 1.0f, 1.0f, 1.0f};
             if (grow) {
-                g = load4(grow + c);
+                g = __builtin_bit_cast(f32x4, EARLY ? gv[EARLY ? d * 4 + i / 4 : 0] : gate_at(d, i / 4));
 #pragma unroll
                 for (int j = 0; j < 4; ++j) g[j] = 1.0f / (1.0f + __builtin_amdgcn_exp2f(-g[j] * kLog2e));
             }

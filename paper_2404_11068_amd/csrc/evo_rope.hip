@@ -261,22 +261,24 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(KArgs k) {
     rope_body<E, P, NORM, BWD>(k, angles, line);
 }
 
-// dw = sum of the workgroups' parts in fp64: 16 columns a workgroup, 16 threads each
-__global__ __launch_bounds__(256) void rope_dw_kernel(const float *part0, int n0, float *dw0, const float *part1, int n1,
-                                                      float *dw1, int d) {
-    __shared__ double sums[256];
+// dw = sum of the workgroups' parts in fp64: 16 columns a workgroup, 64 threads each
+__global__ __launch_bounds__(1024) void rope_dw_kernel(const float *part0, int n0, float *dw0, const float *part1, int n1,
+                                                       float *dw1, int d) {
+    __shared__ double sums[1024];
     const float *part = blockIdx.y ? part1 : part0;
     float *dw = blockIdx.y ? dw1 : dw0;
     const int n = blockIdx.y ? n1 : n0;
     if (!dw) return;
     const int col = blockIdx.x * 16 + (threadIdx.x & 15), r0 = threadIdx.x >> 4;
     double sum = 0.0;
-    if (col < d)
-        for (int r = r0; r < n; r += 16) sum += (double)part[(int64_t)r * d + col];
+    if (col < d) {
+#pragma unroll 8
+        for (int r = r0; r < n; r += 64) sum += (double)part[(int64_t)r * d + col];
+    }
     sums[threadIdx.x] = sum;
     __syncthreads();
     if (threadIdx.x < 16 && col < d) {
-        for (int i = 1; i < 16; ++i) sum += sums[threadIdx.x + 16 * i];
+        for (int i = 1; i < 64; ++i) sum += sums[threadIdx.x + 16 * i];
         dw[col] = (float)sum;
     }
 }
@@ -285,7 +287,7 @@ __global__ __launch_bounds__(256) void rope_dw_kernel(const float *part0, int n0
 void plan(const RopeArgs &a, bool bwd, KArgs *k) {
     const int64_t all = a.set[0].tokens + a.set[1].tokens;
     int tb = 1;
-    while (tb < kMaxTok && all / (2 * tb) >= 1024) tb *= 2;
+    while (tb < kMaxTok && all / (2 * tb) >= 2048) tb *= 2;
     k->tb = tb;
     const int chunks = a.d / (a.bf16 ? 8 : 4);
     k->gs_log = 0;
@@ -342,7 +344,7 @@ hipError_t launch_rope_bwd(const RopeArgs &a, void *ws, hipStream_t s) {
     k.part = (float *)ws;
     hipError_t e = launch_all<true>(k, s);
     if (e != hipSuccess || !(a.set[0].dw || a.set[1].dw)) return e;
-    rope_dw_kernel<<<dim3((a.d + 15) / 16, 2), 256, 0, s>>>(k.part, (int)k.blocks[0], a.set[0].dw,
+    rope_dw_kernel<<<dim3((a.d + 15) / 16, 2), 1024, 0, s>>>(k.part, (int)k.blocks[0], a.set[0].dw,
                                                          k.part + (int64_t)k.blocks[0] * a.d, (int)k.blocks[1],
                                                          a.set[1].dw, a.d);
     return hipGetLastError();
