@@ -20,7 +20,7 @@ SOURCES = ["evo_fwd.hip", "evo_bwd.hip", "evo_bwd_qbias.hip", "evo_bwd_fused.hip
            "evo_proj_bwd.hip", "evo_pair_bias_bwd.hip", "evo_relpos.hip", "evo_muon.hip",
            "evo_probe.hip", "evo_api.cpp", "evo_ln_api.cpp", "evo_proj_api.cpp", "evo_optim_api.cpp",
            "evo_relpos_api.cpp", "evo_muon_api.cpp", "evo_rope.hip", "evo_rope_api.cpp",
-           "evo_cross_fwd.hip", "evo_cross_bwd.hip", "evo_cross_api.cpp", "evo_graph.cpp"]
+           "evo_cross_fwd.hip", "evo_cross_short.hip", "evo_cross_bwd.hip", "evo_cross_api.cpp", "evo_graph.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

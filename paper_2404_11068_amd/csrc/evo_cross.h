@@ -41,17 +41,17 @@ struct CrArgs {
 struct CrPlan {
     int fwd_splits, kv_splits, q_splits, bias_chunks;
     bool few;  // forward: a workgroup's waves share its rows and take turns with the keys
+    bool brief;       // forward: all keys at once, workgroups walk over the rows of the batch
+    int brief_chunks; // of the rows of a bias plane
+    bool brief_one;   // a wave a row of the batch, not a workgroup
     size_t fwd_part, fwd_ml, fwd_total;
     size_t bwd_da, bwd_part, bwd_total;
 };
 CrPlan cross_plan(const CrArgs &a, bool has_gate, bool has_bias);
 
 hipError_t launch_cross_fwd(CrArgs a, const CrPlan &p, void *ws, hipStream_t s);
+hipError_t launch_cross_short(CrArgs a, const CrPlan &p, hipStream_t s);
 hipError_t launch_cross_bwd(CrArgs a, const CrPlan &p, void *ws, hipStream_t s);
-// sums the fp32 partials [splits][unit][len][D] into out (strides; G heads per unit row as in x)
-hipError_t launch_cross_sum(const CrArgs &a, const float *part, int splits, int64_t units, int len, int group,
-                            void *out, int64_t row, int64_t tok, hipStream_t s);
-
 #if defined(__HIPCC__)
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // A query whose largest logit with its bias is below this has no key left: a
@@ -66,26 +66,21 @@ template <> struct Ty<bf16_t> {
     using Frag = bf16x8;
     static constexpr int VEC = 8;   // elements per 16 bytes
     static constexpr int KS = 16;   // contraction of one product
-    static constexpr int PAD = 16;  // of an LDS row: 8 lanes' 16-byte reads of 8 rows, and 4 rows of a transposed read, touch each bank once
-    __device__ __forceinline__ static Frag row(const E *p) { return *reinterpret_cast<const bf16x8 *>(p); }
     __device__ __forceinline__ static void mma(f32x16 &acc, const Frag &a, const Frag &b) {
         acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, acc, 0, 0, 0);
-    }
-    // operand whose row is column c0 + lane % 32 of the tile, contraction rows r0 + 8 (e / 4) + 4 h + e % 4
-    __device__ __forceinline__ static Frag col(const E *tile, int stride, int r0, int c0, int lane) {
-        const int i = lane & 15, g = lane >> 4;
-        const E *src = tile + (r0 + 4 * (g >> 1) + (i >> 2)) * stride + c0 + 16 * (g & 1) + 4 * (i & 3);
-        const short4tr lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4tr *)(src));
-        const short4tr hi =
-            __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4tr *)(src + 8 * stride));
-        const short8tr both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-        return __builtin_bit_cast(bf16x8, both);
     }
     __device__ __forceinline__ static Frag pack(const f32x16 &p, int s) {
         Frag f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) f[e] = (__bf16)p[8 * s + e];
         return f;
+    }
+    // times 2^by, exact
+    __device__ __forceinline__ static Frag scaled(const Frag &f, int by) {
+        Frag o;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = (__bf16)ldexpf((float)f[e], by);
+        return o;
     }
     __device__ __forceinline__ static float f(E x) { return bf2f(x); }
     // x where it counts: the choice is made on the bits, before any arithmetic sees what lies there
@@ -96,22 +91,73 @@ template <> struct Ty<bf16_t> {
 template <> struct Ty<float> {
     using E = float;
     using Frag = f32x4;
-    static constexpr int VEC = 4, KS = 8, PAD = 4;
-    __device__ __forceinline__ static Frag row(const E *p) { return *reinterpret_cast<const f32x4 *>(p); }
+    static constexpr int VEC = 4, KS = 8;
     __device__ __forceinline__ static void mma(f32x16 &acc, const Frag &a, const Frag &b) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], acc, 0, 0, 0);
     }
-    __device__ __forceinline__ static Frag col(const E *tile, int stride, int r0, int c0, int lane) {
-        const E *src = tile + (r0 + 4 * (lane >> 5)) * stride + c0 + (lane & 31);
-        return Frag{src[0], src[stride], src[2 * stride], src[3 * stride]};
-    }
     __device__ __forceinline__ static Frag pack(const f32x16 &p, int s) {
         return Frag{p[4 * s], p[4 * s + 1], p[4 * s + 2], p[4 * s + 3]};
+    }
+    __device__ __forceinline__ static Frag scaled(const Frag &f, int by) {
+        return Frag{ldexpf(f[0], by), ldexpf(f[1], by), ldexpf(f[2], by), ldexpf(f[3], by)};
     }
     __device__ __forceinline__ static float f(E x) { return x; }
     __device__ __forceinline__ static float f(E x, bool keep) { return __uint_as_float(keep ? __float_as_uint(x) : 0u); }
     __device__ __forceinline__ static E e(float x) { return x; }
+};
+
+// A tile of rows of DP channels in LDS, and the two ways it becomes an operand:
+//   row(tile, r, kk, h): row r, channels KS kk + KS / 2 h and on
+//   col(tile, r0, c0, lane): column c0 + lane % 32, rows r0 + 8 (e / 4) + 4 h + e % 4,
+//     the order in which a product's registers hold its rows
+template <typename T, int DP> struct Tile;
+
+// The 16-byte chunk k of row r sits at chunk k ^ f(r), so that of 64 four-byte banks 16 lanes reading one
+// chunk of 16 rows, 16 lanes writing neighbouring chunks, and 32 lanes of bf16's transposing read (64 bytes
+// of four rows) each touch every one once.  Padded rows can have one of the first and the last only (and
+// cannot be copied to without registers): at 32 bytes of padding conflicts took 40% of the LDS cycles of
+// the forward at 128 channels.
+template <int DP> struct Tile<bf16_t, DP> {
+    using E = uint16_t;
+    static constexpr int CH = DP / 8;
+    __device__ __forceinline__ static int f(int r) {
+        const int low = (r >> 2) & 3;
+        return DP == 32 ? low : DP == 64 ? ((r >> 1) & 1) << 2 | low : (r & 3) << 2 | low;
+    }
+    __device__ __forceinline__ static int at(int r, int chunk) { return r * DP + ((chunk ^ f(r)) << 3); }
+    __device__ __forceinline__ static bf16x8 row(const E *tile, int r, int kk, int h) {
+        return *reinterpret_cast<const bf16x8 *>(tile + at(r, 2 * kk + h));
+    }
+    __device__ __forceinline__ static bf16x8 col(const E *tile, int r0, int c0, int lane) {
+        const int i = lane & 15, g = lane >> 4;
+        const int r = 4 * (g >> 1) + (i >> 2), chunk = (c0 >> 3) + 2 * (g & 1) + ((i & 3) >> 1), low = 4 * (i & 1);
+        const E *lo_at = tile + r0 * DP + at(r, chunk) + low, *hi_at = tile + r0 * DP + at(r + 8, chunk) + low;
+        const short4tr lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4tr *)(lo_at));
+        const short4tr hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4tr *)(hi_at));
+        const short8tr both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        return __builtin_bit_cast(bf16x8, both);
+    }
+};
+
+// fp32: a column is read by 4-byte reads, 32 lanes a row and the two lane halves four rows apart; f is the
+// same for four rows, whose reads differ by a constant then.  Rows are read with conflicts, once for 256
+// cycles of matrix instructions.
+template <int DP> struct Tile<float, DP> {
+    using E = float;
+    static constexpr int CH = DP / 4;
+    __device__ __forceinline__ static int f(int r) {
+        return DP == 32 ? ((r >> 2) & 3) << 1 : ((r >> 2) & 1) << 3 | ((r >> 3) & 1) << 1;
+    }
+    __device__ __forceinline__ static int at(int r, int chunk) { return r * DP + ((chunk ^ f(r)) << 2); }
+    __device__ __forceinline__ static f32x4 row(const E *tile, int r, int kk, int h) {
+        return *reinterpret_cast<const f32x4 *>(tile + at(r, 2 * kk + h));
+    }
+    __device__ __forceinline__ static f32x4 col(const E *tile, int r0, int c0, int lane) {
+        const int c = c0 + (lane & 31);
+        const E *src = tile + at(r0 + 4 * (lane >> 5), c >> 2) + (c & 3);
+        return f32x4{src[0], src[DP], src[2 * DP], src[3 * DP]};
+    }
 };
 
 // combined over the lane halves (lanes l and l + 32 hold parts of one column)
@@ -154,6 +200,10 @@ template <int KT> struct KeyBits {
         for (int j = 1; j < W; ++j) o |= w[j];
         return o != 0;
     }
+    __device__ __forceinline__ bool all() const {
+        static_assert(KT == 32 || KT == 64, "one word");
+        return w[0] == (KT == 64 ? ~0ull : 0xffffffffull);
+    }
     __device__ __forceinline__ bool get(int r) const {
         if (W == 1) return (w[0] >> r) & 1;
         return ((r < 64 ? w[0] : w[W - 1]) >> (r & 63)) & 1;
@@ -161,13 +211,50 @@ template <int KT> struct KeyBits {
     __device__ __forceinline__ uint32_t sub(int s) const { return (uint32_t)(w[s >> 1] >> (32 * (s & 1))); }
 };
 
+// Narrows the steps [t0, t1) of KT keys to those from the first kept key to the last
+template <int KT, int THREADS>
+__device__ __forceinline__ void kept_range(const uint8_t *mask_row, int Lk, int tid, int *lds, int &t0, int &t1) {
+    const int end = min(t1 * KT, Lk);
+    int lo = 0x7fffffff, hi = -1;
+    for (int k = t0 * KT + tid * 16; k < end; k += THREADS * 16) {
+        uint32_t any = 0;
+        if (k + 16 <= end) {
+            u32x4 w;
+            __builtin_memcpy(&w, mask_row + k, 16);
+            any = w[0] | w[1] | w[2] | w[3];
+        } else {
+            for (int i = k; i < end; ++i) any |= mask_row[i];
+        }
+        // 16 keys from a multiple of 16 on lie in one step
+        if (any) {
+            lo = min(lo, k);
+            hi = k;
+        }
+    }
+    for (int m = 1; m < 64; m <<= 1) {
+        lo = min(lo, __shfl_xor(lo, m, 64));
+        hi = max(hi, __shfl_xor(hi, m, 64));
+    }
+    if ((tid & 63) == 0) lds[2 * (tid >> 6)] = lo, lds[2 * (tid >> 6) + 1] = hi;
+    __syncthreads();
+    for (int w = 0; w < THREADS / 64; ++w) {
+        lo = min(lo, lds[2 * w]);
+        hi = max(hi, lds[2 * w + 1]);
+    }
+    __syncthreads();
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    hi = __builtin_amdgcn_readfirstlane(hi);
+    t1 = hi < 0 ? t0 : hi / KT + 1;
+    if (hi >= 0) t0 = lo / KT;
+}
+
 // A tile of ROWS tokens of DP channels on its way from memory to LDS, 16 bytes
 // a thread at a time.  Rows and channels that are not there are read from a
 // valid address and written as zeros (NaN or infinity in a masked place stays
 // outside of every product).
 template <typename T, int DP, int ROWS, int THREADS> struct Stage {
     using E = typename Ty<T>::E;
-    static constexpr int CPR = DP / Ty<T>::VEC, N = ROWS * CPR / THREADS, STR = DP + Ty<T>::PAD;
+    static constexpr int CPR = DP / Ty<T>::VEC, N = ROWS * CPR / THREADS;
     static_assert(ROWS * CPR % THREADS == 0, "whole chunks");
     u32x4 v[N];
     template <class Row, class Keep>
@@ -184,7 +271,35 @@ template <typename T, int DP, int ROWS, int THREADS> struct Stage {
         for (int i = 0; i < N; ++i) {
             const int at = tid + THREADS * i, r = at / CPR, c = at % CPR * Ty<T>::VEC;
             const u32x4 z = {0, 0, 0, 0};
-            *reinterpret_cast<u32x4 *>(tile + r * STR + c) = keep(r) && c < D ? v[i] : z;
+            *reinterpret_cast<u32x4 *>(tile + Tile<T, DP>::at(r, at % CPR)) = keep(r) && c < D ? v[i] : z;
+        }
+    }
+};
+
+// The same without registers in between: global_load_lds, 16 bytes a lane.  The
+// copies are counted by hand: copies_done_and_barrier() before a tile is read.
+// (The compiler does not see them; its own waits on vector memory count in order
+// and only get longer by them.)
+static __device__ const u32x4 kZeros[1] = {};  // what is not there is copied from here
+__device__ __forceinline__ void copy16(const void *from, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds), "v"(from) : "memory");
+}
+__device__ __forceinline__ void copies_done_and_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
+
+template <typename T, int DP, int ROWS, int THREADS> struct Copy {
+    using E = typename Ty<T>::E;
+    using L = Tile<T, DP>;
+    static constexpr int N = ROWS * L::CH / THREADS;
+    static_assert(ROWS * L::CH % THREADS == 0, "whole chunks");
+    template <class Row, class Keep>
+    __device__ __forceinline__ static void run(E *tile, bool whole, int D, int wave, int lane, Row row, Keep keep) {
+        const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)(char *)tile + wave * 1024);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int at = wave * 64 + THREADS * i + lane, r = at / L::CH, c = ((at % L::CH) ^ L::f(r)) * Ty<T>::VEC;
+            const E *p = row(r) + c;
+            if (!whole) p = keep(r) && c < D ? p : (const E *)kZeros;
+            copy16(p, lds + THREADS * i * 16);
         }
     }
 };
@@ -202,21 +317,29 @@ __device__ __forceinline__ void load_rows(typename Ty<T>::Frag (&f)[DP / Ty<T>::
     }
 }
 
-// Four consecutive values of a row that may start at any element, as bits of floats
-__device__ __forceinline__ u32x4 load4(const uint16_t *p) {
+// Four consecutive values of a row that may start at any element
+template <typename E> struct Four;
+template <> struct Four<uint16_t> {
     uint32_t w[2];
-    __builtin_memcpy(w, p, 8);
-    return u32x4{w[0] << 16, w[0] & 0xffff0000u, w[1] << 16, w[1] & 0xffff0000u};
-}
-__device__ __forceinline__ u32x4 load4(const float *p) {
-    u32x4 x;
-    __builtin_memcpy(&x, p, 16);
+    __device__ __forceinline__ uint32_t bits(int i) const { return i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16; }
+    __device__ __forceinline__ void set(int i, uint16_t x) {
+        w[i >> 1] = i & 1 ? (w[i >> 1] & 0xffffu) | (uint32_t)x << 16 : x;
+    }
+};
+template <> struct Four<float> {
+    uint32_t w[4];
+    __device__ __forceinline__ uint32_t bits(int i) const { return w[i]; }
+    __device__ __forceinline__ void set(int i, float x) { w[i] = __float_as_uint(x); }
+};
+template <typename E> __device__ __forceinline__ Four<E> load4(const E *p) {
+    Four<E> x;
+    __builtin_memcpy(&x, p, sizeof(x));
     return x;
 }
 
-// The lane's bias row: its values for the 16 keys of a block that its registers
-// hold.  A block is read in fours of keys; where it ends behind the row, that is
-// the next row's beginning, which does not count, and only where it ends behind
+// The lane's bias row: its values for the 32 keys of a block that its registers
+// pair with.  A block is read in fours of keys; where it ends behind the row, that
+// is the next row's beginning, which does not count, and only where it ends behind
 // the tensor single values are read.
 template <typename T> struct BiasRow {
     using E = typename Ty<T>::E;
@@ -227,24 +350,89 @@ template <typename T> struct BiasRow {
         row = (const E *)a.bias + r * a.Lk;
         room = left < 0x7fffffff ? (int)left : 0x7fffffff;
     }
-    // k0: the block's first key; bits: its kept keys from 4 h on.  What is not kept is 0.
-    __device__ __forceinline__ void get(float (&out)[16], int k0, int h, uint32_t bits, bool whole) const {
-        u32x4 w[4];
+    struct Raw { Four<E> x[4]; };
+    __device__ __forceinline__ Raw request(int k0, int h) const {
+        Raw r;
         if (__all(k0 + 32 <= room)) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = load4(row + k0 + 8 * i + 4 * h);
+            for (int i = 0; i < 4; ++i) r.x[i] = load4(row + k0 + 8 * i + 4 * h);
         } else {
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const bool keep = (bits >> (8 * (i / 4) + i % 4)) & 1;
-                w[i / 4][i % 4] = __float_as_uint(Ty<T>::f(row[keep ? k0 + 8 * (i / 4) + 4 * h + i % 4 : 0]));
+                const int key = k0 + 8 * (i / 4) + 4 * h + i % 4;
+                r.x[i / 4].set(i % 4, row[key < room ? key : 0]);
             }
         }
+        return r;
+    }
+    __device__ __forceinline__ static float value(const Raw &r, int i) { return __uint_as_float(r.x[i / 4].bits(i % 4)); }
+};
+
+// x where the key of register i is kept (bits of a block of 32 keys, the same in all lanes), else the
+// float with the bits `other`: one instruction, its lane mask made by scalar ones.  The choice is one of
+// bits, so that whatever x came to from a masked bias does not matter.
+__device__ __forceinline__ float where_kept(uint32_t bits, int i, float x, uint32_t other) {
+    const uint32_t lo = (bits >> (8 * (i / 4) + i % 4)) & 1, hi = (bits >> (8 * (i / 4) + 4 + i % 4)) & 1;
+    const uint64_t lanes = (lo ? 0xffffffffull : 0) | (hi ? 0xffffffff00000000ull : 0);
+    return __uint_as_float(__builtin_amdgcn_inverse_ballot_w64(lanes) ? __float_as_uint(x) : other);
+}
+constexpr uint32_t kMinusInf = 0xff800000u;
+
+__device__ __forceinline__ float sigmoid(float x) {
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-x * kLog2e));  // both to about one step of fp32
+}
+
+// 16 channels of a token, c = 16 j and on, as the registers of a product hold them (x[0]: channels c + 4 h
+// .. c + 4 h + 3, x[1]: c + 8 + 4 h ..), by 16-byte accesses.  In bf16 a lane reads 8 neighbours and the
+// lane halves swap fours.
+template <typename E> struct Sixteen;
+template <> struct Sixteen<uint16_t> {
+    Four<uint16_t> x[2];
+    __device__ __forceinline__ void swap() {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const bool keep = whole || ((bits >> (8 * (i / 4) + i % 4)) & 1);
-            out[i] = __uint_as_float(keep ? w[i / 4][i % 4] : 0u);
+        for (int i = 0; i < 2; ++i) {
+            const auto r = __builtin_amdgcn_permlane32_swap(x[0].w[i], x[1].w[i], false, false);
+            x[0].w[i] = r[0];
+            x[1].w[i] = r[1];
         }
+    }
+    // every lane of the wave takes part; rows that are not there are given a valid address
+    __device__ __forceinline__ void load(const uint16_t *row, int c, int D, int h) {
+        const u32x4 w = *reinterpret_cast<const u32x4 *>(row + (c + 8 * h < D ? c + 8 * h : 0));
+        x[0].w[0] = w[0], x[0].w[1] = w[1], x[1].w[0] = w[2], x[1].w[1] = w[3];
+    }
+    __device__ __forceinline__ void arrange() { swap(); }  // after load: kept apart, so that it does not wait
+    __device__ __forceinline__ void store(uint16_t *row, int c, int D, int h, bool on) {
+        swap();
+        if (on && c + 8 * h < D) *reinterpret_cast<u32x4 *>(row + c + 8 * h) = u32x4{x[0].w[0], x[0].w[1], x[1].w[0], x[1].w[1]};
+    }
+    __device__ __forceinline__ void set(int g, const float *v) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) x[g].w[i] = (uint32_t)f2bf(v[2 * i]) | (uint32_t)f2bf(v[2 * i + 1]) << 16;
+    }
+};
+template <> struct Sixteen<float> {
+    Four<float> x[2];
+    __device__ __forceinline__ void load(const float *row, int c, int D, int h) {
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            const int at = c + 8 * g + 4 * h;
+            const u32x4 w = *reinterpret_cast<const u32x4 *>(row + (at < D ? at : 0));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[g].w[i] = w[i];
+        }
+    }
+    __device__ __forceinline__ void arrange() {}
+    __device__ __forceinline__ void store(float *row, int c, int D, int h, bool on) {
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            const int at = c + 8 * g + 4 * h;
+            if (on && at < D) *reinterpret_cast<u32x4 *>(row + at) = u32x4{x[g].w[0], x[g].w[1], x[g].w[2], x[g].w[3]};
+        }
+    }
+    __device__ __forceinline__ void set(int g, const float *v) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[g].w[i] = __float_as_uint(v[i]);
     }
 };
 #endif

@@ -97,33 +97,73 @@ Range flat(const void *p, int64_t bytes) { return Range{(uintptr_t)p, (uintptr_t
 
 namespace evo {
 
-// How many workgroups walk one axis together: as many as fill `slots` places,
-// and at least two steps each
-static int split(int64_t wgs, int64_t steps, int64_t slots) {
-    if (wgs <= 0 || steps <= 1 || wgs * 2 > slots) return 1;
-    int64_t n = slots / wgs;
-    if (n > steps / 2) n = steps / 2;
-    if (n < 2) return 1;
-    const int64_t per = up(steps, n);
-    return (int)up(steps, per);
+// How many workgroups share one tile's walk of `steps`: the count of the lowest
+// estimated time, in us.  The steps of the fullest CU count (two workgroups on a CU
+// take 1.3 times one's rate), `one` us each, and a join: a launch, and the
+// parts (bytes of one) written and read once.  The rates are those measured at 32, 64 and
+// 128 channels; e.g. 264 tiles of 65 steps at 64 channels: 83 us unsplit, 87, 74, 78, 73, 88
+// with 2, 3, 4, 5 and 8 (estimated 91, 80, 75, 75, 74, 82).
+static int split(int64_t tiles, int64_t steps, double one, double bytes, double launch) {
+    if (tiles <= 0 || steps <= 1) return 1;
+    int best = 1;
+    double least = 0.0;
+    for (int64_t n = 1; n <= steps && n <= 64; ++n) {
+        const int64_t per = up(steps, n), load = up(tiles * n, 256);
+        if (up(steps, per) != n) continue;
+        const double cost = load * per * one / (load > 1 ? 1.3 : 1.0) + (n > 1 ? launch + n * bytes / 2e6 : 0.0);
+        if (n == 1 || cost < least) best = (int)n, least = cost;
+        if (load > 16) break;  // the GPU is full
+    }
+    return best;
 }
 
 CrPlan cross_plan(const CrArgs &a, bool has_gate, bool has_bias) {
     CrPlan p{};
     const int64_t units = a.N * a.Hk;
     const int few_rows = a.bf16 ? 32 : 64;
+    const int64_t key_steps = up(a.Lk, a.bf16 ? 64 : 32);
+    const double rows_bytes = 4.0 * units * a.M * a.D, keys_bytes = 8.0 * units * a.Lk * a.D;
+    // us a step of the forward: 128 queries by 64 keys, fp32 by 32
+    const int d = a.D <= 32 ? 32 : a.D <= 64 ? 64 : 128;
+    const double one = 0.35 + (a.bf16 ? 0.0088 : 0.0155) * d;
     p.few = a.M <= few_rows;
-    const int64_t tiles = up(a.M, p.few ? few_rows : 128), steps = up(a.Lk, p.few ? (a.bf16 ? 128 : 64) : (a.bf16 ? 64 : 32));
-    p.fwd_splits = split(units * tiles, steps, 512);
+    const int64_t tiles = up(a.M, p.few ? few_rows : 128);
+    if (p.few) {
+        // reading K and V is all there is to do: two workgroups a CU, of four steps at least.  16 rows of 4 key
+        // heads to 4097 keys of 128 channels: 64 us unsplit, 41, 26, 24 and 29 with 2, 4, 8 and 12
+        int64_t n = units * tiles > 0 ? 512 / (units * tiles) : 1;
+        if (n > key_steps / 4) n = key_steps / 4;
+        p.fwd_splits = n < 2 ? 1 : (int)up(key_steps, up(key_steps, n));
+    } else {
+        p.fwd_splits = split(units * tiles, key_steps, one, rows_bytes, 5.0);
+    }
+    // few keys: a workgroup (or, for up to 32 queries, a wave) walks over rows of the batch, where there are
+    // enough.  At 8 heads of 32, 256 queries, 77 keys, gate and bias: 128 rows 22 us (36 by a workgroup a
+    // row), 64 rows 14 (21); 65536 rows of one query to 4 keys, 4 heads of 16: 155 (483)
+    if (a.Lk > 0 && a.Lk <= 128) {
+        p.brief_one = a.M <= 32 && units >= 4096 && 16 * up(a.Lk, 32) * 32 * d * (a.bf16 ? 2 : 4) <= 128 * 1024;
+        p.brief = p.brief_one || (a.bf16 && a.D <= 32 && a.M > 32 && units * tiles >= 1024);
+    }
+    if (p.brief) {
+        const int64_t base = a.N / a.rpb * a.Hk * (p.brief_one ? 1 : tiles), most = up(a.rpb, p.brief_one ? 8 : 2);
+        int64_t n = (p.brief_one ? 1024 : 512) / base;
+        n = n < 1 ? 1 : n > most ? most : n;
+        p.brief_chunks = (int)up(a.rpb, up(a.rpb, n));
+        p.fwd_splits = 1;
+    }
     const auto pad = [](size_t x) { return (x + 255) / 256 * 256; };
     if (p.fwd_splits > 1) {
         p.fwd_part = 0;
         p.fwd_ml = pad((size_t)p.fwd_splits * units * a.M * a.D * 4);
         p.fwd_total = p.fwd_ml + pad((size_t)p.fwd_splits * units * a.M * 8);
     }
-    p.kv_splits = split(units * up(a.Lk, 128), up(a.M, a.bf16 && a.D <= 64 ? 64 : 32), 512);
-    p.q_splits = split(units * up(a.M, 128), up(a.Lk, a.bf16 ? 64 : 32), 512);
-    p.bias_chunks = has_bias ? split(a.N / a.rpb * a.H * up(a.Lq, 64) * up(a.Lk, 64), a.rpb, 512) : 1;
+    p.kv_splits = split(units * up(a.Lk, 128), up(a.M, a.bf16 && a.D <= 64 ? 64 : 32), 1.3 * one, keys_bytes, 5.0);
+    p.q_splits = split(units * up(a.M, 128), key_steps, 1.2 * one, rows_bytes, 5.0);
+    p.bias_chunks = 1;
+    if (has_bias) {
+        const int64_t bias_tiles = a.N / a.rpb * a.H * up(a.Lq, 64) * up(a.Lk, 64);
+        p.bias_chunks = split(bias_tiles, a.rpb, 1.2 * one, 4.0 * (a.N / a.rpb) * a.H * a.Lq * (double)a.Lk, 5.0);
+    }
     p.bwd_da = pad((size_t)units * a.M * 4);
     p.bwd_part = p.bwd_da + (has_gate ? pad((size_t)units * a.M * a.D * (a.bf16 ? 2 : 4)) : 0);
     size_t part = 0;

@@ -43,7 +43,7 @@ __global__ __launch_bounds__(kThreads) void cross_prep_kernel(CrArgs a, int gs_l
 #pragma unroll
             for (int e = 0; e < Y::VEC; ++e) {
                 // sigmoid and one minus it, each without cancellation
-                const float x = Y::f(g[e]), z = __builtin_amdgcn_exp2f(-fabsf(x) * kLog2e), r = 1.0f / (1.0f + z);
+                const float x = Y::f(g[e]), z = __builtin_amdgcn_exp2f(-fabsf(x) * kLog2e), r = __builtin_amdgcn_rcpf(1.0f + z);
                 const float sig = x >= 0.0f ? r : z * r, rest = x >= 0.0f ? z * r : r;
                 da[e] = Y::e(Y::f(d[e]) * sig);  // rounded to the type: the operand of two matrix products
                 dg[e] = Y::e(Y::f(d[e]) * Y::f(o[e]) * rest);
@@ -69,7 +69,7 @@ __device__ __forceinline__ DaView da_view(const CrArgs &a) {
 template <typename T, int DP> struct KeysShape {
     static constexpr bool WIDE = sizeof(typename Ty<T>::E) == 4;
     static constexpr int KEYS = 128, XT = WIDE || DP == 128 ? 32 : 64;
-    static constexpr int STR = DP + Ty<T>::PAD, TILE = XT * STR;
+    static constexpr int TILE = XT * DP;
     static constexpr int WAVES = DP == 128 ? 1 : 2;  // per SIMD: the accumulators of 128 channels take half of its registers
 };
 
@@ -78,6 +78,7 @@ __global__ __launch_bounds__(kThreads, (KeysShape<T, DP>::WAVES)) void cross_key
     using Y = Ty<T>;
     using E = typename Y::E;
     using Frag = typename Y::Frag;
+    using LT = Tile<T, DP>;
     using S = KeysShape<T, DP>;
     constexpr int NK = DP / Y::KS, DT = DP / 32;
     __shared__ __attribute__((aligned(16))) E tiles[2][2][S::TILE];
@@ -146,7 +147,7 @@ __global__ __launch_bounds__(kThreads, (KeysShape<T, DP>::WAVES)) void cross_key
 #pragma unroll
         for (int b = 0; b < S::XT / 32; ++b) {
             f32x16 s = zero16(), dp = zero16();
-            const int off = (32 * b + (lane & 31)) * S::STR + Y::KS / 2 * h;
+            const int r = 32 * b + (lane & 31);
             float add[16];
             if (BIAS) {
                 // the 32 keys of a query's row are neighbours
@@ -164,9 +165,9 @@ __global__ __launch_bounds__(kThreads, (KeysShape<T, DP>::WAVES)) void cross_key
                 }
             }
 #pragma unroll
-            for (int kk = 0; kk < NK; ++kk) Y::mma(s, Y::row(qt + off + Y::KS * kk), kf[kk]);
+            for (int kk = 0; kk < NK; ++kk) Y::mma(s, LT::row(qt, r, kk, h), kf[kk]);
 #pragma unroll
-            for (int kk = 0; kk < NK; ++kk) Y::mma(dp, Y::row(at + off + Y::KS * kk), vf[kk]);
+            for (int kk = 0; kk < NK; ++kk) Y::mma(dp, LT::row(at, r, kk, h), vf[kk]);
             if (BIAS) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], a.scale, add[i]);
@@ -186,8 +187,8 @@ __global__ __launch_bounds__(kThreads, (KeysShape<T, DP>::WAVES)) void cross_key
                 const Frag p = Y::pack(s, g), ds = Y::pack(dp, g);
 #pragma unroll
                 for (int d = 0; d < DT; ++d) {
-                    Y::mma(dvv[d], Y::col(at, S::STR, 32 * b + Y::KS * g, 32 * d, lane), p);
-                    Y::mma(dk[d], Y::col(qt, S::STR, 32 * b + Y::KS * g, 32 * d, lane), ds);
+                    Y::mma(dvv[d], LT::col(at, 32 * b + Y::KS * g, 32 * d, lane), p);
+                    Y::mma(dk[d], LT::col(qt, 32 * b + Y::KS * g, 32 * d, lane), ds);
                 }
             }
         }
@@ -226,7 +227,7 @@ __global__ __launch_bounds__(kThreads, (KeysShape<T, DP>::WAVES)) void cross_key
 template <typename T, int DP> struct RowsShape {
     static constexpr bool WIDE = sizeof(typename Ty<T>::E) == 4;
     static constexpr int KT = WIDE ? 32 : 64, ROWS = 128;
-    static constexpr int STR = DP + Ty<T>::PAD, TILE = KT * STR;
+    static constexpr int TILE = KT * DP;
     static constexpr int WAVES = WIDE && DP == 128 ? 1 : 2;
 };
 
@@ -235,6 +236,7 @@ __global__ __launch_bounds__(kThreads, (RowsShape<T, DP>::WAVES)) void cross_row
     using Y = Ty<T>;
     using E = typename Y::E;
     using Frag = typename Y::Frag;
+    using LT = Tile<T, DP>;
     using S = RowsShape<T, DP>;
     constexpr int NK = DP / Y::KS, DT = DP / 32;
     __shared__ __attribute__((aligned(16))) E tiles[2][2][S::TILE];
@@ -299,23 +301,24 @@ __global__ __launch_bounds__(kThreads, (RowsShape<T, DP>::WAVES)) void cross_row
         if (!now.any()) continue;
 #pragma unroll
         for (int b = 0; b < S::KT / 32; ++b) {
-            const uint32_t bits = now.sub(b), mine = bits >> (4 * h);
+            const uint32_t bits = now.sub(b);
             if (bits == 0) continue;
             const bool whole = bits == 0xffffffffu;
             f32x16 s = zero16(), dp = zero16();
-            const int off = (32 * b + (lane & 31)) * S::STR + Y::KS / 2 * h;
-            float add[16];
-            if (BIAS) brow.get(add, step * S::KT + 32 * b, h, mine, whole);
+            const int r = 32 * b + (lane & 31);
+            typename BiasRow<T>::Raw add;
+            if (BIAS) add = brow.request(step * S::KT + 32 * b, h);
 #pragma unroll
-            for (int kk = 0; kk < NK; ++kk) Y::mma(s, Y::row(kt + off + Y::KS * kk), qf[kk]);
+            for (int kk = 0; kk < NK; ++kk) Y::mma(s, LT::row(kt, r, kk, h), qf[kk]);
 #pragma unroll
-            for (int kk = 0; kk < NK; ++kk) Y::mma(dp, Y::row(vt + off + Y::KS * kk), af[kk]);
+            for (int kk = 0; kk < NK; ++kk) Y::mma(dp, LT::row(vt, r, kk, h), af[kk]);
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-                s[i] = __builtin_amdgcn_exp2f(BIAS ? (fmaf(s[i], a.scale, add[i]) - lse) * kLog2e : fmaf(s[i], to2, shift));
+                s[i] = __builtin_amdgcn_exp2f(BIAS ? (fmaf(s[i], a.scale, BiasRow<T>::value(add, i)) - lse) * kLog2e
+                                                   : fmaf(s[i], to2, shift));
             if (!whole) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = (mine >> (8 * (i / 4) + i % 4)) & 1 ? s[i] : 0.0f;
+                for (int i = 0; i < 16; ++i) s[i] = where_kept(bits, i, s[i], 0);
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i) dp[i] = s[i] * (dp[i] - dsum);
@@ -323,7 +326,7 @@ __global__ __launch_bounds__(kThreads, (RowsShape<T, DP>::WAVES)) void cross_row
             for (int g = 0; g < 32 / Y::KS; ++g) {
                 const Frag ds = Y::pack(dp, g);
 #pragma unroll
-                for (int d = 0; d < DT; ++d) Y::mma(dq[d], Y::col(kt, S::STR, 32 * b + Y::KS * g, 32 * d, lane), ds);
+                for (int d = 0; d < DT; ++d) Y::mma(dq[d], LT::col(kt, 32 * b + Y::KS * g, 32 * d, lane), ds);
             }
         }
     }
@@ -355,7 +358,7 @@ __global__ __launch_bounds__(kThreads, (RowsShape<T, DP>::WAVES)) void cross_row
 // bias: dBias.  tiles = 64-query tiles, ntiles = 64-key tiles, splits = chunks of
 // per_split rows of a plane
 template <typename T, int DP> struct BiasShape {
-    static constexpr int STR = DP + Ty<T>::PAD, TILE = 64 * STR;
+    static constexpr int TILE = 64 * DP;
     static constexpr int WAVES = 4 * TILE * (int)sizeof(typename Ty<T>::E) <= 78 * 1024 ? 2 : 1;
 };
 
@@ -363,6 +366,7 @@ template <typename T, int DP>
 __global__ __launch_bounds__(kThreads, (BiasShape<T, DP>::WAVES)) void cross_bias_kernel(CrArgs a) {
     using Y = Ty<T>;
     using E = typename Y::E;
+    using LT = Tile<T, DP>;
     using S = BiasShape<T, DP>;
     constexpr int NK = DP / Y::KS;
     __shared__ __attribute__((aligned(16))) E tiles[4][S::TILE];  // Q, dA, K, V
@@ -428,11 +432,11 @@ __global__ __launch_bounds__(kThreads, (BiasShape<T, DP>::WAVES)) void cross_bia
         if (n + 1 < n1) request(n + 1);
         if (now.any()) {
             f32x16 s = zero16(), dp = zero16();
-            const int qo = (32 * qb + (lane & 31)) * S::STR + Y::KS / 2 * h, ko = (32 * kb + (lane & 31)) * S::STR + Y::KS / 2 * h;
+            const int qr = 32 * qb + (lane & 31), kr = 32 * kb + (lane & 31);
 #pragma unroll
             for (int kk = 0; kk < NK; ++kk) {
-                Y::mma(s, Y::row(tiles[0] + qo + Y::KS * kk), Y::row(tiles[2] + ko + Y::KS * kk));
-                Y::mma(dp, Y::row(tiles[1] + qo + Y::KS * kk), Y::row(tiles[3] + ko + Y::KS * kk));
+                Y::mma(s, LT::row(tiles[0], qr, kk, h), LT::row(tiles[2], kr, kk, h));
+                Y::mma(dp, LT::row(tiles[1], qr, kk, h), LT::row(tiles[3], kr, kk, h));
             }
             const bool mine = now.get(32 * kb + (lane & 31));
 #pragma unroll
@@ -464,16 +468,20 @@ __global__ __launch_bounds__(kThreads, (BiasShape<T, DP>::WAVES)) void cross_bia
 }
 
 // ---------------------------------------------------------------------------
-// Sums of parts: rows of D channels written at (unit, i) -> token and head, or a flat array (D == 0)
+// Sums of parts: rows of D channels written at (unit, i) -> token and head, or a flat array (no row
+// stride).  With a second output its parts follow the first's.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void cross_sum_kernel(CrArgs a, const float *part, int splits, int64_t stride, int64_t count,
-                                                             int len, int group, void *out, int64_t row_stride, int64_t tok_stride) {
+                                                             int len, int group, void *out0, void *out1, int64_t row_stride, int64_t tok_stride) {
     using Y = Ty<T>;
     using E = typename Y::E;
     const int64_t at = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 4;
     if (at >= count) return;
+    void *out = blockIdx.y ? out1 : out0;
+    part += blockIdx.y * count;
     f32x4 sum = {0, 0, 0, 0};
     const bool whole = at + 4 <= count;
+#pragma unroll 4
     for (int j = 0; j < splits; ++j) {
         const float *p = part + j * stride + at;
         if (whole) {
@@ -500,9 +508,9 @@ __global__ __launch_bounds__(kThreads) void cross_sum_kernel(CrArgs a, const flo
 
 template <typename T>
 void sum_parts(const CrArgs &a, const float *part, int splits, int64_t stride, int64_t count, int len, int group, void *out,
-               int64_t row, int64_t tok, hipStream_t s) {
-    const uint32_t grid = (uint32_t)((count + 4 * kThreads - 1) / (4 * kThreads));
-    cross_sum_kernel<T><<<grid, kThreads, 0, s>>>(a, part, splits, stride, count, len, group, out, row, tok);
+               void *more, int64_t row, int64_t tok, hipStream_t s) {
+    const dim3 grid((uint32_t)((count + 4 * kThreads - 1) / (4 * kThreads)), more ? 2 : 1);
+    cross_sum_kernel<T><<<grid, kThreads, 0, s>>>(a, part, splits, stride, count, len, group, out, more, row, tok);
 }
 
 template <typename T, int DP> void run(CrArgs a, const CrPlan &p, hipStream_t s) {
@@ -522,8 +530,7 @@ template <typename T, int DP> void run(CrArgs a, const CrPlan &p, hipStream_t s)
             cross_keys_kernel<T, DP, false><<<grid, kThreads, 0, s>>>(k);
         if (k.splits > 1) {
             const int64_t count = units * a.Lk * a.D;
-            sum_parts<T>(a, a.part, k.splits, 2 * count, count, a.Lk, 0, a.dk, a.k_row, a.k_tok, s);
-            sum_parts<T>(a, a.part + count, k.splits, 2 * count, count, a.Lk, 0, a.dv, a.k_row, a.k_tok, s);
+            sum_parts<T>(a, a.part, k.splits, 2 * count, count, a.Lk, 0, a.dk, a.dv, a.k_row, a.k_tok, s);
         }
     }
     if (a.M > 0) {
@@ -540,7 +547,7 @@ template <typename T, int DP> void run(CrArgs a, const CrPlan &p, hipStream_t s)
             cross_rows_kernel<T, DP, false><<<grid, kThreads, 0, s>>>(k);
         if (k.splits > 1) {
             const int64_t count = units * a.M * a.D;
-            sum_parts<T>(a, a.part, k.splits, count, count, a.M, 1, a.dq, a.q_row, a.q_tok, s);
+            sum_parts<T>(a, a.part, k.splits, count, count, a.M, 1, a.dq, nullptr, a.q_row, a.q_tok, s);
         }
     }
     if (bias && a.M > 0 && a.Lk > 0) {
@@ -553,7 +560,7 @@ template <typename T, int DP> void run(CrArgs a, const CrPlan &p, hipStream_t s)
         cross_bias_kernel<T, DP><<<(uint32_t)(planes * k.tiles * k.ntiles * k.splits), kThreads, 0, s>>>(k);
         if (k.splits > 1) {
             const int64_t count = planes * a.Lq * a.Lk;
-            sum_parts<T>(a, a.part, k.splits, count, count, 1, 0, a.dbias, 0, 0, s);
+            sum_parts<T>(a, a.part, k.splits, count, count, 1, 0, a.dbias, nullptr, 0, 0, s);
         }
     }
 }
