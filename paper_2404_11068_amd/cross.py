@@ -128,7 +128,7 @@ def cross_attn_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, gate: Opti
     lib = _lib()
     dm, _, _ = _dims(q, k, v, gate, bias, key_mask, rows_per_bias)
     if out is None:
-        out = _empty(q.shape, q.dtype, q, stream)
+        out = torch.empty_like(q) if stream is None and q.is_contiguous() else _empty(q.shape, q.dtype, q, stream)
     else:
         os_ = _block(out, "out")[1]
         _like(out, q, os_, "out")

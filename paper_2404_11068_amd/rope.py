@@ -106,76 +106,86 @@ def rope_steps(frequencies, device="cuda") -> torch.Tensor:
     return torch.tensor(steps, dtype=torch.int64, device=device)
 
 
-def _check_tokens(x: torch.Tensor, what: str, like: Optional[torch.Tensor] = None):
-    if x.dim() != 4:
+def _layout(x: torch.Tensor, what: str):
+    """(shape, row stride, token stride) of [N, L, H, d] heads; an axis of one entry, whose stride says nothing, counts
+    as packed."""
+    shape = x.shape
+    if len(shape) != 4:
         raise ValueError("%s must be [N, L, H, d]" % what)
-    if x.dtype not in _DTYPES:
-        raise ValueError("%s must be float32 or bfloat16" % what)
-    N, L, H, d = x.shape
-    sr, st, sh, sd = x.stride()
-    if (d > 1 and sd != 1) or (H > 1 and sh != d):
+    N, L, H, d = shape
+    row, tok, sh, sd = x.stride()
+    if (sd != 1 and d > 1) or (sh != d and H > 1):
         raise ValueError("the [H, d] block of each token of %s must be contiguous" % what)
-    if like is not None and (x.dtype != like.dtype or x.device != like.device or d != like.shape[3] or N != like.shape[0]):
+    if L <= 1:
+        tok = H * d
+    return shape, row if N > 1 and L > 0 else L * tok, tok
+
+
+def _set(x, y, pos, w, q, what):
+    """Checks of one set of heads x (of dx, too), with y (of dy, too; None: packed); what the dims say of it."""
+    dtype, device = q.dtype, q.device
+    shape, x_row, x_tok = _layout(x, what)
+    N, L, H, d = shape
+    if x is not q and (x.dtype != dtype or x.device != device or d != q.shape[3] or N != q.shape[0]):
         raise ValueError("%s must share its type, device, rows and head dim with the queries" % what)
-    return N, L, H, d, (sr if N > 1 else 0), (st if L > 1 else 0)
+    if y is None:
+        y_tok = H * d
+        y_row = L * y_tok
+    else:
+        y_shape, y_row, y_tok = _layout(y, "output or gradient")
+        if y_shape != shape or y.dtype != dtype or y.device != device:
+            raise ValueError("outputs and gradients must share shape, type and device with their heads")
+    ps = None if pos is None else pos.shape
+    if ps is None or pos.dtype != torch.int32 or ps[-1:] != (L,) or len(ps) > 2 or (len(ps) == 2 and ps[0] != N and ps[0] != 1) \
+            or (L > 1 and pos.stride(-1) != 1) or pos.device != device:
+        raise ValueError("pos_%s must be int32 [%d, %d], [1, %d] or [%d] with contiguous rows, on the device of q"
+                         % (what, N, L, L, L))
+    if w is not None:
+        _check_weight(w, d, q)
+    return H, L, (pos.stride(0) if len(ps) == 2 and ps[0] > 1 else 0), x_row, x_tok, y_row, y_tok
 
 
-def _strides(x: torch.Tensor, fill: bool):
-    """(row, token) strides; of an axis of one entry, whose stride says nothing, the packed value."""
-    N, L, H, d = x.shape
-    tok = x.stride(1) if L > 1 else H * d
-    row = x.stride(0) if N > 1 else (L * tok if fill else 0)
-    return row, tok
+def _check_weight(w: torch.Tensor, d: int, like: torch.Tensor):
+    if w.dtype != torch.float32 or w.shape != (d,) or not w.is_contiguous() or w.device != like.device:
+        raise ValueError("weights and their gradients must be contiguous float32 [%d] tensors on the queries' device" % d)
 
 
-def _check_pos(pos: Optional[torch.Tensor], N: int, L: int, like: torch.Tensor, what: str) -> int:
-    """Checks; returns the positions' row stride."""
-    if pos is None or pos.dtype != torch.int32 or pos.dim() not in (1, 2) or pos.shape[-1] != L or \
-            (pos.dim() == 2 and pos.shape[0] not in (1, N)) or (L > 1 and pos.stride(-1) != 1):
-        raise ValueError("%s must be int32 [%d, %d], [1, %d] or [%d] with contiguous rows" % (what, N, L, L, L))
-    if pos.device != like.device:
-        raise ValueError("tensors must be on one device")
-    return pos.stride(0) if pos.dim() == 2 and pos.shape[0] > 1 else 0
+_NONE = (0, 0, 0, 0, 0, 0, 0)
 
 
-def _check_weight(w: Optional[torch.Tensor], d: int, like: torch.Tensor, what: str):
-    if w is not None and (w.dtype != torch.float32 or w.shape != (d,) or not w.is_contiguous() or w.device != like.device):
-        raise ValueError("%s must be a contiguous float32 [%d] tensor on the queries' device" % (what, d))
-
-
-def _dims(x, y, pos, steps, weights, interleaved, norm, eps, amplitude, pos_names=("pos_q", "pos_k")):
-    """dims for the sets x (of dx, too) and y (of dy, too); also checks."""
-    q = x[0]
-    N, _, _, d, _, _ = _check_tokens(q, "q")
-    if q.device.type != "cuda" or q.device.index != torch._C._cuda_getDevice():
+def _dims(x, y, pos, steps, weights, interleaved, norm, eps, amplitude):
+    """Checks; dims for the sets x (of dx, too) and y (of dy, too)."""
+    q, k = x
+    dtype, device = q.dtype, q.device
+    if dtype not in _DTYPES:
+        raise ValueError("q must be float32 or bfloat16")
+    a = _set(q, y[0], pos[0], weights[0], q, "q")
+    if k is not None:
+        b = _set(k, y[1], pos[1], weights[1], q, "k")
+    elif pos[1] is not None or weights[1] is not None:
+        raise ValueError("pos_k and a weight for keys go with keys")
+    else:
+        b = _NONE
+    if device.type != "cuda" or device.index != torch._C._cuda_getDevice():
         raise ValueError("tensors must be on the current CUDA device")
-    if steps.dtype != torch.int64 or steps.dim() != 1 or not steps.is_contiguous() or steps.device != q.device:
+    st = steps.shape
+    if steps.dtype != torch.int64 or len(st) != 1 or not steps.is_contiguous() or steps.device != device:
         raise ValueError("steps must be a contiguous int64 [rot / 2] tensor on the queries' device")
-    rot = 2 * steps.shape[0]
-    if rot > d:
-        raise ValueError("steps are for %d channels, a head has %d" % (rot, d))
+    N, _, _, d = q.shape
+    if 2 * st[0] > d:
+        raise ValueError("steps are for %d channels, a head has %d" % (2 * st[0], d))
     if not norm and (weights[0] is not None or weights[1] is not None):
         raise ValueError("weights go with norm=True")
-    dm = evo_rope_dims()
-    dm.dtype, dm.head_dim, dm.rot_dim, dm.n_rows = _DTYPES[q.dtype], d, rot, N
-    dm.flags = (_INTERLEAVED if interleaved else 0) | (_NORM if norm else 0)
-    dm.eps, dm.amplitude = eps, amplitude
-    for i in range(2):
-        if x[i] is None:
-            if pos[i] is not None or weights[i] is not None:
-                raise ValueError("%s and a weight for keys go with keys" % pos_names[i])
-            continue
-        _, L, H, _, _, _ = _check_tokens(x[i], "qk"[i], q)
-        if y[i] is not None:
-            _check_tokens(y[i], "gradient or output", q)
-            if y[i].shape != x[i].shape:
-                raise ValueError("outputs and gradients must be shaped like their heads")
-        dm.n_heads[i], dm.len[i] = H, L
-        dm.pos_stride[i] = _check_pos(pos[i], N, L, q, pos_names[i])
-        _check_weight(weights[i], d, q, "weight")
-        dm.x_stride_row[i], dm.x_stride_tok[i] = _strides(x[i], True)
-        dm.y_stride_row[i], dm.y_stride_tok[i] = _strides(y[i], True) if y[i] is not None else (L * H * d, H * d)
-    return dm
+    return evo_rope_dims(_DTYPES[dtype], d, 2 * st[0], (_INTERLEAVED if interleaved else 0) | (_NORM if norm else 0),
+                         (a[0], b[0]), eps, amplitude, N, (a[1], b[1]), (a[2], b[2]), (a[3], b[3]), (a[4], b[4]),
+                         (a[5], b[5]), (a[6], b[6]))
+
+
+def _packed(x: torch.Tensor, like: torch.Tensor, stream):
+    """A contiguous tensor shaped like x."""
+    if stream is None and x.is_contiguous():
+        return torch.empty_like(x)
+    return _empty(x.shape, x.dtype, like, stream)
 
 
 def _addr(t: Optional[torch.Tensor]):
@@ -195,9 +205,9 @@ def rope_fwd(q: torch.Tensor, pos_q: torch.Tensor, steps: torch.Tensor, *, k: Op
     if k is None and out_k is not None:
         raise ValueError("out_k goes with k")
     if out_q is None:
-        out_q = _empty(q.shape, q.dtype, q, stream)
+        out_q = _packed(q, q, stream)
     if k is not None and out_k is None:
-        out_k = _empty(k.shape, k.dtype, q, stream)
+        out_k = _packed(k, q, stream)
     st = lib.evo_rope_fwd(dm, q.data_ptr(), _addr(k), _addr(pos_q), _addr(pos_k), steps.data_ptr(), _addr(weight_q),
                           _addr(weight_k), out_q.data_ptr(), _addr(out_k), _stream(stream))
     if st:
@@ -208,15 +218,13 @@ def rope_fwd(q: torch.Tensor, pos_q: torch.Tensor, steps: torch.Tensor, *, k: Op
 def rope_bwd_workspace_size(q: torch.Tensor, steps: torch.Tensor, *, k: Optional[torch.Tensor] = None,
                             norm: bool = False) -> int:
     """Bytes of workspace that rope_bwd needs for heads shaped like q and k."""
-    dm = evo_rope_dims()
-    N, _, _, d, _, _ = _check_tokens(q, "q")
-    dm.dtype, dm.head_dim, dm.rot_dim, dm.n_rows = _DTYPES[q.dtype], d, 2 * steps.numel(), N
-    dm.flags, dm.amplitude = (_NORM if norm else 0), 1.0
-    for i, x in enumerate((q, k)):
-        if x is not None:
-            dm.len[i], dm.n_heads[i] = x.shape[1], x.shape[2]
-            dm.x_stride_row[i], dm.x_stride_tok[i] = dm.y_stride_row[i], dm.y_stride_tok[i] = \
-                x.shape[1] * x.shape[2] * d, x.shape[2] * d
+    N, _, _, d = _layout(q, "q")[0]
+    sets = [(0, 0) if x is None else (_layout(x, "heads")[0][2], x.shape[1]) for x in (q, k)]
+    heads, lens = zip(*sets)
+    tok = tuple(h * d for h in heads)
+    row = tuple(l * t for l, t in zip(lens, tok))
+    dm = evo_rope_dims(_DTYPES[q.dtype], d, 2 * steps.numel(), _NORM if norm else 0, heads, 0.0, 1.0, N, lens, (0, 0), row,
+                       tok, row, tok)
     return int(_lib().evo_rope_bwd_workspace_size(dm))
 
 
@@ -271,7 +279,7 @@ def rope_bwd(dq: torch.Tensor, pos_q: torch.Tensor, steps: torch.Tensor, *, dk: 
         elif dws[i] is None:
             dws[i] = _empty(w.shape, torch.float32, dq, stream)
         else:
-            _check_weight(dws[i], w.shape[0], dq, "dweight")
+            _check_weight(dws[i], w.shape[0], dq)
     need = lib.evo_rope_bwd_workspace_size(dm)
     if workspace is None:
         ws_bytes, workspace = need, _empty((max(need, 1),), torch.uint8, dq, stream)
