@@ -27,6 +27,7 @@ enum Pairing { kInter, kHalf, kSplit };
 
 struct KArgs {
     RopeArgs a;
+    uint32_t h_mul[2];   // u / heads = u * h_mul >> 32 for a workgroup's units
     uint32_t blocks[2];  // workgroups of each set
     float *part;         // backward: partial sums of dw, [blocks of set 0 + 1][d]
     int tb, gs_log;
@@ -84,6 +85,22 @@ __device__ __forceinline__ float2 turn(uint64_t phase) {
     return float2{quarter == 1 || quarter == 2 ? -cc : cc, quarter >= 2 ? -ss : ss};
 }
 
+template <int CTRL> __device__ __forceinline__ float dpp_add(float x) {
+    return x + __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), CTRL, 0xf, 0xf, true));
+}
+// sum over aligned groups of 2^log lanes, the same in all of them: within 16 lanes by lane
+// permutations of the vector unit (neighbours, pairs, then mirrored halves, whose fours and
+// eights hold equal sums by then)
+__device__ __forceinline__ float group_sum(float x, int log) {
+    if (log > 0) x = dpp_add<0xB1>(x);
+    if (log > 1) x = dpp_add<0x4E>(x);
+    if (log > 2) x = dpp_add<0x141>(x);
+    if (log > 3) x = dpp_add<0x140>(x);
+    if (log > 4) x += __shfl_xor(x, 16, 64);
+    if (log > 5) x += __shfl_xor(x, 32, 64);
+    return x;
+}
+
 // Workgroup b of the set takes token blocks b, b + blocks, ...
 template <typename E, Pairing P, bool NORM, bool BWD>
 __device__ __forceinline__ void rope_body(const KArgs &k, float2 *angles, float *line) {
@@ -125,44 +142,48 @@ __device__ __forceinline__ void rope_body(const KArgs &k, float2 *angles, float 
         // one 64-bit division a block; within it rows and columns are 32 bits (len <= 2^30)
         const int64_t row0 = t0 / s.len;
         const uint32_t col0 = (uint32_t)(t0 - row0 * s.len), len = (uint32_t)s.len;
-        for (int i = tid; i < nt * half; i += kThreads) {
-            const int t = i / half, j = i - t * half;
-            const uint32_t over = (col0 + t) / len;
-            const int64_t pos = s.pos[(row0 + over) * s.pos_stride + (col0 + t - over * len)];
-            const float2 cs = turn((uint64_t)pos * a.steps[j]);
-            angles[i] = float2{cs.x * a.amplitude, (BWD ? -cs.y : cs.y) * a.amplitude};
-        }
-        __syncthreads();
-        const int units = nt * H;
-        // every lane of a wave makes the same number of turns: the shuffles need them all
-        for (int u0 = wave * per_wave; u0 < units; u0 += 4 * per_wave) {
+        // rows that lie between a block's first token and its t-th
+        auto rows_on = [&](int t) { return len >= kMaxTok ? (uint32_t)(col0 + t >= len) : (col0 + t) / len; };
+        const int units = nt * H, stride = 4 * per_wave;
+        struct Unit {
+            u32x4 raw, x;
+            E *to;
+            int t;
+            bool on;
+        };
+        auto fetch = [&](int u0) {
+            Unit r;
             const int u = u0 + (lane >> k.gs_log);
-            const bool on = live && u < units;
-            const int t = on ? u / H : 0, h = on ? u - t * H : 0;
-            const uint32_t over = (col0 + t) / len;
-            const int64_t row = row0 + over, col = col0 + t - over * len;
-            const int64_t at = (int64_t)h * a.d + base;
-            u32x4 raw = {0, 0, 0, 0}, xraw = {0, 0, 0, 0};
-            if (on) {
-                raw = *reinterpret_cast<const u32x4 *>((const E *)s.in + row * s.in_row + col * s.in_tok + at);
-                if (NORM && BWD) xraw = *reinterpret_cast<const u32x4 *>((const E *)s.x + row * s.x_row + col * s.x_tok + at);
+            r.on = live && u < units;
+            r.t = !r.on || nt == 1 ? 0 : H == 1 ? u : (int)__umulhi((uint32_t)u, k.h_mul[which]);
+            const int h = r.on ? u - r.t * H : 0;
+            const uint32_t over = rows_on(r.t);
+            const int64_t row = row0 + over, col = col0 + r.t - over * len, at = (int64_t)h * a.d + base;
+            r.raw = r.x = u32x4{0, 0, 0, 0};
+            r.to = (E *)s.out + row * s.out_row + col * s.out_tok + at;
+            if (r.on) {
+                r.raw = *reinterpret_cast<const u32x4 *>((const E *)s.in + row * s.in_row + col * s.in_tok + at);
+                if (NORM && BWD) r.x = *reinterpret_cast<const u32x4 *>((const E *)s.x + row * s.x_row + col * s.x_tok + at);
             }
+            return r;
+        };
+        auto work = [&](const Unit &r) {
             float v[VEC], o[VEC];
-            Chunk<E>::get(raw, v);
+            Chunk<E>::get(r.raw, v);
             float rstd = 1.0f;
             if (NORM) {
                 float xv[VEC], sum = 0.0f;
-                Chunk<E>::get(BWD ? xraw : raw, xv);
+                Chunk<E>::get(BWD ? r.x : r.raw, xv);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) sum = fmaf(xv[e], xv[e], sum);
-                for (int m = 1; m < gs; m <<= 1) sum += __shfl_xor(sum, m, 64);
+                sum = group_sum(sum, k.gs_log);
                 rstd = 1.0f / sqrtf(fmaf(sum, inv_d, a.eps));
             }
             if (NORM && !BWD) {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) v[e] *= rstd;
             }
-            const float2 *row_angles = angles + t * half;
+            const float2 *row_angles = angles + r.t * half;
             if (P == kInter) {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e)
@@ -181,7 +202,7 @@ __device__ __forceinline__ void rope_body(const KArgs &k, float2 *angles, float 
             } else if (P == kHalf) {
                 u32x4 praw;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) praw[i] = __shfl(raw[i], partner, 64);
+                for (int i = 0; i < 4; ++i) praw[i] = __shfl(r.raw[i], partner, 64);
                 float pv[VEC];
                 Chunk<E>::get(praw, pv);
                 const int j0 = low ? base : base - half;
@@ -220,7 +241,7 @@ __device__ __forceinline__ void rope_body(const KArgs &k, float2 *angles, float 
             }
             if (NORM && BWD) {
                 float xv[VEC], dot = 0.0f;
-                Chunk<E>::get(xraw, xv);
+                Chunk<E>::get(r.x, xv);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
                     xv[e] *= rstd;
@@ -228,13 +249,32 @@ __device__ __forceinline__ void rope_body(const KArgs &k, float2 *angles, float 
                     o[e] *= w[e];
                     dot = fmaf(o[e], xv[e], dot);
                 }
-                for (int m = 1; m < gs; m <<= 1) dot += __shfl_xor(dot, m, 64);
+                dot = group_sum(dot, k.gs_log);
                 dot *= inv_d;
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) o[e] = rstd * fmaf(-xv[e], dot, o[e]);
             }
-            if (on)
-                *reinterpret_cast<u32x4 *>((E *)s.out + row * s.out_row + col * s.out_tok + at) = Chunk<E>::put(o);
+            if (r.on) *reinterpret_cast<u32x4 *>(r.to) = Chunk<E>::put(o);
+        };
+        // every lane of a wave makes the same number of turns: the shuffles need them all.  Two units are
+        // worked on while two are on their way, the first two from before the angles on
+        int u0 = wave * per_wave;
+        Unit r0 = fetch(u0), r1 = fetch(u0 + stride);
+        for (int i = tid; i < nt * half; i += kThreads) {
+            const int t = i / half, j = i - t * half;
+            const uint32_t over = rows_on(t);
+            const int64_t pos = s.pos[(row0 + over) * s.pos_stride + (col0 + t - over * len)];
+            const float2 cs = turn((uint64_t)pos * a.steps[j]);
+            angles[i] = float2{cs.x * a.amplitude, (BWD ? -cs.y : cs.y) * a.amplitude};
+        }
+        __syncthreads();
+        while (u0 < units) {
+            u0 += 2 * stride;
+            const Unit n0 = fetch(u0), n1 = fetch(u0 + stride);
+            work(r0);
+            work(r1);
+            r0 = n0;
+            r1 = n1;
         }
         __syncthreads();
     }
@@ -255,7 +295,7 @@ __device__ __forceinline__ void rope_body(const KArgs &k, float2 *angles, float 
 }
 
 template <typename E, Pairing P, bool NORM, bool BWD>
-__global__ __launch_bounds__(kThreads) void rope_kernel(KArgs k) {
+__global__ __launch_bounds__(kThreads, 4) void rope_kernel(KArgs k) {
     __shared__ float2 angles[kMaxTok * 128];
     __shared__ float line[4 * 64 * Chunk<E>::VEC > 1024 ? 4 * 64 * Chunk<E>::VEC : 1024];
     rope_body<E, P, NORM, BWD>(k, angles, line);
@@ -287,7 +327,10 @@ __global__ __launch_bounds__(1024) void rope_dw_kernel(const float *part0, int n
 void plan(const RopeArgs &a, bool bwd, KArgs *k) {
     const int64_t all = a.set[0].tokens + a.set[1].tokens;
     int tb = 1;
-    while (tb < kMaxTok && all / (2 * tb) >= 2048) tb *= 2;
+    for (int i = 0; i < 2; ++i)
+        k->h_mul[i] = a.set[i].heads > 1 ? (uint32_t)(((uint64_t(1) << 32) + a.set[i].heads - 1) / a.set[i].heads) : 0;
+    // (with more heads a workgroup has one token, and h_mul does not count)
+    while (tb < kMaxTok && a.set[0].heads <= 8192 && a.set[1].heads <= 8192 && all / (2 * tb) >= 2048) tb *= 2;
     k->tb = tb;
     const int chunks = a.d / (a.bf16 ? 8 : 4);
     k->gs_log = 0;
