@@ -110,7 +110,7 @@ static int split(int64_t tiles, int64_t steps, double one, double bytes, double 
     for (int64_t n = 1; n <= steps && n <= 64; ++n) {
         const int64_t per = up(steps, n), load = up(tiles * n, 256);
         if (up(steps, per) != n) continue;
-        const double cost = load * per * one / (load > 1 ? 1.3 : 1.0) + (n > 1 ? launch + n * bytes / 2e6 : 0.0);
+        const double cost = load * per * one / (load > 1 ? 1.3 : 1.0) + (n > 1 ? launch + n * bytes / 1.5e6 : 0.0);
         if (n == 1 || cost < least) best = (int)n, least = cost;
         if (load > 16) break;  // the GPU is full
     }
@@ -158,7 +158,8 @@ CrPlan cross_plan(const CrArgs &a, bool has_gate, bool has_bias) {
         p.fwd_total = p.fwd_ml + pad((size_t)p.fwd_splits * units * a.M * 8);
     }
     p.kv_splits = split(units * up(a.Lk, 128), up(a.M, a.bf16 && a.D <= 64 ? 64 : 32), 1.3 * one, keys_bytes, 5.0);
-    p.q_splits = split(units * up(a.M, 128), key_steps, 1.2 * one, rows_bytes, 5.0);
+    const bool wide_steps = a.bf16 && a.D <= 64 && !has_bias;
+    p.q_splits = split(units * up(a.M, 128), up(a.Lk, wide_steps ? 64 : 32), (wide_steps || !a.bf16 ? 1.2 : 0.6) * one, rows_bytes, 5.0);
     p.bias_chunks = 1;
     if (has_bias) {
         const int64_t bias_tiles = a.N / a.rpb * a.H * up(a.Lq, 64) * up(a.Lk, 64);

@@ -84,7 +84,7 @@ __global__ __launch_bounds__(kThreads, (KeysShape<T, DP>::WAVES)) void cross_key
     __shared__ __attribute__((aligned(16))) E tiles[2][2][S::TILE];
     __shared__ __attribute__((aligned(16))) float stats[2][2][S::XT];
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     uint32_t u = xcd_unit32(blockIdx.x, gridDim.x);
     const int split = u % a.splits;
     u /= a.splits;
@@ -109,87 +109,108 @@ __global__ __launch_bounds__(kThreads, (KeysShape<T, DP>::WAVES)) void cross_key
     for (int i = 0; i < DT; ++i) dk[i] = dvv[i] = zero16();
     const float to2 = a.scale * kLog2e;
 
-    Stage<T, DP, S::XT, kThreads> qs, as;
+    constexpr int NB = S::XT / 32, GP = 32 / Y::KS;
+    using Cp = Copy<T, DP, S::XT, kThreads>;
     float lse_in = 0.0f, dsum_in = 0.0f;
     auto request = [&](int step) {
         const int x0 = step * S::XT;
-        auto in = [&](int r) { return x0 + r < a.M; };
         auto at = [&](int r, int64_t tok) {
             const int x = x0 + r, t = token_of(a, x);
             return (int64_t)t * tok + (int64_t)(x - t * a.G) * a.D;
         };
-        qs.load(qbase, a.D, tid, [&](int r) { return qbase + at(r, a.q_tok); }, in);
-        as.load(abase, a.D, tid, [&](int r) { return abase + at(r, dv.tok); }, in);
         if (tid < S::XT) {
-            // a query without keys, and what lies behind the last: probability exp(-inf)
-            const int x = x0 + tid, xc = min(x, a.M - 1), t = token_of(a, xc), g = xc - t * a.G;
+            const int x = min(x0 + tid, a.M - 1), t = token_of(a, x), g = x - t * a.G;
             lse_in = a.lse[(n * a.H + hk * a.G + g) * a.Lq + t];
-            if (x >= a.M || lse_in == -__builtin_inff()) lse_in = __builtin_inff();
-            dsum_in = x < a.M ? a.dsum[(int64_t)unit * a.M + x] : 0.0f;
+            dsum_in = a.dsum[(int64_t)unit * a.M + x];
+        }
+        const bool whole = a.D == DP && x0 + S::XT <= a.M;
+        auto in = [&](int r) { return x0 + r < a.M; };
+        Cp::run(tiles[step & 1][0], whole, a.D, wave, lane, [&](int r) { return qbase + at(r, a.q_tok); }, in);
+        Cp::run(tiles[step & 1][1], whole, a.D, wave, lane, [&](int r) { return abase + at(r, dv.tok); }, in);
+    };
+    // the bias of a step's queries with the lane's key: the 32 keys of a query's row are neighbours
+    E braw[BIAS ? NB : 1][16];
+    auto request_bias = [&](int step) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const int xb = step * S::XT + 32 * b;
+            if (a.G == 1 && xb + 32 <= a.M) {
+                const E *p = bias + (int64_t)(xb + 4 * h) * a.Lk;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) braw[BIAS ? b : 0][i] = p[(int64_t)(8 * (i / 4) + i % 4) * a.Lk];
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int x = min(xb + 8 * (i / 4) + 4 * h + i % 4, a.M - 1), t = token_of(a, x);
+                    braw[BIAS ? b : 0][i] = bias[((int64_t)(x - t * a.G) * a.Lq + t) * a.Lk];
+                }
+            }
         }
     };
     const int s0 = split * a.per_split, s1 = min(s0 + a.per_split, a.ntiles);
     // a workgroup whose keys are all masked has zeros to write and nothing to read
-    const bool work = __syncthreads_or(keep);
-    if (work && s0 < s1) request(s0);
+    const bool work = __syncthreads_or(keep) && s0 < s1;
+    if (work) {
+        if (BIAS) request_bias(s0);
+        request(s0);
+    }
     for (int step = s0; work && step < s1; ++step) {
-        const int buf = step & 1, x0 = step * S::XT;
-        E *qt = tiles[buf][0], *at = tiles[buf][1];
-        auto in = [&](int r) { return x0 + r < a.M; };
-        qs.store(qt, a.D, tid, in);
-        as.store(at, a.D, tid, in);
+        const int buf = step & 1;
+        const E *qt = tiles[buf][0], *at = tiles[buf][1];
+        asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
         if (tid < S::XT) {
-            stats[buf][0][tid] = BIAS ? lse_in : lse_in * kLog2e;
+            // a query without keys, and what lies behind the last: probability exp(-inf)
+            const float l = step * S::XT + tid >= a.M || lse_in == -__builtin_inff() ? __builtin_inff() : lse_in;
+            stats[buf][0][tid] = BIAS ? l : l * kLog2e;
             stats[buf][1][tid] = dsum_in;
         }
-        __syncthreads();
+        copies_done_and_barrier();
         if (step + 1 < s1) request(step + 1);
+        f32x16 s[NB], dp[NB];
 #pragma unroll
-        for (int b = 0; b < S::XT / 32; ++b) {
-            f32x16 s = zero16(), dp = zero16();
-            const int r = 32 * b + (lane & 31);
-            float add[16];
-            if (BIAS) {
-                // the 32 keys of a query's row are neighbours
-                const int xb = x0 + 32 * b;
-                if (a.G == 1 && xb + 32 <= a.M) {
-                    const E *p = bias + (int64_t)(xb + 4 * h) * a.Lk;
+        for (int b = 0; b < NB; ++b) s[b] = dp[b] = zero16();
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) add[i] = Y::f(p[(int64_t)(8 * (i / 4) + i % 4) * a.Lk], keep);
-                } else {
+        for (int kk = 0; kk < NK; ++kk)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int x = min(xb + 8 * (i / 4) + 4 * h + i % 4, a.M - 1), t = token_of(a, x);
-                        add[i] = Y::f(bias[((int64_t)(x - t * a.G) * a.Lq + t) * a.Lk], keep);
-                    }
-                }
+            for (int b = 0; b < NB; ++b) {
+                Y::mma(s[b], LT::row(qt, 32 * b + (lane & 31), kk, h), kf[kk]);
+                Y::mma(dp[b], LT::row(at, 32 * b + (lane & 31), kk, h), vf[kk]);
             }
+        if (BIAS) {
 #pragma unroll
-            for (int kk = 0; kk < NK; ++kk) Y::mma(s, LT::row(qt, r, kk, h), kf[kk]);
+            for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int kk = 0; kk < NK; ++kk) Y::mma(dp, LT::row(at, r, kk, h), vf[kk]);
-            if (BIAS) {
+                for (int i = 0; i < 16; ++i) s[b][i] = fmaf(s[b][i], a.scale, Y::f(braw[BIAS ? b : 0][i], keep));
+            if (step + 1 < s1) request_bias(step + 1);
+        }
+        // four probabilities of a block, and what the logits' gradients are by them
+        auto four = [&](int b, int i) {
+            const f32x4 l = *reinterpret_cast<const f32x4 *>(&stats[buf][0][32 * b + 2 * i + 4 * h]);
+            const f32x4 d = *reinterpret_cast<const f32x4 *>(&stats[buf][1][32 * b + 2 * i + 4 * h]);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], a.scale, add[i]);
+            for (int e = 0; e < 4; ++e) {
+                s[b][i + e] = __builtin_amdgcn_exp2f(BIAS ? (s[b][i + e] - l[e]) * kLog2e : fmaf(s[b][i + e], to2, -l[e]));
+                dp[b][i + e] = s[b][i + e] * (dp[b][i + e] - d[e]);
             }
+        };
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-                const f32x4 l = *reinterpret_cast<const f32x4 *>(&stats[buf][0][32 * b + 2 * i + 4 * h]);
-                const f32x4 d = *reinterpret_cast<const f32x4 *>(&stats[buf][1][32 * b + 2 * i + 4 * h]);
+        for (int i = 0; i < 16; i += 4) four(0, i);
+        // the products of one block run among the exponentials of the next
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    s[i + e] = __builtin_amdgcn_exp2f(BIAS ? (s[i + e] - l[e]) * kLog2e : fmaf(s[i + e], to2, -l[e]));
-                    dp[i + e] = s[i + e] * (dp[i + e] - d[e]);
+        for (int b = 0; b < NB; ++b) {
+            Frag p[GP], ds[GP];
+#pragma unroll
+            for (int g = 0; g < GP; ++g) p[g] = Y::pack(s[b], g), ds[g] = Y::pack(dp[b], g);
+            constexpr int NJ = GP * DT;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                const int g = j / DT, d = j % DT;
+                Y::mma(dvv[d], LT::col(at, 32 * b + Y::KS * g, 32 * d, lane), p[g]);
+                if (b + 1 < NB) {
+#pragma unroll
+                    for (int i = j * 4 / NJ; i < (j + 1) * 4 / NJ; ++i) four(b + 1 < NB ? b + 1 : 0, 4 * i);
                 }
-            }
-#pragma unroll
-            for (int g = 0; g < 32 / Y::KS; ++g) {
-                const Frag p = Y::pack(s, g), ds = Y::pack(dp, g);
-#pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    Y::mma(dvv[d], LT::col(at, 32 * b + Y::KS * g, 32 * d, lane), p);
-                    Y::mma(dk[d], LT::col(qt, 32 * b + Y::KS * g, 32 * d, lane), ds);
-                }
+                Y::mma(dk[d], LT::col(qt, 32 * b + Y::KS * g, 32 * d, lane), ds[g]);
             }
         }
     }
@@ -224,24 +245,24 @@ __global__ __launch_bounds__(kThreads, (KeysShape<T, DP>::WAVES)) void cross_key
 
 // ---------------------------------------------------------------------------
 // rows: dQ
-template <typename T, int DP> struct RowsShape {
+template <typename T, int DP, bool BIAS> struct RowsShape {
     static constexpr bool WIDE = sizeof(typename Ty<T>::E) == 4;
-    static constexpr int KT = WIDE ? 32 : 64, ROWS = 128;
+    static constexpr int KT = WIDE || DP == 128 || BIAS ? 32 : 64, ROWS = 128;
     static constexpr int TILE = KT * DP;
     static constexpr int WAVES = WIDE && DP == 128 ? 1 : 2;
 };
 
 template <typename T, int DP, bool BIAS>
-__global__ __launch_bounds__(kThreads, (RowsShape<T, DP>::WAVES)) void cross_rows_kernel(CrArgs a) {
+__global__ __launch_bounds__(kThreads, (RowsShape<T, DP, BIAS>::WAVES)) void cross_rows_kernel(CrArgs a) {
     using Y = Ty<T>;
     using E = typename Y::E;
     using Frag = typename Y::Frag;
     using LT = Tile<T, DP>;
-    using S = RowsShape<T, DP>;
+    using S = RowsShape<T, DP, BIAS>;
     constexpr int NK = DP / Y::KS, DT = DP / 32;
     __shared__ __attribute__((aligned(16))) E tiles[2][2][S::TILE];
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     uint32_t u = xcd_unit32(blockIdx.x, gridDim.x);
     const int split = u % a.splits;
     u /= a.splits;
@@ -272,61 +293,102 @@ __global__ __launch_bounds__(kThreads, (RowsShape<T, DP>::WAVES)) void cross_row
     for (int i = 0; i < DT; ++i) dq[i] = zero16();
 
     using Bits = KeyBits<S::KT>;
+    constexpr int NB = S::KT / 32, GP = 32 / Y::KS;
     Bits now, next;
-    Stage<T, DP, S::KT, kThreads> ks, vs;
-    auto request = [&](int step, auto keep) {
+    const bool full_d = a.D == DP;
+    auto request = [&](int step, bool whole, auto keep) {
         const int64_t off = (int64_t)step * S::KT * a.k_tok;
-        ks.load(kbase, a.D, tid, [&](int r) { return kbase + off + (int64_t)r * a.k_tok; }, keep);
-        vs.load(vbase, a.D, tid, [&](int r) { return vbase + off + (int64_t)r * a.k_tok; }, keep);
+        const auto k_row = [&](int r) { return kbase + off + (int64_t)r * a.k_tok; };
+        const auto v_row = [&](int r) { return vbase + off + (int64_t)r * a.k_tok; };
+        E *kt = tiles[step & 1][0], *vt = tiles[step & 1][1];
+        if constexpr (S::KT * LT::CH % kThreads == 0) {
+            Copy<T, DP, S::KT, kThreads>::run(kt, whole, a.D, wave, lane, k_row, keep);
+            Copy<T, DP, S::KT, kThreads>::run(vt, whole, a.D, wave, lane, v_row, keep);
+        } else if (wave < 2) {  // a tile takes half of the workgroup
+            Copy<T, DP, S::KT, kThreads / 2>::run(kt, whole, a.D, wave, lane, k_row, keep);
+        } else {
+            Copy<T, DP, S::KT, kThreads / 2>::run(vt, whole, a.D, wave - 2, lane, v_row, keep);
+        }
     };
-    typename Bits::Bytes bytes;
+    typename BiasRow<T>::Raw braw[BIAS ? NB : 1];
+    auto request_bias = [&](int step) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+            if (BIAS) braw[BIAS ? b : 0] = brow.request(step * S::KT + 32 * b, h);
+    };
+    typename Bits::Bytes bytes = {};
     const int t0 = split * a.per_split, t1 = min(t0 + a.per_split, a.ntiles);
     if (t0 < t1) {
         const auto first = Bits::request(mrow, t0 * S::KT, a.Lk, lane);
-        request(t0, [&](int r) { return t0 * S::KT + r < a.Lk; });
         bytes = Bits::request(mrow, (t0 + 1) * S::KT, a.Lk, lane);
         next.set(first);
+        request_bias(t0);
+        request(t0, full_d && next.all(), [&](int r) { return next.get(r); });
     }
     for (int step = t0; step < t1; ++step) {
-        E *kt = tiles[step & 1][0], *vt = tiles[step & 1][1];
+        const E *kt = tiles[step & 1][0], *vt = tiles[step & 1][1];
+        copies_done_and_barrier();
         now = next;
-        ks.store(kt, a.D, tid, [&](int r) { return now.get(r); });
-        vs.store(vt, a.D, tid, [&](int r) { return now.get(r); });
-        __syncthreads();
         if (step + 1 < t1) {
             next.set(bytes);
-            request(step + 1, [&](int r) { return next.get(r); });
             bytes = Bits::request(mrow, (step + 2) * S::KT, a.Lk, lane);
+            request(step + 1, full_d && next.all(), [&](int r) { return next.get(r); });
         }
-        if (!now.any()) continue;
+        if (!now.any()) {
+            if (step + 1 < t1) request_bias(step + 1);
+            continue;
+        }
+        f32x16 s[NB], dp[NB];
 #pragma unroll
-        for (int b = 0; b < S::KT / 32; ++b) {
-            const uint32_t bits = now.sub(b);
-            if (bits == 0) continue;
-            const bool whole = bits == 0xffffffffu;
-            f32x16 s = zero16(), dp = zero16();
-            const int r = 32 * b + (lane & 31);
-            typename BiasRow<T>::Raw add;
-            if (BIAS) add = brow.request(step * S::KT + 32 * b, h);
+        for (int b = 0; b < NB; ++b) s[b] = dp[b] = zero16();
 #pragma unroll
-            for (int kk = 0; kk < NK; ++kk) Y::mma(s, LT::row(kt, r, kk, h), qf[kk]);
+        for (int kk = 0; kk < NK; ++kk)
 #pragma unroll
-            for (int kk = 0; kk < NK; ++kk) Y::mma(dp, LT::row(vt, r, kk, h), af[kk]);
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                s[i] = __builtin_amdgcn_exp2f(BIAS ? (fmaf(s[i], a.scale, BiasRow<T>::value(add, i)) - lse) * kLog2e
-                                                   : fmaf(s[i], to2, shift));
-            if (!whole) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = where_kept(bits, i, s[i], 0);
+            for (int b = 0; b < NB; ++b) {
+                Y::mma(s[b], LT::row(kt, 32 * b + (lane & 31), kk, h), qf[kk]);
+                Y::mma(dp[b], LT::row(vt, 32 * b + (lane & 31), kk, h), af[kk]);
             }
+        if (BIAS) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) dp[i] = s[i] * (dp[i] - dsum);
+            for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int g = 0; g < 32 / Y::KS; ++g) {
-                const Frag ds = Y::pack(dp, g);
+                for (int i = 0; i < 16; ++i)
+                    s[b][i] = (fmaf(s[b][i], a.scale, BiasRow<T>::value(braw[BIAS ? b : 0], i)) - lse) * kLog2e;
+            if (step + 1 < t1) request_bias(step + 1);
+        } else {
 #pragma unroll
-                for (int d = 0; d < DT; ++d) Y::mma(dq[d], LT::col(kt, 32 * b + Y::KS * g, 32 * d, lane), ds);
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[b][i] = fmaf(s[b][i], to2, shift);
+        }
+        if (!now.all()) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                const uint32_t bits = now.sub(b);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[b][i] = where_kept(bits, i, s[b][i], kMinusInf);
+            }
+        }
+        auto four = [&](int b, int i) {
+#pragma unroll
+            for (int e = i; e < i + 4; ++e) dp[b][e] = __builtin_amdgcn_exp2f(s[b][e]) * (dp[b][e] - dsum);
+        };
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) four(0, i);
+        // the products of one block run among the exponentials of the next
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            Frag ds[GP];
+#pragma unroll
+            for (int g = 0; g < GP; ++g) ds[g] = Y::pack(dp[b], g);
+            constexpr int NJ = GP * DT;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                Y::mma(dq[j % DT], LT::col(kt, 32 * b + Y::KS * (j / DT), 32 * (j % DT), lane), ds[j / DT]);
+                if (b + 1 < NB) {
+#pragma unroll
+                    for (int i = j * 4 / NJ; i < (j + 1) * 4 / NJ; ++i) four(b + 1 < NB ? b + 1 : 0, 4 * i);
+                }
             }
         }
     }
@@ -372,7 +434,7 @@ __global__ __launch_bounds__(kThreads, (BiasShape<T, DP>::WAVES)) void cross_bia
     __shared__ __attribute__((aligned(16))) E tiles[4][S::TILE];  // Q, dA, K, V
     __shared__ __attribute__((aligned(16))) float stats[2][64];
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     const int qb = wave & 1, kb = wave >> 1;
     uint32_t u = blockIdx.x;
     const int chunk = u % a.splits;
@@ -535,9 +597,9 @@ template <typename T, int DP> void run(CrArgs a, const CrPlan &p, hipStream_t s)
     }
     if (a.M > 0) {
         CrArgs k = a;
-        using S = RowsShape<T, DP>;
-        k.tiles = (a.M + S::ROWS - 1) / S::ROWS;
-        k.ntiles = (a.Lk + S::KT - 1) / S::KT;
+        const int kt = bias ? RowsShape<T, DP, true>::KT : RowsShape<T, DP, false>::KT;
+        k.tiles = (a.M + 127) / 128;
+        k.ntiles = (a.Lk + kt - 1) / kt;
         k.splits = p.q_splits;
         k.per_split = (k.ntiles + k.splits - 1) / k.splits;
         const uint32_t grid = (uint32_t)(units * k.tiles * k.splits);
