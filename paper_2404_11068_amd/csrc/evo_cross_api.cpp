@@ -110,7 +110,7 @@ static int split(int64_t tiles, int64_t steps, double one, double bytes, double 
     for (int64_t n = 1; n <= steps && n <= 64; ++n) {
         const int64_t per = up(steps, n), load = up(tiles * n, 256);
         if (up(steps, per) != n) continue;
-        const double cost = load * per * one / (load > 1 ? 1.3 : 1.0) + (n > 1 ? launch + n * bytes / 1.5e6 : 0.0);
+        const double cost = load * per * one / (load > 1 ? 1.3 : 1.0) + (n > 1 ? launch + n * bytes / 2e6 : 0.0);
         if (n == 1 || cost < least) best = (int)n, least = cost;
         if (load > 16) break;  // the GPU is full
     }

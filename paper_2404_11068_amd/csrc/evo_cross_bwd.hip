@@ -4,8 +4,9 @@
 //   dV = P' dA,  dK = dS' Q / sqrt d,  dQ = dS K / sqrt d,  dBias = sum over rows of dS
 //
 // P is formed again from the saved log-sum-exp, in each of three passes:
+//   rows:  a wave owns 32 queries (lane = query) and walks the keys: dQ; before that
+//          it forms D, dgate and dA of its queries, and leaves them for the others
 //   keys:  a wave owns 32 keys (lane = key) and walks the queries: dK, dV
-//   rows:  a wave owns 32 queries (lane = query) and walks the keys: dQ
 //   bias:  a workgroup owns 64 x 64 entries of one bias plane and walks the
 //          rows that share it
 // Every sum runs in a fixed order; where the tiles do not fill the GPU, the
@@ -17,46 +18,7 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// D, dgate and dA: a group of gs lanes per (row, token, head), 16 bytes a lane
-template <typename T>
-__global__ __launch_bounds__(kThreads) void cross_prep_kernel(CrArgs a, int gs_log) {
-    using Y = Ty<T>;
-    using E = typename Y::E;
-    const int lane = threadIdx.x & 63, c = (lane & ((1 << gs_log) - 1)) * Y::VEC;
-    const int64_t rows = a.N * a.Lq * a.H, per = kThreads >> gs_log;
-    const int64_t row = (int64_t)blockIdx.x * per + (threadIdx.x >> gs_log);
-    const bool on = row < rows && c < a.D;
-    const int64_t tok = row / a.H, n = tok / a.Lq;
-    const int head = (int)(row - tok * a.H), t = (int)(tok - n * a.Lq);
-    const int64_t at = (int64_t)head * a.D + c;
-    float sum = 0.0f;
-    if (on) {
-        E o[Y::VEC], d[Y::VEC];
-        *reinterpret_cast<u32x4 *>(o) = *reinterpret_cast<const u32x4 *>((const E *)a.out + n * a.o_row + t * a.o_tok + at);
-        *reinterpret_cast<u32x4 *>(d) = *reinterpret_cast<const u32x4 *>((const E *)a.dout + n * a.o_row + t * a.o_tok + at);
-#pragma unroll
-        for (int e = 0; e < Y::VEC; ++e) sum = fmaf(Y::f(o[e]), Y::f(d[e]), sum);
-        if (a.gate) {
-            const int64_t q = n * a.q_row + t * a.q_tok + at;
-            E g[Y::VEC], dg[Y::VEC], da[Y::VEC];
-            *reinterpret_cast<u32x4 *>(g) = *reinterpret_cast<const u32x4 *>((const E *)a.gate + q);
-#pragma unroll
-            for (int e = 0; e < Y::VEC; ++e) {
-                // sigmoid and one minus it, each without cancellation
-                const float x = Y::f(g[e]), z = __builtin_amdgcn_exp2f(-fabsf(x) * kLog2e), r = __builtin_amdgcn_rcpf(1.0f + z);
-                const float sig = x >= 0.0f ? r : z * r, rest = x >= 0.0f ? z * r : r;
-                da[e] = Y::e(Y::f(d[e]) * sig);  // rounded to the type: the operand of two matrix products
-                dg[e] = Y::e(Y::f(d[e]) * Y::f(o[e]) * rest);
-            }
-            *reinterpret_cast<u32x4 *>((E *)a.dgate + q) = *reinterpret_cast<u32x4 *>(dg);
-            *reinterpret_cast<u32x4 *>((E *)a.da + row * a.D + c) = *reinterpret_cast<u32x4 *>(da);
-        }
-    }
-    for (int k = 1; k < 1 << gs_log; k <<= 1) sum += __shfl_xor(sum, k, 64);
-    if (on && c == 0) a.dsum[((n * a.Hk + head / a.G) * a.Lq + t) * a.G + head % a.G] = sum;
-}
-
-// dA as the kernels read it: the prepared one, or dO itself without a gate
+// dA as the later passes read it: what the first has written, or dO itself without a gate
 struct DaView {
     int64_t row, tok;
 };
@@ -270,7 +232,6 @@ __global__ __launch_bounds__(kThreads, (RowsShape<T, DP, BIAS>::WAVES)) void cro
     const uint32_t unit = u / a.tiles;
     const int64_t n = unit / a.Hk;
     const int hk = unit % a.Hk;
-    const DaView dv = da_view(a);
 
     const int x = tile * S::ROWS + wave * 32 + (lane & 31);
     const bool on = x < a.M;
@@ -278,10 +239,47 @@ __global__ __launch_bounds__(kThreads, (RowsShape<T, DP, BIAS>::WAVES)) void cro
     Frag qf[NK], af[NK];
     const int64_t qoff = n * a.q_row + (int64_t)t * a.q_tok + (int64_t)head * a.D;
     load_rows<T, DP>(qf, (const E *)a.q + qoff, a.D, on, h);
-    load_rows<T, DP>(af, (const E *)(a.gate ? a.da : a.dout) + n * dv.row + (int64_t)t * dv.tok + (int64_t)head * a.D, a.D, on, h);
+    // D, dgate and dA of the lane's query, for this pass and, written by the first split, for the next
+    float dsum = 0.0f;
+    {
+        const int64_t oat = n * a.o_row + (int64_t)t * a.o_tok + (int64_t)head * a.D;
+        const int64_t daat = ((n * a.Lq + t) * a.H + head) * (int64_t)a.D;
+        constexpr int W = Y::KS / 2;
+        struct Bits16 { E e[W]; };
+#pragma unroll
+        for (int kk = 0; kk < NK; ++kk) {
+            const int c = Y::KS * kk + W * h, cc = c < a.D ? c : 0;
+            const bool in = on && c < a.D;
+            const Bits16 o = __builtin_bit_cast(Bits16, *reinterpret_cast<const u32x4 *>((const E *)a.out + oat + cc));
+            Bits16 d = __builtin_bit_cast(Bits16, *reinterpret_cast<const u32x4 *>((const E *)a.dout + oat + cc));
+            float sum = 0.0f;
+#pragma unroll
+            for (int e = 0; e < W; ++e) sum = fmaf(Y::f(o.e[e]), Y::f(d.e[e]), sum);
+            dsum += in ? sum : 0.0f;
+            if (a.gate) {
+                const Bits16 g = __builtin_bit_cast(Bits16, *reinterpret_cast<const u32x4 *>((const E *)a.gate + qoff + cc));
+                Bits16 dg;
+#pragma unroll
+                for (int e = 0; e < W; ++e) {
+                    // sigmoid and one minus it, each without cancellation
+                    const float y = Y::f(g.e[e]), z = __builtin_amdgcn_exp2f(-fabsf(y) * kLog2e), r = __builtin_amdgcn_rcpf(1.0f + z);
+                    const float sig = y >= 0.0f ? r : z * r, rest = y >= 0.0f ? z * r : r, df = Y::f(d.e[e]);
+                    dg.e[e] = Y::e(df * Y::f(o.e[e]) * rest);
+                    d.e[e] = Y::e(df * sig);  // rounded to the type: the operand of two matrix products
+                }
+                if (in && split == 0) {
+                    *reinterpret_cast<u32x4 *>((E *)a.dgate + qoff + c) = __builtin_bit_cast(u32x4, dg);
+                    *reinterpret_cast<u32x4 *>((E *)a.da + daat + c) = __builtin_bit_cast(u32x4, d);
+                }
+            }
+            const u32x4 z = {0, 0, 0, 0};
+            af[kk] = __builtin_bit_cast(Frag, in ? __builtin_bit_cast(u32x4, d) : z);
+        }
+        dsum = half_sum(dsum);
+        if (on && h == 0 && split == 0) a.dsum[(int64_t)unit * a.M + x] = dsum;
+    }
     float lse = a.lse[(n * a.H + head) * a.Lq + t];
     if (!on || lse == -__builtin_inff()) lse = __builtin_inff();
-    const float dsum = a.dsum[(int64_t)unit * a.M + xc];
     const float to2 = a.scale * kLog2e, shift = -lse * kLog2e;
     const BiasRow<T> brow(a, BIAS ? (n / a.rpb * a.H + head) * a.Lq + t : 0);
 
@@ -578,23 +576,6 @@ void sum_parts(const CrArgs &a, const float *part, int splits, int64_t stride, i
 template <typename T, int DP> void run(CrArgs a, const CrPlan &p, hipStream_t s) {
     const int64_t units = a.N * a.Hk;
     const bool bias = a.bias != nullptr;
-    if (a.Lk > 0) {
-        CrArgs k = a;
-        using S = KeysShape<T, DP>;
-        k.tiles = (a.Lk + S::KEYS - 1) / S::KEYS;
-        k.ntiles = (a.M + S::XT - 1) / S::XT;
-        k.splits = p.kv_splits;
-        k.per_split = (k.ntiles + k.splits - 1) / k.splits;
-        const uint32_t grid = (uint32_t)(units * k.tiles * k.splits);
-        if (bias)
-            cross_keys_kernel<T, DP, true><<<grid, kThreads, 0, s>>>(k);
-        else
-            cross_keys_kernel<T, DP, false><<<grid, kThreads, 0, s>>>(k);
-        if (k.splits > 1) {
-            const int64_t count = units * a.Lk * a.D;
-            sum_parts<T>(a, a.part, k.splits, 2 * count, count, a.Lk, 0, a.dk, a.dv, a.k_row, a.k_tok, s);
-        }
-    }
     if (a.M > 0) {
         CrArgs k = a;
         const int kt = bias ? RowsShape<T, DP, true>::KT : RowsShape<T, DP, false>::KT;
@@ -610,6 +591,23 @@ template <typename T, int DP> void run(CrArgs a, const CrPlan &p, hipStream_t s)
         if (k.splits > 1) {
             const int64_t count = units * a.M * a.D;
             sum_parts<T>(a, a.part, k.splits, count, count, a.M, 1, a.dq, nullptr, a.q_row, a.q_tok, s);
+        }
+    }
+    if (a.Lk > 0) {
+        CrArgs k = a;
+        using S = KeysShape<T, DP>;
+        k.tiles = (a.Lk + S::KEYS - 1) / S::KEYS;
+        k.ntiles = (a.M + S::XT - 1) / S::XT;
+        k.splits = p.kv_splits;
+        k.per_split = (k.ntiles + k.splits - 1) / k.splits;
+        const uint32_t grid = (uint32_t)(units * k.tiles * k.splits);
+        if (bias)
+            cross_keys_kernel<T, DP, true><<<grid, kThreads, 0, s>>>(k);
+        else
+            cross_keys_kernel<T, DP, false><<<grid, kThreads, 0, s>>>(k);
+        if (k.splits > 1) {
+            const int64_t count = units * a.Lk * a.D;
+            sum_parts<T>(a, a.part, k.splits, 2 * count, count, a.Lk, 0, a.dk, a.dv, a.k_row, a.k_tok, s);
         }
     }
     if (bias && a.M > 0 && a.Lk > 0) {
@@ -628,10 +626,6 @@ template <typename T, int DP> void run(CrArgs a, const CrPlan &p, hipStream_t s)
 }
 
 template <typename T> void run_dim(const CrArgs &a, const CrPlan &p, hipStream_t s) {
-    int gs_log = 0;
-    while ((Ty<T>::VEC << gs_log) < a.D) ++gs_log;
-    const int64_t rows = a.N * a.Lq * a.H, per = kThreads >> gs_log;
-    if (rows > 0) cross_prep_kernel<T><<<(uint32_t)((rows + per - 1) / per), kThreads, 0, s>>>(a, gs_log);
     a.D <= 32 ? run<T, 32>(a, p, s) : a.D <= 64 ? run<T, 64>(a, p, s) : run<T, 128>(a, p, s);
 }
 
