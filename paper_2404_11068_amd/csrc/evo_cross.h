@@ -248,35 +248,9 @@ __device__ __forceinline__ void kept_range(const uint8_t *mask_row, int Lk, int 
     if (hi >= 0) t0 = lo / KT;
 }
 
-// A tile of ROWS tokens of DP channels on its way from memory to LDS, 16 bytes
-// a thread at a time.  Rows and channels that are not there are read from a
-// valid address and written as zeros (NaN or infinity in a masked place stays
-// outside of every product).
-template <typename T, int DP, int ROWS, int THREADS> struct Stage {
-    using E = typename Ty<T>::E;
-    static constexpr int CPR = DP / Ty<T>::VEC, N = ROWS * CPR / THREADS;
-    static_assert(ROWS * CPR % THREADS == 0, "whole chunks");
-    u32x4 v[N];
-    template <class Row, class Keep>
-    __device__ __forceinline__ void load(const E *safe, int D, int tid, Row row, Keep keep) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int at = tid + THREADS * i, r = at / CPR, c = at % CPR * Ty<T>::VEC;
-            const E *p = keep(r) && c < D ? row(r) + c : safe;
-            v[i] = *reinterpret_cast<const u32x4 *>(p);
-        }
-    }
-    template <class Keep> __device__ __forceinline__ void store(E *tile, int D, int tid, Keep keep) const {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int at = tid + THREADS * i, r = at / CPR, c = at % CPR * Ty<T>::VEC;
-            const u32x4 z = {0, 0, 0, 0};
-            *reinterpret_cast<u32x4 *>(tile + Tile<T, DP>::at(r, at % CPR)) = keep(r) && c < D ? v[i] : z;
-        }
-    }
-};
-
-// The same without registers in between: global_load_lds, 16 bytes a lane.  The
+// A tile of ROWS tokens of DP channels from memory to LDS, without registers in between: global_load_lds,
+// 16 bytes a lane.  Rows and channels that are not there are copied from zeros (NaN or infinity in a masked
+// place stays outside of every product).  The
 // copies are counted by hand: copies_done_and_barrier() before a tile is read.
 // (The compiler does not see them; its own waits on vector memory count in order
 // and only get longer by them.)

@@ -418,8 +418,9 @@ __global__ __launch_bounds__(kThreads, (RowsShape<T, DP, BIAS>::WAVES)) void cro
 // bias: dBias.  tiles = 64-query tiles, ntiles = 64-key tiles, splits = chunks of
 // per_split rows of a plane
 template <typename T, int DP> struct BiasShape {
-    static constexpr int TILE = 64 * DP;
-    static constexpr int WAVES = 4 * TILE * (int)sizeof(typename Ty<T>::E) <= 78 * 1024 ? 2 : 1;
+    static constexpr int TILE = 64 * DP, BYTES = 4 * TILE * (int)sizeof(typename Ty<T>::E);
+    static constexpr int BUFS = BYTES <= 64 * 1024 ? 2 : 1;
+    static constexpr int WAVES = BUFS * BYTES <= 78 * 1024 ? 2 : 1;
 };
 
 template <typename T, int DP>
@@ -429,8 +430,8 @@ __global__ __launch_bounds__(kThreads, (BiasShape<T, DP>::WAVES)) void cross_bia
     using LT = Tile<T, DP>;
     using S = BiasShape<T, DP>;
     constexpr int NK = DP / Y::KS;
-    __shared__ __attribute__((aligned(16))) E tiles[4][S::TILE];  // Q, dA, K, V
-    __shared__ __attribute__((aligned(16))) float stats[2][64];
+    __shared__ __attribute__((aligned(16))) E tiles[S::BUFS][4][S::TILE];  // Q, dA, K, V
+    __shared__ __attribute__((aligned(16))) float stats[S::BUFS][2][64];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     const int qb = wave & 1, kb = wave >> 1;
@@ -458,60 +459,79 @@ __global__ __launch_bounds__(kThreads, (BiasShape<T, DP>::WAVES)) void cross_bia
     }
     f32x16 acc = zero16();
     using Bits = KeyBits<64>;
+    using Cp = Copy<T, DP, 64, kThreads>;
     Bits now, next;
-    Stage<T, DP, 64, kThreads> qs, as, ks, vs;
+    auto bytes_of = [&](int64_t n) { return Bits::request(a.mask ? a.mask + n * a.Lk : nullptr, k0, n < n1 ? a.Lk : 0, lane); };
     float lse_in = 0.0f, dsum_in = 0.0f;
-    auto in_q = [&](int r) { return t0 + r < a.Lq; };
-    auto request = [&](int64_t n) {
-        next.set(Bits::request(a.mask ? a.mask + n * a.Lk : nullptr, k0, a.Lk, lane));
-        const E *q = (const E *)a.q + n * a.q_row + (int64_t)head * a.D;
-        const E *da = (const E *)(a.gate ? a.da : a.dout) + n * dv.row + (int64_t)head * a.D;
-        const E *k = (const E *)a.k + n * a.k_row + (int64_t)hk * a.D, *v = (const E *)a.v + n * a.k_row + (int64_t)hk * a.D;
-        auto keep = [&](int r) { return next.get(r); };
-        qs.load(q, a.D, tid, [&](int r) { return q + (int64_t)(t0 + r) * a.q_tok; }, in_q);
-        as.load(da, a.D, tid, [&](int r) { return da + (int64_t)(t0 + r) * dv.tok; }, in_q);
-        ks.load(k, a.D, tid, [&](int r) { return k + (int64_t)(k0 + r) * a.k_tok; }, keep);
-        vs.load(v, a.D, tid, [&](int r) { return v + (int64_t)(k0 + r) * a.k_tok; }, keep);
+    const bool full_d = a.D == DP, full_q = full_d && t0 + 64 <= a.Lq;
+    auto request = [&](int64_t n, int buf) {
         if (tid < 64) {
             const int t = min(t0 + tid, a.Lq - 1);
             lse_in = a.lse[(n * a.H + head) * a.Lq + t];
-            if (t0 + tid >= a.Lq || lse_in == -__builtin_inff()) lse_in = __builtin_inff();
             dsum_in = a.dsum[((n * a.Hk + hk) * a.Lq + t) * a.G + g];
         }
+        const E *q = (const E *)a.q + n * a.q_row + (int64_t)head * a.D;
+        const E *da = (const E *)(a.gate ? a.da : a.dout) + n * dv.row + (int64_t)head * a.D;
+        const E *k = (const E *)a.k + n * a.k_row + (int64_t)hk * a.D, *v = (const E *)a.v + n * a.k_row + (int64_t)hk * a.D;
+        const auto in_q = [&](int r) { return t0 + r < a.Lq; };
+        const auto keep = [&](int r) { return next.get(r); };
+        const bool full_k = full_d && next.all();
+        Cp::run(tiles[buf][0], full_q, a.D, wave, lane, [&](int r) { return q + (int64_t)(t0 + r) * a.q_tok; }, in_q);
+        Cp::run(tiles[buf][1], full_q, a.D, wave, lane, [&](int r) { return da + (int64_t)(t0 + r) * dv.tok; }, in_q);
+        Cp::run(tiles[buf][2], full_k, a.D, wave, lane, [&](int r) { return k + (int64_t)(k0 + r) * a.k_tok; }, keep);
+        Cp::run(tiles[buf][3], full_k, a.D, wave, lane, [&](int r) { return v + (int64_t)(k0 + r) * a.k_tok; }, keep);
     };
-    if (n0 < n1) request(n0);
+    typename Bits::Bytes bytes = {};
+    if (n0 < n1) {
+        const auto first = bytes_of(n0);
+        bytes = bytes_of(n0 + 1);
+        next.set(first);
+        request(n0, 0);
+    }
+    int buf = 0;
     for (int64_t n = n0; n < n1; ++n) {
+        asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+        if (tid < 64) {
+            stats[buf][0][tid] = t0 + tid >= a.Lq || lse_in == -__builtin_inff() ? __builtin_inff() : lse_in;
+            stats[buf][1][tid] = dsum_in;
+        }
+        copies_done_and_barrier();
         now = next;
-        auto keep = [&](int r) { return now.get(r); };
-        qs.store(tiles[0], a.D, tid, in_q);
-        as.store(tiles[1], a.D, tid, in_q);
-        ks.store(tiles[2], a.D, tid, keep);
-        vs.store(tiles[3], a.D, tid, keep);
-        if (tid < 64) stats[0][tid] = lse_in, stats[1][tid] = dsum_in;
-        __syncthreads();
-        if (n + 1 < n1) request(n + 1);
+        const E *const qt_ = tiles[buf][0], *const at_ = tiles[buf][1], *const kt_ = tiles[buf][2], *const vt_ = tiles[buf][3];
+        const float *const ls = stats[buf][0], *const ds = stats[buf][1];
+        const auto go_on = [&]() {
+            if (n + 1 >= n1) return;
+            next.set(bytes);
+            bytes = bytes_of(n + 2);
+            if (S::BUFS == 2) buf ^= 1;
+            request(n + 1, buf);
+        };
+        if (S::BUFS == 2) go_on();
         if (now.any()) {
             f32x16 s = zero16(), dp = zero16();
             const int qr = 32 * qb + (lane & 31), kr = 32 * kb + (lane & 31);
 #pragma unroll
             for (int kk = 0; kk < NK; ++kk) {
-                Y::mma(s, LT::row(tiles[0], qr, kk, h), LT::row(tiles[2], kr, kk, h));
-                Y::mma(dp, LT::row(tiles[1], qr, kk, h), LT::row(tiles[3], kr, kk, h));
+                Y::mma(s, LT::row(qt_, qr, kk, h), LT::row(kt_, kr, kk, h));
+                Y::mma(dp, LT::row(at_, qr, kk, h), LT::row(vt_, kr, kk, h));
             }
             const bool mine = now.get(32 * kb + (lane & 31));
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
-                const f32x4 l = *reinterpret_cast<const f32x4 *>(&stats[0][32 * qb + 2 * i + 4 * h]);
-                const f32x4 d = *reinterpret_cast<const f32x4 *>(&stats[1][32 * qb + 2 * i + 4 * h]);
+                const f32x4 l = *reinterpret_cast<const f32x4 *>(&ls[32 * qb + 2 * i + 4 * h]);
+                const f32x4 d = *reinterpret_cast<const f32x4 *>(&ds[32 * qb + 2 * i + 4 * h]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float b = __uint_as_float(mine ? __float_as_uint(bias[i + e]) : 0xff800000u);
+                    const float b = __uint_as_float(mine ? __float_as_uint(bias[i + e]) : kMinusInf);
                     const float p = __builtin_amdgcn_exp2f((fmaf(s[i + e], a.scale, b) - l[e]) * kLog2e);
                     acc[i + e] = fmaf(p, dp[i + e] - d[e], acc[i + e]);
                 }
             }
         }
-        __syncthreads();
+        if (S::BUFS == 1) {
+            __syncthreads();
+            go_on();
+        }
     }
     if (key >= a.Lk) return;
     const int64_t all = a.N / a.rpb * a.H * a.Lq * (int64_t)a.Lk;
