@@ -278,17 +278,26 @@ template <typename T, int DP, int ROWS, int THREADS> struct Copy {
     }
 };
 
+// x where on, zeros elsewhere: by a mask, since a choice makes the compiler load x in a branch of its own
+// and wait for it there, one load after the other
+__device__ __forceinline__ u32x4 where(bool on, u32x4 x) {
+    const uint32_t m = on ? 0xffffffffu : 0u;
+    return x & u32x4{m, m, m, m};
+}
+
 // the lane's row of a 32-row block as operand: channels KS kk + (KS / 2) h ..
 template <typename T, int DP>
 __device__ __forceinline__ void load_rows(typename Ty<T>::Frag (&f)[DP / Ty<T>::KS], const typename Ty<T>::E *row, int D, bool on,
                                           int h) {
+    u32x4 x[DP / Ty<T>::KS];
 #pragma unroll
     for (int kk = 0; kk < DP / Ty<T>::KS; ++kk) {
         const int c = Ty<T>::KS * kk + Ty<T>::KS / 2 * h;
-        const u32x4 z = {0, 0, 0, 0};
-        const u32x4 x = *reinterpret_cast<const u32x4 *>(row + (c < D ? c : 0));
-        f[kk] = __builtin_bit_cast(typename Ty<T>::Frag, on && c < D ? x : z);
+        x[kk] = *reinterpret_cast<const u32x4 *>(row + (c < D ? c : 0));
     }
+#pragma unroll
+    for (int kk = 0; kk < DP / Ty<T>::KS; ++kk)
+        f[kk] = __builtin_bit_cast(typename Ty<T>::Frag, where(on && Ty<T>::KS * kk + Ty<T>::KS / 2 * h < D, x[kk]));
 }
 
 // Four consecutive values of a row that may start at any element

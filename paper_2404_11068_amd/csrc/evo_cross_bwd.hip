@@ -250,12 +250,10 @@ __global__ __launch_bounds__(kThreads, (RowsShape<T, DP, BIAS>::WAVES)) void cro
         for (int kk = 0; kk < NK; ++kk) {
             const int c = Y::KS * kk + W * h, cc = c < a.D ? c : 0;
             const bool in = on && c < a.D;
-            const Bits16 o = __builtin_bit_cast(Bits16, *reinterpret_cast<const u32x4 *>((const E *)a.out + oat + cc));
-            Bits16 d = __builtin_bit_cast(Bits16, *reinterpret_cast<const u32x4 *>((const E *)a.dout + oat + cc));
-            float sum = 0.0f;
+            const Bits16 o = __builtin_bit_cast(Bits16, where(in, *reinterpret_cast<const u32x4 *>((const E *)a.out + oat + cc)));
+            Bits16 d = __builtin_bit_cast(Bits16, where(in, *reinterpret_cast<const u32x4 *>((const E *)a.dout + oat + cc)));
 #pragma unroll
-            for (int e = 0; e < W; ++e) sum = fmaf(Y::f(o.e[e]), Y::f(d.e[e]), sum);
-            dsum += in ? sum : 0.0f;
+            for (int e = 0; e < W; ++e) dsum = fmaf(Y::f(o.e[e]), Y::f(d.e[e]), dsum);
             if (a.gate) {
                 const Bits16 g = __builtin_bit_cast(Bits16, *reinterpret_cast<const u32x4 *>((const E *)a.gate + qoff + cc));
                 Bits16 dg;
@@ -272,8 +270,7 @@ __global__ __launch_bounds__(kThreads, (RowsShape<T, DP, BIAS>::WAVES)) void cro
                     *reinterpret_cast<u32x4 *>((E *)a.da + daat + c) = __builtin_bit_cast(u32x4, d);
                 }
             }
-            const u32x4 z = {0, 0, 0, 0};
-            af[kk] = __builtin_bit_cast(Frag, in ? __builtin_bit_cast(u32x4, d) : z);
+            af[kk] = __builtin_bit_cast(Frag, d);
         }
         dsum = half_sum(dsum);
         if (on && h == 0 && split == 0) a.dsum[(int64_t)unit * a.M + x] = dsum;
