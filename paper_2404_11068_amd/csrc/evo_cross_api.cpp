@@ -9,7 +9,7 @@
 
 namespace {
 
-constexpr int64_t kMost = int64_t(1) << 40, kMostLen = 0x7fffffff - 128, kGrid = 0x7fffffff;
+constexpr int64_t kMost = int64_t(1) << 40, kMostLen = int64_t(1) << 30, kGrid = 0x7fffffff;
 
 bool aligned(const void *p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }

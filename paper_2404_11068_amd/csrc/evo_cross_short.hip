@@ -204,34 +204,36 @@ __global__ __launch_bounds__(kThreads, (ShortLds<T, DP, NB, ONE>::SIZE > 80 * 10
     }
 }
 
-template <typename T, int DP, bool BIAS, int NB> void launch(const CrArgs &a, bool one, uint32_t grid, hipStream_t s) {
+template <typename T, int DP, bool BIAS, int NB> hipError_t launch(const CrArgs &a, bool one, uint32_t grid, hipStream_t s) {
     if constexpr (ShortLds<T, DP, NB, true>::FITS) {
         if (one) {
             cross_short_kernel<T, DP, BIAS, NB, true><<<grid, kThreads, 0, s>>>(a);
-            return;
+            return hipGetLastError();
         }
     }
     // (the plan takes four waves a row in bf16 up to 32 channels only)
-    if constexpr (sizeof(typename Ty<T>::E) == 2 && DP == 32) cross_short_kernel<T, DP, BIAS, NB, false><<<grid, kThreads, 0, s>>>(a);
-}
-
-template <typename T, int DP, bool BIAS> void launch_keys(const CrArgs &a, bool one, uint32_t grid, hipStream_t s) {
-    switch ((a.Lk + 31) / 32) {
-        case 0:
-        case 1: launch<T, DP, BIAS, 1>(a, one, grid, s); break;
-        case 2: launch<T, DP, BIAS, 2>(a, one, grid, s); break;
-        case 3: launch<T, DP, BIAS, 3>(a, one, grid, s); break;
-        default: launch<T, DP, BIAS, 4>(a, one, grid, s); break;
+    if constexpr (sizeof(typename Ty<T>::E) == 2 && DP == 32) {
+        if (!one) {
+            cross_short_kernel<T, DP, BIAS, NB, false><<<grid, kThreads, 0, s>>>(a);
+            return hipGetLastError();
+        }
     }
+    return hipErrorInvalidValue;
 }
 
-template <typename T> void launch_dim(const CrArgs &a, bool one, uint32_t grid, hipStream_t s) {
-    if (a.D <= 32)
-        a.bias ? launch_keys<T, 32, true>(a, one, grid, s) : launch_keys<T, 32, false>(a, one, grid, s);
-    else if (a.D <= 64)
-        a.bias ? launch_keys<T, 64, true>(a, one, grid, s) : launch_keys<T, 64, false>(a, one, grid, s);
-    else
-        a.bias ? launch_keys<T, 128, true>(a, one, grid, s) : launch_keys<T, 128, false>(a, one, grid, s);
+template <typename T, int DP> hipError_t launch_keys(const CrArgs &a, bool one, uint32_t grid, hipStream_t s) {
+    switch ((a.Lk + 31) / 32) {
+        case 1: return a.bias ? launch<T, DP, true, 1>(a, one, grid, s) : launch<T, DP, false, 1>(a, one, grid, s);
+        case 2: return a.bias ? launch<T, DP, true, 2>(a, one, grid, s) : launch<T, DP, false, 2>(a, one, grid, s);
+        case 3: return a.bias ? launch<T, DP, true, 3>(a, one, grid, s) : launch<T, DP, false, 3>(a, one, grid, s);
+        case 4: return a.bias ? launch<T, DP, true, 4>(a, one, grid, s) : launch<T, DP, false, 4>(a, one, grid, s);
+    }
+    return hipErrorInvalidValue;
+}
+
+template <typename T> hipError_t launch_dim(const CrArgs &a, bool one, uint32_t grid, hipStream_t s) {
+    return a.D <= 32 ? launch_keys<T, 32>(a, one, grid, s)
+                     : a.D <= 64 ? launch_keys<T, 64>(a, one, grid, s) : launch_keys<T, 128>(a, one, grid, s);
 }
 
 }  // namespace
@@ -241,8 +243,7 @@ hipError_t launch_cross_short(CrArgs a, const CrPlan &p, hipStream_t s) {
     a.splits = p.brief_chunks;
     a.per_split = (int)((a.rpb + a.splits - 1) / a.splits);
     const uint32_t grid = (uint32_t)(a.N / a.rpb * a.splits * a.Hk * a.tiles);
-    a.bf16 ? launch_dim<bf16_t>(a, p.brief_one, grid, s) : launch_dim<float>(a, p.brief_one, grid, s);
-    return hipGetLastError();
+    return a.bf16 ? launch_dim<bf16_t>(a, p.brief_one, grid, s) : launch_dim<float>(a, p.brief_one, grid, s);
 }
 
 }  // namespace evo

@@ -67,6 +67,20 @@ bool overlap_ok(const evo_rope_dims *d, int i, const void *in, int64_t ir, int64
     return a < b ? (int64_t)(b - a) >= span(d, i, ir, it) : (int64_t)(a - b) >= span(d, i, orow, otok);
 }
 
+// what one set writes and another tensor of the other set: apart, or interleaved in one packed buffer
+bool sets_ok(const evo_rope_dims *d, int i, const void *out, int64_t orow, int64_t otok, int j, const void *other,
+             int64_t row, int64_t tok) {
+    if (empty(d, i) || empty(d, j) || !other) return true;
+    const uintptr_t a = (uintptr_t)out, b = (uintptr_t)other;
+    if (a < b ? (int64_t)(b - a) >= span(d, i, orow, otok) : (int64_t)(a - b) >= span(d, j, row, tok)) return true;
+    const int64_t es = d->dtype == EVO_DTYPE_BF16 ? 2 : 4;
+    const int64_t bi = (int64_t)d->n_heads[i] * d->head_dim * es, bj = (int64_t)d->n_heads[j] * d->head_dim * es;
+    // one token stride (of the packed buffer), the blocks side by side within it
+    if (otok != tok || orow != row || otok == 0) return false;
+    const int64_t at = (int64_t)((a < b ? b - a : a - b) % (uintptr_t)(otok * es));
+    return a < b ? at >= bi && at + bj <= otok * es : at >= bj && at + bi <= otok * es;
+}
+
 void fill(const evo_rope_dims *d, evo::RopeArgs *a) {
     for (int i = 0; i < 2; ++i) {
         evo::RopeSet &s = a->set[i];
@@ -116,7 +130,12 @@ int evo_rope_fwd(const evo_rope_dims *d, const void *x0, const void *x1, const i
         s.out_row = d->y_stride_row[i];
         s.out_tok = d->y_stride_tok[i];
     }
-    if (y0 && y0 == y1 && !empty(d, 0) && !empty(d, 1)) return EVO_ERR_INVALID_ARG;
+    for (int i = 0; i < 2; ++i)
+        if (!sets_ok(d, i, y[i], d->y_stride_row[i], d->y_stride_tok[i], 1 - i, x[1 - i], d->x_stride_row[1 - i],
+                     d->x_stride_tok[1 - i]) ||
+            !sets_ok(d, i, y[i], d->y_stride_row[i], d->y_stride_tok[i], 1 - i, y[1 - i], d->y_stride_row[1 - i],
+                     d->y_stride_tok[1 - i]))
+            return EVO_ERR_INVALID_ARG;
     a.steps = steps;
     return evo::launch_rope_fwd(a, (hipStream_t)stream) == hipSuccess ? EVO_OK : EVO_ERR_HIP;
 }
@@ -163,7 +182,14 @@ int evo_rope_bwd(const evo_rope_dims *d, const void *dy0, const void *dy1, const
         s.x_tok = s.out_tok = d->x_stride_tok[i];
     }
     if (dw0 && dw0 == dw1) return EVO_ERR_INVALID_ARG;
-    if (dx0 && dx0 == dx1 && !empty(d, 0) && !empty(d, 1)) return EVO_ERR_INVALID_ARG;
+    for (int i = 0; i < 2; ++i)
+        if (!sets_ok(d, i, dx[i], d->x_stride_row[i], d->x_stride_tok[i], 1 - i, dy[1 - i], d->y_stride_row[1 - i],
+                     d->y_stride_tok[1 - i]) ||
+            !sets_ok(d, i, dx[i], d->x_stride_row[i], d->x_stride_tok[i], 1 - i, dx[1 - i], d->x_stride_row[1 - i],
+                     d->x_stride_tok[1 - i]) ||
+            (a.norm && !sets_ok(d, i, dx[i], d->x_stride_row[i], d->x_stride_tok[i], 1 - i, x[1 - i],
+                                d->x_stride_row[1 - i], d->x_stride_tok[1 - i])))
+            return EVO_ERR_INVALID_ARG;
     a.steps = steps;
     const size_t need = evo::rope_bwd_workspace(a);
     if (need > 0 && (!workspace || workspace_bytes < need)) return EVO_ERR_WORKSPACE;

@@ -139,6 +139,16 @@ CASES = [
     (1, 700, 33, 2, 1, 80, True, 0, None),
     (2, 17, 64, 12, 4, 104, False, 1, None),
     (64, 5, 7, 2, 2, 16, True, 1, "random"),
+    # few keys and many rows of the batch: a wave or a workgroup walks over rows
+    (2048, 1, 4, 2, 2, 16, False, 0, "random"),
+    (1024, 3, 33, 8, 4, 64, True, 1, "length"),
+    (4096, 2, 100, 1, 1, 8, True, 0, None),
+    (4097, 1, 30, 1, 1, 128, False, 0, "last"),
+    (2050, 2, 70, 2, 2, 32, True, 2, "random"),
+    (128, 130, 77, 4, 4, 32, True, 1, "length"),
+    (256, 70, 20, 4, 2, 24, False, 2, "random"),
+    (129, 129, 128, 4, 4, 16, True, 0, None),
+    (130, 129, 64, 4, 4, 32, False, 1, "last"),
 ]
 
 
@@ -158,14 +168,23 @@ def test_forward_and_backward(case, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("rows", [2, 4096])
 @pytest.mark.parametrize("Lq", [1, 100])
-def test_what_masked_places_hold_does_not_matter(dtype, Lq):
+def test_what_masked_places_hold_does_not_matter(dtype, Lq, rows):
     case = (2, Lq, 150, 4, 2, 64, True, 1, "random")
+    if rows > 2:  # few keys, many rows
+        case = (2048 if Lq == 1 else 128, Lq, 50, 4, 2, 32, True, 1, "random")
     q, k, v, g, bias, m, dout = _draw(case, dtype, 2)
-    ref = _check(case, dtype, (q, k, v, g, bias, m, dout), None)
+    ref = _check(case, dtype, (q, k, v, g, bias, m, dout), None) if rows == 2 else None
     off = m == 0
     m2 = m.clone()
     both = off.all(0)                                                  # bias columns that every row masks
+    if rows > 2:
+        m[:, 7] = 0
+        m2, off = m.clone(), m == 0
+        both = off.all(0)
+        ref = cross.cross_attn_fwd(q, k, v, g, bias, m)
+        ref = ref + (cross.cross_attn_bwd(q, k, v, g, bias, m, *ref, dout),)
     for fill in (float("nan"), float("inf"), -float("inf"), torch.finfo(dtype).max):
         k2, v2, b2 = k.clone(), v.clone(), bias.clone()
         k2[off], v2[off] = fill, fill

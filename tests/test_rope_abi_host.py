@@ -104,6 +104,17 @@ def test_rejects_bad_pointers():
     assert _lib().evo_rope_bwd_workspace_size(ctypes.byref(plain)) == 0
 
 
+def test_sets_must_not_overlap_but_in_a_packed_buffer():
+    d = _dims()
+    assert _fwd(d, y0=FAKE + BIG) == 1 and _fwd(d, y1=FAKE) == 1              # on the other set's input
+    assert _fwd(d, y1=FAKE + 7 * BIG + 256) == 1
+    assert _bwd(d, dx0=FAKE + 10 * BIG) == 1 and _bwd(d, dx1=FAKE + 9 * BIG + 1024) == 1 and _bwd(d, dx1=FAKE) == 1
+    # keys on the queries' last head in a packed buffer of tokens of 640 elements
+    p = dict(len=(16, 16), x_stride_row=(16 * 640, 16 * 640), x_stride_tok=(640, 640), y_stride_row=(16 * 640, 16 * 640),
+             y_stride_tok=(640, 640))
+    assert _fwd(_dims(**p), y0=FAKE + 7 * BIG, y1=FAKE + 7 * BIG + 2 * 448) == 1
+
+
 def test_empty_needs_no_pointers():
     none = {k: None for k in ("x0", "x1", "pos0", "pos1", "steps", "w0", "w1", "y0", "y1")}
     assert _fwd(_dims(n_rows=0), **none) == 0
