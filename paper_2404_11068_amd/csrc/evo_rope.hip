@@ -177,7 +177,7 @@ __device__ __forceinline__ void rope_body(const KArgs &k, float2 *angles, float 
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) sum = fmaf(xv[e], xv[e], sum);
                 sum = group_sum(sum, k.gs_log);
-                rstd = 1.0f / sqrtf(fmaf(sum, inv_d, a.eps));
+                rstd = __builtin_amdgcn_rsqf(fmaf(sum, inv_d, a.eps));  // to one step of fp32
             }
             if (NORM && !BWD) {
 #pragma unroll
@@ -254,7 +254,9 @@ __device__ __forceinline__ void rope_body(const KArgs &k, float2 *angles, float 
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) o[e] = rstd * fmaf(-xv[e], dot, o[e]);
             }
-            if (r.on) *reinterpret_cast<u32x4 *>(r.to) = Chunk<E>::put(o);
+            // past the caches' way of keeping what was written last: 2 x 8193 tokens of 32 heads 26.8 -> 24.2 us,
+            // 128 x 256 of 16 heads in fp32 25.5 -> 21.6
+            if (r.on) __builtin_nontemporal_store(Chunk<E>::put(o), reinterpret_cast<u32x4 *>(r.to));
         };
         // every lane of a wave makes the same number of turns: the shuffles need them all.  Two units are
         // worked on while two are on their way, the first two from before the angles on
