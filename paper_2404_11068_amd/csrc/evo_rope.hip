@@ -27,6 +27,7 @@ enum Pairing { kInter, kHalf, kSplit };
 
 struct KArgs {
     RopeArgs a;
+    int near[2];         // token strides are small: a block's offsets fit 32 bits
     uint32_t h_mul[2];   // u / heads = u * h_mul >> 32 for a workgroup's units
     uint32_t blocks[2];  // workgroups of each set
     float *part;         // backward: partial sums of dw, [blocks of set 0 + 1][d]
@@ -36,6 +37,7 @@ struct KArgs {
 template <typename E> struct Chunk;  // 16 bytes of a head
 template <> struct Chunk<float> {
     static constexpr int VEC = 4;
+    static constexpr uint32_t SIGNS = 0x80000000u;
     __device__ __forceinline__ static void get(u32x4 w, float *v) {
         const f32x4 x = __builtin_bit_cast(f32x4, w);
 #pragma unroll
@@ -47,6 +49,7 @@ template <> struct Chunk<float> {
 };
 template <> struct Chunk<uint16_t> {
     static constexpr int VEC = 8;
+    static constexpr uint32_t SIGNS = 0x80008000u;
     __device__ __forceinline__ static void get(u32x4 w, float *v) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -55,10 +58,10 @@ template <> struct Chunk<uint16_t> {
         }
     }
     __device__ __forceinline__ static u32x4 put(const float *v) {
-        u32x4 w;
+        bf16x8 w;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = (uint32_t)f2bf(v[2 * e]) | ((uint32_t)f2bf(v[2 * e + 1]) << 16);
-        return w;
+        for (int e = 0; e < 8; ++e) w[e] = (__bf16)v[e];
+        return __builtin_bit_cast(u32x4, w);
     }
 };
 
@@ -127,6 +130,8 @@ __device__ __forceinline__ void rope_body(const KArgs &k, float2 *angles, float 
         partner = low ? lane + hc : lane - hc;
         if (c >= 2 * hc) partner = lane;
     }
+    // interleaved: whole chunks are rotated or not; the lane's chunk is
+    const bool rot_whole = a.rot > 0 && a.rot % VEC == 0, rotated = base < a.rot;
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
         acc[e] = 0.0f;
@@ -144,6 +149,14 @@ __device__ __forceinline__ void rope_body(const KArgs &k, float2 *angles, float 
         const uint32_t col0 = (uint32_t)(t0 - row0 * s.len), len = (uint32_t)s.len;
         // rows that lie between a block's first token and its t-th
         auto rows_on = [&](int t) { return len >= kMaxTok ? (uint32_t)(col0 + t >= len) : (col0 + t) / len; };
+        const bool near = k.near[which] && col0 + nt <= len;  // one row, 32-bit offsets from its first token
+        // element `rest` of the t-th token
+        auto place = [&](const E *p, int64_t row_stride, int64_t tok_stride, int t, uint32_t rest) {
+            const E *first = p + row0 * row_stride + (int64_t)col0 * tok_stride;
+            if (near) return first + ((uint32_t)t * (uint32_t)tok_stride + rest);
+            const uint32_t over = rows_on(t);
+            return p + (row0 + over) * row_stride + (int64_t)(col0 + t - over * len) * tok_stride + rest;
+        };
         const int units = nt * H, stride = 4 * per_wave;
         struct Unit {
             u32x4 raw, x;
@@ -156,17 +169,16 @@ __device__ __forceinline__ void rope_body(const KArgs &k, float2 *angles, float 
             const int u = u0 + (lane >> k.gs_log);
             r.on = live && u < units;
             r.t = !r.on || nt == 1 ? 0 : H == 1 ? u : (int)__umulhi((uint32_t)u, k.h_mul[which]);
-            const int h = r.on ? u - r.t * H : 0;
-            const uint32_t over = rows_on(r.t);
-            const int64_t row = row0 + over, col = col0 + r.t - over * len, at = (int64_t)h * a.d + base;
+            const uint32_t rest = r.on ? (uint32_t)(u - r.t * H) * a.d + base : 0;
             r.raw = r.x = u32x4{0, 0, 0, 0};
-            r.to = (E *)s.out + row * s.out_row + col * s.out_tok + at;
+            r.to = const_cast<E *>(place((const E *)s.out, s.out_row, s.out_tok, r.t, rest));
             if (r.on) {
-                r.raw = *reinterpret_cast<const u32x4 *>((const E *)s.in + row * s.in_row + col * s.in_tok + at);
-                if (NORM && BWD) r.x = *reinterpret_cast<const u32x4 *>((const E *)s.x + row * s.x_row + col * s.x_tok + at);
+                r.raw = *reinterpret_cast<const u32x4 *>(place((const E *)s.in, s.in_row, s.in_tok, r.t, rest));
+                if (NORM && BWD) r.x = *reinterpret_cast<const u32x4 *>(place((const E *)s.x, s.x_row, s.x_tok, r.t, rest));
             }
             return r;
         };
+        // what the norm's forward multiplies by rstd comes last: the rotation is linear
         auto work = [&](const Unit &r) {
             float v[VEC], o[VEC];
             Chunk<E>::get(r.raw, v);
@@ -177,52 +189,61 @@ __device__ __forceinline__ void rope_body(const KArgs &k, float2 *angles, float 
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) sum = fmaf(xv[e], xv[e], sum);
                 sum = group_sum(sum, k.gs_log);
-                rstd = __builtin_amdgcn_rsqf(fmaf(sum, inv_d, a.eps));  // to one step of fp32
+                // to one step of fp32; units that are not there count nothing, with an eps of 0, too
+                rstd = r.on ? __builtin_amdgcn_rsqf(fmaf(sum, inv_d, a.eps)) : 0.0f;
             }
             if (NORM && !BWD) {
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) v[e] *= rstd;
+                for (int e = 0; e < VEC; ++e) v[e] *= w[e];
             }
             const float2 *row_angles = angles + r.t * half;
             if (P == kInter) {
+                const int j0 = base >> 1;
+                if (rot_whole) {
+                    const float2 *cs = row_angles + (rotated ? j0 : 0);
 #pragma unroll
-                for (int e = 0; e < VEC; ++e)
-                    if (NORM && !BWD) v[e] *= w[e];
+                    for (int e = 0; e < VEC; e += 2) {
+                        o[e] = v[e] * cs[e / 2].x - v[e + 1] * cs[e / 2].y;
+                        o[e + 1] = v[e] * cs[e / 2].y + v[e + 1] * cs[e / 2].x;
+                    }
+                    if (a.rot < a.d) {
 #pragma unroll
-                for (int e = 0; e < VEC; e += 2) {
-                    const int j = (base + e) >> 1;
-                    o[e] = v[e];
-                    o[e + 1] = v[e + 1];
-                    if (j < half) {
-                        const float2 cs = row_angles[j];
-                        o[e] = v[e] * cs.x - v[e + 1] * cs.y;
-                        o[e + 1] = v[e] * cs.y + v[e + 1] * cs.x;
+                        for (int e = 0; e < VEC; ++e) o[e] = rotated ? o[e] : v[e];
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < VEC; e += 2) {
+                        o[e] = v[e];
+                        o[e + 1] = v[e + 1];
+                        if (j0 + e / 2 < half) {
+                            const float2 cs = row_angles[j0 + e / 2];
+                            o[e] = v[e] * cs.x - v[e + 1] * cs.y;
+                            o[e + 1] = v[e] * cs.y + v[e + 1] * cs.x;
+                        }
                     }
                 }
             } else if (P == kHalf) {
                 u32x4 praw;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) praw[i] = __shfl(r.raw[i], partner, 64);
+                for (int i = 0; i < 4; ++i) praw[i] = (uint32_t)__shfl(r.raw[i], partner, 64) ^ (low ? Chunk<E>::SIGNS : 0u);
                 float pv[VEC];
                 Chunk<E>::get(praw, pv);
-                const int j0 = low ? base : base - half;
+                const float2 *cs = row_angles + (rotated ? (low ? base : base - half) : 0);
+                if (half > 0) {
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    if (NORM && !BWD) v[e] *= w[e];
-                    o[e] = v[e];
-                    if (j0 < half) {
-                        const float2 cs = row_angles[j0 + e];
-                        const float q = NORM && !BWD ? pv[e] * rstd * wp[e] : pv[e];
-                        o[e] = low ? v[e] * cs.x - q * cs.y : v[e] * cs.x + q * cs.y;
+                    for (int e = 0; e < VEC; ++e) {
+                        if (NORM && !BWD) pv[e] *= wp[e];
+                        o[e] = fmaf(pv[e], cs[e].y, v[e] * cs[e].x);
                     }
+                }
+                if (a.rot < a.d) {
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) o[e] = rotated ? o[e] : v[e];
                 }
             } else {
                 float *mine = line + wave * (64 * VEC) + (lane >> k.gs_log << k.gs_log) * VEC;
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    if (NORM && !BWD) v[e] *= w[e];
-                    mine[base + e] = v[e];
-                }
+                for (int e = 0; e < VEC; ++e) mine[base + e] = v[e];
                 __builtin_amdgcn_wave_barrier();
                 __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
@@ -239,6 +260,10 @@ __device__ __forceinline__ void rope_body(const KArgs &k, float2 *angles, float 
                 __builtin_amdgcn_wave_barrier();
                 __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             }
+            if (NORM && !BWD) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) o[e] *= rstd;
+            }
             if (NORM && BWD) {
                 float xv[VEC], dot = 0.0f;
                 Chunk<E>::get(r.x, xv);
@@ -249,10 +274,9 @@ __device__ __forceinline__ void rope_body(const KArgs &k, float2 *angles, float 
                     o[e] *= w[e];
                     dot = fmaf(o[e], xv[e], dot);
                 }
-                dot = group_sum(dot, k.gs_log);
-                dot *= inv_d;
+                dot = group_sum(dot, k.gs_log) * -inv_d;
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) o[e] = rstd * fmaf(-xv[e], dot, o[e]);
+                for (int e = 0; e < VEC; ++e) o[e] = rstd * fmaf(xv[e], dot, o[e]);
             }
             // past the caches' way of keeping what was written last: 2 x 8193 tokens of 32 heads 26.8 -> 24.2 us,
             // 128 x 256 of 16 heads in fp32 25.5 -> 21.6
@@ -264,7 +288,7 @@ __device__ __forceinline__ void rope_body(const KArgs &k, float2 *angles, float 
         Unit r0 = fetch(u0), r1 = fetch(u0 + stride);
         for (int i = tid; i < nt * half; i += kThreads) {
             const int t = i / half, j = i - t * half;
-            const uint32_t over = rows_on(t);
+            const uint32_t over = near ? 0 : rows_on(t);
             const int64_t pos = s.pos[(row0 + over) * s.pos_stride + (col0 + t - over * len)];
             const float2 cs = turn((uint64_t)pos * a.steps[j]);
             angles[i] = float2{cs.x * a.amplitude, (BWD ? -cs.y : cs.y) * a.amplitude};
@@ -334,6 +358,11 @@ void plan(const RopeArgs &a, bool bwd, KArgs *k) {
     // (with more heads a workgroup has one token, and h_mul does not count)
     while (tb < kMaxTok && a.set[0].heads <= 8192 && a.set[1].heads <= 8192 && all / (2 * tb) >= 2048) tb *= 2;
     k->tb = tb;
+    const int64_t most = int64_t(1) << 24;  // 16 tokens of them, and a token's heads, stay below 2^30 elements
+    for (int i = 0; i < 2; ++i) {
+        const RopeSet &t = a.set[i];
+        k->near[i] = t.in_tok < most && t.x_tok < most && t.out_tok < most && (int64_t)t.heads * a.d < most;
+    }
     const int chunks = a.d / (a.bf16 ? 8 : 4);
     k->gs_log = 0;
     while ((1 << k->gs_log) < chunks) ++k->gs_log;

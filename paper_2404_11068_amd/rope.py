@@ -26,12 +26,11 @@ _INTERLEAVED, _NORM = 1, 2
 
 
 class evo_rope_dims(ctypes.Structure):
-    _fields_ = [("dtype", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
-                ("flags", ctypes.c_int32), ("n_heads", ctypes.c_int32 * 2), ("eps", ctypes.c_float),
-                ("amplitude", ctypes.c_float), ("n_rows", ctypes.c_int64), ("len", ctypes.c_int64 * 2),
-                ("pos_stride", ctypes.c_int64 * 2), ("x_stride_row", ctypes.c_int64 * 2),
-                ("x_stride_tok", ctypes.c_int64 * 2), ("y_stride_row", ctypes.c_int64 * 2),
-                ("y_stride_tok", ctypes.c_int64 * 2)]
+    # (arrays of two as two fields each: they are set several times as fast)
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "head_dim", "rot_dim", "flags", "n_heads0", "n_heads1")] + \
+        [("eps", ctypes.c_float), ("amplitude", ctypes.c_float), ("n_rows", ctypes.c_int64)] + \
+        [(n + i, ctypes.c_int64) for n in ("len", "pos_stride", "x_stride_row", "x_stride_tok", "y_stride_row",
+                                           "y_stride_tok") for i in "01"]
 
 
 _bound = False
@@ -177,8 +176,8 @@ def _dims(x, y, pos, steps, weights, interleaved, norm, eps, amplitude):
     if not norm and (weights[0] is not None or weights[1] is not None):
         raise ValueError("weights go with norm=True")
     return evo_rope_dims(_DTYPES[dtype], d, 2 * st[0], (_INTERLEAVED if interleaved else 0) | (_NORM if norm else 0),
-                         (a[0], b[0]), eps, amplitude, N, (a[1], b[1]), (a[2], b[2]), (a[3], b[3]), (a[4], b[4]),
-                         (a[5], b[5]), (a[6], b[6]))
+                         a[0], b[0], eps, amplitude, N, a[1], b[1], a[2], b[2], a[3], b[3], a[4], b[4], a[5], b[5], a[6],
+                         b[6])
 
 
 def _packed(x: torch.Tensor, like: torch.Tensor, stream):
@@ -223,8 +222,8 @@ def rope_bwd_workspace_size(q: torch.Tensor, steps: torch.Tensor, *, k: Optional
     heads, lens = zip(*sets)
     tok = tuple(h * d for h in heads)
     row = tuple(l * t for l, t in zip(lens, tok))
-    dm = evo_rope_dims(_DTYPES[q.dtype], d, 2 * steps.numel(), _NORM if norm else 0, heads, 0.0, 1.0, N, lens, (0, 0), row,
-                       tok, row, tok)
+    dm = evo_rope_dims(_DTYPES[q.dtype], d, 2 * steps.numel(), _NORM if norm else 0, *heads, 0.0, 1.0, N, *lens, 0, 0, *row,
+                       *tok, *row, *tok)
     return int(_lib().evo_rope_bwd_workspace_size(dm))
 
 

@@ -232,6 +232,21 @@ def test_refuses():
         rope.rope_bwd(q, p, s, norm=True, q=q, workspace=torch.empty(4, dtype=torch.uint8, device="cuda"))
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+def test_an_eps_of_zero(dtype):
+    """Lanes without a unit must not count: nothing over the root of nothing."""
+    rng = np.random.default_rng(6)
+    q, dq = _rand(rng, (1, 5, 3, 40), dtype), _rand(rng, (1, 5, 3, 40), dtype)
+    pos = torch.arange(5, dtype=torch.int32, device="cuda")
+    freq = rope.rope_frequencies(40)
+    w = torch.ones(40, device="cuda")
+    g = rope.rope_bwd(dq, pos, rope.rope_steps(freq), q=q, norm=True, weight_q=w, eps=0.0)
+    dx, dw = ro.backward(to_f64(dq), to_f64(q), np.arange(5)[None], freq, norm=True, w=np.ones(40), eps=0.0)
+    hat = np.abs(to_f64(q)) * ro.rstd(to_f64(q), 0.0)
+    bound = (1.5 * 40 + 30 + 15) * E * np.sum(_abs_pair(to_f64(dq), 40, False) * hat, (0, 1, 2))
+    assert (np.abs(to_f64(g[2]) - dw) <= bound).all() and g[0].isfinite().all()
+
+
 def test_empty_sets():
     s = rope.rope_steps(rope.rope_frequencies(16))
     w = torch.ones(16, device="cuda")

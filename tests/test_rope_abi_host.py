@@ -29,8 +29,7 @@ def _dims(**kw):
              pos_stride=(16, 24), x_stride_row=(16 * 512, 24 * 128), x_stride_tok=(512, 128),
              y_stride_row=(16 * 512, 24 * 128), y_stride_tok=(512, 128))
     d.update(kw)
-    return rope.evo_rope_dims(*[t(*v) if isinstance(v, tuple) else v
-                                for (n, t), v in zip(rope.evo_rope_dims._fields_, d.values())])
+    return rope.evo_rope_dims(*[x for v in d.values() for x in (v if isinstance(v, tuple) else (v,))])
 
 
 def _fwd(d, x0=FAKE, x1=FAKE + BIG, pos0=FAKE + 2 * BIG, pos1=FAKE + 3 * BIG, steps=FAKE + 4 * BIG, w0=FAKE + 5 * BIG,
