@@ -75,13 +75,6 @@ template <> struct Ty<bf16_t> {
         for (int e = 0; e < 8; ++e) f[e] = (__bf16)p[8 * s + e];
         return f;
     }
-    // times 2^by, exact
-    __device__ __forceinline__ static Frag scaled(const Frag &f, int by) {
-        Frag o;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = (__bf16)ldexpf((float)f[e], by);
-        return o;
-    }
     __device__ __forceinline__ static float f(E x) { return bf2f(x); }
     // x where it counts: the choice is made on the bits, before any arithmetic sees what lies there
     __device__ __forceinline__ static float f(E x, bool keep) { return bf2f(keep ? x : (E)0); }
@@ -98,9 +91,6 @@ template <> struct Ty<float> {
     }
     __device__ __forceinline__ static Frag pack(const f32x16 &p, int s) {
         return Frag{p[4 * s], p[4 * s + 1], p[4 * s + 2], p[4 * s + 3]};
-    }
-    __device__ __forceinline__ static Frag scaled(const Frag &f, int by) {
-        return Frag{ldexpf(f[0], by), ldexpf(f[1], by), ldexpf(f[2], by), ldexpf(f[3], by)};
     }
     __device__ __forceinline__ static float f(E x) { return x; }
     __device__ __forceinline__ static float f(E x, bool keep) { return __uint_as_float(keep ? __float_as_uint(x) : 0u); }

@@ -5,9 +5,11 @@
 // Logits are formed transposed (S' = K Q'): a lane owns a query, so maximum and
 // sum stay in the lane but for one exchange between its halves, and the
 // probabilities go into O' = V' P' as they lie in their registers, V' by the
-// transposing LDS read.  A wave's exponentials of one tile run between the
-// matrix products with V of the tile before, so vector and matrix units work at
-// the same time within a wave, too.  Two shapes of workgroup:
+// transposing LDS read.  Matrix and vector units overlap between the two waves of
+// a SIMD.  Within a wave as well (the products with V a step late, among the next
+// exponentials) long calls were 0 to 4% slower, 4 rows of 1024 x 1024 at 128 channels
+// with a bias 41 us against 37; a few steps with a bias were 2 to 5% faster.  Two shapes of
+// workgroup:
 //   rows: four waves of 32 queries, all waves the same keys
 //   few:  two waves that share 32 queries and take turns with the keys (fp32: 64
 //         queries); for single tokens, where reading K and V is all there is to do
@@ -15,7 +17,7 @@
 // workgroups whose partial results a second kernel joins.
 //
 // The running maximum is kept on whole powers of two (its base-2 logarithm is an
-// integer): rescaling is then exact, for packed probabilities, too.
+// integer): rescaling is then exact.
 #include "evo_cross.h"
 
 namespace evo {
@@ -27,15 +29,13 @@ constexpr int kJoinThreads = 64;
 template <typename T, bool FEW> struct Shape {
     static constexpr bool WIDE = sizeof(typename Ty<T>::E) == 4;
     static constexpr int QW = FEW ? (WIDE ? 2 : 1) : 4, KW = FEW && !WIDE ? 2 : 1, THREADS = 64 * QW * KW;
-    // fp32's matrix products take so long that the exponentials do not matter
-    static constexpr bool LAG = !WIDE;
     static constexpr int KT = WIDE ? 32 : 64, KPW = KT / KW, NS = KPW / 32, ROWS = 32 * QW;
 };
 
-// K of two steps, V of two, or of three where a step's products with V come a step later
+// K and V of two steps
 template <typename T, int DP, bool FEW> struct Lds {
     using S = Shape<T, FEW>;
-    static constexpr int TILE = S::KT * DP, VBUFS = S::LAG ? 3 : 2, SIZE = (2 + VBUFS) * TILE * (int)sizeof(typename Ty<T>::E);
+    static constexpr int TILE = S::KT * DP, SIZE = 4 * TILE * (int)sizeof(typename Ty<T>::E);
     static_assert(S::KW == 1 || 2 * (DP / 32 * 16 + 2) * 256 <= SIZE, "the waves' results fit, at the end");
 };
 
@@ -71,10 +71,10 @@ __global__ __launch_bounds__((Shape<T, FEW>::THREADS), (FEW || (Shape<T, FEW>::W
     if (mrow && t1 - t0 > 8) kept_range<S::KT, S::THREADS>(mrow, a.Lk, tid, (int *)lds, t0, t1);
     E *const kt0 = (E *)lds, *const vt0 = kt0 + 2 * L::TILE;
     const bool full_d = a.D == DP;
-    auto request = [&](int step, int vbuf, bool whole, auto keep) {
+    auto request = [&](int step, bool whole, auto keep) {
         const int64_t off = (int64_t)step * S::KT * a.k_tok;
         Cp::run(kt0 + (step & 1) * L::TILE, whole, a.D, wave, lane, [&](int r) { return kbase + off + (int64_t)r * a.k_tok; }, keep);
-        Cp::run(vt0 + vbuf * L::TILE, whole, a.D, wave, lane, [&](int r) { return vbase + off + (int64_t)r * a.k_tok; }, keep);
+        Cp::run(vt0 + (step & 1) * L::TILE, whole, a.D, wave, lane, [&](int r) { return vbase + off + (int64_t)r * a.k_tok; }, keep);
     };
     typename Bits::Bytes bytes = {}, bytes2 = {};
     if (t0 < t1) {
@@ -113,7 +113,7 @@ __global__ __launch_bounds__((Shape<T, FEW>::THREADS), (FEW || (Shape<T, FEW>::W
     bytes = bytes2;
     if (t0 < t1) {
         request_bias(t0);
-        request(t0, 0, full_d && next.all(), [&](int r) { return next.get(r); });
+        request(t0, full_d && next.all(), [&](int r) { return next.get(r); });
     }
 
     f32x16 o[DT];
@@ -122,22 +122,14 @@ __global__ __launch_bounds__((Shape<T, FEW>::THREADS), (FEW || (Shape<T, FEW>::W
     // base-2 logarithm of the running maximum, a whole number; sum of the lane's half of the keys
     float m = -inf, sum = 0.0f;
     const float to2 = BIAS ? kLog2e : a.scale * kLog2e;
-    // probabilities of the step before and its V: zeros before the first
-    Frag p[NS][GP] = {};
-    const E *vp = vt0 + (L::VBUFS - 1) * L::TILE;
-    auto pv = [&](int b, int g, int d) { Y::mma(o[d], LT::col(vp, (kw * NS + b) * 32 + Y::KS * g, 32 * d, lane), p[b][g]); };
-    if (S::LAG)
-        for (int i = tid; i < L::TILE * (int)sizeof(E) / 16; i += S::THREADS) ((u32x4 *)vp)[i] = u32x4{0, 0, 0, 0};
-    int vbuf = 0;
     for (int step = t0; step < t1; ++step) {
         copies_done_and_barrier();
         now = next;
-        const E *kt = kt0 + (step & 1) * L::TILE, *vt = vt0 + vbuf * L::TILE;
-        vbuf = vbuf == L::VBUFS - 1 ? 0 : vbuf + 1;
+        const E *kt = kt0 + (step & 1) * L::TILE, *vt = vt0 + (step & 1) * L::TILE;
         if (step + 1 < t1) {
             next.set(bytes);
             bytes = Bits::request(mrow, (step + 2) * S::KT, a.Lk, lane);
-            request(step + 1, vbuf, full_d && next.all(), [&](int r) { return next.get(r); });
+            request(step + 1, full_d && next.all(), [&](int r) { return next.get(r); });
         }
         f32x16 s[NS];
         float top = -inf;
@@ -177,38 +169,24 @@ __global__ __launch_bounds__((Shape<T, FEW>::THREADS), (FEW || (Shape<T, FEW>::W
             for (int d = 0; d < DT; ++d)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[d][i] = ldexpf(o[d][i], by);
-            if (S::LAG) {
-#pragma unroll
-                for (int b = 0; b < NS; ++b)
-#pragma unroll
-                    for (int g = 0; g < GP; ++g) p[b][g] = Y::scaled(p[b][g], by);
-            }
             m = higher;
         }
         const float shift = m > -inf ? -m : 0.0f;
-        constexpr int NPV = NS * GP * DT, NE = NS * 16;
-#pragma unroll
-        for (int j = 0; j < NPV; ++j) {
-            if (S::LAG) pv(j / (GP * DT), j / DT % GP, j % DT);
-#pragma unroll
-            for (int e = j * NE / NPV; e < (j + 1) * NE / NPV; ++e) {
-                s[e / 16][e % 16] = __builtin_amdgcn_exp2f(fmaf(s[e / 16][e % 16], to2, shift));
-                sum += s[e / 16][e % 16];
-            }
-        }
 #pragma unroll
         for (int b = 0; b < NS; ++b)
 #pragma unroll
-            for (int g = 0; g < GP; ++g) p[b][g] = Y::pack(s[b], g);
-        vp = vt;
-        if (!S::LAG) {
+            for (int i = 0; i < 16; ++i) {
+                s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], to2, shift));
+                sum += s[b][i];
+            }
 #pragma unroll
-            for (int j = 0; j < NPV; ++j) pv(j / (GP * DT), j / DT % GP, j % DT);
-        }
-    }
-    if (S::LAG && t0 < t1) {
+        for (int b = 0; b < NS; ++b)
 #pragma unroll
-        for (int j = 0; j < NS * GP * DT; ++j) pv(j / (GP * DT), j / DT % GP, j % DT);
+            for (int g = 0; g < GP; ++g) {
+                const Frag p = Y::pack(s[b], g);
+#pragma unroll
+                for (int d = 0; d < DT; ++d) Y::mma(o[d], LT::col(vt, (kw * NS + b) * 32 + Y::KS * g, 32 * d, lane), p);
+            }
     }
 
     sum = half_sum(sum);
