@@ -545,8 +545,8 @@ __global__ __launch_bounds__(kThreads, (BiasShape<T, DP>::WAVES)) void cross_bia
 }
 
 // ---------------------------------------------------------------------------
-// Sums of parts: rows of D channels written at (unit, i) -> token and head, or a flat array (no row
-// stride).  With a second output its parts follow the first's.
+// Sums of parts: rows of D channels written at (unit, i < len) -> token and head, or a flat array
+// (len 0).  With a second output its parts follow the first's.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void cross_sum_kernel(CrArgs a, const float *part, int splits, int64_t stride, int64_t count,
                                                              int len, int group, void *out0, void *out1, int64_t row_stride, int64_t tok_stride) {
@@ -569,7 +569,7 @@ __global__ __launch_bounds__(kThreads) void cross_sum_kernel(CrArgs a, const flo
             for (int e = 0; e < count - at; ++e) sum[e] += p[e];
         }
     }
-    if (!row_stride) {
+    if (!len) {
         for (int e = 0; e < 4 && at + e < count; ++e) ((E *)out)[at + e] = Y::e(sum[e]);
         return;
     }
@@ -637,7 +637,7 @@ template <typename T, int DP> void run(CrArgs a, const CrPlan &p, hipStream_t s)
         cross_bias_kernel<T, DP><<<(uint32_t)(planes * k.tiles * k.ntiles * k.splits), kThreads, 0, s>>>(k);
         if (k.splits > 1) {
             const int64_t count = planes * a.Lq * a.Lk;
-            sum_parts<T>(a, a.part, k.splits, count, count, 1, 0, a.dbias, nullptr, 0, 0, s);
+            sum_parts<T>(a, a.part, k.splits, count, count, 0, 0, a.dbias, nullptr, 0, 0, s);
         }
     }
 }
