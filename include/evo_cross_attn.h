@@ -45,9 +45,9 @@ extern "C" {
 #endif
 
 /* Compiled limits: head_dim a multiple of 8, 8..128; n_heads <= 65535; len_q * (H / Hk) and
- * len_k <= 2^30; element counts <= 2^40; at most 2^31 - 1 workgroups a kernel
- * (n_rows * Hk * ceil(len_q * H / Hk / 32) and n_rows * Hk * ceil(len_k / 128) below that;
- * with a bias also B * H * ceil(len_q / 64) * ceil(len_k / 64)). */
+ * len_k <= 2^30; element counts <= 2^40; fewer than 2^24 workgroups a kernel, that is
+ * n_rows * Hk * ceil(len_q * H / Hk / 128) and n_rows * Hk * ceil(len_k / 128), with a
+ * bias also B * H * ceil(len_q / 64) * ceil(len_k / 64). */
 typedef struct evo_cross_dims {
     int32_t dtype;      /* enum evo_attn_dtype */
     int32_t n_heads;    /* H >= 1 */

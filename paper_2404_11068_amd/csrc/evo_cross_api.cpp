@@ -9,7 +9,8 @@
 
 namespace {
 
-constexpr int64_t kMost = int64_t(1) << 40, kMostLen = int64_t(1) << 30, kGrid = 0x7fffffff;
+constexpr int64_t kMost = int64_t(1) << 40, kMostLen = int64_t(1) << 30;
+constexpr int64_t kGrid = (int64_t(1) << 24) - 1;  // workgroups of 256 threads: a launch counts its threads in 32 bits
 
 bool aligned(const void *p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -56,10 +57,9 @@ int check(const evo_cross_dims *d, bool has_bias, evo::CrArgs *a) {
         if (e) return e;
     }
     // tiles of one unit in any kernel, before splits (which only ever fill up to 512 workgroups)
-    int64_t tiles = up(M, 32) > up(d->len_k, 128) ? up(M, 32) : up(d->len_k, 128);
+    int64_t tiles = up(M, 128) > up(d->len_k, 128) ? up(M, 128) : up(d->len_k, 128);
     if (tiles < 1) tiles = 1;
     if (N > kGrid / tiles / d->n_kv_heads) return EVO_ERR_UNSUPPORTED;
-    if (N * d->len_q > (kGrid * 8) / d->n_heads) return EVO_ERR_UNSUPPORTED;
     *a = evo::CrArgs{};
     a->N = N;
     a->rpb = has_bias ? d->rows_per_bias : (N > 0 ? N : 1);

@@ -125,3 +125,18 @@ def test_binding_refuses_before_any_launch():
         a.update(kw)
         with pytest.raises(ValueError, match=what):
             cross.cross_attn_fwd(**a)
+
+
+@pytest.mark.parametrize("len_q,len_k,most", [(1, 1, 1 << 24), (1, 129, 1 << 23), (129, 1, 1 << 23)])
+def test_launches_count_their_threads_in_32_bits(len_q, len_k, most):
+    # 2^24 workgroups of 256 threads are one too many; a workspace that is missing shows that a call goes on
+    far = {n: FAKE + (i << 38) for i, n in enumerate(("q", "k", "v", "out", "dout", "dq", "dk", "dv", "lse"))}
+    for rows, status in ((most - 1, 4), (most, 2)):
+        d = _dims(n_heads=1, n_kv_heads=1, head_dim=8, n_rows=rows, len_q=len_q, len_k=len_k, q_stride_row=8 * len_q,
+                  q_stride_tok=8, k_stride_row=8 * len_k, k_stride_tok=8, o_stride_row=8 * len_q, o_stride_tok=8)
+        assert _bwd(d, gate=None, bias=None, mask=None, dgate=None, dbias=None, ws=None, **far) == status
+
+
+def test_a_bias_of_too_many_tiles():
+    d = _dims(n_heads=1, n_kv_heads=1, head_dim=8, n_rows=1, len_q=1 << 18, len_k=1 << 18, rows_per_bias=1)
+    assert _fwd(d) == 2 and _bwd(d) == 2
