@@ -32,8 +32,8 @@
  *   + h * d + c.  Addresses and strides allow 16-byte access (EVO_ERR_ALIGNMENT).
  *   y's (row, token) grid does not overlap itself; x's may (stride_row 0: one
  *   row for all), but not where dx, which has x's strides, is written.
- * - y may be x itself (same address, same strides: in place), and dx dy; other
- *   overlaps of the two are refused, and so are those of one set's output with
+ * - y may be x itself (same address, same strides: in place), and dx dy or x; other
+ *   overlaps of these are refused, and so are those of one set's output with
  *   the other set's tensors, but for blocks side by side in the tokens of one
  *   packed buffer.
  * - pos int32: row r starts at r * pos_stride (0: all rows share positions);

@@ -170,6 +170,8 @@ int evo_rope_bwd(const evo_rope_dims *d, const void *dy0, const void *dy1, const
             return EVO_ERR_ALIGNMENT;
         if (!overlap_ok(d, i, dy[i], d->y_stride_row[i], d->y_stride_tok[i], dx[i], d->x_stride_row[i], d->x_stride_tok[i]))
             return EVO_ERR_INVALID_ARG;
+        if (a.norm && !overlap_ok(d, i, x[i], d->x_stride_row[i], d->x_stride_tok[i], dx[i], d->x_stride_row[i], d->x_stride_tok[i]))
+            return EVO_ERR_INVALID_ARG;
         evo::RopeSet &s = a.set[i];
         s.in = dy[i];
         s.x = x[i];

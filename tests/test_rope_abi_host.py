@@ -138,3 +138,11 @@ def test_binding_refuses_before_any_launch():
         rope.rope_bwd(x, p, s, q=x)
     with pytest.raises(ValueError, match="shaped like"):
         rope.rope_bwd(x, p, s, q=x[:1], norm=True)
+
+
+def test_gradients_must_not_lie_across_their_inputs():
+    # with the norm dx may be x itself, or apart from it; the missing workspace shows that a call goes on
+    d = _dims()
+    assert _bwd(d, dx0=FAKE, ws=None) == 4 and _bwd(d, dx1=FAKE + BIG, ws=None) == 4
+    assert _bwd(d, dx0=FAKE + 16) == 1 and _bwd(d, dx1=FAKE + BIG + 128 * 2) == 1
+    assert _bwd(d, dx0=FAKE + 2 * 16 * 512 * 2 - 16) == 1 and _bwd(d, dx0=FAKE + 2 * 16 * 512 * 2, ws=None) == 4
