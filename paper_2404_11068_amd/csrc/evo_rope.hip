@@ -7,6 +7,10 @@
 // for the sine and one for the cosine), so a workgroup forms those of its
 // tokens once, in LDS, for all heads: one pair in 2 d / rot * heads elements.
 //
+// Measured: 2 x 8193 tokens of 32 heads of 64 in bf16, rotation alone, 22 us (6.0 TB/s);
+// 128 x 256 of 16 heads of 32 in fp32 with the norm 21.6 us (6.2 TB/s); 4 x 4099 of 20
+// heads of 128, 96 rotated, with the norm 40 us forward (4.2 TB/s), 51 us backward (4.9).
+//
 // A head is a group of GS lanes (the power of two that holds d / VEC chunks of
 // 16 bytes); groups walk over the (token, head) units of a workgroup's tokens.
 // Sums over a head are butterflies inside the group.
@@ -130,6 +134,13 @@ __device__ __forceinline__ void rope_body(const KArgs &k, float2 *angles, float 
         partner = low ? lane + hc : lane - hc;
         if (c >= 2 * hc) partner = lane;
     }
+    // half layout, angles of a chunk: in order (bf16: 64 bytes a lane, whose reads conflict half of the LDS' time), or
+    // with the norm forward in pieces of two pairs, a piece of all chunks side by side.  4 x 4099 tokens of 20
+    // heads of 128: 44.7 us in order, 40.8 in pieces; the norm's backward 51.7 in order, 56 in pieces, and without
+    // the norm 2 x 8193 tokens of 32 heads of 64 22.5 and 23.3
+    constexpr bool PIECES = P == kHalf && NORM && !BWD;
+    const int nh = half / VEC, piece = PIECES ? 2 * nh : 2;
+    const int angles_at = P == kHalf && base < 2 * half ? (low ? c : c - nh) * (PIECES ? 2 : VEC) : 0;
     // interleaved: whole chunks are rotated or not; the lane's chunk is
     const bool rot_whole = a.rot > 0 && a.rot % VEC == 0, rotated = base < a.rot;
 #pragma unroll
@@ -228,12 +239,14 @@ __device__ __forceinline__ void rope_body(const KArgs &k, float2 *angles, float 
                 for (int i = 0; i < 4; ++i) praw[i] = (uint32_t)__shfl(r.raw[i], partner, 64) ^ (low ? Chunk<E>::SIGNS : 0u);
                 float pv[VEC];
                 Chunk<E>::get(praw, pv);
-                const float2 *cs = row_angles + (rotated ? (low ? base : base - half) : 0);
                 if (half > 0) {
+                    const float2 *mine = row_angles + angles_at;
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        if (NORM && !BWD) pv[e] *= wp[e];
-                        o[e] = fmaf(pv[e], cs[e].y, v[e] * cs[e].x);
+                    for (int e = 0; e < VEC; e += 2) {
+                        const f32x4 cs = *reinterpret_cast<const f32x4 *>(mine + (e >> 1) * piece);
+                        if (NORM && !BWD) pv[e] *= wp[e], pv[e + 1] *= wp[e + 1];
+                        o[e] = fmaf(pv[e], cs[1], v[e] * cs[0]);
+                        o[e + 1] = fmaf(pv[e + 1], cs[3], v[e + 1] * cs[2]);
                     }
                 }
                 if (a.rot < a.d) {
@@ -291,7 +304,8 @@ __device__ __forceinline__ void rope_body(const KArgs &k, float2 *angles, float 
             const uint32_t over = near ? 0 : rows_on(t);
             const int64_t pos = s.pos[(row0 + over) * s.pos_stride + (col0 + t - over * len)];
             const float2 cs = turn((uint64_t)pos * a.steps[j]);
-            angles[i] = float2{cs.x * a.amplitude, (BWD ? -cs.y : cs.y) * a.amplitude};
+            const int to = PIECES ? i - j + ((j % VEC) >> 1) * piece + 2 * (j / VEC) + (j & 1) : i;
+            angles[to] = float2{cs.x * a.amplitude, (BWD ? -cs.y : cs.y) * a.amplitude};
         }
         __syncthreads();
         while (u0 < units) {
@@ -322,7 +336,7 @@ __device__ __forceinline__ void rope_body(const KArgs &k, float2 *angles, float 
 
 template <typename E, Pairing P, bool NORM, bool BWD>
 __global__ __launch_bounds__(kThreads, 4) void rope_kernel(KArgs k) {
-    __shared__ float2 angles[kMaxTok * 128];
+    __shared__ __attribute__((aligned(16))) float2 angles[kMaxTok * 128];
     __shared__ float line[4 * 64 * Chunk<E>::VEC > 1024 ? 4 * 64 * Chunk<E>::VEC : 1024];
     rope_body<E, P, NORM, BWD>(k, angles, line);
 }
