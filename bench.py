@@ -1026,7 +1026,9 @@ KERNEL_SOURCES = {"attn": ("evo_frag.h", "evo_fwd.hip", "evo_bwd.hip", "evo_bwd_
                   "pb_bwd": ("evo_frag.h", "evo_pair_bias_bwd.hip"),
                   "optim": ("evo_frag.h", "evo_optim.hip"),
                   "relpos": ("evo_frag.h", "evo_relpos.hip"),
-                  "muon": ("evo_frag.h", "evo_ns.h", "evo_muon.hip")}
+                  "muon": ("evo_frag.h", "evo_ns.h", "evo_muon.hip"),
+                  "rope": ("evo_frag.h", "evo_rope_kernels.h", "evo_rope.hip"),
+                  "cross": ("evo_frag.h", "evo_cross.h", "evo_cross_fwd.hip", "evo_cross_short.hip", "evo_cross_bwd.hip")}
 
 
 def kernel_family(kernel: str) -> str:
@@ -1044,6 +1046,10 @@ def kernel_family(kernel: str) -> str:
         return "relpos"
     if kernel.startswith("ns_"):
         return "muon"
+    if kernel.startswith("rope_"):
+        return "rope"
+    if kernel.startswith("cross_"):
+        return "cross"
     return "ln" if kernel.startswith("ln_") else "attn"
 
 
