@@ -262,3 +262,24 @@ def test_empty_sets():
     g = rope.rope_bwd(k[:0], p3[:0], s, q=k[:0], norm=True, weight_q=w, dweight_q=dw.fill_(3.0))
     torch.cuda.synchronize()
     assert not dw.any()
+
+
+@pytest.mark.parametrize("rot", [64, 48, 40], ids=["whole", "part", "odd"])
+@pytest.mark.parametrize("interleaved", [False, True], ids=["half", "interleaved"])
+def test_gradients_in_the_place_of_their_heads(rot, interleaved):
+    # with the norm dx may be written over x, or over dy: the same bits as into tensors of its own
+    rng = np.random.default_rng(11)
+    dt = torch.bfloat16
+    q, dq = (torch.tensor(rng.standard_normal((3, 517, 5, 64)), dtype=dt, device="cuda") for _ in range(2))
+    k, dk = (torch.tensor(rng.standard_normal((3, 33, 2, 64)), dtype=dt, device="cuda") for _ in range(2))
+    w = torch.tensor(rng.standard_normal(64), dtype=torch.float32, device="cuda")
+    pos = torch.arange(517, dtype=torch.int32, device="cuda")
+    steps = rope.rope_steps(rope.rope_frequencies(rot))
+    kw = dict(pos_k=pos[:33], norm=True, interleaved=interleaved, weight_q=w, weight_k=w)
+    want = rope.rope_bwd(dq, pos, steps, dk=dk, q=q, k=k, **kw)
+    q2, k2, dq2, dk2 = (t.clone() for t in (q, k, dq, dk))
+    over_x = rope.rope_bwd(dq, pos, steps, dk=dk, q=q2, k=k2, out_q=q2, out_k=k2, **kw)
+    over_dy = rope.rope_bwd(dq2, pos, steps, dk=dk2, q=q, k=k, out_q=dq2, out_k=dk2, **kw)
+    for a, b, c in zip(want, over_x, over_dy):
+        assert torch.equal(a, b) and torch.equal(a, c)
+    assert torch.equal(want[0], q2) and torch.equal(want[1], dk2)
