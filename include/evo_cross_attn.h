@@ -20,7 +20,8 @@
  *   gradients and sigmoid(gate) * dO are rounded to it once), sums, softmax and
  *   log-sum-exp fp32, results rounded once.  fp32: fp32 throughout.
  * - Every sum runs in a fixed order without atomics: repeated calls give
- *   identical bits.  How the work is split depends on the dims alone.
+ *   identical bits.  How the work is split depends on the dims and on whether
+ *   there is a bias alone.
  *
  * Conventions (dtype and status codes from evo_attn.h): device pointers owned
  * by the caller; nothing is allocated or synchronised; the calls enqueue

@@ -98,19 +98,21 @@ Range flat(const void *p, int64_t bytes) { return Range{(uintptr_t)p, (uintptr_t
 namespace evo {
 
 // How many workgroups share one tile's walk of `steps`: the count of the lowest
-// estimated time, in us.  The steps of the fullest CU count (two workgroups on a CU
-// take 1.3 times one's rate), `one` us each, and a join: a launch, and the
-// parts (bytes of one) written and read once.  The rates are those measured at 32, 64 and
-// 128 channels; e.g. 264 tiles of 65 steps at 64 channels: 83 us unsplit, 87, 74, 78, 73, 88
-// with 2, 3, 4, 5 and 8 (estimated 91, 80, 75, 75, 74, 82).
-static int split(int64_t tiles, int64_t steps, double one, double bytes, double launch) {
+// estimated time, in us.  The workgroups of the fullest CU count (several on a CU have `rate`
+// times one's), each 1.5 to begin with and `one` a step; n parts take a launch (5), 0.15 each to be
+// read in turn, and their bytes (of one part) at 2 TB/s, the forward's at 5.5 where others are
+// still at work while they are written.  Fitted to calls of 32, 64 and 128 channels; e.g.
+// forward, 264 tiles of 65 steps at 64 channels: 82 us unsplit, 72, 69, 66, 65, 67 and 71 with 2, 3, 4, 5, 6
+// and 8 (estimated 85, 76, 71, 71, 70, 72, 81).
+static int split(int64_t tiles, int64_t steps, double one, double bytes, double rate, bool forward) {
     if (tiles <= 0 || steps <= 1) return 1;
     int best = 1;
     double least = 0.0;
     for (int64_t n = 1; n <= steps && n <= 64; ++n) {
         const int64_t per = up(steps, n), load = up(tiles * n, 256);
         if (up(steps, per) != n) continue;
-        const double cost = load * per * one / (load > 1 ? 1.3 : 1.0) + (n > 1 ? launch + n * bytes / 2e6 : 0.0);
+        const double join = 5.0 + n * (0.15 + bytes / (forward && load > 2 ? 5.5e6 : 2e6));
+        const double cost = load * (1.5 + per * one) / (load > 1 ? rate : 1.0) + (n > 1 ? join : 0.0);
         if (n == 1 || cost < least) best = (int)n, least = cost;
         if (load > 16) break;  // the GPU is full
     }
@@ -123,23 +125,26 @@ CrPlan cross_plan(const CrArgs &a, bool has_gate, bool has_bias) {
     const int few_rows = a.bf16 ? 32 : 64;
     const int64_t key_steps = up(a.Lk, a.bf16 ? 64 : 32);
     const double rows_bytes = 4.0 * units * a.M * a.D, keys_bytes = 8.0 * units * a.Lk * a.D;
-    // us a step of the forward: 128 queries by 64 keys, fp32 by 32
+    // us a step of the forward: 128 queries by 64 keys, fp32 by 32 (two products at the rate of its matrix
+    // instructions); the lanes' rows of a bias take half a us more
     const int d = a.D <= 32 ? 32 : a.D <= 64 ? 64 : 128;
-    const double one = 0.35 + (a.bf16 ? 0.0088 : 0.0155) * d;
+    const double rate = a.bf16 ? 1.3 : 1.0;  // one workgroup keeps fp32's matrix instructions busy
+    const double bias_step = has_bias && a.bf16 ? 0.5 : 0.0;
+    const double one = (a.bf16 ? 0.33 + 0.0078 * d : 0.1 + 0.031 * d) + bias_step;
     p.few = a.M <= few_rows;
     const int64_t tiles = up(a.M, p.few ? few_rows : 128);
     if (p.few) {
         // reading K and V is all there is to do: two workgroups a CU, of four steps at least.  16 rows of 4 key
-        // heads to 4097 keys of 128 channels: 64 us unsplit, 41, 26, 24 and 29 with 2, 4, 8 and 12
+        // heads to 4097 keys of 128 channels: 64 us unsplit, 41, 25, 24 and 28 with 2, 4, 8 and 12
         int64_t n = units * tiles > 0 ? 512 / (units * tiles) : 1;
         if (n > key_steps / 4) n = key_steps / 4;
         p.fwd_splits = n < 2 ? 1 : (int)up(key_steps, up(key_steps, n));
     } else {
-        p.fwd_splits = split(units * tiles, key_steps, one, rows_bytes, 5.0);
+        p.fwd_splits = split(units * tiles, key_steps, one, rows_bytes, rate, true);
     }
     // few keys: a workgroup (or, for up to 32 queries, a wave) walks over rows of the batch, where there are
-    // enough.  At 8 heads of 32, 256 queries, 77 keys, gate and bias: 128 rows 22 us (36 by a workgroup a
-    // row), 64 rows 14 (21); 65536 rows of one query to 4 keys, 4 heads of 16: 155 (483)
+    // enough.  At 8 heads of 32, 256 queries, 77 keys, gate and bias: 128 rows 22 us (34 by a workgroup a
+    // row), 64 rows 15 (19); 65536 rows of one query to 4 keys, 4 heads of 16: 151 (398)
     if (a.Lk > 0 && a.Lk <= 128) {
         p.brief_one = a.M <= 32 && units >= 4096 && 16 * up(a.Lk, 32) * 32 * d * (a.bf16 ? 2 : 4) <= 128 * 1024;
         p.brief = p.brief_one || (a.bf16 && a.D <= 32 && a.M > 32 && units * tiles >= 1024);
@@ -157,13 +162,17 @@ CrPlan cross_plan(const CrArgs &a, bool has_gate, bool has_bias) {
         p.fwd_ml = pad((size_t)p.fwd_splits * units * a.M * a.D * 4);
         p.fwd_total = p.fwd_ml + pad((size_t)p.fwd_splits * units * a.M * 8);
     }
-    p.kv_splits = split(units * up(a.Lk, 128), up(a.M, a.bf16 && a.D <= 64 ? 64 : 32), 1.3 * one, keys_bytes, 5.0);
+    // steps of the backward's passes; the keys' four products (128 keys by 64 queries, or 32), the rows' three
+    // (128 queries by 64 keys, or 32), a row of the batch for 64 x 64 entries of the bias
+    const double step = a.bf16 ? 0.35 + 0.0088 * d : 0.1 + 0.031 * d;
     const bool wide_steps = a.bf16 && a.D <= 64 && !has_bias;
-    p.q_splits = split(units * up(a.M, 128), up(a.Lk, wide_steps ? 64 : 32), (wide_steps || !a.bf16 ? 1.2 : 0.6) * one, rows_bytes, 5.0);
+    p.kv_splits = split(units * up(a.Lk, 128), up(a.M, a.bf16 && a.D <= 64 ? 64 : 32), (a.bf16 ? 1.3 : 2.1) * step, keys_bytes, rate, false);
+    p.q_splits = split(units * up(a.M, 128), up(a.Lk, wide_steps ? 64 : 32),
+                       (a.bf16 ? wide_steps ? 1.2 : 0.6 : 1.6) * step + bias_step, rows_bytes, rate, false);
     p.bias_chunks = 1;
     if (has_bias) {
         const int64_t bias_tiles = a.N / a.rpb * a.H * up(a.Lq, 64) * up(a.Lk, 64);
-        p.bias_chunks = split(bias_tiles, a.rpb, 1.2 * one, 4.0 * (a.N / a.rpb) * a.H * a.Lq * (double)a.Lk, 5.0);
+        p.bias_chunks = split(bias_tiles, a.rpb, 1.2 * step, 4.0 * (a.N / a.rpb) * a.H * a.Lq * (double)a.Lk, rate, false);
     }
     p.bwd_da = pad((size_t)units * a.M * 4);
     p.bwd_part = p.bwd_da + (has_gate ? pad((size_t)units * a.M * a.D * (a.bf16 ? 2 : 4)) : 0);
@@ -185,7 +194,9 @@ extern "C" {
 size_t evo_cross_fwd_workspace_size(const evo_cross_dims *d) {
     evo::CrArgs a;
     if (check(d, false, &a) || a.N == 0 || a.Lq == 0) return 0;
-    return evo::cross_plan(a, false, false).fwd_total;
+    // with a bias there may be more splits
+    const size_t plain = evo::cross_plan(a, false, false).fwd_total, bias = evo::cross_plan(a, false, true).fwd_total;
+    return plain > bias ? plain : bias;
 }
 
 int evo_cross_fwd(const evo_cross_dims *d, const void *q, const void *k, const void *v, const void *gate, const void *bias,
