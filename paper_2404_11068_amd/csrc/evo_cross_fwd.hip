@@ -23,7 +23,7 @@
 // channels: 4096 queries to 8191 keys, 16 heads, bf16, 277 us (990 TFLOP/s); at 64 channels
 // 2 x 4096 to 4096, 16 heads, 167 us (825), at 32 112 us (610).  fp32 runs at 101 to 116 of the
 // 150 TFLOP/s of a library product.  Single tokens are bound by memory: 16 rows, 16 / 4
-// heads of 128, 4097 keys 20.7 + 4.0 us (4.5 TB/s of the kept keys).
+// heads of 128, 4097 keys 20.1 + 4.0 us (4.6 TB/s of the kept keys).
 #include "evo_cross.h"
 
 namespace evo {
