@@ -160,7 +160,8 @@ CrPlan cross_plan(const CrArgs &a, bool has_gate, bool has_bias) {
     if (p.fwd_splits > 1) {
         p.fwd_part = 0;
         p.fwd_ml = pad((size_t)p.fwd_splits * units * a.M * a.D * 4);
-        p.fwd_total = p.fwd_ml + pad((size_t)p.fwd_splits * units * a.M * 8);
+        p.fwd_lo = p.fwd_ml + pad((size_t)p.fwd_splits * units * a.M * 8);
+        p.fwd_total = p.fwd_lo + pad((size_t)p.fwd_splits * units * a.M * 4);
     }
     // steps of the backward's passes; the keys' four products (128 keys by 64 queries, or 32), the rows' three
     // (128 queries by 64 keys, or 32), a row of the batch for 64 x 64 entries of the bias

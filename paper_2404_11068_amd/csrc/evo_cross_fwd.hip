@@ -17,7 +17,8 @@
 // workgroups whose partial results a second kernel joins.
 //
 // The running maximum is kept on whole powers of two (its base-2 logarithm is an
-// integer): rescaling is then exact.
+// integer): rescaling is then exact.  Far from zero, where fp32 has no such numbers, it is
+// kept as two (Ref).
 //
 // Long calls keep the matrix and the vector unit busy 48 and 54% of the time at 128
 // channels: 4096 queries to 8191 keys, 16 heads, bf16, 277 us (990 TFLOP/s); at 64 channels
@@ -42,7 +43,7 @@ template <typename T, bool FEW> struct Shape {
 template <typename T, int DP, bool FEW> struct Lds {
     using S = Shape<T, FEW>;
     static constexpr int TILE = S::KT * DP, SIZE = 4 * TILE * (int)sizeof(typename Ty<T>::E);
-    static_assert(S::KW == 1 || 2 * (DP / 32 * 16 + 2) * 256 <= SIZE, "the waves' results fit, at the end");
+    static_assert(S::KW == 1 || 2 * (DP / 32 * 16 + 3) * 256 <= SIZE, "the waves' results fit, at the end");
 };
 
 template <typename T, int DP, bool BIAS, bool FEW>
@@ -125,8 +126,10 @@ __global__ __launch_bounds__((Shape<T, FEW>::THREADS), (FEW || (Shape<T, FEW>::W
     f32x16 o[DT];
 #pragma unroll
     for (int i = 0; i < DT; ++i) o[i] = zero16();
-    // base-2 logarithm of the running maximum, a whole number; sum of the lane's half of the keys
-    float m = -inf, sum = 0.0f;
+    // what the running sums are against, as -hi and lo (0, 0 before the first key), how far a logit may rise above it, whether
+    // it is far from zero for any of the wave's queries; sum of the lane's half of the keys
+    float shift = 0.0f, lo = 0.0f, lag = -inf, sum = 0.0f;
+    bool far = false;
     const float to2 = BIAS ? kLog2e : a.scale * kLog2e;
     for (int step = t0; step < t1; ++step) {
         copies_done_and_barrier();
@@ -164,25 +167,50 @@ __global__ __launch_bounds__((Shape<T, FEW>::THREADS), (FEW || (Shape<T, FEW>::W
 #pragma unroll
             for (int i = 0; i < 16; i += 2) top = fmaxf(fmaxf(top, s[b][i]), s[b][i + 1]);
         if (BIAS && step + 1 < t1) request_bias(step + 1);
-        top = half_max(top) * to2;
+        top = half_max(top);
         // the reference rises only when it has fallen behind by 2^8: sums and probabilities
         // stay within fp32 and keep their relative precision
-        if (__any(top > m + 8.0f)) {
-            const float higher = fmaxf(m, __builtin_ceilf(top)), to = higher > -inf ? higher : 0.0f;
-            const int by = (int)fmaxf((m > -inf ? m : to) - to, -1000.0f);
-            sum = ldexpf(sum, by);
+        float over = fmaf(top, to2, shift);
+        if (far) over -= lo;
+        if (__any(over > lag)) {
+            const bool had = lag > 0.0f;
+            Ref to = {-shift, lo};
+            if (over > (had ? 0.0f : -inf)) {
+                to = reference(top, to2);
+                lag = 8.0f;
+            }
+            const float by = had ? (-shift - to.hi) + (lo - to.lo) : 0.0f, whole = __builtin_rintf(by);
+            const int n = (int)fmaxf(whole, -1000.0f);
+            sum = ldexpf(sum, n);
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) o[d][i] = ldexpf(o[d][i], by);
-            m = higher;
+                for (int i = 0; i < 16; ++i) o[d][i] = ldexpf(o[d][i], n);
+            if (__any(by != whole)) {
+                const float f = __builtin_amdgcn_exp2f(by - whole);
+                sum *= f;
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[d][i] *= f;
+            }
+            shift = -to.hi;
+            lo = to.lo;
+            far = __any(lo != 0.0f);
         }
-        const float shift = m > -inf ? -m : 0.0f;
+        float times = to2, plus = shift;
+        if (far) {
+#pragma unroll
+            for (int b = 0; b < NS; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[b][i] = fmaf(s[b][i], to2, shift) - lo;
+            times = 1.0f, plus = 0.0f;
+        }
 #pragma unroll
         for (int b = 0; b < NS; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], to2, shift));
+                s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], times, plus));
                 sum += s[b][i];
             }
 #pragma unroll
@@ -196,31 +224,35 @@ __global__ __launch_bounds__((Shape<T, FEW>::THREADS), (FEW || (Shape<T, FEW>::W
     }
 
     sum = half_sum(sum);
+    Ref ref = {lag > 0.0f ? -shift : -inf, lo};
     if (S::KW > 1) {
         // the two waves' maxima, sums and results, joined: wave kw takes every other block of channels
         float *all = (float *)lds;
-        constexpr int PER = DT * 16 + 2;
+        constexpr int PER = DT * 16 + 3;
         __syncthreads();
         float *mine = all + wave * PER * 64 + lane;
-        mine[0] = m;
-        mine[64] = sum;
+        mine[0] = ref.hi;
+        mine[64] = ref.lo;
+        mine[128] = sum;
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) mine[(2 + d * 16 + i) * 64] = o[d][i];
+            for (int i = 0; i < 16; ++i) mine[(3 + d * 16 + i) * 64] = o[d][i];
         __syncthreads();
-        float mj[S::KW], top = -inf;
+        Ref rj[S::KW];
+        float mj[S::KW];
+        ref = Ref{-inf, 0.0f};
 #pragma unroll
         for (int j = 0; j < S::KW; ++j) {
-            mj[j] = all[(j * S::QW + qw) * PER * 64 + lane];
-            top = fmaxf(top, mj[j]);
+            const float *from = all + (j * S::QW + qw) * PER * 64 + lane;
+            rj[j] = Ref{from[0], from[64]};
+            if (above(rj[j], ref)) ref = rj[j];
         }
-        m = top;
         sum = 0.0f;
 #pragma unroll
         for (int j = 0; j < S::KW; ++j) {
-            mj[j] = mj[j] > -inf ? __builtin_amdgcn_exp2f(mj[j] - top) : 0.0f;
-            sum += mj[j] * all[(j * S::QW + qw) * PER * 64 + 64 + lane];
+            mj[j] = rj[j].hi > -inf ? __builtin_amdgcn_exp2f((rj[j].hi - ref.hi) + (rj[j].lo - ref.lo)) : 0.0f;
+            sum += mj[j] * all[(j * S::QW + qw) * PER * 64 + 128 + lane];
         }
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
@@ -229,7 +261,7 @@ __global__ __launch_bounds__((Shape<T, FEW>::THREADS), (FEW || (Shape<T, FEW>::W
             for (int i = 0; i < 16; ++i) {
                 float v = 0.0f;
 #pragma unroll
-                for (int j = 0; j < S::KW; ++j) v += mj[j] * all[((j * S::QW + qw) * PER + 2 + d * 16 + i) * 64 + lane];
+                for (int j = 0; j < S::KW; ++j) v += mj[j] * all[((j * S::QW + qw) * PER + 3 + d * 16 + i) * 64 + lane];
                 o[d][i] = v;
             }
         }
@@ -237,7 +269,7 @@ __global__ __launch_bounds__((Shape<T, FEW>::THREADS), (FEW || (Shape<T, FEW>::W
     if (!on) return;
     if (a.splits > 1) {
         const int64_t row = ((int64_t)split * a.N * a.Hk + unit) * a.M + x;
-        if (kw == 0 && h == 0) a.part_ml[row] = float2{m, sum};
+        if (kw == 0 && h == 0) a.part_ml[row] = float2{ref.hi, sum}, a.part_lo[row] = ref.lo;
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
             if (S::KW > 1 && d % S::KW != kw) continue;
@@ -249,10 +281,9 @@ __global__ __launch_bounds__((Shape<T, FEW>::THREADS), (FEW || (Shape<T, FEW>::W
         }
         return;
     }
-    if (BIAS && m < kNoKey) sum = 0.0f;
+    if (BIAS && ref.hi < kNoKey) sum = 0.0f;
     const float inv = sum > 0.0f ? 1.0f / sum : sum;
-    if (kw == 0 && h == 0)
-        a.lse[(n * a.H + head) * a.Lq + t] = sum == 0.0f ? -inf : (__builtin_amdgcn_logf(sum) + m) * kLn2;
+    if (kw == 0 && h == 0) a.lse[(n * a.H + head) * a.Lq + t] = log_of(sum, ref);
     E *orow = (E *)a.out + n * a.o_row + (int64_t)t * a.o_tok + (int64_t)head * a.D;
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
@@ -290,23 +321,42 @@ __global__ __launch_bounds__(kJoinThreads) void cross_join_kernel(CrArgs a, int 
     const int64_t tok = (int64_t)head * a.D + c;
     Four<E> gv = {};
     if (a.gate) gv = load4((const E *)a.gate + n * a.q_row + (int64_t)t * a.q_tok + tok);
-    // running maximum and sum over the splits, read ahead
-    float top = -__builtin_inff(), sum = 0.0f;
+    // reference and sum over the splits, read ahead
+    const float inf = __builtin_inff();
+    Ref ref = {-inf, 0.0f};
+    float sum = 0.0f;
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
     for (int j = 0; j < a.splits; ++j) {
         const float2 ml = a.part_ml[j * rows + row];
         const f32x4 p = *reinterpret_cast<const f32x4 *>(a.part + (j * rows + row) * a.D + c);
-        const float higher = fmaxf(top, ml.x), to = higher > -__builtin_inff() ? higher : 0.0f;
-        const float f = __builtin_amdgcn_exp2f(ml.x - to), old = __builtin_amdgcn_exp2f(top - to);
+        const float higher = fmaxf(ref.hi, ml.x), to = higher > -inf ? higher : 0.0f;
+        const float f = __builtin_amdgcn_exp2f(ml.x - to), old = __builtin_amdgcn_exp2f(ref.hi - to);
         sum = fmaf(ml.y, f, sum * old);
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[i] = fmaf(p[i], f, o[i] * old);
-        top = higher;
+        ref.hi = higher;
     }
-    if (has_bias && top < kNoKey) sum = 0.0f;
+    // (next to a reference near zero those far off count nothing, whatever their lo)
+    if (fabsf(ref.hi) >= kFar && ref.hi > -inf) {
+        ref = Ref{-inf, 0.0f};
+        sum = 0.0f;
+        o = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int j = 0; j < a.splits; ++j) {
+            const float2 ml = a.part_ml[j * rows + row];
+            const Ref r = {ml.x, a.part_lo[j * rows + row]};
+            if (r.hi == -inf) continue;
+            const Ref to = above(r, ref) ? r : ref;
+            const float f = __builtin_amdgcn_exp2f((r.hi - to.hi) + (r.lo - to.lo)), old = __builtin_amdgcn_exp2f((ref.hi - to.hi) + (ref.lo - to.lo));
+            sum = fmaf(ml.y, f, sum * old);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = fmaf(a.part[(j * rows + row) * a.D + c + i], f, o[i] * old);
+            ref = to;
+        }
+    }
+    if (has_bias && ref.hi < kNoKey) sum = 0.0f;
     const float inv = sum > 0.0f ? 1.0f / sum : sum;
-    if (c == 0) a.lse[(n * a.H + head) * a.Lq + t] = sum == 0.0f ? -__builtin_inff() : (__builtin_amdgcn_logf(sum) + top) * kLn2;
+    if (c == 0) a.lse[(n * a.H + head) * a.Lq + t] = log_of(sum, ref);
     E e[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -344,6 +394,7 @@ hipError_t launch_cross_fwd(CrArgs a, const CrPlan &p, void *ws, hipStream_t s) 
     a.splits = p.fwd_splits;
     a.part = (float *)((char *)ws + p.fwd_part);
     a.part_ml = (float2 *)((char *)ws + p.fwd_ml);
+    a.part_lo = (float *)((char *)ws + p.fwd_lo);
     a.bf16 ? launch_dim<bf16_t>(a, p.few, s) : launch_dim<float>(a, p.few, s);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;

@@ -158,9 +158,19 @@ __global__ __launch_bounds__(kThreads, (ShortLds<T, DP, NB, ONE>::SIZE > 80 * 10
 #pragma unroll
             for (int i = 0; i < 16; i += 2) top = fmaxf(fmaxf(top, s[b][i]), s[b][i + 1]);
         }
-        // a whole power of two, as in the kernel for many keys
-        top = __builtin_ceilf(half_max(top) * to2);
-        const float shift = top > -inf ? -top : 0.0f;
+        // what the sums are against, as in the kernel for many keys
+        top = half_max(top);
+        Ref ref = {__builtin_ceilf(top * to2), 0.0f};
+        const bool far = __any(fabsf(top * to2) >= kFar && top > -inf);
+        float times = to2, plus = top > -inf ? -ref.hi : 0.0f;
+        if (far) {
+            if (top > -inf) ref = reference(top, to2), plus = -ref.hi;
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[b][i] = fmaf(s[b][i], to2, plus) - ref.lo;
+            times = 1.0f, plus = 0.0f;
+        }
         float sum = 0.0f;
         f32x16 o[DT];
 #pragma unroll
@@ -169,7 +179,7 @@ __global__ __launch_bounds__(kThreads, (ShortLds<T, DP, NB, ONE>::SIZE > 80 * 10
         for (int b = 0; b < NB; ++b) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], to2, shift));
+                s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], times, plus));
                 sum += s[b][i];
             }
 #pragma unroll
@@ -180,11 +190,10 @@ __global__ __launch_bounds__(kThreads, (ShortLds<T, DP, NB, ONE>::SIZE > 80 * 10
             }
         }
         sum = half_sum(sum);
-        if (BIAS && top < kNoKey) sum = 0.0f;
+        if (BIAS && ref.hi < kNoKey) sum = 0.0f;
         const float inv = sum > 0.0f ? 1.0f / sum : sum;
         copies_done();
-        if (h == 0 && on)
-            a.lse[(n * a.H + head) * a.Lq + t] = sum == 0.0f ? -inf : (__builtin_amdgcn_logf(sum) + top) * kLn2;
+        if (h == 0 && on) a.lse[(n * a.H + head) * a.Lq + t] = log_of(sum, ref);
         E *orow = (E *)a.out + n * a.o_row + oat;
 #pragma unroll
         for (int j = 0; j < DT * 2; ++j) {
