@@ -55,7 +55,7 @@ hipError_t launch_cross_short(CrArgs a, const CrPlan &p, hipStream_t s);
 hipError_t launch_cross_bwd(CrArgs a, const CrPlan &p, void *ws, hipStream_t s);
 #if defined(__HIPCC__)
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-// A query whose largest logit with its bias is below this has no key left: a
+// A query whose largest logit (natural, with its bias) is not above this has no key left: a
 // bias of the type's lowest value everywhere is a mask, like -infinity.
 constexpr float kNoKey = -1e30f;
 

@@ -168,6 +168,7 @@ __global__ __launch_bounds__((Shape<T, FEW>::THREADS), (FEW || (Shape<T, FEW>::W
             for (int i = 0; i < 16; i += 2) top = fmaxf(fmaxf(top, s[b][i]), s[b][i + 1]);
         if (BIAS && step + 1 < t1) request_bias(step + 1);
         top = half_max(top);
+        if ((BIAS ? top : top * a.scale) <= kNoKey) top = -inf;  // no key: such logits give exp2(-inf) against 0, too
         // the reference rises only when it has fallen behind by 2^8: sums and probabilities
         // stay within fp32 and keep their relative precision
         float over = fmaf(top, to2, shift);
@@ -281,7 +282,6 @@ __global__ __launch_bounds__((Shape<T, FEW>::THREADS), (FEW || (Shape<T, FEW>::W
         }
         return;
     }
-    if (BIAS && ref.hi < kNoKey) sum = 0.0f;
     const float inv = sum > 0.0f ? 1.0f / sum : sum;
     if (kw == 0 && h == 0) a.lse[(n * a.H + head) * a.Lq + t] = log_of(sum, ref);
     E *orow = (E *)a.out + n * a.o_row + (int64_t)t * a.o_tok + (int64_t)head * a.D;
@@ -308,7 +308,7 @@ __global__ __launch_bounds__((Shape<T, FEW>::THREADS), (FEW || (Shape<T, FEW>::W
 
 // Joins the splits of a row: one thread per four channels
 template <typename T>
-__global__ __launch_bounds__(kJoinThreads) void cross_join_kernel(CrArgs a, int has_bias, int64_t rows) {
+__global__ __launch_bounds__(kJoinThreads) void cross_join_kernel(CrArgs a, int64_t rows) {
     using Y = Ty<T>;
     using E = typename Y::E;
     const int per = a.D / 4;
@@ -354,7 +354,6 @@ __global__ __launch_bounds__(kJoinThreads) void cross_join_kernel(CrArgs a, int 
             ref = to;
         }
     }
-    if (has_bias && ref.hi < kNoKey) sum = 0.0f;
     const float inv = sum > 0.0f ? 1.0f / sum : sum;
     if (c == 0) a.lse[(n * a.H + head) * a.Lq + t] = log_of(sum, ref);
     E e[4];
@@ -401,9 +400,9 @@ hipError_t launch_cross_fwd(CrArgs a, const CrPlan &p, void *ws, hipStream_t s) 
     const int64_t rows = a.N * a.Hk * a.M, threads = rows * (a.D / 4);
     const uint32_t grid = (uint32_t)((threads + kJoinThreads - 1) / kJoinThreads);
     if (a.bf16)
-        cross_join_kernel<bf16_t><<<grid, kJoinThreads, 0, s>>>(a, a.bias != nullptr, rows);
+        cross_join_kernel<bf16_t><<<grid, kJoinThreads, 0, s>>>(a, rows);
     else
-        cross_join_kernel<float><<<grid, kJoinThreads, 0, s>>>(a, a.bias != nullptr, rows);
+        cross_join_kernel<float><<<grid, kJoinThreads, 0, s>>>(a, rows);
     return hipGetLastError();
 }
 

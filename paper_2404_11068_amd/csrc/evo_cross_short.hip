@@ -160,6 +160,7 @@ __global__ __launch_bounds__(kThreads, (ShortLds<T, DP, NB, ONE>::SIZE > 80 * 10
         }
         // what the sums are against, as in the kernel for many keys
         top = half_max(top);
+        if ((BIAS ? top : top * a.scale) <= kNoKey) top = -inf;
         Ref ref = {__builtin_ceilf(top * to2), 0.0f};
         const bool far = __any(fabsf(top * to2) >= kFar && top > -inf);
         float times = to2, plus = top > -inf ? -ref.hi : 0.0f;
@@ -190,7 +191,6 @@ __global__ __launch_bounds__(kThreads, (ShortLds<T, DP, NB, ONE>::SIZE > 80 * 10
             }
         }
         sum = half_sum(sum);
-        if (BIAS && ref.hi < kNoKey) sum = 0.0f;
         const float inv = sum > 0.0f ? 1.0f / sum : sum;
         copies_done();
         if (h == 0 && on) a.lse[(n * a.H + head) * a.Lq + t] = log_of(sum, ref);

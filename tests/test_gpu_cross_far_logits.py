@@ -22,7 +22,7 @@ from tests.test_gpu_cross import F, _bounds, _check, _close, _draw
 
 pytestmark = pytest.mark.gpu
 DTYPES = pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
-LOW = [-1e6, -1e8, -1e10, -1e15, -1e20, -1.2e30, -1e35, "half"]
+LOW = [-1e6, -1e8, -1e10, -1e15, -1e20, -0.9e30, -1.2e30, -1e35, "half"]
 # N, Lq, Lk, H, Hk, d, copies: single tokens, tiles of queries, the keys split over workgroups, and rows of the batch walked
 # over (as often as the last number says the same ones)
 SHAPES = [(2, 1, 200, 4, 4, 32, 1), (2, 70, 200, 4, 2, 64, 1), (1, 40, 3000, 2, 2, 128, 1), (1, 1, 3000, 2, 1, 128, 1),
@@ -138,6 +138,23 @@ def test_far_keys_in_order(shape, dtype):
         args[4][:, 2] = (-(10.0 ** e)).to(dtype)
         args[4][:, 3] = torch.finfo(dtype).max
     _check_far(args, backward=False, copies=copies)
+
+
+@DTYPES
+def test_the_edge_of_no_key(dtype):
+    """A natural logit of -1e30: the numbers next to it on both sides."""
+    N, Lq, Lk, H, d = 2, 6, 90, 2, 32
+    args = _draw((N, Lq, Lk, H, H, d, False, 1, None), dtype, 24)
+    _apart(*args[:2])
+    at = torch.tensor(-1e30, dtype=dtype, device="cuda")
+    up, down = torch.nextafter(at, torch.zeros_like(at)), torch.nextafter(at, torch.full_like(at, -float("inf")))
+    near = torch.stack([torch.nextafter(up, torch.zeros_like(at)), up, at, down, torch.nextafter(down, torch.full_like(at, -float("inf"))),
+                        torch.tensor(-0.8e30, dtype=dtype, device="cuda")])
+    args[4][:] = near.view(1, 1, Lq, 1)
+    for copies, keys in ((1, Lk), (1024, 50)):
+        some = args[:1] + tuple(t[:, :keys].contiguous() for t in args[1:3]) + (None, args[4][..., :keys].contiguous(), None, args[6])
+        _check_far(some, backward=False, copies=copies)
+    assert float(near[5]) > -1e30 > float(near[4])
 
 
 def _same_keys(N, Lq, Lk, H, d, size, dtype, seed):
