@@ -16,6 +16,9 @@
  * - A query with nothing left to attend to gets o = 0, lse = -inf and zero
  *   gradients: all keys masked, Lk == 0, or no logit above -1e30 (a bias of
  *   -inf or of the type's lowest value at every key is a mask).
+ * - Logits are fp32 numbers, and softmax and gradients those of these numbers however far
+ *   from zero they lie (at -1e9 a step is 64: equal biases there make keys equally
+ *   likely, whatever q k' is).
  * - bf16: inputs to the matrix products are bf16 (the probabilities, their
  *   gradients and sigmoid(gate) * dO are rounded to it once), sums, softmax and
  *   log-sum-exp fp32, results rounded once.  fp32: fp32 throughout.

@@ -23,8 +23,8 @@ struct CrArgs {
     float *lse;
     // backward
     const void *dout;
-    void *da;        // sigmoid(gate) * dout, contiguous [N, Lq, H, d] (with a gate)
-    float *dsum;     // [N, Hk, M]
+    void *da;        // sigmoid(gate) * dout, contiguous [N, Lq, H, d] (with a gate or a bias)
+    f32x4 *stats;    // [N, Hk, M]: what a query's probabilities are formed with, and D
     void *dq, *dk, *dv, *dgate, *dbias;
     // partial sums over splits
     float *part;     // [splits][rows][d]

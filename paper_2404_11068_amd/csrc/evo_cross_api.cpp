@@ -175,8 +175,8 @@ CrPlan cross_plan(const CrArgs &a, bool has_gate, bool has_bias) {
         const int64_t bias_tiles = a.N / a.rpb * a.H * up(a.Lq, 64) * up(a.Lk, 64);
         p.bias_chunks = split(bias_tiles, a.rpb, 1.2 * step, 4.0 * (a.N / a.rpb) * a.H * a.Lq * (double)a.Lk, rate, false);
     }
-    p.bwd_da = pad((size_t)units * a.M * 4);
-    p.bwd_part = p.bwd_da + (has_gate ? pad((size_t)units * a.M * a.D * (a.bf16 ? 2 : 4)) : 0);
+    p.bwd_da = pad((size_t)units * a.M * 16);
+    p.bwd_part = p.bwd_da + (has_gate || has_bias ? pad((size_t)units * a.M * a.D * (a.bf16 ? 2 : 4)) : 0);
     size_t part = 0;
     const auto more = [&](int splits, size_t one) {
         if (splits > 1 && part < splits * one) part = splits * one;

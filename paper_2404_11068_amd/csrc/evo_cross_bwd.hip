@@ -5,7 +5,7 @@
 //
 // P is formed again from the saved log-sum-exp, in each of three passes:
 //   rows:  a wave owns 32 queries (lane = query) and walks the keys: dQ; before that
-//          it forms D, dgate and dA of its queries, and leaves them for the others
+//          it forms D, dgate and dA of its queries, and leaves them for the others (stats, da)
 //   keys:  a wave owns 32 keys (lane = key) and walks the queries: dK, dV
 //   bias:  a workgroup owns 64 x 64 entries of one bias plane and walks the
 //          rows that share it
@@ -24,12 +24,21 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// dA as the later passes read it: what the first has written, or dO itself without a gate
+// A log-sum-exp beyond this no longer holds the logarithm of the sum to 2^-14: fp32's steps there are 2^-13 and more.
+// Such a query's wave walks the keys once more, before its pass, for the largest logit and the sum against it, and P is
+// formed with those.  With a bias, P = exp(x - base) of a logit x, base = lse, or the largest x with 1 / sum
+// multiplied onto D and dA, whose multiples all gradients are: nothing changes for the passes.  Without a bias (where
+// dA may be dO itself), P = exp2((s - rest) scale log2 e + base) of s = q k', (base, rest) = (-lse log2 e, 0), or
+// (-log2 sum, largest s); steps whose queries all have a rest of 0 leave it out.  Queries without keys: base = inf, -inf.
+// With both as terms of every exponent the passes took 2% (64 channels) to 10% longer (32 channels with a bias).
+constexpr float kFarLse = 1024.0f;
+
+// dA as the later passes read it: what the first has written, or dO itself without gate and bias
 struct DaView {
     int64_t row, tok;
 };
 __device__ __forceinline__ DaView da_view(const CrArgs &a) {
-    return a.gate ? DaView{(int64_t)a.Lq * a.H * a.D, (int64_t)a.H * a.D} : DaView{a.o_row, a.o_tok};
+    return a.da ? DaView{(int64_t)a.Lq * a.H * a.D, (int64_t)a.H * a.D} : DaView{a.o_row, a.o_tok};
 }
 
 // ---------------------------------------------------------------------------
@@ -50,7 +59,7 @@ __global__ __launch_bounds__(kThreads, (KeysShape<T, DP>::WAVES)) void cross_key
     using S = KeysShape<T, DP>;
     constexpr int NK = DP / Y::KS, DT = DP / 32;
     __shared__ __attribute__((aligned(16))) E tiles[2][2][S::TILE];
-    __shared__ __attribute__((aligned(16))) float stats[2][2][S::XT];
+    __shared__ __attribute__((aligned(16))) float stats[2][BIAS ? 2 : 3][S::XT];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     uint32_t u = xcd_unit32(blockIdx.x, gridDim.x);
@@ -62,7 +71,7 @@ __global__ __launch_bounds__(kThreads, (KeysShape<T, DP>::WAVES)) void cross_key
     const int hk = unit % a.Hk;
     const DaView dv = da_view(a);
     const E *qbase = (const E *)a.q + n * a.q_row + (int64_t)hk * a.G * a.D;
-    const E *abase = (const E *)(a.gate ? a.da : a.dout) + n * dv.row + (int64_t)hk * a.G * a.D;
+    const E *abase = (const E *)(a.da ? a.da : a.dout) + n * dv.row + (int64_t)hk * a.G * a.D;
 
     const int key = tile * S::KEYS + wave * 32 + (lane & 31), keyc = min(key, a.Lk - 1);
     const bool keep = key < a.Lk && (!a.mask || a.mask[n * a.Lk + key]);
@@ -79,18 +88,18 @@ __global__ __launch_bounds__(kThreads, (KeysShape<T, DP>::WAVES)) void cross_key
 
     constexpr int NB = S::XT / 32, GP = 32 / Y::KS;
     using Cp = Copy<T, DP, S::XT, kThreads>;
-    float lse_in = 0.0f, dsum_in = 0.0f;
+    const f32x4 *sbase = a.stats + (int64_t)unit * a.M;
+    float2 stats_in = {};
+    float rest_in = 0.0f;
     auto request = [&](int step) {
         const int x0 = step * S::XT;
         auto at = [&](int r, int64_t tok) {
             const int x = x0 + r, t = token_of(a, x);
             return (int64_t)t * tok + (int64_t)(x - t * a.G) * a.D;
         };
-        if (tid < S::XT) {
-            const int x = min(x0 + tid, a.M - 1), t = token_of(a, x), g = x - t * a.G;
-            lse_in = a.lse[(n * a.H + hk * a.G + g) * a.Lq + t];
-            dsum_in = a.dsum[(int64_t)unit * a.M + x];
-        }
+        const float *from = (const float *)(sbase + (uint32_t)min(x0 + lane % S::XT, a.M - 1));
+        if (tid < S::XT) stats_in = *reinterpret_cast<const float2 *>(from);
+        if (!BIAS) rest_in = from[2];  // (all waves look whether there is one)
         const bool whole = a.D == DP && x0 + S::XT <= a.M;
         auto in = [&](int r) { return x0 + r < a.M; };
         Cp::run(tiles[step & 1][0], whole, a.D, wave, lane, [&](int r) { return qbase + at(r, a.q_tok); }, in);
@@ -127,11 +136,13 @@ __global__ __launch_bounds__(kThreads, (KeysShape<T, DP>::WAVES)) void cross_key
         const E *qt = tiles[buf][0], *at = tiles[buf][1];
         asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
         if (tid < S::XT) {
-            // a query without keys, and what lies behind the last: probability exp(-inf)
-            const float l = step * S::XT + tid >= a.M || lse_in == -__builtin_inff() ? __builtin_inff() : lse_in;
-            stats[buf][0][tid] = BIAS ? l : l * kLog2e;
-            stats[buf][1][tid] = dsum_in;
+            // what lies behind the last query: probability exp(-inf)
+            const bool in = step * S::XT + tid < a.M;
+            stats[buf][0][tid] = in ? stats_in.x : BIAS ? __builtin_inff() : -__builtin_inff();
+            stats[buf][1][tid] = stats_in.y;
+            if (!BIAS) stats[buf][BIAS ? 0 : 2][tid] = rest_in;
         }
+        const bool any_rest = !BIAS && __any(rest_in != 0.0f);
         copies_done_and_barrier();
         if (step + 1 < s1) request(step + 1);
         f32x16 s[NB], dp[NB];
@@ -151,13 +162,19 @@ __global__ __launch_bounds__(kThreads, (KeysShape<T, DP>::WAVES)) void cross_key
                 for (int i = 0; i < 16; ++i) s[b][i] = fmaf(s[b][i], a.scale, Y::f(braw[BIAS ? b : 0][i], keep));
             if (step + 1 < s1) request_bias(step + 1);
         }
+        if (any_rest) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[b][i] -= stats[buf][BIAS ? 0 : 2][32 * b + 8 * (i / 4) + 4 * h + i % 4];
+        }
         // four probabilities of a block, and what the logits' gradients are by them
         auto four = [&](int b, int i) {
             const f32x4 l = *reinterpret_cast<const f32x4 *>(&stats[buf][0][32 * b + 2 * i + 4 * h]);
             const f32x4 d = *reinterpret_cast<const f32x4 *>(&stats[buf][1][32 * b + 2 * i + 4 * h]);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                s[b][i + e] = __builtin_amdgcn_exp2f(BIAS ? (s[b][i + e] - l[e]) * kLog2e : fmaf(s[b][i + e], to2, -l[e]));
+                s[b][i + e] = __builtin_amdgcn_exp2f(BIAS ? (s[b][i + e] - l[e]) * kLog2e : fmaf(s[b][i + e], to2, l[e]));
                 dp[b][i + e] = s[b][i + e] * (dp[b][i + e] - d[e]);
             }
         };
@@ -240,23 +257,77 @@ __global__ __launch_bounds__(kThreads, (RowsShape<T, DP, BIAS>::WAVES)) void cro
     Frag qf[NK], af[NK];
     const int64_t qoff = n * a.q_row + (int64_t)t * a.q_tok + (int64_t)head * a.D;
     load_rows<T, DP>(qf, (const E *)a.q + qoff, a.D, on, h);
+    const float inf = __builtin_inff(), lse = a.lse[(n * a.H + head) * a.Lq + t], to2 = a.scale * kLog2e;
+    constexpr int W = Y::KS / 2;
+    struct Bits16 { E e[W]; };
+    const int64_t oat = n * a.o_row + (int64_t)t * a.o_tok + (int64_t)head * a.D;
+    u32x4 oin[NK], din[NK], gin[NK];
+#pragma unroll
+    for (int kk = 0; kk < NK; ++kk) {
+        const int c = Y::KS * kk + W * h, cc = c < a.D ? c : 0;
+        oin[kk] = *reinterpret_cast<const u32x4 *>((const E *)a.out + oat + cc);
+        din[kk] = *reinterpret_cast<const u32x4 *>((const E *)a.dout + oat + cc);
+        gin[kk] = a.gate ? *reinterpret_cast<const u32x4 *>((const E *)a.gate + qoff + cc) : u32x4{};
+    }
+    const BiasRow<T> brow(a, BIAS ? (n / a.rpb * a.H + head) * a.Lq + t : 0);
+    const E *kbase = (const E *)a.k + n * a.k_row + (int64_t)hk * a.D;
+    const E *vbase = (const E *)a.v + n * a.k_row + (int64_t)hk * a.D;
+    const uint8_t *mrow = a.mask ? a.mask + n * a.Lk : nullptr;
+
+    const bool live = on && lse != -inf, far = live && fabsf(lse) > kFarLse && fabsf(lse) < inf;
+    const bool any_far = __any(far);
+    float base = BIAS ? (live ? lse : inf) : (live ? -lse * kLog2e : -inf), rest = 0.0f, times = 1.0f;
+    if (any_far) {
+        // rows of K straight from memory, one a lane: rare, and without barriers that the other waves would have to meet
+        const float unit2 = BIAS ? kLog2e : to2;
+        float top = -inf, sum = 0.0f;
+        for (int k0 = 0; k0 < a.Lk; k0 += 32) {
+            const int key = k0 + (lane & 31), keyc = min(key, a.Lk - 1);
+            const bool keep = key < a.Lk && (!mrow || mrow[keyc]);
+            const uint32_t bits = (uint32_t)__ballot(keep);
+            if (!bits) continue;
+            Frag kf[NK];
+            load_rows<T, DP>(kf, kbase + (int64_t)keyc * a.k_tok, a.D, keep, h);
+            f32x16 s = zero16();
+#pragma unroll
+            for (int kk = 0; kk < NK; ++kk) Y::mma(s, kf[kk], qf[kk]);
+            if (BIAS) {
+                const auto raw = brow.request(k0, h);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], a.scale, BiasRow<T>::value(raw, i));
+            }
+            float higher = top;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[i] = where_kept(bits, i, s[i], kMinusInf);
+                higher = fmaxf(higher, s[i]);
+            }
+            higher = half_max(higher);
+            const float to = higher > -inf ? higher : 0.0f;
+            sum *= __builtin_amdgcn_exp2f((top - to) * unit2);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sum += __builtin_amdgcn_exp2f((s[i] - to) * unit2);
+            top = higher;
+        }
+        sum = half_sum(sum);
+        if (far && BIAS) base = top, times = 1.0f / sum;
+        if (far && !BIAS) base = -__builtin_amdgcn_logf(sum), rest = top;
+    }
+
     // D, dgate and dA of the lane's query, for this pass and, written by the first split, for the next
     float dsum = 0.0f;
     {
-        const int64_t oat = n * a.o_row + (int64_t)t * a.o_tok + (int64_t)head * a.D;
         const int64_t daat = ((n * a.Lq + t) * a.H + head) * (int64_t)a.D;
-        constexpr int W = Y::KS / 2;
-        struct Bits16 { E e[W]; };
 #pragma unroll
         for (int kk = 0; kk < NK; ++kk) {
-            const int c = Y::KS * kk + W * h, cc = c < a.D ? c : 0;
+            const int c = Y::KS * kk + W * h;
             const bool in = on && c < a.D;
-            const Bits16 o = __builtin_bit_cast(Bits16, where(in, *reinterpret_cast<const u32x4 *>((const E *)a.out + oat + cc)));
-            Bits16 d = __builtin_bit_cast(Bits16, where(in, *reinterpret_cast<const u32x4 *>((const E *)a.dout + oat + cc)));
+            const Bits16 o = __builtin_bit_cast(Bits16, where(in, oin[kk]));
+            Bits16 d = __builtin_bit_cast(Bits16, where(in, din[kk]));
 #pragma unroll
             for (int e = 0; e < W; ++e) dsum = fmaf(Y::f(o.e[e]), Y::f(d.e[e]), dsum);
             if (a.gate) {
-                const Bits16 g = __builtin_bit_cast(Bits16, *reinterpret_cast<const u32x4 *>((const E *)a.gate + qoff + cc));
+                const Bits16 g = __builtin_bit_cast(Bits16, gin[kk]);
                 Bits16 dg;
 #pragma unroll
                 for (int e = 0; e < W; ++e) {
@@ -264,26 +335,20 @@ __global__ __launch_bounds__(kThreads, (RowsShape<T, DP, BIAS>::WAVES)) void cro
                     const float y = Y::f(g.e[e]), z = __builtin_amdgcn_exp2f(-fabsf(y) * kLog2e), r = __builtin_amdgcn_rcpf(1.0f + z);
                     const float sig = y >= 0.0f ? r : z * r, rest = y >= 0.0f ? z * r : r, df = Y::f(d.e[e]);
                     dg.e[e] = Y::e(df * Y::f(o.e[e]) * rest);
-                    d.e[e] = Y::e(df * sig);  // rounded to the type: the operand of two matrix products
+                    d.e[e] = Y::e(BIAS ? df * sig * times : df * sig);  // rounded to the type: the operand of two matrix products
                 }
-                if (in && split == 0) {
-                    *reinterpret_cast<u32x4 *>((E *)a.dgate + qoff + c) = __builtin_bit_cast(u32x4, dg);
-                    *reinterpret_cast<u32x4 *>((E *)a.da + daat + c) = __builtin_bit_cast(u32x4, d);
-                }
+                if (in && split == 0) *reinterpret_cast<u32x4 *>((E *)a.dgate + qoff + c) = __builtin_bit_cast(u32x4, dg);
+            } else if (BIAS && any_far) {
+#pragma unroll
+                for (int e = 0; e < W; ++e) d.e[e] = Y::e(Y::f(d.e[e]) * times);
             }
+            if ((BIAS || a.gate) && in && split == 0) *reinterpret_cast<u32x4 *>((E *)a.da + daat + c) = __builtin_bit_cast(u32x4, d);
             af[kk] = __builtin_bit_cast(Frag, d);
         }
         dsum = half_sum(dsum);
-        if (on && h == 0 && split == 0) a.dsum[(int64_t)unit * a.M + x] = dsum;
+        if (BIAS) dsum *= times;
+        if (on && h == 0 && split == 0) a.stats[(int64_t)unit * a.M + x] = f32x4{base, dsum, rest, 0.0f};
     }
-    float lse = a.lse[(n * a.H + head) * a.Lq + t];
-    if (!on || lse == -__builtin_inff()) lse = __builtin_inff();
-    const float to2 = a.scale * kLog2e, shift = -lse * kLog2e;
-    const BiasRow<T> brow(a, BIAS ? (n / a.rpb * a.H + head) * a.Lq + t : 0);
-
-    const E *kbase = (const E *)a.k + n * a.k_row + (int64_t)hk * a.D;
-    const E *vbase = (const E *)a.v + n * a.k_row + (int64_t)hk * a.D;
-    const uint8_t *mrow = a.mask ? a.mask + n * a.Lk : nullptr;
     f32x16 dq[DT];
 #pragma unroll
     for (int i = 0; i < DT; ++i) dq[i] = zero16();
@@ -349,13 +414,19 @@ __global__ __launch_bounds__(kThreads, (RowsShape<T, DP, BIAS>::WAVES)) void cro
             for (int b = 0; b < NB; ++b)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    s[b][i] = (fmaf(s[b][i], a.scale, BiasRow<T>::value(braw[BIAS ? b : 0], i)) - lse) * kLog2e;
+                    s[b][i] = (fmaf(s[b][i], a.scale, BiasRow<T>::value(braw[BIAS ? b : 0], i)) - base) * kLog2e;
             if (step + 1 < t1) request_bias(step + 1);
         } else {
+            if (any_far) {
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[b][i] -= rest;
+            }
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[b][i] = fmaf(s[b][i], to2, shift);
+                for (int i = 0; i < 16; ++i) s[b][i] = fmaf(s[b][i], to2, base);
         }
         if (!now.all()) {
 #pragma unroll
@@ -455,16 +526,12 @@ __global__ __launch_bounds__(kThreads, (BiasShape<T, DP>::WAVES)) void cross_bia
     using Cp = Copy<T, DP, 64, kThreads>;
     Bits now, next;
     auto bytes_of = [&](int64_t n) { return Bits::request(a.mask ? a.mask + n * a.Lk : nullptr, k0, n < n1 ? a.Lk : 0, lane); };
-    float lse_in = 0.0f, dsum_in = 0.0f;
+    float2 stats_in = {};
     const bool full_d = a.D == DP, full_q = full_d && t0 + 64 <= a.Lq;
     auto request = [&](int64_t n, int buf) {
-        if (tid < 64) {
-            const int t = min(t0 + tid, a.Lq - 1);
-            lse_in = a.lse[(n * a.H + head) * a.Lq + t];
-            dsum_in = a.dsum[((n * a.Hk + hk) * a.Lq + t) * a.G + g];
-        }
+        if (tid < 64) stats_in = *reinterpret_cast<const float2 *>(a.stats + ((n * a.Hk + hk) * a.Lq + min(t0 + tid, a.Lq - 1)) * a.G + g);
         const E *q = (const E *)a.q + n * a.q_row + (int64_t)head * a.D;
-        const E *da = (const E *)(a.gate ? a.da : a.dout) + n * dv.row + (int64_t)head * a.D;
+        const E *da = (const E *)(a.da ? a.da : a.dout) + n * dv.row + (int64_t)head * a.D;
         const E *k = (const E *)a.k + n * a.k_row + (int64_t)hk * a.D, *v = (const E *)a.v + n * a.k_row + (int64_t)hk * a.D;
         const auto in_q = [&](int r) { return t0 + r < a.Lq; };
         const auto keep = [&](int r) { return next.get(r); };
@@ -485,8 +552,8 @@ __global__ __launch_bounds__(kThreads, (BiasShape<T, DP>::WAVES)) void cross_bia
     for (int64_t n = n0; n < n1; ++n) {
         asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
         if (tid < 64) {
-            stats[buf][0][tid] = t0 + tid >= a.Lq || lse_in == -__builtin_inff() ? __builtin_inff() : lse_in;
-            stats[buf][1][tid] = dsum_in;
+            stats[buf][0][tid] = t0 + tid < a.Lq ? stats_in.x : __builtin_inff();
+            stats[buf][1][tid] = stats_in.y;
         }
         copies_done_and_barrier();
         now = next;
@@ -645,8 +712,8 @@ template <typename T> void run_dim(const CrArgs &a, const CrPlan &p, hipStream_t
 }  // namespace
 
 hipError_t launch_cross_bwd(CrArgs a, const CrPlan &p, void *ws, hipStream_t s) {
-    a.dsum = (float *)ws;
-    a.da = (char *)ws + p.bwd_da;
+    a.stats = (f32x4 *)ws;
+    a.da = a.gate || a.bias ? (char *)ws + p.bwd_da : nullptr;
     a.part = (float *)((char *)ws + p.bwd_part);
     a.bf16 ? run_dim<bf16_t>(a, p, s) : run_dim<float>(a, p, s);
     return hipGetLastError();
