@@ -38,7 +38,8 @@
  *   packed buffer.
  * - pos int32: row r starts at r * pos_stride (0: all rows share positions);
  *   steps uint64 [rot_dim / 2], w and dw fp32 [d].
- * - Angles and all arithmetic are fp32 (phases exact), rounded once.
+ * - Angles and all arithmetic are fp32 (phases exact), rounded once.  The mean of squares may leave fp32's range, at an
+ *   eps of 0 and for large channels: only where 1 / sqrt(mean(x^2) + eps) itself does is dx infinite.
  */
 #ifndef EVO_ROPE_H
 #define EVO_ROPE_H
