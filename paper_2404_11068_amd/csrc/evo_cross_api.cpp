@@ -6,6 +6,7 @@
 #include <math.h>
 
 #include "evo_cross.h"
+#include "evo_views.h"
 
 namespace {
 
@@ -256,13 +257,18 @@ int evo_cross_bwd(const evo_cross_dims *d, const void *q, const void *k, const v
     const Range outs[5] = {qr(dq), qr(dgate), kr(dk), kr(dv), flat(dbias, nb)};
     const Range ins[7] = {qr(q), qr(gate), kr(k), kr(v), orr(out), orr(dout), flat(bias, nb)};
     const bool packed[5] = {packed_q, packed_q, packed_k, packed_k, false};
+    const int64_t qb = (int64_t)a.H * a.D * (int64_t)es, kb = (int64_t)a.Hk * a.D * (int64_t)es;
+    const auto view = [&](int i) {
+        return i < 2 ? evo::View{outs[i].lo, a.q_row * (int64_t)es, a.q_tok * (int64_t)es, a.N, a.Lq, qb}
+                     : evo::View{outs[i].lo, a.k_row * (int64_t)es, a.k_tok * (int64_t)es, a.N, a.Lk, kb};
+    };
     for (int i = 0; i < 5; ++i) {
         if (outs[i].lo == outs[i].hi) continue;
         for (const Range &r : ins)
             if (r.lo != r.hi && r.lo < outs[i].hi && outs[i].lo < r.hi) return EVO_ERR_INVALID_ARG;
         for (int j = 0; j < i; ++j)
             if (outs[j].lo != outs[j].hi && outs[j].lo < outs[i].hi && outs[i].lo < outs[j].hi &&
-                (outs[i].lo == outs[j].lo || !(packed[i] && packed[j])))
+                !(packed[i] && packed[j] && evo::views_apart(view(i), view(j))))
                 return EVO_ERR_INVALID_ARG;
     }
     const evo::CrPlan p = evo::cross_plan(a, gate != nullptr, bias != nullptr);

@@ -1,0 +1,34 @@
+"""Host-side checks of the attention to states of another length (no GPU): which tensors of a call may lie in one buffer.
+Fake addresses, never touched; a workspace that is missing (status 4) shows that a call goes on."""
+import pytest
+
+from tests.test_cross_abi_host import A, BWD, FWD, _bwd, _dims, _fwd
+
+PLAIN = dict(gate=None, bias=None, mask=None, dgate=None, dbias=None, ws=None)
+
+
+def _packed(**kw):
+    """Queries of 512 and keys of 128 channels in tokens of 1024 and 512."""
+    d = dict(q_stride_row=10 * 1024, q_stride_tok=1024, k_stride_row=300 * 512, k_stride_tok=512)
+    d.update(kw)
+    return _dims(**d)
+
+
+@pytest.mark.parametrize("shift,status", [(1024, 4), (-1024, 4), (512, 1), (-512, 1), (1008, 1), (1040, 1), (16, 1), (0, 1),
+                                          (1024 + 2048, 4), (1024 + 5 * 2048, 4), (512 + 2048, 1)])
+def test_packed_gradients_of_queries_and_gate(shift, status):
+    # dgate beside dq in each token, or half under it
+    assert _bwd(_packed(), dgate=A(11) + shift, ws=None) == status
+
+
+@pytest.mark.parametrize("shift,status", [(256, 4), (512, 4), (768, 4), (128, 1), (240, 1), (800, 1), (1024, 1), (1280, 4)])
+def test_packed_gradients_of_keys_and_values(shift, status):
+    kw = dict(PLAIN, dv=A(12) + shift)
+    assert _bwd(_packed(), **kw) == status
+
+
+def test_gradients_of_queries_and_keys_in_one_buffer():
+    # self-attention's projections: queries, keys and values of one token side by side
+    d = dict(len_k=10, k_stride_row=10 * 1024, k_stride_tok=1024)
+    for dk, dv, status in ((1024, 1280, 4), (1024, 1024, 1), (1024, 1264, 1), (1008, 1280, 1), (1024, 1808, 1), (1792, 1024, 4)):
+        assert _bwd(_packed(**d), **dict(PLAIN, dk=A(11) + dk, dv=A(11) + dv)) == status, (dk, dv)
