@@ -6,6 +6,7 @@
 #include <math.h>
 
 #include "evo_rope_kernels.h"
+#include "evo_views.h"
 
 namespace {
 
@@ -73,12 +74,12 @@ bool sets_ok(const evo_rope_dims *d, int i, const void *out, int64_t orow, int64
     if (empty(d, i) || empty(d, j) || !other) return true;
     const uintptr_t a = (uintptr_t)out, b = (uintptr_t)other;
     if (a < b ? (int64_t)(b - a) >= span(d, i, orow, otok) : (int64_t)(a - b) >= span(d, j, row, tok)) return true;
+    if (otok != tok || orow != row || otok == 0) return false;  // one pair of strides, of the packed buffer
     const int64_t es = d->dtype == EVO_DTYPE_BF16 ? 2 : 4;
-    const int64_t bi = (int64_t)d->n_heads[i] * d->head_dim * es, bj = (int64_t)d->n_heads[j] * d->head_dim * es;
-    // one token stride (of the packed buffer), the blocks side by side within it
-    if (otok != tok || orow != row || otok == 0) return false;
-    const int64_t at = (int64_t)((a < b ? b - a : a - b) % (uintptr_t)(otok * es));
-    return a < b ? at >= bi && at + bj <= otok * es : at >= bj && at + bi <= otok * es;
+    const auto view = [&](int s, uintptr_t at, int64_t r, int64_t t) {
+        return evo::View{at, r * es, t * es, d->n_rows, d->len[s], (int64_t)d->n_heads[s] * d->head_dim * es};
+    };
+    return evo::views_apart(view(i, a, orow, otok), view(j, b, row, tok));
 }
 
 void fill(const evo_rope_dims *d, evo::RopeArgs *a) {
