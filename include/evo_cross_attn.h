@@ -37,7 +37,8 @@
  *   access.  Inputs may repeat rows or tokens (stride 0: one set of states for
  *   all rows); outputs must not overlap themselves (so with repeated states the
  *   backward takes its gradients at other strides: copy the dims, run it on
- *   expanded inputs), each other or an input.
+ *   expanded inputs), each other or an input.  Blocks side by side in the tokens
+ *   of one packed buffer do not overlap.
  */
 #ifndef EVO_CROSS_ATTN_H
 #define EVO_CROSS_ATTN_H

@@ -34,8 +34,8 @@
  *   row for all), but not where dx, which has x's strides, is written.
  * - y may be x itself (same address, same strides: in place), and dx dy or x; other
  *   overlaps of these are refused, and so are those of one set's output with
- *   the other set's tensors, but for blocks side by side in the tokens of one
- *   packed buffer.
+ *   the other set's tensors.  Blocks side by side in the tokens of one packed
+ *   buffer do not overlap, with one token a row, too.
  * - pos int32: row r starts at r * pos_stride (0: all rows share positions);
  *   steps uint64 [rot_dim / 2], w and dw fp32 [d].
  * - Angles and all arithmetic are fp32 (phases exact), rounded once.  The mean of squares may leave fp32's range, at an

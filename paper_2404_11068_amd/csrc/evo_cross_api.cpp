@@ -84,15 +84,13 @@ int check(const evo_cross_dims *d, bool has_bias, evo::CrArgs *a) {
 
 bool apart_o(const evo::CrArgs &a) { return apart(a.N, a.Lq, (int64_t)a.H * a.D, a.o_row, a.o_tok); }
 
-// the address range of a token tensor
-struct Range {
-    uintptr_t lo, hi;
-};
-Range range(const evo::CrArgs &a, const void *p, int len, int heads, int64_t row, int64_t tok) {
-    const int64_t n = ((a.N - 1) * row + (int64_t)(len - 1) * tok + (int64_t)heads * a.D) * (a.bf16 ? 2 : 4);
-    return Range{(uintptr_t)p, (uintptr_t)p + (p && len > 0 ? (uintptr_t)n : 0)};
+// tensors that are not there (or empty) have no block
+evo::View view(const evo::CrArgs &a, const void *p, int len, int heads, int64_t row, int64_t tok) {
+    const int64_t es = a.bf16 ? 2 : 4;
+    return evo::View{(uintptr_t)p, row * es, tok * es, a.N, len, p && len > 0 ? (int64_t)heads * a.D * es : 0};
 }
-Range flat(const void *p, int64_t bytes) { return Range{(uintptr_t)p, (uintptr_t)p + (p ? (uintptr_t)bytes : 0)}; }
+evo::View flat(const void *p, int64_t bytes) { return evo::View{(uintptr_t)p, 0, 0, 1, 1, p ? bytes : 0}; }
+bool apart(const evo::View &x, const evo::View &y) { return x.block == 0 || y.block == 0 || evo::views_apart(x, y); }
 
 }  // namespace
 
@@ -213,11 +211,11 @@ int evo_cross_fwd(const evo_cross_dims *d, const void *q, const void *k, const v
     if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(gate, 16) || !aligned(out, 16) ||
         !aligned(bias, es) || !aligned(lse, 4))
         return EVO_ERR_ALIGNMENT;
-    const Range o = range(a, out, a.Lq, a.H, a.o_row, a.o_tok);
-    const Range in[4] = {range(a, q, a.Lq, a.H, a.q_row, a.q_tok), range(a, gate, a.Lq, a.H, a.q_row, a.q_tok),
-                         range(a, k, a.Lk, a.Hk, a.k_row, a.k_tok), range(a, v, a.Lk, a.Hk, a.k_row, a.k_tok)};
-    for (const Range &r : in)
-        if (r.lo < o.hi && o.lo < r.hi && r.lo != r.hi) return EVO_ERR_INVALID_ARG;
+    const evo::View o = view(a, out, a.Lq, a.H, a.o_row, a.o_tok);
+    const evo::View in[4] = {view(a, q, a.Lq, a.H, a.q_row, a.q_tok), view(a, gate, a.Lq, a.H, a.q_row, a.q_tok),
+                             view(a, k, a.Lk, a.Hk, a.k_row, a.k_tok), view(a, v, a.Lk, a.Hk, a.k_row, a.k_tok)};
+    for (const evo::View &r : in)
+        if (!apart(o, r)) return EVO_ERR_INVALID_ARG;
     const evo::CrPlan p = evo::cross_plan(a, gate != nullptr, bias != nullptr);
     if (p.fwd_total > 0 && (!ws || ws_bytes < p.fwd_total)) return EVO_ERR_WORKSPACE;
     if (p.fwd_total > 0 && !aligned(ws, 256)) return EVO_ERR_ALIGNMENT;
@@ -249,27 +247,17 @@ int evo_cross_bwd(const evo_cross_dims *d, const void *q, const void *k, const v
         if (!aligned(x, 16)) return EVO_ERR_ALIGNMENT;
     if (!aligned(bias, es) || !aligned(dbias, es) || !aligned(lse, 4)) return EVO_ERR_ALIGNMENT;
     // outputs apart from every input and from each other; views of one packed buffer may interleave
-    const bool packed_q = a.q_tok > (int64_t)a.H * a.D, packed_k = a.k_tok > (int64_t)a.Hk * a.D;
-    const auto qr = [&](const void *x) { return range(a, x, a.Lq, a.H, a.q_row, a.q_tok); };
-    const auto kr = [&](const void *x) { return range(a, x, a.Lk, a.Hk, a.k_row, a.k_tok); };
-    const auto orr = [&](const void *x) { return range(a, x, a.Lq, a.H, a.o_row, a.o_tok); };
+    const auto qr = [&](const void *x) { return view(a, x, a.Lq, a.H, a.q_row, a.q_tok); };
+    const auto kr = [&](const void *x) { return view(a, x, a.Lk, a.Hk, a.k_row, a.k_tok); };
+    const auto orr = [&](const void *x) { return view(a, x, a.Lq, a.H, a.o_row, a.o_tok); };
     const int64_t nb = a.N / a.rpb * a.H * a.Lq * (int64_t)a.Lk * (int64_t)es;
-    const Range outs[5] = {qr(dq), qr(dgate), kr(dk), kr(dv), flat(dbias, nb)};
-    const Range ins[7] = {qr(q), qr(gate), kr(k), kr(v), orr(out), orr(dout), flat(bias, nb)};
-    const bool packed[5] = {packed_q, packed_q, packed_k, packed_k, false};
-    const int64_t qb = (int64_t)a.H * a.D * (int64_t)es, kb = (int64_t)a.Hk * a.D * (int64_t)es;
-    const auto view = [&](int i) {
-        return i < 2 ? evo::View{outs[i].lo, a.q_row * (int64_t)es, a.q_tok * (int64_t)es, a.N, a.Lq, qb}
-                     : evo::View{outs[i].lo, a.k_row * (int64_t)es, a.k_tok * (int64_t)es, a.N, a.Lk, kb};
-    };
+    const evo::View outs[5] = {qr(dq), qr(dgate), kr(dk), kr(dv), flat(dbias, nb)};
+    const evo::View ins[7] = {qr(q), qr(gate), kr(k), kr(v), orr(out), orr(dout), flat(bias, nb)};
     for (int i = 0; i < 5; ++i) {
-        if (outs[i].lo == outs[i].hi) continue;
-        for (const Range &r : ins)
-            if (r.lo != r.hi && r.lo < outs[i].hi && outs[i].lo < r.hi) return EVO_ERR_INVALID_ARG;
+        for (const evo::View &r : ins)
+            if (!apart(outs[i], r)) return EVO_ERR_INVALID_ARG;
         for (int j = 0; j < i; ++j)
-            if (outs[j].lo != outs[j].hi && outs[j].lo < outs[i].hi && outs[i].lo < outs[j].hi &&
-                !(packed[i] && packed[j] && evo::views_apart(view(i), view(j))))
-                return EVO_ERR_INVALID_ARG;
+            if (!apart(outs[i], outs[j])) return EVO_ERR_INVALID_ARG;
     }
     const evo::CrPlan p = evo::cross_plan(a, gate != nullptr, bias != nullptr);
     if (p.bwd_total > 0 && (!ws || ws_bytes < p.bwd_total)) return EVO_ERR_WORKSPACE;

@@ -54,32 +54,23 @@ int check_dims(const evo_rope_dims *d, bool bwd) {
     return EVO_OK;
 }
 
-// bytes from the first to past the last element
-int64_t span(const evo_rope_dims *d, int i, int64_t row, int64_t tok) {
+evo::View view(const evo_rope_dims *d, int i, const void *p, int64_t row, int64_t tok) {
     const int64_t es = d->dtype == EVO_DTYPE_BF16 ? 2 : 4;
-    return ((d->n_rows - 1) * row + (d->len[i] - 1) * tok + (int64_t)d->n_heads[i] * d->head_dim) * es;
+    return evo::View{(uintptr_t)p, row * es, tok * es, d->n_rows, d->len[i], (int64_t)d->n_heads[i] * d->head_dim * es};
 }
 
 // in place (one address, one pair of strides) or apart
 bool overlap_ok(const evo_rope_dims *d, int i, const void *in, int64_t ir, int64_t it, const void *out, int64_t orow,
                 int64_t otok) {
     if (in == out && (ir == orow || d->n_rows == 1) && (it == otok || d->len[i] == 1)) return true;
-    const uintptr_t a = (uintptr_t)in, b = (uintptr_t)out;
-    return a < b ? (int64_t)(b - a) >= span(d, i, ir, it) : (int64_t)(a - b) >= span(d, i, orow, otok);
+    return evo::views_apart(view(d, i, in, ir, it), view(d, i, out, orow, otok));
 }
 
-// what one set writes and another tensor of the other set: apart, or interleaved in one packed buffer
+// what one set writes and another tensor of the other set: apart, which blocks of one packed buffer are, too
 bool sets_ok(const evo_rope_dims *d, int i, const void *out, int64_t orow, int64_t otok, int j, const void *other,
              int64_t row, int64_t tok) {
     if (empty(d, i) || empty(d, j) || !other) return true;
-    const uintptr_t a = (uintptr_t)out, b = (uintptr_t)other;
-    if (a < b ? (int64_t)(b - a) >= span(d, i, orow, otok) : (int64_t)(a - b) >= span(d, j, row, tok)) return true;
-    if (otok != tok || orow != row || otok == 0) return false;  // one pair of strides, of the packed buffer
-    const int64_t es = d->dtype == EVO_DTYPE_BF16 ? 2 : 4;
-    const auto view = [&](int s, uintptr_t at, int64_t r, int64_t t) {
-        return evo::View{at, r * es, t * es, d->n_rows, d->len[s], (int64_t)d->n_heads[s] * d->head_dim * es};
-    };
-    return evo::views_apart(view(i, a, orow, otok), view(j, b, row, tok));
+    return evo::views_apart(view(d, i, out, orow, otok), view(d, j, other, row, tok));
 }
 
 void fill(const evo_rope_dims *d, evo::RopeArgs *a) {

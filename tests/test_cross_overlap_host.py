@@ -32,3 +32,23 @@ def test_gradients_of_queries_and_keys_in_one_buffer():
     d = dict(len_k=10, k_stride_row=10 * 1024, k_stride_tok=1024)
     for dk, dv, status in ((1024, 1280, 4), (1024, 1024, 1), (1024, 1264, 1), (1008, 1280, 1), (1024, 1808, 1), (1792, 1024, 4)):
         assert _bwd(_packed(**d), **dict(PLAIN, dk=A(11) + dk, dv=A(11) + dv)) == status, (dk, dv)
+
+
+@pytest.mark.parametrize("rows", [1, 4])
+def test_one_token_a_row(rows):
+    """The token stride of a single token says nothing: blocks lie side by side within the row stride."""
+    q = dict(n_rows=rows, rows_per_bias=1, len_q=1, q_stride_row=1024, o_stride_row=512)
+    for tok in (512, 1024, 0):
+        for shift, status in ((1024, 4), (512, 1), (1008, 1), (1536, 1 if rows > 1 else 4)):
+            assert _bwd(_dims(**q, q_stride_tok=tok), dgate=A(11) + shift, ws=None) == status, (tok, shift)
+    k = dict(n_rows=rows, rows_per_bias=1, len_k=1, k_stride_row=256)
+    for tok in (128, 256):
+        for shift, status in ((256, 4), (128, 1), (384, 1 if rows > 1 else 4)):
+            assert _bwd(_dims(**k, k_stride_tok=tok), dv=A(12) + shift, ws=None) == status, (tok, shift)
+
+
+def test_output_beside_the_queries():
+    """The forward's output in another place of the tokens its queries lie in."""
+    d = dict(len_q=10, len_k=3000, k_stride_row=384000, q_stride_row=10240, q_stride_tok=1024, o_stride_row=10240, o_stride_tok=1024)
+    for shift, status in ((1024, 4), (1008, 1), (0, 1), (512, 1)):
+        assert _fwd(_dims(**d), out=A(1) + shift, gate=None, ws=None) == status

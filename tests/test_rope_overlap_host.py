@@ -31,3 +31,30 @@ def test_rows_within_tokens():
     assert _run((4, 4), (8, 2), 640, 1280, 0, 1024) == 4
     assert _run((4, 4), (8, 2), 640, 1280, 0, 1664) == 1               # set 0's second row lies there
     assert _run((4, 4), (8, 2), 640, 1280, 0, 1024 + 2560) == 4
+
+
+@pytest.mark.parametrize("tok", [(512, 128), (640, 640), (1024, 128)])
+def test_one_token_a_row(tok):
+    """The token stride of a single token says nothing: blocks lie side by side within the row stride."""
+    for rows in (1, 2, 4):
+        assert _run((1, 1), (8, 2), 640, tok, 0, 1024, rows) == 4
+        assert _run((1, 1), (8, 2), 640, tok, 0, 1008, rows) == 1
+        assert _run((1, 1), (8, 2), 640, tok, 0, 1040, rows) == (1 if rows > 1 else 4)
+        assert _run((1, 1), (2, 8), 640, tok[::-1], 0, 256, rows) == 4
+        assert _run((1, 1), (2, 8), 640, tok[::-1], 256 + 1024 - 16, 256, rows) == 1
+
+
+def test_lengths_of_their_own_in_one_buffer():
+    """One row of the batch, whose row stride says nothing either, and the last tokens' queries beside all keys."""
+    assert _run((3, 16), (8, 2), (3 * 640, 16 * 640), 640, 13 * 1280, 1024, 1) == 4
+    assert _run((3, 16), (8, 2), (3 * 640, 16 * 640), 640, 13 * 1280 + 16, 1024, 1) == 1
+    assert _run((1, 16), (8, 2), (640, 16 * 640), (512, 640), 15 * 1280, 1024, 1) == 4
+    assert _run((1, 16), (8, 2), 16 * 640, (512, 640), 15 * 1280, 1024, 3) == 4
+    assert _run((1, 16), (8, 2), 16 * 640, (512, 640), 15 * 1280 - 16, 1024, 3) == 1
+
+
+def test_gradients_beside_their_inputs():
+    """dx in another place of the tokens x lies in, or dy."""
+    d = _dims(n_rows=2, len=(16, 16), x_stride_row=(16 * 1024, 16 * 256), x_stride_tok=(1024, 256), y_stride_row=(16 * 512, 16 * 128))
+    assert _bwd(d, x0=AT, dx0=AT + 1024, x1=AT + (1 << 28), dx1=AT + (1 << 28) + 256, ws=None) == 4
+    assert _bwd(d, x0=AT, dx0=AT + 1008, x1=AT + (1 << 28), dx1=AT + (1 << 28) + 256, ws=None) == 1
