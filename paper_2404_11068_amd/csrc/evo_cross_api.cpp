@@ -91,6 +91,19 @@ evo::View view(const evo::CrArgs &a, const void *p, int len, int heads, int64_t 
 }
 evo::View flat(const void *p, int64_t bytes) { return evo::View{(uintptr_t)p, 0, 0, 1, 1, p ? bytes : 0}; }
 bool apart(const evo::View &x, const evo::View &y) { return x.block == 0 || y.block == 0 || evo::views_apart(x, y); }
+// outputs first .. n_outs - 1 from every input and from those before them
+bool all_apart(const evo::View *outs, int first, int n_outs, const evo::View *ins, int n_ins) {
+    for (int i = first; i < n_outs; ++i) {
+        for (int j = 0; j < n_ins; ++j)
+            if (!apart(outs[i], ins[j])) return false;
+        for (int j = 0; j < i; ++j)
+            if (!apart(outs[i], outs[j])) return false;
+    }
+    return true;
+}
+int64_t bias_bytes(const evo::CrArgs &a, const void *bias) {
+    return bias ? a.N / a.rpb * a.H * a.Lq * (int64_t)a.Lk * (a.bf16 ? 2 : 4) : 0;
+}
 
 }  // namespace
 
@@ -211,14 +224,15 @@ int evo_cross_fwd(const evo_cross_dims *d, const void *q, const void *k, const v
     if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(gate, 16) || !aligned(out, 16) ||
         !aligned(bias, es) || !aligned(lse, 4))
         return EVO_ERR_ALIGNMENT;
-    const evo::View o = view(a, out, a.Lq, a.H, a.o_row, a.o_tok);
-    const evo::View in[4] = {view(a, q, a.Lq, a.H, a.q_row, a.q_tok), view(a, gate, a.Lq, a.H, a.q_row, a.q_tok),
-                             view(a, k, a.Lk, a.Hk, a.k_row, a.k_tok), view(a, v, a.Lk, a.Hk, a.k_row, a.k_tok)};
-    for (const evo::View &r : in)
-        if (!apart(o, r)) return EVO_ERR_INVALID_ARG;
     const evo::CrPlan p = evo::cross_plan(a, gate != nullptr, bias != nullptr);
+    const evo::View outs[3] = {view(a, out, a.Lq, a.H, a.o_row, a.o_tok), flat(lse, a.N * a.H * a.Lq * 4), flat(ws, (int64_t)p.fwd_total)};
+    const evo::View ins[6] = {view(a, q, a.Lq, a.H, a.q_row, a.q_tok), view(a, gate, a.Lq, a.H, a.q_row, a.q_tok),
+                              view(a, k, a.Lk, a.Hk, a.k_row, a.k_tok), view(a, v, a.Lk, a.Hk, a.k_row, a.k_tok),
+                              flat(bias, bias_bytes(a, bias)), flat(mask, a.N * a.Lk)};
+    if (!all_apart(outs, 0, 2, ins, 6)) return EVO_ERR_INVALID_ARG;
     if (p.fwd_total > 0 && (!ws || ws_bytes < p.fwd_total)) return EVO_ERR_WORKSPACE;
     if (p.fwd_total > 0 && !aligned(ws, 256)) return EVO_ERR_ALIGNMENT;
+    if (!all_apart(outs, 2, 3, ins, 6)) return EVO_ERR_INVALID_ARG;
     a.q = q, a.k = k, a.v = v, a.gate = gate, a.bias = bias, a.mask = mask, a.out = out, a.lse = lse;
     return evo::launch_cross_fwd(a, p, ws, (hipStream_t)stream) == hipSuccess ? EVO_OK : EVO_ERR_HIP;
 }
@@ -246,22 +260,18 @@ int evo_cross_bwd(const evo_cross_dims *d, const void *q, const void *k, const v
     for (const void *x : wide)
         if (!aligned(x, 16)) return EVO_ERR_ALIGNMENT;
     if (!aligned(bias, es) || !aligned(dbias, es) || !aligned(lse, 4)) return EVO_ERR_ALIGNMENT;
-    // outputs apart from every input and from each other; views of one packed buffer may interleave
     const auto qr = [&](const void *x) { return view(a, x, a.Lq, a.H, a.q_row, a.q_tok); };
     const auto kr = [&](const void *x) { return view(a, x, a.Lk, a.Hk, a.k_row, a.k_tok); };
     const auto orr = [&](const void *x) { return view(a, x, a.Lq, a.H, a.o_row, a.o_tok); };
-    const int64_t nb = a.N / a.rpb * a.H * a.Lq * (int64_t)a.Lk * (int64_t)es;
-    const evo::View outs[5] = {qr(dq), qr(dgate), kr(dk), kr(dv), flat(dbias, nb)};
-    const evo::View ins[7] = {qr(q), qr(gate), kr(k), kr(v), orr(out), orr(dout), flat(bias, nb)};
-    for (int i = 0; i < 5; ++i) {
-        for (const evo::View &r : ins)
-            if (!apart(outs[i], r)) return EVO_ERR_INVALID_ARG;
-        for (int j = 0; j < i; ++j)
-            if (!apart(outs[i], outs[j])) return EVO_ERR_INVALID_ARG;
-    }
+    const int64_t nb = bias_bytes(a, bias);
     const evo::CrPlan p = evo::cross_plan(a, gate != nullptr, bias != nullptr);
+    const evo::View outs[6] = {qr(dq), qr(dgate), kr(dk), kr(dv), flat(dbias, nb), flat(ws, (int64_t)p.bwd_total)};
+    const evo::View ins[9] = {qr(q), qr(gate), kr(k), kr(v), orr(out), orr(dout), flat(bias, nb), flat(lse, a.N * a.H * a.Lq * 4),
+                              flat(mask, a.N * a.Lk)};
+    if (!all_apart(outs, 0, 5, ins, 9)) return EVO_ERR_INVALID_ARG;
     if (p.bwd_total > 0 && (!ws || ws_bytes < p.bwd_total)) return EVO_ERR_WORKSPACE;
     if (p.bwd_total > 0 && !aligned(ws, 256)) return EVO_ERR_ALIGNMENT;
+    if (!all_apart(outs, 5, 6, ins, 9)) return EVO_ERR_INVALID_ARG;
     a.q = q, a.k = k, a.v = v, a.gate = gate, a.bias = bias, a.mask = mask, a.out = (void *)out, a.lse = (float *)lse;
     a.dout = dout, a.dq = dq, a.dk = dk, a.dv = dv, a.dgate = dgate, a.dbias = dbias;
     return evo::launch_cross_bwd(a, p, ws, (hipStream_t)stream) == hipSuccess ? EVO_OK : EVO_ERR_HIP;

@@ -52,3 +52,21 @@ def test_output_beside_the_queries():
     d = dict(len_q=10, len_k=3000, k_stride_row=384000, q_stride_row=10240, q_stride_tok=1024, o_stride_row=10240, o_stride_tok=1024)
     for shift, status in ((1024, 4), (1008, 1), (0, 1), (512, 1)):
         assert _fwd(_dims(**d), out=A(1) + shift, gate=None, ws=None) == status
+
+
+def test_outputs_on_masks_statistics_and_workspaces():
+    """Everything a call writes is apart from everything it reads or writes besides."""
+    d = _dims(len_q=1, len_k=3000, q_stride_row=512, k_stride_row=384000, o_stride_row=512, rows_per_bias=1)
+    assert _fwd(d, ws=None) == 4                                              # as it is, a call that lacks a workspace only
+    for kw in (dict(out=FWD["bias"]), dict(out=FWD["mask"]), dict(out=FWD["lse"]), dict(out=FWD["lse"] - 4096 + 16),
+               dict(lse=FWD["q"] + 64), dict(lse=FWD["gate"]), dict(lse=FWD["k"] + 4), dict(lse=FWD["v"]), dict(lse=FWD["bias"]),
+               dict(lse=FWD["mask"] + 11996)):
+        assert _fwd(d, **dict(kw, ws=None)) == 1, kw
+    for name in ("q", "k", "v", "gate", "bias", "mask", "out", "lse"):
+        assert _fwd(d, ws=FWD[name]) == 1 and _fwd(d, ws=FWD[name], ws_bytes=16) == 4, name
+    assert _bwd(d, ws=None) == 4
+    for out in ("dq", "dk", "dv", "dgate", "dbias"):
+        for other in ("lse", "mask"):
+            assert _bwd(d, **{out: BWD[other], "ws": None}) == 1, (out, other)
+    for name in ("q", "k", "v", "gate", "bias", "mask", "out", "lse", "dout", "dq", "dk", "dv", "dgate", "dbias"):
+        assert _bwd(d, ws=BWD[name]) == 1, name
