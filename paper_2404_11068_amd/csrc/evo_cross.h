@@ -270,7 +270,7 @@ __device__ __forceinline__ void kept_range(const uint8_t *mask_row, int Lk, int 
 // and only get longer by them.)
 static __device__ const u32x4 kZeros[1] = {};  // what is not there is copied from here
 __device__ __forceinline__ void copy16(const void *from, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds), "v"(from) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds), "v"(from) : "memory");
 }
 __device__ __forceinline__ void copies_done_and_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
 

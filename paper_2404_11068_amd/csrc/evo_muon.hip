@@ -507,7 +507,7 @@ __device__ __forceinline__ const char *scalar(const char *p) {
 
 // 16 bytes per lane from base + off to LDS at lds + 16 lane.  In asm because the compiler would
 // wait for all copies in flight before every LDS read; nothing but the counter below waits for these.
-// (M0 holds the LDS address)
+// (M0 holds the LDS address; nothing else in these kernels uses it)
 __device__ __forceinline__ void copy_to_lds(const char *base, uint32_t off, uint32_t lds) {
     asm volatile(
         "s_mov_b32 m0, %0\n\t"
@@ -515,7 +515,7 @@ __device__ __forceinline__ void copy_to_lds(const char *base, uint32_t off, uint
         "global_load_lds_dwordx4 %1, %2"
         :
         : "s"(lds), "v"(off), "s"(base)
-        : "memory", "m0");
+        : "memory");
 }
 template <int N>
 __device__ __forceinline__ void wait_copies_and_barrier() {
