@@ -268,6 +268,8 @@ __device__ __forceinline__ void kept_range(const uint8_t *mask_row, int Lk, int 
 // copies are counted by hand: copies_done_and_barrier() before a tile is read.
 // (The compiler does not see them; its own waits on vector memory count in order
 // and only get longer by them.)
+// (M0 holds the LDS address.  It is a reserved register: the compiler keeps nothing in it across statements and
+// does not take it as a clobber; nothing else in these kernels' code uses it.)
 static __device__ const u32x4 kZeros[1] = {};  // what is not there is copied from here
 __device__ __forceinline__ void copy16(const void *from, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds), "v"(from) : "memory");

@@ -57,7 +57,8 @@ int check(const evo_cross_dims *d, bool has_bias, evo::CrArgs *a) {
         const int e = check_stride(st[i], i % 2 == 0 ? N : (i == 3 ? d->len_k : d->len_q), es);
         if (e) return e;
     }
-    // tiles of one unit in any kernel, before splits (which only ever fill up to 512 workgroups)
+    // tiles of one unit in any kernel, before splits: those are made of up to 4096 workgroups, and make at most 4096 more
+    // of them (split), far below the limit
     int64_t tiles = up(M, 128) > up(d->len_k, 128) ? up(M, 128) : up(d->len_k, 128);
     if (tiles < 1) tiles = 1;
     if (N > kGrid / tiles / d->n_kv_heads) return EVO_ERR_UNSUPPORTED;
@@ -155,8 +156,12 @@ CrPlan cross_plan(const CrArgs &a, bool has_gate, bool has_bias) {
         p.fwd_splits = split(units * tiles, key_steps, one, rows_bytes, rate, true);
     }
     // few keys: a workgroup (or, for up to 32 queries, a wave) walks over rows of the batch, where there are
-    // enough.  At 8 heads of 32, 256 queries, 77 keys, gate and bias: 128 rows 22 us (34 by a workgroup a
-    // row), 64 rows 15 (19); 65536 rows of one query to 4 keys, 4 heads of 16: 151 (398)
+    // enough.  A workgroup (a workgroup a row beside it): 256 queries to 77 keys, 8 heads of 32, gate, bias and mask, 16,
+    // 32, 64, 128 rows 10.4 us (9.2), 10.9 (12.4), 15.4 (20.0), 24.7 (34.7), without them 7.5 (6.0), 7.9 (7.3), 9.9 (10.6),
+    // 16.9 (18.6): from 1024 units and tiles on (64 rows here) no form loses.  A wave: one query to 4 keys, 4 heads of
+    // 16, 256, 512, 1024, 2048, 8192 rows 5.7 (5.1), 5.8 (6.5), 6.5 (10.1), 8.9 (17.1), 23.5 (54.2); 8 queries to 60 keys,
+    // 4 heads of 64 with a bias, 256, 512, 1024, 2048, 4096 rows 9.6 (6.7), 10.8 (13.5), 22.9 (23.6), 42.4 (40.7), 78.4 (83).
+    // More than 32 channels have no form of four waves: with 3 blocks of keys and a bias 32 channels take 216 registers.
     if (a.Lk > 0 && a.Lk <= 128) {
         p.brief_one = a.M <= 32 && units >= 4096 && 16 * up(a.Lk, 32) * 32 * d * (a.bf16 ? 2 : 4) <= 128 * 1024;
         p.brief = p.brief_one || (a.bf16 && a.D <= 32 && a.M > 32 && units * tiles >= 1024);

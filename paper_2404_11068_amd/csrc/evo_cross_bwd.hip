@@ -11,7 +11,7 @@
 //          rows that share it
 //
 // The passes are bound like the forward (at 64 channels the matrix units are busy 34 to 38% of
-// the time, the vector units 53 to 55%): 2 x 4096 to 4096, 16 heads of 64, bf16, 502 us for all,
+// the time, the vector units 53 to 55%): 2 x 4096 to 4096, 16 heads of 64, bf16, 525 us for all,
 // 4096 to 8191, 16 heads of 128, 1200 us (800 TFLOP/s of the seven products).  One pass would save two
 // products, and sum dQ over workgroups, by atomics or by partial sums of all of it.
 //
@@ -229,6 +229,8 @@ template <typename T, int DP, bool BIAS> struct RowsShape {
     static constexpr bool WIDE = sizeof(typename Ty<T>::E) == 4;
     static constexpr int KT = WIDE || DP == 128 || BIAS ? 32 : 64, ROWS = 128;
     static constexpr int TILE = KT * DP;
+    // (bf16 at 128 channels with a bias does not fit two waves a SIMD: 53 vector registers are spilled, 104 bytes a lane.  2 x 1024
+    // to 1024, 8 heads: 152 us for the whole backward; one wave a SIMD was not measured)
     static constexpr int WAVES = WIDE && DP == 128 ? 1 : 2;
 };
 

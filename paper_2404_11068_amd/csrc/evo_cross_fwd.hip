@@ -20,11 +20,11 @@
 // integer): rescaling is then exact.  Far from zero, where fp32 has no such numbers, it is
 // kept as two (Ref).
 //
-// Long calls keep the matrix and the vector unit busy 48 and 54% of the time at 128
-// channels: 4096 queries to 8191 keys, 16 heads, bf16, 277 us (990 TFLOP/s); at 64 channels
-// 2 x 4096 to 4096, 16 heads, 167 us (825), at 32 112 us (610).  fp32 runs at 101 to 116 of the
+// Long calls keep the matrix and the vector unit busy 49 and 56% of the time at 128
+// channels: 4096 queries to 8191 keys, 16 heads, bf16, 274 to 282 us (975 to 1000 TFLOP/s); at 64 channels
+// 2 x 4096 to 4096, 16 heads, 173 to 177 us (780 to 800), at 32 114 to 124 us (555 to 600).  fp32 runs at 101 to 116 of the
 // 150 TFLOP/s of a library product.  Single tokens are bound by memory: 16 rows, 16 / 4
-// heads of 128, 4097 keys 20.1 + 4.0 us (4.6 TB/s of the kept keys).
+// heads of 128, 4097 keys 20.6 + 4.0 us (4.6 TB/s of the kept keys).
 #include "evo_cross.h"
 
 namespace evo {

@@ -8,7 +8,7 @@
 // read once, and while a row is worked on, K and V of the next are copied to LDS
 // and its queries and gate to registers.  Before, a workgroup a row: 128 rows of 256
 // queries to 77 keys, 8 heads of 32, gate, bias, mask took 30 us, the bias' loads
-// half of it; now 22 (vector unit 45% busy, waves wait 45% of
+// half of it; now 23 (vector unit 45% busy, waves wait 47% of
 // their time: two workgroups a CU fit the registers).
 //
 // Two shapes: the four waves of a workgroup share a row (32 queries each), or each

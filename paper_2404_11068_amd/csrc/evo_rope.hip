@@ -8,8 +8,8 @@
 // tokens once, in LDS, for all heads: one pair in 2 d / rot * heads elements.
 //
 // Measured: 2 x 8193 tokens of 32 heads of 64 in bf16, rotation alone, 22 us (6.0 TB/s);
-// 128 x 256 of 16 heads of 32 in fp32 with the norm 21.6 us (6.2 TB/s); 4 x 4099 of 20
-// heads of 128, 96 rotated, with the norm 40 us forward (4.2 TB/s), 51 us backward (4.9).
+// 128 x 256 of 16 heads of 32 in fp32 with the norm 22 us (6.1 TB/s); 4 x 4099 of 20
+// heads of 128, 96 rotated, with the norm 40 us forward (4.2 TB/s), 53 us backward (4.8).
 //
 // A head is a group of GS lanes (the power of two that holds d / VEC chunks of
 // 16 bytes); groups walk over the (token, head) units of a workgroup's tokens.

@@ -63,8 +63,10 @@ def rope_frequencies(rot_dim: int, base: float = 10000.0, *, factor: float = 1.0
     "linear": all frequencies divided by factor (positions interpolated).
     "base": a base larger by factor^(rot_dim / (rot_dim - 2)): the last pair is divided by factor, the first kept.
     "turns": pairs that make `fast` turns or more over trained_length keep their frequency, those that make
-        `slow` or fewer have it divided, between them the share kept runs along the logarithm of the turns;
-        rope_amplitude(factor) goes with it.
+        `slow` or fewer have it divided, between them the share kept runs along the logarithm of the turns,
+        which is along the pair's index, with bounds between whole pairs; rope_amplitude(factor) goes with it.
+        A checkpoint of another ramp (linear in the turns, bounds rounded to whole pairs) has frequencies of
+        its own, some of them by a third apart: give rope_steps that list.
     """
     if rot_dim < 0 or rot_dim % 2 or not base > 0 or not factor > 0:
         raise ValueError("rot_dim must be even and not negative, base and factor positive")
@@ -91,8 +93,8 @@ def rope_amplitude(factor: float) -> float:
 
 def rope_steps(frequencies, device="cuda") -> torch.Tensor:
     """int64 [rot / 2]: each frequency (radians per position: a list, or a float tensor, which is read on the
-    host) as turns per position times 2^64, modulo whole turns.  Laid out once; off by at most half of 2^-64
-    turns, that is 2^-34 turns at position 2^31."""
+    host) as turns per position times 2^64, modulo whole turns.  Laid out once (0.2 to 0.5 ms for 64 pairs on the
+    host; not within a capture); off by at most half of 2^-64 turns, that is 2^-34 turns at position 2^31."""
     if isinstance(frequencies, torch.Tensor):
         device = frequencies.device
         frequencies = frequencies.double().tolist()
