@@ -24,7 +24,7 @@ struct CrArgs {
     // backward
     const void *dout;
     void *da;        // sigmoid(gate) * dout, contiguous [N, Lq, H, d] (with a gate or a bias)
-    f32x4 *stats;    // [N, Hk, M]: what a query's probabilities are formed with, and D
+    f32x4 *stats;    // [N, Hk, M]: (base, D, rest) of a query, base and rest: what its probabilities are formed with
     void *dq, *dk, *dv, *dgate, *dbias;
     // partial sums over splits
     float *part;     // [splits][rows][d]

@@ -5,7 +5,7 @@
 //
 // P is formed again from the saved log-sum-exp, in each of three passes:
 //   rows:  a wave owns 32 queries (lane = query) and walks the keys: dQ; before that
-//          it forms D, dgate and dA of its queries, and leaves them for the others (stats, da)
+//          it forms D, dgate and dA of its queries, and leaves them for the others
 //   keys:  a wave owns 32 keys (lane = key) and walks the queries: dK, dV
 //   bias:  a workgroup owns 64 x 64 entries of one bias plane and walks the
 //          rows that share it
@@ -47,6 +47,8 @@ template <typename T, int DP> struct KeysShape {
     static constexpr bool WIDE = sizeof(typename Ty<T>::E) == 4;
     static constexpr int KEYS = 128, XT = WIDE || DP == 128 ? 32 : 64;
     static constexpr int TILE = XT * DP;
+    // (bf16 at 64 channels with a bias spills 2 registers around its loop; addresses in scalar registers avoid it and take 44.9 us
+    // where this takes 43.4, 2 x 1024 to 1024, 8 heads)
     static constexpr int WAVES = DP == 128 ? 1 : 2;  // per SIMD: the accumulators of 128 channels take half of its registers
 };
 
@@ -88,7 +90,6 @@ __global__ __launch_bounds__(kThreads, (KeysShape<T, DP>::WAVES)) void cross_key
 
     constexpr int NB = S::XT / 32, GP = 32 / Y::KS;
     using Cp = Copy<T, DP, S::XT, kThreads>;
-    const f32x4 *sbase = a.stats + (int64_t)unit * a.M;
     float2 stats_in = {};
     float rest_in = 0.0f;
     auto request = [&](int step) {
@@ -97,7 +98,7 @@ __global__ __launch_bounds__(kThreads, (KeysShape<T, DP>::WAVES)) void cross_key
             const int x = x0 + r, t = token_of(a, x);
             return (int64_t)t * tok + (int64_t)(x - t * a.G) * a.D;
         };
-        const float *from = (const float *)(sbase + (uint32_t)min(x0 + lane % S::XT, a.M - 1));
+        const float *from = (const float *)(a.stats + (int64_t)unit * a.M + min(x0 + lane % S::XT, a.M - 1));
         if (tid < S::XT) stats_in = *reinterpret_cast<const float2 *>(from);
         if (!BIAS) rest_in = from[2];  // (all waves look whether there is one)
         const bool whole = a.D == DP && x0 + S::XT <= a.M;
@@ -229,8 +230,8 @@ template <typename T, int DP, bool BIAS> struct RowsShape {
     static constexpr bool WIDE = sizeof(typename Ty<T>::E) == 4;
     static constexpr int KT = WIDE || DP == 128 || BIAS ? 32 : 64, ROWS = 128;
     static constexpr int TILE = KT * DP;
-    // (bf16 at 128 channels with a bias does not fit two waves a SIMD: 53 vector registers are spilled, 104 bytes a lane.  2 x 1024
-    // to 1024, 8 heads: 152 us for the whole backward; one wave a SIMD was not measured)
+    // (bf16 at 128 channels with a bias does not fit two waves a SIMD: 29 vector registers are spilled, 104 bytes a lane.  2 x 1024
+    // to 1024, 8 heads: 150 us for the whole backward; one wave a SIMD was not measured)
     static constexpr int WAVES = WIDE && DP == 128 ? 1 : 2;
 };
 
@@ -276,10 +277,48 @@ __global__ __launch_bounds__(kThreads, (RowsShape<T, DP, BIAS>::WAVES)) void cro
     const E *vbase = (const E *)a.v + n * a.k_row + (int64_t)hk * a.D;
     const uint8_t *mrow = a.mask ? a.mask + n * a.Lk : nullptr;
 
+    // the first tiles are on their way while D, dgate and dA are formed: 2 x 1024 to 1024, 8 heads of 64 with a bias 27.4 -> 24.8 us;
+    // at 128 channels, where registers are short, 45.4 -> 47.4: there they come after
+    using Bits = KeyBits<S::KT>;
+    constexpr int NB = S::KT / 32, GP = 32 / Y::KS;
+    Bits now, next;
+    const bool full_d = a.D == DP;
+    auto request = [&](int step, bool whole, auto keep) {
+        const int64_t off = (int64_t)step * S::KT * a.k_tok;
+        const auto k_row = [&](int r) { return kbase + off + (int64_t)r * a.k_tok; };
+        const auto v_row = [&](int r) { return vbase + off + (int64_t)r * a.k_tok; };
+        E *kt = tiles[step & 1][0], *vt = tiles[step & 1][1];
+        if constexpr (S::KT * LT::CH % kThreads == 0) {
+            Copy<T, DP, S::KT, kThreads>::run(kt, whole, a.D, wave, lane, k_row, keep);
+            Copy<T, DP, S::KT, kThreads>::run(vt, whole, a.D, wave, lane, v_row, keep);
+        } else if (wave < 2) {  // a tile takes half of the workgroup
+            Copy<T, DP, S::KT, kThreads / 2>::run(kt, whole, a.D, wave, lane, k_row, keep);
+        } else {
+            Copy<T, DP, S::KT, kThreads / 2>::run(vt, whole, a.D, wave - 2, lane, v_row, keep);
+        }
+    };
+    typename BiasRow<T>::Raw braw[BIAS ? NB : 1];
+    auto request_bias = [&](int step) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+            if (BIAS) braw[BIAS ? b : 0] = brow.request(step * S::KT + 32 * b, h);
+    };
+    typename Bits::Bytes bytes = {};
+    const int t0 = split * a.per_split, t1 = min(t0 + a.per_split, a.ntiles);
+    const auto first_tiles = [&] {
+        if (t0 >= t1) return;
+        const auto first = Bits::request(mrow, t0 * S::KT, a.Lk, lane);
+        bytes = Bits::request(mrow, (t0 + 1) * S::KT, a.Lk, lane);
+        next.set(first);
+        request_bias(t0);
+        request(t0, full_d && next.all(), [&](int r) { return next.get(r); });
+    };
+    if (DP <= 64) first_tiles();
+
     const bool live = on && lse != -inf, far = live && fabsf(lse) > kFarLse && fabsf(lse) < inf;
     const bool any_far = __any(far);
     float base = BIAS ? (live ? lse : inf) : (live ? -lse * kLog2e : -inf), rest = 0.0f, times = 1.0f;
-    if (any_far) {
+    if (__builtin_expect(any_far, 0)) {
         // rows of K straight from memory, one a lane: rare, and without barriers that the other waves would have to meet
         const float unit2 = BIAS ? kLog2e : to2;
         float top = -inf, sum = 0.0f;
@@ -355,39 +394,7 @@ __global__ __launch_bounds__(kThreads, (RowsShape<T, DP, BIAS>::WAVES)) void cro
 #pragma unroll
     for (int i = 0; i < DT; ++i) dq[i] = zero16();
 
-    using Bits = KeyBits<S::KT>;
-    constexpr int NB = S::KT / 32, GP = 32 / Y::KS;
-    Bits now, next;
-    const bool full_d = a.D == DP;
-    auto request = [&](int step, bool whole, auto keep) {
-        const int64_t off = (int64_t)step * S::KT * a.k_tok;
-        const auto k_row = [&](int r) { return kbase + off + (int64_t)r * a.k_tok; };
-        const auto v_row = [&](int r) { return vbase + off + (int64_t)r * a.k_tok; };
-        E *kt = tiles[step & 1][0], *vt = tiles[step & 1][1];
-        if constexpr (S::KT * LT::CH % kThreads == 0) {
-            Copy<T, DP, S::KT, kThreads>::run(kt, whole, a.D, wave, lane, k_row, keep);
-            Copy<T, DP, S::KT, kThreads>::run(vt, whole, a.D, wave, lane, v_row, keep);
-        } else if (wave < 2) {  // a tile takes half of the workgroup
-            Copy<T, DP, S::KT, kThreads / 2>::run(kt, whole, a.D, wave, lane, k_row, keep);
-        } else {
-            Copy<T, DP, S::KT, kThreads / 2>::run(vt, whole, a.D, wave - 2, lane, v_row, keep);
-        }
-    };
-    typename BiasRow<T>::Raw braw[BIAS ? NB : 1];
-    auto request_bias = [&](int step) {
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-            if (BIAS) braw[BIAS ? b : 0] = brow.request(step * S::KT + 32 * b, h);
-    };
-    typename Bits::Bytes bytes = {};
-    const int t0 = split * a.per_split, t1 = min(t0 + a.per_split, a.ntiles);
-    if (t0 < t1) {
-        const auto first = Bits::request(mrow, t0 * S::KT, a.Lk, lane);
-        bytes = Bits::request(mrow, (t0 + 1) * S::KT, a.Lk, lane);
-        next.set(first);
-        request_bias(t0);
-        request(t0, full_d && next.all(), [&](int r) { return next.get(r); });
-    }
+    if (DP > 64) first_tiles();
     for (int step = t0; step < t1; ++step) {
         const E *kt = tiles[step & 1][0], *vt = tiles[step & 1][1];
         copies_done_and_barrier();
