@@ -15,7 +15,8 @@
  *   its dK and dV are zeros.
  * - A query with nothing left to attend to gets o = 0, lse = -inf and zero
  *   gradients: all keys masked, Lk == 0, or no logit above -1e30 (a bias of
- *   -inf or of the type's lowest value at every key is a mask).
+ *   -inf or of the type's lowest value at every key is a mask; K and V of keys that
+ *   only a bias masks are read, and have to be finite).
  * - Logits are fp32 numbers, and softmax and gradients those of these numbers however far
  *   from zero they lie (at -1e9 a step is 64: equal biases there make keys equally
  *   likely, whatever q k' is).

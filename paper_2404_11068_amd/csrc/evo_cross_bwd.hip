@@ -10,8 +10,8 @@
 //   bias:  a workgroup owns 64 x 64 entries of one bias plane and walks the
 //          rows that share it
 //
-// The passes are bound like the forward (at 64 channels the matrix units are busy 34 to 38% of
-// the time, the vector units 53 to 55%): 2 x 4096 to 4096, 16 heads of 64, bf16, 525 us for all,
+// The passes are bound like the forward (at 64 channels the matrix units are busy 33 to 37% of
+// the time, the vector units 52 to 53%): 2 x 4096 to 4096, 16 heads of 64, bf16, 525 us for all,
 // 4096 to 8191, 16 heads of 128, 1200 us (800 TFLOP/s of the seven products).  One pass would save two
 // products, and sum dQ over workgroups, by atomics or by partial sums of all of it.
 //

@@ -85,3 +85,33 @@ def test_gradients_at_far_products(N, Lq, Lk, H, d, size, dtype):
     b[1][..., 0] = abs(far) * b[1][..., -1]
     for name, got, r, bound in zip(("dq", "dk", "dv"), grads, want, b):
         _close(got, r, bound, u, name)
+
+
+@DTYPES
+@pytest.mark.parametrize("gate", [False, True], ids=["plain", "gate"])
+@pytest.mark.parametrize("N,Lq,Lk,H,Hk,d", [(3, 45, 70, 6, 2, 40), (1, 20, 2100, 2, 1, 104)], ids=["rows", "split"])
+def test_strided_tensors_far_and_near(N, Lq, Lk, H, Hk, d, gate, dtype):
+    """Views of packed buffers, tokens outermost, with a bias that puts every third query far off: the bits of tensors of
+    their own, a workspace of just the size asked for (nothing behind it is touched), and gradients in packed buffers."""
+    q, k, v, g, bias, _, dout = _draw((N, Lq, Lk, H, Hk, d, gate, 1, None), dtype, 34)
+    bias[:, :, ::3] = -1e9
+    out, lse = cross.cross_attn_fwd(q, k, v, g, bias)
+    want = cross.cross_attn_bwd(q, k, v, g, bias, None, out, lse, dout)
+    qg = torch.zeros(Lq, N, 2 * H, d, dtype=dtype, device="cuda").transpose(0, 1)
+    kv = torch.zeros(Lk, N, 2 * Hk, d, dtype=dtype, device="cuda").transpose(0, 1)
+    od = torch.zeros(Lq, N, 3 * H, d, dtype=dtype, device="cuda").transpose(0, 1)
+    qv, gv, kv_, vv, ov, dv_ = qg[:, :, :H], qg[:, :, H:], kv[:, :, :Hk], kv[:, :, Hk:], od[:, :, :H], od[:, :, 2 * H:]
+    for to, x in ((qv, q), (kv_, k), (vv, v), (dv_, dout)) + (((gv, g),) if gate else ()):
+        to.copy_(x)
+    o2, l2 = cross.cross_attn_fwd(qv, kv_, vv, gv if gate else None, bias, out=ov)
+    assert torch.equal(o2, out) and torch.equal(l2, lse)
+    need = cross.cross_attn_bwd_workspace_size(q, k, gate, True)
+    room = torch.full((need + 4096,), 171, dtype=torch.uint8, device="cuda")
+    dqg, dkv = torch.full_like(qg, 7.0), torch.full_like(kv, 7.0)
+    kw = dict(dgate=dqg[:, :, H:]) if gate else {}
+    got = cross.cross_attn_bwd(qv, kv_, vv, gv if gate else None, bias, None, ov, lse, dv_, dq=dqg[:, :, :H], dk=dkv[:, :, :Hk],
+                               dv=dkv[:, :, Hk:], workspace=room[:need], **kw)
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert a is None or torch.equal(a, b)
+    assert (room[need:] == 171).all() and (gate or (dqg[:, :, H:] == 7.0).all())
